@@ -571,6 +571,147 @@ int alr_gemm(int32_t dtype, int32_t a_mn, int32_t b_mn, int32_t accumulate, cons
  */
 int alr_gemm_form(int32_t dtype, int32_t M, int32_t Nc, int32_t K, int32_t* form, int32_t* split);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators on logits in hand, and the embedding of a block's tokens: what surrounds the slot
+ * loss in a training program.  The paper's trainer has them from its framework: the target's
+ * rollout draws tokens and stores labels (App. A), the drafter embeds a block's anchor and mask
+ * tokens.
+ *   alr_embed -> (model) -> logits -> alr_sample_tokens / alr_top_logits
+ *             -> alr_distill_fwd_bwd -> (model's backward) -> alr_embed_grad
+ *
+ * Logits Z: N rows of V elements (ALR_BF16 or ALR_F32), consecutive rows ldz >= V elements apart
+ * (any ldz; the base 16-byte aligned, rows need not be).  V <= ALR_LOGITS_MAX_V.  N = 0 is allowed
+ * everywhere.  None of these calls needs a workspace but alr_embed_grad.
+ * ------------------------------------------------------------------------------------- */
+#define ALR_LOGITS_MAX_V 262144
+#define ALR_TOP_MAX 256
+
+/*
+ * The K largest logits of each row, the label that alr_distill_* reads (1 <= K <= ALR_TOP_MAX).
+ *   top_val [N, K] float, top_idx [N, K] int32: by value descending, equal values by token id
+ *            ascending.  A logit of -inf (a masked token) or NaN is never listed: a row with fewer
+ *            than K others ends in entries (-inf, -1).
+ *   lse, lse_rest [N] (nullable): log-sum-exp of z / temperature over the whole row and over the
+ *            tokens that are not listed (-inf for none).
+ * A row that holds +inf gives unspecified log-sum-exps.
+ */
+int alr_top_logits(const void* Z, int32_t dtype, int64_t N, int32_t V, int64_t ldz, int32_t K,
+                   float temperature, float* top_val, int32_t* top_idx, float* lse,
+                   float* lse_rest, void* stream);
+
+/* Problem description of alr_distill_*. */
+typedef struct {
+    int64_t N;          /* rows, N >= 0                                                       */
+    int64_t ldz;        /* row stride of Z in elements, >= V                                  */
+    int64_t ldg;        /* row stride of G in elements, >= V (ignored by the forward alone)   */
+    int32_t V;          /* vocabulary, 1 <= V <= ALR_LOGITS_MAX_V                             */
+    int32_t K;          /* list length, 1 <= K <= ALR_TOP_MAX                                 */
+    int32_t dtype;      /* of Z and G: ALR_BF16 or ALR_F32                                    */
+    float temperature;  /* > 0, finite: divides both sides' logits                            */
+    float lambda;       /* loss scale (a usual choice is temperature^2)                       */
+} alr_distill_params;
+
+/* Outputs of the distillation forward, device pointers, length N unless stated. */
+typedef struct {
+    float* loss_row;    /* l_r (required)                                                     */
+    float* ent_row;     /* entropy of the label: l - ent is the KL divergence (nullable)      */
+    float* lse;         /* log-sum-exp of z / temperature (required: the backward reads it)   */
+    float* lse_rest;    /* the same over the tokens not listed (required when rest is given)  */
+    int32_t* argmax;    /* greedy token, lowest id on ties, -1 for a row of -inf (nullable)   */
+    float* loss_total;  /* [1] L = lambda * sum w l / sum w, 0 when sum w = 0                 */
+    float* weight_sum;  /* [1] sum w                                                          */
+    float* wl_sum;      /* [1] sum w l (nullable; see alr_loss_from_sums)                     */
+} alr_distill_outputs;
+
+/*
+ * Distillation loss of student logits against a teacher's top logits, in the form of the compact
+ * labels above (Sec. 3.1 under Eq. 1) for logits in hand, any list length and any temperature.
+ *   top_val, top_idx [N, K]: the teacher's logits and their tokens (alr_top_logits writes them; the
+ *            readout's log-probabilities do as well).  An entry whose token lies outside [0, V)
+ *            is absent.  The tokens of a row are distinct.
+ *   rest [N] or NULL: log-sum-exp of the teacher's logits / temperature over the tokens that are
+ *            not listed (lse_rest of alr_top_logits).  The label is the softmax of
+ *            (top_val / temperature, rest), its last entry one bin for all other tokens; without
+ *            rest it is the softmax of the list alone.
+ *   weight [N] or NULL (ones): w_r.  Rows of weight 0 are not read: their loss, entropy and
+ *            log-sum-exps are 0, argmax -1, gradient 0.
+ *   l_r = -sum_i p_i log q(top_idx_i) - p_0 log q_0, q = softmax(z / temperature), q_0 the mass of
+ *            the tokens not listed.  A row without a label (every entry absent, rest -inf), or whose
+ *            logits are all -inf, has loss 0 and gradient 0 and still counts in sum w.
+ * The loss is +inf where the student gives no mass to a token of the label.
+ */
+int alr_distill_fwd(const alr_distill_params* p, const void* Z, const float* top_val,
+                    const int32_t* top_idx, const float* rest, const float* weight,
+                    const alr_distill_outputs* out, void* stream);
+
+/*
+ * Gradient of L with respect to Z, written to G [N, V] (row stride ldg; may be Z itself when
+ * ldg = ldz, else it does not overlap Z):
+ *   G[r, v] = lambda w_r / (temperature sum w) * (q_v - p_v)             for a listed v,
+ *             lambda w_r / (temperature sum w) * q_v (1 - p_0 / q_0)     otherwise.
+ *   lse, lse_rest [N]: of the forward (lse_rest NULL when rest is NULL); weight_sum [1]: sum w of
+ *   the batch (the forward's, or the sum over the shards of a row-sharded batch).
+ */
+int alr_distill_bwd(const alr_distill_params* p, const void* Z, const float* top_val,
+                    const int32_t* top_idx, const float* rest, const float* weight,
+                    const float* lse, const float* lse_rest, const float* weight_sum, void* G,
+                    void* stream);
+
+/*
+ * Both in one pass over the logits: sum w does not depend on them, so the gradient needs no second
+ * call.  batch_weight_sum [1] or NULL: the normaliser of a row-sharded batch (default: this call's
+ * own sum w).  Outputs and G as in the two calls.
+ */
+int alr_distill_fwd_bwd(const alr_distill_params* p, const void* Z, const float* top_val,
+                        const int32_t* top_idx, const float* rest, const float* weight,
+                        const float* batch_weight_sum, const alr_distill_outputs* out, void* G,
+                        void* stream);
+
+/*
+ * One token per row, drawn from given random numbers (as the draws of alr_ira_draw).
+ *   u [N] uint32: independent uniform random integers.
+ *   temperature [N] float or NULL (1): <= 0 takes the greedy token.
+ *   top_k [N] int32 or NULL: keep the k first tokens in the order (value descending, id ascending);
+ *            <= 0 keeps all.
+ *   top_p [N] float or NULL: then, in that order, the tokens before which less than top_p of the
+ *            kept mass lies (one at least); >= 1 keeps all.
+ *   min_p [N] float or NULL: then the tokens of at least min_p (at most 1) times the largest
+ *            probability.
+ * A token's weight is the whole number floor(2^31 exp2((z - max) log2(e) / temperature)), each step
+ * rounded to fp32; tokens of weight 0 (below 2^-31 of the largest) are never kept.  Sums of weights
+ * are exact, so a draw depends on nothing but its inputs.  With S the weight of the kept tokens:
+ *   token [N] int32: the lowest id at which the running sum of the kept weights, in the order of
+ *            ids, exceeds floor(u S / 2^32); -1 for a row without a candidate;
+ *   prob [N] float (nullable): the token's weight / S (0 for token -1);
+ *   n_kept [N] int32 (nullable): the number of tokens kept.
+ * Logits of -inf (masked tokens) and NaN are no candidates; +inf has all the mass.
+ */
+int alr_sample_tokens(const void* Z, int32_t dtype, int64_t N, int32_t V, int64_t ldz,
+                      const uint32_t* u, const float* temperature, const int32_t* top_k,
+                      const float* top_p, const float* min_p, int32_t* token, float* prob,
+                      int32_t* n_kept, void* stream);
+
+/*
+ * out[i] = scale * E[tokens[i]] for the table E [V, d]: out [N, d] of the same type, the product
+ * taken in fp32 and rounded once.  A token outside [0, V) (padding) gives a row of zeros.
+ */
+int alr_embed(const void* E, int32_t dtype, int32_t V, int32_t d, const int32_t* tokens, int64_t N,
+              float scale, void* out, void* stream);
+
+/* Workspace bytes alr_embed_grad needs (0 on invalid sizes). */
+size_t alr_embed_grad_workspace_size(int32_t V, int32_t d, int64_t N);
+
+/*
+ * Gradient of the table: dE[v] = scale * sum over {i : tokens[i] = v} of dY[i], for dY [N, d] of
+ * `dtype` and dE [V, d] float, the sums in fp32 and in an order that depends on the tokens alone
+ * (bit for bit the same in every call).  accumulate == 0 overwrites dE, zeros for tokens that do
+ * not occur; else the sums are added to it and other rows are not touched.  Tokens outside [0, V)
+ * contribute nothing.  N <= 2^24.
+ */
+int alr_embed_grad(const void* dY, int32_t dtype, int32_t V, int32_t d, const int32_t* tokens,
+                   int64_t N, float scale, int32_t accumulate, float* dE, void* workspace,
+                   size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -48,6 +48,20 @@ class AlrTopkFwdOutputs(ctypes.Structure):
     _fields_ = [(f, _c_p) for f in _TOPK_FIELDS]
 
 
+class AlrDistillParams(ctypes.Structure):
+    _fields_ = [("N", _c_i64), ("ldz", _c_i64), ("ldg", _c_i64), ("V", _c_i32), ("K", _c_i32),
+                ("dtype", _c_i32), ("temperature", _c_f), ("lam", _c_f)]
+
+
+_DISTILL_FIELDS = ("loss_row", "ent_row", "lse", "lse_rest", "argmax", "loss_total", "weight_sum",
+                   "wl_sum")
+ALR_TOP_MAX, ALR_LOGITS_MAX_V = 256, 262144
+
+
+class AlrDistillOutputs(ctypes.Structure):
+    _fields_ = [(f, _c_p) for f in _DISTILL_FIELDS]
+
+
 # name -> (restype, argtypes); must match include/alr.h
 SIGNATURES = {
     "alr_version": (ctypes.c_char_p, []),
@@ -111,6 +125,20 @@ SIGNATURES = {
                                    _c_p]),
     "alr_gemm": (_c_int, [_c_i32, _c_i32, _c_i32, _c_i32, _c_p, _c_p, _c_p, _c_i32, _c_i32,
                           _c_i32, _c_p]),
+    "alr_top_logits": (_c_int, [_c_p, _c_i32, _c_i64, _c_i32, _c_i64, _c_i32, _c_f, _c_p, _c_p,
+                                _c_p, _c_p, _c_p]),
+    "alr_distill_fwd": (_c_int, [ctypes.POINTER(AlrDistillParams), _c_p, _c_p, _c_p, _c_p, _c_p,
+                                 ctypes.POINTER(AlrDistillOutputs), _c_p]),
+    "alr_distill_bwd": (_c_int, [ctypes.POINTER(AlrDistillParams), _c_p, _c_p, _c_p, _c_p, _c_p,
+                                 _c_p, _c_p, _c_p, _c_p, _c_p]),
+    "alr_distill_fwd_bwd": (_c_int, [ctypes.POINTER(AlrDistillParams), _c_p, _c_p, _c_p, _c_p,
+                                     _c_p, _c_p, ctypes.POINTER(AlrDistillOutputs), _c_p, _c_p]),
+    "alr_sample_tokens": (_c_int, [_c_p, _c_i32, _c_i64, _c_i32, _c_i64, _c_p, _c_p, _c_p, _c_p,
+                                   _c_p, _c_p, _c_p, _c_p, _c_p]),
+    "alr_embed": (_c_int, [_c_p, _c_i32, _c_i32, _c_i32, _c_p, _c_i64, _c_f, _c_p, _c_p]),
+    "alr_embed_grad_workspace_size": (_c_sz, [_c_i32, _c_i32, _c_i64]),
+    "alr_embed_grad": (_c_int, [_c_p, _c_i32, _c_i32, _c_i32, _c_p, _c_i64, _c_f, _c_i32, _c_p,
+                                _c_p, _c_sz, _c_p]),
     "alr_gemm_form": (_c_int, [_c_i32, _c_i32, _c_i32, _c_i32, _c_p, _c_p]),
 }
 
@@ -622,6 +650,124 @@ def alr_gemm(A, B, C, M, Nc, K, a_mn=False, b_mn=False, accumulate=False, stream
     _check(lib().alr_gemm(dtype_code(dt), int(a_mn), int(b_mn), int(accumulate),
                           _ptr(A, "A", M * K, dt), _ptr(B, "B", Nc * K, dt),
                           _ptr(C, "C", M * Nc, _F32), M, Nc, K, _stream(stream)))
+
+
+# ------------------------------------- operators on logits in hand, embedding ---
+def _matrix(t, name):
+    """(pointer, rows, columns, row stride) of a matrix whose rows are contiguous and any stride
+    apart, on the current CUDA device."""
+    if not isinstance(t, _Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if not t.is_cuda or t.get_device() != _cuda_device():
+        raise ValueError(f"{name} must be on the current CUDA device (got {t.device})")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix (got {t.dim()} dimensions)")
+    n, m = t.shape
+    row, col = t.stride()
+    if (col != 1 and m > 1) or (row < m and n > 1):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap "
+                         f"(got strides {row}, {col})")
+    return t.data_ptr(), n, m, (row if n > 1 else m)
+
+
+def alr_top_logits(Z, K, out: dict, temperature=1.0, stream=None):
+    """Z [N, V] (rows any stride apart); out: top_val [N, K], top_idx [N, K] int32; optional lse,
+    lse_rest [N]."""
+    z, N, V, ld = _matrix(Z, "Z")
+    _check(lib().alr_top_logits(z, dtype_code(Z.dtype), N, V, ld, K, float(temperature),
+                                _ptr(out["top_val"], "top_val", N * K, _F32),
+                                _ptr(out["top_idx"], "top_idx", N * K, _I32),
+                                _ptr(out.get("lse"), "lse", N, _F32),
+                                _ptr(out.get("lse_rest"), "lse_rest", N, _F32), _stream(stream)))
+
+
+def _distill(Z, top_val, top_idx, rest, weight, temperature, lam, G=None):
+    """(params, Z, top_val, top_idx, rest, weight, G) for the C call."""
+    z, N, V, ldz = _matrix(Z, "Z")
+    g, ldg = None, V
+    if G is not None:
+        g, gn, gv, ldg = _matrix(G, "G")
+        if (gn, gv) != (N, V) or G.dtype != Z.dtype:
+            raise ValueError(f"G must be [{N}, {V}] of {Z.dtype} (got {list(G.shape)}, {G.dtype})")
+    if top_val.dim() != 2 or top_val.shape[0] != N:
+        raise ValueError(f"top_val must be [{N}, K] (got {list(top_val.shape)})")
+    K = top_val.shape[1]
+    p = AlrDistillParams(N=N, ldz=ldz, ldg=ldg, V=V, K=K, dtype=dtype_code(Z.dtype),
+                         temperature=float(temperature), lam=float(lam))
+    return (p, z, _ptr(top_val, "top_val", N * K, _F32), _ptr(top_idx, "top_idx", N * K, _I32),
+            _ptr(rest, "rest", N, _F32), _ptr(weight, "weight", N, _F32), g)
+
+
+def _distill_outputs(N, out):
+    spec = {f: (1 if f in ("loss_total", "weight_sum", "wl_sum") else N,
+                _I32 if f == "argmax" else _F32) for f in _DISTILL_FIELDS}
+    return AlrDistillOutputs(*[_ptr(out.get(f), f, *spec[f]) for f in _DISTILL_FIELDS])
+
+
+def alr_distill_fwd(Z, top_val, top_idx, out: dict, rest=None, weight=None, temperature=1.0,
+                    lam=1.0, stream=None):
+    """Z [N, V] student logits, top_val / top_idx [N, K] the teacher's; out: loss_row, lse [N],
+    loss_total, weight_sum [1] (and lse_rest [N] with rest); optional ent_row, argmax [N], wl_sum."""
+    p, *args, _ = _distill(Z, top_val, top_idx, rest, weight, temperature, lam)
+    o = _distill_outputs(p.N, out)
+    _check(lib().alr_distill_fwd(ctypes.byref(p), *args, ctypes.byref(o), _stream(stream)))
+
+
+def alr_distill_bwd(Z, top_val, top_idx, lse, lse_rest, weight_sum, G, rest=None, weight=None,
+                    temperature=1.0, lam=1.0, stream=None):
+    """G [N, V] of Z's type (may be Z) from a forward's lse, lse_rest (None without rest) and
+    weight_sum."""
+    p, *args, g = _distill(Z, top_val, top_idx, rest, weight, temperature, lam, G)
+    _check(lib().alr_distill_bwd(ctypes.byref(p), *args, _ptr(lse, "lse", p.N, _F32),
+                                 _ptr(lse_rest, "lse_rest", p.N, _F32),
+                                 _ptr(weight_sum, "weight_sum", 1, _F32), g, _stream(stream)))
+
+
+def alr_distill_fwd_bwd(Z, top_val, top_idx, out: dict, G, rest=None, weight=None,
+                        batch_weight_sum=None, temperature=1.0, lam=1.0, stream=None):
+    """alr_distill_fwd and alr_distill_bwd in one pass over the logits."""
+    p, *args, g = _distill(Z, top_val, top_idx, rest, weight, temperature, lam, G)
+    o = _distill_outputs(p.N, out)
+    _check(lib().alr_distill_fwd_bwd(ctypes.byref(p), *args,
+                                     _ptr(batch_weight_sum, "batch_weight_sum", 1, _F32),
+                                     ctypes.byref(o), g, _stream(stream)))
+
+
+def alr_sample_tokens(Z, u, out: dict, temperature=None, top_k=None, top_p=None, min_p=None,
+                      stream=None):
+    """Z [N, V]; u [N] random integers (an int32 tensor holding the uint32 bits); temperature,
+    top_p, min_p [N] float, top_k [N] int32; out: token [N] int32; optional prob [N], n_kept [N]
+    int32."""
+    z, N, V, ld = _matrix(Z, "Z")
+    _check(lib().alr_sample_tokens(z, dtype_code(Z.dtype), N, V, ld, _ptr(u, "u", N, _I32),
+                                   _ptr(temperature, "temperature", N, _F32),
+                                   _ptr(top_k, "top_k", N, _I32), _ptr(top_p, "top_p", N, _F32),
+                                   _ptr(min_p, "min_p", N, _F32),
+                                   _ptr(out["token"], "token", N, _I32),
+                                   _ptr(out.get("prob"), "prob", N, _F32),
+                                   _ptr(out.get("n_kept"), "n_kept", N, _I32), _stream(stream)))
+
+
+def alr_embed(E, tokens, out, scale=1.0, stream=None):
+    """out [N, d] = scale * E[tokens], E [V, d], tokens [N] int32."""
+    V, d = E.shape
+    N, dt = tokens.numel(), E.dtype
+    _check(lib().alr_embed(_ptr(E, "E"), dtype_code(dt), V, d, _ptr(tokens, "tokens", N, _I32), N,
+                           float(scale), _ptr(out, "out", N * d, dt), _stream(stream)))
+
+
+def alr_embed_grad_workspace_size(V, d, N) -> int:
+    return lib().alr_embed_grad_workspace_size(V, d, N)
+
+
+def alr_embed_grad(dY, tokens, dE, workspace, scale=1.0, accumulate=False, stream=None):
+    """dE [V, d] float (+)= scale * the sums of dY's rows [N, d] by token."""
+    V, d = dE.shape
+    N, dt = tokens.numel(), dY.dtype
+    _check(lib().alr_embed_grad(_ptr(dY, "dY", N * d, dt), dtype_code(dt), V, d,
+                                _ptr(tokens, "tokens", N, _I32), N, float(scale), int(accumulate),
+                                _ptr(dE, "dE", V * d, _F32), _ws(workspace), _nbytes(workspace),
+                                _stream(stream)))
 
 
 # ------------------------------------------------------------------ convenience ---

@@ -1381,3 +1381,227 @@ int alr_gemm(int32_t dtype, int32_t a_mn, int32_t b_mn, int32_t accumulate, cons
 }
 
 }  // extern "C"
+
+// ------------------------------------------------ operators on logits in hand, embedding ---
+namespace {
+
+constexpr int64_t kMostRows = int64_t(1) << 26;   // times a cluster of CTAs fits a grid
+
+int check_logits(const void* Z, int dtype, int64_t N, int32_t V, int64_t ldz) {
+  if (dtype != ALR_BF16 && dtype != ALR_F32)
+    return fail(ALR_ERR_UNSUPPORTED, "dtype %d is not ALR_BF16 or ALR_F32", dtype);
+  if (N < 0 || N > kMostRows)
+    return fail(ALR_ERR_INVALID_ARG, "N = %lld must lie in [0, 2^26]", (long long)N);
+  if (V < 1 || V > ALR_LOGITS_MAX_V)
+    return fail(ALR_ERR_INVALID_ARG, "V = %d must lie in [1, %d]", V, ALR_LOGITS_MAX_V);
+  if (ldz < V || ldz > (int64_t(1) << 40))
+    return fail(ALR_ERR_INVALID_ARG, "the row stride %lld must be at least V = %d and at most 2^40",
+                (long long)ldz, V);
+  if (N > 0 && (Z == nullptr || !aligned16(Z)))
+    return fail(ALR_ERR_INVALID_ARG, "Z must be non-NULL and 16-byte aligned");
+  return ALR_OK;
+}
+
+int check_temperature(float t) {
+  if (!(t > 0.f) || !(1.f / t > 0.f) || !(1.f / t < 3.4e38f))
+    return fail(ALR_ERR_INVALID_ARG, "temperature must be > 0 and finite");
+  return ALR_OK;
+}
+
+int check_distill(const alr_distill_params* p, const void* Z, const float* top_val,
+                  const int32_t* top_idx) {
+  if (p == nullptr) return fail(ALR_ERR_INVALID_ARG, "params is NULL");
+  int rc = check_logits(Z, p->dtype, p->N, p->V, p->ldz);
+  if (rc != ALR_OK) return rc;
+  if (p->K < 1 || p->K > ALR_TOP_MAX)
+    return fail(ALR_ERR_INVALID_ARG, "K = %d must lie in [1, %d]", p->K, ALR_TOP_MAX);
+  if ((rc = check_temperature(p->temperature)) != ALR_OK) return rc;
+  if (!(p->lambda == p->lambda)) return fail(ALR_ERR_INVALID_ARG, "lambda is NaN");
+  if (p->N > 0 && (top_val == nullptr || top_idx == nullptr))
+    return fail(ALR_ERR_INVALID_ARG, "top_val and top_idx must be non-NULL");
+  return ALR_OK;
+}
+
+int check_distill_out(const alr_distill_params* p, const float* rest,
+                      const alr_distill_outputs* out) {
+  if (out == nullptr || out->loss_total == nullptr || out->weight_sum == nullptr)
+    return fail(ALR_ERR_INVALID_ARG, "loss_total and weight_sum must be non-NULL");
+  if (p->N > 0 && (out->loss_row == nullptr || out->lse == nullptr))
+    return fail(ALR_ERR_INVALID_ARG, "loss_row and lse must be non-NULL");
+  if (p->N > 0 && rest != nullptr && out->lse_rest == nullptr)
+    return fail(ALR_ERR_INVALID_ARG, "lse_rest must be non-NULL when rest is given");
+  return ALR_OK;
+}
+
+int check_distill_grad(const alr_distill_params* p, const void* Z, const void* G) {
+  if (p->ldg < p->V || p->ldg > (int64_t(1) << 40))
+    return fail(ALR_ERR_INVALID_ARG, "ldg = %lld must be at least V = %d and at most 2^40",
+                (long long)p->ldg, p->V);
+  if (p->N > 0 && (G == nullptr || !aligned16(G)))
+    return fail(ALR_ERR_INVALID_ARG, "G must be non-NULL and 16-byte aligned");
+  if (p->N > 0 && G == Z && p->ldg != p->ldz)
+    return fail(ALR_ERR_INVALID_ARG, "G may be Z only with ldg = ldz (%lld, %lld)",
+                (long long)p->ldg, (long long)p->ldz);
+  return ALR_OK;
+}
+
+alr::DistillArgs distill_args(const alr_distill_params* p) {
+  return {p->N, p->ldz, p->ldg, p->V, p->K, p->dtype == ALR_BF16 ? 0 : 1, 1.f / p->temperature,
+          p->lambda};
+}
+
+int run_distill(const alr_distill_params* p, bool fwd, bool grad, const void* Z,
+                const float* top_val, const int32_t* top_idx, const float* rest,
+                const float* weight, const float* norm, const alr::DistillRows& o,
+                const alr::DistillSums& t, void* G, void* stream) {
+  DevInfo info;
+  const int rc = require_sm103(&info);
+  if (rc != ALR_OK) return rc;
+  const cudaError_t e = alr::launch_distill(distill_args(p), fwd, grad, Z, top_val, top_idx, rest,
+                                            weight, norm, o, t, G,
+                                            static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? ALR_OK : cuda_fail(e, "distillation launch");
+}
+
+int check_embed(int dtype, int32_t V, int32_t d, const int32_t* tokens, int64_t N, int64_t most) {
+  if (dtype != ALR_BF16 && dtype != ALR_F32)
+    return fail(ALR_ERR_UNSUPPORTED, "dtype %d is not ALR_BF16 or ALR_F32", dtype);
+  if (V < 1 || d < 1) return fail(ALR_ERR_INVALID_ARG, "bad sizes V=%d d=%d", V, d);
+  if (N < 0 || N > most)
+    return fail(ALR_ERR_INVALID_ARG, "N = %lld must lie in [0, %lld]", (long long)N,
+                (long long)most);
+  if (N > 0 && tokens == nullptr) return fail(ALR_ERR_INVALID_ARG, "tokens must be non-NULL");
+  return ALR_OK;
+}
+
+constexpr int64_t kMostGradRows = int64_t(1) << 24;
+
+}  // namespace
+
+extern "C" {
+
+int alr_top_logits(const void* Z, int32_t dtype, int64_t N, int32_t V, int64_t ldz, int32_t K,
+                   float temperature, float* top_val, int32_t* top_idx, float* lse,
+                   float* lse_rest, void* stream) {
+  ALR_RANGE();
+  int rc = check_logits(Z, dtype, N, V, ldz);
+  if (rc != ALR_OK) return rc;
+  if (K < 1 || K > ALR_TOP_MAX)
+    return fail(ALR_ERR_INVALID_ARG, "K = %d must lie in [1, %d]", K, ALR_TOP_MAX);
+  if ((rc = check_temperature(temperature)) != ALR_OK) return rc;
+  if (N > 0 && (top_val == nullptr || top_idx == nullptr))
+    return fail(ALR_ERR_INVALID_ARG, "top_val and top_idx must be non-NULL");
+  if (N == 0) return ALR_OK;
+  DevInfo info;
+  if ((rc = require_sm103(&info)) != ALR_OK) return rc;
+  const cudaError_t e = alr::launch_top_logits(dtype == ALR_BF16 ? 0 : 1, Z, N, V, ldz, K,
+                                               1.f / temperature, top_val, top_idx, lse, lse_rest,
+                                               static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? ALR_OK : cuda_fail(e, "top logits launch");
+}
+
+int alr_distill_fwd(const alr_distill_params* p, const void* Z, const float* top_val,
+                    const int32_t* top_idx, const float* rest, const float* weight,
+                    const alr_distill_outputs* out, void* stream) {
+  ALR_RANGE();
+  int rc = check_distill(p, Z, top_val, top_idx);
+  if (rc != ALR_OK) return rc;
+  if ((rc = check_distill_out(p, rest, out)) != ALR_OK) return rc;
+  return run_distill(p, true, false, Z, top_val, top_idx, rest, weight, nullptr,
+                     {out->loss_row, out->ent_row, out->lse, out->lse_rest, out->argmax},
+                     {out->loss_total, out->weight_sum, out->wl_sum}, nullptr, stream);
+}
+
+int alr_distill_bwd(const alr_distill_params* p, const void* Z, const float* top_val,
+                    const int32_t* top_idx, const float* rest, const float* weight,
+                    const float* lse, const float* lse_rest, const float* weight_sum, void* G,
+                    void* stream) {
+  ALR_RANGE();
+  int rc = check_distill(p, Z, top_val, top_idx);
+  if (rc != ALR_OK) return rc;
+  if ((rc = check_distill_grad(p, Z, G)) != ALR_OK) return rc;
+  if (p->N == 0) return ALR_OK;
+  if (lse == nullptr || weight_sum == nullptr || (rest != nullptr && lse_rest == nullptr))
+    return fail(ALR_ERR_INVALID_ARG,
+                "lse and weight_sum (and lse_rest when rest is given) must be non-NULL");
+  return run_distill(p, false, true, Z, top_val, top_idx, rest, weight, weight_sum,
+                     {nullptr, nullptr, const_cast<float*>(lse), const_cast<float*>(lse_rest),
+                      nullptr},
+                     {nullptr, nullptr, nullptr}, G, stream);
+}
+
+int alr_distill_fwd_bwd(const alr_distill_params* p, const void* Z, const float* top_val,
+                        const int32_t* top_idx, const float* rest, const float* weight,
+                        const float* batch_weight_sum, const alr_distill_outputs* out, void* G,
+                        void* stream) {
+  ALR_RANGE();
+  int rc = check_distill(p, Z, top_val, top_idx);
+  if (rc != ALR_OK) return rc;
+  if ((rc = check_distill_out(p, rest, out)) != ALR_OK) return rc;
+  if ((rc = check_distill_grad(p, Z, G)) != ALR_OK) return rc;
+  return run_distill(p, true, true, Z, top_val, top_idx, rest, weight, batch_weight_sum,
+                     {out->loss_row, out->ent_row, out->lse, out->lse_rest, out->argmax},
+                     {out->loss_total, out->weight_sum, out->wl_sum}, G, stream);
+}
+
+int alr_sample_tokens(const void* Z, int32_t dtype, int64_t N, int32_t V, int64_t ldz,
+                      const uint32_t* u, const float* temperature, const int32_t* top_k,
+                      const float* top_p, const float* min_p, int32_t* token, float* prob,
+                      int32_t* n_kept, void* stream) {
+  ALR_RANGE();
+  int rc = check_logits(Z, dtype, N, V, ldz);
+  if (rc != ALR_OK) return rc;
+  if (N == 0) return ALR_OK;
+  if (u == nullptr || token == nullptr)
+    return fail(ALR_ERR_INVALID_ARG, "u and token must be non-NULL");
+  DevInfo info;
+  if ((rc = require_sm103(&info)) != ALR_OK) return rc;
+  const cudaError_t e = alr::launch_sample(dtype == ALR_BF16 ? 0 : 1, Z, N, V, ldz,
+                                           {u, temperature, top_k, top_p, min_p}, token, prob,
+                                           n_kept, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? ALR_OK : cuda_fail(e, "sampling launch");
+}
+
+int alr_embed(const void* E, int32_t dtype, int32_t V, int32_t d, const int32_t* tokens, int64_t N,
+              float scale, void* out, void* stream) {
+  ALR_RANGE();
+  int rc = check_embed(dtype, V, d, tokens, N, kMostRows);
+  if (rc != ALR_OK) return rc;
+  if (N == 0) return ALR_OK;
+  if (E == nullptr || out == nullptr || !aligned16(E) || !aligned16(out))
+    return fail(ALR_ERR_INVALID_ARG, "E and out must be non-NULL and 16-byte aligned");
+  DevInfo info;
+  if ((rc = require_sm103(&info)) != ALR_OK) return rc;
+  const cudaError_t e = alr::launch_embed(dtype == ALR_BF16 ? 0 : 1, E, V, d, tokens, N, scale, out,
+                                          static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? ALR_OK : cuda_fail(e, "embedding launch");
+}
+
+size_t alr_embed_grad_workspace_size(int32_t V, int32_t d, int64_t N) {
+  if (V < 1 || d < 1 || N < 0 || N > kMostGradRows) return 0;
+  return alr::embed_grad_workspace(V, d, int(N));
+}
+
+int alr_embed_grad(const void* dY, int32_t dtype, int32_t V, int32_t d, const int32_t* tokens,
+                   int64_t N, float scale, int32_t accumulate, float* dE, void* workspace,
+                   size_t ws_bytes, void* stream) {
+  ALR_RANGE();
+  int rc = check_embed(dtype, V, d, tokens, N, kMostGradRows);
+  if (rc != ALR_OK) return rc;
+  if (dE == nullptr || !aligned16(dE))
+    return fail(ALR_ERR_INVALID_ARG, "dE must be non-NULL and 16-byte aligned");
+  if (N > 0 && (dY == nullptr || !aligned16(dY)))
+    return fail(ALR_ERR_INVALID_ARG, "dY must be non-NULL and 16-byte aligned");
+  const size_t need = alr::embed_grad_workspace(V, d, int(N));
+  if (workspace == nullptr || !aligned16(workspace) || ws_bytes < need)
+    return fail(ALR_ERR_INVALID_ARG,
+                "workspace must be 16-byte aligned and hold %zu bytes (got %zu)", need, ws_bytes);
+  DevInfo info;
+  if ((rc = require_sm103(&info)) != ALR_OK) return rc;
+  const cudaError_t e = alr::launch_embed_grad(dtype == ALR_BF16 ? 0 : 1, dY, V, d, tokens, int(N),
+                                               scale, accumulate != 0, dE, workspace,
+                                               static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? ALR_OK : cuda_fail(e, "embedding gradient launch");
+}
+
+}  // extern "C"

@@ -223,6 +223,54 @@ cudaError_t launch_transpose32(const float* in, float* out, int R, int C, int ld
 cudaError_t launch_transpose32_pair(const float* a, float* a_out, int Ca, const float* b,
                                     float* b_out, int Cb, int R, int ld_out, cudaStream_t s);
 
+// Distillation from a teacher's top logits (distill_kernels.cu).
+struct DistillArgs {
+  long long N, ldz, ldg;   // rows, row strides of the logits and of the gradient (elements)
+  int V, K, dtype;
+  float inv_t, lambda;     // 1 / temperature
+};
+struct DistillRows {       // per-row results; a gradient alone reads lse and lse_rest
+  float* loss_row;
+  float* ent_row;
+  float* lse;
+  float* lse_rest;
+  int32_t* argmax;
+};
+struct DistillSums {
+  float* loss_total;
+  float* weight_sum;
+  float* wl_sum;
+};
+// norm: sum of the weights that the gradient divides by (nullptr with fwd: the rows' own).
+cudaError_t launch_distill(const DistillArgs& a, bool fwd, bool grad, const void* Z,
+                           const float* top_val, const int32_t* top_idx, const float* rest,
+                           const float* weight, const float* norm, const DistillRows& o,
+                           const DistillSums& t, void* G, cudaStream_t s);
+
+// Top logits and sampling (sample_kernels.cu).
+constexpr int kTopMost = 256;        // ALR_TOP_MAX
+cudaError_t launch_top_logits(int dtype, const void* Z, long long N, int V, long long ldz, int K,
+                              float inv_t, float* top_val, int32_t* top_idx, float* lse,
+                              float* lse_rest, cudaStream_t s);
+struct SampleArgs {
+  const uint32_t* u;
+  const float* temperature;   // each of these may be nullptr
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+};
+cudaError_t launch_sample(int dtype, const void* Z, long long N, int V, long long ldz,
+                          const SampleArgs& a, int32_t* token, float* prob, int32_t* n_kept,
+                          cudaStream_t s);
+
+// Embedding lookup and the gradient of the table (embed_kernels.cu).
+cudaError_t launch_embed(int dtype, const void* table, int V, int d, const int32_t* tokens,
+                         long long N, float scale, void* out, cudaStream_t s);
+size_t embed_grad_workspace(int V, int d, int N);
+cudaError_t launch_embed_grad(int dtype, const void* dY, int V, int d, const int32_t* tokens,
+                              int N, float scale, bool accumulate, float* dE, void* workspace,
+                              cudaStream_t s);
+
 // Record `msg` as this host thread's alr_last_error() text and return `code` (api.cu).
 int set_last_error(int code, const char* msg);
 
