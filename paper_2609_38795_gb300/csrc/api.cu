@@ -1599,7 +1599,7 @@ int alr_embed_grad(const void* dY, int32_t dtype, int32_t V, int32_t d, const in
   DevInfo info;
   if ((rc = require_sm103(&info)) != ALR_OK) return rc;
   const cudaError_t e = alr::launch_embed_grad(dtype == ALR_BF16 ? 0 : 1, dY, V, d, tokens, int(N),
-                                               scale, accumulate != 0, dE, workspace,
+                                               scale, accumulate != 0, dE, workspace, info.sms,
                                                static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? ALR_OK : cuda_fail(e, "embedding gradient launch");
 }

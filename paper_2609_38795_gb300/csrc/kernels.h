@@ -269,7 +269,7 @@ cudaError_t launch_embed(int dtype, const void* table, int V, int d, const int32
 size_t embed_grad_workspace(int V, int d, int N);
 cudaError_t launch_embed_grad(int dtype, const void* dY, int V, int d, const int32_t* tokens,
                               int N, float scale, bool accumulate, float* dE, void* workspace,
-                              cudaStream_t s);
+                              int sms, cudaStream_t s);
 
 // Record `msg` as this host thread's alr_last_error() text and return `code` (api.cu).
 int set_last_error(int code, const char* msg);
