@@ -79,10 +79,10 @@ ALR_DEV void put_sum(float* dst, const float (&acc)[kCols], float scale, bool ac
   }
 }
 
-// Zeros in those of 32 table rows from v0 on whose bit in `present` is clear (whole block).
-ALR_DEV void zero_rows(float* dE, int V, int d, int v0, uint32_t present) {
-  for (int k = 0; k < 32 && v0 + k < V; ++k) {
-    if (present >> k & 1) continue;
+// Zeros in the table rows [v0, v0 + n) whose bit in `present` is clear (whole block).
+ALR_DEV void zero_rows(float* dE, int d, int v0, int n, const uint32_t* present) {
+  for (int k = 0; k < n; ++k) {
+    if (present[k >> 5] >> (k & 31) & 1) continue;
     float* row = dE + (long long)(v0 + k) * d;
     if (d % 4 == 0)
       for (int c = threadIdx.x; c < d / 4; c += blockDim.x)
@@ -92,21 +92,19 @@ ALR_DEV void zero_rows(float* dE, int V, int d, int v0, uint32_t present) {
   }
 }
 
-// --- few rows: one kernel.  Blocks [0, N * slices) take a row and a slice of its columns: the
-// first row of each token gathers all rows of it, kFewGroups groups of threads taking every
-// kFewGroups-th one.  The other blocks zero the table rows of absent tokens.
+// --- few rows: one kernel.  Blocks [0, N * slices) take a row and a slice of `lanes` packs of its
+// columns: the first row of each token gathers all rows of it, each group of `lanes` threads taking
+// every (kFewThreads / lanes)-th one.  The other blocks zero the table rows of absent tokens.
 constexpr int kFewRows = 512;
 constexpr int kFewThreads = 256;
-constexpr int kFewGroups = 4;
-constexpr int kFewLanes = kFewThreads / kFewGroups;   // packs of a slice
 
 template <typename E, int kCols>
 __global__ void __launch_bounds__(kFewThreads)
     embed_grad_few_kernel(const E* dY, int V, int d, const int32_t* tokens, int N, int slices,
-                          float scale, int accumulate, float* dE) {
+                          int lanes, float scale, int accumulate, float* dE) {
   __shared__ int tok[kFewRows];
   __shared__ int rows[kFewRows];
-  __shared__ float sums[kFewGroups][kFewLanes * kCols];
+  __shared__ float sums[kFewThreads * kCols];
   __shared__ int n_rows, earlier;
   __shared__ uint32_t present;
   pdl_wait_and_release();
@@ -121,7 +119,7 @@ __global__ void __launch_bounds__(kFewThreads)
     for (int j = threadIdx.x; j < N; j += kFewThreads)
       if (tok[j] >= v0 && tok[j] - v0 < 32) atomicOr(&present, 1u << (tok[j] - v0));
     __syncthreads();
-    zero_rows(dE, V, d, v0, present);
+    zero_rows(dE, d, v0, min(32, V - v0), &present);
     return;
   }
   const int i = blockIdx.x / slices, slice = blockIdx.x - i * slices, v = tok[i];
@@ -142,23 +140,22 @@ __global__ void __launch_bounds__(kFewThreads)
     if (threadIdx.x == 0) n_rows = n;
   }
   __syncthreads();
-  const int group = threadIdx.x / kFewLanes, lane = threadIdx.x % kFewLanes;
-  const int pack = slice * kFewLanes + lane, packs = d / kCols, n = n_rows;
+  const int group = threadIdx.x / lanes, lane = threadIdx.x % lanes, groups = kFewThreads / lanes;
+  const int pack = slice * lanes + lane, packs = d / kCols, n = n_rows;
   float acc[kCols] = {};
   if (pack < packs) {
 #pragma unroll 8
-    for (int k = group; k < n; k += kFewGroups)
+    for (int k = group; k < n; k += groups)
       add_pack(acc, reinterpret_cast<const Pack<E, kCols>*>(dY)[(long long)rows[k] * packs + pack]);
   }
   if (n > 1) {
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) sums[group][lane * kCols + c] = acc[c];
+    for (int c = 0; c < kCols; ++c) sums[c * kFewThreads + threadIdx.x] = acc[c];
     __syncthreads();
     if (group == 0)
+      for (int g = 1; g < min(groups, n); ++g)
 #pragma unroll
-      for (int g = 1; g < kFewGroups; ++g)
-#pragma unroll
-        for (int c = 0; c < kCols; ++c) acc[c] += sums[g][lane * kCols + c];
+        for (int c = 0; c < kCols; ++c) acc[c] += sums[c * kFewThreads + g * lanes + lane];
   }
   if (group == 0 && pack < packs)
     put_sum(dE + (long long)v * d + pack * kCols, acc, scale, accumulate != 0);
@@ -171,6 +168,21 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortCtas = 8;
 constexpr int kSortBits = 9;            // of the key at most in a pass
 constexpr int kSortBins = 1 << kSortBits;
+constexpr int kSortBatch = 8;           // steps of 32 keys that a warp has in flight
+
+// Lanes that hold the same digit (the keys past the end, all ones, differ from any digit in the bit
+// above).  A ballot for each bit: a match instruction takes a turn for each distinct value (the first
+// sweep over 32768 tokens of a 32000-token table 11.5 K cycles with it, 6.6 K with ballots).
+ALR_DEV unsigned digit_peers(uint32_t digit, int bits) {
+  unsigned peers = 0xffffffffu;
+#pragma unroll
+  for (int b = 0; b <= kSortBits; ++b) {
+    if (b > bits) break;
+    const unsigned set = __ballot_sync(0xffffffffu, digit >> b & 1);
+    peers &= digit >> b & 1 ? set : ~set;
+  }
+  return peers;
+}
 
 struct GradPlan {
   int chunk, n_chunks, passes, bits;
@@ -180,7 +192,7 @@ struct GradPlan {
 // Rows of a chunk: enough chunks to fill the device, few partial sums for a token in every row.
 GradPlan grad_plan(int V, int d, int N) {
   GradPlan g{};
-  g.chunk = N <= 4096 ? 16 : N <= 16384 ? 32 : N <= 65536 ? 64 : 128;
+  g.chunk = N <= 8192 ? 16 : N <= 16384 ? 32 : N <= 65536 ? 64 : 128;
   g.n_chunks = (N + g.chunk - 1) / g.chunk;
   int bits = 1;
   while ((long long)V >> bits != 0) ++bits;    // keys 0 .. V
@@ -196,7 +208,7 @@ GradPlan grad_plan(int V, int d, int N) {
     g.tok_off[k] = take(size_t(N) * 4);
     g.row_off[k] = take(size_t(N) * 4);
   }
-  g.list_off = take(size_t(g.n_chunks) * 4);
+  g.list_off = take(size_t(g.n_chunks) * 8);
   g.count_off = take(4);
   g.present_off = take((size_t(V) + 31) / 32 * 4);
   g.part_off = take(size_t(g.n_chunks) * 2 * d * sizeof(float));
@@ -204,12 +216,12 @@ GradPlan grad_plan(int V, int d, int N) {
   return g;
 }
 
-// Also: `present`, a bit for each token that occurs (nullptr: not wanted), and the starts of the
-// runs of more than `chunk` rows in `list` (in any order), their number in *count.
+// Also: `present`, a bit for each token that occurs (nullptr: not wanted), and the runs of more than
+// `chunk` rows in `list` (first place in the order and token, in any order), their number in *count.
 __global__ void __launch_bounds__(kSortThreads)
     embed_sort_kernel(const int32_t* tokens, int N, int V, int passes, int bits, int chunk,
                       uint32_t* tok0, uint32_t* row0, uint32_t* tok1, uint32_t* row1,
-                      uint32_t* present, int32_t* list, int32_t* count) {
+                      uint32_t* present, int2* list, int32_t* count) {
   __shared__ uint32_t hist[kSortWarps][kSortBins];
   __shared__ uint32_t cta_total[kSortBins];
   __shared__ uint32_t scan[kSortWarps];
@@ -226,17 +238,39 @@ __global__ void __launch_bounds__(kSortThreads)
   uint32_t *src_t = nullptr, *src_r = nullptr, *dst_t = tok0, *dst_r = row0;
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * bits;
-    auto load = [&](int p) -> uint32_t {
-      if (pass > 0) return __ldcg(src_t + p);
-      const int v = tokens[p];
-      return v >= 0 && v < V ? uint32_t(v) : uint32_t(V);
+    // keys (and rows) of kSortBatch steps, all loads in flight; ~0 past the end
+    const uint32_t* keys = pass > 0 ? src_t : reinterpret_cast<const uint32_t*>(tokens);
+    // keys (and rows) of kSortBatch steps, all loads in flight; ~0 past the end
+    auto load = [&](int s0, uint32_t (&key)[kSortBatch], uint32_t (&row)[kSortBatch], bool rows) {
+#pragma unroll
+      for (int j = 0; j < kSortBatch; ++j) {
+        const int p = min(begin + (s0 + j) * 32 + lane, N - 1);
+        key[j] = __ldcg(keys + p);
+        row[j] = uint32_t(p);
+      }
+      if (rows && pass > 0)
+#pragma unroll
+        for (int j = 0; j < kSortBatch; ++j) row[j] = __ldcg(src_r + row[j]);
+#pragma unroll
+      for (int j = 0; j < kSortBatch; ++j) {
+        if (key[j] >= uint32_t(V)) key[j] = uint32_t(V);   // first pass: outside [0, V)
+        if (s0 + j >= steps || begin + (s0 + j) * 32 + lane >= N) key[j] = 0xffffffffu;
+      }
     };
     for (int b = lane; b < bins; b += 32) hist[warp][b] = 0;
     __syncwarp();
-#pragma unroll 4
-    for (int s = 0; s < steps; ++s) {
-      const int p = begin + s * 32 + lane;
-      if (p < N) atomicAdd(&hist[warp][(load(p) >> shift) & (bins - 1)], 1u);
+    uint32_t key[kSortBatch], row[kSortBatch];
+    for (int s0 = 0; s0 < steps; s0 += kSortBatch) {
+      load(s0, key, row, false);
+#pragma unroll
+      for (int j = 0; j < kSortBatch; ++j) {
+        if (s0 + j >= steps) break;
+        const uint32_t digit =
+            key[j] != 0xffffffffu ? (key[j] >> shift) & (bins - 1) : 0xffffffffu;
+        const unsigned peers = digit_peers(digit, bits);
+        if (digit != 0xffffffffu && (peers >> lane) == 1u) hist[warp][digit] += __popc(peers);
+        __syncwarp();
+      }
     }
     __syncthreads();
     // offsets: of the digit, of this block within it, of each warp within the block
@@ -275,22 +309,25 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
       for (int w = 0; w < kSortWarps; ++w) hist[w][b] += base;
     __syncthreads();
-    for (int s = 0; s < steps; ++s) {
-      const int p = begin + s * 32 + lane;
-      const bool in = p < N;
-      const uint32_t key = in ? load(p) : 0u;
-      const uint32_t digit = in ? (key >> shift) & (bins - 1) : 0xffffffffu;
-      const unsigned peers = __match_any_sync(0xffffffffu, digit);
-      if (in) {
-        const int at = int(hist[warp][digit]) + __popc(peers & ((1u << lane) - 1u));
-        dst_t[at] = key;
-        dst_r[at] = pass > 0 ? __ldcg(src_r + p) : uint32_t(p);
+    for (int s0 = 0; s0 < steps; s0 += kSortBatch) {
+      load(s0, key, row, true);
+#pragma unroll
+      for (int j = 0; j < kSortBatch; ++j) {
+        if (s0 + j >= steps) break;
+        const bool in = key[j] != 0xffffffffu;
+        const uint32_t digit = in ? (key[j] >> shift) & (bins - 1) : 0xffffffffu;
+        const unsigned peers = digit_peers(digit, bits);
+        const bool last = in && (peers >> lane) == 1u;
+        uint32_t at = 0;
+        if (in) {
+          at = hist[warp][digit] + __popc(peers & ((1u << lane) - 1u));
+          dst_t[at] = key[j];
+          dst_r[at] = row[j];
+        }
+        __syncwarp();
+        if (last) hist[warp][digit] = at + 1;
+        __syncwarp();
       }
-      __syncwarp();
-      if (in && (peers >> lane) == 1u) hist[warp][digit] += __popc(peers);   // the last of them
-      __syncwarp();
-      if (pass == 0 && in && present != nullptr && key < uint32_t(V))
-        atomicOr(present + (key >> 5), 1u << (key & 31));
     }
     cluster_sync();   // the sorted pairs are written; cta_total may be overwritten
     src_t = dst_t;
@@ -298,14 +335,18 @@ __global__ void __launch_bounds__(kSortThreads)
     dst_t = src_t == tok0 ? tok1 : tok0;
     dst_r = src_r == row0 ? row1 : row0;
   }
-  for (int p = me; p + chunk < N; p += all) {
-    const uint32_t t = __ldcg(src_t + p);
-    if (t < uint32_t(V) && (p == 0 || __ldcg(src_t + p - 1) != t) && __ldcg(src_t + p + chunk) == t)
-      list[atomicAdd(count, 1)] = p;
+#pragma unroll 4
+  for (int p = me; p < N; p += all) {
+    const uint32_t t = __ldcg(src_t + p), before = p > 0 ? __ldcg(src_t + p - 1) : 0xffffffffu;
+    const uint32_t far = p + chunk < N ? __ldcg(src_t + p + chunk) : 0xffffffffu;
+    if (t >= uint32_t(V) || t == before) continue;   // no token's first row
+    if (present != nullptr) atomicOr(present + (t >> 5), 1u << (t & 31));
+    if (far == t) list[atomicAdd(count, 1)] = make_int2(p, int(t));
   }
 }
 
-// --- sums of a chunk's runs (blocks [0, n_chunks * slices)), zeros for absent tokens (the others).
+// --- sums of a chunk's runs (blocks [0, n_chunks * slices): a chunk and a slice of the columns),
+// zeros for absent tokens (the others).
 constexpr int kChunkThreads = 256;
 constexpr int kChunkMost = 128;
 constexpr int kChunkBatch = 8;
@@ -322,7 +363,7 @@ __global__ void __launch_bounds__(kChunkThreads)
   pdl_wait_and_release();
   if (int(blockIdx.x) >= n_chunks * slices) {
     const int g = int(blockIdx.x) - n_chunks * slices;
-    zero_rows(dE, V, d, g * 32, present[g]);
+    zero_rows(dE, d, g * 32, min(32, V - g * 32), present + g);
     return;
   }
   const int c = blockIdx.x / slices, slice = blockIdx.x - c * slices;
@@ -389,7 +430,9 @@ __global__ void __launch_bounds__(kChunkThreads)
 
 // --- long runs: partial sums of the chunks, in order.  A warp takes 128 columns of a run; of a run
 // of many chunks the block's warps take an equal share each, joined in order through shared memory.
-constexpr int kJoinThreads = 256;
+// The items (run, 128 columns) go to the blocks in turn, so that the columns of one run of many
+// chunks are different blocks' (eight to a block: 145 us for one of 480 chunks, 2048 columns).
+constexpr int kJoinThreads = 1024;
 constexpr int kJoinWarps = kJoinThreads / 32;
 constexpr int kJoinFew = 16;   // partial sums that one warp adds
 
@@ -426,7 +469,7 @@ ALR_DEV void put_join(float* dE, uint32_t t, int d, int col, float4 s, float sca
 }
 
 __global__ void __launch_bounds__(kJoinThreads)
-    embed_join_kernel(int d, const uint32_t* tok_s, int N, int chunk, const int32_t* list,
+    embed_join_kernel(int d, const uint32_t* tok_s, int N, int chunk, const int2* list,
                       const int32_t* count, float scale, int accumulate, const float* part,
                       float* dE) {
   __shared__ float4 sums[kJoinWarps][32];
@@ -434,15 +477,16 @@ __global__ void __launch_bounds__(kJoinThreads)
   pdl_wait_and_release();
   const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
   const int groups = (d + 127) / 128, items = *count * groups;
-  for (int i0 = blockIdx.x * kJoinWarps; i0 < items; i0 += gridDim.x * kJoinWarps) {
-    const int i = i0 + warp;
+  for (int i0 = 0; i0 < items; i0 += gridDim.x * kJoinWarps) {
+    const int i = i0 + warp * gridDim.x + blockIdx.x;
     if (lane == 0) todo[warp] = make_int4(0, 0, 0, 0);
     if (i < items) {
-      const int p = list[i / groups], g = i % groups, c = p / chunk;
-      const uint32_t t = tok_s[p];
+      const int2 run = list[i / groups];
+      const int g = i % groups, c = run.x / chunk;
+      const uint32_t t = uint32_t(run.y);
       // chunks after c that begin with the token: lanes test 32 of them, ever closer together
       int more = 0;
-      for (int step = 1 << 15; step > 0; step >>= 5) {
+      for (int step = N / chunk < 1024 ? 32 : 1 << 15; step > 0; step >>= 5) {
         const long long at = (long long)(c + more + (lane + 1) * (long long)step) * chunk;
         more += step * __popc(__ballot_sync(0xffffffffu, at < N && tok_s[at < N ? at : 0] == t));
       }
@@ -484,18 +528,20 @@ cudaError_t embed_grad_cols(const E* dY, int V, int d, const int32_t* tokens, in
                             cudaStream_t s) {
   const int packs = d / kCols, zero_blocks = accumulate ? 0 : (V + 31) / 32;
   if (N <= kFewRows) {
-    const int slices = (packs + kFewLanes - 1) / kFewLanes;
+    // narrow slices, and so many groups for a token of many rows, while the blocks fit the device
+    const int lanes = (long long)N * ((packs + 15) / 16) <= 16 * sms ? 16 : 64;
+    const int slices = (packs + lanes - 1) / lanes;
     if (N == 0 && accumulate) return cudaSuccess;
     return launch_pdl(embed_grad_few_kernel<E, kCols>, dim3(unsigned(N * slices + zero_blocks)),
-                      dim3(kFewThreads), 0, s, dY, V, d, tokens, N, slices, scale, int(accumulate),
-                      dE);
+                      dim3(kFewThreads), 0, s, dY, V, d, tokens, N, slices, lanes, scale,
+                      int(accumulate), dE);
   }
   const GradPlan g = grad_plan(V, d, N);
   uint32_t* tok[2] = {reinterpret_cast<uint32_t*>(ws + g.tok_off[0]),
                       reinterpret_cast<uint32_t*>(ws + g.tok_off[1])};
   uint32_t* row[2] = {reinterpret_cast<uint32_t*>(ws + g.row_off[0]),
                       reinterpret_cast<uint32_t*>(ws + g.row_off[1])};
-  int32_t* list = reinterpret_cast<int32_t*>(ws + g.list_off);
+  int2* list = reinterpret_cast<int2*>(ws + g.list_off);
   int32_t* count = reinterpret_cast<int32_t*>(ws + g.count_off);
   uint32_t* present = accumulate ? nullptr : reinterpret_cast<uint32_t*>(ws + g.present_off);
   float* part = reinterpret_cast<float*>(ws + g.part_off);
@@ -518,7 +564,7 @@ cudaError_t embed_grad_cols(const E* dY, int V, int d, const int32_t* tokens, in
                  dim3(kChunkThreads), 0, s, dY, V, d, tok[in], row[in], N, g.chunk, g.n_chunks,
                  slices, scale, int(accumulate), dE, part, present);
   if (e != cudaSuccess) return e;
-  return launch_pdl(embed_join_kernel, dim3(unsigned(2 * sms)), dim3(kJoinThreads), 0, s, d, tok[in],
+  return launch_pdl(embed_join_kernel, dim3(unsigned(sms)), dim3(kJoinThreads), 0, s, d, tok[in],
                     N, g.chunk, list, count, scale, int(accumulate), part, dE);
 }
 
