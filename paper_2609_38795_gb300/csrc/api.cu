@@ -1458,7 +1458,7 @@ int run_distill(const alr_distill_params* p, bool fwd, bool grad, const void* Z,
   const int rc = require_sm103(&info);
   if (rc != ALR_OK) return rc;
   const cudaError_t e = alr::launch_distill(distill_args(p), fwd, grad, Z, top_val, top_idx, rest,
-                                            weight, norm, o, t, G,
+                                            weight, norm, o, t, G, info.sms,
                                             static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? ALR_OK : cuda_fail(e, "distillation launch");
 }

@@ -4,146 +4,319 @@
 // of the tokens that are not listed (one bin for all of them).  With s = z / T, m = max s,
 // S = sum exp(s - m), R = log-sum-exp of s over the tokens not listed:
 //   l = log S + sum_i p_i (m - s_i) + p_0 (m - R)        (no large numbers cancel)
-//   dl / dz_v = (q_v - p_v) / T for a listed v, else q_v (1 - p_0 / q_0) / T,   q = exp(s) / sum.
-// A bitmap of the listed tokens in shared memory keeps them out of R's sum, which is taken from the
+//   dl / dz_v = (q_v - p_v) / T for a listed v, else exp(s_v - R) (q_0 - p_0) / T,
+// with q = exp(s) / sum and q_0 the mass outside the list; both factors of the second form are at most 1.
+// A bit for each listed token, in shared memory, keeps it out of R's sum, which is taken from the
 // largest logit outside the list: exact however small the mass there is (taking the listed terms
 // off the whole sum would leave rounding errors of the size of the list's own).  Differences of
 // logits are taken before the division by T: they are exact for neighbours.
+//
+// Memory-bound: a row is read once into the registers of a cluster (row_cluster.cuh); its sums are
+// exchanged between the warps once, through distributed shared memory, and the gradient is formed from the
+// same registers.
 #include "kernels.h"
 #include "launch.h"
-#include "row_reduce.cuh"
+#include "row_cluster.cuh"
 
 namespace alr {
 namespace {
 
-constexpr int kRowThreads = 512;
+enum { kFwd = 1, kGrad = 2 };
 
-struct Label {
-  float p;     // this thread's probability (threads >= K: 0)
-  float p0;    // the tail bin's
-  float ent;   // entropy of the label
-  bool has;    // some probability is positive
-  int idx;     // this thread's token, -1 for none
+// The row's label in a block's shared memory.
+struct LabelShared {
+  int idx[kTopMost];       // token, -1 for an absent entry
+  float p[kTopMost];       // probability
+  float z[kTopMost];       // the student's logit
+  float p0, ent;           // the tail bin's probability; entropy
+  int has;                 // some probability is positive
 };
 
-// The row's label; thread i holds entry i.
-ALR_DEV Label row_label(const float* top_val, const int32_t* top_idx, const float* rest,
-                        const DistillArgs& a, long long r, float* buf) {
-  Label l{};
-  l.idx = -1;
-  float x = kNegInf;
-  if (int(threadIdx.x) < a.K) {
-    const int v = top_idx[r * a.K + threadIdx.x];
-    if (v >= 0 && v < a.V) {
-      l.idx = v;
-      x = top_val[r * a.K + threadIdx.x];
+// One warp reads the row's label.  `z` is read for tokens in [lo, hi); the bits of those of
+// the block's range are set in `listed` (a byte for each pack, from pack `base` on).
+template <typename E>
+ALR_DEV void read_label(const E* row, const float* val, const int32_t* tok, const float* rest,
+                        const DistillArgs& a, bool all_z, int base, int n_packs, int off,
+                        uint32_t* listed, LabelShared& l) {
+  const int lane = threadIdx.x & 31;
+  constexpr int kMost = kTopMost / 32;
+  float x[kMost];
+  float tm = kNegInf;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    const int i = k * 32 + lane;
+    x[k] = kNegInf;
+    if (k * 32 >= a.K) continue;
+    int v = i < a.K ? tok[i] : -1;
+    if (v < 0 || v >= a.V) v = -1;
+    if (v >= 0) {
+      x[k] = val[i];
+      const int e = v + off, pack = e / kPerPack<E> - base;
+      const bool here = pack >= 0 && pack < n_packs;
+      if (here || all_z) l.z[i] = to_float(row[v]);
+      if (here) atomicOr(&listed[pack >> 2], 1u << ((pack & 3) * 8 + e % kPerPack<E>));
     }
+    if (i < a.K) l.idx[i] = v;
+    tm = fmaxf(tm, x[k]);
   }
-  const float x0 = rest != nullptr ? rest[r] : kNegInf;
-  const float tm = block_reduce(x, MaxOp(), buf), m = fmaxf(tm * a.inv_t, x0);
-  l.has = m > kNegInf;
-  if (!l.has) return l;
-  const float step = tm > kNegInf ? tm * a.inv_t - m : 0.f;     // 0 unless the bin leads
-  x = x > kNegInf ? (x - tm) * a.inv_t + step : kNegInf;
-  const float d0 = x0 - m;
-  const float e = x > kNegInf ? expf(x) : 0.f, e0 = d0 > kNegInf ? expf(d0) : 0.f;
-  const float sum = block_reduce(e, AddOp(), buf) + e0;
-  const float ls = logf(sum);
-  l.p = e / sum;
-  l.p0 = e0 / sum;
-  // H = sum p (log sum - x)
-  const float h = l.p > 0.f ? l.p * (ls - x) : 0.f;
-  l.ent = block_reduce(h, AddOp(), buf) + (l.p0 > 0.f ? l.p0 * (ls - d0) : 0.f);
-  return l;
+  tm = warp_reduce(tm, MaxOp());
+  const float x0 = rest != nullptr ? *rest : kNegInf, m = fmaxf(tm * a.inv_t, x0);
+  const bool has = m > kNegInf;
+  const float step = tm > kNegInf ? tm * a.inv_t - m : 0.f;   // 0 unless the bin leads
+  const float d0 = x0 - m, e0 = d0 > kNegInf ? expf(d0) : 0.f;
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    if (k * 32 >= a.K) break;
+    x[k] = x[k] > kNegInf ? (x[k] - tm) * a.inv_t + step : kNegInf;
+    sum += x[k] > kNegInf ? expf(x[k]) : 0.f;
+  }
+  sum = warp_reduce(sum, AddOp()) + (has ? e0 : 0.f);
+  const float ls = logf(sum), inv = has ? 1.f / sum : 0.f;
+  float h = 0.f;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    const int i = k * 32 + lane;
+    if (i >= a.K) break;
+    const float p = x[k] > kNegInf ? expf(x[k]) * inv : 0.f;
+    l.p[i] = p;
+    if (p > 0.f) h += p * (ls - x[k]);
+  }
+  h = warp_reduce(h, AddOp());
+  if (lane == 0) {
+    const float p0 = has ? e0 * inv : 0.f;
+    l.p0 = p0;
+    l.has = has;
+    l.ent = p0 > 0.f ? h + p0 * (ls - d0) : h;
+  }
 }
 
-// One block per row.  kFwd: the row's loss, entropy, log-sum-exps and greedy token; kGrad: the
-// gradient of its logits, from this row's sums (both) or from lse, lse_rest of an earlier forward.
-template <typename E, bool kFwd, bool kGrad>
-__global__ void __launch_bounds__(kRowThreads)
+ALR_DEV uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// Gradient of a pack: c exp2((x - ref) k + b) in the row's element type, the elements of `skip` and
+// those outside the row left alone.
+template <typename E>
+ALR_DEV void put_grad(E* g, bool aligned, int v, int V, uint32_t skip, const uint4& raw, float ref,
+                      float k, float b, float c) {
+  float q[kPerPack<E>];
+  const uint64_t ref2 = f2_pack(ref, ref), k2 = f2_pack(k, k), b2 = f2_pack(b, b),
+                 c2 = f2_pack(c, c);
+#pragma unroll
+  for (int e = 0; e < kPerPack<E>; e += 2) {
+    const uint64_t x = f2_pack(pack_elem<E>(raw, e), pack_elem<E>(raw, e + 1));
+    f2_unpack(f2_mul(f2_ex2(f2_fma(f2_sub(x, ref2), k2, b2)), c2), q[e], q[e + 1]);
+  }
+  if (aligned && skip == 0 && v >= 0 && v + kPerPack<E> <= V) {
+    uint4 o;
+    if constexpr (sizeof(E) == 2)
+      o = make_uint4(pack_bf16(q[0], q[1]), pack_bf16(q[2], q[3]), pack_bf16(q[4], q[5]),
+                     pack_bf16(q[6], q[7]));
+    else
+      o = make_uint4(__float_as_uint(q[0]), __float_as_uint(q[1]), __float_as_uint(q[2]),
+                     __float_as_uint(q[3]));
+    __stcs(reinterpret_cast<uint4*>(g + v), o);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < kPerPack<E>; ++e)
+    if (!(skip >> e & 1) && v + e >= 0 && v + e < V) g[v + e] = E(q[e]);
+}
+
+// One cluster per row.  kFwd: the row's loss, entropy, log-sum-exps and greedy token; kGrad: the
+// gradient of its logits, from this row's sums or (kGrad alone) from lse, lse_rest of a forward.
+template <typename E, int kPacks, int kMode>
+__global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
     distill_row_kernel(const E* Z, const float* top_val, const int32_t* top_idx, const float* rest,
                        const float* weight, const float* weight_sum, DistillArgs a,
-                       DistillRows o, E* G) {
-  extern __shared__ uint32_t in_list[];
-  __shared__ float buf[32];
-  __shared__ int ibuf[32];
+                       DistillRows o, E* G, int cluster) {
+  __shared__ uint32_t listed[kRowThreadsMost * kPacks / 4];
+  __shared__ LabelShared lab;
+  __shared__ float2 rec[kRowWarpsMost];   // of each warp: largest logit outside the list, sum
   pdl_wait_and_release();
-  const long long r = blockIdx.x;
+  const int rank = cluster > 1 ? int(blockIdx.x) % cluster : 0;
+  const long long r = cluster > 1 ? blockIdx.x / cluster : blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32, n_warps = blockDim.x / 32;
   const E* z = Z + r * a.ldz;
   E* g = G + r * a.ldg;
+  const RowPlace<E, kPacks> at(r * a.ldz, rank);
   const float w = weight != nullptr ? weight[r] : 1.f;
   if (w == 0.f) {   // not read
-    if (kFwd && threadIdx.x == 0) {
+    if ((kMode & kFwd) && rank == 0 && tid == 0) {
       o.loss_row[r] = 0.f;
       if (o.ent_row != nullptr) o.ent_row[r] = 0.f;
       o.lse[r] = 0.f;
       if (o.lse_rest != nullptr) o.lse_rest[r] = 0.f;
       if (o.argmax != nullptr) o.argmax[r] = -1;
     }
-    if constexpr (kGrad)
-      for (int v = threadIdx.x; v < a.V; v += kRowThreads) g[v] = E(0.f);
+    if constexpr ((kMode & kGrad) != 0) {
+      const RowPlace<E, kPacks> to(r * a.ldg, rank);
+#pragma unroll
+      for (int i = 0; i < kPacks; ++i) {
+        const int v = to.elem(i);
+        if (v >= 0 && v + kPerPack<E> <= a.V) {
+          __stcs(reinterpret_cast<uint4*>(g + v), make_uint4(0, 0, 0, 0));
+        } else {
+#pragma unroll
+          for (int e = 0; e < kPerPack<E>; ++e)
+            if (v + e >= 0 && v + e < a.V) g[v + e] = E(0.f);
+        }
+      }
+    }
     return;
   }
-  for (int i = threadIdx.x; i < (a.V + 31) / 32; i += kRowThreads) in_list[i] = 0;
-  const Label l = row_label(top_val, top_idx, rest, a, r, buf);
+  uint4 raw[kPacks];
+#pragma unroll
+  for (int i = 0; i < kPacks; ++i) raw[i] = load_pack(z, at.elem(i), a.V);
+  const int n_packs = int(blockDim.x) * kPacks;
+  for (int i = tid; i < (n_packs + 3) / 4; i += blockDim.x) listed[i] = 0;
   __syncthreads();
-  if (l.idx >= 0) atomicOr(&in_list[l.idx >> 5], 1u << (l.idx & 31));
-  const float z_i = l.idx >= 0 ? to_float(z[l.idx]) : kNegInf;
+  if (warp == 0)
+    read_label(z, top_val + r * a.K, top_idx + r * a.K, rest != nullptr ? rest + r : nullptr, a,
+               (kMode & kFwd) != 0, at.base, n_packs, at.off, listed, lab);
   __syncthreads();
-  float lse, lse_rest;
-  if constexpr (kFwd) {
-    float m = kNegInf, mo = kNegInf;
-    int at = 0x7fffffff;
-    for (int v = threadIdx.x; v < a.V; v += kRowThreads) {
-      const float x = to_float(z[v]);
-      if (x > m) {
-        m = x;
-        at = v;
-      }
-      if (!(in_list[v >> 5] >> (v & 31) & 1)) mo = fmaxf(mo, x);
+  const uint8_t* listed_bytes = reinterpret_cast<const uint8_t*>(listed) + (at.pack - at.base);
+  const float k = a.inv_t * kLog2e;
+  float ref, b;      // log2 q_v = (z_v - ref) k + b
+  float oref, ob;    // the same for exp(s_v - R) of the tokens outside the list
+  float q0;          // their mass (1 with oref, ob = ref, b where R is not known)
+  bool some;         // the row has a finite logit
+  if constexpr ((kMode & kFwd) != 0) {
+    float m = kNegInf;
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i) {
+      const uint32_t bits = listed_bytes[32 * i];
+      const uint4 x = bits == 0 ? raw[i] : mask_pack<E>(raw[i], bits);
+#pragma unroll
+      for (int e = 0; e < kPerPack<E>; e += 2)
+        m = max3(m, pack_elem<E>(x, e), pack_elem<E>(x, e + 1));
     }
-    const float top = block_reduce(m, MaxOp(), buf);
-    const int first = block_reduce(m == top ? at : 0x7fffffff, MinOp(), ibuf);
-    mo = block_reduce(mo, MaxOp(), buf);
-    const float mt = top > kNegInf ? top : 0.f, c = a.inv_t * kLog2e;
+    m = warp_reduce(m, MaxOp());
+    const float mw = m > kNegInf ? m : 0.f;
+    const uint64_t m2 = f2_pack(mw, mw), k2 = f2_pack(k, k);
+    uint64_t s2 = 0;
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i) {
+      const uint32_t bits = listed_bytes[32 * i];
+      const uint4 x = bits == 0 ? raw[i] : mask_pack<E>(raw[i], bits);
+#pragma unroll
+      for (int e = 0; e < kPerPack<E>; e += 2)
+        s2 = f2_add(s2, f2_ex2(f2_mul(f2_sub(f2_pack(pack_elem<E>(x, e), pack_elem<E>(x, e + 1)), m2),
+                                      k2)));
+    }
+    float sa, sb;
+    f2_unpack(s2, sa, sb);
+    const float sw = warp_reduce(sa + sb, AddOp());
+    if (lane == 0) rec[warp] = make_float2(m, sw);
+    if (cluster > 1)
+      cluster_sync();
+    else
+      __syncthreads();
+    // every warp combines all records, in the same order
+    const int n_rec = n_warps * cluster;
+    float2 t[kRowWarpsMost * kRowClusterMost / 32];
+    float mo = kNegInf;
+    int first = 0x7fffffff;
+#pragma unroll
+    for (int j = 0; j < kRowWarpsMost * kRowClusterMost / 32; ++j) {
+      const int i = j * 32 + lane;
+      t[j] = make_float2(kNegInf, 0.f);
+      if (i < n_rec)
+        t[j] = cluster > 1 ? ld_cluster_f2(cluster_smem_addr(&rec[i % n_warps], i / n_warps))
+                           : rec[i];
+      mo = fmaxf(mo, t[j].x);
+    }
+    if (cluster > 1) cluster_arrive();   // this thread reads no other block's memory any more
+    mo = warp_reduce(mo, MaxOp());
     float So = 0.f;
-    if (mo > kNegInf)
-      for (int v = threadIdx.x; v < a.V; v += kRowThreads)
-        if (!(in_list[v >> 5] >> (v & 31) & 1)) So += ex2((to_float(z[v]) - mo) * c);
-    So = block_reduce(So, AddOp(), buf);
-    const float step = mo > kNegInf ? (mo - mt) * a.inv_t : kNegInf;
-    float S = block_reduce(l.idx >= 0 ? ex2((z_i - mt) * c) : 0.f, AddOp(), buf);
-    if (mo > kNegInf) S += So * expf(step);
-    const float ls = logf(S), lo = logf(So) + step;
-    lse = mt * a.inv_t + ls;
-    lse_rest = mo > kNegInf ? mo * a.inv_t + logf(So) : kNegInf;
-    const float li = l.p > 0.f ? l.p * (ls + (mt - z_i) * a.inv_t) : 0.f;
-    const float loss = block_reduce(li, AddOp(), buf) + (l.p0 > 0.f ? l.p0 * (ls - lo) : 0.f);
-    if (threadIdx.x == 0) {
-      const bool on = l.has && top > kNegInf;
-      o.loss_row[r] = on ? loss : 0.f;
-      if (o.ent_row != nullptr) o.ent_row[r] = on ? l.ent : 0.f;
-      o.lse[r] = lse;
-      if (o.lse_rest != nullptr) o.lse_rest[r] = lse_rest;
-      if (o.argmax != nullptr) o.argmax[r] = top > kNegInf ? first : -1;
+#pragma unroll
+    for (int j = 0; j < kRowWarpsMost * kRowClusterMost / 32; ++j) {
+      if (t[j].x > kNegInf) So += t[j].y * ex2((t[j].x - mo) * k);
+      if (t[j].x == mo && t[j].x > kNegInf) first = min(first, j * 32 + lane);
+    }
+    So = warp_reduce(So, AddOp());
+    first = warp_reduce(first, MinOp());   // the warp that holds the first of the largest, if any
+    float zl = kNegInf;
+    for (int i = lane; i < a.K; i += 32)
+      if (lab.idx[i] >= 0) zl = fmaxf(zl, lab.z[i]);
+    const float top = fmaxf(mo, warp_reduce(zl, MaxOp())), mt = top > kNegInf ? top : 0.f;
+    float S = 0.f;
+    for (int i = lane; i < a.K; i += 32)
+      if (lab.idx[i] >= 0) S += expf((lab.z[i] - mt) * a.inv_t);
+    S = warp_reduce(S, AddOp());
+    const float gap = (mo - mt) * a.inv_t;   // -inf when everything is listed
+    if (mo > kNegInf) S += So * expf(gap);
+    const float ls = logf(S), lo = logf(So);
+    ref = mt;
+    b = -ls * kLog2e;
+    oref = mo > kNegInf ? mo : 0.f;
+    ob = mo > kNegInf ? -lo * kLog2e : 0.f;
+    q0 = mo > kNegInf ? So * expf(gap) / S : 0.f;
+    some = top > kNegInf;
+    if (rank == 0 && warp == 0) {
+      float loss = 0.f;
+      for (int i = lane; i < a.K; i += 32)
+        if (lab.p[i] > 0.f) loss += lab.p[i] * (ls + (mt - lab.z[i]) * a.inv_t);
+      loss = warp_reduce(loss, AddOp());
+      if (lab.p0 > 0.f) loss += lab.p0 * (ls - (lo + gap));
+      if (lane == 0) {
+        const bool on = lab.has && top > kNegInf;
+        o.loss_row[r] = on ? loss : 0.f;
+        if (o.ent_row != nullptr) o.ent_row[r] = on ? lab.ent : 0.f;
+        o.lse[r] = mt * a.inv_t + ls;
+        if (o.lse_rest != nullptr) o.lse_rest[r] = mo > kNegInf ? mo * a.inv_t + lo : kNegInf;
+        if (o.argmax != nullptr && !(top > kNegInf)) o.argmax[r] = -1;
+      }
+    }
+    // the greedy token: the lowest id of the largest logit, in the list or outside; written by the
+    // warp that holds the first one outside (by the first warp when there is none)
+    const bool outside = mo == top && top > kNegInf;
+    const int writer = outside ? first : 0;
+    if (o.argmax != nullptr && top > kNegInf && rank * n_warps + warp == writer) {
+      int v = 0x7fffffff;
+      for (int i = lane; i < a.K; i += 32)
+        if (lab.idx[i] >= 0 && lab.z[i] == top) v = min(v, lab.idx[i]);
+      if (outside) {
+#pragma unroll
+        for (int i = 0; i < kPacks; ++i)
+#pragma unroll
+          for (int e = 0; e < kPerPack<E>; ++e)
+            if (pack_elem<E>(raw[i], e) == top) v = min(v, at.elem(i) + e);
+      }
+      v = warp_reduce(v, MinOp());
+      if (lane == 0) o.argmax[r] = v;
     }
   } else {
-    lse = o.lse[r];
-    lse_rest = rest != nullptr ? o.lse_rest[r] : kNegInf;
-  }
-  if constexpr (kGrad) {
-    const float ws = *weight_sum;
-    const float c = l.has && lse > kNegInf && ws > 0.f ? a.lambda * w / ws * a.inv_t : 0.f;
-    const float k = a.inv_t * kLog2e;
-    // outside the list q_v (1 - p_0 / q_0); q_0 = 0 leaves no token there
-    const float beta = l.p0 > 0.f && lse_rest > kNegInf ? 1.f - l.p0 * expf(lse - lse_rest) : 1.f;
-    const float b = lse > kNegInf ? -lse * kLog2e : 0.f;
-    for (int v = threadIdx.x; v < a.V; v += kRowThreads) {
-      if (in_list[v >> 5] >> (v & 31) & 1) continue;
-      g[v] = E(c != 0.f ? c * beta * ex2(fmaf(to_float(z[v]), k, b)) : 0.f);
+    const float lse = o.lse[r], lse_rest = rest != nullptr ? o.lse_rest[r] : kNegInf;
+    some = lse > kNegInf;
+    ref = oref = 0.f;
+    b = ob = some ? -lse * kLog2e : 0.f;
+    q0 = 1.f;
+    if (rest != nullptr) {
+      ob = lse_rest > kNegInf ? -lse_rest * kLog2e : 0.f;
+      q0 = lse_rest > kNegInf ? expf(lse_rest - lse) : 0.f;
     }
-    if (l.idx >= 0) g[l.idx] = E(c != 0.f ? c * (ex2(fmaf(z_i, k, b)) - l.p) : 0.f);
   }
+  if constexpr ((kMode & kGrad) != 0) {
+    const float ws = *weight_sum;
+    const float c = lab.has && some && ws > 0.f ? a.lambda * w / ws * a.inv_t : 0.f;
+    const float co = c * (q0 - lab.p0);
+    const bool aligned = int(r * a.ldg % kPerPack<E>) == at.off;
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i)
+      put_grad(g, aligned, at.elem(i), a.V, listed_bytes[32 * i],
+               c != 0.f ? raw[i] : neg_inf_pack<E>(), oref, k, ob, co);
+    // the listed tokens of this block's range
+    for (int i = tid; i < a.K; i += blockDim.x) {
+      const int v = lab.idx[i], pack = (v + at.off) / kPerPack<E> - at.base;
+      if (v >= 0 && pack >= 0 && pack < n_packs)
+        g[v] = E(c != 0.f ? c * (ex2(fmaf(lab.z[i] - ref, k, b)) - lab.p[i]) : 0.f);
+    }
+  }
+  if ((kMode & kFwd) && cluster > 1) cluster_wait();   // until no block reads this one's records
 }
 
 // weight_sum = sum of the weights, one block, fixed order.
@@ -175,17 +348,16 @@ __global__ void __launch_bounds__(1024)
   }
 }
 
-template <typename E>
-cudaError_t launch_rows(const DistillArgs& a, bool fwd, bool grad, const void* Z,
-                        const float* top_val, const int32_t* top_idx, const float* rest,
-                        const float* weight, const float* weight_sum, const DistillRows& o, void* G,
-                        cudaStream_t s) {
-  auto kern = fwd ? (grad ? distill_row_kernel<E, true, true> : distill_row_kernel<E, true, false>)
-                  : distill_row_kernel<E, false, true>;
-  const size_t smem = size_t((a.V + 31) / 32) * 4;
-  return launch_pdl(kern, dim3(unsigned(a.N)), dim3(kRowThreads), smem, s,
-                    static_cast<const E*>(Z), top_val, top_idx, rest, weight, weight_sum, a, o,
-                    static_cast<E*>(G));
+template <typename E, int kPacks>
+cudaError_t launch_rows(const RowShape& shape, const DistillArgs& a, bool fwd, bool grad,
+                        const void* Z, const float* top_val, const int32_t* top_idx,
+                        const float* rest, const float* weight, const float* weight_sum,
+                        const DistillRows& o, void* G, cudaStream_t s) {
+  auto kern = fwd ? (grad ? distill_row_kernel<E, kPacks, kFwd | kGrad>
+                          : distill_row_kernel<E, kPacks, kFwd>)
+                  : distill_row_kernel<E, kPacks, kGrad>;
+  return launch_row_clusters(shape, a.N, kern, s, static_cast<const E*>(Z), top_val, top_idx, rest,
+                             weight, weight_sum, a, o, static_cast<E*>(G), shape.cluster);
 }
 
 }  // namespace
@@ -193,7 +365,7 @@ cudaError_t launch_rows(const DistillArgs& a, bool fwd, bool grad, const void* Z
 cudaError_t launch_distill(const DistillArgs& a, bool fwd, bool grad, const void* Z,
                            const float* top_val, const int32_t* top_idx, const float* rest,
                            const float* weight, const float* norm, const DistillRows& o,
-                           const DistillSums& t, void* G, cudaStream_t s) {
+                           const DistillSums& t, void* G, int sms, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   if (fwd) {
     e = launch_pdl(weight_sum_kernel, dim3(1), dim3(1024), 0, s, weight, a.N, t.weight_sum);
@@ -201,10 +373,15 @@ cudaError_t launch_distill(const DistillArgs& a, bool fwd, bool grad, const void
     if (norm == nullptr) norm = t.weight_sum;
   }
   if (a.N > 0) {
-    e = a.dtype == 0 ? launch_rows<__nv_bfloat16>(a, fwd, grad, Z, top_val, top_idx, rest, weight,
-                                                  norm, o, G, s)
-                     : launch_rows<float>(a, fwd, grad, Z, top_val, top_idx, rest, weight, norm, o,
-                                          G, s);
+    const RowShape shape = row_shape(a.N, a.V, a.dtype == 0 ? 2 : 4, sms);
+    const auto run = [&](auto packs) {
+      constexpr int kP = decltype(packs)::value;
+      return a.dtype == 0 ? launch_rows<__nv_bfloat16, kP>(shape, a, fwd, grad, Z, top_val, top_idx,
+                                                           rest, weight, norm, o, G, s)
+                          : launch_rows<float, kP>(shape, a, fwd, grad, Z, top_val, top_idx, rest,
+                                                   weight, norm, o, G, s);
+    };
+    e = with_packs(shape.packs, run);
     if (e != cudaSuccess) return e;
   }
   if (fwd)

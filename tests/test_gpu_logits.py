@@ -226,6 +226,19 @@ def test_distill_masks_and_empty_rows(dtype):
     assert out["loss_total"].item() == 0 and not G.any()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("apart", [60.0, 120.0, 3000.0])
+def test_distill_list_far_above_the_rest(dtype, apart):
+    """The student gives the tokens outside the list next to nothing (below the exponentials' range),
+    the label does not: a large finite loss and a gradient without overflow."""
+    N, V, K = 3, 700, 4
+    val, idx, rest = _teacher(N, V, K, 1.0, seed=41)
+    z = _logits(N, V, 42)
+    z.scatter_add_(1, idx.cpu().long(), torch.full((N, K), apart))
+    out, G, ref = _check_distill(_rows(z, dtype), val, idx, rest, None, 1.0, 1.0)
+    assert np.isfinite(P.np64(out["loss_row"])).all() and torch.isfinite(G).all()
+
+
 def test_distill_normaliser_of_a_sharded_batch():
     """Two halves with the batch's sum of weights give the whole batch's gradient bit for bit."""
     N, V, K = 12, 2000, 8
