@@ -97,34 +97,45 @@ ALR_DEV uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
-// Gradient of a pack: c exp2((x - ref) k + b) in the row's element type, the elements of `skip` and
-// those outside the row left alone.
+// Gradient of a pack, c exp2((x - ref) k + b), in the row's element type; `b` takes ref in.
 template <typename E>
-ALR_DEV void put_grad(E* g, bool aligned, int v, int V, uint32_t skip, const uint4& raw, float ref,
-                      float k, float b, float c) {
+ALR_DEV uint4 grad_pack(const uint4& raw, float k, float b, float c) {
   float q[kPerPack<E>];
-  const uint64_t ref2 = f2_pack(ref, ref), k2 = f2_pack(k, k), b2 = f2_pack(b, b),
-                 c2 = f2_pack(c, c);
+  const uint64_t k2 = f2_pack(k, k), b2 = f2_pack(b, b), c2 = f2_pack(c, c);
 #pragma unroll
   for (int e = 0; e < kPerPack<E>; e += 2) {
     const uint64_t x = f2_pack(pack_elem<E>(raw, e), pack_elem<E>(raw, e + 1));
-    f2_unpack(f2_mul(f2_ex2(f2_fma(f2_sub(x, ref2), k2, b2)), c2), q[e], q[e + 1]);
+    f2_unpack(f2_mul(f2_ex2(f2_fma(x, k2, b2)), c2), q[e], q[e + 1]);
   }
-  if (aligned && skip == 0 && v >= 0 && v + kPerPack<E> <= V) {
-    uint4 o;
-    if constexpr (sizeof(E) == 2)
-      o = make_uint4(pack_bf16(q[0], q[1]), pack_bf16(q[2], q[3]), pack_bf16(q[4], q[5]),
-                     pack_bf16(q[6], q[7]));
-    else
-      o = make_uint4(__float_as_uint(q[0]), __float_as_uint(q[1]), __float_as_uint(q[2]),
-                     __float_as_uint(q[3]));
-    __stcs(reinterpret_cast<uint4*>(g + v), o);
-    return;
-  }
+  if constexpr (sizeof(E) == 2)
+    return make_uint4(pack_bf16(q[0], q[1]), pack_bf16(q[2], q[3]), pack_bf16(q[4], q[5]),
+                      pack_bf16(q[6], q[7]));
+  else
+    return make_uint4(__float_as_uint(q[0]), __float_as_uint(q[1]), __float_as_uint(q[2]),
+                      __float_as_uint(q[3]));
+}
+
+// A pack of results to the row's elements [v, v + kPerPack) within it, but for those of `skip`.
+template <typename E>
+ALR_DEV void store_elems(E* g, int v, int V, uint32_t skip, const uint4& x) {
 #pragma unroll
   for (int e = 0; e < kPerPack<E>; ++e)
-    if (!(skip >> e & 1) && v + e >= 0 && v + e < V) g[v + e] = E(q[e]);
+    if (!(skip >> e & 1) && v + e >= 0 && v + e < V) g[v + e] = E(pack_elem<E>(x, e));
 }
+
+// What a block's first warp makes of the cluster's records, for all of its warps.
+struct RowSums {
+  float ref, b;         // log2 q_v = (z_v - ref) k + b
+  float out_b, out_c;   // gradient outside the list: out_c exp2(z_v k + out_b)
+  float c;              // lambda w / (T sum w); 0 when the row has no gradient
+  float top;            // the largest logit if some token outside the list has it, else NaN
+  int writer;           // the cluster's warp that writes the greedy token
+};
+
+// exp2((x - m) k) with one fma: exp2(x k + b), b = -m k rounded, carries the factor 2^r with
+// r = m k + b, the same for every x, which the caller takes off once.
+ALR_DEV float ref_offset(float m, float k) { return -m * k; }
+ALR_DEV float ref_residual(float m, float k) { return fmaf(m, k, ref_offset(m, k)); }
 
 // One cluster per row.  kFwd: the row's loss, entropy, log-sum-exps and greedy token; kGrad: the
 // gradient of its logits, from this row's sums or (kGrad alone) from lse, lse_rest of a forward.
@@ -135,14 +146,14 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
                        DistillRows o, E* G, int cluster) {
   __shared__ uint32_t listed[kRowThreadsMost * kPacks / 4];
   __shared__ LabelShared lab;
+  __shared__ RowSums sums;
   __shared__ float2 rec[kRowWarpsMost];   // of each warp: largest logit outside the list, sum
   pdl_wait_and_release();
-  const int rank = cluster > 1 ? int(blockIdx.x) % cluster : 0;
-  const long long r = cluster > 1 ? blockIdx.x / cluster : blockIdx.x;
+  const int rank = cluster > 1 ? int(cluster_ctarank()) : 0;
+  const long long r = cluster > 1 ? cluster_id_x() : blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32, n_warps = blockDim.x / 32;
   const E* z = Z + r * a.ldz;
   E* g = G + r * a.ldg;
-  const RowPlace<E, kPacks> at(r * a.ldz, rank);
   const float w = weight != nullptr ? weight[r] : 1.f;
   if (w == 0.f) {   // not read
     if ((kMode & kFwd) && rank == 0 && tid == 0) {
@@ -154,25 +165,23 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
     }
     if constexpr ((kMode & kGrad) != 0) {
       const RowPlace<E, kPacks> to(r * a.ldg, rank);
+      const uint4 zero = make_uint4(0, 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < kPacks; ++i) {
         const int v = to.elem(i);
-        if (v >= 0 && v + kPerPack<E> <= a.V) {
-          __stcs(reinterpret_cast<uint4*>(g + v), make_uint4(0, 0, 0, 0));
-        } else {
-#pragma unroll
-          for (int e = 0; e < kPerPack<E>; ++e)
-            if (v + e >= 0 && v + e < a.V) g[v + e] = E(0.f);
-        }
+        if (v >= 0 && v + kPerPack<E> <= a.V)
+          __stcs(reinterpret_cast<uint4*>(g + v), zero);
+        else
+          store_elems(g, v, a.V, 0, zero);
       }
     }
     return;
   }
+  const RowPlace<E, kPacks> at(r * a.ldz, rank);
   uint4 raw[kPacks];
-#pragma unroll
-  for (int i = 0; i < kPacks; ++i) raw[i] = load_pack(z, at.elem(i), a.V);
+  load_row(raw, z, at, a.V);
   const int n_packs = int(blockDim.x) * kPacks;
-  for (int i = tid; i < (n_packs + 3) / 4; i += blockDim.x) listed[i] = 0;
+  for (int i = tid; i < n_packs / 4; i += blockDim.x) listed[i] = 0;
   __syncthreads();
   if (warp == 0)
     read_label(z, top_val + r * a.K, top_idx + r * a.K, rest != nullptr ? rest + r : nullptr, a,
@@ -180,140 +189,182 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
   __syncthreads();
   const uint8_t* listed_bytes = reinterpret_cast<const uint8_t*>(listed) + (at.pack - at.base);
   const float k = a.inv_t * kLog2e;
-  float ref, b;      // log2 q_v = (z_v - ref) k + b
-  float oref, ob;    // the same for exp(s_v - R) of the tokens outside the list
-  float q0;          // their mass (1 with oref, ob = ref, b where R is not known)
-  bool some;         // the row has a finite logit
   if constexpr ((kMode & kFwd) != 0) {
     float m = kNegInf;
 #pragma unroll
     for (int i = 0; i < kPacks; ++i) {
-      const uint32_t bits = listed_bytes[32 * i];
-      const uint4 x = bits == 0 ? raw[i] : mask_pack<E>(raw[i], bits);
+      mask_pack<E>(raw[i], listed_bytes[32 * i]);   // the listed tokens are handled apart from here on
 #pragma unroll
       for (int e = 0; e < kPerPack<E>; e += 2)
-        m = max3(m, pack_elem<E>(x, e), pack_elem<E>(x, e + 1));
+        m = max3(m, pack_elem<E>(raw[i], e), pack_elem<E>(raw[i], e + 1));
     }
     m = warp_reduce(m, MaxOp());
-    const float mw = m > kNegInf ? m : 0.f;
-    const uint64_t m2 = f2_pack(mw, mw), k2 = f2_pack(k, k);
+    const float mw = m > kNegInf ? m : 0.f, off = ref_offset(mw, k);
+    const uint64_t off2 = f2_pack(off, off), k2 = f2_pack(k, k);
     uint64_t s2 = 0;
 #pragma unroll
-    for (int i = 0; i < kPacks; ++i) {
-      const uint32_t bits = listed_bytes[32 * i];
-      const uint4 x = bits == 0 ? raw[i] : mask_pack<E>(raw[i], bits);
+    for (int i = 0; i < kPacks; ++i)
 #pragma unroll
-      for (int e = 0; e < kPerPack<E>; e += 2)
-        s2 = f2_add(s2, f2_ex2(f2_mul(f2_sub(f2_pack(pack_elem<E>(x, e), pack_elem<E>(x, e + 1)), m2),
-                                      k2)));
-    }
+      for (int e = 0; e < kPerPack<E>; e += 2) {
+        const uint64_t x = f2_pack(pack_elem<E>(raw[i], e), pack_elem<E>(raw[i], e + 1));
+        s2 = f2_add(s2, f2_ex2(f2_fma(x, k2, off2)));
+      }
     float sa, sb;
     f2_unpack(s2, sa, sb);
-    const float sw = warp_reduce(sa + sb, AddOp());
+    const float sw = warp_reduce(sa + sb, AddOp()) * ex2(-ref_residual(mw, k));
     if (lane == 0) rec[warp] = make_float2(m, sw);
     if (cluster > 1)
       cluster_sync();
     else
       __syncthreads();
-    // every warp combines all records, in the same order
-    const int n_rec = n_warps * cluster;
-    float2 t[kRowWarpsMost * kRowClusterMost / 32];
-    float mo = kNegInf;
-    int first = 0x7fffffff;
-#pragma unroll
-    for (int j = 0; j < kRowWarpsMost * kRowClusterMost / 32; ++j) {
-      const int i = j * 32 + lane;
-      t[j] = make_float2(kNegInf, 0.f);
-      if (i < n_rec)
-        t[j] = cluster > 1 ? ld_cluster_f2(cluster_smem_addr(&rec[i % n_warps], i / n_warps))
-                           : rec[i];
-      mo = fmaxf(mo, t[j].x);
+  }
+  if (warp == 0) {
+    float c = 0.f;
+    if constexpr ((kMode & kGrad) != 0) {
+      const float ws = *weight_sum;
+      c = lab.has && ws > 0.f ? a.lambda * w / ws * a.inv_t : 0.f;
     }
-    if (cluster > 1) cluster_arrive();   // this thread reads no other block's memory any more
-    mo = warp_reduce(mo, MaxOp());
-    float So = 0.f;
+    if constexpr ((kMode & kFwd) != 0) {
+      // the records of all warps of the cluster, in the order of the row
+      constexpr int kMost = kRowWarpsMost * kRowClusterMost / 32;
+      const int n_rec = n_warps * cluster;
+      float2 t[kMost];
+      float mo = kNegInf;
 #pragma unroll
-    for (int j = 0; j < kRowWarpsMost * kRowClusterMost / 32; ++j) {
-      if (t[j].x > kNegInf) So += t[j].y * ex2((t[j].x - mo) * k);
-      if (t[j].x == mo && t[j].x > kNegInf) first = min(first, j * 32 + lane);
-    }
-    So = warp_reduce(So, AddOp());
-    first = warp_reduce(first, MinOp());   // the warp that holds the first of the largest, if any
-    float zl = kNegInf;
-    for (int i = lane; i < a.K; i += 32)
-      if (lab.idx[i] >= 0) zl = fmaxf(zl, lab.z[i]);
-    const float top = fmaxf(mo, warp_reduce(zl, MaxOp())), mt = top > kNegInf ? top : 0.f;
-    float S = 0.f;
-    for (int i = lane; i < a.K; i += 32)
-      if (lab.idx[i] >= 0) S += expf((lab.z[i] - mt) * a.inv_t);
-    S = warp_reduce(S, AddOp());
-    const float gap = (mo - mt) * a.inv_t;   // -inf when everything is listed
-    if (mo > kNegInf) S += So * expf(gap);
-    const float ls = logf(S), lo = logf(So);
-    ref = mt;
-    b = -ls * kLog2e;
-    oref = mo > kNegInf ? mo : 0.f;
-    ob = mo > kNegInf ? -lo * kLog2e : 0.f;
-    q0 = mo > kNegInf ? So * expf(gap) / S : 0.f;
-    some = top > kNegInf;
-    if (rank == 0 && warp == 0) {
-      float loss = 0.f;
+      for (int j = 0; j < kMost; ++j) {
+        t[j] = make_float2(kNegInf, 0.f);
+        if (j * 32 >= n_rec) continue;
+        const int i = j * 32 + lane;
+        if (i < n_rec)
+          t[j] = cluster > 1 ? ld_cluster_f2(cluster_smem_addr(&rec[i % n_warps], i / n_warps))
+                             : rec[i];
+        mo = fmaxf(mo, t[j].x);
+      }
+      mo = warp_reduce(mo, MaxOp());
+      float So = 0.f;
+      int first = 0x7fffffff;
+#pragma unroll
+      for (int j = 0; j < kMost; ++j) {
+        if (t[j].x > kNegInf) So += t[j].y * ex2((t[j].x - mo) * k);
+        if (t[j].x == mo && t[j].x > kNegInf) first = min(first, j * 32 + lane);
+      }
+      So = warp_reduce(So, AddOp());
+      first = warp_reduce(first, MinOp());   // the warp with the first of the largest, if any
+      float zl = kNegInf;
       for (int i = lane; i < a.K; i += 32)
-        if (lab.p[i] > 0.f) loss += lab.p[i] * (ls + (mt - lab.z[i]) * a.inv_t);
-      loss = warp_reduce(loss, AddOp());
-      if (lab.p0 > 0.f) loss += lab.p0 * (ls - (lo + gap));
+        if (lab.idx[i] >= 0) zl = fmaxf(zl, lab.z[i]);
+      const float top = fmaxf(mo, warp_reduce(zl, MaxOp())), mt = top > kNegInf ? top : 0.f;
+      float S = 0.f;
+      for (int i = lane; i < a.K; i += 32)
+        if (lab.idx[i] >= 0) S += expf((lab.z[i] - mt) * a.inv_t);
+      S = warp_reduce(S, AddOp());
+      const float gap = (mo - mt) * a.inv_t;   // -inf when everything is listed
+      if (mo > kNegInf) S += So * expf(gap);
+      const float ls = logf(S), lo = logf(So);
+      if (rank == 0) {
+        float loss = 0.f;
+        for (int i = lane; i < a.K; i += 32)
+          if (lab.p[i] > 0.f) loss += lab.p[i] * (ls + (mt - lab.z[i]) * a.inv_t);
+        loss = warp_reduce(loss, AddOp());
+        if (lab.p0 > 0.f) loss += lab.p0 * (ls - (lo + gap));
+        if (lane == 0) {
+          const bool on = lab.has && top > kNegInf;
+          o.loss_row[r] = on ? loss : 0.f;
+          if (o.ent_row != nullptr) o.ent_row[r] = on ? lab.ent : 0.f;
+          o.lse[r] = mt * a.inv_t + ls;
+          if (o.lse_rest != nullptr) o.lse_rest[r] = mo > kNegInf ? mo * a.inv_t + lo : kNegInf;
+        }
+      }
       if (lane == 0) {
-        const bool on = lab.has && top > kNegInf;
-        o.loss_row[r] = on ? loss : 0.f;
-        if (o.ent_row != nullptr) o.ent_row[r] = on ? lab.ent : 0.f;
-        o.lse[r] = mt * a.inv_t + ls;
-        if (o.lse_rest != nullptr) o.lse_rest[r] = mo > kNegInf ? mo * a.inv_t + lo : kNegInf;
-        if (o.argmax != nullptr && !(top > kNegInf)) o.argmax[r] = -1;
+        // the greedy token is written by the warp that holds the first of the largest logits outside
+        // the list, or by the first warp when the list holds all of them
+        sums.top = mo == top ? top : __builtin_nanf("");
+        sums.writer = mo == top && top > kNegInf ? first : 0;
+        if (!(top > kNegInf)) c = 0.f;
+        sums.c = c;
+        sums.b = -ls * kLog2e;
+        const float olog = ref_residual(mo, k) + lo * kLog2e;   // factors that the fma form carries
+        const bool any = mo > kNegInf;
+        sums.out_b = any ? ref_offset(mo, k) : 0.f;
+        sums.out_c = any ? c * (So * expf(gap) / S - lab.p0) * ex2(-olog) : 0.f;
+        sums.ref = mt;
+      }
+    } else if (lane == 0) {
+      const float lse = o.lse[r], lse_rest = rest != nullptr ? o.lse_rest[r] : kNegInf;
+      if (!(lse > kNegInf)) c = 0.f;
+      sums.c = c;
+      sums.ref = 0.f;
+      sums.b = lse > kNegInf ? -lse * kLog2e : 0.f;
+      if (rest == nullptr) {
+        sums.out_b = sums.b;
+        sums.out_c = c;
+      } else {
+        const bool any = lse_rest > kNegInf;
+        sums.out_b = any ? -lse_rest * kLog2e : 0.f;
+        sums.out_c = any ? c * (expf(lse_rest - lse) - lab.p0) : 0.f;
       }
     }
-    // the greedy token: the lowest id of the largest logit, in the list or outside; written by the
-    // warp that holds the first one outside (by the first warp when there is none)
-    const bool outside = mo == top && top > kNegInf;
-    const int writer = outside ? first : 0;
-    if (o.argmax != nullptr && top > kNegInf && rank * n_warps + warp == writer) {
+  }
+  if ((kMode & kFwd) && cluster > 1) cluster_arrive();   // no other block's memory is read any more
+  __syncthreads();
+  if constexpr ((kMode & kFwd) != 0) {
+    if (o.argmax != nullptr && rank * n_warps + warp == sums.writer) {
+      const float top = sums.top;
       int v = 0x7fffffff;
-      for (int i = lane; i < a.K; i += 32)
-        if (lab.idx[i] >= 0 && lab.z[i] == top) v = min(v, lab.idx[i]);
-      if (outside) {
+      float best = top;   // NaN: outside the list there is none
+      if (!(top == top)) {
+        best = kNegInf;
+        for (int i = lane; i < a.K; i += 32)
+          if (lab.idx[i] >= 0) best = fmaxf(best, lab.z[i]);
+        best = warp_reduce(best, MaxOp());
+      } else {
 #pragma unroll
         for (int i = 0; i < kPacks; ++i)
 #pragma unroll
           for (int e = 0; e < kPerPack<E>; ++e)
             if (pack_elem<E>(raw[i], e) == top) v = min(v, at.elem(i) + e);
       }
+      for (int i = lane; i < a.K; i += 32)
+        if (lab.idx[i] >= 0 && lab.z[i] == best) v = min(v, lab.idx[i]);
       v = warp_reduce(v, MinOp());
-      if (lane == 0) o.argmax[r] = v;
-    }
-  } else {
-    const float lse = o.lse[r], lse_rest = rest != nullptr ? o.lse_rest[r] : kNegInf;
-    some = lse > kNegInf;
-    ref = oref = 0.f;
-    b = ob = some ? -lse * kLog2e : 0.f;
-    q0 = 1.f;
-    if (rest != nullptr) {
-      ob = lse_rest > kNegInf ? -lse_rest * kLog2e : 0.f;
-      q0 = lse_rest > kNegInf ? expf(lse_rest - lse) : 0.f;
+      if (lane == 0) o.argmax[r] = best > kNegInf ? v : -1;
     }
   }
   if constexpr ((kMode & kGrad) != 0) {
-    const float ws = *weight_sum;
-    const float c = lab.has && some && ws > 0.f ? a.lambda * w / ws * a.inv_t : 0.f;
-    const float co = c * (q0 - lab.p0);
-    const bool aligned = int(r * a.ldg % kPerPack<E>) == at.off;
+    const float c = sums.c, out_b = sums.out_b, out_c = sums.out_c;
+    if (c == 0.f) {
 #pragma unroll
-    for (int i = 0; i < kPacks; ++i)
-      put_grad(g, aligned, at.elem(i), a.V, listed_bytes[32 * i],
-               c != 0.f ? raw[i] : neg_inf_pack<E>(), oref, k, ob, co);
+      for (int i = 0; i < kPacks; ++i) raw[i] = neg_inf_pack<E>();
+    }
+    const bool aligned = int(r * a.ldg % kPerPack<E>) == at.off;
+    if (aligned && at.whole(a.V)) {
+      uint4* p = reinterpret_cast<uint4*>(g + at.elem(0));
+#pragma unroll
+      for (int i = 0; i < kPacks; ++i) {
+        const uint4 x = grad_pack<E>(raw[i], k, out_b, out_c);
+        const uint32_t skip = listed_bytes[32 * i];
+        if (skip == 0)
+          __stcs(p + 32 * i, x);
+        else
+          store_elems(g, at.elem(i), a.V, skip, x);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPacks; ++i) {
+        const int v = at.elem(i);
+        const uint4 x = grad_pack<E>(raw[i], k, out_b, out_c);
+        const uint32_t skip = listed_bytes[32 * i];
+        if (aligned && skip == 0 && v >= 0 && v + kPerPack<E> <= a.V)
+          __stcs(reinterpret_cast<uint4*>(g + v), x);
+        else
+          store_elems(g, v, a.V, skip, x);
+      }
+    }
     // the listed tokens of this block's range
     for (int i = tid; i < a.K; i += blockDim.x) {
       const int v = lab.idx[i], pack = (v + at.off) / kPerPack<E> - at.base;
       if (v >= 0 && pack >= 0 && pack < n_packs)
-        g[v] = E(c != 0.f ? c * (ex2(fmaf(lab.z[i] - ref, k, b)) - lab.p[i]) : 0.f);
+        g[v] = E(c != 0.f ? c * (ex2(fmaf(lab.z[i] - sums.ref, k, sums.b)) - lab.p[i]) : 0.f);
     }
   }
   if ((kMode & kFwd) && cluster > 1) cluster_wait();   // until no block reads this one's records

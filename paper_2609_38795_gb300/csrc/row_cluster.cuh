@@ -99,6 +99,12 @@ struct RowPlace {
   }
   // First element of pack i (may be negative or past the row).
   ALR_DEV int elem(int i) const { return (pack + 32 * i) * kPerPack<E> - off; }
+  // Every pack of the warp lies within the row: the same answer in all its lanes, and the warp's
+  // loads and stores need no checks.
+  ALR_DEV bool whole(int V) const {
+    const int first = pack - int(threadIdx.x & 31);
+    return first * kPerPack<E> >= off && (first + 32 * kPacks) * kPerPack<E> - off <= V;
+  }
 };
 
 ALR_DEV uint32_t raw_bits(__nv_bfloat16 x) { return __bfloat16_as_ushort(x); }
@@ -129,6 +135,19 @@ ALR_DEV uint4 load_pack(const E* row, int v, int V) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// The thread's packs of a row.
+template <typename E, int kPacks>
+ALR_DEV void load_row(uint4 (&raw)[kPacks], const E* row, const RowPlace<E, kPacks>& at, int V) {
+  if (at.whole(V)) {
+    const uint4* p = reinterpret_cast<const uint4*>(row + at.elem(0));
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i) raw[i] = __ldcs(p + 32 * i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i) raw[i] = load_pack(row, at.elem(i), V);
+  }
+}
+
 // Element e of a pack (e known when unrolled).
 template <typename E>
 ALR_DEV float pack_elem(const uint4& r, int e) {
@@ -139,19 +158,21 @@ ALR_DEV float pack_elem(const uint4& r, int e) {
     return __uint_as_float(w[e]);
 }
 
-// Elements of a pack whose bit in `bits` is set become -inf.
+// Elements of a pack whose bit in `bits` is set become -inf.  A loop over the set bits, of which
+// there are next to none: unrolled selects would be executed for every pack.
 template <typename E>
-ALR_DEV uint4 mask_pack(uint4 r, uint32_t bits) {
-  uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-  for (int e = 0; e < kPerPack<E>; ++e) {
-    if (!(bits >> e & 1)) continue;
-    if constexpr (sizeof(E) == 2)
-      w[e / 2] = e & 1 ? (w[e / 2] & 0xffffu) | 0xff800000u : (w[e / 2] & 0xffff0000u) | 0xff80u;
-    else
-      w[e] = 0xff800000u;
+ALR_DEV void mask_pack(uint4& r, uint32_t bits) {
+  while (bits != 0) {
+    const int e = __ffs(bits) - 1;
+    bits &= bits - 1;
+    const int word = sizeof(E) == 2 ? e >> 1 : e;
+    const uint32_t m = sizeof(E) == 4 ? 0xffffffffu : e & 1 ? 0xffff0000u : 0xffffu;
+    const uint32_t inf = (sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u) & m;
+    if (word == 0) r.x = (r.x & ~m) | inf;
+    if (word == 1) r.y = (r.y & ~m) | inf;
+    if (word == 2) r.z = (r.z & ~m) | inf;
+    if (word == 3) r.w = (r.w & ~m) | inf;
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Records of the cluster's warps, written by each into its own block's shared memory; after a
