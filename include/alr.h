@@ -660,7 +660,7 @@ int alr_distill_bwd(const alr_distill_params* p, const void* Z, const float* top
 /*
  * Both in one pass over the logits: sum w does not depend on them, so the gradient needs no second
  * call.  batch_weight_sum [1] or NULL: the normaliser of a row-sharded batch (default: this call's
- * own sum w).  Outputs and G as in the two calls.
+ * own sum w; not out->weight_sum, which is written).  Outputs and G as in the two calls.
  */
 int alr_distill_fwd_bwd(const alr_distill_params* p, const void* Z, const float* top_val,
                         const int32_t* top_idx, const float* rest, const float* weight,

@@ -1457,8 +1457,10 @@ int run_distill(const alr_distill_params* p, bool fwd, bool grad, const void* Z,
   DevInfo info;
   const int rc = require_sm103(&info);
   if (rc != ALR_OK) return rc;
+  int* status = alr::device_status_ptr();
+  if (status == nullptr) return fail(ALR_ERR_CUDA, "device status word unavailable");
   const cudaError_t e = alr::launch_distill(distill_args(p), fwd, grad, Z, top_val, top_idx, rest,
-                                            weight, norm, o, t, G, info.sms,
+                                            weight, norm, o, t, G, info.sms, status,
                                             static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? ALR_OK : cuda_fail(e, "distillation launch");
 }
@@ -1539,6 +1541,8 @@ int alr_distill_fwd_bwd(const alr_distill_params* p, const void* Z, const float*
   if (rc != ALR_OK) return rc;
   if ((rc = check_distill_out(p, rest, out)) != ALR_OK) return rc;
   if ((rc = check_distill_grad(p, Z, G)) != ALR_OK) return rc;
+  if (batch_weight_sum != nullptr && batch_weight_sum == out->weight_sum)
+    return fail(ALR_ERR_INVALID_ARG, "batch_weight_sum must not be out->weight_sum, which is written");
   return run_distill(p, true, true, Z, top_val, top_idx, rest, weight, batch_weight_sum,
                      {out->loss_row, out->ent_row, out->lse, out->lse_rest, out->argmax},
                      {out->loss_total, out->weight_sum, out->wl_sum}, G, stream);

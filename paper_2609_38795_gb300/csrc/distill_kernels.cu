@@ -11,9 +11,12 @@
 // off the whole sum would leave rounding errors of the size of the list's own).  Differences of
 // logits are taken before the division by T: they are exact for neighbours.
 //
-// Memory-bound: a row is read once into the registers of a cluster (row_cluster.cuh); its sums are
-// exchanged between the warps once, through distributed shared memory, and the gradient is formed from the
-// same registers.
+// Memory-bound: a row is read once, into the registers of a cluster (row_cluster.cuh), its sums are
+// exchanged between all warps once, and the gradient is formed from the same registers.  Clusters stay and
+// take rows in turn: while a row is worked on, the next one comes into shared memory, fetched by a warp
+// of its own that reads its label too.  (One row a cluster, loads straight into registers: all blocks
+// load, compute and store in step, memory idles while they compute, 250 us instead of 1xx for 2048 x
+// 151936 bf16 logits with 40 % of the rows masked.)
 #include "kernels.h"
 #include "launch.h"
 #include "row_cluster.cuh"
@@ -24,20 +27,23 @@ namespace {
 enum { kFwd = 1, kGrad = 2 };
 
 // The row's label in a block's shared memory.
-struct LabelShared {
+struct Label {
   int idx[kTopMost];       // token, -1 for an absent entry
   float p[kTopMost];       // probability
   float z[kTopMost];       // the student's logit
   float p0, ent;           // the tail bin's probability; entropy
+  float z_max, z_sum;      // of the listed tokens' logits (all_z): largest, sum of exponentials from it
   int has;                 // some probability is positive
+  long long row;           // the row (N: there is no further one) and its weight
+  float w;
 };
 
-// One warp reads the row's label.  `z` is read for tokens in [lo, hi); the bits of those of
-// the block's range are set in `listed` (a byte for each pack, from pack `base` on).
+// One warp reads the row's label, with the student's logits of all listed tokens (all_z) or of those
+// in the block's range, whose bits it sets in `listed` (a byte for each pack, from pack `base` on).
 template <typename E>
 ALR_DEV void read_label(const E* row, const float* val, const int32_t* tok, const float* rest,
                         const DistillArgs& a, bool all_z, int base, int n_packs, int off,
-                        uint32_t* listed, LabelShared& l) {
+                        uint32_t* listed, Label& l) {
   const int lane = threadIdx.x & 31;
   constexpr int kMost = kTopMost / 32;
   float x[kMost];
@@ -59,7 +65,7 @@ ALR_DEV void read_label(const E* row, const float* val, const int32_t* tok, cons
     if (i < a.K) l.idx[i] = v;
     tm = fmaxf(tm, x[k]);
   }
-  tm = warp_reduce(tm, MaxOp());
+  tm = warp_max(tm);
   const float x0 = rest != nullptr ? *rest : kNegInf, m = fmaxf(tm * a.inv_t, x0);
   const bool has = m > kNegInf;
   const float step = tm > kNegInf ? tm * a.inv_t - m : 0.f;   // 0 unless the bin leads
@@ -89,6 +95,21 @@ ALR_DEV void read_label(const E* row, const float* val, const int32_t* tok, cons
     l.has = has;
     l.ent = p0 > 0.f ? h + p0 * (ls - d0) : h;
   }
+  if (all_z) {
+    __syncwarp();
+    float zm = kNegInf, zs = 0.f;
+    for (int i = lane; i < a.K; i += 32)
+      if (l.idx[i] >= 0) zm = fmaxf(zm, l.z[i]);
+    zm = warp_max(zm);
+    if (zm > kNegInf)
+      for (int i = lane; i < a.K; i += 32)
+        if (l.idx[i] >= 0) zs += expf((l.z[i] - zm) * a.inv_t);
+    zs = warp_reduce(zs, AddOp());
+    if (lane == 0) {
+      l.z_max = zm;
+      l.z_sum = zs;
+    }
+  }
 }
 
 ALR_DEV uint32_t pack_bf16(float lo, float hi) {
@@ -115,12 +136,20 @@ ALR_DEV uint4 grad_pack(const uint4& raw, float k, float b, float c) {
                       __float_as_uint(q[3]));
 }
 
-// A pack of results to the row's elements [v, v + kPerPack) within it, but for those of `skip`.
+// A pack of results to the row's elements [v, v + kPerPack), those within [lo, hi).
 template <typename E>
-ALR_DEV void store_elems(E* g, int v, int V, uint32_t skip, const uint4& x) {
+ALR_DEV void store_elems(E* g, int v, int lo, int hi, const uint4& x) {
 #pragma unroll
   for (int e = 0; e < kPerPack<E>; ++e)
-    if (!(skip >> e & 1) && v + e >= 0 && v + e < V) g[v + e] = E(pack_elem<E>(x, e));
+    if (v + e >= lo && v + e < hi) g[v + e] = E(pack_elem<E>(x, e));
+}
+
+template <typename E>
+ALR_DEV void store_pack(E* g, int v, int V, const uint4& x) {
+  if (v >= 0 && v + kPerPack<E> <= V)
+    __stcs(reinterpret_cast<uint4*>(g + v), x);
+  else
+    store_elems(g, v, 0, V, x);
 }
 
 // What a block's first warp makes of the cluster's records, for all of its warps.
@@ -137,255 +166,343 @@ struct RowSums {
 ALR_DEV float ref_offset(float m, float k) { return -m * k; }
 ALR_DEV float ref_residual(float m, float k) { return fmaf(m, k, ref_offset(m, k)); }
 
-// One cluster per row.  kFwd: the row's loss, entropy, log-sum-exps and greedy token; kGrad: the
-// gradient of its logits, from this row's sums or (kGrad alone) from lse, lse_rest of a forward.
+// Named barriers: the row's data and label are there; the data is in registers (of the fetching warp
+// and the others); the sums are there; the gradient outside the list is written (of the others).
+enum { kBarFull = 1, kBarTaken, kBarSums, kBarWritten };
+
+template <typename E, int kPacks>
+struct RowBuffer {   // dynamic shared memory: a slice of a row, then `listed` of two rows
+  uint4* data;
+  uint8_t* listed;
+  int n_packs;
+  ALR_DEV RowBuffer(unsigned char* smem, int threads)
+      : data(reinterpret_cast<uint4*>(smem)),
+        listed(smem + size_t(threads) * kPacks * 16),
+        n_packs(threads * kPacks) {}
+  static size_t bytes(int threads) { return size_t(threads) * kPacks * 18; }
+};
+
+// Blocks of T threads that work on rows and a warp that fetches them; cluster i of n takes the rows i,
+// i + n, ...  kFwd: a row's loss, entropy, log-sum-exps and greedy token; kGrad: the gradient of its
+// logits, from this row's sums or (kGrad alone) from lse, lse_rest of a forward.  A wait that runs out
+// is recorded and the kernel goes on to its end with what it has.
 template <typename E, int kPacks, int kMode>
-__global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
+__global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
     distill_row_kernel(const E* Z, const float* top_val, const int32_t* top_idx, const float* rest,
-                       const float* weight, const float* weight_sum, DistillArgs a,
-                       DistillRows o, E* G, int cluster) {
-  __shared__ uint32_t listed[kRowThreadsMost * kPacks / 4];
-  __shared__ LabelShared lab;
-  __shared__ RowSums sums;
-  __shared__ float2 rec[kRowWarpsMost];   // of each warp: largest logit outside the list, sum
+                       const float* weight, const float* norm, DistillArgs a, DistillRows o,
+                       float* weight_sum, E* G, int cluster, int* status) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ Label labels[2];
+  __shared__ RowSums row_sums[2];
+  // of each warp of the cluster: largest logit outside the list, sum of exponentials from it
+  __shared__ float2 recs[2][kRowWarpsMost * kRowClusterMost];
+  __shared__ uint64_t full_bar, rec_bar[2];
+  __shared__ double wbuf[32];
+  __shared__ volatile int abort_word;
+  const int threads = int(blockDim.x) - 32, n_warps = threads / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+  const int rank = int(cluster_ctarank()), first_row = int(cluster_id_x()), step = int(n_clusters_x());
+  const RowBuffer<E, kPacks> buf(smem, threads);
+  const AbortFlag ab{&abort_word, status};
+  const bool fetcher = warp == n_warps;
+  if (tid == 0) {
+    abort_word = 0;
+    mbar_init(&full_bar, 1);
+    mbar_init(&rec_bar[0], 1);
+    mbar_init(&rec_bar[1], 1);
+    fence_mbar_init();
+  }
   pdl_wait_and_release();
-  const int rank = cluster > 1 ? int(cluster_ctarank()) : 0;
-  const long long r = cluster > 1 ? cluster_id_x() : blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32, n_warps = blockDim.x / 32;
-  const E* z = Z + r * a.ldz;
-  E* g = G + r * a.ldg;
-  const float w = weight != nullptr ? weight[r] : 1.f;
-  if (w == 0.f) {   // not read
-    if ((kMode & kFwd) && rank == 0 && tid == 0) {
-      o.loss_row[r] = 0.f;
-      if (o.ent_row != nullptr) o.ent_row[r] = 0.f;
-      o.lse[r] = 0.f;
-      if (o.lse_rest != nullptr) o.lse_rest[r] = 0.f;
-      if (o.argmax != nullptr) o.argmax[r] = -1;
+  if constexpr ((kMode & kFwd) != 0)
+    cluster_sync();   // the peers' barriers are there
+  else
+    __syncthreads();
+
+  const auto next_live = [&](long long r) {   // rows of weight 0 are not read
+    while (r < a.N && weight != nullptr && weight[r] == 0.f) r += step;
+    return r;
+  };
+  // The block's part of row r, whole packs of it, into the buffer.
+  const auto fetch = [&](long long r) {
+    if (lane != 0) return;
+    const RowPlace<E, kPacks> at(r * a.ldz, rank, threads);
+    const int lo = max(at.base, at.off > 0 ? 1 : 0);
+    const int hi = min(at.base + buf.n_packs, (a.V + at.off) / kPerPack<E>);
+    if (hi > lo) {
+      fence_proxy_async_smem();
+      const uint32_t bytes = uint32_t(hi - lo) * 16;
+      mbar_arrive_expect_tx(&full_bar, bytes);
+      bulk_load(smem_u32(buf.data + (lo - at.base)), Z + r * a.ldz + (lo * kPerPack<E> - at.off), bytes,
+                &full_bar);
+    } else {
+      mbar_arrive(&full_bar);
     }
-    if constexpr ((kMode & kGrad) != 0) {
-      const RowPlace<E, kPacks> to(r * a.ldg, rank);
-      const uint4 zero = make_uint4(0, 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < kPacks; ++i) {
-        const int v = to.elem(i);
-        if (v >= 0 && v + kPerPack<E> <= a.V)
-          __stcs(reinterpret_cast<uint4*>(g + v), zero);
-        else
-          store_elems(g, v, a.V, 0, zero);
-      }
-    }
-    return;
+  };
+  long long live = 0;   // fetching warp: the row that it fetches
+  if (fetcher) {
+    live = next_live(first_row);
+    if (live < a.N) fetch(live);
   }
-  const RowPlace<E, kPacks> at(r * a.ldz, rank);
-  uint4 raw[kPacks];
-  load_row(raw, z, at, a.V);
-  const int n_packs = int(blockDim.x) * kPacks;
-  for (int i = tid; i < n_packs / 4; i += blockDim.x) listed[i] = 0;
-  __syncthreads();
-  if (warp == 0)
-    read_label(z, top_val + r * a.K, top_idx + r * a.K, rest != nullptr ? rest + r : nullptr, a,
-               (kMode & kFwd) != 0, at.base, n_packs, at.off, listed, lab);
-  __syncthreads();
-  const uint8_t* listed_bytes = reinterpret_cast<const uint8_t*>(listed) + (at.pack - at.base);
-  const float k = a.inv_t * kLog2e;
-  if constexpr ((kMode & kFwd) != 0) {
-    float m = kNegInf;
-#pragma unroll
-    for (int i = 0; i < kPacks; ++i) {
-      mask_pack<E>(raw[i], listed_bytes[32 * i]);   // the listed tokens are handled apart from here on
-#pragma unroll
-      for (int e = 0; e < kPerPack<E>; e += 2)
-        m = max3(m, pack_elem<E>(raw[i], e), pack_elem<E>(raw[i], e + 1));
-    }
-    m = warp_reduce(m, MaxOp());
-    const float mw = m > kNegInf ? m : 0.f, off = ref_offset(mw, k);
-    const uint64_t off2 = f2_pack(off, off), k2 = f2_pack(k, k);
-    uint64_t s2 = 0;
-#pragma unroll
-    for (int i = 0; i < kPacks; ++i)
-#pragma unroll
-      for (int e = 0; e < kPerPack<E>; e += 2) {
-        const uint64_t x = f2_pack(pack_elem<E>(raw[i], e), pack_elem<E>(raw[i], e + 1));
-        s2 = f2_add(s2, f2_ex2(f2_fma(x, k2, off2)));
-      }
-    float sa, sb;
-    f2_unpack(s2, sa, sb);
-    const float sw = warp_reduce(sa + sb, AddOp()) * ex2(-ref_residual(mw, k));
-    if (lane == 0) rec[warp] = make_float2(m, sw);
-    if (cluster > 1)
-      cluster_sync();
-    else
-      __syncthreads();
+  // sum w, in the same order in every block
+  float wsum = float(a.N);
+  if (weight != nullptr &&
+      ((kMode & kGrad) && norm == nullptr || (kMode & kFwd) && blockIdx.x == 0)) {
+    double s = 0.0;
+#pragma unroll 8
+    for (long long r = tid; r < a.N; r += blockDim.x) s += double(weight[r]);
+    wsum = float(block_reduce(s, AddOp(), wbuf));
   }
-  if (warp == 0) {
-    float c = 0.f;
-    if constexpr ((kMode & kGrad) != 0) {
-      const float ws = *weight_sum;
-      c = lab.has && ws > 0.f ? a.lambda * w / ws * a.inv_t : 0.f;
-    }
-    if constexpr ((kMode & kFwd) != 0) {
-      // the records of all warps of the cluster, in the order of the row
-      constexpr int kMost = kRowWarpsMost * kRowClusterMost / 32;
-      const int n_rec = n_warps * cluster;
-      float2 t[kMost];
-      float mo = kNegInf;
-#pragma unroll
-      for (int j = 0; j < kMost; ++j) {
-        t[j] = make_float2(kNegInf, 0.f);
-        if (j * 32 >= n_rec) continue;
-        const int i = j * 32 + lane;
-        if (i < n_rec)
-          t[j] = cluster > 1 ? ld_cluster_f2(cluster_smem_addr(&rec[i % n_warps], i / n_warps))
-                             : rec[i];
-        mo = fmaxf(mo, t[j].x);
-      }
-      mo = warp_reduce(mo, MaxOp());
-      float So = 0.f;
-      int first = 0x7fffffff;
-#pragma unroll
-      for (int j = 0; j < kMost; ++j) {
-        if (t[j].x > kNegInf) So += t[j].y * ex2((t[j].x - mo) * k);
-        if (t[j].x == mo && t[j].x > kNegInf) first = min(first, j * 32 + lane);
-      }
-      So = warp_reduce(So, AddOp());
-      first = warp_reduce(first, MinOp());   // the warp with the first of the largest, if any
-      float zl = kNegInf;
-      for (int i = lane; i < a.K; i += 32)
-        if (lab.idx[i] >= 0) zl = fmaxf(zl, lab.z[i]);
-      const float top = fmaxf(mo, warp_reduce(zl, MaxOp())), mt = top > kNegInf ? top : 0.f;
-      float S = 0.f;
-      for (int i = lane; i < a.K; i += 32)
-        if (lab.idx[i] >= 0) S += expf((lab.z[i] - mt) * a.inv_t);
-      S = warp_reduce(S, AddOp());
-      const float gap = (mo - mt) * a.inv_t;   // -inf when everything is listed
-      if (mo > kNegInf) S += So * expf(gap);
-      const float ls = logf(S), lo = logf(So);
-      if (rank == 0) {
-        float loss = 0.f;
-        for (int i = lane; i < a.K; i += 32)
-          if (lab.p[i] > 0.f) loss += lab.p[i] * (ls + (mt - lab.z[i]) * a.inv_t);
-        loss = warp_reduce(loss, AddOp());
-        if (lab.p0 > 0.f) loss += lab.p0 * (ls - (lo + gap));
-        if (lane == 0) {
-          const bool on = lab.has && top > kNegInf;
-          o.loss_row[r] = on ? loss : 0.f;
-          if (o.ent_row != nullptr) o.ent_row[r] = on ? lab.ent : 0.f;
-          o.lse[r] = mt * a.inv_t + ls;
-          if (o.lse_rest != nullptr) o.lse_rest[r] = mo > kNegInf ? mo * a.inv_t + lo : kNegInf;
-        }
+  if ((kMode & kFwd) && blockIdx.x == 0 && tid == 0) *weight_sum = wsum;
+  const float ws = norm != nullptr ? *norm : wsum;
+
+  if (fetcher) {
+    for (uint32_t n = 0;; ++n) {
+      const long long r = live;
+      Label& lab = labels[n & 1];
+      if (n > 0) {
+        named_bar_sync(kBarTaken, threads + 32);
+        if (r < a.N) fetch(r);
       }
       if (lane == 0) {
-        // the greedy token is written by the warp that holds the first of the largest logits outside
-        // the list, or by the first warp when the list holds all of them
-        sums.top = mo == top ? top : __builtin_nanf("");
-        sums.writer = mo == top && top > kNegInf ? first : 0;
-        if (!(top > kNegInf)) c = 0.f;
-        sums.c = c;
-        sums.b = -ls * kLog2e;
-        const float olog = ref_residual(mo, k) + lo * kLog2e;   // factors that the fma form carries
-        const bool any = mo > kNegInf;
-        sums.out_b = any ? ref_offset(mo, k) : 0.f;
-        sums.out_c = any ? c * (So * expf(gap) / S - lab.p0) * ex2(-olog) : 0.f;
-        sums.ref = mt;
+        lab.row = r;
+        if (r < a.N) lab.w = weight != nullptr ? weight[r] : 1.f;
       }
-    } else if (lane == 0) {
-      const float lse = o.lse[r], lse_rest = rest != nullptr ? o.lse_rest[r] : kNegInf;
-      if (!(lse > kNegInf)) c = 0.f;
-      sums.c = c;
-      sums.ref = 0.f;
-      sums.b = lse > kNegInf ? -lse * kLog2e : 0.f;
-      if (rest == nullptr) {
-        sums.out_b = sums.b;
-        sums.out_c = c;
-      } else {
-        const bool any = lse_rest > kNegInf;
-        sums.out_b = any ? -lse_rest * kLog2e : 0.f;
-        sums.out_c = any ? c * (expf(lse_rest - lse) - lab.p0) : 0.f;
+      if (r >= a.N) {
+        __syncwarp();
+        named_bar_arrive(kBarFull, threads + 32);
+        break;
       }
+      const E* z = Z + r * a.ldz;
+      const RowPlace<E, kPacks> at(r * a.ldz, rank, threads);
+      // a first and a last pack that are the row's in part
+      if (lane < 2) {
+        const int pack = lane == 0 ? 0 : (a.V + at.off) / kPerPack<E>;
+        const int v = pack * kPerPack<E> - at.off;
+        const bool part = lane == 0 ? at.off > 0 : v < a.V && (v >= 0 || at.off == 0);
+        if (part && pack >= at.base && pack < at.base + buf.n_packs)
+          buf.data[pack - at.base] = load_pack(z, v, a.V);
+      }
+      uint32_t* listed = reinterpret_cast<uint32_t*>(buf.listed + (n & 1) * buf.n_packs);
+      for (int i = lane; i < buf.n_packs / 4; i += 32) listed[i] = 0;
+      __syncwarp();
+      read_label(z, top_val + r * a.K, top_idx + r * a.K, rest != nullptr ? rest + r : nullptr, a,
+                 (kMode & kFwd) != 0, at.base, buf.n_packs, at.off, listed, lab);
+      live = next_live(r + step);
+      mbar_wait(&full_bar, n & 1, ab);
+      __syncwarp();
+      named_bar_arrive(kBarFull, threads + 32);
     }
-  }
-  if ((kMode & kFwd) && cluster > 1) cluster_arrive();   // no other block's memory is read any more
-  __syncthreads();
-  if constexpr ((kMode & kFwd) != 0) {
-    if (o.argmax != nullptr && rank * n_warps + warp == sums.writer) {
-      const float top = sums.top;
-      int v = 0x7fffffff;
-      float best = top;   // NaN: outside the list there is none
-      if (!(top == top)) {
-        best = kNegInf;
-        for (int i = lane; i < a.K; i += 32)
-          if (lab.idx[i] >= 0) best = fmaxf(best, lab.z[i]);
-        best = warp_reduce(best, MaxOp());
-      } else {
+  } else {
+    const float k = a.inv_t * kLog2e;
+    long long next = first_row;
+    for (uint32_t n = 0;; ++n) {
+      const uint32_t par = n & 1, phase = (n >> 1) & 1;
+      const Label& lab = labels[par];
+      named_bar_sync(kBarFull, threads + 32);
+      const long long r = lab.row;
+      for (; next < r && next < a.N; next += step) {   // rows of weight 0
+        if ((kMode & kFwd) && rank == 0 && tid == 0) {
+          o.loss_row[next] = 0.f;
+          if (o.ent_row != nullptr) o.ent_row[next] = 0.f;
+          o.lse[next] = 0.f;
+          if (o.lse_rest != nullptr) o.lse_rest[next] = 0.f;
+          if (o.argmax != nullptr) o.argmax[next] = -1;
+        }
+        if constexpr ((kMode & kGrad) != 0) {
+          const RowPlace<E, kPacks> to(next * a.ldg, rank, threads);
+#pragma unroll
+          for (int i = 0; i < kPacks; ++i)
+            store_pack(G + next * a.ldg, to.elem(i), a.V, make_uint4(0, 0, 0, 0));
+        }
+      }
+      if (r >= a.N) break;
+      next = r + step;
+      E* g = G + r * a.ldg;
+      RowSums& sums = row_sums[par];
+      const RowPlace<E, kPacks> at(r * a.ldz, rank, threads);
+      const int local = at.pack - at.base;
+      const uint8_t* listed = buf.listed + par * buf.n_packs + local;
+      const bool whole = at.whole(a.V);
+      uint4 raw[kPacks];
+#pragma unroll
+      for (int i = 0; i < kPacks; ++i) {
+        raw[i] = buf.data[local + 32 * i];
+        if (!whole) {
+          const int v = at.elem(i);
+          if (v >= a.V || v + kPerPack<E> <= 0) raw[i] = neg_inf_pack<E>();
+        }
+      }
+      named_bar_arrive(kBarTaken, threads + 32);
+      if constexpr ((kMode & kFwd) != 0) {
+        float m = kNegInf;
+#pragma unroll
+        for (int i = 0; i < kPacks; ++i) {
+          mask_pack<E>(raw[i], listed[32 * i]);   // the listed tokens are handled apart from here on
+#pragma unroll
+          for (int e = 0; e < kPerPack<E>; e += 2)
+            m = max3(m, pack_elem<E>(raw[i], e), pack_elem<E>(raw[i], e + 1));
+        }
+        m = warp_max(m);
+        const float mw = m > kNegInf ? m : 0.f, off = ref_offset(mw, k);
+        const uint64_t off2 = f2_pack(off, off), k2 = f2_pack(k, k);
+        uint64_t s2 = 0;
 #pragma unroll
         for (int i = 0; i < kPacks; ++i)
 #pragma unroll
-          for (int e = 0; e < kPerPack<E>; ++e)
-            if (pack_elem<E>(raw[i], e) == top) v = min(v, at.elem(i) + e);
+          for (int e = 0; e < kPerPack<E>; e += 2) {
+            const uint64_t x = f2_pack(pack_elem<E>(raw[i], e), pack_elem<E>(raw[i], e + 1));
+            s2 = f2_add(s2, f2_ex2(f2_fma(x, k2, off2)));
+          }
+        float sa, sb;
+        f2_unpack(s2, sa, sb);
+        const float sw = warp_reduce(sa + sb, AddOp()) * ex2(-ref_residual(mw, k));
+        if (lane < cluster)   // to every block of the cluster
+          st_async_f2(cluster_smem_addr(&recs[par][rank * n_warps + warp], lane), m, sw,
+                      cluster_smem_addr(&rec_bar[par], lane));
       }
-      for (int i = lane; i < a.K; i += 32)
-        if (lab.idx[i] >= 0 && lab.z[i] == best) v = min(v, lab.idx[i]);
-      v = warp_reduce(v, MinOp());
-      if (lane == 0) o.argmax[r] = best > kNegInf ? v : -1;
+      // The first warp makes the row's sums of the records; what the others wait for comes first.
+      float ls = 0.f, lo = 0.f, gap = 0.f, mt = 0.f;
+      bool any = false, some = false;
+      if (warp == 0) {
+        float c = lab.has && ws > 0.f ? a.lambda * lab.w / ws * a.inv_t : 0.f;
+        if constexpr ((kMode & kFwd) != 0) {
+          const int n_rec = n_warps * cluster;
+          if (lane == 0) mbar_arrive_expect_tx(&rec_bar[par], uint32_t(n_rec) * 8);
+          const float zl = lab.z_max;
+          __syncwarp();
+          mbar_wait_cluster(&rec_bar[par], phase, ab);
+          constexpr int kMost = kRowWarpsMost * kRowClusterMost / 32 + 1;
+          float mo = kNegInf, So = 0.f;
+          float2 t[kMost];
+#pragma unroll
+          for (int j = 0; j < kMost; ++j) {
+            t[j] = make_float2(kNegInf, 0.f);
+            if (j * 32 + lane < n_rec) t[j] = recs[par][j * 32 + lane];
+            mo = fmaxf(mo, t[j].x);
+          }
+          mo = warp_max(mo);
+          int first = 0x7fffffff;
+#pragma unroll
+          for (int j = kMost - 1; j >= 0; --j) {
+            if (!(t[j].x > kNegInf)) continue;
+            So += t[j].y * ex2((t[j].x - mo) * k);
+            if (t[j].x == mo) first = j * 32 + lane;
+          }
+          So = warp_reduce(So, AddOp());
+          first = warp_min(first);   // the warp with the first of the largest, if any
+          any = mo > kNegInf;
+          const float top = fmaxf(mo, zl);
+          some = top > kNegInf;
+          mt = some ? top : 0.f;
+          gap = (mo - mt) * a.inv_t;   // -inf when everything is listed
+          const float So_t = any ? So * expf(gap) : 0.f;
+          const float S = So_t + (zl > kNegInf ? lab.z_sum * expf((zl - mt) * a.inv_t) : 0.f);
+          ls = logf(S);
+          lo = logf(So);
+          if (lane == 0) {
+            if (!some) c = 0.f;
+            sums.c = c;
+            sums.ref = mt;
+            sums.b = -ls * kLog2e;
+            const float carried = ref_residual(mo, k) + lo * kLog2e;   // by the fma form, and R
+            sums.out_b = any ? ref_offset(mo, k) : 0.f;
+            sums.out_c = any ? c * (So_t / S - lab.p0) * ex2(-carried) : 0.f;
+            // the greedy token is written by the warp that holds the first of the largest logits
+            // outside the list, or by the first warp when the list holds all of them
+            sums.top = mo == top && any ? top : __builtin_nanf("");
+            sums.writer = mo == top && any ? first : 0;
+            if (rank == 0) {
+              o.lse[r] = mt * a.inv_t + ls;
+              if (o.lse_rest != nullptr) o.lse_rest[r] = any ? mo * a.inv_t + lo : kNegInf;
+            }
+          }
+        } else if (lane == 0) {
+          const float lse = o.lse[r], lse_rest = rest != nullptr ? o.lse_rest[r] : kNegInf;
+          if (!(lse > kNegInf)) c = 0.f;
+          sums.c = c;
+          sums.ref = 0.f;
+          sums.b = lse > kNegInf ? -lse * kLog2e : 0.f;
+          if (rest == nullptr) {
+            sums.out_b = sums.b;
+            sums.out_c = c;
+          } else {
+            const bool known = lse_rest > kNegInf;
+            sums.out_b = known ? -lse_rest * kLog2e : 0.f;
+            sums.out_c = known ? c * (expf(lse_rest - lse) - lab.p0) : 0.f;
+          }
+        }
+      }
+      named_bar_sync(kBarSums, threads);
+      if constexpr ((kMode & kFwd) != 0) {
+        if (rank == 0 && warp == 0) {
+          float loss = 0.f;
+          for (int i = lane; i < a.K; i += 32)
+            if (lab.p[i] > 0.f) loss += lab.p[i] * (ls + (mt - lab.z[i]) * a.inv_t);
+          loss = warp_reduce(loss, AddOp());
+          if (lab.p0 > 0.f) loss += lab.p0 * (ls - (lo + gap));
+          if (lane == 0) {
+            const bool on = lab.has && some;
+            o.loss_row[r] = on ? loss : 0.f;
+            if (o.ent_row != nullptr) o.ent_row[r] = on ? lab.ent : 0.f;
+          }
+        }
+        if (o.argmax != nullptr && rank * n_warps + warp == sums.writer) {
+          float best = sums.top;   // NaN: no token outside the list has the largest logit
+          int v = 0x7fffffff;
+          if (best == best) {
+#pragma unroll
+            for (int i = 0; i < kPacks; ++i)
+#pragma unroll
+              for (int e = 0; e < kPerPack<E>; ++e)
+                if (pack_elem<E>(raw[i], e) == best) v = min(v, at.elem(i) + e);
+          } else {
+            best = lab.z_max;
+          }
+          for (int i = lane; i < a.K; i += 32)
+            if (lab.idx[i] >= 0 && lab.z[i] == best) v = min(v, lab.idx[i]);
+          v = warp_min(v);
+          if (lane == 0) o.argmax[r] = best > kNegInf ? v : -1;
+        }
+      }
+      if constexpr ((kMode & kGrad) != 0) {
+        const float c = sums.c, out_b = sums.out_b, out_c = sums.out_c;
+        if (c == 0.f) {
+#pragma unroll
+          for (int i = 0; i < kPacks; ++i) raw[i] = neg_inf_pack<E>();
+        }
+        if (int(r * a.ldg % kPerPack<E>) == at.off) {
+          if (whole) {
+            uint4* p = reinterpret_cast<uint4*>(g + at.elem(0));
+#pragma unroll
+            for (int i = 0; i < kPacks; ++i)
+              __stcs(p + 32 * i, grad_pack<E>(raw[i], k, out_b, out_c));
+          } else {
+#pragma unroll
+            for (int i = 0; i < kPacks; ++i)
+              store_pack(g, at.elem(i), a.V, grad_pack<E>(raw[i], k, out_b, out_c));
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kPacks; ++i)
+            store_elems(g, at.elem(i), 0, a.V, grad_pack<E>(raw[i], k, out_b, out_c));
+        }
+        // over them, the listed tokens of this block's range
+        named_bar_sync(kBarWritten, threads);
+        for (int i = tid; i < a.K; i += threads) {
+          const int v = lab.idx[i], pack = (v + at.off) / kPerPack<E> - at.base;
+          if (v >= 0 && pack >= 0 && pack < buf.n_packs)
+            g[v] = E(c != 0.f ? c * (ex2(fmaf(lab.z[i] - sums.ref, k, sums.b)) - lab.p[i]) : 0.f);
+        }
+      }
     }
   }
-  if constexpr ((kMode & kGrad) != 0) {
-    const float c = sums.c, out_b = sums.out_b, out_c = sums.out_c;
-    if (c == 0.f) {
-#pragma unroll
-      for (int i = 0; i < kPacks; ++i) raw[i] = neg_inf_pack<E>();
-    }
-    const bool aligned = int(r * a.ldg % kPerPack<E>) == at.off;
-    if (aligned && at.whole(a.V)) {
-      uint4* p = reinterpret_cast<uint4*>(g + at.elem(0));
-#pragma unroll
-      for (int i = 0; i < kPacks; ++i) {
-        const uint4 x = grad_pack<E>(raw[i], k, out_b, out_c);
-        const uint32_t skip = listed_bytes[32 * i];
-        if (skip == 0)
-          __stcs(p + 32 * i, x);
-        else
-          store_elems(g, at.elem(i), a.V, skip, x);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kPacks; ++i) {
-        const int v = at.elem(i);
-        const uint4 x = grad_pack<E>(raw[i], k, out_b, out_c);
-        const uint32_t skip = listed_bytes[32 * i];
-        if (aligned && skip == 0 && v >= 0 && v + kPerPack<E> <= a.V)
-          __stcs(reinterpret_cast<uint4*>(g + v), x);
-        else
-          store_elems(g, v, a.V, skip, x);
-      }
-    }
-    // the listed tokens of this block's range
-    for (int i = tid; i < a.K; i += blockDim.x) {
-      const int v = lab.idx[i], pack = (v + at.off) / kPerPack<E> - at.base;
-      if (v >= 0 && pack >= 0 && pack < n_packs)
-        g[v] = E(c != 0.f ? c * (ex2(fmaf(lab.z[i] - sums.ref, k, sums.b)) - lab.p[i]) : 0.f);
-    }
-  }
-  if ((kMode & kFwd) && cluster > 1) cluster_wait();   // until no block reads this one's records
-}
-
-// weight_sum = sum of the weights, one block, fixed order.
-__global__ void __launch_bounds__(1024)
-    weight_sum_kernel(const float* weight, long long N, float* weight_sum) {
-  __shared__ double buf[32];
-  pdl_wait_and_release();
-  double s = 0.0;
-  if (weight != nullptr)
-    for (long long r = threadIdx.x; r < N; r += 1024) s += double(weight[r]);
-  s = block_reduce(s, AddOp(), buf);
-  if (threadIdx.x == 0) *weight_sum = weight != nullptr ? float(s) : float(N);
+  if constexpr ((kMode & kFwd) != 0) cluster_sync();   // until no block writes into this one's records
 }
 
 // L = lambda sum w l / sum w, one block, fixed order.
 __global__ void __launch_bounds__(1024)
-    distill_loss_kernel(const float* weight, const float* loss_row, const float* weight_sum,
-                        long long N, float lambda, float* loss_total, float* wl_sum) {
+    distill_loss_kernel(const float* weight, const float* loss_row, float* weight_sum, long long N,
+                        float lambda, float* loss_total, float* wl_sum) {
   __shared__ double buf[32];
   pdl_wait_and_release();
   double s = 0.0;
@@ -393,6 +510,7 @@ __global__ void __launch_bounds__(1024)
     s += double(loss_row[r]) * (weight != nullptr ? double(weight[r]) : 1.0);
   s = block_reduce(s, AddOp(), buf);
   if (threadIdx.x == 0) {
+    if (N == 0) *weight_sum = 0.f;
     const double ws = *weight_sum;
     *loss_total = ws > 0.0 ? float(double(lambda) * s / ws) : 0.f;
     if (wl_sum != nullptr) *wl_sum = float(s);
@@ -402,13 +520,16 @@ __global__ void __launch_bounds__(1024)
 template <typename E, int kPacks>
 cudaError_t launch_rows(const RowShape& shape, const DistillArgs& a, bool fwd, bool grad,
                         const void* Z, const float* top_val, const int32_t* top_idx,
-                        const float* rest, const float* weight, const float* weight_sum,
-                        const DistillRows& o, void* G, cudaStream_t s) {
+                        const float* rest, const float* weight, const float* norm,
+                        const DistillRows& o, float* weight_sum, void* G, int sms, int* status,
+                        cudaStream_t s) {
   auto kern = fwd ? (grad ? distill_row_kernel<E, kPacks, kFwd | kGrad>
                           : distill_row_kernel<E, kPacks, kFwd>)
                   : distill_row_kernel<E, kPacks, kGrad>;
-  return launch_row_clusters(shape, a.N, kern, s, static_cast<const E*>(Z), top_val, top_idx, rest,
-                             weight, weight_sum, a, o, static_cast<E*>(G), shape.cluster);
+  return launch_row_clusters(shape, shape.threads + 32, RowBuffer<E, kPacks>::bytes(shape.threads),
+                             a.N, sms, kern, s, static_cast<const E*>(Z), top_val, top_idx, rest,
+                             weight, norm, a, o, weight_sum, static_cast<E*>(G), shape.cluster,
+                             status);
 }
 
 }  // namespace
@@ -416,23 +537,18 @@ cudaError_t launch_rows(const RowShape& shape, const DistillArgs& a, bool fwd, b
 cudaError_t launch_distill(const DistillArgs& a, bool fwd, bool grad, const void* Z,
                            const float* top_val, const int32_t* top_idx, const float* rest,
                            const float* weight, const float* norm, const DistillRows& o,
-                           const DistillSums& t, void* G, int sms, cudaStream_t s) {
+                           const DistillSums& t, void* G, int sms, int* status, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
-  if (fwd) {
-    e = launch_pdl(weight_sum_kernel, dim3(1), dim3(1024), 0, s, weight, a.N, t.weight_sum);
-    if (e != cudaSuccess) return e;
-    if (norm == nullptr) norm = t.weight_sum;
-  }
   if (a.N > 0) {
     const RowShape shape = row_shape(a.N, a.V, a.dtype == 0 ? 2 : 4, sms);
-    const auto run = [&](auto packs) {
+    e = with_packs(shape.packs, [&](auto packs) {
       constexpr int kP = decltype(packs)::value;
-      return a.dtype == 0 ? launch_rows<__nv_bfloat16, kP>(shape, a, fwd, grad, Z, top_val, top_idx,
-                                                           rest, weight, norm, o, G, s)
-                          : launch_rows<float, kP>(shape, a, fwd, grad, Z, top_val, top_idx, rest,
-                                                   weight, norm, o, G, s);
-    };
-    e = with_packs(shape.packs, run);
+      return a.dtype == 0
+                 ? launch_rows<__nv_bfloat16, kP>(shape, a, fwd, grad, Z, top_val, top_idx, rest,
+                                                  weight, norm, o, t.weight_sum, G, sms, status, s)
+                 : launch_rows<float, kP>(shape, a, fwd, grad, Z, top_val, top_idx, rest, weight,
+                                          norm, o, t.weight_sum, G, sms, status, s);
+    });
     if (e != cudaSuccess) return e;
   }
   if (fwd)

@@ -245,7 +245,7 @@ struct DistillSums {
 cudaError_t launch_distill(const DistillArgs& a, bool fwd, bool grad, const void* Z,
                            const float* top_val, const int32_t* top_idx, const float* rest,
                            const float* weight, const float* norm, const DistillRows& o,
-                           const DistillSums& t, void* G, int sms, cudaStream_t s);
+                           const DistillSums& t, void* G, int sms, int* status, cudaStream_t s);
 
 // Top logits and sampling (sample_kernels.cu).
 constexpr int kTopMost = 256;        // ALR_TOP_MAX

@@ -3,12 +3,14 @@
 // A row (up to 1 MB) is read from memory once and stays on chip for all that an operator does with it:
 // C blocks of T threads hold kPacks 16-byte packs each.  Warps own consecutive stretches of the
 // row, in the order (block, warp, pack, lane), so that "first" and "running sum" follow from records per
-// warp, and every warp-wide load is 512 consecutive bytes.
+// warp, and every warp-wide access is 512 consecutive bytes.
 //
 // Rows need not be 16-byte aligned: packs are counted from the 16-byte boundary at or below the row's
 // first element, and the elements of the first and the last pack that are not the row's read as -inf.
 #pragma once
 
+#include <algorithm>
+#include <mutex>
 #include <type_traits>
 
 #include "launch.h"
@@ -16,7 +18,7 @@
 
 namespace alr {
 
-constexpr int kRowThreadsMost = 512;
+constexpr int kRowThreadsMost = 480;   // and a warp that fetches: 512, two blocks of 64 registers an SM
 constexpr int kRowWarpsMost = kRowThreadsMost / 32;
 constexpr int kRowClusterMost = 8;
 
@@ -28,9 +30,9 @@ struct RowShape {
 constexpr int kRowPackChoices[] = {2, 5, 10, 18};
 
 // Few rows: as many blocks as give every SM one, and few packs a thread (the row's latency is what
-// counts).  Many rows: the fewest blocks that hold the row at 10 packs a thread, 2 to 4 blocks of 512
-// threads at most to an SM, whose loads overlap the others' arithmetic.  18 packs a thread are for
-// fp32 rows of more than 160 K tokens, which 8 blocks of 512 threads hold no other way.
+// counts).  Many rows: the fewest blocks that hold the row at 10 packs a thread, so that two blocks or
+// more share an SM and one's transfers overlap the other's arithmetic.  18 packs a thread are for
+// fp32 rows of more than 150 K tokens, which 8 blocks hold no other way.
 inline RowShape row_shape(long long N, int V, int elem_bytes, int sms) {
   const int per = 16 / elem_bytes;
   const int need = (V + per - 1) / per + 1;   // one more for a row that starts inside a pack
@@ -50,9 +52,35 @@ inline RowShape row_shape(long long N, int V, int elem_bytes, int sms) {
       }
   }
   const int t = (need + s.cluster * s.packs - 1) / (s.cluster * s.packs);
-  s.threads = (t + 31) / 32 * 32;
-  if (s.threads < 64) s.threads = 64;
+  s.threads = std::max(64, (t + 31) / 32 * 32);
   return s;
+}
+
+// Clusters of a kernel that the device holds at once (0: none); asked for once per kernel and shape.
+inline int resident_clusters(const void* kern, const cudaLaunchConfig_t& cfg, int cluster) {
+  struct Known {
+    const void* kern;
+    int dev, threads, cluster;
+    size_t smem;
+    int n;
+  };
+  static Known table[256];
+  static int used = 0;
+  static std::mutex mu;
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  const int threads = int(cfg.blockDim.x);
+  const std::lock_guard<std::mutex> lock(mu);
+  for (int i = 0; i < used; ++i)
+    if (table[i].kern == kern && table[i].dev == dev && table[i].threads == threads &&
+        table[i].cluster == cluster && table[i].smem == cfg.dynamicSmemBytes)
+      return table[i].n;
+  if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();   // a shape the device cannot place: not an error of the call
+    n = 0;
+  }
+  if (used < 256) table[used++] = {kern, dev, threads, cluster, cfg.dynamicSmemBytes, n};
+  return n;
 }
 
 // Calls f(std::integral_constant<int, packs>).
@@ -66,20 +94,30 @@ cudaError_t with_packs(int packs, F f) {
   }
 }
 
-// N rows, a cluster (or, of one, a block) each.
+// Launches clusters that take the N rows in turn: as many as there are rows, or as the device holds.
 template <typename... KArgs, typename... Args>
-cudaError_t launch_row_clusters(const RowShape& shape, long long N, void (*kern)(KArgs...),
-                                cudaStream_t s, const Args&... args) {
+cudaError_t launch_row_clusters(const RowShape& shape, int threads, size_t smem, long long N, int sms,
+                                void (*kern)(KArgs...), cudaStream_t s, const Args&... args) {
+  cudaError_t e =
+      cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+  if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[2] = {pdl_attribute(), {}};
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = unsigned(shape.cluster);
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(unsigned(N * shape.cluster));
-  cfg.blockDim = dim3(unsigned(shape.threads));
+  cfg.gridDim = dim3(unsigned(shape.cluster));
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cfg.attrs = attr;
-  cfg.numAttrs = shape.cluster > 1 ? 2 : 1;
+  cfg.numAttrs = 2;
+  long long clusters = N;
+  if (N * shape.cluster > sms) {
+    const int most = resident_clusters(reinterpret_cast<const void*>(kern), cfg, shape.cluster);
+    if (most > 0) clusters = std::min<long long>(N, most);
+  }
+  cfg.gridDim = dim3(unsigned(std::min<long long>(clusters, 1 << 20) * shape.cluster));
   return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
@@ -92,9 +130,9 @@ struct RowPlace {
   int off;    // elements of the first pack that lie before the row
   int pack;   // this lane's pack 0; pack i is 32 i further
   int base;   // the block's first pack
-  ALR_DEV RowPlace(long long row_start, int rank) {
+  ALR_DEV RowPlace(long long row_start, int rank, int threads) {
     off = int(row_start % kPerPack<E>);
-    base = rank * int(blockDim.x) * kPacks;
+    base = rank * threads * kPacks;
     pack = base + (int(threadIdx.x) / 32) * 32 * kPacks + (int(threadIdx.x) & 31);
   }
   // First element of pack i (may be negative or past the row).
@@ -135,19 +173,6 @@ ALR_DEV uint4 load_pack(const E* row, int v, int V) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The thread's packs of a row.
-template <typename E, int kPacks>
-ALR_DEV void load_row(uint4 (&raw)[kPacks], const E* row, const RowPlace<E, kPacks>& at, int V) {
-  if (at.whole(V)) {
-    const uint4* p = reinterpret_cast<const uint4*>(row + at.elem(0));
-#pragma unroll
-    for (int i = 0; i < kPacks; ++i) raw[i] = __ldcs(p + 32 * i);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kPacks; ++i) raw[i] = load_pack(row, at.elem(i), V);
-  }
-}
-
 // Element e of a pack (e known when unrolled).
 template <typename E>
 ALR_DEV float pack_elem(const uint4& r, int e) {
@@ -175,17 +200,50 @@ ALR_DEV void mask_pack(uint4& r, uint32_t bits) {
   }
 }
 
-// Records of the cluster's warps, written by each into its own block's shared memory; after a
-// cluster_sync (one block: __syncthreads) any thread reads record i of the n = C * warps, in the
-// order of the row.
-ALR_DEV float2 ld_cluster_f2(uint32_t addr) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-  return v;
+// A pair of floats into another block's (or this one's) shared memory, counted by the mbarrier there.
+ALR_DEV void st_async_f2(uint32_t cluster_addr, float x, float y, uint32_t cluster_mbar) {
+  asm volatile(
+      "st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(
+          cluster_addr),
+      "r"(__float_as_uint(x)), "r"(__float_as_uint(y)), "r"(cluster_mbar)
+      : "memory");
 }
-ALR_DEV void cluster_arrive() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+
+// mbar_wait for a phase that other blocks of the cluster complete.
+ALR_DEV bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, const AbortFlag& ab) {
+  const uint64_t t0 = global_timer_ns();
+  for (uint32_t i = 1;; ++i) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendHintNs)
+        : "memory");
+    if (done) return true;
+    if (i % kWaitCheckEvery == 0) {
+      if (*ab.smem) return false;
+      if (global_timer_ns() - t0 > kWaitLimitNs) {
+        *ab.smem = 1;
+        atomicExch(ab.status, kStatusTimeout);
+        return false;
+      }
+    }
+  }
 }
-ALR_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// Consecutive bytes of global memory into shared memory (all 16-byte multiples).
+ALR_DEV void bulk_load(uint32_t smem, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+          smem),
+      "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
+      : "memory");
+}
+
+ALR_DEV void named_bar_arrive(int id, int nthreads) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
+}
 
 }  // namespace alr

@@ -33,6 +33,14 @@ ALR_DEV T warp_reduce(T v, Op op) {
   return v;
 }
 
+// Largest float of the warp, in one instruction (NaN is not passed).
+ALR_DEV float warp_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+ALR_DEV int warp_min(int v) { return __reduce_min_sync(0xffffffffu, v); }
+
 // op over the values of all threads of the block (a multiple of 32, at most 1024), in a fixed
 // order; every thread gets the result.  `buf`: 32 entries of shared memory, free again on return.
 template <typename T, typename Op>

@@ -81,6 +81,9 @@ def test_refusals(lib):
         (lambda: bwd(params(ldg=99)), I, "ldg = 99"), (lambda: bwd(params(), G=None), I, "G must be"),
         (lambda: bwd(params(), G=MIS), I, "aligned"), (lambda: bwd(params(), lse=None), I, "lse"),
         (lambda: bwd(params(), rest=A16), I, "lse_rest"),
+        (lambda: lib.alr_distill_fwd_bwd(ctypes.byref(params()), A16, A16, A16, None, None,
+                                         ctypes.c_void_p(0x20000), ctypes.byref(outs()), A16, None), I,
+         "batch_weight_sum"),
         (lambda: both(params(ldz=120)), I, "ldg = ldz"), (lambda: both(params(), Z=MIS), I, "aligned"),
         (lambda: embed(dt=3), U, "dtype 3"), (lambda: embed(V=0), I, "V=0"), (lambda: embed(d=0), I, "d=0"),
         (lambda: embed(N=-2), I, "N = -2"), (lambda: embed(tok=None), I, "tokens"),
