@@ -1497,7 +1497,7 @@ int alr_top_logits(const void* Z, int32_t dtype, int64_t N, int32_t V, int64_t l
   DevInfo info;
   if ((rc = require_sm103(&info)) != ALR_OK) return rc;
   const cudaError_t e = alr::launch_top_logits(dtype == ALR_BF16 ? 0 : 1, Z, N, V, ldz, K,
-                                               1.f / temperature, top_val, top_idx, lse, lse_rest,
+                                               1.f / temperature, top_val, top_idx, lse, lse_rest, info.sms,
                                                static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? ALR_OK : cuda_fail(e, "top logits launch");
 }
@@ -1562,7 +1562,7 @@ int alr_sample_tokens(const void* Z, int32_t dtype, int64_t N, int32_t V, int64_
   if ((rc = require_sm103(&info)) != ALR_OK) return rc;
   const cudaError_t e = alr::launch_sample(dtype == ALR_BF16 ? 0 : 1, Z, N, V, ldz,
                                            {u, temperature, top_k, top_p, min_p}, token, prob,
-                                           n_kept, static_cast<cudaStream_t>(stream));
+                                           n_kept, info.sms, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? ALR_OK : cuda_fail(e, "sampling launch");
 }
 

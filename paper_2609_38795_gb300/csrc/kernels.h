@@ -251,7 +251,7 @@ cudaError_t launch_distill(const DistillArgs& a, bool fwd, bool grad, const void
 constexpr int kTopMost = 256;        // ALR_TOP_MAX
 cudaError_t launch_top_logits(int dtype, const void* Z, long long N, int V, long long ldz, int K,
                               float inv_t, float* top_val, int32_t* top_idx, float* lse,
-                              float* lse_rest, cudaStream_t s);
+                              float* lse_rest, int sms, cudaStream_t s);
 struct SampleArgs {
   const uint32_t* u;
   const float* temperature;   // each of these may be nullptr
@@ -260,7 +260,7 @@ struct SampleArgs {
   const float* min_p;
 };
 cudaError_t launch_sample(int dtype, const void* Z, long long N, int V, long long ldz,
-                          const SampleArgs& a, int32_t* token, float* prob, int32_t* n_kept,
+                          const SampleArgs& a, int32_t* token, float* prob, int32_t* n_kept, int sms,
                           cudaStream_t s);
 
 // Embedding lookup and the gradient of the table (embed_kernels.cu).

@@ -33,7 +33,8 @@ constexpr int kRowPackChoices[] = {2, 5, 10, 18};
 // counts).  Many rows: the fewest blocks that hold the row at 10 packs a thread, so that two blocks or
 // more share an SM and one's transfers overlap the other's arithmetic.  18 packs a thread are for
 // fp32 rows of more than 150 K tokens, which 8 blocks hold no other way.
-inline RowShape row_shape(long long N, int V, int elem_bytes, int sms) {
+// `least`: threads that a block should have if the row is long enough.
+inline RowShape row_shape(long long N, int V, int elem_bytes, int sms, int least = 64) {
   const int per = 16 / elem_bytes;
   const int need = (V + per - 1) / per + 1;   // one more for a row that starts inside a pack
   const auto fits = [need](int c, int packs) {
@@ -51,7 +52,10 @@ inline RowShape row_shape(long long N, int V, int elem_bytes, int sms) {
         break;
       }
   }
-  const int t = (need + s.cluster * s.packs - 1) / (s.cluster * s.packs);
+  const auto threads = [&] { return (need + s.cluster * s.packs - 1) / (s.cluster * s.packs); };
+  for (int p : {5, 2})
+    if (s.packs > p && threads() < least && fits(s.cluster, p)) s.packs = p;
+  const int t = threads();
   s.threads = std::max(64, (t + 31) / 32 * 32);
   return s;
 }
@@ -92,6 +96,23 @@ cudaError_t with_packs(int packs, F f) {
     case 10: return f(std::integral_constant<int, 10>{});
     default: return f(std::integral_constant<int, 18>{});
   }
+}
+
+// Launches a cluster for each row.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_row_each(const RowShape& shape, long long N, void (*kern)(KArgs...),
+                            cudaStream_t s, const Args&... args) {
+  cudaLaunchAttribute attr[2] = {pdl_attribute(), {}};
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(shape.cluster);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(N * shape.cluster));
+  cfg.blockDim = dim3(unsigned(shape.threads));
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
 // Launches clusters that take the N rows in turn: as many as there are rows, or as the device holds.
@@ -241,6 +262,12 @@ ALR_DEV void bulk_load(uint32_t smem, const void* src, uint32_t bytes, uint64_t*
       "l"(__cvta_generic_to_global(src)), "r"(bytes), "r"(smem_u32(bar))
       : "memory");
 }
+
+// The two halves of cluster_sync.
+ALR_DEV void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+ALR_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 ALR_DEV void named_bar_arrive(int id, int nthreads) {
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(nthreads) : "memory");

@@ -1,16 +1,34 @@
 // A teacher's top logits, and the next token of a rollout drawn from given random numbers.
 //
 // Both pick from a row by the order (value descending, token id ascending).  A logit that is -inf or
-// NaN is no candidate.  Selection is a radix select over the 8-bit digits of an order-preserving
-// 32-bit key; equal values at the threshold go to the lowest ids.
+// NaN is no candidate.  A row lies in the registers of a cluster (row_cluster.cuh), read once.
+//
+// Few tokens of many (top logits, top-k, most nuclei): the K-th largest of the largest logits that the
+// threads hold is a lower bound of the row's K-th largest, and next to no more than K logits reach it.
+// Those go to the cluster's first block, which sorts them and does the rest.
+// Many tokens (a flat nucleus, a top-k past kTopMost), or so many equal ones that they would not fit:
+// a radix select over an order-preserving key, with a histogram of counts or weights per digit in
+// each block's shared memory, added up over the cluster.
 #include "kernels.h"
 #include "launch.h"
-#include "row_reduce.cuh"
+#include "row_cluster.cuh"
 
 namespace alr {
 namespace {
 
-constexpr int kRowThreads = 512;
+constexpr int kBins = 2048;              // 11 bits of the key
+constexpr int kCandBlock = 1024;         // candidates that a block collects at most
+constexpr int kCandAll = 2048;           // and a cluster
+constexpr int kCandSort = 256;           // up to here an entry's place is counted, beyond they are sorted
+constexpr int kListMost = 2 * kTopMost + 3 * kRowWarpsMost * kRowClusterMost;
+constexpr int kWarpsMost = kRowWarpsMost * kRowClusterMost;
+
+// An entry: larger is earlier in the order.
+ALR_DEV unsigned long long entry(uint32_t key, int v) {
+  return ((unsigned long long)key << 32) | uint32_t(~v);
+}
+ALR_DEV uint32_t entry_key(unsigned long long e) { return uint32_t(e >> 32); }
+ALR_DEV int entry_id(unsigned long long e) { return int(~uint32_t(e)); }
 
 // What a row keeps: keys above `key`, and of the tokens with that key those up to id `last`.
 struct Cut {
@@ -19,172 +37,518 @@ struct Cut {
   ALR_DEV bool keeps(uint32_t k, int v) const { return k > key || (k == key && v <= last); }
 };
 
-struct SelectShared {
-  unsigned long long hist[256];
-  unsigned long long scan[256];
-  uint32_t prefix;
-  unsigned long long above;
-  int count[32];
-  int found;
-  float buf[32];
+struct Shared {
+  union {
+    struct {
+      unsigned long long all[kCandAll];   // first block: the cluster's candidates, sorted
+      float list[kListMost];              // largest logits of the warps' threads
+    } few;
+    struct {
+      uint32_t lo[kBins], hi[kBins];      // histogram: sums of the low 16 bits, of the others
+      unsigned long long total[kBins];    // over the cluster
+    } many;
+  };
+  unsigned long long cand[kCandBlock];
+  unsigned long long rec[kWarpsMost];     // of each warp of the cluster: a sum
+  float2 frec[kWarpsMost];
+  float fbuf[32];                         // and the bound's result
   unsigned long long lbuf[32];
   int ibuf[32];
+  int n_cand, n_block[kRowClusterMost];
+  float bound;
+  uint32_t digit;
+  unsigned long long above, found, kept;
+  int flag;
 };
 
-// The token with the n-th lowest id (n >= 1) among those with `key` that `cut` keeps.
-template <typename E>
-ALR_DEV int nth_equal(const E* z, int V, const Cut& cut, uint32_t key, long long n,
-                      SelectShared& sh) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, n_warps = blockDim.x / 32;
-  if (threadIdx.x == 0) sh.found = V - 1;
-  long long before = 0;
-  __syncthreads();
-  for (int base = 0; base < V; base += blockDim.x) {
-    const int v = base + threadIdx.x;
-    bool is = false;
-    if (v < V) {
-      const float x = to_float(z[v]);
-      is = x > kNegInf && order_key(x) == key && cut.keeps(key, v);
-    }
-    const unsigned ball = __ballot_sync(0xffffffffu, is);
-    if (lane == 0) sh.count[warp] = __popc(ball);
-    __syncthreads();
-    long long mine = before, all = 0;
-    for (int w = 0; w < n_warps; ++w) {
-      if (w < warp) mine += sh.count[w];
-      all += sh.count[w];
-    }
-    mine += __popc(ball & ((2u << lane) - 1u));
-    if (is && mine == n) sh.found = v;
-    before += all;
-    __syncthreads();
-    if (before >= n) break;
-  }
-  return sh.found;
+ALR_DEV float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
-// The key at which the summed weights of the kept tokens, from the largest key down, first reach
-// more than... `need(above)` says whether a sum `above` of all larger keys still lacks something.
-// weight(x): whole weight of a token.  Returns the key; `above` gets the sum over larger keys.
-template <typename E, typename W, typename Need>
-ALR_DEV uint32_t select_key(const E* z, int V, const Cut& cut, W weight, Need need,
-                            unsigned long long& above_out, SelectShared& sh) {
-  uint32_t prefix = 0;
-  unsigned long long above = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += blockDim.x) sh.hist[i] = 0;
-    __syncthreads();
-    for (int v = threadIdx.x; v < V; v += blockDim.x) {
-      const float x = to_float(z[v]);
-      if (!(x > kNegInf)) continue;
-      const uint32_t k = order_key(x);
-      if (!cut.keeps(k, v)) continue;
-      if (shift < 24 && (k >> (shift + 8)) != (prefix >> (shift + 8))) continue;
-      atomicAdd(&sh.hist[(k >> shift) & 255], weight(x));
+// The row of a cluster in registers, and what all its threads need to know.
+template <typename E, int kPacks>
+struct Row {
+  uint4 raw[kPacks];
+  RowPlace<E, kPacks> at;
+  int V, rank, cluster, warp, lane, n_warps;
+  Shared& sh;
+
+  ALR_DEV Row(const E* z, long long start, int V_, int cluster_, Shared& s)
+      : at(start, int(cluster_ctarank()), int(blockDim.x)),
+        V(V_),
+        rank(int(cluster_ctarank())),
+        cluster(cluster_),
+        warp(int(threadIdx.x) / 32),
+        lane(int(threadIdx.x) & 31),
+        n_warps(int(blockDim.x) / 32),
+        sh(s) {
+    if (at.whole(V)) {
+      const uint4* p = reinterpret_cast<const uint4*>(z + at.elem(0));
+#pragma unroll
+      for (int i = 0; i < kPacks; ++i) raw[i] = __ldcs(p + 32 * i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPacks; ++i) raw[i] = load_pack(z, at.elem(i), V);
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      int d = 255;
-      for (; d > 0; --d) {   // the digit whose bin the need ends in
-        if (sh.hist[d] != 0 && !need(above + sh.hist[d])) break;
-        above += sh.hist[d];
+    cluster_arrive();   // row_bound waits: the other blocks run, their shared memory is there
+  }
+  ALR_DEV float x(int i, int e) const { return pack_elem<E>(raw[i], e); }
+  ALR_DEV int id(int i, int e) const { return at.elem(i) + e; }
+  ALR_DEV int record() const { return rank * n_warps + warp; }
+  ALR_DEV int records() const { return cluster * n_warps; }
+
+  // Largest element of a pack; NaN elements become -inf first.
+  ALR_DEV float pack_max(int i) {
+    float m = kNegInf;
+#pragma unroll
+    for (int e = 0; e < kPerPack<E>; e += 2) m = max3_nan(m, x(i, e), x(i, e + 1));
+    if (m != m) {
+      uint32_t bits = 0;
+      m = kNegInf;
+#pragma unroll
+      for (int e = 0; e < kPerPack<E>; ++e) {
+        bits |= uint32_t(x(i, e) != x(i, e)) << e;
+        m = fmaxf(m, x(i, e));
       }
-      sh.prefix = prefix | (uint32_t(d) << shift);
-      sh.above = above;
+      mask_pack<E>(raw[i], bits);
+    }
+    return m;
+  }
+
+  // Value `v` of a warp-uniform kind into slot `at` of every block's array.
+  template <typename T>
+  ALR_DEV void to_all(T* slot, T v) const {
+    if (lane < cluster) {
+      const uint32_t a = cluster_smem_addr(slot, lane);
+      if constexpr (sizeof(T) == 8) {
+        unsigned long long b;
+        memcpy(&b, &v, 8);
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(b) : "memory");
+      } else {
+        uint32_t b;
+        memcpy(&b, &v, 4);
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(b) : "memory");
+      }
+    }
+  }
+};
+
+// The n-th (from 1) unit of weight f(x, id) >= 0, counted in the order of ids over the whole row: the
+// id of the token that holds it, that token's weight and the sum of all weights.  n(total) gives n.
+struct Found {
+  int id;
+  unsigned long long weight, total;
+};
+template <typename E, int kPacks, typename F, typename N>
+ALR_DEV Found find_unit(Row<E, kPacks>& row, F f, N nth) {
+  Shared& sh = row.sh;
+  unsigned long long s = 0;
+#pragma unroll
+  for (int i = 0; i < kPacks; ++i)
+#pragma unroll
+    for (int e = 0; e < kPerPack<E>; ++e) s += f(row.x(i, e), row.id(i, e));
+  s = warp_reduce(s, AddOp());
+  row.to_all(&sh.rec[row.record()], s);
+  cluster_sync();
+  unsigned long long total = 0, before = 0;
+  for (int i = row.lane; i < row.records(); i += 32) {
+    const unsigned long long t = sh.rec[i];
+    total += t;
+    if (i < row.record()) before += t;
+  }
+  total = warp_reduce(total, AddOp());
+  before = warp_reduce(before, AddOp());
+  const unsigned long long n = nth(total);
+  if (before < n && n <= before + s) {   // this warp holds it
+    bool done = false;
+#pragma unroll 1
+    for (int i = 0; i < kPacks && !done; ++i) {
+      uint4 r = row.raw[0];
+#pragma unroll
+      for (int j = 1; j < kPacks; ++j)
+        if (j == i) r = row.raw[j];
+      unsigned long long mine = 0;
+#pragma unroll
+      for (int e = 0; e < kPerPack<E>; ++e) mine += f(pack_elem<E>(r, e), row.id(i, e));
+      unsigned long long incl = mine;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
+        if (row.lane >= off) incl += t;
+      }
+      const unsigned long long all = __shfl_sync(0xffffffffu, incl, 31);
+      if (n <= before + all) {
+        unsigned long long run = before + incl - mine, w = 0;
+        int id = -1;
+#pragma unroll
+        for (int e = 0; e < kPerPack<E>; ++e) {
+          const unsigned long long t = f(pack_elem<E>(r, e), row.id(i, e));
+          if (id < 0 && run < n && n <= run + t) {
+            id = row.id(i, e);
+            w = t;
+          }
+          run += t;
+        }
+        const unsigned got = __ballot_sync(0xffffffffu, id >= 0);
+        const int src = __ffs(got) - 1;
+        id = __shfl_sync(0xffffffffu, id, src & 31);
+        w = __shfl_sync(0xffffffffu, w, src & 31);
+        row.to_all(&sh.found, (unsigned long long)uint32_t(id));
+        row.to_all(&sh.kept, w);
+        done = true;
+      }
+      before += all;
+    }
+  }
+  cluster_sync();
+  const Found r{int(uint32_t(sh.found)), sh.kept, total};
+  cluster_sync();   // before `found` and `rec` are written again
+  return r;
+}
+
+// Radix select among the tokens that `cut` keeps: the largest key at which the summed weights, from
+// the largest key down, no longer satisfy need(sum); need(0) may be false (then the first key).
+// weight: up to 2^31.  need.set() gets the sum of all weights before the first choice.
+struct Selected {
+  uint32_t key;
+  unsigned long long above, total;   // sums over larger keys, over all
+};
+template <typename E, int kPacks, typename W, typename Need>
+ALR_DEV Selected select_key(Row<E, kPacks>& row, const Cut& cut, W weight, Need need) {
+  Shared& sh = row.sh;
+  // a bf16 key is in the upper 16 bits, the low ones follow from the sign
+  constexpr int kLevels = sizeof(E) == 2 ? 2 : 3;
+  constexpr int kShift[3] = {21, sizeof(E) == 2 ? 16 : 10, 0};
+  uint32_t prefix = 0;
+  unsigned long long above = 0, total = 0;
+  const int tid = threadIdx.x, threads = blockDim.x;
+  for (int level = 0; level < kLevels; ++level) {
+    const int shift = kShift[level], up = level == 0 ? 32 : kShift[level - 1];
+    const uint32_t mask = (1u << (up - shift)) - 1u;
+    const int bins = int(mask) + 1;
+    for (int b = tid; b < bins; b += threads) sh.many.lo[b] = sh.many.hi[b] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i)
+#pragma unroll
+      for (int e = 0; e < kPerPack<E>; ++e) {
+        const float x = row.x(i, e);
+        if (!(x > kNegInf)) continue;
+        const uint32_t k = order_key(x);
+        if (level > 0 && (k ^ prefix) >> up != 0) continue;
+        if (!cut.keeps(k, row.id(i, e))) continue;
+        const uint32_t w = weight(x), b = (k >> shift) & mask;
+        if (w & 0xffffu) atomicAdd(&sh.many.lo[b], w & 0xffffu);
+        if (w >> 16) atomicAdd(&sh.many.hi[b], w >> 16);
+      }
+    cluster_sync();
+    // a share of the bins each: their sums over the cluster, to all blocks
+    const int share = (bins + row.cluster - 1) / row.cluster;
+    for (int b = row.rank * share + tid; b < min(bins, (row.rank + 1) * share); b += threads) {
+      unsigned long long t = 0;
+      for (int c = 0; c < row.cluster; ++c) {
+        t += uint32_t(ld_cluster_s32(cluster_smem_addr(&sh.many.lo[b], c)));
+        t += (unsigned long long)uint32_t(ld_cluster_s32(cluster_smem_addr(&sh.many.hi[b], c))) << 16;
+      }
+      for (int c = 0; c < row.cluster; ++c)
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_smem_addr(&sh.many.total[b], c)),
+                     "l"(t)
+                     : "memory");
+    }
+    cluster_sync();
+    // from the largest bin down: thread t takes the bins [bins - 1 - t n, ...) downwards
+    const int n = (bins + threads - 1) / threads;
+    unsigned long long mine = 0;
+    for (int j = 0; j < n; ++j) {
+      const int b = bins - 1 - (tid * n + j);
+      if (b >= 0) mine += sh.many.total[b];
+    }
+    unsigned long long incl = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
+      if (row.lane >= off) incl += t;
+    }
+    if (row.lane == 31) sh.lbuf[row.warp] = incl;
+    __syncthreads();
+    unsigned long long run = above + incl - mine, all = 0;
+    for (int w = 0; w < row.n_warps; ++w) {
+      if (w < row.warp) run += sh.lbuf[w];
+      all += sh.lbuf[w];
+    }
+    if (level == 0) {
+      total = all;
+      need.set(all);
+    }
+    for (int j = 0; j < n; ++j) {
+      const int b = bins - 1 - (tid * n + j);
+      if (b < 0) break;
+      const unsigned long long t = sh.many.total[b];
+      if (t != 0 && (run == above ? (above == 0 || need(run)) : need(run)) && !need(run + t)) {
+        sh.digit = uint32_t(b);
+        sh.above = run;
+      }
+      run += t;
     }
     __syncthreads();
-    prefix = sh.prefix;
+    prefix |= sh.digit << shift;
     above = sh.above;
     __syncthreads();
   }
-  above_out = above;
-  return prefix;
+  if (sizeof(E) == 2 && !(prefix >> 31)) prefix |= 0xffffu;   // negative: the low bits are inverted
+  return {prefix, above, total};
 }
 
-// The cut that keeps the k first tokens (k >= 1) of the row.
-template <typename E>
-ALR_DEV Cut cut_top_k(const E* z, int V, long long k, SelectShared& sh) {
+// The last id kept of the tokens with `key` that `cut` keeps, n (>= 1) of them.
+template <typename E, int kPacks>
+ALR_DEV int nth_equal(Row<E, kPacks>& row, const Cut& cut, uint32_t key, unsigned long long n) {
+  const Found f = find_unit(
+      row,
+      [&](float x, int v) -> unsigned long long {
+        return x > kNegInf && order_key(x) == key && cut.keeps(key, v);
+      },
+      [n](unsigned long long total) { return n < total ? n : total; });
+  return f.id;
+}
+
+struct NeedCount {
+  unsigned long long k;
+  ALR_DEV void set(unsigned long long) {}
+  ALR_DEV bool operator()(unsigned long long got) const { return got < k; }
+};
+struct NeedMass {
+  double p, lim;
+  ALR_DEV void set(unsigned long long total) { lim = p * double(total); }
+  ALR_DEV bool operator()(unsigned long long got) const { return double(got) < lim; }
+};
+
+// The cut that keeps the k first candidates of the row, which has more.
+template <typename E, int kPacks>
+ALR_DEV Cut cut_top_k(Row<E, kPacks>& row, int k) {
   const Cut all{0u, 0x7fffffff};
-  unsigned long long above;
-  const uint32_t key = select_key(
-      z, V, all, [](float) { return 1ull; },
-      [k](unsigned long long got) { return got < (unsigned long long)k; }, above, sh);
-  return {key, nth_equal(z, V, all, key, k - (long long)above, sh)};
+  NeedCount need{(unsigned long long)k};
+  const Selected s = select_key(row, all, [](float) { return 1u; }, need);
+  return {s.key, nth_equal(row, all, s.key, k - s.above)};
+}
+
+// A lower bound of the row's K-th largest logit that few more reach (-inf when the threads hold too few),
+// and the largest logit.  All blocks get both.
+struct Bound {
+  float least, top;
+};
+template <typename E, int kPacks>
+ALR_DEV Bound row_bound(Row<E, kPacks>& row, int K) {
+  Shared& sh = row.sh;
+  float t = kNegInf;
+#pragma unroll
+  for (int i = 0; i < kPacks; ++i) t = fmaxf(t, row.pack_max(i));
+  // the `per` largest of the warp's 32, into all blocks' lists
+  const int n_rec = row.records();
+  const int per = K > 1 ? min(32, 2 * ((K + n_rec - 1) / n_rec) + 1) : 1;
+  cluster_wait();
+  for (int j = 0; j < per; ++j) {
+    const float m = warp_max(t);
+    row.to_all(&sh.few.list[row.record() * per + j], m);
+    const unsigned who = __ballot_sync(0xffffffffu, t == m);
+    if (row.lane == __ffs(who) - 1) t = kNegInf;
+  }
+  if (threadIdx.x == 0) sh.n_cand = 0;
+  cluster_sync();
+  if (row.warp == 0) {
+    // The list's K-th largest by bisection of the keys' upper half: the largest prefix that K reach.
+    constexpr int kMost = (kListMost + 31) / 32;
+    const int n = n_rec * per;
+    uint32_t key[kMost];
+    float top = kNegInf;
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+      key[j] = 0;
+      if (j * 32 >= n) continue;
+      const int i = j * 32 + row.lane;
+      const float v = i < n ? sh.few.list[i] : kNegInf;
+      if (v > kNegInf) key[j] = order_key(v) >> 16;
+      top = fmaxf(top, v);
+    }
+    top = warp_max(top);
+    uint32_t least = 0;
+    if (K > 0)
+      for (uint32_t bit = 0x8000u; bit != 0; bit >>= 1) {
+        int reach = 0;
+#pragma unroll
+        for (int j = 0; j < kMost; ++j)
+          if (j * 32 < n) reach += key[j] >= (least | bit);
+        if (__reduce_add_sync(0xffffffffu, reach) >= K) least |= bit;
+      }
+    if (row.lane == 0) {
+      sh.bound = least != 0 ? key_value(least << 16) : kNegInf;
+      sh.fbuf[0] = top;
+    }
+  }
+  __syncthreads();
+  return {sh.bound, sh.fbuf[0]};
+}
+
+// Element e of a pack, e not known to the compiler.
+template <typename E>
+ALR_DEV float pack_elem_at(const uint4& r, int e) {
+  const int word = sizeof(E) == 2 ? e >> 1 : e;
+  const uint32_t w = word == 0 ? r.x : word == 1 ? r.y : word == 2 ? r.z : r.w;
+  return __uint_as_float(sizeof(E) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16);
+}
+
+// Collects the entries that take(x, id) wants, of those that reach `least`, in the blocks' lists, and says
+// how many the cluster has; -1: more than fit.
+template <typename E, int kPacks, typename F>
+ALR_DEV int collect(Row<E, kPacks>& row, float least, F take) {
+  Shared& sh = row.sh;
+#pragma unroll
+  for (int i = 0; i < kPacks; ++i) {
+    float m = kNegInf;
+#pragma unroll
+    for (int e = 0; e < kPerPack<E>; e += 2) m = max3(m, row.x(i, e), row.x(i, e + 1));
+    if (!(m >= least) || !(m > kNegInf)) continue;
+#pragma unroll 1
+    for (int e = 0; e < kPerPack<E>; ++e) {
+      const float x = pack_elem_at<E>(row.raw[i], e);
+      if (!(x >= least) || !(x > kNegInf) || !take(x, row.id(i, e))) continue;
+      const int at = atomicAdd(&sh.n_cand, 1);
+      if (at < kCandBlock) sh.cand[at] = entry(order_key(x), row.id(i, e));
+    }
+  }
+  __syncthreads();
+  if (row.warp == 0) row.to_all(&sh.n_block[row.rank], sh.n_cand);
+  cluster_sync();
+  int all = 0;
+  bool fits = true;
+  for (int c = 0; c < row.cluster; ++c) {
+    fits = fits && sh.n_block[c] <= kCandBlock;
+    all += sh.n_block[c];
+  }
+  return fits && all <= kCandAll ? all : -1;
+}
+
+// First block: the candidates in order in few.all (n of them, known to all blocks).
+template <typename E, int kPacks>
+ALR_DEV void sort_candidates(Row<E, kPacks>& row, int n) {
+  Shared& sh = row.sh;
+  const int tid = threadIdx.x, threads = blockDim.x;
+  unsigned long long* to = sh.few.all;
+  auto gather = [&](int i) {   // candidate i of the cluster's
+    int c = 0;
+    while (i >= sh.n_block[c]) i -= sh.n_block[c++];
+    const uint32_t a = cluster_smem_addr(&sh.cand[i], c);
+    unsigned long long v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+    return v;
+  };
+  if (n <= kCandSort) {
+    unsigned long long* raw = sh.few.all + kCandSort;
+    for (int i = tid; i < n; i += threads) raw[i] = gather(i);
+    __syncthreads();
+    for (int i = tid; i < n; i += threads) {
+      const unsigned long long v = raw[i];
+      int place = 0;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) place += raw[j] > v;
+      to[place] = v;
+    }
+    __syncthreads();
+    return;
+  }
+  int size = 2 * kCandSort;
+  while (size < n) size *= 2;
+  for (int i = tid; i < size; i += threads) to[i] = i < n ? gather(i) : 0ull;
+  __syncthreads();
+  for (int k = 2; k <= size; k *= 2)
+    for (int j = k / 2; j > 0; j /= 2) {
+      for (int p = tid; p < size / 2; p += threads) {
+        const int a = 2 * p - (p & (j - 1)), b = a + j;
+        const unsigned long long u = to[a], v = to[b];
+        if ((u < v) == ((a & k) == 0)) {
+          to[a] = v;
+          to[b] = u;
+        }
+      }
+      __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------- top logits ---
-template <typename E>
-__global__ void __launch_bounds__(kRowThreads)
+template <typename E, int kPacks>
+__global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
     top_logits_kernel(const E* Z, long long ldz, int V, int K, float inv_t, float* top_val,
-                      int32_t* top_idx, float* lse, float* lse_rest) {
-  __shared__ SelectShared sh;
-  __shared__ uint32_t key[kTopMost];
-  __shared__ int id[kTopMost];
-  __shared__ int n_got;
+                      int32_t* top_idx, float* lse, float* lse_rest, int cluster) {
+  __shared__ Shared sh;
   pdl_wait_and_release();
-  const long long r = blockIdx.x;
-  const E* z = Z + r * ldz;
+  const long long r = cluster_id_x();
+  Row<E, kPacks> row(Z + r * ldz, r * ldz, V, cluster, sh);
+  const Bound bound = row_bound(row, K);
+  float least = bound.least;
+  int n = collect(row, least, [](float, int) { return true; });
+  Cut cut{0u, 0x7fffffff};
+  if (n < 0) {   // more than fit reach the bound: find the exact cut
+    cluster_sync();
+    cut = cut_top_k(row, K);
+    if (threadIdx.x == 0) sh.n_cand = 0;
+    __syncthreads();
+    n = collect(row, key_value(cut.key), [&](float x, int v) { return cut.keeps(order_key(x), v); });
+  }
+  // the others' sums, each warp's from its own largest; the candidates are the first block's
+  const float k = inv_t * kLog2e;
+  const bool exact = cut.last != 0x7fffffff;
+  const auto other = [&](int i, int e) {
+    const float x = row.x(i, e);
+    const bool taken = exact ? x > kNegInf && cut.keeps(order_key(x), row.id(i, e)) : x >= least;
+    return taken ? kNegInf : x;
+  };
   float m = kNegInf;
-  int finite = 0;
-  for (int v = threadIdx.x; v < V; v += blockDim.x) {
-    const float x = to_float(z[v]);
-    if (x > kNegInf) {
-      m = fmaxf(m, x);
-      ++finite;
+#pragma unroll
+  for (int i = 0; i < kPacks; ++i)
+#pragma unroll
+    for (int e = 0; e < kPerPack<E>; e += 2) m = max3(m, other(i, e), other(i, e + 1));
+  m = warp_max(m);
+  float s = 0.f;
+  if (m > kNegInf)
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i)
+#pragma unroll
+      for (int e = 0; e < kPerPack<E>; ++e) s += ex2((other(i, e) - m) * k);
+  s = warp_reduce(s, AddOp());
+  row.to_all(&sh.frec[row.record()], make_float2(m, s));
+  cluster_sync();
+  if (row.rank == 0) {
+    sort_candidates(row, n);
+    const int tid = threadIdx.x, threads = blockDim.x, got = min(n, K);
+    for (int i = tid; i < K; i += threads) {
+      top_val[r * K + i] = i < got ? key_value(entry_key(sh.few.all[i])) : kNegInf;
+      top_idx[r * K + i] = i < got ? entry_id(sh.few.all[i]) : -1;
+    }
+    // the rest: candidates past the K first, and all others
+    float mo = kNegInf;
+    for (int i = K + tid; i < n; i += threads) mo = fmaxf(mo, key_value(entry_key(sh.few.all[i])));
+    for (int i = tid; i < row.records(); i += threads) mo = fmaxf(mo, sh.frec[i].x);
+    mo = block_reduce(mo, MaxOp(), sh.fbuf);
+    float so = 0.f, sl = 0.f;
+    if (mo > kNegInf) {
+      for (int i = K + tid; i < n; i += threads)
+        so += ex2((key_value(entry_key(sh.few.all[i])) - mo) * k);
+      for (int i = tid; i < row.records(); i += threads)
+        if (sh.frec[i].x > kNegInf) so += sh.frec[i].y * ex2((sh.frec[i].x - mo) * k);
+    }
+    so = block_reduce(so, AddOp(), sh.fbuf);
+    for (int i = tid; i < got; i += threads)
+      sl += ex2((key_value(entry_key(sh.few.all[i])) - bound.top) * k);
+    sl = block_reduce(sl, AddOp(), sh.fbuf);
+    if (tid == 0) {
+      const bool any = mo > kNegInf;
+      if (any) sl += so * ex2((mo - bound.top) * k);
+      if (lse != nullptr) lse[r] = n > 0 ? bound.top * inv_t + logf(sl) : kNegInf;
+      if (lse_rest != nullptr) lse_rest[r] = any ? mo * inv_t + logf(so) : kNegInf;
     }
   }
-  m = block_reduce(m, MaxOp(), sh.buf);
-  finite = block_reduce(finite, AddOp(), sh.ibuf);
-  const int n = min(K, finite);
-  Cut cut{0xffffffffu, -1};
-  if (n > 0) cut = cut_top_k(z, V, n, sh);
-  if (threadIdx.x == 0) n_got = 0;
-  __syncthreads();
-  const float c = inv_t * kLog2e;
-  // the tokens not listed are summed from their own maximum: what they hold next to the listed ones
-  // may be below the range of the largest one's exponential
-  float mo = kNegInf;
-  for (int v = threadIdx.x; v < V; v += blockDim.x) {
-    const float x = to_float(z[v]);
-    if (!(x > kNegInf)) continue;
-    const uint32_t k = order_key(x);
-    if (cut.keeps(k, v)) {
-      const int at = atomicAdd(&n_got, 1);
-      if (at < kTopMost) {
-        key[at] = k;
-        id[at] = v;
-      }
-    } else {
-      mo = fmaxf(mo, x);
-    }
-  }
-  mo = block_reduce(mo, MaxOp(), sh.buf);
-  float So = 0.f, S = 0.f;
-  for (int v = threadIdx.x; v < V; v += blockDim.x) {
-    const float x = to_float(z[v]);
-    if (x > kNegInf && !cut.keeps(order_key(x), v)) So += ex2((x - mo) * c);
-  }
-  So = block_reduce(So, AddOp(), sh.buf);
-  for (int i = threadIdx.x; i < n; i += blockDim.x) S += ex2((key_value(key[i]) - m) * c);
-  S = block_reduce(S, AddOp(), sh.buf);
-  if (mo > kNegInf) S += So * ex2((mo - m) * c);
-  // an entry's place is the number of entries before it in the order
-  for (int i = threadIdx.x; i < K; i += blockDim.x) {
-    if (i < n) {
-      int place = 0;
-      for (int j = 0; j < n; ++j)
-        place += key[j] > key[i] || (key[j] == key[i] && id[j] < id[i]);
-      top_val[r * K + place] = key_value(key[i]);
-      top_idx[r * K + place] = id[i];
-    } else {
-      top_val[r * K + i] = kNegInf;
-      top_idx[r * K + i] = -1;
-    }
-  }
-  if (threadIdx.x == 0) {
-    if (lse != nullptr) lse[r] = n > 0 ? m * inv_t + logf(S) : kNegInf;
-    if (lse_rest != nullptr) lse_rest[r] = mo > kNegInf ? mo * inv_t + logf(So) : kNegInf;
-  }
+  cluster_sync();   // no block's candidates are read any more
 }
 
 // ------------------------------------------------------------------ sampling ---
@@ -193,145 +557,205 @@ __global__ void __launch_bounds__(kRowThreads)
 // the split of a row over threads can change a draw.
 struct Weight {
   float m, c;
-  ALR_DEV float real(float x) const { return x == m ? 1.f : exp2f(__fmul_rn(__fsub_rn(x, m), c)); }
-  ALR_DEV unsigned long long operator()(float x) const {
-    return (unsigned long long)(real(x) * 2147483648.f);
+  // exp2f and ex2.approx agree where the weight is not 0 (every float of [-64, 0] was compared)
+  ALR_DEV float real(float x) const { return x == m ? 1.f : ex2(__fmul_rn(__fsub_rn(x, m), c)); }
+  ALR_DEV uint32_t operator()(float x) const { return __float2uint_rz(real(x) * 2147483648.f); }
+};
+
+struct SampleOut {
+  int32_t* token;
+  float* prob;
+  int32_t* n_kept;
+  ALR_DEV void put(long long r, int t, float p, int n) const {
+    token[r] = t;
+    if (prob != nullptr) prob[r] = p;
+    if (n_kept != nullptr) n_kept[r] = n;
   }
 };
 
-template <typename E>
-__global__ void __launch_bounds__(kRowThreads)
-    sample_kernel(const E* Z, long long ldz, int V, SampleArgs a, int32_t* token, float* prob,
-                  int32_t* n_kept) {
-  __shared__ SelectShared sh;
-  pdl_wait_and_release();
-  const long long r = blockIdx.x;
-  const E* z = Z + r * ldz;
-  float m = kNegInf;
-  int at = 0x7fffffff;
-  for (int v = threadIdx.x; v < V; v += blockDim.x) {
-    const float x = to_float(z[v]);
-    if (x > m) {
-      m = x;
-      at = v;
-    }
+// First block: draws from the `n` candidates in few.all, the row's first ones in order.  total: the mass
+// that top_p refers to (0: the candidates' own).  False: the nucleus goes on past the candidates.
+template <typename E, int kPacks>
+ALR_DEV bool draw_from_candidates(Row<E, kPacks>& row, int n, unsigned long long total,
+                                  const Weight& weight, float top_p, float min_p, uint32_t u,
+                                  long long r, const SampleOut& out) {
+  Shared& sh = row.sh;
+  const int tid = threadIdx.x, threads = blockDim.x;
+  unsigned long long* w = sh.few.all + kCandAll / 2;   // weights, in order (n <= kCandAll / 2)
+  unsigned long long sum = 0;
+  for (int i = tid; i < n; i += threads) {
+    w[i] = weight(key_value(entry_key(sh.few.all[i])));
+    sum += w[i];
   }
-  const float top = block_reduce(m, MaxOp(), sh.buf);
-  const int first = block_reduce(m == top ? at : 0x7fffffff, MinOp(), sh.ibuf);
+  sum = block_reduce(sum, AddOp(), sh.lbuf);
+  const double lim = double(top_p) * double(total != 0 ? total : sum);
+  if (total != 0 && double(sum) < lim) return false;
+  // tokens kept: a prefix
+  int kept = 0;
+  for (int i = tid; i < n; i += threads) {
+    unsigned long long before = 0;
+    if (top_p < 1.f)
+      for (int j = 0; j < i; ++j) before += w[j];
+    const float x = key_value(entry_key(sh.few.all[i]));
+    kept += w[i] > 0 && (i == 0 || ((top_p >= 1.f || double(before) < lim) &&
+                                    (x == weight.m || weight.real(x) >= min_p)));
+  }
+  kept = block_reduce(kept, AddOp(), sh.ibuf);
+  unsigned long long S = 0;
+  for (int i = tid; i < kept; i += threads) S += w[i];
+  S = block_reduce(S, AddOp(), sh.lbuf);
+  const unsigned long long target = __umul64hi((unsigned long long)u << 32, S);
+  for (int i = tid; i < kept; i += threads) {
+    const uint32_t id = uint32_t(entry_id(sh.few.all[i]));
+    unsigned long long before = 0;
+    for (int j = 0; j < kept; ++j)
+      if (uint32_t(entry_id(sh.few.all[j])) < id) before += w[j];
+    if (before <= target && target < before + w[i])
+      out.put(r, int(id), float(double(w[i]) / double(S)), kept);
+  }
+  return true;
+}
+
+template <typename E, int kPacks>
+__global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
+    sample_kernel(const E* Z, long long ldz, int V, SampleArgs a, SampleOut out, int cluster) {
+  __shared__ Shared sh;
+  pdl_wait_and_release();
+  const long long r = cluster_id_x();
+  Row<E, kPacks> row(Z + r * ldz, r * ldz, V, cluster, sh);
   const float T = a.temperature != nullptr ? a.temperature[r] : 1.f;
-  if (!(top > kNegInf) || !(T > 0.f)) {
-    if (threadIdx.x == 0) {
-      const bool some = top > kNegInf;
-      token[r] = some ? first : -1;
-      if (prob != nullptr) prob[r] = some ? 1.f : 0.f;
-      if (n_kept != nullptr) n_kept[r] = some ? 1 : 0;
-    }
+  const int top_k = a.top_k != nullptr ? a.top_k[r] : 0;
+  const float top_p = a.top_p != nullptr ? a.top_p[r] : 1.f;
+  const float min_p = a.min_p != nullptr ? fminf(a.min_p[r], 1.f) : 0.f;
+  const uint32_t u = a.u[r];
+  const bool greedy = !(T > 0.f), few = top_k > 0 && top_k <= kTopMost;
+  // how many of the first tokens are looked at on their own; a nucleus may go on past them
+  const int K = greedy ? 1 : few ? top_k : top_p < 1.f && !(top_k > 0 && top_k < V) ? kTopMost : 0;
+  const Bound bound = row_bound(row, K);
+  if (!(bound.top > kNegInf)) {
+    if (row.rank == 0 && threadIdx.x == 0) out.put(r, -1, 0.f, 0);
+    cluster_sync();
     return;
   }
-  const Weight weight{top, __fdiv_rn(kLog2e, T)};
-  Cut cut{0u, 0x7fffffff};
-  const int k = a.top_k != nullptr ? a.top_k[r] : 0;
-  if (k > 0 && k < V) {
-    int finite = 0;
-    for (int v = threadIdx.x; v < V; v += blockDim.x) finite += to_float(z[v]) > kNegInf;
-    finite = block_reduce(finite, AddOp(), sh.ibuf);
-    if (k < finite) cut = cut_top_k(z, V, k, sh);
-  }
-  const float min_p = a.min_p != nullptr ? fminf(a.min_p[r], 1.f) : 0.f;
-  auto total = [&](int& count, float least) {
-    unsigned long long s = 0;
-    int n = 0;
-    for (int v = threadIdx.x; v < V; v += blockDim.x) {
-      const float x = to_float(z[v]);
-      if (!(x > kNegInf) || !cut.keeps(order_key(x), v)) continue;
-      const unsigned long long w = weight(x);
-      if (w == 0 || (x != top && weight.real(x) < least)) continue;
-      s += w;
-      ++n;
+  const Weight weight{bound.top, greedy ? 0.f : __fdiv_rn(kLog2e, T)};
+  bool done = false;
+  if (K > 0) {
+    const int n = collect(row, bound.least, [](float, int) { return true; });
+    unsigned long long total = 0;
+    if (n >= 0 && n <= kCandAll / 2) {
+      if (!greedy && !few) {   // the mass of the whole row
+        unsigned long long s = 0;
+#pragma unroll
+        for (int i = 0; i < kPacks; ++i)
+#pragma unroll
+          for (int e = 0; e < kPerPack<E>; ++e) s += weight(row.x(i, e));
+        s = warp_reduce(s, AddOp());
+        row.to_all(&sh.rec[row.record()], s);
+        cluster_sync();
+        for (int i = row.lane; i < row.records(); i += 32) total += sh.rec[i];
+        total = warp_reduce(total, AddOp());
+      }
+      if (row.rank == 0) {
+        sort_candidates(row, n);
+        done = true;
+        if (greedy) {
+          if (threadIdx.x == 0) out.put(r, entry_id(sh.few.all[0]), 1.f, 1);
+        } else {
+          done = draw_from_candidates(row, few ? min(n, K) : n, total, weight, top_p, min_p, u, r, out);
+        }
+      }
+      if (row.warp == 0) {
+        if (row.rank == 0) row.to_all(&sh.flag, int(done));
+      }
+      cluster_sync();
+      done = sh.flag != 0;
     }
-    count = block_reduce(n, AddOp(), sh.ibuf);
-    return block_reduce(s, AddOp(), sh.lbuf);
-  };
-  const float top_p = a.top_p != nullptr ? a.top_p[r] : 1.f;
-  int n = 0;
-  if (top_p < 1.f) {
-    const double lim = double(top_p) * double(total(n, 0.f));
-    unsigned long long above;
-    const uint32_t key = select_key(
-        z, V, cut, weight, [lim](unsigned long long got) { return double(got) < lim; }, above, sh);
-    // tokens with this key while the sum before them is below the limit, one at least
-    const unsigned long long w = weight(key_value(key));
-    long long more = 1;
-    if (w > 0) {
-      more = (long long)((lim - double(above)) / double(w));
-      more = more < 1 ? 1 : more;
-      while (more > 1 && !(double(above + (more - 1) * w) < lim)) --more;
-      while (double(above + more * w) < lim) ++more;
-    }
-    cut = {key, nth_equal(z, V, cut, key, more, sh)};
   }
-  const unsigned long long S = total(n, min_p);
-  // floor(u S / 2^32): the first token, in the order of ids, whose running sum exceeds it
-  const unsigned long long u = a.u[r];
-  const unsigned long long target = __umul64hi(u << 32, S);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, n_warps = blockDim.x / 32;
-  unsigned long long before = 0;
-  for (int base = 0; base < V; base += blockDim.x) {
-    const int v = base + threadIdx.x;
-    unsigned long long w = 0;
-    if (v < V) {
-      const float x = to_float(z[v]);
-      if (x > kNegInf && cut.keeps(order_key(x), v)) {
-        w = weight(x);
-        if (x != top && weight.real(x) < min_p) w = 0;
+  if (!done) {   // uniform in the cluster
+    cluster_sync();
+    Cut cut{0u, 0x7fffffff};
+    if (greedy) {
+      cut = cut_top_k(row, 1);
+    } else {
+      if (top_k > 0 && top_k < V) {
+        // as many candidates at all?
+        const Found all = find_unit(
+            row, [](float x, int) -> unsigned long long { return x > kNegInf; },
+            [](unsigned long long) { return 1ull; });
+        if ((unsigned long long)top_k < all.total) cut = cut_top_k(row, top_k);
+      }
+      if (top_p < 1.f) {
+        NeedMass need{double(top_p), 0.0};
+        const Selected s = select_key(row, cut, weight, need);
+        // tokens with this key while the sum before them is below the limit, one at least
+        const double lim = double(top_p) * double(s.total);
+        const unsigned long long w = weight(key_value(s.key));
+        unsigned long long more = 1;
+        if (w > 0) {
+          const double want = (lim - double(s.above)) / double(w);
+          more = want < 1.0 ? 1ull : (unsigned long long)want;
+          while (more > 1 && !(double(s.above + (more - 1) * w) < lim)) --more;
+          while (double(s.above + more * w) < lim) ++more;
+        }
+        cut = {s.key, nth_equal(row, cut, s.key, more)};
       }
     }
-    unsigned long long incl = w;
+    int kept = 0;
+    const auto mass = [&](float x, int v) -> unsigned long long {
+      if (!(x > kNegInf) || !cut.keeps(order_key(x), v)) return 0;
+      if (x != weight.m && weight.real(x) < min_p) return 0;
+      return weight(x);
+    };
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
-      if (lane >= off) incl += t;
+    for (int i = 0; i < kPacks; ++i)
+#pragma unroll
+      for (int e = 0; e < kPerPack<E>; ++e) kept += mass(row.x(i, e), row.id(i, e)) != 0;
+    kept = int(warp_reduce(kept, AddOp()));
+    row.to_all(&sh.frec[row.record()], make_float2(__int_as_float(kept), 0.f));
+    const Found f = find_unit(row, mass, [u](unsigned long long total) {
+      return __umul64hi((unsigned long long)u << 32, total) + 1;
+    });
+    if (row.rank == 0 && row.warp == 0) {
+      int n = 0;
+      for (int i = row.lane; i < row.records(); i += 32) n += __float_as_int(sh.frec[i].x);
+      n = warp_reduce(n, AddOp());
+      if (row.lane == 0) out.put(r, f.id, float(double(f.weight) / double(f.total)), n);
     }
-    if (lane == 31) sh.lbuf[warp] = incl;
-    __syncthreads();
-    unsigned long long mine = before, all = 0;
-    for (int i = 0; i < n_warps; ++i) {
-      if (i < warp) mine += sh.lbuf[i];
-      all += sh.lbuf[i];
-    }
-    if (w > 0 && mine + incl - w <= target && mine + incl > target) {
-      token[r] = v;
-      if (prob != nullptr) prob[r] = float(double(w) / double(S));
-    }
-    before += all;
-    __syncthreads();
-    if (before > target) break;
   }
-  if (threadIdx.x == 0 && n_kept != nullptr) n_kept[r] = n;
+  cluster_sync();   // no block's memory is read any more
+}
+
+template <typename F>
+cudaError_t by_shape(int dtype, long long N, int V, int sms, F f) {
+  const RowShape shape = row_shape(N, V, dtype == 0 ? 2 : 4, sms, 256);
+  return with_packs(shape.packs, [&](auto packs) {
+    return dtype == 0 ? f(shape, packs, static_cast<const __nv_bfloat16*>(nullptr))
+                      : f(shape, packs, static_cast<const float*>(nullptr));
+  });
 }
 
 }  // namespace
 
 cudaError_t launch_top_logits(int dtype, const void* Z, long long N, int V, long long ldz, int K,
                               float inv_t, float* top_val, int32_t* top_idx, float* lse,
-                              float* lse_rest, cudaStream_t s) {
-  if (dtype == 0)
-    return launch_pdl(top_logits_kernel<__nv_bfloat16>, dim3(unsigned(N)), dim3(kRowThreads), 0, s,
-                      static_cast<const __nv_bfloat16*>(Z), ldz, V, K, inv_t, top_val, top_idx, lse,
-                      lse_rest);
-  return launch_pdl(top_logits_kernel<float>, dim3(unsigned(N)), dim3(kRowThreads), 0, s,
-                    static_cast<const float*>(Z), ldz, V, K, inv_t, top_val, top_idx, lse,
-                    lse_rest);
+                              float* lse_rest, int sms, cudaStream_t s) {
+  return by_shape(dtype, N, V, sms, [&](const RowShape& shape, auto packs, auto* e) {
+    using E = std::remove_cv_t<std::remove_pointer_t<decltype(e)>>;
+    return launch_row_each(shape, N, top_logits_kernel<E, decltype(packs)::value>, s,
+                           static_cast<const E*>(Z), ldz, V, K, inv_t, top_val, top_idx, lse, lse_rest,
+                           shape.cluster);
+  });
 }
 
 cudaError_t launch_sample(int dtype, const void* Z, long long N, int V, long long ldz,
-                          const SampleArgs& a, int32_t* token, float* prob, int32_t* n_kept,
+                          const SampleArgs& a, int32_t* token, float* prob, int32_t* n_kept, int sms,
                           cudaStream_t s) {
-  if (dtype == 0)
-    return launch_pdl(sample_kernel<__nv_bfloat16>, dim3(unsigned(N)), dim3(kRowThreads), 0, s,
-                      static_cast<const __nv_bfloat16*>(Z), ldz, V, a, token, prob, n_kept);
-  return launch_pdl(sample_kernel<float>, dim3(unsigned(N)), dim3(kRowThreads), 0, s,
-                    static_cast<const float*>(Z), ldz, V, a, token, prob, n_kept);
+  return by_shape(dtype, N, V, sms, [&](const RowShape& shape, auto packs, auto* e) {
+    using E = std::remove_cv_t<std::remove_pointer_t<decltype(e)>>;
+    const SampleOut out{token, prob, n_kept};
+    return launch_row_each(shape, N, sample_kernel<E, decltype(packs)::value>, s,
+                           static_cast<const E*>(Z), ldz, V, a, out, shape.cluster);
+  });
 }
 
 }  // namespace alr
