@@ -3,12 +3,13 @@
 // Both pick from a row by the order (value descending, token id ascending).  A logit that is -inf or
 // NaN is no candidate.  A row lies in the registers of a cluster (row_cluster.cuh), read once.
 //
-// Few tokens of many (top logits, top-k, most nuclei): the K-th largest of the largest logits that the
-// threads hold is a lower bound of the row's K-th largest, and next to no more than K logits reach it.
-// Those go to the cluster's first block, which sorts them and does the rest.
-// Many tokens (a flat nucleus, a top-k past kTopMost), or so many equal ones that they would not fit:
-// a radix select over an order-preserving key, with a histogram of counts or weights per digit in
-// each block's shared memory, added up over the cluster.
+// Few tokens of many (top logits, top-k): the K-th largest of the largest logits that the threads hold is a
+// lower bound of the row's K-th largest, and next to no more than K logits reach it.  Those go to the
+// cluster's first block, which sorts them and does the rest.
+// Any number of tokens (a nucleus, a top-k past kTopMost): a histogram of counts or weights over even steps
+// of the logit below the largest, in each block's shared memory and added up over the cluster, tells the
+// step in which the cut falls; that step's logits are sorted as above.
+// So many equal logits that they do not fit: a radix select over an order-preserving key.
 #include "kernels.h"
 #include "launch.h"
 #include "row_cluster.cuh"
@@ -49,14 +50,15 @@ struct Shared {
     } many;
   };
   unsigned long long cand[kCandBlock];
+  uint32_t small[256];                    // histogram of the list's keys
   unsigned long long rec[kWarpsMost];     // of each warp of the cluster: a sum
   float2 frec[kWarpsMost];
   float fbuf[32];                         // and the bound's result
   unsigned long long lbuf[32];
   int ibuf[32];
   int n_cand, n_block[kRowClusterMost];
-  float bound;
-  uint32_t digit;
+  float top;
+  uint32_t digit, reach;
   unsigned long long above, found, kept;
   int flag;
 };
@@ -313,14 +315,26 @@ ALR_DEV int nth_equal(Row<E, kPacks>& row, const Cut& cut, uint32_t key, unsigne
   return f.id;
 }
 
+// What a cut is asked for: k tokens, or the share p of a mass.  reach(): how many tokens of weight w each,
+// one at least, after a sum `above`.
 struct NeedCount {
   unsigned long long k;
   ALR_DEV void set(unsigned long long) {}
+  ALR_DEV unsigned long long reach(unsigned long long above, unsigned long long) const {
+    return k - above;
+  }
   ALR_DEV bool operator()(unsigned long long got) const { return got < k; }
 };
 struct NeedMass {
   double p, lim;
   ALR_DEV void set(unsigned long long total) { lim = p * double(total); }
+  ALR_DEV unsigned long long reach(unsigned long long above, unsigned long long w) const {
+    const double want = (lim - double(above)) / double(w);
+    unsigned long long n = want < 1.0 ? 1ull : (unsigned long long)want;
+    while (n > 1 && !(double(above + (n - 1) * w) < lim)) --n;
+    while (double(above + n * w) < lim) ++n;
+    return n;
+  }
   ALR_DEV bool operator()(unsigned long long got) const { return double(got) < lim; }
 };
 
@@ -355,39 +369,50 @@ ALR_DEV Bound row_bound(Row<E, kPacks>& row, int K) {
     if (row.lane == __ffs(who) - 1) t = kNegInf;
   }
   if (threadIdx.x == 0) sh.n_cand = 0;
+  for (int i = threadIdx.x; i < 256; i += blockDim.x) sh.small[i] = 0;
   cluster_sync();
-  if (row.warp == 0) {
-    // The list's K-th largest by bisection of the keys' upper half: the largest prefix that K reach.
-    constexpr int kMost = (kListMost + 31) / 32;
-    const int n = n_rec * per;
-    uint32_t key[kMost];
-    float top = kNegInf;
-#pragma unroll
-    for (int j = 0; j < kMost; ++j) {
-      key[j] = 0;
-      if (j * 32 >= n) continue;
-      const int i = j * 32 + row.lane;
-      const float v = i < n ? sh.few.list[i] : kNegInf;
-      if (v > kNegInf) key[j] = order_key(v) >> 16;
-      top = fmaxf(top, v);
+  const int n = n_rec * per;
+  float top = kNegInf;
+  for (int i = row.lane; i < n_rec; i += 32) top = fmaxf(top, sh.few.list[i * per]);
+  top = warp_max(top);
+  if (K <= 1) return {K == 1 ? top : kNegInf, top};
+  // The upper half of the list's K-th largest key, 8 bits at a time.
+  uint32_t prefix = 0, reach = uint32_t(K);
+  for (int shift = 24; shift >= 16; shift -= 8) {
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+      const float v = sh.few.list[i];
+      const uint32_t key = order_key(v);
+      if (v > kNegInf && (shift == 24 || key >> 24 == prefix >> 24))
+        atomicAdd(&sh.small[(key >> shift) & 255], 1u);
     }
-    top = warp_max(top);
-    uint32_t least = 0;
-    if (K > 0)
-      for (uint32_t bit = 0x8000u; bit != 0; bit >>= 1) {
-        int reach = 0;
+    __syncthreads();
+    if (row.warp == 0) {   // lane l: the bins 255 - 8 l and the seven below
+      uint32_t mine = 0;
+      for (int j = 0; j < 8; ++j) mine += sh.small[255 - 8 * row.lane - j];
+      uint32_t incl = mine;
 #pragma unroll
-        for (int j = 0; j < kMost; ++j)
-          if (j * 32 < n) reach += key[j] >= (least | bit);
-        if (__reduce_add_sync(0xffffffffu, reach) >= K) least |= bit;
+      for (int off = 1; off < 32; off <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, incl, off);
+        if (row.lane >= off) incl += o;
       }
-    if (row.lane == 0) {
-      sh.bound = least != 0 ? key_value(least << 16) : kNegInf;
-      sh.fbuf[0] = top;
+      if (row.lane == 31) sh.digit = incl >= reach ? 0u : 0xffffffffu;   // too few
+      __syncwarp();
+      uint32_t run = incl - mine;
+      if (run < reach && incl >= reach) {
+        int b = 255 - 8 * row.lane;
+        while (run + sh.small[b] < reach) run += sh.small[b--];
+        sh.digit = uint32_t(b);
+        sh.reach = reach - run;
+      }
     }
+    __syncthreads();
+    if (sh.digit == 0xffffffffu) return {kNegInf, top};
+    prefix |= sh.digit << shift;
+    reach = sh.reach;
+    for (int i = threadIdx.x; i < 256; i += blockDim.x) sh.small[i] = 0;
+    __syncthreads();
   }
-  __syncthreads();
-  return {sh.bound, sh.fbuf[0]};
+  return {key_value(prefix), top};
 }
 
 // Element e of a pack, e not known to the compiler.
@@ -429,28 +454,39 @@ ALR_DEV int collect(Row<E, kPacks>& row, float least, F take) {
   return fits && all <= kCandAll ? all : -1;
 }
 
-// First block: the candidates in order in few.all (n of them, known to all blocks).
+// First block: the cluster's n candidates into its own memory; after it and a cluster_sync the other
+// blocks are not needed any more.
 template <typename E, int kPacks>
-ALR_DEV void sort_candidates(Row<E, kPacks>& row, int n) {
+ALR_DEV void gather_candidates(Row<E, kPacks>& row, int n) {
   Shared& sh = row.sh;
+  if (row.rank != 0) return;
+  unsigned long long* to = sh.few.all + (n <= kCandSort ? kCandSort : 0);
+  int base = 0;
+  for (int c = 0; c < row.cluster; ++c) {
+    const int m = sh.n_block[c];
+    for (int i = threadIdx.x; i < m; i += blockDim.x) {
+      unsigned long long v;
+      asm volatile("ld.shared::cluster.u64 %0, [%1];"
+                   : "=l"(v)
+                   : "r"(cluster_smem_addr(&sh.cand[i], c))
+                   : "memory");
+      to[base + i] = v;
+    }
+    base += m;
+  }
+}
+
+// First block: the gathered candidates in order, in few.all.
+ALR_DEV void sort_candidates(Shared& sh, int n) {
   const int tid = threadIdx.x, threads = blockDim.x;
   unsigned long long* to = sh.few.all;
-  auto gather = [&](int i) {   // candidate i of the cluster's
-    int c = 0;
-    while (i >= sh.n_block[c]) i -= sh.n_block[c++];
-    const uint32_t a = cluster_smem_addr(&sh.cand[i], c);
-    unsigned long long v;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
-    return v;
-  };
+  __syncthreads();
   if (n <= kCandSort) {
-    unsigned long long* raw = sh.few.all + kCandSort;
-    for (int i = tid; i < n; i += threads) raw[i] = gather(i);
-    __syncthreads();
+    const unsigned long long* raw = to + kCandSort;
     for (int i = tid; i < n; i += threads) {
       const unsigned long long v = raw[i];
       int place = 0;
-#pragma unroll 4
+#pragma unroll 8
       for (int j = 0; j < n; ++j) place += raw[j] > v;
       to[place] = v;
     }
@@ -459,7 +495,7 @@ ALR_DEV void sort_candidates(Row<E, kPacks>& row, int n) {
   }
   int size = 2 * kCandSort;
   while (size < n) size *= 2;
-  for (int i = tid; i < size; i += threads) to[i] = i < n ? gather(i) : 0ull;
+  for (int i = n + tid; i < size; i += threads) to[i] = 0ull;
   __syncthreads();
   for (int k = 2; k <= size; k *= 2)
     for (int j = k / 2; j > 0; j /= 2) {
@@ -485,41 +521,56 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
   const long long r = cluster_id_x();
   Row<E, kPacks> row(Z + r * ldz, r * ldz, V, cluster, sh);
   const Bound bound = row_bound(row, K);
-  float least = bound.least;
-  int n = collect(row, least, [](float, int) { return true; });
-  Cut cut{0u, 0x7fffffff};
+  int n = collect(row, bound.least, [](float, int) { return true; });
+  Cut cut{0u, -1};
   if (n < 0) {   // more than fit reach the bound: find the exact cut
     cluster_sync();
-    cut = cut_top_k(row, K);
+    Row<E, kPacks> copy = row;
+    cut = cut_top_k(copy, K);
     if (threadIdx.x == 0) sh.n_cand = 0;
     __syncthreads();
     n = collect(row, key_value(cut.key), [&](float x, int v) { return cut.keeps(order_key(x), v); });
   }
+  gather_candidates(row, n);
   // the others' sums, each warp's from its own largest; the candidates are the first block's
-  const float k = inv_t * kLog2e;
-  const bool exact = cut.last != 0x7fffffff;
-  const auto other = [&](int i, int e) {
-    const float x = row.x(i, e);
-    const bool taken = exact ? x > kNegInf && cut.keeps(order_key(x), row.id(i, e)) : x >= least;
-    return taken ? kNegInf : x;
-  };
+  const float k = inv_t * kLog2e, least = cut.last >= 0 ? key_value(cut.key) : bound.least;
   float m = kNegInf;
+#pragma unroll
+  for (int i = 0; i < kPacks; ++i) {
+    float p = kNegInf;
+#pragma unroll
+    for (int e = 0; e < kPerPack<E>; e += 2) p = max3(p, row.x(i, e), row.x(i, e + 1));
+    if (p >= least) {
+      uint32_t bits = 0;
+      p = kNegInf;
+#pragma unroll 1
+      for (int e = 0; e < kPerPack<E>; ++e) {
+        const float x = pack_elem_at<E>(row.raw[i], e);
+        const bool taken =
+            x >= least && (cut.last < 0 || cut.keeps(x > kNegInf ? order_key(x) : 0u, row.id(i, e)));
+        bits |= uint32_t(taken) << e;
+        if (!taken) p = fmaxf(p, x);
+      }
+      mask_pack<E>(row.raw[i], bits);
+    }
+    m = fmaxf(m, p);
+  }
+  m = warp_max(m);
+  const float mw = m > kNegInf ? m : 0.f;
+  const uint64_t m2 = f2_pack(mw, mw), k2 = f2_pack(k, k);
+  uint64_t s2 = 0;
 #pragma unroll
   for (int i = 0; i < kPacks; ++i)
 #pragma unroll
-    for (int e = 0; e < kPerPack<E>; e += 2) m = max3(m, other(i, e), other(i, e + 1));
-  m = warp_max(m);
-  float s = 0.f;
-  if (m > kNegInf)
-#pragma unroll
-    for (int i = 0; i < kPacks; ++i)
-#pragma unroll
-      for (int e = 0; e < kPerPack<E>; ++e) s += ex2((other(i, e) - m) * k);
-  s = warp_reduce(s, AddOp());
+    for (int e = 0; e < kPerPack<E>; e += 2)
+      s2 = f2_add(s2, f2_ex2(f2_mul(f2_sub(f2_pack(row.x(i, e), row.x(i, e + 1)), m2), k2)));
+  float sa, sb;
+  f2_unpack(s2, sa, sb);
+  const float s = warp_reduce(sa + sb, AddOp());
   row.to_all(&sh.frec[row.record()], make_float2(m, s));
-  cluster_sync();
+  cluster_sync();   // no other block's memory is read any more
   if (row.rank == 0) {
-    sort_candidates(row, n);
+    sort_candidates(sh, n);
     const int tid = threadIdx.x, threads = blockDim.x, got = min(n, K);
     for (int i = tid; i < K; i += threads) {
       top_val[r * K + i] = i < got ? key_value(entry_key(sh.few.all[i])) : kNegInf;
@@ -548,7 +599,6 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
       if (lse_rest != nullptr) lse_rest[r] = any ? mo * inv_t + logf(so) : kNegInf;
     }
   }
-  cluster_sync();   // no block's candidates are read any more
 }
 
 // ------------------------------------------------------------------ sampling ---
@@ -573,28 +623,23 @@ struct SampleOut {
   }
 };
 
-// First block: draws from the `n` candidates in few.all, the row's first ones in order.  total: the mass
-// that top_p refers to (0: the candidates' own).  False: the nucleus goes on past the candidates.
-template <typename E, int kPacks>
-ALR_DEV bool draw_from_candidates(Row<E, kPacks>& row, int n, unsigned long long total,
-                                  const Weight& weight, float top_p, float min_p, uint32_t u,
-                                  long long r, const SampleOut& out) {
-  Shared& sh = row.sh;
+// First block: draws from the n first tokens of the row, in order in few.all.
+ALR_DEV void draw_from_candidates(Shared& sh, int n, const Weight& weight, float top_p, float min_p,
+                                  uint32_t u, long long r, const SampleOut& out) {
   const int tid = threadIdx.x, threads = blockDim.x;
-  unsigned long long* w = sh.few.all + kCandAll / 2;   // weights, in order (n <= kCandAll / 2)
+  unsigned long long* w = sh.few.all + kTopMost;   // weights, in order
   unsigned long long sum = 0;
   for (int i = tid; i < n; i += threads) {
     w[i] = weight(key_value(entry_key(sh.few.all[i])));
     sum += w[i];
   }
   sum = block_reduce(sum, AddOp(), sh.lbuf);
-  const double lim = double(top_p) * double(total != 0 ? total : sum);
-  if (total != 0 && double(sum) < lim) return false;
-  // tokens kept: a prefix
-  int kept = 0;
+  const double lim = double(top_p) * double(sum);
+  int kept = 0;   // tokens kept: a prefix
   for (int i = tid; i < n; i += threads) {
     unsigned long long before = 0;
     if (top_p < 1.f)
+#pragma unroll 8
       for (int j = 0; j < i; ++j) before += w[j];
     const float x = key_value(entry_key(sh.few.all[i]));
     kept += w[i] > 0 && (i == 0 || ((top_p >= 1.f || double(before) < lim) &&
@@ -608,12 +653,175 @@ ALR_DEV bool draw_from_candidates(Row<E, kPacks>& row, int n, unsigned long long
   for (int i = tid; i < kept; i += threads) {
     const uint32_t id = uint32_t(entry_id(sh.few.all[i]));
     unsigned long long before = 0;
+#pragma unroll 8
     for (int j = 0; j < kept; ++j)
-      if (uint32_t(entry_id(sh.few.all[j])) < id) before += w[j];
+      before += uint32_t(entry_id(sh.few.all[j])) < id ? w[j] : 0ull;
     if (before <= target && target < before + w[i])
       out.put(r, int(id), float(double(w[i]) / double(S)), kept);
   }
-  return true;
+}
+
+// Even steps of the logit below the largest, kBins over the 32 octaves below which weights are 0.
+struct Steps {
+  float top, scale;
+  ALR_DEV int operator()(float x) const {
+    return x == top ? 0 : min(kBins - 1, __float2int_rz((top - x) * scale));
+  }
+};
+
+// The cut that keeps, of the tokens of positive weight that `cut` keeps, the first ones whose summed worth
+// need() still asks for before them (one at least); `cut` itself when need() is content with all of them.
+// worth: 0 .. 2^31 for x, 0 only where the weight is 0.
+template <typename E, int kPacks, typename W, typename Need>
+ALR_DEV Cut cut_by_steps(Row<E, kPacks>& row, const Cut& cut, const Steps& bin, W worth, Need need) {
+  Shared& sh = row.sh;
+  const int tid = threadIdx.x, threads = blockDim.x;
+  for (int b = tid; b < kBins; b += threads) sh.many.lo[b] = sh.many.hi[b] = 0;
+  if (tid == 0) {
+    sh.n_cand = 0;
+    sh.digit = 0xffffffffu;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int i = 0; i < kPacks; ++i)
+#pragma unroll
+    for (int e = 0; e < kPerPack<E>; ++e) {
+      const float x = row.x(i, e);
+      if (!(x > kNegInf)) continue;
+      const uint32_t w = worth(x);
+      if (w == 0 || !cut.keeps(order_key(x), row.id(i, e))) continue;
+      const int b = bin(x);
+      if (w & 0xffffu) atomicAdd(&sh.many.lo[b], w & 0xffffu);
+      if (w >> 16) atomicAdd(&sh.many.hi[b], w >> 16);
+    }
+  cluster_sync();
+  const int share = (kBins + row.cluster - 1) / row.cluster;
+  for (int b = row.rank * share + tid; b < min(kBins, (row.rank + 1) * share); b += threads) {
+    unsigned long long t = 0;
+    for (int c = 0; c < row.cluster; ++c) {
+      t += uint32_t(ld_cluster_s32(cluster_smem_addr(&sh.many.lo[b], c)));
+      t += (unsigned long long)uint32_t(ld_cluster_s32(cluster_smem_addr(&sh.many.hi[b], c))) << 16;
+    }
+    for (int c = 0; c < row.cluster; ++c)
+      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_smem_addr(&sh.many.total[b], c)),
+                   "l"(t)
+                   : "memory");
+  }
+  cluster_sync();
+  const int n = (kBins + threads - 1) / threads;
+  unsigned long long mine = 0;
+  for (int j = tid * n; j < min(kBins, (tid + 1) * n); ++j) mine += sh.many.total[j];
+  unsigned long long incl = mine;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
+    if (row.lane >= off) incl += t;
+  }
+  if (row.lane == 31) sh.lbuf[row.warp] = incl;
+  __syncthreads();
+  unsigned long long run = incl - mine, total = 0;
+  for (int w = 0; w < row.n_warps; ++w) {
+    if (w < row.warp) run += sh.lbuf[w];
+    total += sh.lbuf[w];
+  }
+  need.set(total);
+  if (need(total)) return cut;   // all of them (uniform: nothing below is waited for)
+  for (int j = tid * n; j < min(kBins, (tid + 1) * n); ++j) {
+    const unsigned long long t = sh.many.total[j];
+    if (t != 0 && (run == 0 || need(run)) && !need(run + t)) {
+      sh.digit = uint32_t(j);
+      sh.above = run;
+    }
+    run += t;
+  }
+  __syncthreads();
+  const int step = int(sh.digit);
+  const unsigned long long above = sh.above;
+  // that step's tokens, in order
+  const int got = collect(row, kNegInf, [&](float x, int v) {
+    return bin(x) == step && worth(x) != 0 && cut.keeps(order_key(x), v);
+  });
+  if (got < 0) {   // too many of them
+    cluster_sync();
+    Cut c = cut;
+    const Selected s = select_key(row, c, worth, need);
+    const unsigned long long w = worth(key_value(s.key));
+    unsigned long long more = need.reach(s.above, w);
+    c = {s.key, nth_equal(row, c, s.key, more)};
+    return c;
+  }
+  gather_candidates(row, got);
+  if (row.rank == 0) {
+    sort_candidates(sh, got);
+    // the last token before which need() asks for more
+    const int m = (got + threads - 1) / threads;
+    unsigned long long own = 0;
+    for (int i = tid * m; i < min(got, (tid + 1) * m); ++i)
+      own += worth(key_value(entry_key(sh.few.all[i])));
+    unsigned long long in = own;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const unsigned long long t = __shfl_up_sync(0xffffffffu, in, off);
+      if (row.lane >= off) in += t;
+    }
+    if (row.lane == 31) sh.lbuf[row.warp] = in;
+    __syncthreads();
+    unsigned long long at = above + in - own;
+    for (int w = 0; w < row.warp; ++w) at += sh.lbuf[w];
+    for (int i = tid * m; i < min(got, (tid + 1) * m); ++i) {
+      const unsigned long long w = worth(key_value(entry_key(sh.few.all[i])));
+      if ((at == 0 || need(at)) && !need(at + w)) sh.found = sh.few.all[i];
+      at += w;
+    }
+    __syncthreads();
+    if (row.warp == 0) row.to_all(&sh.kept, sh.found);
+  }
+  cluster_sync();
+  const unsigned long long last = sh.kept;
+  cluster_sync();
+  return {entry_key(last), entry_id(last)};
+}
+
+// Any settings: the cut, then the draw over the whole row.
+template <typename E, int kPacks>
+__device__ __noinline__ void sample_many(Row<E, kPacks> row, const Weight weight, bool greedy, int top_k,
+                                         float top_p, float min_p, uint32_t u, long long r,
+                                         const SampleOut out) {
+  Shared& sh = row.sh;
+  Cut cut{0u, 0x7fffffff};
+  const Steps bin{weight.m, weight.c * (kBins / 32)};
+  if (greedy) {
+    cut = cut_top_k(row, 1);
+  } else {
+    if (top_k > 0 && top_k < row.V)
+      cut = cut_by_steps(row, cut, bin, [&](float x) { return weight(x) != 0 ? 1u : 0u; },
+                         NeedCount{(unsigned long long)top_k});
+    if (top_p < 1.f) cut = cut_by_steps(row, cut, bin, weight, NeedMass{double(top_p), 0.0});
+  }
+  const auto mass = [&](float x, int v) -> unsigned long long {
+    if (!(x > kNegInf) || !cut.keeps(order_key(x), v)) return 0;
+    if (x != weight.m && weight.real(x) < min_p) return 0;
+    return weight(x);
+  };
+  int kept = 0;
+  const Found f = find_unit(
+      row,
+      [&](float x, int v) -> unsigned long long {
+        const unsigned long long w = mass(x, v);
+        kept += w != 0;   // counted in the first sweep; what the search adds is not read
+        return w;
+      },
+      [&](unsigned long long total) {
+        const int n = int(warp_reduce(kept, AddOp()));
+        row.to_all(&sh.frec[row.record()], make_float2(__int_as_float(n), 0.f));
+        return __umul64hi((unsigned long long)u << 32, total) + 1;
+      });
+  if (row.rank == 0 && row.warp == 0) {
+    int n = 0;
+    for (int i = row.lane; i < row.records(); i += 32) n += __float_as_int(sh.frec[i].x);
+    n = warp_reduce(n, AddOp());
+    if (row.lane == 0) out.put(r, f.id, float(double(f.weight) / double(f.total)), n);
+  }
 }
 
 template <typename E, int kPacks>
@@ -628,100 +836,30 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
   const float top_p = a.top_p != nullptr ? a.top_p[r] : 1.f;
   const float min_p = a.min_p != nullptr ? fminf(a.min_p[r], 1.f) : 0.f;
   const uint32_t u = a.u[r];
-  const bool greedy = !(T > 0.f), few = top_k > 0 && top_k <= kTopMost;
-  // how many of the first tokens are looked at on their own; a nucleus may go on past them
-  const int K = greedy ? 1 : few ? top_k : top_p < 1.f && !(top_k > 0 && top_k < V) ? kTopMost : 0;
+  const bool greedy = !(T > 0.f);
+  const int K = greedy ? 1 : top_k > 0 && top_k <= kTopMost ? top_k : 0;   // few tokens
   const Bound bound = row_bound(row, K);
-  if (!(bound.top > kNegInf)) {
+  if (!(bound.top > kNegInf)) {   // no candidate; all blocks agree, and none reads another's memory
     if (row.rank == 0 && threadIdx.x == 0) out.put(r, -1, 0.f, 0);
-    cluster_sync();
     return;
   }
   const Weight weight{bound.top, greedy ? 0.f : __fdiv_rn(kLog2e, T)};
-  bool done = false;
   if (K > 0) {
     const int n = collect(row, bound.least, [](float, int) { return true; });
-    unsigned long long total = 0;
-    if (n >= 0 && n <= kCandAll / 2) {
-      if (!greedy && !few) {   // the mass of the whole row
-        unsigned long long s = 0;
-#pragma unroll
-        for (int i = 0; i < kPacks; ++i)
-#pragma unroll
-          for (int e = 0; e < kPerPack<E>; ++e) s += weight(row.x(i, e));
-        s = warp_reduce(s, AddOp());
-        row.to_all(&sh.rec[row.record()], s);
-        cluster_sync();
-        for (int i = row.lane; i < row.records(); i += 32) total += sh.rec[i];
-        total = warp_reduce(total, AddOp());
-      }
-      if (row.rank == 0) {
-        sort_candidates(row, n);
-        done = true;
-        if (greedy) {
-          if (threadIdx.x == 0) out.put(r, entry_id(sh.few.all[0]), 1.f, 1);
-        } else {
-          done = draw_from_candidates(row, few ? min(n, K) : n, total, weight, top_p, min_p, u, r, out);
-        }
-      }
-      if (row.warp == 0) {
-        if (row.rank == 0) row.to_all(&sh.flag, int(done));
-      }
-      cluster_sync();
-      done = sh.flag != 0;
+    if (n >= 0) {
+      gather_candidates(row, n);
+      cluster_sync();   // no other block's memory is read any more
+      if (row.rank != 0) return;
+      sort_candidates(sh, n);
+      if (!greedy)
+        draw_from_candidates(sh, min(n, K), weight, top_p, min_p, u, r, out);
+      else if (threadIdx.x == 0)
+        out.put(r, entry_id(sh.few.all[0]), 1.f, 1);
+      return;
     }
-  }
-  if (!done) {   // uniform in the cluster
     cluster_sync();
-    Cut cut{0u, 0x7fffffff};
-    if (greedy) {
-      cut = cut_top_k(row, 1);
-    } else {
-      if (top_k > 0 && top_k < V) {
-        // as many candidates at all?
-        const Found all = find_unit(
-            row, [](float x, int) -> unsigned long long { return x > kNegInf; },
-            [](unsigned long long) { return 1ull; });
-        if ((unsigned long long)top_k < all.total) cut = cut_top_k(row, top_k);
-      }
-      if (top_p < 1.f) {
-        NeedMass need{double(top_p), 0.0};
-        const Selected s = select_key(row, cut, weight, need);
-        // tokens with this key while the sum before them is below the limit, one at least
-        const double lim = double(top_p) * double(s.total);
-        const unsigned long long w = weight(key_value(s.key));
-        unsigned long long more = 1;
-        if (w > 0) {
-          const double want = (lim - double(s.above)) / double(w);
-          more = want < 1.0 ? 1ull : (unsigned long long)want;
-          while (more > 1 && !(double(s.above + (more - 1) * w) < lim)) --more;
-          while (double(s.above + more * w) < lim) ++more;
-        }
-        cut = {s.key, nth_equal(row, cut, s.key, more)};
-      }
-    }
-    int kept = 0;
-    const auto mass = [&](float x, int v) -> unsigned long long {
-      if (!(x > kNegInf) || !cut.keeps(order_key(x), v)) return 0;
-      if (x != weight.m && weight.real(x) < min_p) return 0;
-      return weight(x);
-    };
-#pragma unroll
-    for (int i = 0; i < kPacks; ++i)
-#pragma unroll
-      for (int e = 0; e < kPerPack<E>; ++e) kept += mass(row.x(i, e), row.id(i, e)) != 0;
-    kept = int(warp_reduce(kept, AddOp()));
-    row.to_all(&sh.frec[row.record()], make_float2(__int_as_float(kept), 0.f));
-    const Found f = find_unit(row, mass, [u](unsigned long long total) {
-      return __umul64hi((unsigned long long)u << 32, total) + 1;
-    });
-    if (row.rank == 0 && row.warp == 0) {
-      int n = 0;
-      for (int i = row.lane; i < row.records(); i += 32) n += __float_as_int(sh.frec[i].x);
-      n = warp_reduce(n, AddOp());
-      if (row.lane == 0) out.put(r, f.id, float(double(f.weight) / double(f.total)), n);
-    }
   }
+  sample_many(row, weight, greedy, top_k, top_p, min_p, u, r, out);
   cluster_sync();   // no block's memory is read any more
 }
 
