@@ -267,6 +267,10 @@ ALR_DEV void bulk_load(uint32_t smem, const void* src, uint32_t bytes, uint64_t*
 ALR_DEV void cluster_arrive() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
+// Without ordering anything: arrive early, where loads are in flight that a release would wait for.
+ALR_DEV void cluster_arrive_relaxed() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
 ALR_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 ALR_DEV void named_bar_arrive(int id, int nthreads) {

@@ -18,10 +18,10 @@ namespace alr {
 namespace {
 
 constexpr int kBins = 2048;              // 11 bits of the key
-constexpr int kCandBlock = 1024;         // candidates that a block collects at most
-constexpr int kCandAll = 2048;           // and a cluster
+constexpr int kCandMost = 1024;          // candidates of a row
 constexpr int kCandSort = 256;           // up to here an entry's place is counted, beyond they are sorted
-constexpr int kListMost = 2 * kTopMost + 3 * kRowWarpsMost * kRowClusterMost;
+constexpr int kListMost = kTopMost + 2 * kRowWarpsMost * kRowClusterMost;
+constexpr int kListCount = 256;          // a list that long is ranked by counting, a longer one by histogram
 constexpr int kWarpsMost = kRowWarpsMost * kRowClusterMost;
 
 // An entry: larger is earlier in the order.
@@ -41,7 +41,9 @@ struct Cut {
 struct Shared {
   union {
     struct {
-      unsigned long long all[kCandAll];   // first block: the cluster's candidates, sorted
+      unsigned long long all[kCandMost];  // first block: the candidates in order
+      unsigned long long w[kTopMost];     // their weights
+      unsigned long long before[kTopMost];
       float list[kListMost];              // largest logits of the warps' threads
     } few;
     struct {
@@ -49,18 +51,18 @@ struct Shared {
       unsigned long long total[kBins];    // over the cluster
     } many;
   };
-  unsigned long long cand[kCandBlock];
+  unsigned long long cand[kCandMost];     // first block: the row's candidates
   uint32_t small[256];                    // histogram of the list's keys
   unsigned long long rec[kWarpsMost];     // of each warp of the cluster: a sum
   float2 frec[kWarpsMost];
   float fbuf[32];                         // and the bound's result
   unsigned long long lbuf[32];
   int ibuf[32];
-  int n_cand, n_block[kRowClusterMost];
+  int n_cand;                             // first block: their number, more than kCandMost: too many
   float top;
   uint32_t digit, reach;
   unsigned long long above, found, kept;
-  int flag;
+  int kept_n;
 };
 
 ALR_DEV float max3_nan(float a, float b, float c) {
@@ -75,6 +77,7 @@ struct Row {
   uint4 raw[kPacks];
   RowPlace<E, kPacks> at;
   int V, rank, cluster, warp, lane, n_warps;
+  float most;   // largest element that the thread holds (from row_bound on)
   Shared& sh;
 
   ALR_DEV Row(const E* z, long long start, int V_, int cluster_, Shared& s)
@@ -94,7 +97,7 @@ struct Row {
 #pragma unroll
       for (int i = 0; i < kPacks; ++i) raw[i] = load_pack(z, at.elem(i), V);
     }
-    cluster_arrive();   // row_bound waits: the other blocks run, their shared memory is there
+    cluster_arrive_relaxed();   // row_bound waits: the other blocks run, their shared memory is there
   }
   ALR_DEV float x(int i, int e) const { return pack_elem<E>(raw[i], e); }
   ALR_DEV int id(int i, int e) const { return at.elem(i) + e; }
@@ -358,9 +361,15 @@ ALR_DEV Bound row_bound(Row<E, kPacks>& row, int K) {
   float t = kNegInf;
 #pragma unroll
   for (int i = 0; i < kPacks; ++i) t = fmaxf(t, row.pack_max(i));
+  row.most = t;
   // the `per` largest of the warp's 32, into all blocks' lists
-  const int n_rec = row.records();
-  const int per = K > 1 ? min(32, 2 * ((K + n_rec - 1) / n_rec) + 1) : 1;
+  const int n_rec = row.records(), tid = threadIdx.x, threads = blockDim.x;
+  const int per = K > 1 ? min(32, (K + n_rec - 1) / n_rec + 1) : 1, n = n_rec * per;
+  if (tid == 0) {
+    sh.n_cand = 0;
+    sh.found = 0;
+  }
+  for (int i = tid; i < 256; i += threads) sh.small[i] = 0;
   cluster_wait();
   for (int j = 0; j < per; ++j) {
     const float m = warp_max(t);
@@ -368,18 +377,35 @@ ALR_DEV Bound row_bound(Row<E, kPacks>& row, int K) {
     const unsigned who = __ballot_sync(0xffffffffu, t == m);
     if (row.lane == __ffs(who) - 1) t = kNegInf;
   }
-  if (threadIdx.x == 0) sh.n_cand = 0;
-  for (int i = threadIdx.x; i < 256; i += blockDim.x) sh.small[i] = 0;
   cluster_sync();
-  const int n = n_rec * per;
   float top = kNegInf;
   for (int i = row.lane; i < n_rec; i += 32) top = fmaxf(top, sh.few.list[i * per]);
   top = warp_max(top);
   if (K <= 1) return {K == 1 ? top : kNegInf, top};
-  // The upper half of the list's K-th largest key, 8 bits at a time.
+  if (n <= kListCount) {
+    // an entry's place is the number of entries before it; groups of threads count a share each
+    const int groups = max(1, threads / n), share = (n + groups - 1) / groups;
+    for (int w = tid; w < n * groups; w += threads) {
+      const int i = w % n, from = w / n * share, to = min(n, from + share);
+      const float v = sh.few.list[i];
+      uint32_t place = 0;
+#pragma unroll 8
+      for (int j = from; j < to; ++j) {
+        const float o = sh.few.list[j];
+        place += o > v || (o == v && j < i);
+      }
+      if (place != 0) atomicAdd(&sh.small[i], place);
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += threads)
+      if (sh.small[i] == uint32_t(K - 1)) sh.digit = __float_as_uint(sh.few.list[i]);
+    __syncthreads();
+    return {K <= n ? __uint_as_float(sh.digit) : kNegInf, top};
+  }
+  // the upper half of the K-th largest key, 8 bits at a time
   uint32_t prefix = 0, reach = uint32_t(K);
   for (int shift = 24; shift >= 16; shift -= 8) {
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    for (int i = tid; i < n; i += threads) {
       const float v = sh.few.list[i];
       const uint32_t key = order_key(v);
       if (v > kNegInf && (shift == 24 || key >> 24 == prefix >> 24))
@@ -409,7 +435,7 @@ ALR_DEV Bound row_bound(Row<E, kPacks>& row, int K) {
     if (sh.digit == 0xffffffffu) return {kNegInf, top};
     prefix |= sh.digit << shift;
     reach = sh.reach;
-    for (int i = threadIdx.x; i < 256; i += blockDim.x) sh.small[i] = 0;
+    for (int i = tid; i < 256; i += threads) sh.small[i] = 0;
     __syncthreads();
   }
   return {key_value(prefix), top};
@@ -423,71 +449,59 @@ ALR_DEV float pack_elem_at(const uint4& r, int e) {
   return __uint_as_float(sizeof(E) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16);
 }
 
-// Collects the entries that take(x, id) wants, of those that reach `least`, in the blocks' lists, and says
-// how many the cluster has; -1: more than fit.
+// Sends the entries that take(x, id) wants, of those that reach `least`, to the cluster's first block.
+// After the cluster_sync in it the first block has them, `n_cand` in number.
 template <typename E, int kPacks, typename F>
-ALR_DEV int collect(Row<E, kPacks>& row, float least, F take) {
+ALR_DEV void collect(Row<E, kPacks>& row, float least, F take) {
   Shared& sh = row.sh;
+  if (row.most >= least && row.most > kNegInf) {
+    const uint32_t count = cluster_smem_addr(&sh.n_cand, 0);
 #pragma unroll
-  for (int i = 0; i < kPacks; ++i) {
-    float m = kNegInf;
+    for (int i = 0; i < kPacks; ++i) {
+      float m = kNegInf;
 #pragma unroll
-    for (int e = 0; e < kPerPack<E>; e += 2) m = max3(m, row.x(i, e), row.x(i, e + 1));
-    if (!(m >= least) || !(m > kNegInf)) continue;
-#pragma unroll 1
-    for (int e = 0; e < kPerPack<E>; ++e) {
-      const float x = pack_elem_at<E>(row.raw[i], e);
-      if (!(x >= least) || !(x > kNegInf) || !take(x, row.id(i, e))) continue;
-      const int at = atomicAdd(&sh.n_cand, 1);
-      if (at < kCandBlock) sh.cand[at] = entry(order_key(x), row.id(i, e));
+      for (int e = 0; e < kPerPack<E>; e += 2) m = max3(m, row.x(i, e), row.x(i, e + 1));
+      if (!(m >= least) || !(m > kNegInf)) continue;
+      uint32_t bits = 0;
+#pragma unroll
+      for (int e = 0; e < kPerPack<E>; ++e)
+        bits |= uint32_t(row.x(i, e) >= least && row.x(i, e) > kNegInf) << e;
+      for (; bits != 0; bits &= bits - 1) {
+        const int e = __ffs(bits) - 1;
+        const float x = pack_elem_at<E>(row.raw[i], e);
+        if (!take(x, row.id(i, e))) continue;
+        int at;
+        asm volatile("atom.shared::cluster.add.s32 %0, [%1], 1;" : "=r"(at) : "r"(count) : "memory");
+        if (at < kCandMost)
+          asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_smem_addr(&sh.cand[at], 0)),
+                       "l"(entry(order_key(x), row.id(i, e)))
+                       : "memory");
+      }
     }
   }
-  __syncthreads();
-  if (row.warp == 0) row.to_all(&sh.n_block[row.rank], sh.n_cand);
   cluster_sync();
-  int all = 0;
-  bool fits = true;
-  for (int c = 0; c < row.cluster; ++c) {
-    fits = fits && sh.n_block[c] <= kCandBlock;
-    all += sh.n_block[c];
-  }
-  return fits && all <= kCandAll ? all : -1;
 }
 
-// First block: the cluster's n candidates into its own memory; after it and a cluster_sync the other
-// blocks are not needed any more.
+// How many candidates the row has, known to all blocks.  The others then wait in the cluster barrier
+// until all have read it; the first block arrives at once and waits (cluster_wait) when it is done.
 template <typename E, int kPacks>
-ALR_DEV void gather_candidates(Row<E, kPacks>& row, int n) {
-  Shared& sh = row.sh;
-  if (row.rank != 0) return;
-  unsigned long long* to = sh.few.all + (n <= kCandSort ? kCandSort : 0);
-  int base = 0;
-  for (int c = 0; c < row.cluster; ++c) {
-    const int m = sh.n_block[c];
-    for (int i = threadIdx.x; i < m; i += blockDim.x) {
-      unsigned long long v;
-      asm volatile("ld.shared::cluster.u64 %0, [%1];"
-                   : "=l"(v)
-                   : "r"(cluster_smem_addr(&sh.cand[i], c))
-                   : "memory");
-      to[base + i] = v;
-    }
-    base += m;
-  }
+ALR_DEV int candidates(Row<E, kPacks>& row) {
+  const int n = ld_cluster_s32(cluster_smem_addr(&row.sh.n_cand, 0));
+  cluster_arrive();
+  if (row.rank != 0 || n > kCandMost) cluster_wait();
+  return n;
 }
 
-// First block: the gathered candidates in order, in few.all.
+// First block: the n candidates in order, in few.all.
 ALR_DEV void sort_candidates(Shared& sh, int n) {
   const int tid = threadIdx.x, threads = blockDim.x;
   unsigned long long* to = sh.few.all;
-  __syncthreads();
   if (n <= kCandSort) {
-    const unsigned long long* raw = to + kCandSort;
     for (int i = tid; i < n; i += threads) {
-      const unsigned long long v = raw[i];
+      const unsigned long long v = sh.cand[i];
       int place = 0;
 #pragma unroll 8
-      for (int j = 0; j < n; ++j) place += raw[j] > v;
+      for (int j = 0; j < n; ++j) place += sh.cand[j] > v;
       to[place] = v;
     }
     __syncthreads();
@@ -495,7 +509,7 @@ ALR_DEV void sort_candidates(Shared& sh, int n) {
   }
   int size = 2 * kCandSort;
   while (size < n) size *= 2;
-  for (int i = n + tid; i < size; i += threads) to[i] = 0ull;
+  for (int i = tid; i < size; i += threads) to[i] = i < n ? sh.cand[i] : 0ull;
   __syncthreads();
   for (int k = 2; k <= size; k *= 2)
     for (int j = k / 2; j > 0; j /= 2) {
@@ -521,17 +535,18 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
   const long long r = cluster_id_x();
   Row<E, kPacks> row(Z + r * ldz, r * ldz, V, cluster, sh);
   const Bound bound = row_bound(row, K);
-  int n = collect(row, bound.least, [](float, int) { return true; });
+  collect(row, bound.least, [](float, int) { return true; });
+  int n = candidates(row);
   Cut cut{0u, -1};
-  if (n < 0) {   // more than fit reach the bound: find the exact cut
-    cluster_sync();
+  if (n > kCandMost) {   // more than fit reach the bound: find the exact cut
     Row<E, kPacks> copy = row;
     cut = cut_top_k(copy, K);
     if (threadIdx.x == 0) sh.n_cand = 0;
-    __syncthreads();
-    n = collect(row, key_value(cut.key), [&](float x, int v) { return cut.keeps(order_key(x), v); });
+    cluster_sync();
+    collect(row, key_value(cut.key), [&](float x, int v) { return cut.keeps(order_key(x), v); });
+    n = candidates(row);
   }
-  gather_candidates(row, n);
+  if (row.rank == 0) cluster_wait();   // the records below go over the cluster
   // the others' sums, each warp's from its own largest; the candidates are the first block's
   const float k = inv_t * kLog2e, least = cut.last >= 0 ? key_value(cut.key) : bound.least;
   float m = kNegInf;
@@ -623,42 +638,70 @@ struct SampleOut {
   }
 };
 
-// First block: draws from the n first tokens of the row, in order in few.all.
+// First block: draws from the n <= kTopMost first tokens of the row, in order in few.all.
 ALR_DEV void draw_from_candidates(Shared& sh, int n, const Weight& weight, float top_p, float min_p,
                                   uint32_t u, long long r, const SampleOut& out) {
-  const int tid = threadIdx.x, threads = blockDim.x;
-  unsigned long long* w = sh.few.all + kTopMost;   // weights, in order
-  unsigned long long sum = 0;
+  const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31;
+  unsigned long long* w = sh.few.w;
   for (int i = tid; i < n; i += threads) {
     w[i] = weight(key_value(entry_key(sh.few.all[i])));
-    sum += w[i];
+    sh.few.before[i] = 0;
   }
-  sum = block_reduce(sum, AddOp(), sh.lbuf);
-  const double lim = double(top_p) * double(sum);
-  int kept = 0;   // tokens kept: a prefix
-  for (int i = tid; i < n; i += threads) {
-    unsigned long long before = 0;
-    if (top_p < 1.f)
-#pragma unroll 8
-      for (int j = 0; j < i; ++j) before += w[j];
-    const float x = key_value(entry_key(sh.few.all[i]));
-    kept += w[i] > 0 && (i == 0 || ((top_p >= 1.f || double(before) < lim) &&
-                                    (x == weight.m || weight.real(x) >= min_p)));
+  __syncthreads();
+  if (tid < 32) {   // lane l: the tokens [8 l, 8 l + 8); kept is a prefix
+    constexpr int kOwn = kTopMost / 32;
+    unsigned long long mine = 0;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j)
+      if (lane * kOwn + j < n) mine += w[lane * kOwn + j];
+    unsigned long long incl = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
+      if (lane >= off) incl += t;
+    }
+    const unsigned long long sum = __shfl_sync(0xffffffffu, incl, 31);
+    const double lim = double(top_p) * double(sum);
+    unsigned long long before = incl - mine, S = 0;
+    int kept = 0;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) {
+      const int i = lane * kOwn + j;
+      if (i >= n || w[i] == 0) break;
+      const float x = key_value(entry_key(sh.few.all[i]));
+      if (i > 0 && !((top_p >= 1.f || double(before) < lim) &&
+                     (x == weight.m || weight.real(x) >= min_p)))
+        break;
+      before += w[i];
+      S += w[i];
+      ++kept;
+    }
+    S = warp_reduce(S, AddOp());
+    kept = warp_reduce(kept, AddOp());
+    if (lane == 0) {
+      sh.kept = S;
+      sh.kept_n = kept;
+    }
   }
-  kept = block_reduce(kept, AddOp(), sh.ibuf);
-  unsigned long long S = 0;
-  for (int i = tid; i < kept; i += threads) S += w[i];
-  S = block_reduce(S, AddOp(), sh.lbuf);
-  const unsigned long long target = __umul64hi((unsigned long long)u << 32, S);
-  for (int i = tid; i < kept; i += threads) {
+  __syncthreads();
+  const int kept = sh.kept_n;
+  const unsigned long long S = sh.kept;
+  // the kept weight before each token in the order of ids; groups of threads add a share each
+  const int groups = max(1, threads / kept), share = (kept + groups - 1) / groups;
+  for (int t = tid; t < kept * groups; t += threads) {
+    const int i = t % kept, from = t / kept * share, to = min(kept, from + share);
     const uint32_t id = uint32_t(entry_id(sh.few.all[i]));
     unsigned long long before = 0;
-#pragma unroll 8
-    for (int j = 0; j < kept; ++j)
+#pragma unroll 4
+    for (int j = from; j < to; ++j)
       before += uint32_t(entry_id(sh.few.all[j])) < id ? w[j] : 0ull;
-    if (before <= target && target < before + w[i])
-      out.put(r, int(id), float(double(w[i]) / double(S)), kept);
+    if (before != 0) atomicAdd(&sh.few.before[i], before);
   }
+  __syncthreads();
+  const unsigned long long target = __umul64hi((unsigned long long)u << 32, S);
+  for (int i = tid; i < kept; i += threads)
+    if (sh.few.before[i] <= target && target < sh.few.before[i] + w[i])
+      out.put(r, entry_id(sh.few.all[i]), float(double(w[i]) / double(S)), kept);
 }
 
 // Even steps of the logit below the largest, kBins over the 32 octaves below which weights are 0.
@@ -738,19 +781,15 @@ ALR_DEV Cut cut_by_steps(Row<E, kPacks>& row, const Cut& cut, const Steps& bin, 
   const int step = int(sh.digit);
   const unsigned long long above = sh.above;
   // that step's tokens, in order
-  const int got = collect(row, kNegInf, [&](float x, int v) {
+  collect(row, kNegInf, [&](float x, int v) {
     return bin(x) == step && worth(x) != 0 && cut.keeps(order_key(x), v);
   });
-  if (got < 0) {   // too many of them
-    cluster_sync();
-    Cut c = cut;
-    const Selected s = select_key(row, c, worth, need);
-    const unsigned long long w = worth(key_value(s.key));
-    unsigned long long more = need.reach(s.above, w);
-    c = {s.key, nth_equal(row, c, s.key, more)};
-    return c;
+  const int got = candidates(row);
+  if (got > kCandMost) {   // too many of them
+    const Selected s = select_key(row, cut, worth, need);
+    return {s.key, nth_equal(row, cut, s.key, need.reach(s.above, worth(key_value(s.key))))};
   }
-  gather_candidates(row, got);
+  if (row.rank == 0) cluster_wait();
   if (row.rank == 0) {
     sort_candidates(sh, got);
     // the last token before which need() asks for more
@@ -845,19 +884,18 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
   }
   const Weight weight{bound.top, greedy ? 0.f : __fdiv_rn(kLog2e, T)};
   if (K > 0) {
-    const int n = collect(row, bound.least, [](float, int) { return true; });
-    if (n >= 0) {
-      gather_candidates(row, n);
-      cluster_sync();   // no other block's memory is read any more
+    collect(row, bound.least, [](float, int) { return true; });
+    const int n = candidates(row);
+    if (n <= kCandMost) {
       if (row.rank != 0) return;
       sort_candidates(sh, n);
       if (!greedy)
         draw_from_candidates(sh, min(n, K), weight, top_p, min_p, u, r, out);
       else if (threadIdx.x == 0)
         out.put(r, entry_id(sh.few.all[0]), 1.f, 1);
+      cluster_wait();   // the others have read n
       return;
     }
-    cluster_sync();
   }
   sample_many(row, weight, greedy, top_k, top_p, min_p, u, r, out);
   cluster_sync();   // no block's memory is read any more
