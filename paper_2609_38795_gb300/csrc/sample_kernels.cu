@@ -20,8 +20,9 @@ namespace {
 constexpr int kBins = 2048;              // 11 bits of the key
 constexpr int kCandMost = 1024;          // candidates of a row
 constexpr int kCandSort = 256;           // up to here an entry's place is counted, beyond they are sorted
+constexpr int kSlots = 4;                // places that a warp has for its candidates without asking
 constexpr int kListMost = kTopMost + 2 * kRowWarpsMost * kRowClusterMost;
-constexpr int kListCount = 256;          // a list that long is ranked by counting, a longer one by histogram
+constexpr int kListWarp = 256;           // a list that long is one warp's work, a longer one the block's
 constexpr int kWarpsMost = kRowWarpsMost * kRowClusterMost;
 
 // An entry: larger is earlier in the order.
@@ -43,7 +44,6 @@ struct Shared {
     struct {
       unsigned long long all[kCandMost];  // first block: the candidates in order
       unsigned long long w[kTopMost];     // their weights
-      unsigned long long before[kTopMost];
       float list[kListMost];              // largest logits of the warps' threads
     } few;
     struct {
@@ -51,14 +51,15 @@ struct Shared {
       unsigned long long total[kBins];    // over the cluster
     } many;
   };
-  unsigned long long cand[kCandMost];     // first block: the row's candidates
+  unsigned long long cand[kCandMost];     // first block: candidates, kSlots places a warp, then more
+  int count[kWarpsMost + 1];              // first block: in each warp's places; then their offsets
   uint32_t small[256];                    // histogram of the list's keys
   unsigned long long rec[kWarpsMost];     // of each warp of the cluster: a sum
   float2 frec[kWarpsMost];
   float fbuf[32];                         // and the bound's result
   unsigned long long lbuf[32];
   int ibuf[32];
-  int n_cand;                             // first block: their number, more than kCandMost: too many
+  int n_more;                             // first block: candidates past the warps' places
   float top;
   uint32_t digit, reach;
   unsigned long long above, found, kept;
@@ -104,7 +105,14 @@ struct Row {
   ALR_DEV int record() const { return rank * n_warps + warp; }
   ALR_DEV int records() const { return cluster * n_warps; }
 
-  // Largest element of a pack; NaN elements become -inf first.
+  // Largest element of a pack.
+  ALR_DEV float largest(int i) const {
+    float m = kNegInf;
+#pragma unroll
+    for (int e = 0; e < kPerPack<E>; e += 2) m = max3(m, x(i, e), x(i, e + 1));
+    return m;
+  }
+  // The same; NaN elements become -inf first.
   ALR_DEV float pack_max(int i) {
     float m = kNegInf;
 #pragma unroll
@@ -120,6 +128,26 @@ struct Row {
       mask_pack<E>(raw[i], bits);
     }
     return m;
+  }
+
+  // A row with +inf logits: they have all the mass, so 0 for them and -inf for the others.
+  ALR_DEV void only_infinite() {
+#pragma unroll 1
+    for (int i = 0; i < kPacks; ++i) {
+      uint4 p = raw[0];
+#pragma unroll
+      for (int j = 1; j < kPacks; ++j)
+        if (j == i) p = raw[j];
+      uint32_t bits = 0;
+#pragma unroll
+      for (int e = 0; e < kPerPack<E>; ++e) bits |= uint32_t(pack_elem<E>(p, e) != -kNegInf) << e;
+      uint4 z = make_uint4(0, 0, 0, 0);
+      mask_pack<E>(z, bits);
+#pragma unroll
+      for (int j = 0; j < kPacks; ++j)
+        if (j == i) raw[j] = z;
+    }
+    most = most == -kNegInf ? 0.f : kNegInf;
   }
 
   // Value `v` of a warp-uniform kind into slot `at` of every block's array.
@@ -142,18 +170,21 @@ struct Row {
 
 // The n-th (from 1) unit of weight f(x, id) >= 0, counted in the order of ids over the whole row: the
 // id of the token that holds it, that token's weight and the sum of all weights.  n(total) gives n.
+// f is 0 for logits below `least`.
 struct Found {
   int id;
   unsigned long long weight, total;
 };
 template <typename E, int kPacks, typename F, typename N>
-ALR_DEV Found find_unit(Row<E, kPacks>& row, F f, N nth) {
+ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
   Shared& sh = row.sh;
   unsigned long long s = 0;
 #pragma unroll
-  for (int i = 0; i < kPacks; ++i)
+  for (int i = 0; i < kPacks; ++i) {
+    if (!(row.largest(i) >= least)) continue;
 #pragma unroll
     for (int e = 0; e < kPerPack<E>; ++e) s += f(row.x(i, e), row.id(i, e));
+  }
   s = warp_reduce(s, AddOp());
   row.to_all(&sh.rec[row.record()], s);
   cluster_sync();
@@ -310,7 +341,7 @@ ALR_DEV Selected select_key(Row<E, kPacks>& row, const Cut& cut, W weight, Need 
 template <typename E, int kPacks>
 ALR_DEV int nth_equal(Row<E, kPacks>& row, const Cut& cut, uint32_t key, unsigned long long n) {
   const Found f = find_unit(
-      row,
+      row, key_value(key),
       [&](float x, int v) -> unsigned long long {
         return x > kNegInf && order_key(x) == key && cut.keeps(key, v);
       },
@@ -365,11 +396,9 @@ ALR_DEV Bound row_bound(Row<E, kPacks>& row, int K) {
   // the `per` largest of the warp's 32, into all blocks' lists
   const int n_rec = row.records(), tid = threadIdx.x, threads = blockDim.x;
   const int per = K > 1 ? min(32, (K + n_rec - 1) / n_rec + 1) : 1, n = n_rec * per;
-  if (tid == 0) {
-    sh.n_cand = 0;
-    sh.found = 0;
-  }
-  for (int i = tid; i < 256; i += threads) sh.small[i] = 0;
+  if (tid == 0) sh.n_more = 0;
+  if (n > kListWarp)
+    for (int i = tid; i < 256; i += threads) sh.small[i] = 0;
   cluster_wait();
   for (int j = 0; j < per; ++j) {
     const float m = warp_max(t);
@@ -382,25 +411,27 @@ ALR_DEV Bound row_bound(Row<E, kPacks>& row, int K) {
   for (int i = row.lane; i < n_rec; i += 32) top = fmaxf(top, sh.few.list[i * per]);
   top = warp_max(top);
   if (K <= 1) return {K == 1 ? top : kNegInf, top};
-  if (n <= kListCount) {
-    // an entry's place is the number of entries before it; groups of threads count a share each
-    const int groups = max(1, threads / n), share = (n + groups - 1) / groups;
-    for (int w = tid; w < n * groups; w += threads) {
-      const int i = w % n, from = w / n * share, to = min(n, from + share);
-      const float v = sh.few.list[i];
-      uint32_t place = 0;
-#pragma unroll 8
-      for (int j = from; j < to; ++j) {
-        const float o = sh.few.list[j];
-        place += o > v || (o == v && j < i);
+  if (n <= kListWarp) {   // the upper half of the K-th largest key, bit by bit
+    if (row.warp == 0) {
+      uint32_t key[kListWarp / 32], least = 0;
+#pragma unroll
+      for (int j = 0; j < kListWarp / 32; ++j) {
+        const int i = j * 32 + row.lane;
+        const float v = i < n ? sh.few.list[i] : kNegInf;
+        key[j] = v > kNegInf ? order_key(v) >> 16 : 0u;
       }
-      if (place != 0) atomicAdd(&sh.small[i], place);
+#pragma unroll 1
+      for (uint32_t bit = 0x8000u; bit != 0; bit >>= 1) {
+        int reach = 0;
+#pragma unroll
+        for (int j = 0; j < kListWarp / 32; ++j)
+          if (j * 32 < n) reach += __popc(__ballot_sync(0xffffffffu, key[j] >= (least | bit)));
+        if (reach >= K) least |= bit;
+      }
+      if (row.lane == 0) sh.digit = least;
     }
     __syncthreads();
-    for (int i = tid; i < n; i += threads)
-      if (sh.small[i] == uint32_t(K - 1)) sh.digit = __float_as_uint(sh.few.list[i]);
-    __syncthreads();
-    return {K <= n ? __uint_as_float(sh.digit) : kNegInf, top};
+    return {sh.digit != 0 ? key_value(sh.digit << 16) : kNegInf, top};
   }
   // the upper half of the K-th largest key, 8 bits at a time
   uint32_t prefix = 0, reach = uint32_t(K);
@@ -449,67 +480,139 @@ ALR_DEV float pack_elem_at(const uint4& r, int e) {
   return __uint_as_float(sizeof(E) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16);
 }
 
-// Sends the entries that take(x, id) wants, of those that reach `least`, to the cluster's first block.
-// After the cluster_sync in it the first block has them, `n_cand` in number.
+// Sends the entries that take(x, id) wants, of those that reach `least`, to the cluster's first block: a
+// warp's first ones into its own places there, more of them to places that it asks for.  All blocks are
+// in step afterwards.
 template <typename E, int kPacks, typename F>
 ALR_DEV void collect(Row<E, kPacks>& row, float least, F take) {
   Shared& sh = row.sh;
-  if (row.most >= least && row.most > kNegInf) {
-    const uint32_t count = cluster_smem_addr(&sh.n_cand, 0);
+  int total = 0;
+  const bool has = row.most >= least && row.most > kNegInf;
+  if (__any_sync(0xffffffffu, has)) {
+    const auto each = [&](auto f) {
+      if (!has) return;
 #pragma unroll
-    for (int i = 0; i < kPacks; ++i) {
-      float m = kNegInf;
+      for (int i = 0; i < kPacks; ++i) {
+        const float m = row.largest(i);
+        if (!(m >= least) || !(m > kNegInf)) continue;
+        uint32_t bits = 0;
 #pragma unroll
-      for (int e = 0; e < kPerPack<E>; e += 2) m = max3(m, row.x(i, e), row.x(i, e + 1));
-      if (!(m >= least) || !(m > kNegInf)) continue;
-      uint32_t bits = 0;
-#pragma unroll
-      for (int e = 0; e < kPerPack<E>; ++e)
-        bits |= uint32_t(row.x(i, e) >= least && row.x(i, e) > kNegInf) << e;
-      for (; bits != 0; bits &= bits - 1) {
-        const int e = __ffs(bits) - 1;
-        const float x = pack_elem_at<E>(row.raw[i], e);
-        if (!take(x, row.id(i, e))) continue;
-        int at;
-        asm volatile("atom.shared::cluster.add.s32 %0, [%1], 1;" : "=r"(at) : "r"(count) : "memory");
-        if (at < kCandMost)
-          asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_smem_addr(&sh.cand[at], 0)),
-                       "l"(entry(order_key(x), row.id(i, e)))
-                       : "memory");
+        for (int e = 0; e < kPerPack<E>; ++e)
+          bits |= uint32_t(row.x(i, e) >= least && row.x(i, e) > kNegInf) << e;
+        for (; bits != 0; bits &= bits - 1) {
+          const int e = __ffs(bits) - 1;
+          const float x = pack_elem_at<E>(row.raw[i], e);
+          if (take(x, row.id(i, e))) f(entry(order_key(x), row.id(i, e)));
+        }
       }
+    };
+    int mine = 0;
+    unsigned long long first = 0;
+    each([&](unsigned long long e) {
+      if (mine++ == 0) first = e;
+    });
+    int at = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, at, off);
+      if (row.lane >= off) at += o;
     }
+    total = __shfl_sync(0xffffffffu, at, 31);
+    at -= mine;
+    int more = 0;
+    if (total > kSlots) {
+      if (row.lane == 0)
+        asm volatile("atom.shared::cluster.add.s32 %0, [%1], %2;"
+                     : "=r"(more)
+                     : "r"(cluster_smem_addr(&sh.n_more, 0)), "r"(total - kSlots)
+                     : "memory");
+      more = __shfl_sync(0xffffffffu, more, 0) + row.records() * kSlots - kSlots;
+    }
+    const auto send = [&](unsigned long long e) {
+      const int to = at < kSlots ? row.record() * kSlots + at : more + at;
+      if (to < kCandMost)
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_smem_addr(&sh.cand[to], 0)), "l"(e)
+                     : "memory");
+      ++at;
+    };
+    if (mine == 1)
+      send(first);
+    else if (mine > 1)
+      each(send);
   }
+  if (row.lane == 0)
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(
+                     cluster_smem_addr(&sh.count[row.record()], 0)),
+                 "r"(min(total, kSlots))
+                 : "memory");
   cluster_sync();
 }
 
-// How many candidates the row has, known to all blocks.  The others then wait in the cluster barrier
-// until all have read it; the first block arrives at once and waits (cluster_wait) when it is done.
+// Whether all candidates fit, known to all blocks.  The others then wait in the cluster barrier until all
+// have read it; the first block arrives at once and waits (cluster_wait) when it is done.
 template <typename E, int kPacks>
-ALR_DEV int candidates(Row<E, kPacks>& row) {
-  const int n = ld_cluster_s32(cluster_smem_addr(&row.sh.n_cand, 0));
+ALR_DEV bool candidates_fit(Row<E, kPacks>& row) {
+  const int n = row.rank == 0 ? row.sh.n_more : ld_cluster_s32(cluster_smem_addr(&row.sh.n_more, 0));
+  const bool fit = row.records() * kSlots + n <= kCandMost;
   cluster_arrive();
-  if (row.rank != 0 || n > kCandMost) cluster_wait();
-  return n;
+  if (row.rank != 0 || !fit) cluster_wait();
+  return fit;
 }
 
-// First block: the n candidates in order, in few.all.
-ALR_DEV void sort_candidates(Shared& sh, int n) {
-  const int tid = threadIdx.x, threads = blockDim.x;
-  unsigned long long* to = sh.few.all;
+// First block: the candidates in order, in few.all; returns their number.
+template <typename E, int kPacks>
+ALR_DEV int sort_candidates(Row<E, kPacks>& row) {
+  Shared& sh = row.sh;
+  const int tid = threadIdx.x, threads = blockDim.x, n_rec = row.records();
+  if (row.warp == 0) {   // offsets of the warps' places: lane l has the records [4 l, 4 l + 4)
+    static_assert(kWarpsMost <= 128, "four records a lane");
+    int c[4], mine = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      c[j] = row.lane * 4 + j < n_rec ? sh.count[row.lane * 4 + j] : 0;
+      mine += c[j];
+    }
+    int at = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, at, off);
+      if (row.lane >= off) at += o;
+    }
+    if (row.lane == 31) sh.kept_n = at;
+    at -= mine;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (row.lane * 4 + j < n_rec) sh.count[row.lane * 4 + j] = at;
+      at += c[j];
+    }
+    if (row.lane == 31) sh.count[n_rec] = sh.kept_n;
+  }
+  __syncthreads();
+  const int base = sh.count[n_rec], n = base + sh.n_more;
+  unsigned long long *to = sh.few.all, *raw = n <= kCandSort ? to + kCandSort : to;
+  for (int i = tid; i < n_rec * kSlots; i += threads) {
+    const int w = i / kSlots, j = i % kSlots;
+    if (sh.count[w] + j < sh.count[w + 1]) raw[sh.count[w] + j] = sh.cand[i];
+  }
+  for (int i = tid; i < sh.n_more; i += threads) raw[base + i] = sh.cand[n_rec * kSlots + i];
   if (n <= kCandSort) {
-    for (int i = tid; i < n; i += threads) {
-      const unsigned long long v = sh.cand[i];
+    __syncthreads();
+    // eight lanes count for an entry
+    for (int i0 = 0; i0 < n; i0 += threads / 8) {
+      const int i = i0 + tid / 8;
+      const unsigned long long v = i < n ? raw[i] : 0ull;
       int place = 0;
-#pragma unroll 8
-      for (int j = 0; j < n; ++j) place += sh.cand[j] > v;
-      to[place] = v;
+      for (int j = tid & 7; j < n; j += 8) place += raw[j] > v;
+#pragma unroll
+      for (int off = 4; off > 0; off >>= 1) place += __shfl_xor_sync(0xffffffffu, place, off);
+      if ((tid & 7) == 0 && i < n) to[place] = v;
     }
     __syncthreads();
-    return;
+    return n;
   }
   int size = 2 * kCandSort;
   while (size < n) size *= 2;
-  for (int i = tid; i < size; i += threads) to[i] = i < n ? sh.cand[i] : 0ull;
+  for (int i = n + tid; i < size; i += threads) to[i] = 0ull;
   __syncthreads();
   for (int k = 2; k <= size; k *= 2)
     for (int j = k / 2; j > 0; j /= 2) {
@@ -523,6 +626,7 @@ ALR_DEV void sort_candidates(Shared& sh, int n) {
       }
       __syncthreads();
     }
+  return n;
 }
 
 // ---------------------------------------------------------------- top logits ---
@@ -536,15 +640,14 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
   Row<E, kPacks> row(Z + r * ldz, r * ldz, V, cluster, sh);
   const Bound bound = row_bound(row, K);
   collect(row, bound.least, [](float, int) { return true; });
-  int n = candidates(row);
   Cut cut{0u, -1};
-  if (n > kCandMost) {   // more than fit reach the bound: find the exact cut
+  if (!candidates_fit(row)) {   // more than fit reach the bound: find the exact cut
     Row<E, kPacks> copy = row;
     cut = cut_top_k(copy, K);
-    if (threadIdx.x == 0) sh.n_cand = 0;
+    if (threadIdx.x == 0) sh.n_more = 0;
     cluster_sync();
     collect(row, key_value(cut.key), [&](float x, int v) { return cut.keeps(order_key(x), v); });
-    n = candidates(row);
+    candidates_fit(row);
   }
   if (row.rank == 0) cluster_wait();   // the records below go over the cluster
   // the others' sums, each warp's from its own largest; the candidates are the first block's
@@ -585,7 +688,7 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
   row.to_all(&sh.frec[row.record()], make_float2(m, s));
   cluster_sync();   // no other block's memory is read any more
   if (row.rank == 0) {
-    sort_candidates(sh, n);
+    const int n = sort_candidates(row);
     const int tid = threadIdx.x, threads = blockDim.x, got = min(n, K);
     for (int i = tid; i < K; i += threads) {
       top_val[r * K + i] = i < got ? key_value(entry_key(sh.few.all[i])) : kNegInf;
@@ -623,7 +726,13 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
 struct Weight {
   float m, c;
   // exp2f and ex2.approx agree where the weight is not 0 (every float of [-64, 0] was compared)
-  ALR_DEV float real(float x) const { return x == m ? 1.f : ex2(__fmul_rn(__fsub_rn(x, m), c)); }
+  ALR_DEV float real(float x) const { return ex2(__fmul_rn(__fsub_rn(x, m), c)); }
+  // Logits below have a real weight under w (and above: not certainly over it); with a margin for the
+  // rounding of the three steps.
+  ALR_DEV float below(float w) const {
+    const float d = (log2f(w) - 0.01f) / c;
+    return d == d ? m + d - 1e-6f * fabsf(m) : kNegInf;
+  }
   ALR_DEV uint32_t operator()(float x) const { return __float2uint_rz(real(x) * 2147483648.f); }
 };
 
@@ -643,17 +752,16 @@ ALR_DEV void draw_from_candidates(Shared& sh, int n, const Weight& weight, float
                                   uint32_t u, long long r, const SampleOut& out) {
   const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31;
   unsigned long long* w = sh.few.w;
-  for (int i = tid; i < n; i += threads) {
-    w[i] = weight(key_value(entry_key(sh.few.all[i])));
-    sh.few.before[i] = 0;
-  }
+  for (int i = tid; i < n; i += threads) w[i] = weight(key_value(entry_key(sh.few.all[i])));
   __syncthreads();
   if (tid < 32) {   // lane l: the tokens [8 l, 8 l + 8); kept is a prefix
     constexpr int kOwn = kTopMost / 32;
-    unsigned long long mine = 0;
+    unsigned long long own[kOwn], mine = 0;
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j)
-      if (lane * kOwn + j < n) mine += w[lane * kOwn + j];
+    for (int j = 0; j < kOwn; ++j) {
+      own[j] = lane * kOwn + j < n ? w[lane * kOwn + j] : 0ull;
+      mine += own[j];
+    }
     unsigned long long incl = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -661,23 +769,24 @@ ALR_DEV void draw_from_candidates(Shared& sh, int n, const Weight& weight, float
       if (lane >= off) incl += t;
     }
     const unsigned long long sum = __shfl_sync(0xffffffffu, incl, 31);
-    const double lim = double(top_p) * double(sum);
+    // the sum before a token, a whole number, is below top_p sum: below that number rounded up
+    const unsigned long long lim =
+        top_p >= 1.f ? ~0ull : (unsigned long long)ceil(fmax(double(top_p), 0.0) * double(sum));
     unsigned long long before = incl - mine, S = 0;
     int kept = 0;
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       const int i = lane * kOwn + j;
-      if (i >= n || w[i] == 0) break;
-      const float x = key_value(entry_key(sh.few.all[i]));
-      if (i > 0 && !((top_p >= 1.f || double(before) < lim) &&
-                     (x == weight.m || weight.real(x) >= min_p)))
-        break;
-      before += w[i];
-      S += w[i];
-      ++kept;
+      const bool keep = own[j] != 0 && (i == 0 || (before < lim &&
+                        weight.real(key_value(entry_key(sh.few.all[min(i, n - 1)]))) >= min_p));
+      before += own[j];
+      if (keep) {
+        S += own[j];
+        ++kept;
+      }
     }
     S = warp_reduce(S, AddOp());
-    kept = warp_reduce(kept, AddOp());
+    kept = __reduce_add_sync(0xffffffffu, kept);
     if (lane == 0) {
       sh.kept = S;
       sh.kept_n = kept;
@@ -685,58 +794,58 @@ ALR_DEV void draw_from_candidates(Shared& sh, int n, const Weight& weight, float
   }
   __syncthreads();
   const int kept = sh.kept_n;
-  const unsigned long long S = sh.kept;
-  // the kept weight before each token in the order of ids; groups of threads add a share each
-  const int groups = max(1, threads / kept), share = (kept + groups - 1) / groups;
-  for (int t = tid; t < kept * groups; t += threads) {
-    const int i = t % kept, from = t / kept * share, to = min(kept, from + share);
-    const uint32_t id = uint32_t(entry_id(sh.few.all[i]));
+  const unsigned long long S = sh.kept, target = __umul64hi((unsigned long long)u << 32, S);
+  // the kept weight before each token in the order of ids: eight lanes add it up
+  for (int i0 = 0; i0 < kept; i0 += threads / 8) {
+    const int i = i0 + tid / 8;
+    const uint32_t id = i < kept ? uint32_t(entry_id(sh.few.all[i])) : 0u;
     unsigned long long before = 0;
-#pragma unroll 4
-    for (int j = from; j < to; ++j)
+    for (int j = tid & 7; j < kept; j += 8)
       before += uint32_t(entry_id(sh.few.all[j])) < id ? w[j] : 0ull;
-    if (before != 0) atomicAdd(&sh.few.before[i], before);
+#pragma unroll
+    for (int off = 4; off > 0; off >>= 1) before += __shfl_xor_sync(0xffffffffu, before, off);
+    if ((tid & 7) == 0 && i < kept && before <= target && target < before + w[i])
+      out.put(r, int(id), float(double(w[i]) / double(S)), kept);
   }
-  __syncthreads();
-  const unsigned long long target = __umul64hi((unsigned long long)u << 32, S);
-  for (int i = tid; i < kept; i += threads)
-    if (sh.few.before[i] <= target && target < sh.few.before[i] + w[i])
-      out.put(r, entry_id(sh.few.all[i]), float(double(w[i]) / double(S)), kept);
 }
 
 // Even steps of the logit below the largest, kBins over the 32 octaves below which weights are 0.
 struct Steps {
   float top, scale;
   ALR_DEV int operator()(float x) const {
-    return x == top ? 0 : min(kBins - 1, __float2int_rz((top - x) * scale));
+    return min(kBins - 1, __float2int_rz((top - x) * scale));
   }
 };
 
 // The cut that keeps, of the tokens of positive weight that `cut` keeps, the first ones whose summed worth
 // need() still asks for before them (one at least); `cut` itself when need() is content with all of them.
-// worth: 0 .. 2^31 for x, 0 only where the weight is 0.
+// worth: 0 .. 2^31 for x, 0 where the weight is 0, as it is below `least`.
 template <typename E, int kPacks, typename W, typename Need>
-ALR_DEV Cut cut_by_steps(Row<E, kPacks>& row, const Cut& cut, const Steps& bin, W worth, Need need) {
+ALR_DEV Cut cut_by_steps(Row<E, kPacks>& row, const Cut& cut, const Steps& bin, float least, W worth,
+                         Need need) {
   Shared& sh = row.sh;
   const int tid = threadIdx.x, threads = blockDim.x;
   for (int b = tid; b < kBins; b += threads) sh.many.lo[b] = sh.many.hi[b] = 0;
   if (tid == 0) {
-    sh.n_cand = 0;
+    sh.n_more = 0;
     sh.digit = 0xffffffffu;
   }
   __syncthreads();
-#pragma unroll 1
-  for (int i = 0; i < kPacks; ++i)
+  const float lowest = fmaxf(least, key_value(cut.key));
+  const bool cut_any = cut.key != 0;
+#pragma unroll
+  for (int i = 0; i < kPacks; ++i) {
+    if (!(row.largest(i) >= lowest)) continue;
 #pragma unroll
     for (int e = 0; e < kPerPack<E>; ++e) {
       const float x = row.x(i, e);
-      if (!(x > kNegInf)) continue;
       const uint32_t w = worth(x);
-      if (w == 0 || !cut.keeps(order_key(x), row.id(i, e))) continue;
+      if (w == 0 || (cut_any && !cut.keeps(order_key(x), row.id(i, e)))) continue;
       const int b = bin(x);
       if (w & 0xffffu) atomicAdd(&sh.many.lo[b], w & 0xffffu);
       if (w >> 16) atomicAdd(&sh.many.hi[b], w >> 16);
     }
+  }
   cluster_sync();
   const int share = (kBins + row.cluster - 1) / row.cluster;
   for (int b = row.rank * share + tid; b < min(kBins, (row.rank + 1) * share); b += threads) {
@@ -781,17 +890,16 @@ ALR_DEV Cut cut_by_steps(Row<E, kPacks>& row, const Cut& cut, const Steps& bin, 
   const int step = int(sh.digit);
   const unsigned long long above = sh.above;
   // that step's tokens, in order
-  collect(row, kNegInf, [&](float x, int v) {
-    return bin(x) == step && worth(x) != 0 && cut.keeps(order_key(x), v);
+  collect(row, lowest, [&](float x, int v) {
+    return bin(x) == step && worth(x) != 0 && (!cut_any || cut.keeps(order_key(x), v));
   });
-  const int got = candidates(row);
-  if (got > kCandMost) {   // too many of them
+  if (!candidates_fit(row)) {   // too many of them
     const Selected s = select_key(row, cut, worth, need);
     return {s.key, nth_equal(row, cut, s.key, need.reach(s.above, worth(key_value(s.key))))};
   }
   if (row.rank == 0) cluster_wait();
   if (row.rank == 0) {
-    sort_candidates(sh, got);
+    const int got = sort_candidates(row);
     // the last token before which need() asks for more
     const int m = (got + threads - 1) / threads;
     unsigned long long own = 0;
@@ -829,22 +937,26 @@ __device__ __noinline__ void sample_many(Row<E, kPacks> row, const Weight weight
   Shared& sh = row.sh;
   Cut cut{0u, 0x7fffffff};
   const Steps bin{weight.m, weight.c * (kBins / 32)};
+  const float least = weight.below(0x1p-31f);
   if (greedy) {
     cut = cut_top_k(row, 1);
   } else {
     if (top_k > 0 && top_k < row.V)
-      cut = cut_by_steps(row, cut, bin, [&](float x) { return weight(x) != 0 ? 1u : 0u; },
+      cut = cut_by_steps(row, cut, bin, least, [&](float x) { return weight(x) != 0 ? 1u : 0u; },
                          NeedCount{(unsigned long long)top_k});
-    if (top_p < 1.f) cut = cut_by_steps(row, cut, bin, weight, NeedMass{double(top_p), 0.0});
+    if (top_p < 1.f) cut = cut_by_steps(row, cut, bin, least, weight, NeedMass{double(top_p), 0.0});
   }
+  const bool all = cut.key == 0;
+  const float edge = all ? kNegInf : key_value(cut.key);
   const auto mass = [&](float x, int v) -> unsigned long long {
-    if (!(x > kNegInf) || !cut.keeps(order_key(x), v)) return 0;
-    if (x != weight.m && weight.real(x) < min_p) return 0;
-    return weight(x);
+    if (!all && !(x > edge || (x == edge && v <= cut.last))) return 0;
+    const float w = weight.real(x);
+    if (!(w >= min_p) && !(x == weight.m)) return 0;
+    return __float2uint_rz(w * 2147483648.f);
   };
   int kept = 0;
   const Found f = find_unit(
-      row,
+      row, fmaxf(fmaxf(least, edge), min_p > 0.f ? weight.below(min_p) : kNegInf),
       [&](float x, int v) -> unsigned long long {
         const unsigned long long w = mass(x, v);
         kept += w != 0;   // counted in the first sweep; what the search adds is not read
@@ -882,13 +994,14 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
     if (row.rank == 0 && threadIdx.x == 0) out.put(r, -1, 0.f, 0);
     return;
   }
-  const Weight weight{bound.top, greedy ? 0.f : __fdiv_rn(kLog2e, T)};
+  const bool infinite = bound.top == -kNegInf;
+  if (infinite) row.only_infinite();
+  const Weight weight{infinite ? 0.f : bound.top, greedy ? 0.f : __fdiv_rn(kLog2e, T)};
   if (K > 0) {
-    collect(row, bound.least, [](float, int) { return true; });
-    const int n = candidates(row);
-    if (n <= kCandMost) {
+    collect(row, infinite ? 0.f : bound.least, [](float, int) { return true; });
+    if (candidates_fit(row)) {
       if (row.rank != 0) return;
-      sort_candidates(sh, n);
+      const int n = sort_candidates(row);
       if (!greedy)
         draw_from_candidates(sh, min(n, K), weight, top_p, min_p, u, r, out);
       else if (threadIdx.x == 0)
