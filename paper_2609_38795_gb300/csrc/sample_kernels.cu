@@ -20,6 +20,7 @@ namespace {
 constexpr int kBins = 2048;              // 11 bits of the key
 constexpr int kCandMost = 1024;          // candidates of a row
 constexpr int kCandSort = 256;           // up to here an entry's place is counted, beyond they are sorted
+constexpr int kStreamThreads = 512;      // of a block that reads a row by itself
 constexpr int kSlots = 4;                // places that a warp has for its candidates without asking
 constexpr int kListMost = kTopMost + 2 * kRowWarpsMost * kRowClusterMost;
 constexpr int kListWarp = 256;           // a list that long is one warp's work, a longer one the block's
@@ -47,7 +48,7 @@ struct Shared {
       float list[kListMost];              // largest logits of the warps' threads
     } few;
     struct {
-      uint32_t lo[kBins], hi[kBins];      // histogram: sums of the low 16 bits, of the others
+      uint32_t lo[kBins], hi[kBins];      // histogram: sums, and the carries out of them
       unsigned long long total[kBins];    // over the cluster
     } many;
   };
@@ -72,24 +73,131 @@ ALR_DEV float max3_nan(float a, float b, float c) {
   return r;
 }
 
-// The row of a cluster in registers, and what all its threads need to know.
-template <typename E, int kPacks>
-struct Row {
-  uint4 raw[kPacks];
-  RowPlace<E, kPacks> at;
+// Element e of a pack, e not known to the compiler.
+template <typename E>
+ALR_DEV float pack_elem_at(const uint4& r, int e) {
+  const int word = sizeof(E) == 2 ? e >> 1 : e;
+  const uint32_t w = word == 0 ? r.x : word == 1 ? r.y : word == 2 ? r.z : r.w;
+  return __uint_as_float(sizeof(E) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16);
+}
+
+ALR_DEV float pack_largest(const uint4& r, std::integral_constant<int, 2>) {
+  float m = kNegInf;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2)
+    m = max3(m, pack_elem<__nv_bfloat16>(r, e), pack_elem<__nv_bfloat16>(r, e + 1));
+  return m;
+}
+ALR_DEV float pack_largest(const uint4& r, std::integral_constant<int, 4>) {
+  return max3(max3(kNegInf, pack_elem<float>(r, 0), pack_elem<float>(r, 1)), pack_elem<float>(r, 2),
+              pack_elem<float>(r, 3));
+}
+template <typename E>
+ALR_DEV float largest(const uint4& r) {
+  return pack_largest(r, std::integral_constant<int, int(sizeof(E))>{});
+}
+
+// NaN elements of a pack become -inf.
+template <typename E>
+ALR_DEV void clean(uint4& r) {
+  float m = kNegInf;
+#pragma unroll
+  for (int e = 0; e < kPerPack<E>; e += 2)
+    m = max3_nan(m, pack_elem<E>(r, e), pack_elem<E>(r, e + 1));
+  if (m == m) return;
+  uint32_t bits = 0;
+#pragma unroll
+  for (int e = 0; e < kPerPack<E>; ++e) bits |= uint32_t(pack_elem<E>(r, e) != pack_elem<E>(r, e)) << e;
+  mask_pack<E>(r, bits);
+}
+
+// What all threads of a row's cluster need to know.  kSolo: the cluster is one block.
+template <bool kSolo>
+struct RowCommon {
   int V, rank, cluster, warp, lane, n_warps;
-  float most;   // largest element that the thread holds (from row_bound on)
+  float most;      // largest element that the thread holds (from row_bound on)
+  bool infinite;   // the row has +inf logits, which have all the mass: they read as 0, others as -inf
   Shared& sh;
 
-  ALR_DEV Row(const E* z, long long start, int V_, int cluster_, Shared& s)
-      : at(start, int(cluster_ctarank()), int(blockDim.x)),
-        V(V_),
-        rank(int(cluster_ctarank())),
-        cluster(cluster_),
+  ALR_DEV RowCommon(int V_, int cluster_, Shared& s)
+      : V(V_),
+        rank(kSolo ? 0 : int(cluster_ctarank())),
+        cluster(kSolo ? 1 : cluster_),
         warp(int(threadIdx.x) / 32),
         lane(int(threadIdx.x) & 31),
         n_warps(int(blockDim.x) / 32),
-        sh(s) {
+        most(kNegInf),
+        infinite(false),
+        sh(s) {}
+  ALR_DEV int record() const { return rank * n_warps + warp; }
+  ALR_DEV int records() const { return cluster * n_warps; }
+  ALR_DEV void sync() const {
+    if constexpr (kSolo)
+      __syncthreads();
+    else
+      cluster_sync();
+  }
+  // A warp-uniform value into a slot of every block's shared memory.
+  template <typename T>
+  ALR_DEV void to_all(T* slot, T v) const {
+    if constexpr (kSolo) {
+      if (lane == 0) *slot = v;
+    } else if (lane < cluster) {
+      put(cluster_smem_addr(slot, lane), v);
+    }
+  }
+  template <typename T>
+  ALR_DEV void to_first(T* slot, T v) const {
+    if constexpr (kSolo)
+      *slot = v;
+    else
+      put(cluster_smem_addr(slot, 0), v);
+  }
+  template <typename T>
+  ALR_DEV static void put(uint32_t a, T v) {
+    if constexpr (sizeof(T) == 8) {
+      unsigned long long b;
+      memcpy(&b, &v, 8);
+      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(b) : "memory");
+    } else {
+      uint32_t b;
+      memcpy(&b, &v, 4);
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(b) : "memory");
+    }
+  }
+  ALR_DEV int add_first(int* slot, int v) const {
+    if constexpr (kSolo) return atomicAdd(slot, v);
+    int r;
+    asm volatile("atom.shared::cluster.add.s32 %0, [%1], %2;"
+                 : "=r"(r)
+                 : "r"(cluster_smem_addr(slot, 0)), "r"(v)
+                 : "memory");
+    return r;
+  }
+  ALR_DEV uint32_t from(const uint32_t* slot, int block) const {
+    if constexpr (kSolo) return *slot;
+    return uint32_t(ld_cluster_s32(cluster_smem_addr(slot, block)));
+  }
+};
+
+template <typename E>
+ALR_DEV void zero_for_infinite(uint4& r) {
+  uint32_t bits = 0;
+#pragma unroll
+  for (int e = 0; e < kPerPack<E>; ++e) bits |= uint32_t(pack_elem<E>(r, e) != -kNegInf) << e;
+  r = make_uint4(0, 0, 0, 0);
+  mask_pack<E>(r, bits);
+}
+
+// The row in the registers of a cluster: each warp a stretch of it.
+template <typename E_, int kPacks>
+struct Row : RowCommon<false> {
+  using E = E_;
+  uint4 raw[kPacks];
+  RowPlace<E, kPacks> at;
+
+  ALR_DEV Row(const E* z, long long start, int V_, int cluster_, Shared& s)
+      : RowCommon<false>(V_, cluster_, s), at(start, int(cluster_ctarank()), int(blockDim.x)) {
     if (at.whole(V)) {
       const uint4* p = reinterpret_cast<const uint4*>(z + at.elem(0));
 #pragma unroll
@@ -98,73 +206,104 @@ struct Row {
 #pragma unroll
       for (int i = 0; i < kPacks; ++i) raw[i] = load_pack(z, at.elem(i), V);
     }
-    cluster_arrive_relaxed();   // row_bound waits: the other blocks run, their shared memory is there
+    cluster_arrive_relaxed();   // ready() waits: the other blocks run, their shared memory is there
   }
-  ALR_DEV float x(int i, int e) const { return pack_elem<E>(raw[i], e); }
-  ALR_DEV int id(int i, int e) const { return at.elem(i) + e; }
-  ALR_DEV int record() const { return rank * n_warps + warp; }
-  ALR_DEV int records() const { return cluster * n_warps; }
-
-  // Largest element of a pack.
-  ALR_DEV float largest(int i) const {
-    float m = kNegInf;
+  ALR_DEV void ready() const { cluster_wait(); }
+  // f(pack, id of its first element) for the thread's packs, in order; every lane of the warp calls.
+  template <typename F>
+  ALR_DEV void each(F f) {
 #pragma unroll
-    for (int e = 0; e < kPerPack<E>; e += 2) m = max3(m, x(i, e), x(i, e + 1));
-    return m;
+    for (int i = 0; i < kPacks; ++i) f(raw[i], at.elem(i));
   }
-  // The same; NaN elements become -inf first.
-  ALR_DEV float pack_max(int i) {
-    float m = kNegInf;
+  template <typename F>
+  ALR_DEV void each_first(F f) {   // before all others: NaN elements go
 #pragma unroll
-    for (int e = 0; e < kPerPack<E>; e += 2) m = max3_nan(m, x(i, e), x(i, e + 1));
-    if (m != m) {
-      uint32_t bits = 0;
-      m = kNegInf;
-#pragma unroll
-      for (int e = 0; e < kPerPack<E>; ++e) {
-        bits |= uint32_t(x(i, e) != x(i, e)) << e;
-        m = fmaxf(m, x(i, e));
-      }
-      mask_pack<E>(raw[i], bits);
-    }
-    return m;
-  }
-
-  // A row with +inf logits: they have all the mass, so 0 for them and -inf for the others.
-  ALR_DEV void only_infinite() {
-#pragma unroll 1
     for (int i = 0; i < kPacks; ++i) {
-      uint4 p = raw[0];
+      clean<E>(raw[i]);
+      f(raw[i], at.elem(i));
+    }
+  }
+  // The same, packs of all lanes one after another; f returns true to stop (the same in all lanes).
+  template <typename F>
+  ALR_DEV void each_until(F f) {
+    bool stop = false;
+#pragma unroll 1
+    for (int i = 0; i < kPacks && !stop; ++i) {
+      uint4 r = raw[0];
 #pragma unroll
       for (int j = 1; j < kPacks; ++j)
-        if (j == i) p = raw[j];
-      uint32_t bits = 0;
-#pragma unroll
-      for (int e = 0; e < kPerPack<E>; ++e) bits |= uint32_t(pack_elem<E>(p, e) != -kNegInf) << e;
-      uint4 z = make_uint4(0, 0, 0, 0);
-      mask_pack<E>(z, bits);
-#pragma unroll
-      for (int j = 0; j < kPacks; ++j)
-        if (j == i) raw[j] = z;
+        if (j == i) r = raw[j];
+      stop = f(r, at.elem(i));
     }
+  }
+  ALR_DEV void only_infinite() {
+    infinite = true;
+#pragma unroll
+    for (int i = 0; i < kPacks; ++i) zero_for_infinite<E>(raw[i]);
     most = most == -kNegInf ? 0.f : kNegInf;
   }
+};
 
-  // Value `v` of a warp-uniform kind into slot `at` of every block's array.
-  template <typename T>
-  ALR_DEV void to_all(T* slot, T v) const {
-    if (lane < cluster) {
-      const uint32_t a = cluster_smem_addr(slot, lane);
-      if constexpr (sizeof(T) == 8) {
-        unsigned long long b;
-        memcpy(&b, &v, 8);
-        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(b) : "memory");
-      } else {
-        uint32_t b;
-        memcpy(&b, &v, 4);
-        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(b) : "memory");
+// The row read anew (from the second time on, out of L2) by one block: each warp a stretch of it.
+template <typename E_>
+struct StreamRow : RowCommon<true> {
+  using E = E_;
+  static constexpr int kBatch = 8;
+  const E* z;
+  int first, end, off;   // packs of this warp; the row starts `off` elements into pack 0
+
+  ALR_DEV StreamRow(const E* z_, long long start, int V_, Shared& s)
+      : RowCommon<true>(V_, 1, s), z(z_), off(int(start % kPerPack<E>)) {
+    const int packs = (V + off + kPerPack<E> - 1) / kPerPack<E>;
+    const int share = ((packs + n_warps - 1) / n_warps + 31) / 32 * 32;
+    first = min(packs, warp * share);
+    end = min(packs, first + share);
+  }
+  ALR_DEV void ready() const { __syncthreads(); }   // the last row's shared memory is free
+  ALR_DEV void load(uint4 (&raw)[kBatch], int p) const {
+    const int v = p * kPerPack<E> - off;
+    if (v - lane * kPerPack<E> >= 0 &&
+        v + (32 * kBatch - lane) * kPerPack<E> <= V) {   // all of the warp's within the row
+      const uint4* q = reinterpret_cast<const uint4*>(z + v);
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) raw[j] = q[32 * j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) raw[j] = load_pack(z, v + 32 * j * kPerPack<E>, V);
+    }
+  }
+  template <typename F>
+  ALR_DEV void each(F f) {
+    for (int p = first + lane; p - lane < end; p += 32 * kBatch) {
+      uint4 raw[kBatch];
+      load(raw, p);
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        if (p - lane + 32 * j >= end) break;
+        clean<E>(raw[j]);
+        if (infinite) zero_for_infinite<E>(raw[j]);
+        f(raw[j], (p + 32 * j) * kPerPack<E> - off);
       }
     }
+  }
+  template <typename F>
+  ALR_DEV void each_first(F f) {
+    each(f);
+  }
+  template <typename F>
+  ALR_DEV void each_until(F f) {
+    bool stop = false;
+    for (int p = first + lane; p - lane < end && !stop; p += 32) {
+      const int v = p * kPerPack<E> - off;
+      uint4 r = load_pack(z, v, V);
+      clean<E>(r);
+      if (infinite) zero_for_infinite<E>(r);
+      stop = f(r, v);
+    }
+  }
+  ALR_DEV void only_infinite() {
+    infinite = true;
+    most = most == -kNegInf ? 0.f : kNegInf;
   }
 };
 
@@ -175,19 +314,19 @@ struct Found {
   int id;
   unsigned long long weight, total;
 };
-template <typename E, int kPacks, typename F, typename N>
-ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
+template <typename R, typename F, typename N>
+ALR_DEV Found find_unit(R& row, float least, F f, N nth) {
+  using E = typename R::E;
   Shared& sh = row.sh;
   unsigned long long s = 0;
+  row.each([&](const uint4& p, int id) {
+    if (!(largest<E>(p) >= least)) return;
 #pragma unroll
-  for (int i = 0; i < kPacks; ++i) {
-    if (!(row.largest(i) >= least)) continue;
-#pragma unroll
-    for (int e = 0; e < kPerPack<E>; ++e) s += f(row.x(i, e), row.id(i, e));
-  }
+    for (int e = 0; e < kPerPack<E>; ++e) s += f(pack_elem<E>(p, e), id + e);
+  });
   s = warp_reduce(s, AddOp());
   row.to_all(&sh.rec[row.record()], s);
-  cluster_sync();
+  row.sync();
   unsigned long long total = 0, before = 0;
   for (int i = row.lane; i < row.records(); i += 32) {
     const unsigned long long t = sh.rec[i];
@@ -197,17 +336,12 @@ ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
   total = warp_reduce(total, AddOp());
   before = warp_reduce(before, AddOp());
   const unsigned long long n = nth(total);
-  if (before < n && n <= before + s) {   // this warp holds it
-    bool done = false;
-#pragma unroll 1
-    for (int i = 0; i < kPacks && !done; ++i) {
-      uint4 r = row.raw[0];
-#pragma unroll
-      for (int j = 1; j < kPacks; ++j)
-        if (j == i) r = row.raw[j];
+  if (before < n && n <= before + s)   // this warp holds it
+    row.each_until([&](const uint4& p, int id) {
       unsigned long long mine = 0;
+      if (largest<E>(p) >= least)
 #pragma unroll
-      for (int e = 0; e < kPerPack<E>; ++e) mine += f(pack_elem<E>(r, e), row.id(i, e));
+        for (int e = 0; e < kPerPack<E>; ++e) mine += f(pack_elem<E>(p, e), id + e);
       unsigned long long incl = mine;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
@@ -215,33 +349,56 @@ ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
         if (row.lane >= off) incl += t;
       }
       const unsigned long long all = __shfl_sync(0xffffffffu, incl, 31);
-      if (n <= before + all) {
-        unsigned long long run = before + incl - mine, w = 0;
-        int id = -1;
+      if (n > before + all) {
+        before += all;
+        return false;
+      }
+      unsigned long long run = before + incl - mine, w = 0;
+      int at = -1;
+      if (run < n && n <= run + mine)
 #pragma unroll
         for (int e = 0; e < kPerPack<E>; ++e) {
-          const unsigned long long t = f(pack_elem<E>(r, e), row.id(i, e));
-          if (id < 0 && run < n && n <= run + t) {
-            id = row.id(i, e);
+          const unsigned long long t = f(pack_elem<E>(p, e), id + e);
+          if (at < 0 && run < n && n <= run + t) {
+            at = id + e;
             w = t;
           }
           run += t;
         }
-        const unsigned got = __ballot_sync(0xffffffffu, id >= 0);
-        const int src = __ffs(got) - 1;
-        id = __shfl_sync(0xffffffffu, id, src & 31);
-        w = __shfl_sync(0xffffffffu, w, src & 31);
-        row.to_all(&sh.found, (unsigned long long)uint32_t(id));
-        row.to_all(&sh.kept, w);
-        done = true;
-      }
-      before += all;
+      const int src = (__ffs(__ballot_sync(0xffffffffu, at >= 0)) - 1) & 31;
+      row.to_all(&sh.found, (unsigned long long)uint32_t(__shfl_sync(0xffffffffu, at, src)));
+      row.to_all(&sh.kept, __shfl_sync(0xffffffffu, w, src));
+      return true;
+    });
+  row.sync();
+  const Found r{int(uint32_t(sh.found)), sh.kept, total};
+  row.sync();   // before `found` and `rec` are written again
+  return r;
+}
+
+// A weight (up to 2^31) into its bin: 32 bits of the sum and a count of the carries.
+ALR_DEV void add_bin(Shared& sh, uint32_t b, uint32_t w) {
+  if (atomicAdd(&sh.many.lo[b], w) + w < w) atomicAdd(&sh.many.hi[b], 1u);
+}
+
+// many.total of all blocks from the blocks' histograms; each block adds up a share of the bins.
+template <typename R>
+ALR_DEV void total_bins(R& row, int bins) {
+  Shared& sh = row.sh;
+  const int share = (bins + row.cluster - 1) / row.cluster;
+  for (int b = row.rank * share + int(threadIdx.x); b < min(bins, (row.rank + 1) * share);
+       b += blockDim.x) {
+    unsigned long long t = 0;
+    for (int c = 0; c < row.cluster; ++c)
+      t += row.from(&sh.many.lo[b], c) + ((unsigned long long)row.from(&sh.many.hi[b], c) << 32);
+    for (int c = 0; c < row.cluster; ++c) {
+      if (row.cluster == 1)
+        sh.many.total[b] = t;
+      else
+        R::put(cluster_smem_addr(&sh.many.total[b], c), t);
     }
   }
-  cluster_sync();
-  const Found r{int(uint32_t(sh.found)), sh.kept, total};
-  cluster_sync();   // before `found` and `rec` are written again
-  return r;
+  row.sync();
 }
 
 // Radix select among the tokens that `cut` keeps: the largest key at which the summed weights, from
@@ -251,8 +408,9 @@ struct Selected {
   uint32_t key;
   unsigned long long above, total;   // sums over larger keys, over all
 };
-template <typename E, int kPacks, typename W, typename Need>
-ALR_DEV Selected select_key(Row<E, kPacks>& row, const Cut& cut, W weight, Need need) {
+template <typename R, typename W, typename Need>
+ALR_DEV Selected select_key(R& row, const Cut& cut, W weight, Need need) {
+  using E = typename R::E;
   Shared& sh = row.sh;
   // a bf16 key is in the upper 16 bits, the low ones follow from the sign
   constexpr int kLevels = sizeof(E) == 2 ? 2 : 3;
@@ -266,34 +424,20 @@ ALR_DEV Selected select_key(Row<E, kPacks>& row, const Cut& cut, W weight, Need 
     const int bins = int(mask) + 1;
     for (int b = tid; b < bins; b += threads) sh.many.lo[b] = sh.many.hi[b] = 0;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kPacks; ++i)
-#pragma unroll
+    row.each([&](const uint4& p, int id) {
+#pragma unroll 1
       for (int e = 0; e < kPerPack<E>; ++e) {
-        const float x = row.x(i, e);
+        const float x = pack_elem_at<E>(p, e);
         if (!(x > kNegInf)) continue;
         const uint32_t k = order_key(x);
         if (level > 0 && (k ^ prefix) >> up != 0) continue;
-        if (!cut.keeps(k, row.id(i, e))) continue;
-        const uint32_t w = weight(x), b = (k >> shift) & mask;
-        if (w & 0xffffu) atomicAdd(&sh.many.lo[b], w & 0xffffu);
-        if (w >> 16) atomicAdd(&sh.many.hi[b], w >> 16);
+        if (!cut.keeps(k, id + e)) continue;
+        const uint32_t w = weight(x);
+        if (w != 0) add_bin(sh, (k >> shift) & mask, w);
       }
-    cluster_sync();
-    // a share of the bins each: their sums over the cluster, to all blocks
-    const int share = (bins + row.cluster - 1) / row.cluster;
-    for (int b = row.rank * share + tid; b < min(bins, (row.rank + 1) * share); b += threads) {
-      unsigned long long t = 0;
-      for (int c = 0; c < row.cluster; ++c) {
-        t += uint32_t(ld_cluster_s32(cluster_smem_addr(&sh.many.lo[b], c)));
-        t += (unsigned long long)uint32_t(ld_cluster_s32(cluster_smem_addr(&sh.many.hi[b], c))) << 16;
-      }
-      for (int c = 0; c < row.cluster; ++c)
-        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_smem_addr(&sh.many.total[b], c)),
-                     "l"(t)
-                     : "memory");
-    }
-    cluster_sync();
+    });
+    row.sync();
+    total_bins(row, bins);
     // from the largest bin down: thread t takes the bins [bins - 1 - t n, ...) downwards
     const int n = (bins + threads - 1) / threads;
     unsigned long long mine = 0;
@@ -338,8 +482,8 @@ ALR_DEV Selected select_key(Row<E, kPacks>& row, const Cut& cut, W weight, Need 
 }
 
 // The last id kept of the tokens with `key` that `cut` keeps, n (>= 1) of them.
-template <typename E, int kPacks>
-ALR_DEV int nth_equal(Row<E, kPacks>& row, const Cut& cut, uint32_t key, unsigned long long n) {
+template <typename R>
+ALR_DEV int nth_equal(R& row, const Cut& cut, uint32_t key, unsigned long long n) {
   const Found f = find_unit(
       row, key_value(key),
       [&](float x, int v) -> unsigned long long {
@@ -373,8 +517,8 @@ struct NeedMass {
 };
 
 // The cut that keeps the k first candidates of the row, which has more.
-template <typename E, int kPacks>
-ALR_DEV Cut cut_top_k(Row<E, kPacks>& row, int k) {
+template <typename R>
+ALR_DEV Cut cut_top_k(R& row, int k) {
   const Cut all{0u, 0x7fffffff};
   NeedCount need{(unsigned long long)k};
   const Selected s = select_key(row, all, [](float) { return 1u; }, need);
@@ -386,27 +530,27 @@ ALR_DEV Cut cut_top_k(Row<E, kPacks>& row, int k) {
 struct Bound {
   float least, top;
 };
-template <typename E, int kPacks>
-ALR_DEV Bound row_bound(Row<E, kPacks>& row, int K) {
+template <typename R>
+ALR_DEV Bound row_bound(R& row, int K) {
+  using E = typename R::E;
   Shared& sh = row.sh;
   float t = kNegInf;
-#pragma unroll
-  for (int i = 0; i < kPacks; ++i) t = fmaxf(t, row.pack_max(i));
+  row.each_first([&](const uint4& p, int) { t = fmaxf(t, largest<E>(p)); });
   row.most = t;
   // the `per` largest of the warp's 32, into all blocks' lists
   const int n_rec = row.records(), tid = threadIdx.x, threads = blockDim.x;
   const int per = K > 1 ? min(32, (K + n_rec - 1) / n_rec + 1) : 1, n = n_rec * per;
+  row.ready();
   if (tid == 0) sh.n_more = 0;
   if (n > kListWarp)
     for (int i = tid; i < 256; i += threads) sh.small[i] = 0;
-  cluster_wait();
   for (int j = 0; j < per; ++j) {
     const float m = warp_max(t);
     row.to_all(&sh.few.list[row.record() * per + j], m);
     const unsigned who = __ballot_sync(0xffffffffu, t == m);
     if (row.lane == __ffs(who) - 1) t = kNegInf;
   }
-  cluster_sync();
+  row.sync();
   float top = kNegInf;
   for (int i = row.lane; i < n_rec; i += 32) top = fmaxf(top, sh.few.list[i * per]);
   top = warp_max(top);
@@ -472,44 +616,38 @@ ALR_DEV Bound row_bound(Row<E, kPacks>& row, int K) {
   return {key_value(prefix), top};
 }
 
-// Element e of a pack, e not known to the compiler.
-template <typename E>
-ALR_DEV float pack_elem_at(const uint4& r, int e) {
-  const int word = sizeof(E) == 2 ? e >> 1 : e;
-  const uint32_t w = word == 0 ? r.x : word == 1 ? r.y : word == 2 ? r.z : r.w;
-  return __uint_as_float(sizeof(E) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16);
-}
-
 // Sends the entries that take(x, id) wants, of those that reach `least`, to the cluster's first block: a
 // warp's first ones into its own places there, more of them to places that it asks for.  All blocks are
 // in step afterwards.
-template <typename E, int kPacks, typename F>
-ALR_DEV void collect(Row<E, kPacks>& row, float least, F take) {
+template <typename R, typename F>
+ALR_DEV void collect(R& row, float least, F take) {
+  using E = typename R::E;
   Shared& sh = row.sh;
   int total = 0;
   const bool has = row.most >= least && row.most > kNegInf;
   if (__any_sync(0xffffffffu, has)) {
     const auto each = [&](auto f) {
       if (!has) return;
-#pragma unroll
-      for (int i = 0; i < kPacks; ++i) {
-        const float m = row.largest(i);
-        if (!(m >= least) || !(m > kNegInf)) continue;
+      row.each([&](const uint4& p, int id) {
+        const float m = largest<E>(p);
+        if (!(m >= least) || !(m > kNegInf)) return;
         uint32_t bits = 0;
 #pragma unroll
         for (int e = 0; e < kPerPack<E>; ++e)
-          bits |= uint32_t(row.x(i, e) >= least && row.x(i, e) > kNegInf) << e;
+          bits |= uint32_t(pack_elem<E>(p, e) >= least && pack_elem<E>(p, e) > kNegInf) << e;
         for (; bits != 0; bits &= bits - 1) {
           const int e = __ffs(bits) - 1;
-          const float x = pack_elem_at<E>(row.raw[i], e);
-          if (take(x, row.id(i, e))) f(entry(order_key(x), row.id(i, e)));
+          const float x = pack_elem_at<E>(p, e);
+          if (take(x, id + e)) f(entry(order_key(x), id + e));
         }
-      }
+      });
     };
     int mine = 0;
-    unsigned long long first = 0;
+    unsigned long long first = 0, second = 0;
     each([&](unsigned long long e) {
-      if (mine++ == 0) first = e;
+      if (mine == 0) first = e;
+      if (mine == 1) second = e;
+      ++mine;
     });
     int at = mine;
 #pragma unroll
@@ -521,47 +659,45 @@ ALR_DEV void collect(Row<E, kPacks>& row, float least, F take) {
     at -= mine;
     int more = 0;
     if (total > kSlots) {
-      if (row.lane == 0)
-        asm volatile("atom.shared::cluster.add.s32 %0, [%1], %2;"
-                     : "=r"(more)
-                     : "r"(cluster_smem_addr(&sh.n_more, 0)), "r"(total - kSlots)
-                     : "memory");
+      if (row.lane == 0) more = row.add_first(&sh.n_more, total - kSlots);
       more = __shfl_sync(0xffffffffu, more, 0) + row.records() * kSlots - kSlots;
     }
     const auto send = [&](unsigned long long e) {
       const int to = at < kSlots ? row.record() * kSlots + at : more + at;
-      if (to < kCandMost)
-        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_smem_addr(&sh.cand[to], 0)), "l"(e)
-                     : "memory");
+      if (to < kCandMost) row.to_first(&sh.cand[to], e);
       ++at;
     };
-    if (mine == 1)
-      send(first);
-    else if (mine > 1)
+    if (__any_sync(0xffffffffu, mine > 2)) {
       each(send);
+    } else {
+      if (mine > 0) send(first);
+      if (mine > 1) send(second);
+    }
   }
-  if (row.lane == 0)
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(
-                     cluster_smem_addr(&sh.count[row.record()], 0)),
-                 "r"(min(total, kSlots))
-                 : "memory");
-  cluster_sync();
+  if (row.lane == 0) row.to_first(&sh.count[row.record()], min(total, kSlots));
+  row.sync();
 }
 
 // Whether all candidates fit, known to all blocks.  The others then wait in the cluster barrier until all
-// have read it; the first block arrives at once and waits (cluster_wait) when it is done.
-template <typename E, int kPacks>
-ALR_DEV bool candidates_fit(Row<E, kPacks>& row) {
+// have read it; the first block arrives at once and waits (others_know) when it likes to.
+ALR_DEV bool candidates_fit(const RowCommon<true>& row) {
+  return row.records() * kSlots + row.sh.n_more <= kCandMost;
+}
+ALR_DEV void others_know(const RowCommon<true>&) {}
+ALR_DEV bool candidates_fit(const RowCommon<false>& row) {
   const int n = row.rank == 0 ? row.sh.n_more : ld_cluster_s32(cluster_smem_addr(&row.sh.n_more, 0));
   const bool fit = row.records() * kSlots + n <= kCandMost;
   cluster_arrive();
   if (row.rank != 0 || !fit) cluster_wait();
   return fit;
 }
+ALR_DEV void others_know(const RowCommon<false>& row) {
+  if (row.rank == 0) cluster_wait();
+}
 
 // First block: the candidates in order, in few.all; returns their number.
-template <typename E, int kPacks>
-ALR_DEV int sort_candidates(Row<E, kPacks>& row) {
+template <typename R>
+ALR_DEV int sort_candidates(R& row) {
   Shared& sh = row.sh;
   const int tid = threadIdx.x, threads = blockDim.x, n_rec = row.records();
   if (row.warp == 0) {   // offsets of the warps' places: lane l has the records [4 l, 4 l + 4)
@@ -630,69 +766,92 @@ ALR_DEV int sort_candidates(Row<E, kPacks>& row) {
 }
 
 // ---------------------------------------------------------------- top logits ---
-template <typename E, int kPacks>
-__global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
-    top_logits_kernel(const E* Z, long long ldz, int V, int K, float inv_t, float* top_val,
-                      int32_t* top_idx, float* lse, float* lse_rest, int cluster) {
-  __shared__ Shared sh;
-  pdl_wait_and_release();
-  const long long r = cluster_id_x();
-  Row<E, kPacks> row(Z + r * ldz, r * ldz, V, cluster, sh);
+struct TopOut {
+  float* val;
+  int32_t* idx;
+  float* lse;
+  float* lse_rest;
+};
+
+template <typename R>
+__device__ __noinline__ Cut exact_top_k(R row, int K) {
+  return cut_top_k(row, K);
+}
+
+template <typename R>
+ALR_DEV void top_logits_row(R& row, int K, float inv_t, const TopOut& out, long long r) {
+  using E = typename R::E;
+  Shared& sh = row.sh;
   const Bound bound = row_bound(row, K);
   collect(row, bound.least, [](float, int) { return true; });
   Cut cut{0u, -1};
   if (!candidates_fit(row)) {   // more than fit reach the bound: find the exact cut
-    Row<E, kPacks> copy = row;
-    cut = cut_top_k(copy, K);
+    cut = exact_top_k(row, K);
     if (threadIdx.x == 0) sh.n_more = 0;
-    cluster_sync();
+    row.sync();
     collect(row, key_value(cut.key), [&](float x, int v) { return cut.keeps(order_key(x), v); });
-    candidates_fit(row);
+    (void)candidates_fit(row);
   }
-  if (row.rank == 0) cluster_wait();   // the records below go over the cluster
-  // the others' sums, each warp's from its own largest; the candidates are the first block's
+  others_know(row);   // the records below go over the cluster
+  // The others' sums, each warp's from its own largest; the candidates are the first block's.
   const float k = inv_t * kLog2e, least = cut.last >= 0 ? key_value(cut.key) : bound.least;
-  float m = kNegInf;
-#pragma unroll
-  for (int i = 0; i < kPacks; ++i) {
-    float p = kNegInf;
-#pragma unroll
-    for (int e = 0; e < kPerPack<E>; e += 2) p = max3(p, row.x(i, e), row.x(i, e + 1));
-    if (p >= least) {
+  const auto without = [&](uint4 p, int id) {
+    if (largest<E>(p) >= least) {
       uint32_t bits = 0;
-      p = kNegInf;
 #pragma unroll 1
       for (int e = 0; e < kPerPack<E>; ++e) {
-        const float x = pack_elem_at<E>(row.raw[i], e);
+        const float x = pack_elem_at<E>(p, e);
         const bool taken =
-            x >= least && (cut.last < 0 || cut.keeps(x > kNegInf ? order_key(x) : 0u, row.id(i, e)));
+            x >= least && (cut.last < 0 || cut.keeps(x > kNegInf ? order_key(x) : 0u, id + e));
         bits |= uint32_t(taken) << e;
-        if (!taken) p = fmaxf(p, x);
       }
-      mask_pack<E>(row.raw[i], bits);
+      mask_pack<E>(p, bits);
     }
-    m = fmaxf(m, p);
+    return p;
+  };
+  float m = kNegInf;
+  if constexpr (std::is_base_of_v<RowCommon<true>, R>) {
+    m = least;   // read once more, not twice: from the bound, or again if that is too far above
+  } else {
+    row.each([&](uint4& p, int id) {
+      p = without(p, id);
+      m = fmaxf(m, largest<E>(p));
+    });
+    m = warp_max(m);
   }
-  m = warp_max(m);
-  const float mw = m > kNegInf ? m : 0.f;
-  const uint64_t m2 = f2_pack(mw, mw), k2 = f2_pack(k, k);
-  uint64_t s2 = 0;
+  const auto sum_from = [&](float ref) {
+    const uint64_t m2 = f2_pack(ref, ref), k2 = f2_pack(k, k);
+    uint64_t s2 = 0;
+    row.each([&](const uint4& q, int id) {
+      uint4 p = q;
+      if constexpr (std::is_base_of_v<RowCommon<true>, R>) p = without(q, id);
 #pragma unroll
-  for (int i = 0; i < kPacks; ++i)
-#pragma unroll
-    for (int e = 0; e < kPerPack<E>; e += 2)
-      s2 = f2_add(s2, f2_ex2(f2_mul(f2_sub(f2_pack(row.x(i, e), row.x(i, e + 1)), m2), k2)));
-  float sa, sb;
-  f2_unpack(s2, sa, sb);
-  const float s = warp_reduce(sa + sb, AddOp());
+      for (int e = 0; e < kPerPack<E>; e += 2)
+        s2 = f2_add(s2, f2_ex2(f2_mul(f2_sub(f2_pack(pack_elem<E>(p, e), pack_elem<E>(p, e + 1)), m2),
+                                      k2)));
+    });
+    float a, b;
+    f2_unpack(s2, a, b);
+    return warp_reduce(a + b, AddOp());
+  };
+  float s = m > kNegInf ? sum_from(m) : 0.f;
+  if constexpr (std::is_base_of_v<RowCommon<true>, R>) {
+    if (m > kNegInf && !(s > 0x1p-60f)) {   // (the same in the whole warp)
+      m = kNegInf;
+      row.each([&](const uint4& p, int id) { m = fmaxf(m, largest<E>(without(p, id))); });
+      m = warp_max(m);
+      s = m > kNegInf ? sum_from(m) : 0.f;
+    }
+    if (!(s > 0.f)) m = kNegInf;
+  }
   row.to_all(&sh.frec[row.record()], make_float2(m, s));
-  cluster_sync();   // no other block's memory is read any more
+  row.sync();   // no other block's memory is read any more
   if (row.rank == 0) {
     const int n = sort_candidates(row);
     const int tid = threadIdx.x, threads = blockDim.x, got = min(n, K);
     for (int i = tid; i < K; i += threads) {
-      top_val[r * K + i] = i < got ? key_value(entry_key(sh.few.all[i])) : kNegInf;
-      top_idx[r * K + i] = i < got ? entry_id(sh.few.all[i]) : -1;
+      out.val[r * K + i] = i < got ? key_value(entry_key(sh.few.all[i])) : kNegInf;
+      out.idx[r * K + i] = i < got ? entry_id(sh.few.all[i]) : -1;
     }
     // the rest: candidates past the K first, and all others
     float mo = kNegInf;
@@ -713,9 +872,31 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
     if (tid == 0) {
       const bool any = mo > kNegInf;
       if (any) sl += so * ex2((mo - bound.top) * k);
-      if (lse != nullptr) lse[r] = n > 0 ? bound.top * inv_t + logf(sl) : kNegInf;
-      if (lse_rest != nullptr) lse_rest[r] = any ? mo * inv_t + logf(so) : kNegInf;
+      if (out.lse != nullptr) out.lse[r] = n > 0 ? bound.top * inv_t + logf(sl) : kNegInf;
+      if (out.lse_rest != nullptr) out.lse_rest[r] = any ? mo * inv_t + logf(so) : kNegInf;
     }
+  }
+}
+
+template <typename E, int kPacks>
+__global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
+    top_logits_kernel(const E* Z, long long ldz, int V, int K, float inv_t, TopOut out, int cluster) {
+  __shared__ Shared sh;
+  pdl_wait_and_release();
+  const long long r = cluster_id_x();
+  Row<E, kPacks> row(Z + r * ldz, r * ldz, V, cluster, sh);
+  top_logits_row(row, K, inv_t, out, r);
+}
+
+template <typename E>
+__global__ void __launch_bounds__(kStreamThreads, 2)
+    top_logits_stream_kernel(const E* Z, long long N, long long ldz, int V, int K, float inv_t,
+                             TopOut out) {
+  __shared__ Shared sh;
+  pdl_wait_and_release();
+  for (long long r = blockIdx.x; r < N; r += gridDim.x) {
+    StreamRow<E> row(Z + r * ldz, r * ldz, V, sh);
+    top_logits_row(row, K, inv_t, out, r);
   }
 }
 
@@ -820,9 +1001,9 @@ struct Steps {
 // The cut that keeps, of the tokens of positive weight that `cut` keeps, the first ones whose summed worth
 // need() still asks for before them (one at least); `cut` itself when need() is content with all of them.
 // worth: 0 .. 2^31 for x, 0 where the weight is 0, as it is below `least`.
-template <typename E, int kPacks, typename W, typename Need>
-ALR_DEV Cut cut_by_steps(Row<E, kPacks>& row, const Cut& cut, const Steps& bin, float least, W worth,
-                         Need need) {
+template <typename R, typename W, typename Need>
+ALR_DEV Cut cut_by_steps(R& row, const Cut& cut, const Steps& bin, float least, W worth, Need need) {
+  using E = typename R::E;
   Shared& sh = row.sh;
   const int tid = threadIdx.x, threads = blockDim.x;
   for (int b = tid; b < kBins; b += threads) sh.many.lo[b] = sh.many.hi[b] = 0;
@@ -833,33 +1014,17 @@ ALR_DEV Cut cut_by_steps(Row<E, kPacks>& row, const Cut& cut, const Steps& bin, 
   __syncthreads();
   const float lowest = fmaxf(least, key_value(cut.key));
   const bool cut_any = cut.key != 0;
-#pragma unroll
-  for (int i = 0; i < kPacks; ++i) {
-    if (!(row.largest(i) >= lowest)) continue;
+  row.each([&](const uint4& p, int id) {
+    if (!(largest<E>(p) >= lowest)) return;
 #pragma unroll
     for (int e = 0; e < kPerPack<E>; ++e) {
-      const float x = row.x(i, e);
+      const float x = pack_elem<E>(p, e);
       const uint32_t w = worth(x);
-      if (w == 0 || (cut_any && !cut.keeps(order_key(x), row.id(i, e)))) continue;
-      const int b = bin(x);
-      if (w & 0xffffu) atomicAdd(&sh.many.lo[b], w & 0xffffu);
-      if (w >> 16) atomicAdd(&sh.many.hi[b], w >> 16);
+      if (w != 0 && (!cut_any || cut.keeps(order_key(x), id + e))) add_bin(sh, bin(x), w);
     }
-  }
-  cluster_sync();
-  const int share = (kBins + row.cluster - 1) / row.cluster;
-  for (int b = row.rank * share + tid; b < min(kBins, (row.rank + 1) * share); b += threads) {
-    unsigned long long t = 0;
-    for (int c = 0; c < row.cluster; ++c) {
-      t += uint32_t(ld_cluster_s32(cluster_smem_addr(&sh.many.lo[b], c)));
-      t += (unsigned long long)uint32_t(ld_cluster_s32(cluster_smem_addr(&sh.many.hi[b], c))) << 16;
-    }
-    for (int c = 0; c < row.cluster; ++c)
-      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_smem_addr(&sh.many.total[b], c)),
-                   "l"(t)
-                   : "memory");
-  }
-  cluster_sync();
+  });
+  row.sync();
+  total_bins(row, kBins);
   const int n = (kBins + threads - 1) / threads;
   unsigned long long mine = 0;
   for (int j = tid * n; j < min(kBins, (tid + 1) * n); ++j) mine += sh.many.total[j];
@@ -897,7 +1062,7 @@ ALR_DEV Cut cut_by_steps(Row<E, kPacks>& row, const Cut& cut, const Steps& bin, 
     const Selected s = select_key(row, cut, worth, need);
     return {s.key, nth_equal(row, cut, s.key, need.reach(s.above, worth(key_value(s.key))))};
   }
-  if (row.rank == 0) cluster_wait();
+  others_know(row);
   if (row.rank == 0) {
     const int got = sort_candidates(row);
     // the last token before which need() asks for more
@@ -923,15 +1088,15 @@ ALR_DEV Cut cut_by_steps(Row<E, kPacks>& row, const Cut& cut, const Steps& bin, 
     __syncthreads();
     if (row.warp == 0) row.to_all(&sh.kept, sh.found);
   }
-  cluster_sync();
+  row.sync();
   const unsigned long long last = sh.kept;
-  cluster_sync();
+  row.sync();
   return {entry_key(last), entry_id(last)};
 }
 
 // Any settings: the cut, then the draw over the whole row.
-template <typename E, int kPacks>
-__device__ __noinline__ void sample_many(Row<E, kPacks> row, const Weight weight, bool greedy, int top_k,
+template <typename R>
+__device__ __noinline__ void sample_many(R row, const Weight weight, bool greedy, int top_k,
                                          float top_p, float min_p, uint32_t u, long long r,
                                          const SampleOut out) {
   Shared& sh = row.sh;
@@ -975,13 +1140,9 @@ __device__ __noinline__ void sample_many(Row<E, kPacks> row, const Weight weight
   }
 }
 
-template <typename E, int kPacks>
-__global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
-    sample_kernel(const E* Z, long long ldz, int V, SampleArgs a, SampleOut out, int cluster) {
-  __shared__ Shared sh;
-  pdl_wait_and_release();
-  const long long r = cluster_id_x();
-  Row<E, kPacks> row(Z + r * ldz, r * ldz, V, cluster, sh);
+template <typename R>
+ALR_DEV void sample_row(R& row, const SampleArgs& a, const SampleOut& out, long long r) {
+  Shared& sh = row.sh;
   const float T = a.temperature != nullptr ? a.temperature[r] : 1.f;
   const int top_k = a.top_k != nullptr ? a.top_k[r] : 0;
   const float top_p = a.top_p != nullptr ? a.top_p[r] : 1.f;
@@ -1006,45 +1167,74 @@ __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
         draw_from_candidates(sh, min(n, K), weight, top_p, min_p, u, r, out);
       else if (threadIdx.x == 0)
         out.put(r, entry_id(sh.few.all[0]), 1.f, 1);
-      cluster_wait();   // the others have read n
+      others_know(row);
       return;
     }
   }
   sample_many(row, weight, greedy, top_k, top_p, min_p, u, r, out);
-  cluster_sync();   // no block's memory is read any more
 }
 
-template <typename F>
-cudaError_t by_shape(int dtype, long long N, int V, int sms, F f) {
-  const RowShape shape = row_shape(N, V, dtype == 0 ? 2 : 4, sms, 256);
-  return with_packs(shape.packs, [&](auto packs) {
-    return dtype == 0 ? f(shape, packs, static_cast<const __nv_bfloat16*>(nullptr))
-                      : f(shape, packs, static_cast<const float*>(nullptr));
-  });
+template <typename E, int kPacks>
+__global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
+    sample_kernel(const E* Z, long long ldz, int V, SampleArgs a, SampleOut out, int cluster) {
+  __shared__ Shared sh;
+  pdl_wait_and_release();
+  const long long r = cluster_id_x();
+  Row<E, kPacks> row(Z + r * ldz, r * ldz, V, cluster, sh);
+  sample_row(row, a, out, r);
 }
+
+template <typename E>
+__global__ void __launch_bounds__(kStreamThreads, 2)
+    sample_stream_kernel(const E* Z, long long N, long long ldz, int V, SampleArgs a, SampleOut out) {
+  __shared__ Shared sh;
+  pdl_wait_and_release();
+  for (long long r = blockIdx.x; r < N; r += gridDim.x) {
+    StreamRow<E> row(Z + r * ldz, r * ldz, V, sh);
+    sample_row(row, a, out, r);
+  }
+}
+
+// One block reads a row by itself where there are rows for every SM, and threads of a row's own enough: no
+// cluster barriers, and blocks of an SM that read while others select.
+bool stream_rows(long long N, int V, int sms) { return N >= sms && V >= 2048; }
 
 }  // namespace
 
 cudaError_t launch_top_logits(int dtype, const void* Z, long long N, int V, long long ldz, int K,
                               float inv_t, float* top_val, int32_t* top_idx, float* lse,
                               float* lse_rest, int sms, cudaStream_t s) {
-  return by_shape(dtype, N, V, sms, [&](const RowShape& shape, auto packs, auto* e) {
-    using E = std::remove_cv_t<std::remove_pointer_t<decltype(e)>>;
-    return launch_row_each(shape, N, top_logits_kernel<E, decltype(packs)::value>, s,
-                           static_cast<const E*>(Z), ldz, V, K, inv_t, top_val, top_idx, lse, lse_rest,
-                           shape.cluster);
-  });
+  const TopOut out{top_val, top_idx, lse, lse_rest};
+  const auto run = [&](auto* z) {
+    using E = std::remove_cv_t<std::remove_pointer_t<decltype(z)>>;
+    if (stream_rows(N, V, sms))
+      return launch_pdl(top_logits_stream_kernel<E>, dim3(unsigned(std::min<long long>(N, 1 << 20))),
+                        dim3(kStreamThreads), 0, s, z, N, ldz, V, K, inv_t, out);
+    const RowShape shape = row_shape(N, V, int(sizeof(E)), sms, 256);
+    return with_packs(shape.packs, [&](auto packs) {
+      return launch_row_each(shape, N, top_logits_kernel<E, decltype(packs)::value>, s, z, ldz, V, K,
+                             inv_t, out, shape.cluster);
+    });
+  };
+  return dtype == 0 ? run(static_cast<const __nv_bfloat16*>(Z)) : run(static_cast<const float*>(Z));
 }
 
 cudaError_t launch_sample(int dtype, const void* Z, long long N, int V, long long ldz,
                           const SampleArgs& a, int32_t* token, float* prob, int32_t* n_kept, int sms,
                           cudaStream_t s) {
-  return by_shape(dtype, N, V, sms, [&](const RowShape& shape, auto packs, auto* e) {
-    using E = std::remove_cv_t<std::remove_pointer_t<decltype(e)>>;
-    const SampleOut out{token, prob, n_kept};
-    return launch_row_each(shape, N, sample_kernel<E, decltype(packs)::value>, s,
-                           static_cast<const E*>(Z), ldz, V, a, out, shape.cluster);
-  });
+  const SampleOut out{token, prob, n_kept};
+  const auto run = [&](auto* z) {
+    using E = std::remove_cv_t<std::remove_pointer_t<decltype(z)>>;
+    if (stream_rows(N, V, sms))
+      return launch_pdl(sample_stream_kernel<E>, dim3(unsigned(std::min<long long>(N, 1 << 20))),
+                        dim3(kStreamThreads), 0, s, z, N, ldz, V, a, out);
+    const RowShape shape = row_shape(N, V, int(sizeof(E)), sms, 256);
+    return with_packs(shape.packs, [&](auto packs) {
+      return launch_row_each(shape, N, sample_kernel<E, decltype(packs)::value>, s, z, ldz, V, a, out,
+                             shape.cluster);
+    });
+  };
+  return dtype == 0 ? run(static_cast<const __nv_bfloat16*>(Z)) : run(static_cast<const float*>(Z));
 }
 
 }  // namespace alr
