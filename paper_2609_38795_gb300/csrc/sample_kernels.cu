@@ -55,7 +55,8 @@ struct Shared {
   unsigned long long cand[kCandMost];     // first block: candidates, kSlots places a warp, then more
   int count[kWarpsMost + 1];              // first block: in each warp's places; then their offsets
   uint32_t small[256];                    // histogram of the list's keys
-  unsigned long long rec[kWarpsMost];     // of each warp of the cluster: a sum
+  unsigned long long rec[kWarpsMost];     // of each warp of the cluster (or batch of a streamed row): a sum
+  unsigned long long grid[8 * kStreamThreads / 32];   // of a batch's packs and warps
   float2 frec[kWarpsMost];
   float fbuf[32];                         // and the bound's result
   unsigned long long lbuf[32];
@@ -244,62 +245,53 @@ struct Row : RowCommon<false> {
   }
 };
 
-// The row read anew (from the second time on, out of L2) by one block: each warp a stretch of it.
+// The row read anew (from the second time on, out of L2) by one block: pack j of a thread in batch b is
+// (b kBatch + j) T + its number, so that however few tokens a mask leaves, many threads hold some.
 template <typename E_>
 struct StreamRow : RowCommon<true> {
   using E = E_;
   static constexpr int kBatch = 8;
   const E* z;
-  int first, end, off;   // packs of this warp; the row starts `off` elements into pack 0
+  int off, packs, batches;   // the row starts `off` elements into pack 0
 
   ALR_DEV StreamRow(const E* z_, long long start, int V_, Shared& s)
       : RowCommon<true>(V_, 1, s), z(z_), off(int(start % kPerPack<E>)) {
-    const int packs = (V + off + kPerPack<E> - 1) / kPerPack<E>;
-    const int share = ((packs + n_warps - 1) / n_warps + 31) / 32 * 32;
-    first = min(packs, warp * share);
-    end = min(packs, first + share);
+    packs = (V + off + kPerPack<E> - 1) / kPerPack<E>;
+    batches = (packs + kStreamThreads * kBatch - 1) / (kStreamThreads * kBatch);
   }
   ALR_DEV void ready() const { __syncthreads(); }   // the last row's shared memory is free
-  ALR_DEV void load(uint4 (&raw)[kBatch], int p) const {
-    const int v = p * kPerPack<E> - off;
-    if (v - lane * kPerPack<E> >= 0 &&
-        v + (32 * kBatch - lane) * kPerPack<E> <= V) {   // all of the warp's within the row
+  // First element of the thread's pack j in batch b.
+  ALR_DEV int elem(int b, int j) const {
+    return ((b * kBatch + j) * kStreamThreads + int(threadIdx.x)) * kPerPack<E> - off;
+  }
+  ALR_DEV void load(uint4 (&raw)[kBatch], int b) const {
+    const int v = elem(b, 0);
+    if ((b > 0 || off == 0) && elem(b + 1, 0) - int(threadIdx.x) * kPerPack<E> <= V) {   // a full batch
       const uint4* q = reinterpret_cast<const uint4*>(z + v);
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) raw[j] = q[32 * j];
+      for (int j = 0; j < kBatch; ++j) raw[j] = q[kStreamThreads * j];
     } else {
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) raw[j] = load_pack(z, v + 32 * j * kPerPack<E>, V);
+      for (int j = 0; j < kBatch; ++j) raw[j] = load_pack(z, elem(b, j), V);
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      clean<E>(raw[j]);
+      if (infinite) zero_for_infinite<E>(raw[j]);
     }
   }
   template <typename F>
   ALR_DEV void each(F f) {
-    for (int p = first + lane; p - lane < end; p += 32 * kBatch) {
+    for (int b = 0; b < batches; ++b) {
       uint4 raw[kBatch];
-      load(raw, p);
+      load(raw, b);
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        if (p - lane + 32 * j >= end) break;
-        clean<E>(raw[j]);
-        if (infinite) zero_for_infinite<E>(raw[j]);
-        f(raw[j], (p + 32 * j) * kPerPack<E> - off);
-      }
+      for (int j = 0; j < kBatch; ++j) f(raw[j], elem(b, j));
     }
   }
   template <typename F>
   ALR_DEV void each_first(F f) {
     each(f);
-  }
-  template <typename F>
-  ALR_DEV void each_until(F f) {
-    bool stop = false;
-    for (int p = first + lane; p - lane < end && !stop; p += 32) {
-      const int v = p * kPerPack<E> - off;
-      uint4 r = load_pack(z, v, V);
-      clean<E>(r);
-      if (infinite) zero_for_infinite<E>(r);
-      stop = f(r, v);
-    }
   }
   ALR_DEV void only_infinite() {
     infinite = true;
@@ -314,9 +306,8 @@ struct Found {
   int id;
   unsigned long long weight, total;
 };
-template <typename R, typename F, typename N>
-ALR_DEV Found find_unit(R& row, float least, F f, N nth) {
-  using E = typename R::E;
+template <typename E, int kPacks, typename F, typename N>
+ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
   Shared& sh = row.sh;
   unsigned long long s = 0;
   row.each([&](const uint4& p, int id) {
@@ -399,6 +390,84 @@ ALR_DEV void total_bins(R& row, int bins) {
     }
   }
   row.sync();
+}
+
+// The order of a streamed row is batch, pack, thread: sums per batch tell the batch, sums per pack and
+// warp of that batch the warp.
+template <typename E, typename F, typename N>
+ALR_DEV Found find_unit(StreamRow<E>& row, float least, F f, N nth) {
+  Shared& sh = row.sh;
+  constexpr int kBatch = StreamRow<E>::kBatch, kWarps = kStreamThreads / 32;
+  static_assert(262144 / kPerPack<E> / (kStreamThreads * kBatch) + 2 <= kWarpsMost, "a sum per batch");
+  for (int i = threadIdx.x; i < row.batches; i += blockDim.x) sh.rec[i] = 0;
+  __syncthreads();
+  const auto of_pack = [&](const uint4& p, int id) {
+    unsigned long long s = 0;
+    if (largest<E>(p) >= least)
+#pragma unroll
+      for (int e = 0; e < kPerPack<E>; ++e) s += f(pack_elem<E>(p, e), id + e);
+    return s;
+  };
+  uint4 raw[kBatch];
+  for (int b = 0; b < row.batches; ++b) {
+    row.load(raw, b);
+    unsigned long long s = 0;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) s += of_pack(raw[j], row.elem(b, j));
+    if (!__any_sync(0xffffffffu, s != 0)) continue;
+    s = warp_reduce(s, AddOp());
+    if (row.lane == 0) atomicAdd(&sh.rec[b], s);
+  }
+  __syncthreads();
+  unsigned long long total = 0;
+  for (int b = 0; b < row.batches; ++b) total += sh.rec[b];
+  const unsigned long long n = nth(total);
+  unsigned long long before = 0;
+  int b = 0;
+  while (b < row.batches - 1 && before + sh.rec[b] < n) before += sh.rec[b++];
+  row.load(raw, b);
+  unsigned long long own[kBatch];
+#pragma unroll
+  for (int j = 0; j < kBatch; ++j) {
+    own[j] = of_pack(raw[j], row.elem(b, j));
+    const unsigned long long s = warp_reduce(own[j], AddOp());
+    if (row.lane == 0) sh.grid[j * kWarps + row.warp] = s;
+  }
+  __syncthreads();
+  int at = 0;
+  while (at < kBatch * kWarps - 1 && before + sh.grid[at] < n) before += sh.grid[at++];
+  if (row.warp == at % kWarps) {
+    const int j = at / kWarps;
+    uint4 p = raw[0];
+    unsigned long long mine = own[0];
+#pragma unroll
+    for (int i = 1; i < kBatch; ++i)
+      if (i == j) {
+        p = raw[i];
+        mine = own[i];
+      }
+    unsigned long long incl = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
+      if (row.lane >= off) incl += t;
+    }
+    unsigned long long run = before + incl - mine;
+    if (run < n && n <= run + mine)
+      for (int e = 0; e < kPerPack<E>; ++e) {
+        const int id = row.elem(b, j) + e;
+        const unsigned long long t = f(pack_elem_at<E>(p, e), id);
+        if (run < n && n <= run + t) {
+          sh.found = uint32_t(id);
+          sh.kept = t;
+        }
+        run += t;
+      }
+  }
+  __syncthreads();
+  const Found r{int(uint32_t(sh.found)), sh.kept, total};
+  __syncthreads();   // before `found` and `rec` are written again
+  return r;
 }
 
 // Radix select among the tokens that `cut` keeps: the largest key at which the summed weights, from
@@ -678,6 +747,64 @@ ALR_DEV void collect(R& row, float least, F take) {
   row.sync();
 }
 
+// row_bound and collect in one reading of the row by one block, for up to kStreamFew tokens: the K-th
+// largest of the threads' largest logits, once the first packs are there (and again after the next ones),
+// is a bound that every later pack is held against as it comes by.
+constexpr int kStreamFew = 128;
+
+template <typename R>
+ALR_DEV Bound bound_and_collect(R& row, int K) {
+  if constexpr (std::is_base_of_v<RowCommon<true>, R>) {
+    using E = typename R::E;
+    if (K <= kStreamFew) {
+      Shared& sh = row.sh;
+      constexpr int kBatch = R::kBatch;
+      row.ready();
+      if (threadIdx.x == 0) sh.n_more = 0;
+      for (int i = threadIdx.x; i < row.records(); i += blockDim.x) sh.count[i] = 0;
+      __syncthreads();
+      float most = kNegInf, least = kNegInf;
+      for (int b = 0; b < row.batches; ++b) {
+        uint4 raw[kBatch];
+        row.load(raw, b);
+        float top[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          top[j] = largest<E>(raw[j]);
+          most = fmaxf(most, top[j]);
+        }
+        if (b < 2 || least == kNegInf) {   // bit by bit of the upper half of the keys
+          const uint32_t key = most > kNegInf ? order_key(most) >> 16 : 0u;
+          uint32_t bound = 0;
+          for (uint32_t bit = 0x8000u; bit != 0; bit >>= 1)
+            if (__syncthreads_count(key >= (bound | bit)) >= K) bound |= bit;
+          if (bound != 0) least = key_value(bound << 16);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          if (!(top[j] >= least) || !(top[j] > kNegInf)) continue;
+          uint32_t bits = 0;
+#pragma unroll
+          for (int e = 0; e < kPerPack<E>; ++e)
+            bits |= uint32_t(pack_elem<E>(raw[j], e) >= least && pack_elem<E>(raw[j], e) > kNegInf) << e;
+          int at = row.records() * kSlots + atomicAdd(&sh.n_more, __popc(bits));
+          for (; bits != 0; bits &= bits - 1, ++at) {
+            const int e = __ffs(bits) - 1;
+            if (at < kCandMost)
+              sh.cand[at] = entry(order_key(pack_elem_at<E>(raw[j], e)), row.elem(b, j) + e);
+          }
+        }
+      }
+      row.most = most;
+      const float top = block_reduce(most, MaxOp(), sh.fbuf);   // and all candidates are there
+      return {least, top};
+    }
+  }
+  const Bound b = row_bound(row, K);
+  if (K > 0 && b.top > kNegInf) collect(row, b.least, [](float, int) { return true; });
+  return b;
+}
+
 // Whether all candidates fit, known to all blocks.  The others then wait in the cluster barrier until all
 // have read it; the first block arrives at once and waits (others_know) when it likes to.
 ALR_DEV bool candidates_fit(const RowCommon<true>& row) {
@@ -782,9 +909,19 @@ template <typename R>
 ALR_DEV void top_logits_row(R& row, int K, float inv_t, const TopOut& out, long long r) {
   using E = typename R::E;
   Shared& sh = row.sh;
-  const Bound bound = row_bound(row, K);
-  collect(row, bound.least, [](float, int) { return true; });
+  const Bound bound = bound_and_collect(row, K);
   Cut cut{0u, -1};
+  if (!(bound.top > kNegInf)) {   // nothing to list; all blocks agree, none reads another's memory
+    for (int i = threadIdx.x; row.rank == 0 && i < K; i += blockDim.x) {
+      out.val[r * K + i] = kNegInf;
+      out.idx[r * K + i] = -1;
+    }
+    if (row.rank == 0 && threadIdx.x == 0) {
+      if (out.lse != nullptr) out.lse[r] = kNegInf;
+      if (out.lse_rest != nullptr) out.lse_rest[r] = kNegInf;
+    }
+    return;
+  }
   if (!candidates_fit(row)) {   // more than fit reach the bound: find the exact cut
     cut = exact_top_k(row, K);
     if (threadIdx.x == 0) sh.n_more = 0;
@@ -1150,16 +1287,14 @@ ALR_DEV void sample_row(R& row, const SampleArgs& a, const SampleOut& out, long 
   const uint32_t u = a.u[r];
   const bool greedy = !(T > 0.f);
   const int K = greedy ? 1 : top_k > 0 && top_k <= kTopMost ? top_k : 0;   // few tokens
-  const Bound bound = row_bound(row, K);
+  const Bound bound = K > 0 ? bound_and_collect(row, K) : row_bound(row, 0);
   if (!(bound.top > kNegInf)) {   // no candidate; all blocks agree, and none reads another's memory
     if (row.rank == 0 && threadIdx.x == 0) out.put(r, -1, 0.f, 0);
     return;
   }
   const bool infinite = bound.top == -kNegInf;
-  if (infinite) row.only_infinite();
   const Weight weight{infinite ? 0.f : bound.top, greedy ? 0.f : __fdiv_rn(kLog2e, T)};
-  if (K > 0) {
-    collect(row, infinite ? 0.f : bound.least, [](float, int) { return true; });
+  if (K > 0 && (!infinite || K == 1)) {   // (with K = 1 only +inf reaches the bound)
     if (candidates_fit(row)) {
       if (row.rank != 0) return;
       const int n = sort_candidates(row);
@@ -1171,6 +1306,7 @@ ALR_DEV void sample_row(R& row, const SampleArgs& a, const SampleOut& out, long 
       return;
     }
   }
+  if (infinite) row.only_infinite();
   sample_many(row, weight, greedy, top_k, top_p, min_p, u, r, out);
 }
 
