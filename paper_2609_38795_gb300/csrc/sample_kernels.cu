@@ -216,6 +216,14 @@ struct Row : RowCommon<false> {
 #pragma unroll
     for (int i = 0; i < kPacks; ++i) f(raw[i], at.elem(i));
   }
+  // The same for an f of many instructions: a loop, so that the code stays in the instruction cache
+  // (unrolled, the sweeps over weights stalled on it most of their time).  Only on a copy of the row,
+  // which lies in local memory for it.
+  template <typename F>
+  ALR_DEV void each_heavy(F f) {
+#pragma unroll 1
+    for (int i = 0; i < kPacks; ++i) f(raw[i], at.elem(i));
+  }
   template <typename F>
   ALR_DEV void each_first(F f) {   // before all others: NaN elements go
 #pragma unroll
@@ -264,29 +272,55 @@ struct StreamRow : RowCommon<true> {
   ALR_DEV int elem(int b, int j) const {
     return ((b * kBatch + j) * kStreamThreads + int(threadIdx.x)) * kPerPack<E> - off;
   }
-  ALR_DEV void load(uint4 (&raw)[kBatch], int b) const {
-    const int v = elem(b, 0);
-    if ((b > 0 || off == 0) && elem(b + 1, 0) - int(threadIdx.x) * kPerPack<E> <= V) {   // a full batch
+  // Packs first .. first + kN of the thread, counted through the batches.
+  template <int kN>
+  ALR_DEV void load(uint4 (&raw)[kN], int first) const {
+    const int v = elem(0, first);
+    if ((first > 0 || off == 0) && elem(0, first + kN) - int(threadIdx.x) * kPerPack<E> <= V) {
       const uint4* q = reinterpret_cast<const uint4*>(z + v);
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) raw[j] = q[kStreamThreads * j];
+      for (int j = 0; j < kN; ++j) raw[j] = q[kStreamThreads * j];
     } else {
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) raw[j] = load_pack(z, elem(b, j), V);
+      for (int j = 0; j < kN; ++j) raw[j] = load_pack(z, elem(0, first + j), V);
     }
 #pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
+    for (int j = 0; j < kN; ++j) {
       clean<E>(raw[j]);
       if (infinite) zero_for_infinite<E>(raw[j]);
     }
+  }
+  ALR_DEV uint4 load_one(int i) const {
+    uint4 p = load_pack(z, elem(0, i), V);
+    clean<E>(p);
+    if (infinite) zero_for_infinite<E>(p);
+    return p;
   }
   template <typename F>
   ALR_DEV void each(F f) {
     for (int b = 0; b < batches; ++b) {
       uint4 raw[kBatch];
-      load(raw, b);
+      load(raw, b * kBatch);
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) f(raw[j], elem(b, j));
+    }
+  }
+  // The same for an f of many instructions, with fewer copies of it.
+  static constexpr int kHeavy = 2;
+  template <typename F>
+  ALR_DEV void each_heavy(F f) {
+    const int most = (packs + kStreamThreads - 1) / kStreamThreads;   // of a thread
+#pragma unroll 1
+    for (int i = 0; i < most; i += 2 * kHeavy) {
+      uint4 raw[2 * kHeavy];
+      load(raw, i);
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int j = 0; j < kHeavy; ++j) f(raw[j], elem(0, i + h * kHeavy + j));
+#pragma unroll
+        for (int j = 0; j < kHeavy; ++j) raw[j] = raw[j + kHeavy];
+      }
     }
   }
   template <typename F>
@@ -301,19 +335,33 @@ struct StreamRow : RowCommon<true> {
 
 // The n-th (from 1) unit of weight f(x, id) >= 0, counted in the order of ids over the whole row: the
 // id of the token that holds it, that token's weight and the sum of all weights.  n(total) gives n.
-// f is 0 for logits below `least`.
+// f(x, id) is 0 for logits below `least`; f.pack(pack, id) is the sum over a pack's elements.
 struct Found {
   int id;
   unsigned long long weight, total;
+  int count;   // this thread's tokens, where f counts them
 };
+template <typename F>
+ALR_DEV auto counted(const F& f) -> decltype(f.count) { return f.count; }
+ALR_DEV int counted(...) { return 0; }
+template <typename E, typename F>
+struct OfPack {
+  F f;
+  ALR_DEV unsigned long long operator()(float x, int id) { return f(x, id); }
+  ALR_DEV unsigned long long pack(const uint4& p, int id) {
+    unsigned long long s = 0;
+#pragma unroll 1
+    for (int e = 0; e < kPerPack<E>; ++e) s += f(pack_elem_at<E>(p, e), id + e);
+    return s;
+  }
+};
+
 template <typename E, int kPacks, typename F, typename N>
 ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
   Shared& sh = row.sh;
   unsigned long long s = 0;
-  row.each([&](const uint4& p, int id) {
-    if (!(largest<E>(p) >= least)) return;
-#pragma unroll
-    for (int e = 0; e < kPerPack<E>; ++e) s += f(pack_elem<E>(p, e), id + e);
+  row.each_heavy([&](const uint4& p, int id) {
+    if (largest<E>(p) >= least) s += f.pack(p, id);
   });
   s = warp_reduce(s, AddOp());
   row.to_all(&sh.rec[row.record()], s);
@@ -326,13 +374,11 @@ ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
   }
   total = warp_reduce(total, AddOp());
   before = warp_reduce(before, AddOp());
+  const int count = counted(f);   // of the first sweep; what the search adds is not wanted
   const unsigned long long n = nth(total);
   if (before < n && n <= before + s)   // this warp holds it
     row.each_until([&](const uint4& p, int id) {
-      unsigned long long mine = 0;
-      if (largest<E>(p) >= least)
-#pragma unroll
-        for (int e = 0; e < kPerPack<E>; ++e) mine += f(pack_elem<E>(p, e), id + e);
+      const unsigned long long mine = largest<E>(p) >= least ? f.pack(p, id) : 0ull;
       unsigned long long incl = mine;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
@@ -347,9 +393,9 @@ ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
       unsigned long long run = before + incl - mine, w = 0;
       int at = -1;
       if (run < n && n <= run + mine)
-#pragma unroll
+#pragma unroll 1
         for (int e = 0; e < kPerPack<E>; ++e) {
-          const unsigned long long t = f(pack_elem<E>(p, e), id + e);
+          const unsigned long long t = f(pack_elem_at<E>(p, e), id + e);
           if (at < 0 && run < n && n <= run + t) {
             at = id + e;
             w = t;
@@ -362,7 +408,7 @@ ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
       return true;
     });
   row.sync();
-  const Found r{int(uint32_t(sh.found)), sh.kept, total};
+  const Found r{int(uint32_t(sh.found)), sh.kept, total, count};
   row.sync();   // before `found` and `rec` are written again
   return r;
 }
@@ -402,18 +448,24 @@ ALR_DEV Found find_unit(StreamRow<E>& row, float least, F f, N nth) {
   for (int i = threadIdx.x; i < row.batches; i += blockDim.x) sh.rec[i] = 0;
   __syncthreads();
   const auto of_pack = [&](const uint4& p, int id) {
-    unsigned long long s = 0;
-    if (largest<E>(p) >= least)
-#pragma unroll
-      for (int e = 0; e < kPerPack<E>; ++e) s += f(pack_elem<E>(p, e), id + e);
-    return s;
+    return largest<E>(p) >= least ? f.pack(p, id) : 0ull;
   };
-  uint4 raw[kBatch];
+  const int most = (row.packs + kStreamThreads - 1) / kStreamThreads;   // packs of a thread
+  static_assert(kBatch % 2 == 0, "a batch is whole loads");
+#pragma unroll 1
   for (int b = 0; b < row.batches; ++b) {
-    row.load(raw, b);
     unsigned long long s = 0;
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) s += of_pack(raw[j], row.elem(b, j));
+#pragma unroll 1
+    for (int i = b * kBatch; i < min(most, (b + 1) * kBatch); i += 4) {
+      uint4 raw[4];
+      row.load(raw, i);
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        s += of_pack(raw[0], row.elem(0, i + 2 * h)) + of_pack(raw[1], row.elem(0, i + 2 * h + 1));
+        raw[0] = raw[2];
+        raw[1] = raw[3];
+      }
+    }
     if (!__any_sync(0xffffffffu, s != 0)) continue;
     s = warp_reduce(s, AddOp());
     if (row.lane == 0) atomicAdd(&sh.rec[b], s);
@@ -421,16 +473,15 @@ ALR_DEV Found find_unit(StreamRow<E>& row, float least, F f, N nth) {
   __syncthreads();
   unsigned long long total = 0;
   for (int b = 0; b < row.batches; ++b) total += sh.rec[b];
+  const int count = counted(f);   // of the first sweep; what the search adds is not wanted
   const unsigned long long n = nth(total);
   unsigned long long before = 0;
   int b = 0;
   while (b < row.batches - 1 && before + sh.rec[b] < n) before += sh.rec[b++];
-  row.load(raw, b);
-  unsigned long long own[kBatch];
-#pragma unroll
+#pragma unroll 1
   for (int j = 0; j < kBatch; ++j) {
-    own[j] = of_pack(raw[j], row.elem(b, j));
-    const unsigned long long s = warp_reduce(own[j], AddOp());
+    const unsigned long long s =
+        warp_reduce(of_pack(row.load_one(b * kBatch + j), row.elem(b, j)), AddOp());
     if (row.lane == 0) sh.grid[j * kWarps + row.warp] = s;
   }
   __syncthreads();
@@ -438,14 +489,8 @@ ALR_DEV Found find_unit(StreamRow<E>& row, float least, F f, N nth) {
   while (at < kBatch * kWarps - 1 && before + sh.grid[at] < n) before += sh.grid[at++];
   if (row.warp == at % kWarps) {
     const int j = at / kWarps;
-    uint4 p = raw[0];
-    unsigned long long mine = own[0];
-#pragma unroll
-    for (int i = 1; i < kBatch; ++i)
-      if (i == j) {
-        p = raw[i];
-        mine = own[i];
-      }
+    const uint4 p = row.load_one(b * kBatch + j);
+    const unsigned long long mine = of_pack(p, row.elem(b, j));
     unsigned long long incl = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -465,7 +510,7 @@ ALR_DEV Found find_unit(StreamRow<E>& row, float least, F f, N nth) {
       }
   }
   __syncthreads();
-  const Found r{int(uint32_t(sh.found)), sh.kept, total};
+  const Found r{int(uint32_t(sh.found)), sh.kept, total, count};
   __syncthreads();   // before `found` and `rec` are written again
   return r;
 }
@@ -493,7 +538,7 @@ ALR_DEV Selected select_key(R& row, const Cut& cut, W weight, Need need) {
     const int bins = int(mask) + 1;
     for (int b = tid; b < bins; b += threads) sh.many.lo[b] = sh.many.hi[b] = 0;
     __syncthreads();
-    row.each([&](const uint4& p, int id) {
+    row.each_heavy([&](const uint4& p, int id) {
 #pragma unroll 1
       for (int e = 0; e < kPerPack<E>; ++e) {
         const float x = pack_elem_at<E>(p, e);
@@ -553,11 +598,11 @@ ALR_DEV Selected select_key(R& row, const Cut& cut, W weight, Need need) {
 // The last id kept of the tokens with `key` that `cut` keeps, n (>= 1) of them.
 template <typename R>
 ALR_DEV int nth_equal(R& row, const Cut& cut, uint32_t key, unsigned long long n) {
+  const auto is = [&](float x, int v) -> unsigned long long {
+    return x > kNegInf && order_key(x) == key && cut.keeps(key, v);
+  };
   const Found f = find_unit(
-      row, key_value(key),
-      [&](float x, int v) -> unsigned long long {
-        return x > kNegInf && order_key(x) == key && cut.keeps(key, v);
-      },
+      row, key_value(key), OfPack<typename R::E, decltype(is)>{is},
       [n](unsigned long long total) { return n < total ? n : total; });
   return f.id;
 }
@@ -685,11 +730,11 @@ ALR_DEV Bound row_bound(R& row, int K) {
   return {key_value(prefix), top};
 }
 
-// Sends the entries that take(x, id) wants, of those that reach `least`, to the cluster's first block: a
+// Sends the entries that take(x, id) wants, of those in [least, most], to the cluster's first block: a
 // warp's first ones into its own places there, more of them to places that it asks for.  All blocks are
 // in step afterwards.
-template <typename R, typename F>
-ALR_DEV void collect(R& row, float least, F take) {
+template <bool kHeavy = false, typename R, typename F>
+ALR_DEV void collect(R& row, float least, float most, F take) {
   using E = typename R::E;
   Shared& sh = row.sh;
   int total = 0;
@@ -697,19 +742,25 @@ ALR_DEV void collect(R& row, float least, F take) {
   if (__any_sync(0xffffffffu, has)) {
     const auto each = [&](auto f) {
       if (!has) return;
-      row.each([&](const uint4& p, int id) {
+      const auto of_pack = [&](const uint4& p, int id) {
         const float m = largest<E>(p);
         if (!(m >= least) || !(m > kNegInf)) return;
         uint32_t bits = 0;
 #pragma unroll
-        for (int e = 0; e < kPerPack<E>; ++e)
-          bits |= uint32_t(pack_elem<E>(p, e) >= least && pack_elem<E>(p, e) > kNegInf) << e;
+        for (int e = 0; e < kPerPack<E>; ++e) {
+          const float x = pack_elem<E>(p, e);
+          bits |= uint32_t(x >= least && x <= most && x > kNegInf) << e;
+        }
         for (; bits != 0; bits &= bits - 1) {
           const int e = __ffs(bits) - 1;
           const float x = pack_elem_at<E>(p, e);
           if (take(x, id + e)) f(entry(order_key(x), id + e));
         }
-      });
+      };
+      if constexpr (kHeavy)
+        row.each_heavy(of_pack);
+      else
+        row.each(of_pack);
     };
     int mine = 0;
     unsigned long long first = 0, second = 0;
@@ -766,7 +817,7 @@ ALR_DEV Bound bound_and_collect(R& row, int K) {
       float most = kNegInf, least = kNegInf;
       for (int b = 0; b < row.batches; ++b) {
         uint4 raw[kBatch];
-        row.load(raw, b);
+        row.load(raw, b * kBatch);
         float top[kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
@@ -801,7 +852,7 @@ ALR_DEV Bound bound_and_collect(R& row, int K) {
     }
   }
   const Bound b = row_bound(row, K);
-  if (K > 0 && b.top > kNegInf) collect(row, b.least, [](float, int) { return true; });
+  if (K > 0 && b.top > kNegInf) collect(row, b.least, -kNegInf, [](float, int) { return true; });
   return b;
 }
 
@@ -926,7 +977,7 @@ ALR_DEV void top_logits_row(R& row, int K, float inv_t, const TopOut& out, long 
     cut = exact_top_k(row, K);
     if (threadIdx.x == 0) sh.n_more = 0;
     row.sync();
-    collect(row, key_value(cut.key), [&](float x, int v) { return cut.keeps(order_key(x), v); });
+    collect(row, key_value(cut.key), -kNegInf, [&](float x, int v) { return cut.keeps(order_key(x), v); });
     (void)candidates_fit(row);
   }
   others_know(row);   // the records below go over the cluster
@@ -1151,11 +1202,11 @@ ALR_DEV Cut cut_by_steps(R& row, const Cut& cut, const Steps& bin, float least, 
   __syncthreads();
   const float lowest = fmaxf(least, key_value(cut.key));
   const bool cut_any = cut.key != 0;
-  row.each([&](const uint4& p, int id) {
+  row.each_heavy([&](const uint4& p, int id) {
     if (!(largest<E>(p) >= lowest)) return;
-#pragma unroll
+#pragma unroll 2
     for (int e = 0; e < kPerPack<E>; ++e) {
-      const float x = pack_elem<E>(p, e);
+      const float x = pack_elem_at<E>(p, e);
       const uint32_t w = worth(x);
       if (w != 0 && (!cut_any || cut.keeps(order_key(x), id + e))) add_bin(sh, bin(x), w);
     }
@@ -1192,7 +1243,10 @@ ALR_DEV Cut cut_by_steps(R& row, const Cut& cut, const Steps& bin, float least, 
   const int step = int(sh.digit);
   const unsigned long long above = sh.above;
   // that step's tokens, in order
-  collect(row, lowest, [&](float x, int v) {
+  const float hi = bin.top - float(step) / bin.scale, lo = bin.top - float(step + 1) / bin.scale;
+  const float wide = 1e-6f * (fabsf(bin.top) + fabsf(lo)) + 0.01f / bin.scale;   // for the roundings
+  collect<true>(row, lo - wide > lowest && step < kBins - 1 ? lo - wide : lowest,
+                hi + wide < -kNegInf ? hi + wide : -kNegInf, [&](float x, int v) {
     return bin(x) == step && worth(x) != 0 && (!cut_any || cut.keeps(order_key(x), v));
   });
   if (!candidates_fit(row)) {   // too many of them
@@ -1231,6 +1285,45 @@ ALR_DEV Cut cut_by_steps(R& row, const Cut& cut, const Steps& bin, float least, 
   return {entry_key(last), entry_id(last)};
 }
 
+// Weights of the tokens kept: those above `edge`, at it up to id `last`, of a real weight of min_p at least.
+template <typename E>
+struct Mass {
+  Weight weight;
+  float edge;
+  int last;
+  float min_p;
+  int count;   // of tokens in the packs summed up
+  ALR_DEV unsigned long long operator()(float x, int id) const {
+    if (!(x > edge || (x == edge && id <= last))) return 0;
+    const float w = weight.real(x);
+    return w >= min_p || x == weight.m ? __float2uint_rz(w * 2147483648.f) : 0u;
+  }
+  ALR_DEV unsigned long long pack(const uint4& p, int id) {
+    unsigned long long s = 0;
+    bool at_edge = false;
+#pragma unroll
+    for (int e = 0; e < kPerPack<E>; ++e) {
+      const float x = pack_elem<E>(p, e), w = weight.real(x);
+      uint32_t q = __float2uint_rz(w * 2147483648.f);
+      if (!(x >= edge) || !(w >= min_p || x == weight.m)) q = 0;
+      at_edge |= x == edge;
+      s += q;
+      count += q != 0;
+    }
+    if (at_edge && id + kPerPack<E> > last)   // tokens at the edge, some past the last one
+#pragma unroll 1
+      for (int e = 0; e < kPerPack<E>; ++e) {
+        const float x = pack_elem_at<E>(p, e);
+        if (!(x == edge) || id + e <= last) continue;
+        const float w = weight.real(x);
+        const uint32_t q = w >= min_p || x == weight.m ? __float2uint_rz(w * 2147483648.f) : 0u;
+        s -= q;
+        count -= q != 0;
+      }
+    return s;
+  }
+};
+
 // Any settings: the cut, then the draw over the whole row.
 template <typename R>
 __device__ __noinline__ void sample_many(R row, const Weight weight, bool greedy, int top_k,
@@ -1249,29 +1342,20 @@ __device__ __noinline__ void sample_many(R row, const Weight weight, bool greedy
     if (top_p < 1.f) cut = cut_by_steps(row, cut, bin, least, weight, NeedMass{double(top_p), 0.0});
   }
   const bool all = cut.key == 0;
-  const float edge = all ? kNegInf : key_value(cut.key);
-  const auto mass = [&](float x, int v) -> unsigned long long {
-    if (!all && !(x > edge || (x == edge && v <= cut.last))) return 0;
-    const float w = weight.real(x);
-    if (!(w >= min_p) && !(x == weight.m)) return 0;
-    return __float2uint_rz(w * 2147483648.f);
-  };
-  int kept = 0;
+  Mass<typename R::E> mass{weight, all ? kNegInf : key_value(cut.key), all ? 0x7fffffff : cut.last, min_p, 0};
   const Found f = find_unit(
-      row, fmaxf(fmaxf(least, edge), min_p > 0.f ? weight.below(min_p) : kNegInf),
-      [&](float x, int v) -> unsigned long long {
-        const unsigned long long w = mass(x, v);
-        kept += w != 0;   // counted in the first sweep; what the search adds is not read
-        return w;
-      },
-      [&](unsigned long long total) {
-        const int n = int(warp_reduce(kept, AddOp()));
-        row.to_all(&sh.frec[row.record()], make_float2(__int_as_float(n), 0.f));
-        return __umul64hi((unsigned long long)u << 32, total) + 1;
-      });
+      row, fmaxf(fmaxf(least, mass.edge), min_p > 0.f ? weight.below(min_p) : kNegInf), mass,
+      [&](unsigned long long total) { return __umul64hi((unsigned long long)u << 32, total) + 1; });
+  // the number of tokens kept, if anyone asks
+  if (out.n_kept != nullptr) {
+    const int n = int(warp_reduce(f.count, AddOp()));
+    row.to_all(&sh.frec[row.record()], make_float2(__int_as_float(n), 0.f));
+    row.sync();
+  }
   if (row.rank == 0 && row.warp == 0) {
     int n = 0;
-    for (int i = row.lane; i < row.records(); i += 32) n += __float_as_int(sh.frec[i].x);
+    if (out.n_kept != nullptr)
+      for (int i = row.lane; i < row.records(); i += 32) n += __float_as_int(sh.frec[i].x);
     n = warp_reduce(n, AddOp());
     if (row.lane == 0) out.put(r, f.id, float(double(f.weight) / double(f.total)), n);
   }
