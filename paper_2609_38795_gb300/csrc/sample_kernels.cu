@@ -98,6 +98,16 @@ ALR_DEV float largest(const uint4& r) {
   return pack_largest(r, std::integral_constant<int, int(sizeof(E))>{});
 }
 
+// Elements of a pack that reach `least`, a bit each.  Where few do, a loop over the bits set costs the warp
+// an element's instructions or two; a loop over the elements costs it all of them for one lane's one.
+template <typename E>
+ALR_DEV uint32_t reaching(const uint4& r, float least) {
+  uint32_t bits = 0;
+#pragma unroll
+  for (int e = 0; e < kPerPack<E>; ++e) bits |= uint32_t(pack_elem<E>(r, e) >= least) << e;
+  return bits;
+}
+
 // NaN elements of a pack become -inf.
 template <typename E>
 ALR_DEV void clean(uint4& r) {
@@ -335,7 +345,7 @@ struct StreamRow : RowCommon<true> {
 
 // The n-th (from 1) unit of weight f(x, id) >= 0, counted in the order of ids over the whole row: the
 // id of the token that holds it, that token's weight and the sum of all weights.  n(total) gives n.
-// f(x, id) is 0 for logits below `least`; f.pack(pack, id) is the sum over a pack's elements.
+// f(x, id) is 0 for logits below `least`; f.pack and f.few sum over a pack's elements, the second one by one.
 struct Found {
   int id;
   unsigned long long weight, total;
@@ -348,20 +358,33 @@ template <typename E, typename F>
 struct OfPack {
   F f;
   ALR_DEV unsigned long long operator()(float x, int id) { return f(x, id); }
-  ALR_DEV unsigned long long pack(const uint4& p, int id) {
+  ALR_DEV unsigned long long pack(const uint4& p, int id, float least) { return few(p, id, least); }
+  ALR_DEV unsigned long long few(const uint4& p, int id, float least) {
     unsigned long long s = 0;
-#pragma unroll 1
-    for (int e = 0; e < kPerPack<E>; ++e) s += f(pack_elem_at<E>(p, e), id + e);
+    for (uint32_t bits = reaching<E>(p, least); bits != 0; bits &= bits - 1) {
+      const int e = __ffs(bits) - 1;
+      s += f(pack_elem_at<E>(p, e), id + e);
+    }
     return s;
   }
 };
+
+// The sum of a pack's weights; all lanes of a warp call.
+template <typename E, typename F>
+ALR_DEV unsigned long long sum_of_pack(F& f, const uint4& p, int id, float least) {
+  const bool some = largest<E>(p) >= least;
+  const int lanes = __popc(__ballot_sync(0xffffffffu, some));
+  if (lanes == 0) return 0;
+  if (lanes >= 8) return f.pack(p, id, least);
+  return some ? f.few(p, id, least) : 0ull;
+}
 
 template <typename E, int kPacks, typename F, typename N>
 ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
   Shared& sh = row.sh;
   unsigned long long s = 0;
   row.each_heavy([&](const uint4& p, int id) {
-    if (largest<E>(p) >= least) s += f.pack(p, id);
+    s += sum_of_pack<E>(f, p, id, least);
   });
   s = warp_reduce(s, AddOp());
   row.to_all(&sh.rec[row.record()], s);
@@ -378,7 +401,7 @@ ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
   const unsigned long long n = nth(total);
   if (before < n && n <= before + s)   // this warp holds it
     row.each_until([&](const uint4& p, int id) {
-      const unsigned long long mine = largest<E>(p) >= least ? f.pack(p, id) : 0ull;
+      const unsigned long long mine = sum_of_pack<E>(f, p, id, least);
       unsigned long long incl = mine;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
@@ -448,7 +471,7 @@ ALR_DEV Found find_unit(StreamRow<E>& row, float least, F f, N nth) {
   for (int i = threadIdx.x; i < row.batches; i += blockDim.x) sh.rec[i] = 0;
   __syncthreads();
   const auto of_pack = [&](const uint4& p, int id) {
-    return largest<E>(p) >= least ? f.pack(p, id) : 0ull;
+    return sum_of_pack<E>(f, p, id, least);
   };
   const int most = (row.packs + kStreamThreads - 1) / kStreamThreads;   // packs of a thread
   static_assert(kBatch % 2 == 0, "a batch is whole loads");
@@ -1204,8 +1227,8 @@ ALR_DEV Cut cut_by_steps(R& row, const Cut& cut, const Steps& bin, float least, 
   const bool cut_any = cut.key != 0;
   row.each_heavy([&](const uint4& p, int id) {
     if (!(largest<E>(p) >= lowest)) return;
-#pragma unroll 2
-    for (int e = 0; e < kPerPack<E>; ++e) {
+    for (uint32_t bits = reaching<E>(p, lowest); bits != 0; bits &= bits - 1) {
+      const int e = __ffs(bits) - 1;
       const float x = pack_elem_at<E>(p, e);
       const uint32_t w = worth(x);
       if (w != 0 && (!cut_any || cut.keeps(order_key(x), id + e))) add_bin(sh, bin(x), w);
@@ -1298,7 +1321,17 @@ struct Mass {
     const float w = weight.real(x);
     return w >= min_p || x == weight.m ? __float2uint_rz(w * 2147483648.f) : 0u;
   }
-  ALR_DEV unsigned long long pack(const uint4& p, int id) {
+  ALR_DEV unsigned long long few(const uint4& p, int id, float least) {
+    unsigned long long s = 0;
+    for (uint32_t bits = reaching<E>(p, least); bits != 0; bits &= bits - 1) {
+      const int e = __ffs(bits) - 1;
+      const unsigned long long q = (*this)(pack_elem_at<E>(p, e), id + e);
+      s += q;
+      count += q != 0;
+    }
+    return s;
+  }
+  ALR_DEV unsigned long long pack(const uint4& p, int id, float) {
     unsigned long long s = 0;
     bool at_edge = false;
 #pragma unroll
