@@ -15,7 +15,7 @@
 // exchanged between all warps once, and the gradient is formed from the same registers.  Clusters stay and
 // take rows in turn: while a row is worked on, the next one comes into shared memory, fetched by a warp
 // of its own that reads its label too.  (One row a cluster, loads straight into registers: all blocks
-// load, compute and store in step, memory idles while they compute, 250 us instead of 1xx for 2048 x
+// load, compute and store in step, memory idles while they compute, 250 us for 2048 x
 // 151936 bf16 logits with 40 % of the rows masked.)
 #include "kernels.h"
 #include "launch.h"
@@ -150,6 +150,42 @@ ALR_DEV void store_pack(E* g, int v, int V, const uint4& x) {
     __stcs(reinterpret_cast<uint4*>(g + v), x);
   else
     store_elems(g, v, 0, V, x);
+}
+
+// A warp's consecutive packs to a row whose 16-byte boundaries lie `shift` elements (1 .. kPerPack - 1)
+// before theirs: what goes into one there is the end of one pack and the start of the next.  Called for
+// the thread's packs i in order; `prev`: the thread's pack i - 1.
+template <typename E>
+ALR_DEV void store_shifted(E* g, int v, int V, int shift, bool first, bool last, const uint4& prev,
+                           const uint4& x) {
+  const int lane = threadIdx.x & 31, bytes = shift * int(sizeof(E));
+  // the pack before this one: the lane below's, or the last lane's of the row of packs before
+  const uint32_t own[4] = {x.x, x.y, x.z, x.w};
+  const uint32_t old[4] = {prev.x, prev.y, prev.z, prev.w};
+  uint32_t c[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    c[j] = __shfl_sync(0xffffffffu, lane == 31 ? old[j] : own[j], (lane + 31) & 31);
+    c[j + 4] = own[j];
+  }
+  // the 16 bytes of c that start 16 - bytes in
+  const int from = 3 - (bytes >> 2);
+  uint32_t b[6], s[5];
+#pragma unroll
+  for (int j = 0; j < 6; ++j) b[j] = from & 2 ? c[j + 2] : c[j];
+#pragma unroll
+  for (int j = 0; j < 5; ++j) s[j] = from & 1 ? b[j + 1] : b[j];
+  const uint32_t pick = bytes & 2 ? 0x5432u : 0x7654u;
+  const uint4 o = make_uint4(__byte_perm(s[0], s[1], pick), __byte_perm(s[1], s[2], pick),
+                             __byte_perm(s[2], s[3], pick), __byte_perm(s[3], s[4], pick));
+  const int at = v - shift;
+  if (first && lane == 0)   // the end of another warp's pack is that warp's
+    store_elems(g, v, 0, min(V, v + kPerPack<E> - shift), x);
+  else if (at >= 0 && at + kPerPack<E> <= V)
+    __stcs(reinterpret_cast<uint4*>(g + at), o);
+  else
+    store_elems(g, at, 0, V, o);
+  if (last && lane == 31) store_elems(g, v, max(0, v + kPerPack<E> - shift), V, x);
 }
 
 // What a block's first warp makes of the cluster's records, for all of its warps.
@@ -482,9 +518,15 @@ __global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
               store_pack(g, at.elem(i), a.V, grad_pack<E>(raw[i], k, out_b, out_c));
           }
         } else {
+          const int shift =
+              (int(r * a.ldg % kPerPack<E>) - at.off + kPerPack<E>) % kPerPack<E>;
+          uint4 prev = make_uint4(0, 0, 0, 0);
 #pragma unroll
-          for (int i = 0; i < kPacks; ++i)
-            store_elems(g, at.elem(i), 0, a.V, grad_pack<E>(raw[i], k, out_b, out_c));
+          for (int i = 0; i < kPacks; ++i) {
+            const uint4 x = grad_pack<E>(raw[i], k, out_b, out_c);
+            store_shifted(g, at.elem(i), a.V, shift, i == 0, i == kPacks - 1, prev, x);
+            prev = x;
+          }
         }
         // over them, the listed tokens of this block's range
         named_bar_sync(kBarWritten, threads);

@@ -56,6 +56,7 @@ struct Shared {
   int count[kWarpsMost + 1];              // first block: in each warp's places; then their offsets
   uint32_t small[256];                    // histogram of the list's keys
   unsigned long long rec[kWarpsMost];     // of each warp of the cluster (or batch of a streamed row): a sum
+  unsigned long long rec2[kWarpsMost];
   unsigned long long grid[8 * kStreamThreads / 32];   // of a batch's packs and warps
   float2 frec[kWarpsMost];
   float fbuf[32];                         // and the bound's result
@@ -824,7 +825,7 @@ ALR_DEV void collect(R& row, float least, float most, F take) {
 // row_bound and collect in one reading of the row by one block, for up to kStreamFew tokens: the K-th
 // largest of the threads' largest logits, once the first packs are there (and again after the next ones),
 // is a bound that every later pack is held against as it comes by.
-constexpr int kStreamFew = 128;
+constexpr int kStreamFew = 200;
 
 template <typename R>
 ALR_DEV Bound bound_and_collect(R& row, int K) {
@@ -847,7 +848,7 @@ ALR_DEV Bound bound_and_collect(R& row, int K) {
           top[j] = largest<E>(raw[j]);
           most = fmaxf(most, top[j]);
         }
-        if (b < 2 || least == kNegInf) {   // bit by bit of the upper half of the keys
+        if (b < 2 || K > 64 || least == kNegInf) {   // bit by bit of the upper half of the keys
           const uint32_t key = most > kNegInf ? order_key(most) >> 16 : 0u;
           uint32_t bound = 0;
           for (uint32_t bit = 0x8000u; bit != 0; bit >>= 1)
@@ -1064,15 +1065,21 @@ ALR_DEV void top_logits_row(R& row, int K, float inv_t, const TopOut& out, long 
       out.val[r * K + i] = i < got ? key_value(entry_key(sh.few.all[i])) : kNegInf;
       out.idx[r * K + i] = i < got ? entry_id(sh.few.all[i]) : -1;
     }
-    // the rest: candidates past the K first, and all others
+    // the rest: candidates past the K first, and all others (who have the candidates below `least`, which
+    // a streamed row collected before its bound rose)
     float mo = kNegInf;
-    for (int i = K + tid; i < n; i += threads) mo = fmaxf(mo, key_value(entry_key(sh.few.all[i])));
+    for (int i = K + tid; i < n; i += threads) {
+      const float v = key_value(entry_key(sh.few.all[i]));
+      if (v >= least) mo = fmaxf(mo, v);
+    }
     for (int i = tid; i < row.records(); i += threads) mo = fmaxf(mo, sh.frec[i].x);
     mo = block_reduce(mo, MaxOp(), sh.fbuf);
     float so = 0.f, sl = 0.f;
     if (mo > kNegInf) {
-      for (int i = K + tid; i < n; i += threads)
-        so += ex2((key_value(entry_key(sh.few.all[i])) - mo) * k);
+      for (int i = K + tid; i < n; i += threads) {
+        const float v = key_value(entry_key(sh.few.all[i]));
+        if (v >= least) so += ex2((v - mo) * k);
+      }
       for (int i = tid; i < row.records(); i += threads)
         if (sh.frec[i].x > kNegInf) so += sh.frec[i].y * ex2((sh.frec[i].x - mo) * k);
     }
@@ -1212,48 +1219,86 @@ struct Steps {
 // The cut that keeps, of the tokens of positive weight that `cut` keeps, the first ones whose summed worth
 // need() still asks for before them (one at least); `cut` itself when need() is content with all of them.
 // worth: 0 .. 2^31 for x, 0 where the weight is 0, as it is below `least`.
+// The histogram is of the logits that reach `near` first: a trained model's nucleus ends among those few,
+// and a place in a histogram is what costs most here.  Where it goes on, all logits have one.
 template <typename R, typename W, typename Need>
-ALR_DEV Cut cut_by_steps(R& row, const Cut& cut, const Steps& bin, float least, W worth, Need need) {
+ALR_DEV Cut cut_by_steps(R& row, const Cut& cut, const Steps& bin, float least, float near, W worth,
+                         Need need) {
   using E = typename R::E;
   Shared& sh = row.sh;
   const int tid = threadIdx.x, threads = blockDim.x;
-  for (int b = tid; b < kBins; b += threads) sh.many.lo[b] = sh.many.hi[b] = 0;
-  if (tid == 0) {
-    sh.n_more = 0;
-    sh.digit = 0xffffffffu;
-  }
-  __syncthreads();
   const float lowest = fmaxf(least, key_value(cut.key));
   const bool cut_any = cut.key != 0;
-  row.each_heavy([&](const uint4& p, int id) {
-    if (!(largest<E>(p) >= lowest)) return;
-    for (uint32_t bits = reaching<E>(p, lowest); bits != 0; bits &= bits - 1) {
-      const int e = __ffs(bits) - 1;
-      const float x = pack_elem_at<E>(p, e);
-      const uint32_t w = worth(x);
-      if (w != 0 && (!cut_any || cut.keeps(order_key(x), id + e))) add_bin(sh, bin(x), w);
-    }
-  });
-  row.sync();
-  total_bins(row, kBins);
   const int n = (kBins + threads - 1) / threads;
-  unsigned long long mine = 0;
-  for (int j = tid * n; j < min(kBins, (tid + 1) * n); ++j) mine += sh.many.total[j];
-  unsigned long long incl = mine;
+  unsigned long long run = 0;
+  for (float from = fmaxf(near, lowest);; from = lowest) {
+    for (int b = tid; b < kBins; b += threads) sh.many.lo[b] = sh.many.hi[b] = 0;
+    if (tid == 0) {
+      sh.n_more = 0;
+      sh.digit = 0xffffffffu;
+    }
+    __syncthreads();
+    unsigned long long below = 0;   // what has no place in the histogram
+    row.each_heavy([&](const uint4& p, int id) {
+      const bool some = largest<E>(p) >= lowest;
+      const int lanes = __popc(__ballot_sync(0xffffffffu, some));
+      const auto place = [&](float x, int v, uint32_t w) {
+        if (w != 0 && (!cut_any || cut.keeps(order_key(x), v))) add_bin(sh, bin(x), w);
+      };
+      if (from > lowest && lanes >= 8) {
+        uint32_t bits = 0;
 #pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
-    if (row.lane >= off) incl += t;
+        for (int e = 0; e < kPerPack<E>; ++e) {
+          const float x = pack_elem<E>(p, e);
+          const uint32_t w = worth(x);
+          below += x >= from ? 0u : w;
+          bits |= uint32_t(x >= from) << e;
+        }
+        for (; bits != 0; bits &= bits - 1) {
+          const int e = __ffs(bits) - 1;
+          const float x = pack_elem_at<E>(p, e);
+          place(x, id + e, worth(x));
+        }
+      } else if (some) {
+        for (uint32_t bits = reaching<E>(p, lowest); bits != 0; bits &= bits - 1) {
+          const int e = __ffs(bits) - 1;
+          const float x = pack_elem_at<E>(p, e);
+          const uint32_t w = worth(x);
+          if (x >= from)
+            place(x, id + e, w);
+          else
+            below += w;
+        }
+      }
+    });
+    below = warp_reduce(below, AddOp());
+    row.to_all(&sh.rec[row.record()], below);
+    row.sync();
+    total_bins(row, kBins);
+    unsigned long long mine = 0;
+    for (int j = tid * n; j < min(kBins, (tid + 1) * n); ++j) mine += sh.many.total[j];
+    unsigned long long incl = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
+      if (row.lane >= off) incl += t;
+    }
+    if (row.lane == 31) sh.lbuf[row.warp] = incl;
+    __syncthreads();
+    run = incl - mine;
+    unsigned long long placed = 0, rest = 0;
+    for (int w = 0; w < row.n_warps; ++w) {
+      if (w < row.warp) run += sh.lbuf[w];
+      placed += sh.lbuf[w];
+    }
+    for (int i = row.lane; i < row.records(); i += 32) rest += sh.rec[i];
+    rest = warp_reduce(rest, AddOp());
+    need.set(placed + rest);
+    // (what follows is the same in all threads of the cluster)
+    if (!need(placed)) break;
+    if (from == lowest) return cut;   // all of them
+    row.sync();
   }
-  if (row.lane == 31) sh.lbuf[row.warp] = incl;
-  __syncthreads();
-  unsigned long long run = incl - mine, total = 0;
-  for (int w = 0; w < row.n_warps; ++w) {
-    if (w < row.warp) run += sh.lbuf[w];
-    total += sh.lbuf[w];
-  }
-  need.set(total);
-  if (need(total)) return cut;   // all of them (uniform: nothing below is waited for)
   for (int j = tid * n; j < min(kBins, (tid + 1) * n); ++j) {
     const unsigned long long t = sh.many.total[j];
     if (t != 0 && (run == 0 || need(run)) && !need(run + t)) {
@@ -1370,9 +1415,12 @@ __device__ __noinline__ void sample_many(R row, const Weight weight, bool greedy
     cut = cut_top_k(row, 1);
   } else {
     if (top_k > 0 && top_k < row.V)
-      cut = cut_by_steps(row, cut, bin, least, [&](float x) { return weight(x) != 0 ? 1u : 0u; },
+      cut = cut_by_steps(row, cut, bin, least, least, [&](float x) { return weight(x) != 0 ? 1u : 0u; },
                          NeedCount{(unsigned long long)top_k});
-    if (top_p < 1.f) cut = cut_by_steps(row, cut, bin, least, weight, NeedMass{double(top_p), 0.0});
+    if (top_p < 1.f) {
+      cut = cut_by_steps(row, cut, bin, least, cut.key == 0 ? weight.below(0x1p-16f) : least, weight,
+                         NeedMass{fmax(double(top_p), 0.0), 0.0});
+    }
   }
   const bool all = cut.key == 0;
   Mass<typename R::E> mass{weight, all ? kNegInf : key_value(cut.key), all ? 0x7fffffff : cut.last, min_p, 0};

@@ -116,6 +116,26 @@ def test_top_logits_ties_masks_and_special_rows(dtype, V):
         _check_top(_rows(z, dtype, V + 3), K)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V,stride", [(2048, 0), (5003, 5007), (33001, 0), (140000, 140008)])
+def test_top_logits_of_many_rows(dtype, V, stride):
+    """As many rows as the device has SMs and more, each read by one block: logits in no order, rising and
+    falling along the row (the largest last, or all first), masked to a stretch, all equal."""
+    N = 330 if V < 10000 else 170
+    z = _logits(N, V, V, masked=V // 50)
+    up = torch.arange(V).float() / V
+    z[3], z[4] = 9 * up, -9 * up
+    z[5] += 30 * up
+    z[6, V // 60:] = NEG
+    z[7, : V - V // 60] = NEG
+    z[8] = NEG
+    z[9] = 1.5
+    z[10] = (up * 20).floor()
+    Z = _rows(z, dtype, stride)
+    for K in (1, 8, 64, 199, 256) if V < 100000 else (8, 199):
+        _check_top(Z, K, T=0.9)
+
+
 # ------------------------------------------------------------------------ distillation ---
 def _teacher(N, V, K, T, seed, dtype=F32):
     t = lo.top_logits(_logits(N, V, seed).numpy(), K, T)
@@ -194,6 +214,22 @@ def test_distill(dtype, tail, N, V, K, stride):
         weight[1] = 0.0
     _check_distill(_rows(_logits(N, V, V + 1), dtype, stride), val, idx, rest if tail else None,
                    weight, T, lam, ldg=stride)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [5, 33, 1001, 9999, 60001])
+@pytest.mark.parametrize("apart", [(0, 1), (3, 0), (5, 2), (8, 3)])
+def test_distill_rows_of_two_alignments(dtype, V, apart):
+    """Rows of Z and of G that start at different places of their 16-byte packs, every difference of them
+    among the rows; nothing outside a row is written."""
+    N, K = 17 if V < 10000 else 9, 4
+    val, idx, rest = _teacher(N, V, K, 1.0, seed=V)
+    Z = _rows(_logits(N, V, V + 2), dtype, V + apart[0])
+    ldg = V + apart[1]
+    _check_distill(Z, val, idx, rest, None, 1.0, 1.0, ldg=ldg)
+    buf = torch.full((N, ldg + 3), 77.0, dtype=dtype, device="cuda")
+    alr.alr_distill_fwd_bwd(Z, val, idx, _distill_out(N), buf[:, :V], rest=rest)
+    assert (buf[:, V:] == 77).all()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -350,6 +386,40 @@ def test_sample_settings_differ_by_row(dtype):
     same = _check_sample(z, _draws(N, 7), T, top_k=k, top_p=p, min_p=m)
     for key in out:
         assert torch.equal(out[key], same[key])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V,stride,scale", [(2048, 0, 3.0), (5003, 5007, 1.3), (33001, 0, 1.3),
+                                            (120000, 120008, 4.0)])
+def test_sample_of_many_rows(dtype, V, stride, scale):
+    """As many rows as the device has SMs and more, each with settings of its own; among them masked
+    stretches, constant rows, steps of equal logits and rows without a candidate."""
+    N = 340 if V < 10000 else 160
+    g = torch.Generator().manual_seed(V)
+    r = lambda: torch.rand(N, generator=g).cuda()  # noqa: E731
+    z = _logits(N, V, V + 1, scale=scale, masked=V // 50)
+    up = torch.arange(V).float() / V
+    z[3], z[4] = 9 * up, -9 * up
+    z[5, V // 60:] = NEG
+    z[6, : V - V // 60] = NEG
+    z[7] = NEG
+    z[8] = 1.5
+    z[9] = (up * 20).floor()
+    z[10] = float("nan")
+    z[11, 1::3] = float("nan")
+    Z = _rows(z, dtype, stride)
+    T = torch.where(r() < 0.15, 0.0, 0.2 + 1.5 * r())
+    T[3:12] = 1.0
+    k = torch.where(r() < 0.4, 0, 1 + (r() * 300).int()).int()
+    k[12], k[13] = 1500, V - 1
+    p = torch.where(r() < 0.4, 1.0, r())
+    m = torch.where(r() < 0.6, 0.0, r() * 0.3)
+    _check_sample(Z, _draws(N, 3), T, top_k=k, top_p=p, min_p=m)
+    if V > 100000:
+        return
+    k[:], p[:] = 0, 0.9
+    _check_sample(Z, _draws(N, 4), T, top_p=p)
+    _check_sample(Z, _draws(N, 5), T)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
