@@ -1446,8 +1446,8 @@ int check_distill_grad(const alr_distill_params* p, const void* Z, const void* G
 }
 
 alr::DistillArgs distill_args(const alr_distill_params* p) {
-  return {p->N, p->ldz, p->ldg, p->V, p->K, p->dtype == ALR_BF16 ? 0 : 1, 1.f / p->temperature,
-          p->lambda};
+  return {p->N, p->ldz, p->ldg, p->V, p->K, p->dtype == ALR_BF16 ? 0 : 1, p->temperature,
+          1.f / p->temperature, p->lambda};
 }
 
 int run_distill(const alr_distill_params* p, bool fwd, bool grad, const void* Z,

@@ -11,12 +11,16 @@
 // off the whole sum would leave rounding errors of the size of the list's own).  Differences of
 // logits are taken before the division by T: they are exact for neighbours.
 //
-// Memory-bound: a row is read once, into the registers of a cluster (row_cluster.cuh), its sums are
-// exchanged between all warps once, and the gradient is formed from the same registers.  Clusters stay and
-// take rows in turn: while a row is worked on, the next one comes into shared memory, fetched by a warp
-// of its own that reads its label too.  (One row a cluster, loads straight into registers: all blocks
-// load, compute and store in step, memory idles while they compute, 250 us for 2048 x
-// 151936 bf16 logits with 40 % of the rows masked.)
+// A row is read once, into the registers of a cluster (row_cluster.cuh), its sums are exchanged between all
+// warps once, and the gradient is formed from the same registers.  Clusters stay and take rows in turn: while
+// a row is worked on, the next one comes into shared memory, fetched by a warp of its own that reads its
+// label too.  (One row a cluster, loads straight into registers: all blocks load, compute and store in
+// step and memory idles while they compute, 250 us instead of 215 for 2048 x 151936 bf16 logits with 40 %
+// of the rows masked.)  4.6 TB/s then, 0.68 of the copy rate; the gradient alone, whose blocks wait for
+// nobody, 4.55 TB/s on rows of two alignments (2000 x 60001).  What is left is the blocks' waits for one
+// another's sums (a third of a row's 17 K cycles).  Tried and slower: the sums of the next row taken before
+// the last one's gradient, so that nobody waits (280 us with both rows in registers and one block to an SM,
+// 293 with rows over 8 blocks), the next row brought into L2 only (no change).
 #include "kernels.h"
 #include "launch.h"
 #include "row_cluster.cuh"
@@ -201,6 +205,17 @@ struct RowSums {
 // r = m k + b, the same for every x, which the caller takes off once.
 ALR_DEV float ref_offset(float m, float k) { return -m * k; }
 ALR_DEV float ref_residual(float m, float k) { return fmaf(m, k, ref_offset(m, k)); }
+
+// exp(x / T - lse) = 2^((x - ref) k + log_scale) with ref a logit next to T lse: the products then are of
+// small numbers, and what ref leaves of lse is the scale.  (exp2(x k - lse log2 e) loses 2^-24 |lse| on the
+// way, up to half as much again as lse's own rounding costs.)
+struct FromLse {
+  float ref, log_scale;
+};
+ALR_DEV FromLse from_lse(float lse, float t, float k) {
+  const float ref = lse * t;
+  return {ref, fmaf(-lse, t, ref) * k};
+}
 
 // Named barriers: the row's data and label are there; the data is in registers (of the fetching warp
 // and the others); the sums are there; the gradient outside the list is written (of the others).
@@ -448,23 +463,27 @@ __global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
             sums.top = mo == top && any ? top : __builtin_nanf("");
             sums.writer = mo == top && any ? first : 0;
             if (rank == 0) {
-              o.lse[r] = mt * a.inv_t + ls;
-              if (o.lse_rest != nullptr) o.lse_rest[r] = any ? mo * a.inv_t + lo : kNegInf;
+              o.lse[r] = mt / a.t + ls;
+              if (o.lse_rest != nullptr) o.lse_rest[r] = any ? mo / a.t + lo : kNegInf;
             }
           }
         } else if (lane == 0) {
           const float lse = o.lse[r], lse_rest = rest != nullptr ? o.lse_rest[r] : kNegInf;
-          if (!(lse > kNegInf)) c = 0.f;
+          const bool known = lse > kNegInf, rest_known = lse_rest > kNegInf;
+          if (!known) c = 0.f;
           sums.c = c;
-          sums.ref = 0.f;
-          sums.b = lse > kNegInf ? -lse * kLog2e : 0.f;
+          const FromLse q = from_lse(known ? lse : 0.f, a.t, k);
+          sums.ref = q.ref;
+          sums.b = q.log_scale;
           if (rest == nullptr) {
-            sums.out_b = sums.b;
-            sums.out_c = c;
+            sums.out_b = ref_offset(q.ref, k);
+            sums.out_c = c * ex2(q.log_scale - ref_residual(q.ref, k));
           } else {
-            const bool known = lse_rest > kNegInf;
-            sums.out_b = known ? -lse_rest * kLog2e : 0.f;
-            sums.out_c = known ? c * (expf(lse_rest - lse) - lab.p0) : 0.f;
+            const FromLse o = from_lse(rest_known ? lse_rest : 0.f, a.t, k);
+            sums.out_b = ref_offset(o.ref, k);
+            sums.out_c = rest_known ? c * (expf(lse_rest - lse) - lab.p0) *
+                                          ex2(o.log_scale - ref_residual(o.ref, k))
+                                    : 0.f;
           }
         }
       }

@@ -16,7 +16,8 @@ struct alignas(sizeof(E) * kCols) Pack {
 
 // ---------------------------------------------------------------------- lookup ---
 // out[i] = scale * E[token_i] (fp32 product, rounded once); a token outside [0, V) gives zeros.
-// Memory-bound: a warp moves 32 kEmbedBatch packs of one row, all loads issued before the stores.
+// Memory-bound: a warp moves 32 kEmbedBatch packs of one row, all loads issued before the stores
+// (32768 x 4096 bf16 rows, 15 of 16 the same token: 43.5 us, 6.55 TB/s).
 constexpr int kEmbedThreads = 256;
 constexpr int kEmbedBatch = 8;
 
@@ -55,7 +56,11 @@ __global__ void __launch_bounds__(kEmbedThreads)
 //   A run of at most P rows belongs to the chunk that it starts in, which follows it into the
 // next one and writes the table's row.  A longer run leaves one partial sum in each chunk that it
 // touches, and a last kernel adds those in order.
-// Few rows take one kernel instead, in which the block of each row looks for its token's others.
+//   32768 x 2048 bf16 rows into a 32000-token fp32 table, 15 of 16 rows one token: 101 us; sort 21 (latency of
+// its two passes on 8 SMs), chunks and the zeros of absent tokens 66 (396 MB, 6 TB/s), join 12.  The zeros
+// written beside the sort instead, by blocks that look up their rows themselves: 149 us.
+// Few rows take one kernel instead, in which the block of each row looks for its token's others (192 rows
+// with their lookup: 12 us, two launches, most of it the host's two calls).
 
 template <typename E, int kCols>
 ALR_DEV void add_pack(float (&acc)[kCols], const Pack<E, kCols>& x) {
@@ -189,7 +194,8 @@ struct GradPlan {
   size_t tok_off[2], row_off[2], list_off, count_off, present_off, part_off, total;
 };
 
-// Rows of a chunk: enough chunks to fill the device, few partial sums for a token in every row.
+// Rows of a chunk: enough chunks to fill the device, few partial sums for a token in every row (32768
+// rows: 101 us at 64, 110 at 32).
 GradPlan grad_plan(int V, int d, int N) {
   GradPlan g{};
   g.chunk = N <= 8192 ? 16 : N <= 16384 ? 32 : N <= 65536 ? 64 : 128;

@@ -227,7 +227,7 @@ cudaError_t launch_transpose32_pair(const float* a, float* a_out, int Ca, const 
 struct DistillArgs {
   long long N, ldz, ldg;   // rows, row strides of the logits and of the gradient (elements)
   int V, K, dtype;
-  float inv_t, lambda;     // 1 / temperature
+  float t, inv_t, lambda;  // temperature, 1 / temperature
 };
 struct DistillRows {       // per-row results; a gradient alone reads lse and lse_rest
   float* loss_row;
