@@ -703,7 +703,10 @@ ALR_DEV Bound row_bound(R& row, int K) {
   float top = kNegInf;
   for (int i = row.lane; i < n_rec; i += 32) top = fmaxf(top, sh.few.list[i * per]);
   top = warp_max(top);
-  if (K <= 1) return {K == 1 ? top : kNegInf, top};
+  if (K <= 1) {
+    __syncthreads();   // every warp has read the list: a histogram is cleared over it next
+    return {K == 1 ? top : kNegInf, top};
+  }
   if (n <= kListWarp) {   // the upper half of the K-th largest key, bit by bit
     if (row.warp == 0) {
       uint32_t key[kListWarp / 32], least = 0;
@@ -1219,11 +1222,12 @@ ALR_DEV void draw_from_candidates(Shared& sh, int n, const Weight& weight, float
   }
 }
 
-// Even steps of the logit below the largest, kBins over the 32 octaves below which weights are 0.
+// Even steps of the logit below the largest, kBins over the 32 octaves below which weights are 0.  The
+// conversion takes anything below 0 to 0: no logit has a place outside the bins.
 struct Steps {
   float top, scale;
   ALR_DEV int operator()(float x) const {
-    return min(kBins - 1, __float2int_rz((top - x) * scale));
+    return int(min(uint32_t(kBins - 1), __float2uint_rz((top - x) * scale)));
   }
 };
 

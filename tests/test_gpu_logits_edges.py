@@ -1,0 +1,47 @@
+"""Edges of the operators on logits in hand: calls repeated for the same bits, settings and temperatures at
+the ends of their ranges, masks of the type's lowest value.  Tolerances are those of test_gpu_logits.py
+unless a test derives its own."""
+
+import pytest
+import torch
+
+from paper_2609_38795_gb300 import alr
+from tests.test_gpu_logits import (BF, F32, _check_sample, _draws, _lib, _logits, _new,  # noqa: F401
+                                   _rows)
+
+pytestmark = pytest.mark.gpu
+
+
+def _trained(N, V, seed, lift=24.0):
+    """A few tokens far above a wide bulk: the largest logit is nowhere near 0."""
+    z = _logits(N, V, seed, scale=2.5)
+    n = min(40, V)
+    g = torch.Generator().manual_seed(seed + 1)
+    tok = torch.randint(0, V, (N, n), generator=g)
+    return z.scatter(1, tok, lift - 0.5 * torch.arange(n).float().expand(N, n))
+
+
+def _same_every_time(Z, u, T, repeats, **kw):
+    """The oracle's draws, and the same bits in every one of many calls in a row."""
+    want = _check_sample(Z, u, T, **kw)
+    outs = [dict(token=_new(len(u), dtype=torch.int32), prob=_new(len(u)),
+                 n_kept=_new(len(u), dtype=torch.int32)) for _ in range(repeats)]
+    for out in outs:
+        alr.alr_sample_tokens(Z, u, out, temperature=T, **kw)
+    for out in outs:
+        for key, x in out.items():
+            assert torch.equal(x.view(torch.int32), want[key].view(torch.int32)), key
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("N,V", [(330, 2048), (330, 5003), (24, 5003), (3, 40001)])
+def test_nucleus_draws_are_the_same_in_every_call(dtype, N, V):
+    """No top-k, or one past the few: the row's largest logit goes straight into a histogram.  Rows one block
+    reads, several blocks to an SM, and rows of clusters; largest logits far above and far below 0."""
+    for lift in (24.0, -50.0):
+        Z = _rows(_trained(N, V, V, lift) + min(lift, 0.0), dtype)
+        f = lambda x: torch.full((N,), x, device="cuda")  # noqa: E731
+        _same_every_time(Z, _draws(N, 1), f(0.9), 40, top_p=f(0.95))
+        _same_every_time(Z, _draws(N, 2), f(1.3), 10, min_p=f(0.01))
+        _same_every_time(Z, _draws(N, 3), f(1.1), 10, top_p=f(0.9),
+                         top_k=torch.full((N,), 700, dtype=torch.int32, device="cuda"))
