@@ -897,7 +897,9 @@ ALR_DEV Bound bound_and_collect(R& row, int K) {
 // Whether all candidates fit, known to all blocks.  The others then wait in the cluster barrier until all
 // have read it; the first block arrives at once and waits (others_know) when it likes to.
 ALR_DEV bool candidates_fit(const RowCommon<true>& row) {
-  return row.records() * kSlots + row.sh.n_more <= kCandMost;
+  const bool fit = row.records() * kSlots + row.sh.n_more <= kCandMost;
+  if (!fit) __syncthreads();   // all have read it: what the block does then begins with setting it to 0
+  return fit;
 }
 ALR_DEV void others_know(const RowCommon<true>&) {}
 ALR_DEV bool candidates_fit(const RowCommon<false>& row) {

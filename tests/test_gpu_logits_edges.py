@@ -45,3 +45,31 @@ def test_nucleus_draws_are_the_same_in_every_call(dtype, N, V):
         _same_every_time(Z, _draws(N, 2), f(1.3), 10, min_p=f(0.01))
         _same_every_time(Z, _draws(N, 3), f(1.1), 10, top_p=f(0.9),
                          top_k=torch.full((N,), 700, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V", [2048, 9001])
+def test_draws_among_many_equal_tokens_are_the_same_in_every_call(dtype, V):
+    """Rows that one block reads, several blocks to an SM, whose candidates do not fit: constant rows, steps of
+    equal logits, rows with fewer tokens left than the top-k, +inf in some."""
+    N = 330
+    z = torch.full((N, V), 1.5)
+    up = torch.arange(V).float() / V
+    z[0::5] = (up * 3).floor() - 40
+    z[1::5, V // 70:] = float("-inf")
+    z[2::5] = _trained(len(z[2::5]), V, V)
+    z[3::40, 7] = float("inf")
+    finite = z.clone()
+    finite[3::40] = float("-inf")
+    finite[3::40, 7] = 0.0                                   # all mass on the +inf
+    i = lambda x: torch.full((N,), x, dtype=torch.int32, device="cuda")  # noqa: E731
+    T = torch.full((N,), 0.8, device="cuda")
+    for k, p in ((50, 0.95), (190, 1.0), (230, 0.5), (1, 1.0)):
+        kw = dict(top_k=i(k), top_p=torch.full((N,), p, device="cuda"))
+        want = _check_sample(_rows(finite, dtype), _draws(N, k), T, **kw)
+        for _ in range(30):
+            out = dict(token=_new(N, dtype=torch.int32), prob=_new(N), n_kept=_new(N, dtype=torch.int32))
+            alr.alr_sample_tokens(_rows(z, dtype), _draws(N, k), out, temperature=T, **kw)
+            for key, x in out.items():
+                assert torch.equal(x, want[key]), key
+    _same_every_time(_rows(finite, dtype), _draws(N, 9), torch.zeros(N, device="cuda"), 30)
