@@ -670,7 +670,8 @@ int alr_distill_fwd_bwd(const alr_distill_params* p, const void* Z, const float*
 /*
  * One token per row, drawn from given random numbers (as the draws of alr_ira_draw).
  *   u [N] uint32: independent uniform random integers.
- *   temperature [N] float or NULL (1): <= 0 takes the greedy token.
+ *   temperature [N] float or NULL (1): <= 0, NaN, or so small that log2(e) / temperature overflows
+ *            (below 4.24e-39) takes the greedy token.
  *   top_k [N] int32 or NULL: keep the k first tokens in the order (value descending, id ascending);
  *            <= 0 keeps all.
  *   top_p [N] float or NULL: then, in that order, the tokens before which less than top_p of the

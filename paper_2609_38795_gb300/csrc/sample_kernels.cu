@@ -1468,7 +1468,9 @@ ALR_DEV void sample_row(R& row, const SampleArgs& a, const SampleOut& out, long 
   const float top_p = a.top_p != nullptr ? a.top_p[r] : 1.f;
   const float min_p = a.min_p != nullptr ? fminf(a.min_p[r], 1.f) : 0.f;
   const uint32_t u = a.u[r];
-  const bool greedy = !(T > 0.f);
+  // (a scale that overflows would make the largest token's weight 0 * inf: T = 0 is its limit)
+  const float scale = __fdiv_rn(kLog2e, T);
+  const bool greedy = !(T > 0.f) || scale == -kNegInf;
   const int K = greedy ? 1 : top_k > 0 && top_k <= kTopMost ? top_k : 0;   // few tokens
   const Bound bound = K > 0 ? bound_and_collect(row, K) : row_bound(row, 0);
   if (!(bound.top > kNegInf)) {   // no candidate; all blocks agree, and none reads another's memory
@@ -1476,7 +1478,7 @@ ALR_DEV void sample_row(R& row, const SampleArgs& a, const SampleOut& out, long 
     return;
   }
   const bool infinite = bound.top == -kNegInf;
-  const Weight weight{infinite ? 0.f : bound.top, greedy ? 0.f : __fdiv_rn(kLog2e, T)};
+  const Weight weight{infinite ? 0.f : bound.top, greedy ? 0.f : scale};
   if (K > 0 && (!infinite || K == 1)) {   // (with K = 1 only +inf reaches the bound)
     if (candidates_fit(row)) {
       if (row.rank != 0) return;

@@ -73,3 +73,28 @@ def test_draws_among_many_equal_tokens_are_the_same_in_every_call(dtype, V):
             for key, x in out.items():
                 assert torch.equal(x, want[key]), key
     _same_every_time(_rows(finite, dtype), _draws(N, 9), torch.zeros(N, device="cuda"), 30)
+
+
+# Below log2(e) / the largest float a temperature's scale is infinite; 5e-39 is above.
+TINY = 4e-39
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("N,V", [(8, 5003), (330, 2048)])
+def test_temperatures_too_small_for_a_scale_are_greedy(dtype, N, V):
+    """T = 0 is their limit; every output is written, also where the neighbours draw."""
+    z = _logits(N, V, 61)
+    z[1] = 2.0                                               # the lowest id of equal tokens
+    z[2] = float("-inf")
+    Z = _rows(z, dtype)
+    T = torch.where(torch.arange(N) % 3 == 0, 1.0, TINY).cuda()
+    T[4], T[5], T[7] = 1e-45, 5e-39, float("nan")
+    as_zero = torch.where(T >= 5e-39, T, 0.0)
+    f = lambda x: torch.full((N,), x, device="cuda")  # noqa: E731
+    i = lambda x: torch.full((N,), x, dtype=torch.int32, device="cuda")  # noqa: E731
+    for kw in (dict(), dict(top_k=i(5)), dict(top_p=f(0.9)), dict(min_p=f(0.1)), dict(top_k=i(700))):
+        want = _check_sample(Z, _draws(N, 5), as_zero, **kw)
+        got = dict(token=_new(N, dtype=torch.int32), prob=_new(N), n_kept=_new(N, dtype=torch.int32))
+        alr.alr_sample_tokens(Z, _draws(N, 5), got, temperature=T, **kw)
+        for key in got:
+            assert torch.equal(got[key], want[key]), key
