@@ -677,7 +677,7 @@ int alr_distill_fwd_bwd(const alr_distill_params* p, const void* Z, const float*
  *   top_p [N] float or NULL: then, in that order, the tokens before which less than top_p of the
  *            kept mass lies (one at least); >= 1 keeps all.
  *   min_p [N] float or NULL: then the tokens of at least min_p (at most 1) times the largest
- *            probability.
+ *            probability.  (A top_p or min_p of NaN cuts nothing.)
  * A token's weight is the whole number floor(2^31 exp2((z - max) log2(e) / temperature)), each step
  * rounded to fp32; tokens of weight 0 (below 2^-31 of the largest) are never kept.  Sums of weights
  * are exact, so a draw depends on nothing but its inputs.  With S the weight of the kept tokens:

@@ -1465,8 +1465,9 @@ ALR_DEV void sample_row(R& row, const SampleArgs& a, const SampleOut& out, long 
   Shared& sh = row.sh;
   const float T = a.temperature != nullptr ? a.temperature[r] : 1.f;
   const int top_k = a.top_k != nullptr ? a.top_k[r] : 0;
-  const float top_p = a.top_p != nullptr ? a.top_p[r] : 1.f;
-  const float min_p = a.min_p != nullptr ? fminf(a.min_p[r], 1.f) : 0.f;
+  float top_p = a.top_p != nullptr ? a.top_p[r] : 1.f, min_p = a.min_p != nullptr ? a.min_p[r] : 0.f;
+  if (!(top_p < 1.f)) top_p = 1.f;   // (NaN too)
+  min_p = min_p > 0.f ? fminf(min_p, 1.f) : 0.f;
   const uint32_t u = a.u[r];
   // (a scale that overflows would make the largest token's weight 0 * inf: T = 0 is its limit)
   const float scale = __fdiv_rn(kLog2e, T);

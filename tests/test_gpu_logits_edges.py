@@ -98,3 +98,19 @@ def test_temperatures_too_small_for_a_scale_are_greedy(dtype, N, V):
         alr.alr_sample_tokens(Z, _draws(N, 5), got, temperature=T, **kw)
         for key in got:
             assert torch.equal(got[key], want[key]), key
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("N,V", [(6, 5003), (330, 2048)])
+def test_settings_that_are_not_numbers_cut_nothing(dtype, N, V):
+    """A NaN top_p or min_p is one that is not given, with a top-k and without."""
+    Z = _rows(_logits(N, V, 71), dtype)
+    u, T, nan = _draws(N, 6), torch.full((N,), 0.9, device="cuda"), torch.full((N,), float("nan"), device="cuda")
+    for k in (0, 20, 600):
+        kw = dict(top_k=torch.full((N,), k, dtype=torch.int32, device="cuda"))
+        want = _check_sample(Z, u, T, **kw)
+        for more in (dict(top_p=nan), dict(min_p=nan), dict(top_p=nan, min_p=nan)):
+            got = dict(token=_new(N, dtype=torch.int32), prob=_new(N), n_kept=_new(N, dtype=torch.int32))
+            alr.alr_sample_tokens(Z, u, got, temperature=T, **kw, **more)
+            for key in got:
+                assert torch.equal(got[key], want[key]), (k, more.keys(), key)
