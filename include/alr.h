@@ -591,6 +591,7 @@ int alr_gemm_form(int32_t dtype, int32_t M, int32_t Nc, int32_t K, int32_t* form
  *   top_val [N, K] float, top_idx [N, K] int32: by value descending, equal values by token id
  *            ascending.  A logit of -inf (a masked token) or NaN is never listed: a row with fewer
  *            than K others ends in entries (-inf, -1).
+ *   temperature: finite and at least 4.25e-39, as alr_distill_params'.
  *   lse, lse_rest [N] (nullable): log-sum-exp of z / temperature over the whole row and over the
  *            tokens that are not listed (-inf for none).
  * A row that holds +inf gives unspecified log-sum-exps.
@@ -607,7 +608,8 @@ typedef struct {
     int32_t V;          /* vocabulary, 1 <= V <= ALR_LOGITS_MAX_V                             */
     int32_t K;          /* list length, 1 <= K <= ALR_TOP_MAX                                 */
     int32_t dtype;      /* of Z and G: ALR_BF16 or ALR_F32                                    */
-    float temperature;  /* > 0, finite: divides both sides' logits                            */
+    float temperature;  /* >= 4.25e-39 (log2(e) / temperature is a float), finite: divides
+                           both sides' logits                                                 */
     float lambda;       /* loss scale (a usual choice is temperature^2)                       */
 } alr_distill_params;
 

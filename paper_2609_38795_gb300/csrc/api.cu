@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
@@ -1403,8 +1404,10 @@ int check_logits(const void* Z, int dtype, int64_t N, int32_t V, int64_t ldz) {
 }
 
 int check_temperature(float t) {
-  if (!(t > 0.f) || !(1.f / t > 0.f) || !(1.f / t < 3.4e38f))
-    return fail(ALR_ERR_INVALID_ARG, "temperature must be > 0 and finite");
+  // the kernels multiply by log2(e) / t as well as by 1 / t
+  const float k = 1.f / t * 1.4426950408889634f;
+  if (!(t > 0.f) || !(1.f / t > 0.f) || !std::isfinite(k))
+    return fail(ALR_ERR_INVALID_ARG, "temperature must be finite and at least 4.25e-39");
   return ALR_OK;
 }
 

@@ -122,3 +122,17 @@ def test_binding_refuses_host_tensors():
         alr.alr_top_logits(Z.numpy(), 3, {})
     with pytest.raises(ValueError, match="CUDA device"):
         alr.alr_embed(Z, i, Z)
+
+
+def test_temperatures_whose_scale_overflows_are_refused(lib):
+    """1 / T is a float down to 2.94e-39, log2(e) / T, by which the kernels multiply, down to 4.24e-39."""
+    p = lambda T: alr.AlrDistillParams(N=4, ldz=100, ldg=100, V=100, K=8, dtype=1, temperature=T,  # noqa: E731
+                                       lam=1.0)
+    o = alr.AlrDistillOutputs(**{f: 0x20000 for f in alr._DISTILL_FIELDS})
+    for T in (3e-39, 4.2e-39):
+        for call in (lambda: lib.alr_top_logits(A16, 1, 4, 100, 100, 8, T, A16, A16, None, None, None),
+                     lambda: lib.alr_distill_fwd(ctypes.byref(p(T)), A16, A16, A16, None, None,
+                                                 ctypes.byref(o), None),
+                     lambda: lib.alr_distill_bwd(ctypes.byref(p(T)), A16, A16, A16, None, None, A16, None, A16,
+                                                 A16, None)):
+            assert call() == alr.ALR_ERR_INVALID_ARG and "temperature" in lib.alr_last_error().decode(), T
