@@ -122,15 +122,22 @@ ALR_DEV uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
-// Gradient of a pack, c exp2((x - ref) k + b), in the row's element type; `b` takes ref in.
+// exp2((x - ref) k) of two elements.  The difference first: one fma, x k - ref k, would carry the rounding of
+// ref k, which for logits / T past 2^30 (a mask by a large finite number over a whole stretch of the row, a
+// tiny T) is out of the exponential's range, and of a float's for the type's lowest value: NaN.
+ALR_DEV uint64_t exp2_from(uint64_t x, uint64_t ref, uint64_t k) {
+  return f2_ex2(f2_mul(f2_sub(x, ref), k));
+}
+
+// Gradient of a pack, c exp2((x - ref) k), in the row's element type.
 template <typename E>
-ALR_DEV uint4 grad_pack(const uint4& raw, float k, float b, float c) {
+ALR_DEV uint4 grad_pack(const uint4& raw, float ref, float k, float c) {
   float q[kPerPack<E>];
-  const uint64_t k2 = f2_pack(k, k), b2 = f2_pack(b, b), c2 = f2_pack(c, c);
+  const uint64_t ref2 = f2_pack(ref, ref), k2 = f2_pack(k, k), c2 = f2_pack(c, c);
 #pragma unroll
   for (int e = 0; e < kPerPack<E>; e += 2) {
     const uint64_t x = f2_pack(pack_elem<E>(raw, e), pack_elem<E>(raw, e + 1));
-    f2_unpack(f2_mul(f2_ex2(f2_fma(x, k2, b2)), c2), q[e], q[e + 1]);
+    f2_unpack(f2_mul(exp2_from(x, ref2, k2), c2), q[e], q[e + 1]);
   }
   if constexpr (sizeof(E) == 2)
     return make_uint4(pack_bf16(q[0], q[1]), pack_bf16(q[2], q[3]), pack_bf16(q[4], q[5]),
@@ -195,16 +202,11 @@ ALR_DEV void store_shifted(E* g, int v, int V, int shift, bool first, bool last,
 // What a block's first warp makes of the cluster's records, for all of its warps.
 struct RowSums {
   float ref, b;         // log2 q_v = (z_v - ref) k + b
-  float out_b, out_c;   // gradient outside the list: out_c exp2(z_v k + out_b)
+  float out_ref, out_c; // gradient outside the list: out_c exp2((z_v - out_ref) k)
   float c;              // lambda w / (T sum w); 0 when the row has no gradient
   float top;            // the largest logit if some token outside the list has it, else NaN
   int writer;           // the cluster's warp that writes the greedy token
 };
-
-// exp2((x - m) k) with one fma: exp2(x k + b), b = -m k rounded, carries the factor 2^r with
-// r = m k + b, the same for every x, which the caller takes off once.
-ALR_DEV float ref_offset(float m, float k) { return -m * k; }
-ALR_DEV float ref_residual(float m, float k) { return fmaf(m, k, ref_offset(m, k)); }
 
 // exp(x / T - lse) = 2^((x - ref) k + log_scale) with ref a logit next to T lse: the products then are of
 // small numbers, and what ref leaves of lse is the scale.  (exp2(x k - lse log2 e) loses 2^-24 |lse| on the
@@ -394,19 +396,19 @@ __global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
             m = max3(m, pack_elem<E>(raw[i], e), pack_elem<E>(raw[i], e + 1));
         }
         m = warp_max(m);
-        const float mw = m > kNegInf ? m : 0.f, off = ref_offset(mw, k);
-        const uint64_t off2 = f2_pack(off, off), k2 = f2_pack(k, k);
+        const float mw = m > kNegInf ? m : 0.f;
+        const uint64_t ref2 = f2_pack(mw, mw), k2 = f2_pack(k, k);
         uint64_t s2 = 0;
 #pragma unroll
         for (int i = 0; i < kPacks; ++i)
 #pragma unroll
           for (int e = 0; e < kPerPack<E>; e += 2) {
             const uint64_t x = f2_pack(pack_elem<E>(raw[i], e), pack_elem<E>(raw[i], e + 1));
-            s2 = f2_add(s2, f2_ex2(f2_fma(x, k2, off2)));
+            s2 = f2_add(s2, exp2_from(x, ref2, k2));
           }
         float sa, sb;
         f2_unpack(s2, sa, sb);
-        const float sw = warp_reduce(sa + sb, AddOp()) * ex2(-ref_residual(mw, k));
+        const float sw = warp_reduce(sa + sb, AddOp());
         if (lane < cluster)   // to every block of the cluster
           st_async_f2(cluster_smem_addr(&recs[par][rank * n_warps + warp], lane), m, sw,
                       cluster_smem_addr(&rec_bar[par], lane));
@@ -455,9 +457,8 @@ __global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
             sums.c = c;
             sums.ref = mt;
             sums.b = -ls * kLog2e;
-            const float carried = ref_residual(mo, k) + lo * kLog2e;   // by the fma form, and R
-            sums.out_b = any ? ref_offset(mo, k) : 0.f;
-            sums.out_c = any ? c * (So_t / S - lab.p0) * ex2(-carried) : 0.f;
+            sums.out_ref = any ? mo : 0.f;
+            sums.out_c = any ? c * (So_t / S - lab.p0) / So : 0.f;
             // the greedy token is written by the warp that holds the first of the largest logits
             // outside the list, or by the first warp when the list holds all of them
             sums.top = mo == top && any ? top : __builtin_nanf("");
@@ -476,14 +477,12 @@ __global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
           sums.ref = q.ref;
           sums.b = q.log_scale;
           if (rest == nullptr) {
-            sums.out_b = ref_offset(q.ref, k);
-            sums.out_c = c * ex2(q.log_scale - ref_residual(q.ref, k));
+            sums.out_ref = q.ref;
+            sums.out_c = c * ex2(q.log_scale);
           } else {
             const FromLse o = from_lse(rest_known ? lse_rest : 0.f, a.t, k);
-            sums.out_b = ref_offset(o.ref, k);
-            sums.out_c = rest_known ? c * (expf(lse_rest - lse) - lab.p0) *
-                                          ex2(o.log_scale - ref_residual(o.ref, k))
-                                    : 0.f;
+            sums.out_ref = o.ref;
+            sums.out_c = rest_known ? c * (expf(lse_rest - lse) - lab.p0) * ex2(o.log_scale) : 0.f;
           }
         }
       }
@@ -520,7 +519,7 @@ __global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
         }
       }
       if constexpr ((kMode & kGrad) != 0) {
-        const float c = sums.c, out_b = sums.out_b, out_c = sums.out_c;
+        const float c = sums.c, out_ref = sums.out_ref, out_c = sums.out_c;
         if (c == 0.f) {
 #pragma unroll
           for (int i = 0; i < kPacks; ++i) raw[i] = neg_inf_pack<E>();
@@ -530,11 +529,11 @@ __global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
             uint4* p = reinterpret_cast<uint4*>(g + at.elem(0));
 #pragma unroll
             for (int i = 0; i < kPacks; ++i)
-              __stcs(p + 32 * i, grad_pack<E>(raw[i], k, out_b, out_c));
+              __stcs(p + 32 * i, grad_pack<E>(raw[i], out_ref, k, out_c));
           } else {
 #pragma unroll
             for (int i = 0; i < kPacks; ++i)
-              store_pack(g, at.elem(i), a.V, grad_pack<E>(raw[i], k, out_b, out_c));
+              store_pack(g, at.elem(i), a.V, grad_pack<E>(raw[i], out_ref, k, out_c));
           }
         } else {
           const int shift =
@@ -542,7 +541,7 @@ __global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
           uint4 prev = make_uint4(0, 0, 0, 0);
 #pragma unroll
           for (int i = 0; i < kPacks; ++i) {
-            const uint4 x = grad_pack<E>(raw[i], k, out_b, out_c);
+            const uint4 x = grad_pack<E>(raw[i], out_ref, k, out_c);
             store_shifted(g, at.elem(i), a.V, shift, i == 0, i == kPacks - 1, prev, x);
             prev = x;
           }

@@ -2,12 +2,15 @@
 the ends of their ranges, masks of the type's lowest value.  Tolerances are those of test_gpu_logits.py
 unless a test derives its own."""
 
+import numpy as np
 import pytest
 import torch
 
+from oracle import logits_oracle as lo
 from paper_2609_38795_gb300 import alr
-from tests.test_gpu_logits import (BF, F32, _check_sample, _draws, _lib, _logits, _new,  # noqa: F401
-                                   _rows)
+from tests import parity as P
+from tests.test_gpu_logits import (BF, EPS, F32, LSE_TOL, _check_lse, _check_sample, _distill_out,  # noqa: F401
+                                   _draws, _lib, _logits, _new, _rows)
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +117,88 @@ def test_settings_that_are_not_numbers_cut_nothing(dtype, N, V):
             alr.alr_sample_tokens(Z, u, got, temperature=T, **kw, **more)
             for key in got:
                 assert torch.equal(got[key], want[key]), (k, more.keys(), key)
+
+
+def _masks(V, K, value):
+    """A row's tokens masked to `value` in long stretches: none, the upper half, the lower third, all but
+    three tokens (fewer than the list's), all but the K (+ 2) tokens of the list and two more."""
+    m = torch.zeros(5, V, dtype=torch.bool)
+    m[1, V // 2:] = True
+    m[2, : V // 3] = True
+    m[3], m[3, [5, V // 2, V - 1]] = True, False
+    m[4], m[4, V // 7: V // 7 + K] = True, False
+    return m, value
+
+
+def _distil_masked(dtype, V, value, T):
+    """(Z, val, idx, rest, live logits' size): student and teacher under the same masks."""
+    K = 8
+    value = torch.finfo(dtype).min if value is None else value
+    m, _ = _masks(V, K, value)
+    z = _logits(5, V, V).masked_fill(m, value)
+    Z = _rows(z, dtype, V + 3)
+    t = lo.top_logits(_logits(5, V, V + 1).to(dtype).double().masked_fill(m, float(Z.min())).numpy(), K, T)
+    with np.errstate(over="ignore"):                         # past fp32's range: -inf
+        f = lambda x: torch.tensor(x.astype(np.float32), device="cuda")  # noqa: E731
+        val, rest = f(t["top_val"]), f(t["lse_rest"])
+    return Z, val, torch.tensor(t["top_idx"], dtype=torch.int32, device="cuda"), rest, z[~m].abs().max().item() / T
+
+
+def _check_masked(Z, val, idx, rest, T, big):
+    """The bounds of test_gpu_logits.py with `big` the live logits' size (a masked logit is not rounded)."""
+    N, V = Z.shape
+    n = lambda t: None if t is None else t.cpu().numpy()  # noqa: E731
+    ref = lo.distill(Z.float().cpu().numpy(), n(val), n(idx), n(rest), None, T, 1.0)
+    kw = dict(rest=rest, temperature=T)
+    out, one, two, G = _distill_out(N), _distill_out(N), Z.clone(), Z.clone()
+    alr.alr_distill_fwd(Z, val, idx, out, **kw)
+    alr.alr_distill_fwd_bwd(Z, val, idx, one, G, **kw)
+    alr.alr_distill_bwd(Z, val, idx, out["lse"], out["lse_rest"] if rest is not None else None, out["weight_sum"],
+                        two, **kw)
+    p_rel = 8 * EPS * (21 + big)
+    for o in (out, one):
+        with np.errstate(over="ignore"):
+            _check_lse(o["lse"], ref["lse"].astype(np.float32).astype(np.float64))
+            if rest is not None:
+                _check_lse(o["lse_rest"], ref["lse_rest"].astype(np.float32).astype(np.float64))
+        assert np.array_equal(P.npi(o["argmax"]), ref["argmax"])
+        tol = 2 * LSE_TOL + p_rel * (np.abs(ref["loss_row"]) + big) + 8 * EPS * big
+        assert (np.abs(P.np64(o["loss_row"]) - ref["loss_row"]) <= tol).all()
+        assert (np.abs(P.np64(o["ent_row"]) - ref["ent_row"]) <= p_rel * (ref["ent_row"] + 4)).all()
+    half = 2.0 ** -8 if Z.dtype == BF else 2 * EPS
+    gtol = ref["size"] * (2 * LSE_TOL + p_rel + 8 * EPS * big) + half * np.abs(ref["G"]) + 1e-36
+    for g in (G, two):
+        assert (np.abs(P.np64(g) - ref["G"]) <= gtol).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("value", [-1e10, -1e30, None])
+@pytest.mark.parametrize("V,T", [(5003, 1.0), (40001, 0.5), (40001, 2.0)])
+def test_distill_with_tokens_masked_by_large_numbers(dtype, tail, value, V, T):
+    """Masks by finite numbers up to the type's lowest value (None), over stretches longer than a warp's part
+    of the row: next to nothing of the mass, no NaN anywhere."""
+    Z, val, idx, rest, big = _distil_masked(dtype, V, value, T)
+    _check_masked(Z, val, idx, rest if tail else None, T, big)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [1e-6, 1e-9, 1e-30])
+def test_distill_at_tiny_temperatures(dtype, T):
+    """Logits / T far past 2^24: losses in proportion, gradients of one-hot rows, nothing overflows on the way."""
+    N, V, K = 4, 3001, 4
+    g = torch.Generator().manual_seed(81)
+    z = torch.stack([torch.randperm(V, generator=g) for _ in range(N)]).float() * 0.125 - 150   # distinct
+    Z = _rows(z if dtype == F32 else (z / 32).round() * 4, dtype)
+    t = lo.top_logits(Z.roll(1, 0).float().cpu().numpy(), K, T)
+    val = torch.tensor(t["top_val"], dtype=F32, device="cuda")
+    idx = torch.tensor(t["top_idx"], dtype=torch.int32, device="cuda")
+    # the oracle from each row's largest on (loss and gradient are the same): logits / T themselves are past fp64
+    below = lambda x: (x - x.max(1, keepdim=True).values).double().cpu().numpy()  # noqa: E731
+    ref = lo.distill(below(Z.double()), below(val.double()), idx.cpu().numpy(), None, None, T, T)
+    out, G = _distill_out(N), Z.clone()
+    alr.alr_distill_fwd_bwd(Z, val, idx, out, G, temperature=T, lam=T)
+    want = ref["loss_row"]
+    assert (np.abs(P.np64(out["loss_row"]) - want) <= 16 * EPS * want + 1e-3).all() and (want > 1).all()
+    # a probability is that of one of n equal tokens, or 0
+    assert (np.abs(P.np64(G) - ref["G"]) <= 2.0 ** -8 * np.abs(ref["G"])).all()
