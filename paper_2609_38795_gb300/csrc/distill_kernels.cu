@@ -70,10 +70,12 @@ ALR_DEV void read_label(const E* row, const float* val, const int32_t* tok, cons
     tm = fmaxf(tm, x[k]);
   }
   tm = warp_max(tm);
-  const float x0 = rest != nullptr ? *rest : kNegInf, m = fmaxf(tm * a.inv_t, x0);
-  const bool has = m > kNegInf;
-  const float step = tm > kNegInf ? tm * a.inv_t - m : 0.f;   // 0 unless the bin leads
-  const float d0 = x0 - m, e0 = d0 > kNegInf ? expf(d0) : 0.f;
+  // The larger of the list's first and the bin leads; m may leave a float's range (the type's lowest value
+  // by T < 1) though the list has its softmax, so not m but its parts say whether there is a label.
+  const float x0 = rest != nullptr ? *rest : kNegInf, tl = tm * a.inv_t, m = fmaxf(tl, x0);
+  const bool has = tm > kNegInf || x0 > kNegInf;
+  const float step = x0 > tl ? tl - x0 : 0.f;   // 0 unless the bin leads
+  const float d0 = x0 - m, e0 = d0 > kNegInf ? expf(d0) : 0.f;   // (-inf - -inf: no bin)
   float sum = 0.f;
 #pragma unroll
   for (int k = 0; k < kMost; ++k) {

@@ -202,3 +202,29 @@ def test_distill_at_tiny_temperatures(dtype, T):
     assert (np.abs(P.np64(out["loss_row"]) - want) <= 16 * EPS * want + 1e-3).all() and (want > 1).all()
     # a probability is that of one of n equal tokens, or 0
     assert (np.abs(P.np64(G) - ref["G"]) <= 2.0 ** -8 * np.abs(ref["G"])).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [0.5, 1.0, 2.0])
+def test_distill_rows_of_the_lowest_value(dtype, T):
+    """Every token of student and teacher masked to the type's lowest value: all equal, so the label is even
+    over its entries and q over the vocabulary, also where the logits / T leave fp32's range."""
+    N, V, K, low = 3, 5003, 8, torch.finfo(dtype).min
+    Z = _rows(torch.full((N, V), low), dtype)
+    val = torch.full((N, K), low, device="cuda")
+    idx = torch.arange(K, dtype=torch.int32, device="cuda").expand(N, K).contiguous()
+    rest = torch.full((N,), low, device="cuda") / T          # T = 0.5: -inf, no bin
+    out, G = _distill_out(N), Z.clone()
+    alr.alr_distill_fwd_bwd(Z, val, idx, out, G, rest=rest, temperature=T)
+    p0 = 0.0 if T < 1 else 1 / (K + 1)
+    p = (1 - p0) / K
+    loss = np.log(V) - (p0 * np.log(V - K) if p0 else 0.0)
+    assert np.allclose(P.np64(out["loss_row"]), loss, rtol=0, atol=LSE_TOL)
+    assert np.allclose(P.np64(out["ent_row"]), np.log(1 / p), rtol=0, atol=8 * EPS * 8)
+    assert torch.equal(out["lse"], rest)                     # log V is below its rounding
+    want = np.full((N, V), 1 / V)
+    want[:, :K] -= p
+    want[:, K:] -= p0 / (V - K)
+    want /= N * T
+    tol = (2.0 ** -8 if dtype == BF else 0) * np.abs(want) + 3 * LSE_TOL * (1 / V + p) / (N * T)
+    assert (np.abs(P.np64(G) - want) <= tol).all() and out["argmax"].eq(0).all()
