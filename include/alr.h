@@ -653,6 +653,9 @@ int alr_distill_fwd(const alr_distill_params* p, const void* Z, const float* top
  *             lambda w_r / (temperature sum w) * q_v (1 - p_0 / q_0)     otherwise.
  *   lse, lse_rest [N]: of the forward (lse_rest NULL when rest is NULL); weight_sum [1]: sum w of
  *   the batch (the forward's, or the sum over the shards of a row-sharded batch).
+ * q = exp(z / temperature - lse) is off by 2^-24 |lse| relative, the rounding of lse; where |lse| is
+ * 2^24 or more (or infinite) the row's gradient is 0, where |lse_rest| is, that of the tokens not
+ * listed.  alr_distill_fwd_bwd has neither limit.
  */
 int alr_distill_bwd(const alr_distill_params* p, const void* Z, const float* top_val,
                     const int32_t* top_idx, const float* rest, const float* weight,

@@ -213,6 +213,9 @@ struct RowSums {
 // exp(x / T - lse) = 2^((x - ref) k + log_scale) with ref a logit next to T lse: the products then are of
 // small numbers, and what ref leaves of lse is the scale.  (exp2(x k - lse log2 e) loses 2^-24 |lse| on the
 // way, up to half as much again as lse's own rounding costs.)
+// q is off by 2^-24 |lse| relative, the rounding of lse itself.  From kLseMost on that says nothing (an lse of
+// tokens masked by large finite numbers alone, a tiny T): the gradient is 0 there.
+constexpr float kLseMost = 16777216.f;
 struct FromLse {
   float ref, log_scale;
 };
@@ -472,7 +475,7 @@ __global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
           }
         } else if (lane == 0) {
           const float lse = o.lse[r], lse_rest = rest != nullptr ? o.lse_rest[r] : kNegInf;
-          const bool known = lse > kNegInf, rest_known = lse_rest > kNegInf;
+          const bool known = fabsf(lse) < kLseMost, rest_known = fabsf(lse_rest) < kLseMost;
           if (!known) c = 0.f;
           sums.c = c;
           const FromLse q = from_lse(known ? lse : 0.f, a.t, k);
@@ -483,7 +486,7 @@ __global__ void __launch_bounds__(kRowThreadsMost + 32, kPacks > 10 ? 1 : 2)
             sums.out_c = c * ex2(q.log_scale);
           } else {
             const FromLse o = from_lse(rest_known ? lse_rest : 0.f, a.t, k);
-            sums.out_ref = o.ref;
+            sums.out_ref = rest_known ? o.ref : -kNegInf;   // from there every exponential is 0
             sums.out_c = rest_known ? c * (expf(lse_rest - lse) - lab.p0) * ex2(o.log_scale) : 0.f;
           }
         }

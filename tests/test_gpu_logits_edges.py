@@ -228,3 +228,28 @@ def test_distill_rows_of_the_lowest_value(dtype, T):
     want /= N * T
     tol = (2.0 ** -8 if dtype == BF else 0) * np.abs(want) + 3 * LSE_TOL * (1 / V + p) / (N * T)
     assert (np.abs(P.np64(G) - want) <= tol).all() and out["argmax"].eq(0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("value", [-1e10, -1e30, None])
+@pytest.mark.parametrize("T", [0.7, 1.0, 1.3])
+def test_distill_gradient_alone_next_to_masks_of_large_numbers(dtype, value, T):
+    """Log-sum-exps of masked tokens alone, of a size at which a float says nothing about differences of
+    logits: the gradient from a forward's results is finite, 0 for the row or for the tokens that they are of."""
+    Z, val, idx, rest, big = _distil_masked(dtype, 5003, value, T)
+    _check_masked(Z, val, idx, rest, T, big)
+    N, V = Z.shape
+    Z[0] = Z.min()                                           # everything masked
+    out, two = _distill_out(N), Z.clone()
+    alr.alr_distill_fwd(Z, val, idx, out, rest=rest, temperature=T)
+    alr.alr_distill_bwd(Z, val, idx, out["lse"], out["lse_rest"], out["weight_sum"], two, rest=rest, temperature=T)
+    assert torch.isfinite(two).all() and not two[0].any() and two[1:].any(1).all()
+    # up to there exp(z / T - lse) is that of the numbers given: z - T lse is exact enough
+    z = torch.tensor([[2.0 ** 24 - 64, 0.0, -1.0]], device="cuda") * T
+    lse, ws = torch.full((1,), 2.0 ** 24 - 64, device="cuda"), torch.ones(1, device="cuda")
+    G, one = torch.empty_like(z), torch.zeros(1, 1, device="cuda")
+    idx = torch.tensor([[1]], dtype=torch.int32, device="cuda")
+    alr.alr_distill_bwd(z, one, idx, lse, None, ws, G, temperature=T)
+    t = float(np.float32(T))
+    q = np.exp(z[0, 0].item() / t - lse.item())
+    assert abs(G[0, 0].item() * t - q) <= 32 * EPS * q and G[0, 2] == 0 and abs(G[0, 1].item() * t + 1) <= 8 * EPS
