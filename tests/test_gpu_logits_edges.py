@@ -253,3 +253,15 @@ def test_distill_gradient_alone_next_to_masks_of_large_numbers(dtype, value, T):
     t = float(np.float32(T))
     q = np.exp(z[0, 0].item() / t - lse.item())
     assert abs(G[0, 0].item() * t - q) <= 32 * EPS * q and G[0, 2] == 0 and abs(G[0, 1].item() * t + 1) <= 8 * EPS
+
+
+@pytest.mark.parametrize("N,V", [(6, 2056), (330, 2056)])
+def test_rest_far_below_the_list(N, V):
+    """The tokens not listed are all 0, 2048 of them, the list 38 to 42 above: log 2048 within a step of fp32's
+    logarithm (2^-21 here), for both forms of a row: nothing is added to 0 and the sum is a whole number."""
+    z = torch.zeros(N, V)
+    z[:, 100:108] = 38 + 4 * torch.arange(N).float()[:, None] / N + 0.01 * torch.arange(8)
+    for dtype in (BF, F32):
+        out = dict(top_val=_new(N, 8), top_idx=_new(N, 8, dtype=torch.int32), lse=_new(N), lse_rest=_new(N))
+        alr.alr_top_logits(_rows(z, dtype), 8, out)
+        assert (np.abs(P.np64(out["lse_rest"]) - np.log(2048)) <= 2.0 ** -21).all()
