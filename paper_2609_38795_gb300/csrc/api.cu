@@ -1500,8 +1500,8 @@ int alr_top_logits(const void* Z, int32_t dtype, int64_t N, int32_t V, int64_t l
   DevInfo info;
   if ((rc = require_sm103(&info)) != ALR_OK) return rc;
   const cudaError_t e = alr::launch_top_logits(dtype == ALR_BF16 ? 0 : 1, Z, N, V, ldz, K,
-                                               1.f / temperature, top_val, top_idx, lse, lse_rest, info.sms,
-                                               static_cast<cudaStream_t>(stream));
+                                               temperature, top_val, top_idx, lse, lse_rest,
+                                               info.sms, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? ALR_OK : cuda_fail(e, "top logits launch");
 }
 

@@ -250,7 +250,7 @@ cudaError_t launch_distill(const DistillArgs& a, bool fwd, bool grad, const void
 // Top logits and sampling (sample_kernels.cu).
 constexpr int kTopMost = 256;        // ALR_TOP_MAX
 cudaError_t launch_top_logits(int dtype, const void* Z, long long N, int V, long long ldz, int K,
-                              float inv_t, float* top_val, int32_t* top_idx, float* lse,
+                              float t, float* top_val, int32_t* top_idx, float* lse,
                               float* lse_rest, int sms, cudaStream_t s);
 struct SampleArgs {
   const uint32_t* u;

@@ -997,7 +997,7 @@ __device__ __noinline__ Cut exact_top_k(R row, int K) {
 }
 
 template <typename R>
-ALR_DEV void top_logits_row(R& row, int K, float inv_t, const TopOut& out, long long r) {
+ALR_DEV void top_logits_row(R& row, int K, float t, const TopOut& out, long long r) {
   using E = typename R::E;
   Shared& sh = row.sh;
   const Bound bound = bound_and_collect(row, K);
@@ -1022,7 +1022,7 @@ ALR_DEV void top_logits_row(R& row, int K, float inv_t, const TopOut& out, long 
   }
   others_know(row);   // the records below go over the cluster
   // The others' sums, each warp's from its own largest; the candidates are the first block's.
-  const float k = inv_t * kLog2e, least = cut.last >= 0 ? key_value(cut.key) : bound.least;
+  const float k = 1.f / t * kLog2e, least = cut.last >= 0 ? key_value(cut.key) : bound.least;
   const auto without = [&](uint4 p, int id) {
     if (largest<E>(p) >= least) {
       uint32_t bits = 0;
@@ -1110,31 +1110,31 @@ ALR_DEV void top_logits_row(R& row, int K, float inv_t, const TopOut& out, long 
     if (tid == 0) {
       const bool any = mo > kNegInf;
       if (any) sl += so * ex2((mo - bound.top) * k);
-      if (out.lse != nullptr) out.lse[r] = n > 0 ? bound.top * inv_t + logf(sl) : kNegInf;
-      if (out.lse_rest != nullptr) out.lse_rest[r] = any ? mo * inv_t + logf(so) : kNegInf;
+      if (out.lse != nullptr) out.lse[r] = n > 0 ? bound.top / t + logf(sl) : kNegInf;
+      if (out.lse_rest != nullptr) out.lse_rest[r] = any ? mo / t + logf(so) : kNegInf;
     }
   }
 }
 
 template <typename E, int kPacks>
 __global__ void __launch_bounds__(kRowThreadsMost, kPacks > 10 ? 1 : 2)
-    top_logits_kernel(const E* Z, long long ldz, int V, int K, float inv_t, TopOut out, int cluster) {
+    top_logits_kernel(const E* Z, long long ldz, int V, int K, float t, TopOut out, int cluster) {
   __shared__ Shared sh;
   pdl_wait_and_release();
   const long long r = cluster_id_x();
   Row<E, kPacks> row(Z + r * ldz, r * ldz, V, cluster, sh);
-  top_logits_row(row, K, inv_t, out, r);
+  top_logits_row(row, K, t, out, r);
 }
 
 template <typename E>
 __global__ void __launch_bounds__(kStreamThreads, 2)
-    top_logits_stream_kernel(const E* Z, long long N, long long ldz, int V, int K, float inv_t,
+    top_logits_stream_kernel(const E* Z, long long N, long long ldz, int V, int K, float t,
                              TopOut out) {
   __shared__ Shared sh;
   pdl_wait_and_release();
   for (long long r = blockIdx.x; r < N; r += gridDim.x) {
     StreamRow<E> row(Z + r * ldz, r * ldz, V, sh);
-    top_logits_row(row, K, inv_t, out, r);
+    top_logits_row(row, K, t, out, r);
   }
 }
 
@@ -1528,18 +1528,18 @@ bool stream_rows(long long N, int V, int sms) { return N >= sms && V >= 2048; }
 }  // namespace
 
 cudaError_t launch_top_logits(int dtype, const void* Z, long long N, int V, long long ldz, int K,
-                              float inv_t, float* top_val, int32_t* top_idx, float* lse,
+                              float t, float* top_val, int32_t* top_idx, float* lse,
                               float* lse_rest, int sms, cudaStream_t s) {
   const TopOut out{top_val, top_idx, lse, lse_rest};
   const auto run = [&](auto* z) {
     using E = std::remove_cv_t<std::remove_pointer_t<decltype(z)>>;
     if (stream_rows(N, V, sms))
       return launch_pdl(top_logits_stream_kernel<E>, dim3(unsigned(std::min<long long>(N, 1 << 20))),
-                        dim3(kStreamThreads), 0, s, z, N, ldz, V, K, inv_t, out);
+                        dim3(kStreamThreads), 0, s, z, N, ldz, V, K, t, out);
     const RowShape shape = row_shape(N, V, int(sizeof(E)), sms, 256);
     return with_packs(shape.packs, [&](auto packs) {
       return launch_row_each(shape, N, top_logits_kernel<E, decltype(packs)::value>, s, z, ldz, V, K,
-                             inv_t, out, shape.cluster);
+                             t, out, shape.cluster);
     });
   };
   return dtype == 0 ? run(static_cast<const __nv_bfloat16*>(Z)) : run(static_cast<const float*>(Z));

@@ -265,3 +265,18 @@ def test_rest_far_below_the_list(N, V):
         out = dict(top_val=_new(N, 8), top_idx=_new(N, 8, dtype=torch.int32), lse=_new(N), lse_rest=_new(N))
         alr.alr_top_logits(_rows(z, dtype), 8, out)
         assert (np.abs(P.np64(out["lse_rest"]) - np.log(2048)) <= 2.0 ** -21).all()
+
+
+@pytest.mark.parametrize("N", [40, 330])
+def test_log_sum_exp_of_one_token_is_its_quotient(N):
+    """lse = z / T where a token has all the mass, rounded once; the same for the rest."""
+    V, T = 2100, 0.7
+    g = torch.Generator().manual_seed(91)
+    z = torch.full((N, V), float("-inf"))
+    z[:, 9], z[:, 2001] = 300 + 100 * torch.rand(N, generator=g), 100 * torch.rand(N, generator=g)
+    out = dict(top_val=_new(N, 1), top_idx=_new(N, 1, dtype=torch.int32), lse=_new(N), lse_rest=_new(N))
+    alr.alr_top_logits(_rows(z, F32), 1, out, temperature=T)
+    t = float(np.float32(T))
+    for key, col in (("lse", 9), ("lse_rest", 2001)):
+        want = z[:, col].double().numpy() / t
+        assert (np.abs(P.np64(out[key]) - want) <= EPS * np.abs(want)).all(), key
