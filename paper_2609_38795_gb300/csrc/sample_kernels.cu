@@ -836,62 +836,65 @@ ALR_DEV void collect(R& row, float least, float most, F take) {
   row.sync();
 }
 
-// row_bound and collect in one reading of the row by one block, for up to kStreamFew tokens: the K-th
-// largest of the threads' largest logits, once the first packs are there (and again after the next ones),
-// is a bound that every later pack is held against as it comes by.
-constexpr int kStreamFew = 200;
-
+// row_bound and collect in one reading of the row by one block: the K-th largest of the threads' largest
+// logits, once the first packs are there (and again after the next ones), is a bound that every later pack is
+// held against as it comes by.  768 x 151936 rows, us, in one reading and as row_bound and collect: top 64
+// 167 and 182, top 256 236 and 296, tokens of a top-k of 64 85 and 155, of 256 146 and 197.
 template <typename R>
 ALR_DEV Bound bound_and_collect(R& row, int K) {
   if constexpr (std::is_base_of_v<RowCommon<true>, R>) {
     using E = typename R::E;
-    if (K <= kStreamFew) {
-      Shared& sh = row.sh;
-      constexpr int kBatch = R::kBatch;
-      row.ready();
-      if (threadIdx.x == 0) sh.n_more = 0;
-      for (int i = threadIdx.x; i < row.records(); i += blockDim.x) sh.count[i] = 0;
-      __syncthreads();
-      float most = kNegInf, least = kNegInf;
-      for (int b = 0; b < row.batches; ++b) {
-        uint4 raw[kBatch];
-        row.load(raw, b * kBatch);
-        float top[kBatch];
+    static_assert(kTopMost <= kStreamThreads, "a thread's largest for each of the K");
+    Shared& sh = row.sh;
+    constexpr int kBatch = R::kBatch;
+    row.ready();
+    if (threadIdx.x == 0) sh.n_more = 0;
+    for (int i = threadIdx.x; i < row.records(); i += blockDim.x) sh.count[i] = 0;
+    __syncthreads();
+    float most = kNegInf, least = kNegInf;
+    for (int b = 0; b < row.batches; ++b) {
+      uint4 raw[kBatch];
+      row.load(raw, b * kBatch);
+      float top[kBatch];
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-          top[j] = largest<E>(raw[j]);
-          most = fmaxf(most, top[j]);
-        }
-        if (b < 2 || K > 64 || least == kNegInf) {   // bit by bit of the upper half of the keys
-          const uint32_t key = most > kNegInf ? order_key(most) >> 16 : 0u;
-          uint32_t bound = 0;
-          for (uint32_t bit = 0x8000u; bit != 0; bit >>= 1)
-            if (__syncthreads_count(key >= (bound | bit)) >= K) bound |= bit;
-          if (bound != 0) least = key_value(bound << 16);
-        }
+      for (int j = 0; j < kBatch; ++j) {
+        top[j] = largest<E>(raw[j]);
+        most = fmaxf(most, top[j]);
+      }
+      // Bit by bit of the upper half of the keys.  For few tokens the bound rises little after two batches (top
+      // 8: 109 us, 114 with a bound in every batch; top 64 167 and 150, a token of its top-k 85 and 92), for many it
+      // does (top 96: 170, 193 without).  Rows that rise from end to end overflow it and take the radix select:
+      // 903 us for the top 64 of 768, 699 for tokens of a top-k.
+      if (b < 2 || K > 64 || least == kNegInf) {
+        const uint32_t key = most > kNegInf ? order_key(most) >> 16 : 0u;
+        uint32_t bound = 0;
+        for (uint32_t bit = 0x8000u; bit != 0; bit >>= 1)
+          if (__syncthreads_count(key >= (bound | bit)) >= K) bound |= bit;
+        if (bound != 0) least = key_value(bound << 16);
+      }
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-          if (!(top[j] >= least) || !(top[j] > kNegInf)) continue;
-          uint32_t bits = 0;
+      for (int j = 0; j < kBatch; ++j) {
+        if (!(top[j] >= least) || !(top[j] > kNegInf)) continue;
+        uint32_t bits = 0;
 #pragma unroll
-          for (int e = 0; e < kPerPack<E>; ++e)
-            bits |= uint32_t(pack_elem<E>(raw[j], e) >= least && pack_elem<E>(raw[j], e) > kNegInf) << e;
-          int at = row.records() * kSlots + atomicAdd(&sh.n_more, __popc(bits));
-          for (; bits != 0; bits &= bits - 1, ++at) {
-            const int e = __ffs(bits) - 1;
-            if (at < kCandMost)
-              sh.cand[at] = entry(order_key(pack_elem_at<E>(raw[j], e)), row.elem(b, j) + e);
-          }
+        for (int e = 0; e < kPerPack<E>; ++e)
+          bits |= uint32_t(pack_elem<E>(raw[j], e) >= least && pack_elem<E>(raw[j], e) > kNegInf) << e;
+        int at = row.records() * kSlots + atomicAdd(&sh.n_more, __popc(bits));
+        for (; bits != 0; bits &= bits - 1, ++at) {
+          const int e = __ffs(bits) - 1;
+          if (at < kCandMost)
+            sh.cand[at] = entry(order_key(pack_elem_at<E>(raw[j], e)), row.elem(b, j) + e);
         }
       }
-      row.most = most;
-      const float top = block_reduce(most, MaxOp(), sh.fbuf);   // and all candidates are there
-      return {least, top};
     }
+    row.most = most;
+    const float top = block_reduce(most, MaxOp(), sh.fbuf);   // and all candidates are there
+    return {least, top};
+  } else {
+    const Bound b = row_bound(row, K);
+    if (b.top > kNegInf) collect(row, b.least, -kNegInf, [](float, int) { return true; });
+    return b;
   }
-  const Bound b = row_bound(row, K);
-  if (K > 0 && b.top > kNegInf) collect(row, b.least, -kNegInf, [](float, int) { return true; });
-  return b;
 }
 
 // Whether all candidates fit, known to all blocks.  The others then wait in the cluster barrier until all
@@ -1522,7 +1525,10 @@ __global__ void __launch_bounds__(kStreamThreads, 2)
 }
 
 // One block reads a row by itself where there are rows for every SM and a row has a pack for each second
-// thread at least (see the top of the file for both sides).
+// thread at least.  Streamed and in clusters, us, for [tokens of top-k and top-p; a nucleus; top 64]: 152 rows of
+// 151936 bf16 [20, 66, 40] and [103, 115, 70], 768 [82, 250, 168] and [164, 438, 285]; 152 of 32000 fp32 [12, 35,
+// 16] and [28, 41, 27]; 152 of 8192 bf16 [10, 30, 13] and [14, 25, 19]; 152 of 2048 bf16 [9, 30, 16] and [40, 21,
+// 34].  A nucleus of rows up to 8192 is the cluster's (768 of 2048: 89 and 45), but the settings are on the device.
 bool stream_rows(long long N, int V, int sms) { return N >= sms && V >= 2048; }
 
 }  // namespace
