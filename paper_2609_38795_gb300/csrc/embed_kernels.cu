@@ -244,7 +244,6 @@ __global__ void __launch_bounds__(kSortThreads)
   uint32_t *src_t = nullptr, *src_r = nullptr, *dst_t = tok0, *dst_r = row0;
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * bits;
-    // keys (and rows) of kSortBatch steps, all loads in flight; ~0 past the end
     const uint32_t* keys = pass > 0 ? src_t : reinterpret_cast<const uint32_t*>(tokens);
     // keys (and rows) of kSortBatch steps, all loads in flight; ~0 past the end
     auto load = [&](int s0, uint32_t (&key)[kSortBatch], uint32_t (&row)[kSortBatch], bool rows) {
@@ -301,12 +300,7 @@ __global__ void __launch_bounds__(kSortThreads)
         total += n;
       }
     }
-    uint32_t incl = total;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const uint32_t t = __shfl_up_sync(0xffffffffu, incl, off);
-      if (lane >= off) incl += t;
-    }
+    uint32_t incl = warp_scan(total);
     if (lane == 31) scan[warp] = incl;
     __syncthreads();
     for (int w = 0; w < warp; ++w) incl += scan[w];

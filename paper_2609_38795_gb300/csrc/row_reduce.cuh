@@ -17,10 +17,6 @@ struct MaxOp {
   template <typename T>
   ALR_DEV T operator()(T a, T b) const { return a > b ? a : b; }
 };
-struct MinOp {
-  template <typename T>
-  ALR_DEV T operator()(T a, T b) const { return a < b ? a : b; }
-};
 struct AddOp {
   template <typename T>
   ALR_DEV T operator()(T a, T b) const { return a + b; }
@@ -30,6 +26,18 @@ template <typename T, typename Op>
 ALR_DEV T warp_reduce(T v, Op op) {
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, off));
+  return v;
+}
+
+// Sum of the lanes up to and with this one.
+template <typename T>
+ALR_DEV T warp_scan(T v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const T t = __shfl_up_sync(0xffffffffu, v, off);
+    if (lane >= off) v += t;
+  }
   return v;
 }
 

@@ -68,12 +68,10 @@ struct Shared {
   int count[kWarpsMost + 1];              // first block: in each warp's places; then their offsets
   uint32_t small[256];                    // histogram of the list's keys
   unsigned long long rec[kWarpsMost];     // of each warp of the cluster (or batch of a streamed row): a sum
-  unsigned long long rec2[kWarpsMost];
   unsigned long long grid[8 * kStreamThreads / 32];   // of a batch's packs and warps
   float2 frec[kWarpsMost];
   float fbuf[32];
   unsigned long long lbuf[32];
-  int ibuf[32];
   int n_more;                             // first block: candidates past the warps' places
   uint32_t digit, reach;
   unsigned long long above, found, kept;
@@ -414,12 +412,7 @@ ALR_DEV Found find_unit(Row<E, kPacks>& row, float least, F f, N nth) {
   if (before < n && n <= before + s)   // this warp holds it
     row.each_until([&](const uint4& p, int id) {
       const unsigned long long mine = sum_of_pack<E>(f, p, id, least);
-      unsigned long long incl = mine;
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
-        if (row.lane >= off) incl += t;
-      }
+      unsigned long long incl = warp_scan(mine);
       const unsigned long long all = __shfl_sync(0xffffffffu, incl, 31);
       if (n > before + all) {
         before += all;
@@ -526,12 +519,7 @@ ALR_DEV Found find_unit(StreamRow<E>& row, float least, F f, N nth) {
     const int j = at / kWarps;
     const uint4 p = row.load_one(b * kBatch + j);
     const unsigned long long mine = of_pack(p, row.elem(b, j));
-    unsigned long long incl = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
-      if (row.lane >= off) incl += t;
-    }
+    unsigned long long incl = warp_scan(mine);
     unsigned long long run = before + incl - mine;
     if (run < n && n <= run + mine)
       for (int e = 0; e < kPerPack<E>; ++e) {
@@ -594,12 +582,7 @@ ALR_DEV Selected select_key(R& row, const Cut& cut, W weight, Need need) {
       const int b = bins - 1 - (tid * n + j);
       if (b >= 0) mine += sh.many.total[b];
     }
-    unsigned long long incl = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
-      if (row.lane >= off) incl += t;
-    }
+    unsigned long long incl = warp_scan(mine);
     if (row.lane == 31) sh.lbuf[row.warp] = incl;
     __syncthreads();
     unsigned long long run = above + incl - mine, all = 0;
@@ -742,12 +725,7 @@ ALR_DEV Bound row_bound(R& row, int K) {
     if (row.warp == 0) {   // lane l: the bins 255 - 8 l and the seven below
       uint32_t mine = 0;
       for (int j = 0; j < 8; ++j) mine += sh.small[255 - 8 * row.lane - j];
-      uint32_t incl = mine;
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const uint32_t o = __shfl_up_sync(0xffffffffu, incl, off);
-        if (row.lane >= off) incl += o;
-      }
+      uint32_t incl = warp_scan(mine);
       if (row.lane == 31) sh.digit = incl >= reach ? 0u : 0xffffffffu;   // too few
       __syncwarp();
       uint32_t run = incl - mine;
@@ -807,12 +785,7 @@ ALR_DEV void collect(R& row, float least, float most, F take) {
       if (mine == 1) second = e;
       ++mine;
     });
-    int at = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, at, off);
-      if (row.lane >= off) at += o;
-    }
+    int at = warp_scan(mine);
     total = __shfl_sync(0xffffffffu, at, 31);
     at -= mine;
     int more = 0;
@@ -929,12 +902,7 @@ ALR_DEV int sort_candidates(R& row) {
       c[j] = row.lane * 4 + j < n_rec ? sh.count[row.lane * 4 + j] : 0;
       mine += c[j];
     }
-    int at = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, at, off);
-      if (row.lane >= off) at += o;
-    }
+    int at = warp_scan(mine);
     if (row.lane == 31) sh.kept_n = at;
     at -= mine;
 #pragma unroll
@@ -1184,12 +1152,7 @@ ALR_DEV void draw_from_candidates(Shared& sh, int n, const Weight& weight, float
       own[j] = lane * kOwn + j < n ? w[lane * kOwn + j] : 0ull;
       mine += own[j];
     }
-    unsigned long long incl = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
-      if (lane >= off) incl += t;
-    }
+    unsigned long long incl = warp_scan(mine);
     const unsigned long long sum = __shfl_sync(0xffffffffu, incl, 31);
     // the sum before a token, a whole number, is below top_p sum: below that number rounded up
     const unsigned long long lim =
@@ -1302,12 +1265,7 @@ ALR_DEV Cut cut_by_steps(R& row, const Cut& cut, const Steps& bin, float least, 
     total_bins(row, kBins);
     unsigned long long mine = 0;
     for (int j = tid * n; j < min(kBins, (tid + 1) * n); ++j) mine += sh.many.total[j];
-    unsigned long long incl = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const unsigned long long t = __shfl_up_sync(0xffffffffu, incl, off);
-      if (row.lane >= off) incl += t;
-    }
+    unsigned long long incl = warp_scan(mine);
     if (row.lane == 31) sh.lbuf[row.warp] = incl;
     __syncthreads();
     run = incl - mine;
@@ -1354,12 +1312,7 @@ ALR_DEV Cut cut_by_steps(R& row, const Cut& cut, const Steps& bin, float least, 
     unsigned long long own = 0;
     for (int i = tid * m; i < min(got, (tid + 1) * m); ++i)
       own += worth(key_value(entry_key(sh.few.all[i])));
-    unsigned long long in = own;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const unsigned long long t = __shfl_up_sync(0xffffffffu, in, off);
-      if (row.lane >= off) in += t;
-    }
+    unsigned long long in = warp_scan(own);
     if (row.lane == 31) sh.lbuf[row.warp] = in;
     __syncthreads();
     unsigned long long at = above + in - own;
