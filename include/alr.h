@@ -574,8 +574,8 @@ int alr_gemm_form(int32_t dtype, int32_t M, int32_t Nc, int32_t K, int32_t* form
 /* ---------------------------------------------------------------------------------------
  * Operators on logits in hand, and the embedding of a block's tokens: what surrounds the slot
  * loss in a training program.  The paper's trainer has them from its framework: the target's
- * rollout draws tokens and stores labels (App. A), the drafter embeds a block's anchor and mask
- * tokens.
+ * rollout takes its tokens (greedily in the paper, App. A, which is temperature 0 here; drawn tokens
+ * are for other rollouts) and stores labels, the drafter embeds a block's anchor and mask tokens.
  *   alr_embed -> (model) -> logits -> alr_sample_tokens / alr_top_logits
  *             -> alr_distill_fwd_bwd -> (model's backward) -> alr_embed_grad
  *
@@ -683,9 +683,10 @@ int alr_distill_fwd_bwd(const alr_distill_params* p, const void* Z, const float*
  *            kept mass lies (one at least); >= 1 keeps all.
  *   min_p [N] float or NULL: then the tokens of at least min_p (at most 1) times the largest
  *            probability.  (A top_p or min_p of NaN cuts nothing.)
- * A token's weight is the whole number floor(2^31 exp2((z - max) log2(e) / temperature)), each step
- * rounded to fp32; tokens of weight 0 (below 2^-31 of the largest) are never kept.  Sums of weights
- * are exact, so a draw depends on nothing but its inputs.  With S the weight of the kept tokens:
+ * A token's weight is the whole number floor(2^31 exp2((z - max) c)) with c = log2(e) / temperature,
+ * quotient, difference, product and exponential each rounded to fp32; tokens of weight 0 (below
+ * 2^-31 of the largest) are never kept.  Sums of weights are exact, so a draw depends on nothing but
+ * its inputs.  With S the weight of the kept tokens:
  *   token [N] int32: the lowest id at which the running sum of the kept weights, in the order of
  *            ids, exceeds floor(u S / 2^32); -1 for a row without a candidate;
  *   prob [N] float (nullable): the token's weight / S (0 for token -1);

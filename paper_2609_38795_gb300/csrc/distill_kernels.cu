@@ -14,13 +14,13 @@
 // A row is read once, into the registers of a cluster (row_cluster.cuh), its sums are exchanged between all
 // warps once, and the gradient is formed from the same registers.  Clusters stay and take rows in turn: while
 // a row is worked on, the next one comes into shared memory, fetched by a warp of its own that reads its
-// label too.  (One row a cluster, loads straight into registers: all blocks load, compute and store in
-// step and memory idles while they compute, 250 us instead of 215 for 2048 x 151936 bf16 logits with 40 %
-// of the rows masked.)  4.6 TB/s then, 0.68 of the copy rate; the gradient alone, whose blocks wait for
-// nobody, 4.55 TB/s on rows of two alignments (2000 x 60001).  What is left is the blocks' waits for one
-// another's sums (a third of a row's 17 K cycles).  Tried and slower: the sums of the next row taken before
-// the last one's gradient, so that nobody waits (280 us with both rows in registers and one block to an SM,
-// 293 with rows over 8 blocks), the next row brought into L2 only (no change).
+// label too.  2048 x 151936 bf16 logits with 40 % of the rows masked: 228 us, 4.4 TB/s, 0.64 of the copy rate;
+// the gradient alone, whose blocks wait for nobody, 4.45 TB/s on rows of two alignments (2000 x 60001).  What is
+// left is the blocks' waits for one another's sums (a third of a row's 17 K cycles).  Tried and slower, against
+// 215 us when exponentials were of one fma (see exp2_from): one row a cluster, loads straight into registers
+// (250: all blocks load, compute and store in step, and memory idles while they compute); the sums of the next
+// row taken before the last one's gradient, so that nobody waits (280 with both rows in registers and one block
+// to an SM, 293 with rows over 8 blocks); the next row brought into L2 only (no change).
 #include "kernels.h"
 #include "launch.h"
 #include "row_cluster.cuh"
@@ -126,7 +126,8 @@ ALR_DEV uint32_t pack_bf16(float lo, float hi) {
 
 // exp2((x - ref) k) of two elements.  The difference first: one fma, x k - ref k, would carry the rounding of
 // ref k, which for logits / T past 2^30 (a mask by a large finite number over a whole stretch of the row, a
-// tiny T) is out of the exponential's range, and of a float's for the type's lowest value: NaN.
+// tiny T) is out of the exponential's range, and of a float's for the type's lowest value: NaN.  (It was 223 us
+// instead of 229 for loss and gradient of the rows above, nothing for either alone.)
 ALR_DEV uint64_t exp2_from(uint64_t x, uint64_t ref, uint64_t k) {
   return f2_ex2(f2_mul(f2_sub(x, ref), k));
 }

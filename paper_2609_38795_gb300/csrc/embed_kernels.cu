@@ -194,8 +194,8 @@ struct GradPlan {
   size_t tok_off[2], row_off[2], list_off, count_off, present_off, part_off, total;
 };
 
-// Rows of a chunk: enough chunks to fill the device, few partial sums for a token in every row (32768
-// rows: 101 us at 64, 110 at 32).
+// Rows of a chunk: enough chunks to fill the device, few partial sums for a token in every row (4000 rows:
+// 61.6 us at 16, 61.1 at 32; 12000: 74 at 32, 79 at 16; 32768: 102 at 64, 110 at 32; 100000: 202 at 128, 207 at 64).
 GradPlan grad_plan(int V, int d, int N) {
   GradPlan g{};
   g.chunk = N <= 8192 ? 16 : N <= 16384 ? 32 : N <= 65536 ? 64 : 128;
@@ -431,7 +431,8 @@ __global__ void __launch_bounds__(kChunkThreads)
 // --- long runs: partial sums of the chunks, in order.  A warp takes 128 columns of a run; of a run
 // of many chunks the block's warps take an equal share each, joined in order through shared memory.
 // The items (run, 128 columns) go to the blocks in turn, so that the columns of one run of many
-// chunks are different blocks' (eight to a block: 145 us for one of 480 chunks, 2048 columns).
+// chunks are different blocks' (in an earlier form, eight to a
+// block, the join took 145 us for one run of 480 chunks, 2048 columns).
 constexpr int kJoinThreads = 1024;
 constexpr int kJoinWarps = kJoinThreads / 32;
 constexpr int kJoinFew = 16;   // partial sums that one warp adds

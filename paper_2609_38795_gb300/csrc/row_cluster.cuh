@@ -32,8 +32,8 @@ constexpr int kRowPackChoices[] = {2, 5, 10, 18};
 // Few rows: as many blocks as give every SM one, and few packs a thread (the row's latency is what
 // counts).  Many rows: the fewest blocks that hold the row at 10 packs a thread, two or more of which share
 // an SM, so that one's transfers overlap the other's arithmetic (loss and gradient of 2048 x 151936 bf16 logits,
-// 40 % of the rows masked: 214 us in clusters of 4; 297 in clusters of 8 half as large, 241 in clusters of 2
-// twice as large, one block to an SM).  18 packs a thread are for fp32 rows of more than 150 K tokens,
+// 40 % of the rows masked, in an earlier form of the kernel: 214 us in clusters of 4; 297 in clusters of 8 half
+// as large, 241 in clusters of 2 twice as large, one block to an SM).  18 packs a thread are for fp32 rows of more than 150 K tokens,
 // which 8 blocks hold no other way.
 // `least`: threads that a block should have if the row is long enough.
 inline RowShape row_shape(long long N, int V, int elem_bytes, int sms, int least = 64) {

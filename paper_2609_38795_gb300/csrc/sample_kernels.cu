@@ -6,7 +6,7 @@
 // Rows.  Few rows: each in the registers of a cluster, read once (row_cluster.cuh, `Row`): the row's latency is
 // what counts.  From a row per SM on: each read by one block (`StreamRow`), two blocks to an SM, no cluster
 // barriers, and one block reads while the other selects; what needs a second sweep finds the row in L2.
-// 768 x 151936 bf16 rows, top-k and top-p: 80 us streamed (2.9 TB/s), 154 us in clusters.
+// 768 x 151936 bf16 rows, top-k and top-p: 78 us streamed (3.0 TB/s), 164 us in clusters.
 //
 // Few tokens of many (top logits, top-k): the K-th largest of the largest logits that the threads hold is a
 // lower bound of the row's K-th largest, and not many more than K logits reach it.  Those are sorted by the
@@ -16,8 +16,8 @@
 // of the logit below the largest, in each block's shared memory and added up over the cluster, tells the
 // step in which the cut falls; that step's logits are sorted as above.  A returning shared-memory atomic
 // for each logit is what that costs (some 150 K cycles for 2 x 152 K logits on an SM), so only the logits of
-// the upper 16 octaves have one at first.  A nucleus of trained rows: 249 us for 768 x 151936, of a random
-// head's, whose bulk it takes in, 746 us.
+// the upper 16 octaves have one at first.  A nucleus of trained rows: 244 us for 768 x 151936, of a random
+// head's, whose bulk it takes in, 738 us.
 // So many equal logits that they do not fit: a radix select over an order-preserving key.
 //
 // Bound by latency and instructions, not by memory: see the figures at the steps.  Sweeps over weights are
@@ -1115,7 +1115,7 @@ __global__ void __launch_bounds__(kStreamThreads, 2)
 // the split of a row over threads can change a draw.
 struct Weight {
   float m, c;
-  // exp2f and ex2.approx agree where the weight is not 0 (every float of [-64, 0] was compared)
+  // exp2f and ex2.approx agree where the weight is not 0 (all 1.1e9 floats of [-64, 0] were compared)
   ALR_DEV float real(float x) const { return ex2(__fmul_rn(__fsub_rn(x, m), c)); }
   // Logits below have a real weight under w (and above: not certainly over it); with a margin for the
   // rounding of the three steps.
@@ -1207,8 +1207,9 @@ struct Steps {
 // need() still asks for before them (one at least); `cut` itself when need() is content with all of them.
 // worth: 0 .. 2^31 for x, 0 where the weight is 0, as it is below `least`.
 // The histogram is of the logits that reach `near` first: a trained model's nucleus ends among those few,
-// and a place in a histogram is what costs most here.  Where it goes on, all logits have one.  (768 trained
-// rows at temperatures to 1.3, settings of their own: 209 us with 16 octaves first, 434 with all 32.)
+// and a place in a histogram is what costs most here.  Where it goes on, all logits have one.  A nucleus of 768 x
+// 151936 trained rows, us, with 16 octaves first and all 32 at once: 245 and 240 at a temperature of 0.8, 265 and
+// 438 at 1, 266 and 560 at 1.3, 752 and 627 at 1.6, where it takes in the bulk; of a random head 740 and 696.
 template <typename R, typename W, typename Need>
 ALR_DEV Cut cut_by_steps(R& row, const Cut& cut, const Steps& bin, float least, float near, W worth,
                          Need need) {
