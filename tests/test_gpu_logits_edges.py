@@ -280,3 +280,34 @@ def test_log_sum_exp_of_one_token_is_its_quotient(N):
     for key, col in (("lse", 9), ("lse_rest", 2001)):
         want = z[:, col].double().numpy() / t
         assert (np.abs(P.np64(out[key]) - want) <= EPS * np.abs(want)).all(), key
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("N,V", [(12, 9001), (330, 2500)])
+def test_sampling_and_top_logits_under_masks_by_large_numbers(dtype, N, V):
+    """Masks by finite numbers down to the type's lowest value, whole rows of it, few tokens left; temperatures
+    from 1e-30 to infinity."""
+    low = torch.finfo(dtype).min
+    z = _logits(N, V, 101)
+    z[1::6, V // 3:] = low
+    z[2::6, 30:] = -1e10
+    z[3::6] = low
+    z[4::6] = z[4::6].masked_fill(torch.rand(z[4::6].shape, generator=torch.Generator().manual_seed(1)) < 0.99, low)
+    z[5::6] += 1e30
+    z[5::6, : V // 2] = -1e30
+    Z = _rows(z, dtype, V + 1)
+    f = lambda x: torch.full((N,), x, device="cuda")  # noqa: E731
+    i = lambda x: torch.full((N,), x, dtype=torch.int32, device="cuda")  # noqa: E731
+    for T in (1e-30, 0.6, 1.0, 40.0, 1e30, float("inf")):
+        for kw in (dict(top_p=f(0.9)), dict(top_k=i(60), top_p=f(0.95)), dict(top_k=i(500)), dict(min_p=f(0.05)), {}):
+            _check_sample(Z, _draws(N, 8), f(T), **kw)
+    for K in (1, 8, 64, 256):
+        for T in (0.6, 1.0, 3.0):
+            out = dict(top_val=_new(N, K), top_idx=_new(N, K, dtype=torch.int32), lse=_new(N), lse_rest=_new(N))
+            alr.alr_top_logits(Z, K, out, temperature=T)
+            ref = lo.top_logits(Z.float().cpu().numpy(), K, T)
+            assert np.array_equal(P.npi(out["top_idx"]), ref["top_idx"])
+            assert np.array_equal(P.np64(out["top_val"]), ref["top_val"])
+            with np.errstate(over="ignore"):                 # past fp32's range: -inf
+                _check_lse(out["lse"], ref["lse"].astype(np.float32).astype(np.float64))
+                _check_lse(out["lse_rest"], ref["lse_rest"].astype(np.float32).astype(np.float64))
