@@ -719,6 +719,121 @@ int alr_embed_grad(const void* dY, int32_t dtype, int32_t V, int32_t d, const in
                    int64_t N, float scale, int32_t accumulate, float* dE, void* workspace,
                    size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * The key-value cache of a rollout, in pages: what a target's rollout (App. A: 13 tokens and more from
+ * each anchor, over the cached corpus prefix of its sample) does in every layer and step around the
+ * operators above.
+ *   alr_kv_plan (once a step) -> per layer: alr_kv_append -> alr_kv_attention
+ *
+ * Sequence s has table[s, j] (table [n_seq, cols] int32) as its j-th page, page tokens in each: its
+ * token t is in slot table[s, t / page] * page + t % page.  Lengths, tables and slots stay on the
+ * device; nothing is read back, so a step can be captured into a graph and replayed as they change.
+ * ------------------------------------------------------------------------------------- */
+#define ALR_KV_MAX_SEQS 8192
+#define ALR_KV_MAX_DIM 256
+
+/* A layer's keys and values: element (page, token, head, i) of each is at
+ * page * stride_page + token * stride_token + head * stride_head + i, so a cache may be laid out by
+ * tokens or by heads.  Strides in elements, multiples of 16 bytes; K and V 16-byte aligned; dim a
+ * multiple of 16 bytes, at most ALR_KV_MAX_DIM; n_pages * page < 2^31. */
+typedef struct {
+    void* K;
+    void* V;
+    int64_t stride_page;
+    int64_t stride_token;
+    int64_t stride_head;
+    int32_t n_pages;
+    int32_t page;       /* tokens of a page, >= 1                                             */
+    int32_t heads;      /* key-value heads                                                    */
+    int32_t dim;        /* of a head                                                          */
+    int32_t dtype;      /* ALR_BF16 or ALR_F32                                                */
+} alr_kv_cache;
+
+/* Outputs of alr_kv_plan, device pointers. */
+typedef struct {
+    int32_t* len;        /* [S] lengths after the step (required; may be the input)           */
+    int32_t* slot;       /* [T] slot of each new token, -1 for none (required if T > 0)       */
+    int32_t* pool_used;  /* [1] pages taken from the pool after the step (required; may be
+                            the input)                                                        */
+    int32_t* start;      /* [S + 1] first row of each sequence in the batch (nullable)        */
+    int32_t* tok_seq;    /* [T] sequence of each row, -1 for none (nullable)                  */
+    int32_t* tok_len;    /* [T] tokens up to and with the row's own, 0 for none (nullable)    */
+    int32_t* n_refused;  /* [1] sequences whose tokens found no place (nullable)              */
+} alr_kv_plan_outputs;
+
+/*
+ * Block tables and slot map of a step.  Sequence s of S <= ALR_KV_MAX_SEQS holds len[s] tokens and gets
+ * add[s] >= 0 more, as consecutive rows of a batch of T, sequences in order (start[s] is the sum of
+ * the add before s); add[s] < 0: the sequence has ended, its pages go back to the pool, its length to
+ * 0, its table's row stays as it is.
+ *   pool [n_pool], pool_used [1]: the free pages are pool[pool_used..n_pool); what lies before is not
+ *            read.  The n ended pages (by sequence, then by position) are written to
+ *            pool[pool_used - n..pool_used), then pages are taken from there on, in that order, and
+ *            written behind the pages that their sequences hold in table [S, cols].
+ *   A sequence whose tokens would pass cols pages or row T, or for which (with those before it) too few
+ *   pages are free, is refused: it keeps its length, its rows get slot -1, and sequences after
+ *   it that need pages of the pool are refused too if the pages up to and with theirs are too many.
+ * Lengths outside [0, cols * page] count as the nearest bound.  One launch, no workspace.
+ */
+int alr_kv_plan(int32_t S, int32_t page, int32_t cols, int32_t n_pool, int32_t T,
+                const int32_t* len, const int32_t* add, int32_t* pool, const int32_t* pool_used,
+                int32_t* table, const alr_kv_plan_outputs* out, void* stream);
+
+/*
+ * New keys and values into the cache: row i of K_new and V_new ([T, heads, dim] of src_dtype, rows ld
+ * elements apart, heads dim apart) to slot[i], rounded to the cache's type.  A slot outside
+ * [0, n_pages * page) takes nothing.  Slots of a call are distinct (of rows with the same slot any
+ * one may stay, in each 16 bytes of its own).
+ * K_new, V_new 16-byte aligned, ld a multiple of 16 bytes.
+ */
+int alr_kv_append(const alr_kv_cache* cache, const void* K_new, const void* V_new,
+                  int32_t src_dtype, int64_t T, int64_t ld, const int32_t* slot, void* stream);
+
+/* Problem description of alr_kv_attention. */
+typedef struct {
+    int64_t N;                /* query rows                                                   */
+    int64_t ldq;              /* elements between rows of Q, a multiple of 16 bytes           */
+    int64_t ldo;              /* elements between rows of out, a multiple of 16 bytes         */
+    int32_t H;                /* query heads, a multiple of cache->heads: head h reads
+                                 key-value head h / (H / heads)                               */
+    int32_t n_seq;            /* rows of the table                                            */
+    int32_t cols;             /* pages of each                                                */
+    int32_t rows_per_seq;     /* see below, >= 1                                              */
+    int32_t rows_per_prefix;  /* see below, >= 1                                              */
+    float scale;              /* of q k^T (usually dim^-1/2), finite                          */
+} alr_kv_attention_params;
+
+/* Workspace bytes alr_kv_attention needs (0 on invalid sizes); has_prefix: with a prefix. */
+size_t alr_kv_attention_workspace_size(int64_t N, int32_t H, int32_t dim, int32_t has_prefix);
+
+/*
+ * Attention of query rows over the cache.  Row r reads the first prefix_len[r] tokens of sequence
+ * prefix_seq[r] (if given) and the first len[r] of sequence seq[r]:
+ *   x_t = scale q k_t,   out[r, h] = sum_t exp(x_t - lse) v_t,   lse[r, h] = log sum_t exp(x_t).
+ * One row for each sequence is a decoding step; several rows with len counting up are a block of new
+ * tokens under a causal mask (tok_seq and tok_len of alr_kv_plan are its seq and len); a prefix shared
+ * by many rows is stored once.
+ *   Q [N, H, dim], out [N, H, dim] of the cache's type (row strides ldq, ldo; out may not overlap Q);
+ *   table [n_seq, cols] int32; len [N], prefix_len [N] int32: outside [0, cols * page] the nearest
+ *            bound counts;
+ *   seq [N] int32 or NULL (row r reads sequence r / rows_per_seq); prefix_seq [N] and prefix_len [N]
+ *            int32, both or neither.  A sequence outside [0, n_seq) holds no tokens;
+ *            a table entry outside [0, n_pages) holds none at its positions.
+ *   rows_per_seq, rows_per_prefix: how many consecutive rows, from row 0, read the same seq (with seq
+ *            NULL exactly, else usually) and the same prefix_seq (usually): a matter of speed, as rows
+ *            that read the same tokens together share their loads.
+ *   lse [N, H] float or NULL.  A row without tokens, or whose scores are all -inf, gives zeros and
+ *            -inf; a score of NaN or +inf gives NaN.  What lies in slots that a row does not read (NaN
+ *            included) does not reach it.
+ * Scores, exponentials, sums and outputs are held in fp32; for a bf16 cache the weights exp(x_t - m) are
+ * rounded to bf16 for their product with v.  Calls that run at the same time need workspaces of their
+ * own.
+ */
+int alr_kv_attention(const alr_kv_cache* cache, const alr_kv_attention_params* p, const void* Q,
+                     const int32_t* table, const int32_t* len, const int32_t* seq,
+                     const int32_t* prefix_len, const int32_t* prefix_seq, void* out, float* lse,
+                     void* workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

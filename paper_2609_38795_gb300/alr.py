@@ -62,6 +62,26 @@ class AlrDistillOutputs(ctypes.Structure):
     _fields_ = [(f, _c_p) for f in _DISTILL_FIELDS]
 
 
+class AlrKvCache(ctypes.Structure):
+    _fields_ = [("K", _c_p), ("V", _c_p), ("stride_page", _c_i64), ("stride_token", _c_i64),
+                ("stride_head", _c_i64), ("n_pages", _c_i32), ("page", _c_i32), ("heads", _c_i32),
+                ("dim", _c_i32), ("dtype", _c_i32)]
+
+
+_KV_PLAN_FIELDS = ("len", "slot", "pool_used", "start", "tok_seq", "tok_len", "n_refused")
+ALR_KV_MAX_SEQS, ALR_KV_MAX_DIM = 8192, 256
+
+
+class AlrKvPlanOutputs(ctypes.Structure):
+    _fields_ = [(f, _c_p) for f in _KV_PLAN_FIELDS]
+
+
+class AlrKvAttentionParams(ctypes.Structure):
+    _fields_ = [("N", _c_i64), ("ldq", _c_i64), ("ldo", _c_i64), ("H", _c_i32), ("n_seq", _c_i32),
+                ("cols", _c_i32), ("rows_per_seq", _c_i32), ("rows_per_prefix", _c_i32),
+                ("scale", _c_f)]
+
+
 # name -> (restype, argtypes); must match include/alr.h
 SIGNATURES = {
     "alr_version": (ctypes.c_char_p, []),
@@ -139,6 +159,14 @@ SIGNATURES = {
     "alr_embed_grad_workspace_size": (_c_sz, [_c_i32, _c_i32, _c_i64]),
     "alr_embed_grad": (_c_int, [_c_p, _c_i32, _c_i32, _c_i32, _c_p, _c_i64, _c_f, _c_i32, _c_p,
                                 _c_p, _c_sz, _c_p]),
+    "alr_kv_plan": (_c_int, [_c_i32, _c_i32, _c_i32, _c_i32, _c_i32, _c_p, _c_p, _c_p, _c_p, _c_p,
+                             ctypes.POINTER(AlrKvPlanOutputs), _c_p]),
+    "alr_kv_append": (_c_int, [ctypes.POINTER(AlrKvCache), _c_p, _c_p, _c_i32, _c_i64, _c_i64, _c_p,
+                               _c_p]),
+    "alr_kv_attention_workspace_size": (_c_sz, [_c_i64, _c_i32, _c_i32, _c_i32]),
+    "alr_kv_attention": (_c_int, [ctypes.POINTER(AlrKvCache), ctypes.POINTER(AlrKvAttentionParams),
+                                  _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_sz,
+                                  _c_p]),
     "alr_gemm_form": (_c_int, [_c_i32, _c_i32, _c_i32, _c_i32, _c_p, _c_p]),
 }
 
@@ -768,6 +796,110 @@ def alr_embed_grad(dY, tokens, dE, workspace, scale=1.0, accumulate=False, strea
                                 _ptr(tokens, "tokens", N, _I32), N, float(scale), int(accumulate),
                                 _ptr(dE, "dE", V * d, _F32), _ws(workspace), _nbytes(workspace),
                                 _stream(stream)))
+
+
+# ------------------------------------------------------- paged key-value cache ---
+def _strided(t, name, dims, dtype=None):
+    """Data pointer of a strided view on the current CUDA device whose last dimension is contiguous
+    and whose elements do not overlap."""
+    if not isinstance(t, _Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if not t.is_cuda or t.get_device() != _cuda_device():
+        raise ValueError(f"{name} must be on the current CUDA device (got {t.device})")
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions (got {t.dim()})")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
+    if not t.is_contiguous():
+        shape, stride = t.shape, t.stride()
+        reach = 1
+        for st, n in sorted((st, n) for st, n in zip(stride, shape) if n > 1):
+            if st < reach:
+                raise ValueError(f"{name}'s elements must not overlap (got strides {stride})")
+            reach = st * (n - 1) + reach
+        if shape[-1] > 1 and stride[-1] != 1:
+            raise ValueError(f"{name}'s last dimension must be contiguous (got strides {stride})")
+    return t.data_ptr()
+
+
+def _kv_cache(K, V):
+    """The cache of two views [n_pages, page, heads, dim] with the same strides."""
+    k, v = _strided(K, "K", 4), _strided(V, "V", 4, K.dtype)
+    shape, stride = K.shape, K.stride()
+    if V.shape != shape or V.stride() != stride:
+        raise ValueError(f"K and V must be laid out alike (got {list(shape)}, {stride} and "
+                         f"{list(V.shape)}, {V.stride()})")
+    # the stride of a dimension of one entry is never used
+    sp, st, sh = (s if n > 1 else 0 for s, n in zip(stride[:3], shape[:3]))
+    return AlrKvCache(k, v, sp, st, sh, *shape, dtype_code(K.dtype))
+
+
+def alr_kv_plan(len, add, pool, pool_used, table, page, out: dict, stream=None):
+    """len, add [S], pool [n_pool], pool_used [1], table [S, cols], all int32; out: len [S] (may be
+    len), slot [T], pool_used [1] (may be pool_used); optional start [S + 1], tok_seq, tok_len [T],
+    n_refused [1]."""
+    S, T, n_pool = len.numel(), out["slot"].numel(), pool.numel()
+    if table.dim() != 2 or table.shape[0] < S:
+        raise ValueError(f"table must be [{S}, cols] (got {[*table.shape]})")
+    cols = table.shape[1]
+    sizes = dict(len=S, slot=T, pool_used=1, start=S + 1, tok_seq=T, tok_len=T, n_refused=1)
+    o = AlrKvPlanOutputs(*[_ptr(out[f] if f in ("len", "slot", "pool_used") else out.get(f), f, n, _I32)
+                           for f, n in sizes.items()])
+    _check(lib().alr_kv_plan(S, page, cols, n_pool, T, _ptr(len, "len", S, _I32),
+                             _ptr(add, "add", S, _I32), _ptr(pool, "pool", n_pool, _I32),
+                             _ptr(pool_used, "pool_used", 1, _I32), _ptr(table, "table", S * cols, _I32),
+                             ctypes.byref(o), _stream(stream)))
+
+
+def alr_kv_append(K_new, V_new, K, V, slot, stream=None):
+    """K_new, V_new [T, heads, dim] (rows any stride apart) into slot [T] int32 of the cache's views
+    K, V [n_pages, page, heads, dim]."""
+    c = _kv_cache(K, V)
+    k, v = _strided(K_new, "K_new", 3), _strided(V_new, "V_new", 3, K_new.dtype)
+    T, heads, dim = K_new.shape
+    ld, st = K_new.stride(0) if T > 1 else heads * dim, K_new.stride(1)
+    if (heads, dim) != (c.heads, c.dim) or (heads > 1 and st != dim) or V_new.shape != K_new.shape or \
+            (T > 0 and V_new.stride() != K_new.stride()):
+        raise ValueError(f"K_new and V_new must be rows of [{c.heads}, {c.dim}] laid out alike (got "
+                         f"{[*K_new.shape]}, {K_new.stride()} and {[*V_new.shape]}, {V_new.stride()})")
+    _check(lib().alr_kv_append(ctypes.byref(c), k, v, dtype_code(K_new.dtype), T, ld,
+                               _ptr(slot, "slot", T, _I32), _stream(stream)))
+
+
+def alr_kv_attention_workspace_size(N, H, dim, prefix=False) -> int:
+    return lib().alr_kv_attention_workspace_size(N, H, dim, int(prefix))
+
+
+def _kv_rows(t, name, dtype=None):
+    """(pointer, row stride) of rows [N, H, dim] that lie any stride apart."""
+    p = _strided(t, name, 3, dtype)
+    N, H, dim = t.shape
+    if H > 1 and t.stride(1) != dim:
+        raise ValueError(f"{name}'s heads must be contiguous (got strides {t.stride()})")
+    return p, (t.stride(0) if N > 1 else H * dim)
+
+
+def alr_kv_attention(Q, K, V, table, len, out, workspace, seq=None, prefix_len=None, prefix_seq=None,
+                     lse=None, scale=None, rows_per_seq=1, rows_per_prefix=1, stream=None):
+    """Q, out [N, H, dim] (rows any stride apart), K, V [n_pages, page, heads, dim] views of the cache,
+    table [n_seq, cols], len, seq, prefix_len, prefix_seq [N] int32; optional lse [N, H].  scale:
+    dim^-1/2 by default."""
+    c = _kv_cache(K, V)
+    q, ldq = _kv_rows(Q, "Q", K.dtype)
+    o, ldo = _kv_rows(out, "out", K.dtype)
+    N, H, dim = Q.shape
+    if out.shape != Q.shape or dim != c.dim:
+        raise ValueError(f"Q and out must be [N, H, {c.dim}] (got {[*Q.shape]}, {[*out.shape]})")
+    if table.dim() != 2:
+        raise ValueError(f"table must be [n_seq, cols] (got {[*table.shape]})")
+    n_seq, cols = table.shape
+    p = AlrKvAttentionParams(N, ldq, ldo, H, n_seq, cols, rows_per_seq, rows_per_prefix,
+                             dim ** -0.5 if scale is None else float(scale))
+    _check(lib().alr_kv_attention(
+        ctypes.byref(c), ctypes.byref(p), q, _ptr(table, "table", n_seq * cols, _I32),
+        _ptr(len, "len", N, _I32), _ptr(seq, "seq", N, _I32),
+        _ptr(prefix_len, "prefix_len", N, _I32), _ptr(prefix_seq, "prefix_seq", N, _I32), o,
+        _ptr(lse, "lse", N * H, _F32), _ws(workspace), _nbytes(workspace), _stream(stream)))
 
 
 # ------------------------------------------------------------------ convenience ---

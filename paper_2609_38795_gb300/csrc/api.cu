@@ -1612,3 +1612,144 @@ int alr_embed_grad(const void* dY, int32_t dtype, int32_t V, int32_t d, const in
 }
 
 }  // extern "C"
+
+// ------------------------------------------------------------ paged key-value cache ---
+namespace {
+
+int check_cache(const alr_kv_cache* c, alr::KvCache* out) {
+  if (c == nullptr) return fail(ALR_ERR_INVALID_ARG, "cache is NULL");
+  if (c->dtype != ALR_BF16 && c->dtype != ALR_F32)
+    return fail(ALR_ERR_UNSUPPORTED, "dtype %d is not ALR_BF16 or ALR_F32", c->dtype);
+  const int pack = int(16 / elem_size(c->dtype));
+  if (c->page < 1 || c->heads < 1 || c->n_pages < 0 ||
+      int64_t(c->n_pages) * c->page > INT32_MAX)
+    return fail(ALR_ERR_INVALID_ARG, "bad cache sizes n_pages=%d page=%d heads=%d (n_pages * page < 2^31)",
+                c->n_pages, c->page, c->heads);
+  if (c->dim < 1 || c->dim > ALR_KV_MAX_DIM || c->dim % pack != 0)
+    return fail(ALR_ERR_INVALID_ARG, "dim = %d must be a multiple of %d and at most %d", c->dim, pack,
+                ALR_KV_MAX_DIM);
+  for (const int64_t st : {c->stride_page, c->stride_token, c->stride_head})
+    if (st < 0 || st > (int64_t(1) << 40) || st % pack != 0)
+      return fail(ALR_ERR_INVALID_ARG, "cache strides must be multiples of %d in [0, 2^40]", pack);
+  if (c->n_pages > 0 && (c->K == nullptr || c->V == nullptr || !aligned16(c->K) || !aligned16(c->V)))
+    return fail(ALR_ERR_INVALID_ARG, "K and V must be non-NULL and 16-byte aligned");
+  *out = {c->K, c->V, c->stride_page, c->stride_token, c->stride_head, c->n_pages, c->page, c->heads,
+          c->dim, c->dtype == ALR_BF16 ? 0 : 1};
+  return ALR_OK;
+}
+
+constexpr int64_t kMostKvRows = int64_t(1) << 24;
+
+bool kv_rows_fit(int64_t N, int32_t H) { return N >= 0 && N <= kMostKvRows && H >= 1 && H <= 1024; }
+
+}  // namespace
+
+extern "C" {
+
+int alr_kv_plan(int32_t S, int32_t page, int32_t cols, int32_t n_pool, int32_t T,
+                const int32_t* len, const int32_t* add, int32_t* pool, const int32_t* pool_used,
+                int32_t* table, const alr_kv_plan_outputs* out, void* stream) {
+  ALR_RANGE();
+  if (S < 0 || S > ALR_KV_MAX_SEQS)
+    return fail(ALR_ERR_INVALID_ARG, "S = %d must lie in [0, %d]", S, ALR_KV_MAX_SEQS);
+  if (page < 1 || cols < 1 || int64_t(page) * cols > INT32_MAX)
+    return fail(ALR_ERR_INVALID_ARG, "bad sizes page=%d cols=%d (page * cols < 2^31)", page, cols);
+  if (n_pool < 0 || T < 0) return fail(ALR_ERR_INVALID_ARG, "bad sizes n_pool=%d T=%d", n_pool, T);
+  if (out == nullptr || out->pool_used == nullptr || pool_used == nullptr)
+    return fail(ALR_ERR_INVALID_ARG, "pool_used and its output must be non-NULL");
+  if (S > 0 && (len == nullptr || add == nullptr || table == nullptr || out->len == nullptr))
+    return fail(ALR_ERR_INVALID_ARG, "len, add, table and the output len must be non-NULL");
+  if (n_pool > 0 && pool == nullptr) return fail(ALR_ERR_INVALID_ARG, "pool must be non-NULL");
+  if (T > 0 && out->slot == nullptr) return fail(ALR_ERR_INVALID_ARG, "slot must be non-NULL");
+  DevInfo info;
+  const int rc = require_sm103(&info);
+  if (rc != ALR_OK) return rc;
+  const cudaError_t e = alr::launch_kv_plan(
+      {S, page, cols, n_pool, T, len, add, pool, pool_used, table, out->len, out->slot,
+       out->pool_used, out->start, out->tok_seq, out->tok_len, out->n_refused},
+      static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? ALR_OK : cuda_fail(e, "cache plan launch");
+}
+
+int alr_kv_append(const alr_kv_cache* cache, const void* K_new, const void* V_new,
+                  int32_t src_dtype, int64_t T, int64_t ld, const int32_t* slot, void* stream) {
+  ALR_RANGE();
+  alr::KvCache c;
+  int rc = check_cache(cache, &c);
+  if (rc != ALR_OK) return rc;
+  if (src_dtype != ALR_BF16 && src_dtype != ALR_F32)
+    return fail(ALR_ERR_UNSUPPORTED, "src_dtype %d is not ALR_BF16 or ALR_F32", src_dtype);
+  if (T < 0 || T > kMostRows)
+    return fail(ALR_ERR_INVALID_ARG, "T = %lld must lie in [0, 2^26]", (long long)T);
+  if (ld < int64_t(c.heads) * c.dim || ld > (int64_t(1) << 40) ||
+      ld * elem_size(src_dtype) % 16 != 0 || c.dim * elem_size(src_dtype) % 16 != 0)
+    return fail(ALR_ERR_INVALID_ARG,
+                "ld = %lld must be at least heads * dim and, as dim, a multiple of 16 bytes",
+                (long long)ld);
+  if (T == 0 || c.n_pages == 0) return ALR_OK;
+  if (K_new == nullptr || V_new == nullptr || !aligned16(K_new) || !aligned16(V_new))
+    return fail(ALR_ERR_INVALID_ARG, "K_new and V_new must be non-NULL and 16-byte aligned");
+  if (slot == nullptr) return fail(ALR_ERR_INVALID_ARG, "slot must be non-NULL");
+  DevInfo info;
+  if ((rc = require_sm103(&info)) != ALR_OK) return rc;
+  const cudaError_t e = alr::launch_kv_append(c, K_new, V_new, src_dtype == ALR_BF16 ? 0 : 1, T, ld,
+                                              slot, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? ALR_OK : cuda_fail(e, "cache append launch");
+}
+
+size_t alr_kv_attention_workspace_size(int64_t N, int32_t H, int32_t dim, int32_t has_prefix) {
+  if (!kv_rows_fit(N, H) || dim < 1 || dim > ALR_KV_MAX_DIM) return 0;
+  return alr::kv_attention_workspace(N, H, dim, has_prefix != 0);
+}
+
+int alr_kv_attention(const alr_kv_cache* cache, const alr_kv_attention_params* p, const void* Q,
+                     const int32_t* table, const int32_t* len, const int32_t* seq,
+                     const int32_t* prefix_len, const int32_t* prefix_seq, void* out, float* lse,
+                     void* workspace, size_t ws_bytes, void* stream) {
+  ALR_RANGE();
+  alr::KvCache c;
+  int rc = check_cache(cache, &c);
+  if (rc != ALR_OK) return rc;
+  if (p == nullptr) return fail(ALR_ERR_INVALID_ARG, "params is NULL");
+  if (!kv_rows_fit(p->N, p->H) || p->H % c.heads != 0)
+    return fail(ALR_ERR_INVALID_ARG,
+                "N = %lld must lie in [0, 2^24] and H = %d be a multiple of heads = %d, at most 1024",
+                (long long)p->N, p->H, c.heads);
+  if (p->n_seq < 0 || p->cols < 1 || int64_t(p->cols) * c.page > INT32_MAX)
+    return fail(ALR_ERR_INVALID_ARG, "bad sizes n_seq=%d cols=%d (cols * page < 2^31)", p->n_seq, p->cols);
+  if (p->rows_per_seq < 1 || p->rows_per_prefix < 1)
+    return fail(ALR_ERR_INVALID_ARG, "rows_per_seq = %d and rows_per_prefix = %d must be at least 1",
+                p->rows_per_seq, p->rows_per_prefix);
+  if (!std::isfinite(p->scale)) return fail(ALR_ERR_INVALID_ARG, "scale must be finite");
+  const int64_t pack = int64_t(16 / elem_size(cache->dtype)), row = int64_t(p->H) * c.dim;
+  for (const int64_t ld : {p->ldq, p->ldo})
+    if (ld < row || ld > (int64_t(1) << 40) || ld % pack != 0)
+      return fail(ALR_ERR_INVALID_ARG,
+                  "ldq = %lld and ldo = %lld must be at least H * dim and multiples of %lld",
+                  (long long)p->ldq, (long long)p->ldo, (long long)pack);
+  if (p->N == 0) return ALR_OK;
+  if (Q == nullptr || out == nullptr || !aligned16(Q) || !aligned16(out))
+    return fail(ALR_ERR_INVALID_ARG, "Q and out must be non-NULL and 16-byte aligned");
+  if (len == nullptr || (table == nullptr && p->n_seq > 0))
+    return fail(ALR_ERR_INVALID_ARG, "table and len must be non-NULL");
+  if ((prefix_len == nullptr) != (prefix_seq == nullptr))
+    return fail(ALR_ERR_INVALID_ARG, "prefix_len and prefix_seq go together");
+  if (seq == nullptr && int64_t(p->n_seq) * p->rows_per_seq < p->N)
+    return fail(ALR_ERR_INVALID_ARG, "without seq the table needs a row for every %d of %lld rows",
+                p->rows_per_seq, (long long)p->N);
+  const size_t need = alr::kv_attention_workspace(p->N, p->H, c.dim, prefix_len != nullptr);
+  if (workspace == nullptr || !aligned16(workspace) || ws_bytes < need)
+    return fail(ALR_ERR_INVALID_ARG,
+                "workspace must be 16-byte aligned and hold %zu bytes (got %zu)", need, ws_bytes);
+  DevInfo info;
+  if ((rc = require_sm103(&info)) != ALR_OK) return rc;
+  int* status = alr::device_status_ptr();
+  if (status == nullptr) return fail(ALR_ERR_CUDA, "device status word unavailable");
+  const cudaError_t e = alr::launch_kv_attention(
+      {c, p->N, p->ldq, p->ldo, p->H, p->n_seq, p->cols, p->rows_per_seq, p->rows_per_prefix,
+       p->scale, Q, table, len, seq, prefix_len, prefix_seq, out, lse, workspace},
+      info.sms, status, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? ALR_OK : cuda_fail(e, "cache attention launch");
+}
+
+}  // extern "C"

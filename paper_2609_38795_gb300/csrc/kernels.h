@@ -271,6 +271,51 @@ cudaError_t launch_embed_grad(int dtype, const void* dY, int V, int d, const int
                               int N, float scale, bool accumulate, float* dE, void* workspace,
                               int sms, cudaStream_t s);
 
+// The paged key-value cache (kv_kernels.cu, kv_attention.cu).
+struct KvCache {
+  void* K;
+  void* V;
+  long long sp, st, sh;      // strides of a page, a token, a head (elements)
+  int n_pages, page, heads, dim, dtype;
+};
+constexpr int kKvMaxSeqs = 8192;     // ALR_KV_MAX_SEQS
+constexpr int kKvMaxDim = 256;       // ALR_KV_MAX_DIM
+struct KvPlan {
+  int S, page, cols, n_pool, T;
+  const int32_t* len;
+  const int32_t* add;
+  int32_t* pool;
+  const int32_t* pool_used;
+  int32_t* table;
+  int32_t* out_len;
+  int32_t* slot;
+  int32_t* out_used;
+  int32_t* start;            // this and the following may be nullptr
+  int32_t* tok_seq;
+  int32_t* tok_len;
+  int32_t* n_refused;
+};
+cudaError_t launch_kv_plan(const KvPlan& p, cudaStream_t s);
+cudaError_t launch_kv_append(const KvCache& c, const void* K_new, const void* V_new, int src_dtype,
+                             long long T, long long ld, const int32_t* slot, cudaStream_t s);
+struct KvAttention {
+  KvCache c;
+  long long N, ldq, ldo;
+  int H, n_seq, cols, rows_per_seq, rows_per_prefix;
+  float scale;
+  const void* Q;
+  const int32_t* table;
+  const int32_t* len;
+  const int32_t* seq;          // may be nullptr
+  const int32_t* prefix_len;   // these two may be nullptr
+  const int32_t* prefix_seq;
+  void* out;
+  float* lse;                  // may be nullptr
+  void* ws;
+};
+size_t kv_attention_workspace(long long N, int H, int dim, bool prefix);
+cudaError_t launch_kv_attention(const KvAttention& a, int sms, int* status, cudaStream_t s);
+
 // Record `msg` as this host thread's alr_last_error() text and return `code` (api.cu).
 int set_last_error(int code, const char* msg);
 

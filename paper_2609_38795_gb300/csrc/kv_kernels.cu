@@ -1,0 +1,258 @@
+// The paged key-value cache: the step's block tables and slot map, and new rows into their slots.
+#include <algorithm>
+
+#include "kernels.h"
+#include "launch.h"
+#include "row_reduce.cuh"
+
+namespace alr {
+namespace {
+
+// ------------------------------------------------------------------------ plan ---
+// Everything follows from sums over the sequences before one: of the tokens asked for (its first row of
+// the batch), of the new pages (its place in the list of free pages) and of the returned ones (theirs).
+// Each block takes those sums over all sequences for itself (S is at most 8192, 8 KB a thousand), the
+// blocks of the one cluster meet at its barrier, so that what is updated in place has been read by all,
+// and share the writing: a token's page is found from its sequence's sums, be it an old one, one out of
+// the pool or one that another sequence returns in this step.  No block reads what another writes.
+//   Bound by latency: two loads, two scans, a barrier, two dependent loads a token.
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWarps = kPlanThreads / 32;
+
+// Sums of the threads before this one (v becomes that), and of all.  buf: kPlanWarps entries, free
+// again on return.
+ALR_DEV long long scan_before(long long& v, long long* buf) {
+  const long long own = v, up = warp_scan(v);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane == 31) buf[warp] = up;
+  __syncthreads();
+  const long long w = warp_scan(lane < kPlanWarps ? buf[lane] : 0ll);
+  const long long before = warp == 0 ? 0ll : __shfl_sync(0xffffffffu, w, warp - 1);
+  const long long all = __shfl_sync(0xffffffffu, w, kPlanWarps - 1);
+  __syncthreads();
+  v = before + up - own;
+  return all;
+}
+
+// Largest i in [0, n) with a[i] <= k: the entry that element k of the running sums a[0] = 0 <= a[1] <= ...
+// belongs to (the last of those with the same sum, which is the one that is not empty).
+ALR_DEV int owner_of(const int* a, int n, int k) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a[mid] <= k) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+struct PlanSums {
+  int* start;   // [S + 1] first row of the batch (at most T)
+  int* len;     // [S] tokens held; ~tokens where the rows get no slot (refused or ended)
+  int* fresh;   // [S] new pages before
+  int* back;    // [S] returned pages before
+};
+
+ALR_DEV int pages_of(long long tokens, int page) { return int((tokens + page - 1) / page); }
+
+__global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlan p, int n_cta) {
+  extern __shared__ int plan_smem[];
+  __shared__ long long buf[kPlanWarps];
+  const int S = p.S, tid = threadIdx.x, rank = blockIdx.x;
+  const PlanSums t = {plan_smem, plan_smem + S + 1, plan_smem + 2 * S + 1, plan_smem + 3 * S + 1};
+  pdl_wait_and_release();
+  const int used = min(max(*p.pool_used, 0), p.n_pool);
+  const long long most = (long long)p.cols * p.page;
+  const int per = (S + kPlanThreads - 1) / kPlanThreads;
+  const int s0 = min(tid * per, S), s1 = min(s0 + per, S);
+
+  long long tokens = 0, back = 0;
+  for (int s = s0; s < s1; ++s) {
+    const int n = int(min((long long)max(p.len[s], 0), most)), a = p.add[s];
+    t.len[s] = n;
+    t.back[s] = int(min(back, (long long)INT32_MAX));
+    t.start[s] = a;                          // for now
+    tokens += max(a, 0);
+    if (a < 0) back += pages_of(n, p.page);
+  }
+  long long before = tokens, back_before = back;
+  const long long all = scan_before(before, buf);
+  const long long n_back = scan_before(back_before, buf);
+  const long long n_free = p.n_pool - used + n_back;
+  long long need = 0, row = before;
+  for (int s = s0; s < s1; ++s) {
+    const int a = t.start[s], n = t.len[s];
+    if (a >= 0 && n + (long long)a <= most && row + a <= p.T)
+      need += pages_of(n + (long long)a, p.page) - pages_of(n, p.page);
+    row += max(a, 0);
+  }
+  long long need_before = need;
+  scan_before(need_before, buf);
+  // the sequences' answers; n_new: the pages that are taken, up to the last sequence that gets any
+  int refused = 0;
+  long long k = need_before, n_new = 0;
+  row = before;
+  cluster_sync();                            // every block has read len and pool_used: they may be written
+  for (int s = s0; s < s1; ++s) {
+    const int a = t.start[s], n = t.len[s];
+    const bool asks = a >= 0 && n + (long long)a <= most && row + a <= p.T;
+    const int w = asks ? pages_of(n + (long long)a, p.page) - pages_of(n, p.page) : 0;
+    const bool ok = asks && (w == 0 || k + w <= n_free);
+    t.back[s] = int(min(back_before + t.back[s], (long long)INT32_MAX));
+    t.fresh[s] = int(min(k, (long long)INT32_MAX));
+    t.start[s] = int(min(row, (long long)p.T));
+    if (!ok) t.len[s] = ~n;
+    if (a >= 0 && !ok) ++refused;
+    if (ok && w > 0) n_new = k + w;
+    if (rank == 0) {
+      p.out_len[s] = a < 0 ? 0 : ok ? n + a : n;
+      if (p.start != nullptr) p.start[s] = int(min(row, (long long)INT32_MAX));
+    }
+    k += w;
+    row += max(a, 0);
+  }
+  const int n_rows = int(min(all, (long long)p.T));
+  if (tid == 0) {
+    t.start[S] = n_rows;
+    if (rank == 0 && p.start != nullptr) p.start[S] = int(min(all, (long long)INT32_MAX));
+  }
+  n_new = block_reduce(n_new, MaxOp(), buf);
+  if (rank == 0) {
+    const long long r = block_reduce((long long)refused, AddOp(), buf);
+    if (tid == 0) {
+      *p.out_used = int(max(used - n_back + n_new, 0ll));
+      if (p.n_refused != nullptr) *p.n_refused = int(r);
+    }
+  }
+  __syncthreads();
+
+  // page number i of the list of free pages: the returned ones, then the pool's
+  const auto returned = [&](int i) {
+    const int s = owner_of(t.back, S, i);
+    return p.table[(long long)s * p.cols + (i - t.back[s])];
+  };
+  const auto page_at = [&](int i) {
+    return i < n_back ? returned(i) : p.pool[used + (i - int(n_back))];
+  };
+  const int first = rank * kPlanThreads + tid, step = n_cta * kPlanThreads;
+  for (long long i = first; i < n_back; i += step) {
+    const long long at = used - n_back + i;
+    if (at >= 0) p.pool[at] = returned(int(i));
+  }
+  for (long long i = first; i < n_new; i += step) {
+    const int s = owner_of(t.fresh, S, int(i));
+    const int n = t.len[s] < 0 ? ~t.len[s] : t.len[s];
+    p.table[(long long)s * p.cols + pages_of(n, p.page) + (int(i) - t.fresh[s])] = page_at(int(i));
+  }
+  // rows: each warp a stretch of its own, whose sequences follow one another
+  const int n_warps = n_cta * kPlanWarps, stretch = ((p.T + n_warps - 1) / n_warps + 31) / 32 * 32;
+  const long long r0 = (long long)(rank * kPlanWarps + (tid >> 5)) * stretch;
+  int s = -1;
+  for (long long r = r0 + (tid & 31); r < min(r0 + stretch, (long long)p.T); r += 32) {
+    int seq = -1, n = 0, slot = -1;
+    if (r < n_rows) {
+      if (s < 0 || r >= t.start[s + 1]) {
+        int i = s < 0 ? S : s + 1;
+        for (int c = 0; c < 4 && i < S && r >= t.start[i + 1]; ++c) ++i;
+        s = i < S && r < t.start[i + 1] ? i : owner_of(t.start, S, int(r));
+      }
+      const int held = t.len[s];
+      if (held >= 0) {
+        const int pos = held + int(r) - t.start[s], j = pos / p.page, old = pages_of(held, p.page);
+        const int pg = j < old ? p.table[(long long)s * p.cols + j] : page_at(t.fresh[s] + (j - old));
+        seq = s;
+        n = pos + 1;
+        const long long at = (long long)pg * p.page + pos % p.page;
+        slot = pg < 0 || at > INT32_MAX ? -1 : int(at);
+      }
+    }
+    p.slot[r] = slot;
+    if (p.tok_seq != nullptr) p.tok_seq[r] = seq;
+    if (p.tok_len != nullptr) p.tok_len[r] = n;
+  }
+}
+
+// ---------------------------------------------------------------------- append ---
+// Memory-bound: a warp moves 32 kAppendBatch packs of 16 bytes (of the cache) of one row, all loads
+// issued before the stores.
+constexpr int kAppendThreads = 256;
+constexpr int kAppendBatch = 4;
+
+template <typename E, typename F>
+__global__ void __launch_bounds__(kAppendThreads)
+    kv_append_kernel(const KvCache c, const F* k_new, const F* v_new, long long T, long long ld,
+                     const int32_t* slot, int pieces) {
+  constexpr int kPack = 16 / sizeof(E);
+  struct alignas(16) Dst { E e[kPack]; };
+  struct alignas(16) Src { F e[kPack]; };
+  pdl_wait_and_release();
+  const long long w = (long long)blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32;
+  const long long i = w / (2 * pieces);
+  if (i >= T) return;
+  const int piece = int(w - i * 2 * pieces), at = slot[i];
+  if (at < 0 || at >= (long long)c.n_pages * c.page) return;
+  const bool is_v = piece >= pieces;
+  const int packs = c.dim / kPack, row = c.heads * packs;
+  const int first = (is_v ? piece - pieces : piece) * 32 * kAppendBatch + (threadIdx.x & 31);
+  const int pg = at / c.page;
+  const F* src = (is_v ? v_new : k_new) + i * ld;
+  E* dst = static_cast<E*>(is_v ? c.V : c.K) + pg * c.sp + (at - pg * c.page) * c.st;
+  Src x[kAppendBatch];
+#pragma unroll
+  for (int j = 0; j < kAppendBatch; ++j)
+    if (first + 32 * j < row) x[j] = *reinterpret_cast<const Src*>(src + (first + 32 * j) * kPack);
+#pragma unroll
+  for (int j = 0; j < kAppendBatch; ++j) {
+    const int q = first + 32 * j;
+    if (q >= row) break;
+    const int head = q / packs;
+    Dst y;
+#pragma unroll
+    for (int e = 0; e < kPack; ++e) y.e[e] = E(to_float(x[j].e[e]));
+    *reinterpret_cast<Dst*>(dst + head * c.sh + (q - head * packs) * kPack) = y;
+  }
+}
+
+template <typename E, typename F>
+cudaError_t run_append(const KvCache& c, const void* K_new, const void* V_new, long long T,
+                       long long ld, const int32_t* slot, cudaStream_t s) {
+  const int row = c.heads * c.dim / int(16 / sizeof(E));
+  const int pieces = (row + 32 * kAppendBatch - 1) / (32 * kAppendBatch);
+  const long long warps = T * 2 * pieces, per = kAppendThreads / 32;
+  return launch_pdl(kv_append_kernel<E, F>, dim3(unsigned((warps + per - 1) / per)),
+                    dim3(kAppendThreads), 0, s, c, static_cast<const F*>(K_new),
+                    static_cast<const F*>(V_new), T, ld, slot, pieces);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_plan(const KvPlan& p, cudaStream_t s) {
+  const int n_cta = p.T <= 4096 ? 1 : 8;
+  const size_t smem = size_t(4 * p.S + 1) * sizeof(int);
+  cudaError_t e = cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       int(size_t(4 * kKvMaxSeqs + 1) * sizeof(int)));
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[2] = {pdl_attribute(), {}};
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {unsigned(n_cta), 1, 1};
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(n_cta);
+  cfg.blockDim = dim3(kPlanThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kv_plan_kernel, p, n_cta);
+}
+
+cudaError_t launch_kv_append(const KvCache& c, const void* K_new, const void* V_new, int src_dtype,
+                             long long T, long long ld, const int32_t* slot, cudaStream_t s) {
+  using B = __nv_bfloat16;
+  if (c.dtype == 0)
+    return src_dtype == 0 ? run_append<B, B>(c, K_new, V_new, T, ld, slot, s)
+                          : run_append<B, float>(c, K_new, V_new, T, ld, slot, s);
+  return src_dtype == 0 ? run_append<float, B>(c, K_new, V_new, T, ld, slot, s)
+                        : run_append<float, float>(c, K_new, V_new, T, ld, slot, s);
+}
+
+}  // namespace alr
