@@ -731,6 +731,7 @@ int alr_embed_grad(const void* dY, int32_t dtype, int32_t V, int32_t d, const in
  * ------------------------------------------------------------------------------------- */
 #define ALR_KV_MAX_SEQS 8192
 #define ALR_KV_MAX_DIM 256
+#define ALR_KV_MAX_PAGE 65536
 
 /* A layer's keys and values: element (page, token, head, i) of each is at
  * page * stride_page + token * stride_token + head * stride_head + i, so a cache may be laid out by
@@ -743,7 +744,7 @@ typedef struct {
     int64_t stride_token;
     int64_t stride_head;
     int32_t n_pages;
-    int32_t page;       /* tokens of a page, >= 1                                             */
+    int32_t page;       /* tokens of a page, 1 <= page <= ALR_KV_MAX_PAGE                     */
     int32_t heads;      /* key-value heads                                                    */
     int32_t dim;        /* of a head                                                          */
     int32_t dtype;      /* ALR_BF16 or ALR_F32                                                */

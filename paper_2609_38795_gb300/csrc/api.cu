@@ -1621,10 +1621,11 @@ int check_cache(const alr_kv_cache* c, alr::KvCache* out) {
   if (c->dtype != ALR_BF16 && c->dtype != ALR_F32)
     return fail(ALR_ERR_UNSUPPORTED, "dtype %d is not ALR_BF16 or ALR_F32", c->dtype);
   const int pack = int(16 / elem_size(c->dtype));
-  if (c->page < 1 || c->heads < 1 || c->n_pages < 0 ||
+  if (c->page < 1 || c->page > ALR_KV_MAX_PAGE || c->heads < 1 || c->n_pages < 0 ||
       int64_t(c->n_pages) * c->page > INT32_MAX)
-    return fail(ALR_ERR_INVALID_ARG, "bad cache sizes n_pages=%d page=%d heads=%d (n_pages * page < 2^31)",
-                c->n_pages, c->page, c->heads);
+    return fail(ALR_ERR_INVALID_ARG,
+                "bad cache sizes n_pages=%d page=%d heads=%d (page <= %d, n_pages * page < 2^31)",
+                c->n_pages, c->page, c->heads, ALR_KV_MAX_PAGE);
   if (c->dim < 1 || c->dim > ALR_KV_MAX_DIM || c->dim % pack != 0)
     return fail(ALR_ERR_INVALID_ARG, "dim = %d must be a multiple of %d and at most %d", c->dim, pack,
                 ALR_KV_MAX_DIM);
@@ -1652,8 +1653,9 @@ int alr_kv_plan(int32_t S, int32_t page, int32_t cols, int32_t n_pool, int32_t T
   ALR_RANGE();
   if (S < 0 || S > ALR_KV_MAX_SEQS)
     return fail(ALR_ERR_INVALID_ARG, "S = %d must lie in [0, %d]", S, ALR_KV_MAX_SEQS);
-  if (page < 1 || cols < 1 || int64_t(page) * cols > INT32_MAX)
-    return fail(ALR_ERR_INVALID_ARG, "bad sizes page=%d cols=%d (page * cols < 2^31)", page, cols);
+  if (page < 1 || page > ALR_KV_MAX_PAGE || cols < 1 || int64_t(page) * cols > INT32_MAX)
+    return fail(ALR_ERR_INVALID_ARG, "bad sizes page=%d cols=%d (page <= %d, page * cols < 2^31)", page,
+                cols, ALR_KV_MAX_PAGE);
   if (n_pool < 0 || T < 0) return fail(ALR_ERR_INVALID_ARG, "bad sizes n_pool=%d T=%d", n_pool, T);
   if (out == nullptr || out->pool_used == nullptr || pool_used == nullptr)
     return fail(ALR_ERR_INVALID_ARG, "pool_used and its output must be non-NULL");

@@ -38,7 +38,7 @@ def _run(lib, cases):
 
 
 CACHES = [(dict(dtype=2), U, "dtype 2"), (dict(page=0), I, "page=0"), (dict(heads=0), I, "heads=0"),
-          (dict(n_pages=-1), I, "n_pages=-1"), (dict(n_pages=1 << 27), I, "2^31"),
+          (dict(n_pages=-1), I, "n_pages=-1"), (dict(n_pages=1 << 27), I, "2^31"), (dict(page=65537), I, "page=65537"),
           (dict(dim=12), I, "dim = 12"), (dict(dim=264), I, "dim = 264"), (dict(dim=0), I, "dim = 0"),
           (dict(dim=6, dtype=1), I, "dim = 6"), (dict(stride_page=4), I, "strides"),
           (dict(stride_token=-8), I, "strides"), (dict(stride_head=(1 << 40) + 8), I, "strides"),
@@ -51,7 +51,7 @@ def test_plan_refusals(lib):
         return lib.alr_kv_plan(S, page, cols, n_pool, T, len, add, pool, used, table, ctypes.byref(out), None)
 
     _run(lib, [(lambda: plan(S=-1), I, "S = -1"), (lambda: plan(S=8193), I, "S = 8193"),
-               (lambda: plan(page=0), I, "page=0"), (lambda: plan(cols=0), I, "cols=0"),
+               (lambda: plan(page=0), I, "page=0"), (lambda: plan(page=65537), I, "page=65537"), (lambda: plan(cols=0), I, "cols=0"),
                (lambda: plan(page=1 << 16, cols=1 << 15), I, "2^31"), (lambda: plan(n_pool=-1), I, "n_pool=-1"),
                (lambda: plan(T=-5), I, "T=-5"), (lambda: plan(len=None), I, "len"),
                (lambda: plan(add=None), I, "add"), (lambda: plan(table=None), I, "table"),
