@@ -9,190 +9,6 @@ namespace {
 
 constexpr int kBlk = 16;       // tokens of a block
 
-// ---------------------------------------------------------------------- schedule ---
-// First row and row count of a tile.
-ALR_DEV int tile_rows(const KvPass& p, long long tile, long long& row0) {
-  const long long g = tile / p.tg;
-  const int i = int(tile - g * p.tg);
-  row0 = g * p.per + (long long)i * p.rows;
-  return int(min((long long)min(p.rows, p.per - i * p.rows), p.a.N - row0));
-}
-
-ALR_DEV int blocks_of(int tokens) { return tokens / kBlk + (tokens % kBlk != 0); }
-
-// Blocks of a tile, counted by one thread.
-ALR_DEV int tile_blocks(const KvPass& p, long long tile) {
-  long long row0;
-  const int n = tile_rows(p, tile, row0);
-  int nb = 0, cur = 0, most = 0;
-  for (int i = 0; i < n; ++i) {
-    const int s = part_seq(p.part, row0 + i), len = part_len(p.a, p.part, row0 + i, s);
-    if (len == 0) continue;
-    if (most > 0 && s != cur) {
-      nb += blocks_of(most);
-      most = 0;
-    }
-    cur = s;
-    most = max(most, len);
-  }
-  return max(nb + blocks_of(most), 1);
-}
-
-// A tile's runs, held by a warp: lane i has row i.
-struct Tile {
-  int seq, len;       // of the row
-  int lead;           // first lane of the row's run (-1: before any)
-  int first;          // of a run's first lane: its first block; INT_MAX elsewhere
-  int most;           // ... and its longest row
-  int nb;             // blocks (all lanes)
-};
-
-ALR_DEV Tile load_tile(const KvPass& p, long long tile) {
-  const int lane = threadIdx.x & 31;
-  long long row0;
-  const int n = tile_rows(p, tile, row0);
-  Tile t;
-  t.seq = lane < n ? part_seq(p.part, row0 + lane) : -1;
-  t.len = lane < n ? part_len(p.a, p.part, row0 + lane, t.seq) : 0;
-  const uint32_t some = __ballot_sync(~0u, t.len > 0), up_to = (2u << lane) - 1;
-  const uint32_t before = some & (up_to >> 1);
-  const int prev = __shfl_sync(~0u, t.seq, before != 0 ? 31 - __clz(before) : 0);
-  const uint32_t leads = __ballot_sync(~0u, t.len > 0 && (before == 0 || prev != t.seq));
-  t.lead = (leads & up_to) != 0 ? 31 - __clz(leads & up_to) : -1;
-  t.most = t.len;
-  for (int off = 1; off < 32; off <<= 1) {
-    const int m = __shfl_down_sync(~0u, t.most, off), l = __shfl_down_sync(~0u, t.lead, off);
-    if (lane + off < 32 && l == t.lead) t.most = max(t.most, m);
-  }
-  const bool lead = (leads >> lane & 1) != 0;
-  const int nb = lead ? blocks_of(t.most) : 0, sum = warp_scan(nb);
-  t.first = lead ? sum - nb : INT_MAX;
-  t.nb = max(__shfl_sync(~0u, sum, 31), 1);
-  return t;
-}
-
-// Position of a worker in the line of blocks.  The loads run ahead of the sums, so a worker has two.
-struct Cursor {
-  Tile t;
-  long long tile;
-  int unit, b;
-  int lead, seq, most, t0;      // the run's first lane, sequence, tokens; the block's first token
-
-  ALR_DEV void enter() {
-    const uint32_t m = __ballot_sync(~0u, t.first <= b);
-    lead = m != 0 ? 31 - __clz(m) : -1;
-    const int from = max(lead, 0);
-    seq = __shfl_sync(~0u, t.seq, from);
-    most = lead < 0 ? 0 : __shfl_sync(~0u, t.most, from);
-    t0 = lead < 0 ? 0 : (b - __shfl_sync(~0u, t.first, from)) * kBlk;
-  }
-  ALR_DEV void start(const KvPass& p, long long tile_, int rest) {   // rest: blocks into the tile's items
-    tile = tile_;
-    t = load_tile(p, tile);
-    unit = rest / t.nb;
-    b = rest - unit * t.nb;
-    enter();
-  }
-  // To the next block; whether it continues the run.
-  ALR_DEV bool advance(const KvPass& p) {
-    if (++b < t.nb) {
-      if (__ballot_sync(~0u, t.first == b) == 0) {
-        t0 += kBlk;
-        return true;
-      }
-      enter();
-      return false;
-    }
-    b = 0;
-    if (++unit == p.n_units) {
-      unit = 0;
-      ++tile;
-      t = load_tile(p, tile);
-    }
-    enter();
-    return false;
-  }
-};
-
-// Start of worker w's stretch of `total` blocks shared by `n` workers.
-ALR_DEV long long stretch(long long total, int n, long long w) { return total * w / n; }
-
-// Every block of the kernel counts the blocks of all tiles (a thread some consecutive ones), finds its
-// workers' starts, and leaves them in `at`: (tile, blocks into the tile's items).  Returns the total.
-struct WorkerStart {
-  long long tile;
-  int rest;
-};
-
-template <int kWarps>
-ALR_DEV long long find_starts(const KvPass& p, WorkerStart* at, long long* buf) {
-  constexpr int kThreads = kWarps * 32;
-  const int tid = threadIdx.x;
-  const long long per = (p.n_tiles + kThreads - 1) / kThreads;
-  const long long a = min(tid * per, p.n_tiles), e = min(a + per, p.n_tiles);
-  long long own = 0;
-  for (long long i = a; i < e; ++i) own += tile_blocks(p, i);
-  // exclusive sums over the threads
-  const int lane = tid & 31, warp = tid >> 5;
-  const long long up = warp_scan(own);
-  if (lane == 31) buf[warp] = up;
-  __syncthreads();
-  long long before = up - own, total = 0;
-  for (int i = 0; i < kWarps; ++i) {
-    if (i < warp) before += buf[i];
-    total += buf[i];
-  }
-  before *= p.n_units;
-  own *= p.n_units;
-  total *= p.n_units;
-  const int n = int(min((long long)p.workers, total));
-  for (int w = 0; w < kWarps; ++w) {
-    const long long id = (long long)w * gridDim.x + blockIdx.x;
-    if (id >= n) break;
-    long long rest = stretch(total, n, id) - before;
-    if (rest < 0 || rest >= own) continue;
-    long long tile = a;
-    for (;; ++tile) {
-      const long long len = (long long)tile_blocks(p, tile) * p.n_units;
-      if (rest < len) break;
-      rest -= len;
-    }
-    at[w] = {tile, int(rest)};
-  }
-  __syncthreads();
-  return total;
-}
-
-// ------------------------------------------------------------------ row by row ---
-// One query over tokens [t0, t1) of a sequence, token by token: lane i holds elements i, i + 32, ... of q
-// and of the sum; (m, l, o): running maximum (log2), sum, weighted values.
-constexpr int kLaneDims = kKvMaxDim / 32;
-
-template <typename E>
-ALR_DEV void walk_tokens(const KvAttention& a, int seq, int t0, int t1, int head,
-                         const float (&q)[kLaneDims], float& m, float& l, float (&o)[kLaneDims]) {
-  const int lane = threadIdx.x & 31;
-  const E* K = static_cast<const E*>(a.c.K) + head * a.c.sh;
-  const E* V = static_cast<const E*>(a.c.V) + head * a.c.sh;
-  for (int t = t0; t < t1; ++t) {
-    const int j = t / a.c.page, pg = a.table[(long long)seq * a.cols + j];
-    if (pg < 0 || pg >= a.c.n_pages) continue;
-    const long long at = pg * a.c.sp + (t - j * a.c.page) * a.c.st;
-    float x = 0.f;
-#pragma unroll
-    for (int i = 0; i < kLaneDims; ++i)
-      if (i * 32 + lane < a.c.dim) x = fmaf(q[i], to_float(K[at + i * 32 + lane]), x);
-    x = warp_reduce(x, AddOp()) * (a.scale * kLog2e);
-    if (x == kNegInf) continue;
-    const float up = fmaxf(m, x), c = ex2(m - up), e = ex2(x - up);
-    m = up;
-    l = fmaf(l, c, e);
-#pragma unroll
-    for (int i = 0; i < kLaneDims; ++i)
-      if (i * 32 + lane < a.c.dim) o[i] = fmaf(e, to_float(V[at + i * 32 + lane]), o[i] * c);
-  }
-}
-
 // ------------------------------------------------------------------------- cores ---
 // A core holds the sums of an item's queries for a warp: load_q, zero, add (one block from the ring, with
 // each query's count of visible tokens), finish.
@@ -551,7 +367,7 @@ __global__ void __launch_bounds__(Core::kWarps * 32, 1) kv_blocks_kernel(const K
       reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
   }
   pdl_wait();
-  const long long total = find_starts<kWarps>(p, starts, buf);
+  const long long total = find_starts<kBlk, kWarps, kWarps>(p, starts, buf);
   const int n = int(min((long long)p.workers, total));
   const int id = warp * gridDim.x + blockIdx.x;
   if (id >= n) {
@@ -560,9 +376,9 @@ __global__ void __launch_bounds__(Core::kWarps * 32, 1) kv_blocks_kernel(const K
     return;
   }
   const long long begin = stretch(total, n, id), end = stretch(total, n, id + 1);
-  Cursor in;                                 // of the loads
+  Cursor<kBlk> in;                                // of the loads
   in.start(p, starts[warp].tile, starts[warp].rest);
-  Cursor at = in;                            // of the sums
+  Cursor<kBlk> at = in;                           // of the sums
 
   // page and position in it of the lane's token (lane % 16) in the next block to load
   int j = 0, off = 0, pg = -1;
@@ -777,32 +593,25 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvPass p
 }
 
 // ---------------------------------------------------------------------- launches ---
-constexpr int kMostSms = 160, kMostWorkers = 8 * kMostSms;
+constexpr int kMostWorkers = 8 * kKvMostSms;
+
+template <typename E>
+cudaError_t run_join(const KvPass& p, cudaStream_t s) {
+  return launch_pdl(kv_join_kernel<E>, dim3(p.workers), dim3(kJoinWarps * 32), 0, s, p);
+}
 
 template <typename Core>
 cudaError_t run_pass(KvPass p, int sms, cudaStream_t s) {
   constexpr int kRing = Core::kWarps * (Core::kStages * 2 * kBlk * Core::kPacks * 16 + Core::kScratch);
   static_assert(kRing <= 220 * 1024, "the rings fit an SM");
-  const int group = p.a.H / p.a.c.heads;
-  p.gs = (group + Core::kMaxQ - 1) / Core::kMaxQ;
-  p.gw = (group + p.gs - 1) / p.gs;
-  p.n_units = p.a.c.heads * p.gs;
-  p.per = int(std::min<long long>(p.part.per, p.a.N));
-  p.rows = std::min(Core::kMaxQ / p.gw, p.per);
-  p.tg = (p.per + p.rows - 1) / p.rows;
-  p.rows = (p.per + p.tg - 1) / p.tg;
-  p.n_tiles = (p.a.N + p.per - 1) / p.per * p.tg;
-  p.step_pg = kBlk / p.a.c.page;
-  p.step_tok = kBlk % p.a.c.page;
-  p.max_q = Core::kMaxQ;
-  const int grid = std::min(sms, kMostSms);
+  shape_pass(p, Core::kMaxQ, 32, kBlk);
+  const int grid = std::min(sms, kKvMostSms);
   p.workers = grid * Core::kWarps;
   const cudaError_t e = cudaFuncSetAttribute(kv_blocks_kernel<Core>,
                                              cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
   if (e != cudaSuccess) return e;
   const cudaError_t f = launch_pdl(kv_blocks_kernel<Core>, dim3(grid), dim3(Core::kWarps * 32), kRing, s, p);
-  if (f != cudaSuccess) return f;
-  return launch_pdl(kv_join_kernel<typename Core::E>, dim3(p.workers), dim3(kJoinWarps * 32), 0, s, p);
+  return f != cudaSuccess ? f : run_join<typename Core::E>(p, s);
 }
 
 template <int kDim>
@@ -814,8 +623,13 @@ cudaError_t run_f32(const KvPass& p, int sms, cudaStream_t s) {
   return run_pass<F32Core<kDim, 8>>(p, sms, s);
 }
 
-cudaError_t run_part(const KvPass& p, int sms, cudaStream_t s) {
+cudaError_t run_part(KvPass p, int sms, int* status, cudaStream_t s) {
   const int dim = p.a.c.dim;
+  const long long queries = std::min<long long>(p.part.per, p.a.N) * (p.a.H / p.a.c.heads);
+  if (p.a.c.dtype == 0 && dim <= 128 && queries > 16 && p.a.c.n_pages > 0) {
+    const cudaError_t e = launch_kv_tc(p, sms, status, s);
+    return e != cudaSuccess ? e : run_join<__nv_bfloat16>(p, s);
+  }
   if (p.a.c.dtype == 0)
     return dim <= 32 ? run_pass<Bf16Core<32>>(p, sms, s) : dim <= 64 ? run_pass<Bf16Core<64>>(p, sms, s)
            : dim <= 128 ? run_pass<Bf16Core<128>>(p, sms, s) : run_pass<Bf16Core<256>>(p, sms, s);
@@ -833,7 +647,7 @@ Layout layout(long long N, int H, int dim, bool prefix) {
   Layout y;
   size_t at = 0;
   y.parts = at;
-  at += up16(size_t(2 * kMostWorkers + 1) * 16 * (dim + 2) * sizeof(float));
+  at += up16(size_t(2 * kMostWorkers + 8) * 16 * (dim + 2) * sizeof(float));
   y.cuts = at;
   at += size_t(kMostWorkers) * sizeof(int4);
   y.pre_o = at;
@@ -862,13 +676,13 @@ cudaError_t launch_kv_attention(const KvAttention& a, int sms, int* status, cuda
     f.part = {a.prefix_seq, a.prefix_len, a.rows_per_prefix};
     f.put_o = reinterpret_cast<float*>(ws + y.pre_o);
     f.put_ml = reinterpret_cast<float*>(ws + y.pre_ml);
-    const cudaError_t e = run_part(f, sms, s);
+    const cudaError_t e = run_part(f, sms, status, s);
     if (e != cudaSuccess) return e;
     p.pre_o = f.put_o;
     p.pre_ml = f.put_ml;
   }
   p.part = {a.seq, a.len, a.rows_per_seq};
-  return run_part(p, sms, s);
+  return run_part(p, sms, status, s);
 }
 
 }  // namespace alr

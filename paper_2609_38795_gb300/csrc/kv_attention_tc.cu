@@ -1,0 +1,577 @@
+// Attention of many query rows that read the same tokens of the paged cache (a block of new tokens, rollouts
+// with a shared prefix), on the 5th-generation tensor cores.
+#include <algorithm>
+#include <cfloat>
+
+#include "launch.h"
+#include "kv_tiles.cuh"
+
+namespace alr {
+namespace {
+
+// Both products have the tokens or the elements of a value on their 128 rows and the queries on their
+// columns, so that few queries waste nothing:
+//   S^T [128 tokens, NQ] = K Q^T          (K tile and Q by rows of elements)
+//   O^T [dim, NQ]       += V^T P^T        (V tile and P by rows of tokens, both read transposed)
+// with S^T twice and O^T in tensor memory.  A thread of the softmax has one token (a lane) and half the
+// queries (columns): no sum crosses lanes until the item ends, the weights leave as 16-byte packs
+// into the shared-memory layout that the second product reads, and the running references are lagging
+// ones, in shared memory: a tile whose scores stay below reference + kLag needs one vote of the threads.
+//   Warps: 8 softmax (two groups of 4, half the queries each), 4 copy (K and V tiles of 128 tokens,
+// gathered by rows of their pages, in a ring), 1 issues products and 3 make its group whole: registers
+// move between groups of 4 (launched with 128 a thread; 2 x 168 + 2 x 88 = 4 x 128).
+constexpr int kBlk = 128;
+constexpr int kSoftWarps = 8, kCopyWarp = 8, kCopyWarps = 4, kMmaWarp = 12;
+constexpr int kWarps = 16, kThreads = kWarps * 32;
+constexpr int kSoftRegs = 168, kOtherRegs = 88;
+static_assert(2 * kSoftRegs + 2 * kOtherRegs <= 4 * 128, "the launch's registers");
+constexpr int kInfo = 8;           // tiles whose masks and flags are kept
+constexpr float kLag = 8.f;        // log2: weights of up to 2^8 relative to the reference
+constexpr float kNoRef = -FLT_MAX;
+
+template <int kNQ_, int kChunks_>
+struct Cfg {
+  static constexpr int kNQ = kNQ_, kChunks = kChunks_;     // queries; 64-element chunks of a row
+  static constexpr int kTile = kChunks * kBlk * 128;       // bytes of a K or V tile
+  static constexpr int kQBytes = kChunks * kNQ * 128;
+  static constexpr int kPBytes = (kNQ / 64) * kBlk * 128;
+  static constexpr int kQBufs = 2, kPBufs = kNQ == 128 && kChunks == 2 ? 1 : 2;
+  static constexpr int kSlots = kChunks == 1 ? 8 : kNQ == 128 ? 4 : 5;
+  static constexpr int kHalf = kNQ / 2;                    // queries of a softmax group
+  static constexpr int kParts = kHalf / 32;                // 32 columns at a time
+  static constexpr int kCols = kNQ == 128 ? 512 : 256;     // tensor memory: S^T, S^T, O^T
+  static constexpr size_t kBig = size_t(kSlots) * kTile + kQBufs * kQBytes + kPBufs * kPBytes;
+};
+
+struct KvMisc {
+  uint64_t full[8], empty[8], q_empty[2], s_full[2], s_empty[2], p_full[2], pv_done[2], drain;
+  uint32_t there[kInfo][kCopyWarps];      // tokens of a tile whose page exists
+  uint32_t info[kInfo];                   // 1: first of its item here, 2: last
+  uint32_t tmem;
+  int abort_word;
+  uint32_t bad[4];                        // queries with a value that is not finite
+  WorkerStart start;
+  long long buf[kWarps];
+};
+
+template <class C>
+struct KvSmem {
+  KvMisc m;
+  float top[kSoftWarps][32];              // a slow tile's maxima
+  float ref[C::kNQ];                      // references (log2)
+  int vis[C::kNQ];                        // tokens of the run that a query sees
+};
+
+template <class C>
+constexpr size_t smem_bytes() { return C::kBig + sizeof(KvSmem<C>); }
+
+ALR_DEV void cp_async16_or_zero(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0)
+               : "memory");
+}
+// Arrive on `bar` once all copies this thread issued so far have landed.
+ALR_DEV void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+ALR_DEV bool any_of(int id, int threads, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r) : "r"(x ? 1u : 0u), "r"(id), "r"(threads) : "memory");
+  return r != 0;
+}
+ALR_DEV void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+      "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]),
+      "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+      : "memory");
+}
+ALR_DEV void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// A wait that runs out is recorded, and every role runs on to the end of its loop (on data that no one
+// will use) with all other waits passed over, so that no barrier is left half full.
+ALR_DEV void wait_on(uint64_t* bar, uint32_t n, const AbortFlag& ab) {   // for completion n (from 0)
+  if (mbar_try_wait(bar, n & 1)) return;
+  if (*ab.smem) return;
+  mbar_wait(bar, n & 1, ab);
+}
+
+ALR_DEV uint32_t bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// Group of the ring that holds tile i's keys, values: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1).
+ALR_DEV long long k_group(long long i) { return i == 0 ? 0 : 2 * i - 1; }
+ALR_DEV long long v_group(long long i, long long n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; }
+
+template <class C>
+__global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int* status) {
+  using E = __nv_bfloat16;
+  constexpr int kNQ = C::kNQ, kSlots = C::kSlots;
+  extern __shared__ __align__(1024) uint8_t tc_smem[];
+  uint8_t* ring = tc_smem;
+  uint8_t* qs = ring + kSlots * C::kTile;
+  uint8_t* ps = qs + C::kQBufs * C::kQBytes;
+  KvSmem<C>& sm = *reinterpret_cast<KvSmem<C>*>(ps + C::kPBufs * C::kPBytes);
+  KvMisc& mi = sm.m;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const KvAttention& a = p.a;
+  const int dim = a.c.dim;
+  const AbortFlag ab{&mi.abort_word, status};
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(&mi.full[i], kCopyWarps * 33);   // every copying thread's copies, and its warp's flags
+      mbar_init(&mi.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&mi.q_empty[i], 1);
+      mbar_init(&mi.s_full[i], 1);
+      mbar_init(&mi.s_empty[i], kSoftWarps);
+      mbar_init(&mi.p_full[i], kSoftWarps);
+      mbar_init(&mi.pv_done[i], 1);
+    }
+    mbar_init(&mi.drain, 1);
+    mi.abort_word = 0;
+    for (int i = 0; i < 4; ++i) mi.bad[i] = 0;
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(&mi.tmem, C::kCols);
+    tmem_relinquish();
+  }
+  if (dim != C::kChunks * 64) {              // what lies past a row's end is never copied: zeros
+    uint4* z = reinterpret_cast<uint4*>(ring);
+    for (int i = threadIdx.x; i < (kSlots * C::kTile + C::kQBufs * C::kQBytes) / 16; i += kThreads)
+      z[i] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
+  tc_fence_before();
+  pdl_wait();
+  const long long total = find_starts<kBlk, kWarps, 1>(p, &mi.start, mi.buf);   // barriers within
+  tc_fence_after();
+  const uint32_t tmem = mi.tmem;
+  const int n_workers = int(min((long long)p.workers, total)), id = blockIdx.x;
+  const long long begin = id < n_workers ? stretch(total, n_workers, id) : 0;
+  const long long end = id < n_workers ? stretch(total, n_workers, id + 1) : 0, count = end - begin;
+  if (threadIdx.x == 0 && count == 0 && id < p.workers) p.cuts[id] = make_int4(0, 0, 0, 0);
+
+  if (warp >= kCopyWarp && warp < kMmaWarp) {
+    // ---- copies
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    const int w = warp - kCopyWarp;
+    constexpr int kRowsAt = 4 / C::kChunks, kPer = 32 / kRowsAt;     // rows of one copy instruction
+    const int pack = lane & (8 * C::kChunks - 1), sub = lane / (8 * C::kChunks);
+    const bool has_pack = pack * 8 < dim;
+    // place of (row r of the tile, this pack): the low bits of r swizzle the packs of 128 bytes
+    const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(qs);
+    const auto place = [&](int r, int rows) {
+      return uint32_t((pack >> 3) * rows * 128 + r * 128 + (((pack & 7) ^ (r & 7)) << 4));
+    };
+    Cursor<kBlk> in;
+    if (count > 0) in.start(p, mi.start.tile, mi.start.rest);
+    int j = 0, off = 0, pg = -1;
+    const auto look_up = [&](bool runs_on) {
+      if (runs_on) {
+        j += p.step_pg;
+        off += p.step_tok;
+        if (off >= a.c.page) off -= a.c.page, ++j;
+      } else {
+        const int tok = in.t0 + w * 32 + lane;
+        j = tok / a.c.page;
+        off = tok - j * a.c.page;
+      }
+      pg = in.t0 + w * 32 + lane < in.most ? a.table[(long long)in.seq * a.cols + j] : -1;
+    };
+    if (count > 0) look_up(false);
+    long long group = 0, item = -1;
+    const auto copy = [&](const void* cache, int kv, long long row, uint32_t all) {
+      const int slot = int(group % kSlots);
+      if (group >= kSlots) wait_on(&mi.empty[slot], uint32_t(group / kSlots - 1), ab);
+      const E* base = static_cast<const E*>(cache) + kv * a.c.sh + pack * 8;
+      const uint32_t dst = ring_at + slot * C::kTile;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int r = i * kRowsAt + sub;
+        const long long from = __shfl_sync(~0u, row, r);
+        if (has_pack) cp_async16_or_zero(dst + place(w * 32 + r, kBlk), base + from, all >> r & 1);
+      }
+      cp_async_arrive(&mi.full[slot]);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&mi.full[slot]);
+      ++group;
+    };
+    long long row_v = 0;
+    uint32_t all_v = 0;
+    int kv_v = 0;
+    for (long long i = 0; i < count; ++i) {
+      const bool first = i == 0 || in.b == 0, last = i + 1 == count || in.b + 1 == in.t.nb;
+      const bool there = pg >= 0 && pg < a.c.n_pages;
+      const uint32_t all = __ballot_sync(~0u, there);
+      const long long row = there ? pg * a.c.sp + off * a.c.st : 0;
+      const int kv = in.unit / p.gs;
+      // flags and masks of tile i: read after its keys have landed; tile i - kInfo is long done with
+      // (its values' slot has been refilled since)
+      if (lane == 0) {
+        mi.there[i % kInfo][w] = all;
+        if (w == 0) mi.info[i % kInfo] = (first ? 1u : 0u) | (last ? 2u : 0u);
+      }
+      if (first) {
+        ++item;
+        const int buf = int(item % C::kQBufs);
+        if (item >= C::kQBufs) wait_on(&mi.q_empty[buf], uint32_t(item / C::kQBufs - 1), ab);
+        long long row0;
+        const int n_rows = max(tile_rows(p, in.tile, row0), 0);
+        const int group_q = a.H / a.c.heads, slice = (in.unit - kv * p.gs) * p.gw;
+        const int gw = min(p.gw, group_q - slice), h0 = kv * group_q + slice;
+        const uint32_t dst = q_at + buf * C::kQBytes;
+        for (int q = w * kRowsAt + sub; q < kNQ; q += kCopyWarps * kRowsAt) {
+          const int r = q / p.gw, h = q - r * p.gw;
+          const bool ok = r < n_rows && h < gw;
+          const E* src = static_cast<const E*>(a.Q) + (ok ? (row0 + r) * a.ldq + (long long)(h0 + h) * dim : 0);
+          if (has_pack) cp_async16_or_zero(dst + place(q, kNQ), src + pack * 8, ok);
+        }
+      }
+      copy(a.c.K, kv, row, all);
+      if (i > 0) copy(a.c.V, kv_v, row_v, all_v);
+      row_v = row;
+      all_v = all;
+      kv_v = kv;
+      if (i + 1 < count) look_up(in.advance(p));
+    }
+    if (count > 0) copy(a.c.V, kv_v, row_v, all_v);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp >= kMmaWarp) {
+    // ---- products
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == kMmaWarp && lane == 0 && count > 0) {
+      constexpr uint32_t i_s = idesc_make(false, 128, kNQ, false, false);
+      constexpr uint32_t i_o = idesc_make(false, 128, kNQ, true, true);
+      const int n_k = (dim + 15) / 16;
+      const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(qs), p_at = smem_u32(ps);
+      long long item = -1;
+      uint32_t prev = 0;
+      const auto values = [&](long long i, uint32_t info) {
+        const long long g = v_group(i, count);
+        const int slot = int(g % kSlots), pb = int(i % C::kPBufs);
+        wait_on(&mi.full[slot], uint32_t(g / kSlots), ab);
+        wait_on(&mi.p_full[pb], uint32_t(i / C::kPBufs), ab);
+        fence_proxy_async_smem();
+        tc_fence_after();
+        const uint32_t va = ring_at + slot * C::kTile, pa = p_at + pb * C::kPBytes;
+#pragma unroll
+        for (int k = 0; k < kBlk / 16; ++k)
+          // dim <= 64: rows 64 to 127 of the result come from whatever lies behind the tile, unused
+          mma_issue<false>(tmem + 2 * kNQ, sdesc_sw128(va + k * 2048, kBlk * 128, 1024),
+                           sdesc_sw128(pa + k * 2048, kBlk * 128, 1024), i_o, !(info & 1) || k > 0);
+        mma_commit(&mi.empty[slot]);
+        mma_commit(&mi.pv_done[pb]);
+      };
+      for (long long i = 0; i < count; ++i) {
+        const long long g = k_group(i);
+        const int slot = int(g % kSlots), sb = int(i & 1);
+        wait_on(&mi.full[slot], uint32_t(g / kSlots), ab);
+        fence_proxy_async_smem();
+        const uint32_t info = mi.info[i % kInfo];
+        if (info & 1) ++item;
+        const int buf = int(item % C::kQBufs);
+        if (i >= 2) wait_on(&mi.s_empty[sb], uint32_t(i / 2 - 1), ab);
+        tc_fence_after();
+        const uint32_t ka = ring_at + slot * C::kTile, qa = q_at + buf * C::kQBytes;
+        for (int k = 0; k < n_k; ++k)
+          mma_issue<false>(tmem + sb * kNQ, sdesc_sw128(ka + (k >> 2) * (kBlk * 128) + (k & 3) * 32, 16, 1024),
+                           sdesc_sw128(qa + (k >> 2) * (kNQ * 128) + (k & 3) * 32, 16, 1024), i_s, k > 0);
+        mma_commit(&mi.empty[slot]);
+        mma_commit(&mi.s_full[sb]);
+        if (info & 2) mma_commit(&mi.q_empty[buf]);
+        if (i > 0) values(i - 1, prev);
+        prev = info;
+      }
+      values(count - 1, prev);
+      mma_commit(&mi.drain);                 // nothing is in flight when the memory is given back
+      mbar_wait_drain(&mi.drain, 0);
+    }
+    __syncwarp();
+  } else {
+    // ---- softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    constexpr int kHalf = C::kHalf, kParts = C::kParts;
+    const int wg = warp >> 2, wq = warp & 3, bar = 1 + wg, tid = threadIdx.x & 127;
+    const uint32_t lanes = tmem + (uint32_t(wq * 32) << 16);
+    const int tok = tid, q0 = wg * kHalf;
+    const float c = a.scale * kLog2e;
+    float l[kHalf];
+    Cursor<kBlk> at;
+    if (count > 0) at.start(p, mi.start.tile, mi.start.rest);
+    float (*lsum)[kHalf] = reinterpret_cast<float (*)[kHalf]>(ps);               // at an item's end
+    KvRowOut* outs = reinterpret_cast<KvRowOut*>(ps + kSoftWarps * kHalf * sizeof(float));
+    int4 cut = make_int4(0, 0, 0, 0);
+    long long i = 0;
+    while (i < count) {
+      long long row0;
+      const int n_rows = max(tile_rows(p, at.tile, row0), 0);
+      const int group_q = a.H / a.c.heads, kv = at.unit / p.gs, slice = (at.unit - kv * p.gs) * p.gw;
+      const int gw = min(p.gw, group_q - slice), h0 = kv * group_q + slice, n_q = n_rows * p.gw;
+      const Tile tile = at.t;
+      const long long tile_id = at.tile;
+      const int unit = at.unit, b0 = at.b, b1 = int(min((long long)tile.nb, b0 + (count - i)));
+      const long long i0 = i;
+      if (tid < kHalf) sm.ref[q0 + tid] = kNoRef;
+#pragma unroll
+      for (int k = 0; k < kHalf; ++k) l[k] = 0.f;
+      int run = -2, least = 0;
+      for (int b = b0; b < b1; ++b, ++i) {
+        if (at.lead != run) {
+          // tokens that the queries see of the run
+          run = at.lead;
+          const int see = run >= 0 && tile.lead == run ? tile.len : 0;
+          least = warp_min(lane < n_rows ? see : INT_MAX);
+          named_bar_sync(bar, 128);
+          if (wq == 0)
+            for (int k = 0; k < kHalf; k += 32) {
+              const int q = q0 + k + lane, v = __shfl_sync(~0u, see, (q / p.gw) & 31);
+              sm.vis[q] = q < n_q ? v : INT_MAX;
+            }
+          named_bar_sync(bar, 128);
+        }
+        const int sb = int(i & 1), pb = int(i % C::kPBufs);
+        wait_on(&mi.s_full[sb], uint32_t(i / 2), ab);
+        tc_fence_after();
+        const uint32_t* there = mi.there[i % kInfo];
+        const bool here = (there[wq] >> lane & 1) != 0;
+        const int pos = at.t0 + tok;
+        const bool plain = least - at.t0 >= kBlk && (there[0] & there[1] & there[2] & there[3]) == ~0u;
+        const uint32_t s_at = lanes + sb * kNQ + q0, o_at = lanes + 2 * kNQ + q0;
+        uint8_t* prow = ps + pb * C::kPBytes + tok * 128;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+          uint32_t s[32];
+          float y[32];
+          tmem_ld32(s_at + part * 32, s);
+          tmem_ld_wait();
+          reg_fence(s);
+          const float* ref = sm.ref + q0 + part * 32;
+          float t = kNegInf;
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) {
+            const float4 r = *reinterpret_cast<const float4*>(ref + k);
+            y[k] = fmaf(__uint_as_float(s[k]), c, -r.x);
+            y[k + 1] = fmaf(__uint_as_float(s[k + 1]), c, -r.y);
+            y[k + 2] = fmaf(__uint_as_float(s[k + 2]), c, -r.z);
+            y[k + 3] = fmaf(__uint_as_float(s[k + 3]), c, -r.w);
+          }
+          const auto mask = [&](float (&v)[32]) {
+            const int* vis = sm.vis + q0 + part * 32;
+#pragma unroll
+            for (int k = 0; k < 32; k += 4) {
+              const int4 r = *reinterpret_cast<const int4*>(vis + k);
+              v[k] = here && pos < r.x ? v[k] : kNegInf;
+              v[k + 1] = here && pos < r.y ? v[k + 1] : kNegInf;
+              v[k + 2] = here && pos < r.z ? v[k + 2] : kNegInf;
+              v[k + 3] = here && pos < r.w ? v[k + 3] : kNegInf;
+            }
+          };
+          if (!plain) mask(y);
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) t = max3(t, y[k], y[k + 1]);
+          if (any_of(bar, 128, t > kLag)) {
+            // a reference moves: maxima over the tile, the sums so far scaled
+            tmem_ld32(s_at + part * 32, s);
+            tmem_ld_wait();
+            reg_fence(s);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) y[k] = __uint_as_float(s[k]) * c;
+            if (!plain) mask(y);
+            float top = kNegInf;
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              const float m = warp_max(y[k]);
+              if (lane == k) top = m;
+            }
+            sm.top[warp][lane] = top;
+            named_bar_sync(bar, 128);
+            const float old = ref[lane];
+            float up = old;
+            for (int k = 0; k < 4; ++k) up = fmaxf(up, sm.top[wg * 4 + k][lane]);
+            const float f = old == up ? 1.f : ex2(old - up);
+            named_bar_sync(bar, 128);
+            if (wq == 0) sm.ref[q0 + part * 32 + lane] = up;
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              y[k] -= __shfl_sync(~0u, up, k);
+              l[part * 32 + k] *= __shfl_sync(~0u, f, k);
+            }
+            if (i > i0) {
+              wait_on(&mi.pv_done[(i - 1) % C::kPBufs], uint32_t((i - 1) / C::kPBufs), ab);
+              tc_fence_after();
+              tmem_ld32(o_at + part * 32, s);
+              tmem_ld_wait();
+              reg_fence(s);
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                s[k] = __float_as_uint(__uint_as_float(s[k]) * __shfl_sync(~0u, f, k));
+              tmem_st32(o_at + part * 32, s);
+              tmem_st_wait();
+            }
+            named_bar_sync(bar, 128);
+          }
+          // this buffer's last product
+          if (part == 0 && i >= C::kPBufs)
+            wait_on(&mi.pv_done[pb], uint32_t(i / C::kPBufs - 1), ab);
+#pragma unroll
+          for (int k = 0; k < 32; k += 8) {
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+              const float u = ex2(y[k + e]), v = ex2(y[k + e + 1]);
+              l[part * 32 + k + e] += u;
+              l[part * 32 + k + e + 1] += v;
+              x[e / 2] = bf16x2(u, v);   // the product's only operand type: off by 2^-8, l is not
+            }
+            const int q = q0 + part * 32 + k;
+            *reinterpret_cast<uint4*>(prow + (q >> 6) * (kBlk * 128) + ((((q & 63) >> 3) ^ (tok & 7)) << 4)) =
+                make_uint4(x[0], x[1], x[2], x[3]);
+          }
+        }
+        tc_fence_before();
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&mi.s_empty[sb]);
+          mbar_arrive(&mi.p_full[pb]);
+        }
+        if (i + 1 < count) at.advance(p);
+      }
+      // ---- the item's results
+      wait_on(&mi.pv_done[(i - 1) % C::kPBufs], uint32_t((i - 1) / C::kPBufs), ab);
+      tc_fence_after();
+      named_bar_sync(3, 256);                // both groups are past their last weights
+      // sums over the warp's tokens: lane k ends with column k's
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) {
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) {
+          const bool upper = (lane & off) != 0;
+#pragma unroll
+          for (int k = 0; k < off; ++k) {
+            float& lo = l[part * 32 + k];
+            const float hi = l[part * 32 + k + off];
+            const float give = upper ? lo : hi, keep = upper ? hi : lo;
+            lo = keep + __shfl_xor_sync(~0u, give, off);
+          }
+        }
+        lsum[warp][part * 32 + lane] = l[part * 32];
+      }
+      named_bar_sync(bar, 128);
+      const bool whole = b0 == 0 && b1 == tile.nb, opens = b0 == 0 && b1 < tile.nb;
+      const long long part_id = 2ll * id + (opens ? 1 : 0);
+      const auto out = [&](int q, int r, float m, float s, bool writer) {
+        return whole ? row_out(p, row0 + r, h0 + q - r * p.gw, m, s, writer)
+                     : part_out(p, part_id, q, m, s, writer);
+      };
+      if (tid < kHalf) {
+        const int q = q0 + tid, r = q / p.gw;
+        float s = 0.f;
+        for (int k = 0; k < 4; ++k) s += lsum[wg * 4 + k][tid];
+        KvRowOut o = {0.f, 0.f, nullptr, nullptr, nullptr};
+        if (q < n_q && q - r * p.gw < gw) o = out(q, r, s == 0.f ? kNegInf : sm.ref[q], s, true);
+        if (!(s - s == 0.f)) atomicOr(&mi.bad[q >> 5], 1u << (q & 31));
+        outs[q] = o;
+      }
+      named_bar_sync(bar, 128);
+      const int d = wq * 32 + lane;
+#pragma unroll 1
+      for (int part = 0; part < kParts; ++part) {
+        if (q0 + part * 32 >= n_q) break;
+        uint32_t s[32];
+        tmem_ld32(lanes + 2 * kNQ + q0 + part * 32, s);
+        tmem_ld_wait();
+        reg_fence(s);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          const int q = q0 + part * 32 + k;
+          const KvRowOut& o = outs[q];
+          const float v[1] = {__uint_as_float(s[k])};
+          if (q < n_q && d < dim && (o.dst != nullptr || o.dst_f != nullptr)) {
+            put<E, 1>(o, d, v);
+            if (!(v[0] - v[0] == 0.f)) atomicOr(&mi.bad[q >> 5], 1u << (q & 31));
+          }
+        }
+      }
+      tc_fence_before();
+      named_bar_sync(3, 256);
+      if (n_rows > 1 && (mi.bad[0] | mi.bad[1] | mi.bad[2] | mi.bad[3]) != 0) {
+        // Weights of 0 times a value that is not finite: such a value may lie in a token that the
+        // query does not see but another of the tile does.  Its tokens again, one by one.
+        for (int q = warp; q < n_q; q += kSoftWarps) {
+          const int r = q / p.gw;
+          if (!(mi.bad[q >> 5] >> (q & 31) & 1) || q - r * p.gw >= gw) continue;
+          float x[kLaneDims], o[kLaneDims] = {}, m = kNegInf, sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < kLaneDims; ++e)
+            x[e] = e * 32 + lane < dim
+                       ? to_float(static_cast<const E*>(a.Q)[(row0 + r) * a.ldq + (long long)(h0 + q - r * p.gw) * dim + e * 32 + lane])
+                       : 0.f;
+          const int lead = __shfl_sync(~0u, tile.lead, r), len = __shfl_sync(~0u, tile.len, r);
+          const int seq = __shfl_sync(~0u, tile.seq, r), first = __shfl_sync(~0u, tile.first, max(lead, 0));
+          const long long t0 = (long long)(b0 - first) * kBlk, t1 = (long long)(b1 - first) * kBlk;
+          if (len > 0)
+            walk_tokens<E>(a, seq, int(max(t0, 0ll)), int(min(t1, (long long)len)), kv, x, m, sum, o);
+          const KvRowOut to = out(q, r, m, sum, lane == 0);
+#pragma unroll
+          for (int e = 0; e < kLaneDims; ++e) {
+            const float v[1] = {o[e]};
+            if (e * 32 + lane < dim) put<E, 1>(to, e * 32 + lane, v);
+          }
+        }
+        named_bar_sync(3, 256);
+        if (threadIdx.x < 4) mi.bad[threadIdx.x] = 0;
+      } else if (n_rows <= 1) {
+        named_bar_sync(3, 256);
+        if (threadIdx.x < 4) mi.bad[threadIdx.x] = 0;
+      }
+      if (opens) {
+        // the workers up to the one with the item's last block
+        const long long item_end = end + (tile.nb - b1);
+        cut = make_int4(int(tile_id), unit, int((item_end * n_workers + total - 1) / total) - 1 - id + 1, 0);
+      }
+    }
+    if (threadIdx.x == 0 && count > 0) p.cuts[id] = cut;
+  }
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tmem_dealloc(tmem, C::kCols);
+  pdl_release();
+}
+
+template <class C>
+cudaError_t run_tc(KvPass& p, int sms, int* status, cudaStream_t s) {
+  static_assert(smem_bytes<C>() <= 227 * 1024, "fits an SM");
+  static_assert(kSoftWarps * C::kHalf * 4 + C::kNQ * sizeof(KvRowOut) <= C::kPBytes * C::kPBufs,
+                "an item's end reuses the weights' place");
+  shape_pass(p, C::kNQ, 32, kBlk);
+  p.workers = std::min(sms, kKvMostSms);
+  const cudaError_t e = cudaFuncSetAttribute(
+      kv_tc_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem_bytes<C>()));
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kv_tc_kernel<C>, dim3(p.workers), dim3(kThreads), smem_bytes<C>(), s, p, status);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_tc(KvPass& p, int sms, int* status, cudaStream_t s) {
+  const int group = p.a.H / p.a.c.heads;
+  const long long queries = std::min<long long>(std::min<long long>(p.part.per, p.a.N), 32) * group;
+  if (p.a.c.dim <= 64)
+    return queries <= 64 ? run_tc<Cfg<64, 1>>(p, sms, status, s) : run_tc<Cfg<128, 1>>(p, sms, status, s);
+  return queries <= 64 ? run_tc<Cfg<64, 2>>(p, sms, status, s) : run_tc<Cfg<128, 2>>(p, sms, status, s);
+}
+
+}  // namespace alr

@@ -132,4 +132,215 @@ ALR_DEV void join_state(float& m, float& l, float& c, float& c2, float m2, float
   m = top;
 }
 
+// ---------------------------------------------------------------------- schedule ---
+// First row and row count of a tile.
+ALR_DEV int tile_rows(const KvPass& p, long long tile, long long& row0) {
+  const long long g = tile / p.tg;
+  const int i = int(tile - g * p.tg);
+  row0 = g * p.per + (long long)i * p.rows;
+  return int(min((long long)min(p.rows, p.per - i * p.rows), p.a.N - row0));
+}
+
+template <int kBlk>
+ALR_DEV int blocks_of(int tokens) { return tokens / kBlk + (tokens % kBlk != 0); }
+
+// Blocks of a tile, counted by one thread.
+template <int kBlk>
+ALR_DEV int tile_blocks(const KvPass& p, long long tile) {
+  long long row0;
+  const int n = tile_rows(p, tile, row0);
+  int nb = 0, cur = 0, most = 0;
+  for (int i = 0; i < n; ++i) {
+    const int s = part_seq(p.part, row0 + i), len = part_len(p.a, p.part, row0 + i, s);
+    if (len == 0) continue;
+    if (most > 0 && s != cur) {
+      nb += blocks_of<kBlk>(most);
+      most = 0;
+    }
+    cur = s;
+    most = max(most, len);
+  }
+  return max(nb + blocks_of<kBlk>(most), 1);
+}
+
+// A tile's runs, held by a warp: lane i has row i.
+struct Tile {
+  int seq, len;       // of the row
+  int lead;           // first lane of the row's run (-1: before any)
+  int first;          // of a run's first lane: its first block; INT_MAX elsewhere
+  int most;           // ... and its longest row
+  int nb;             // blocks (all lanes)
+};
+
+template <int kBlk>
+ALR_DEV Tile load_tile(const KvPass& p, long long tile) {
+  const int lane = threadIdx.x & 31;
+  long long row0;
+  const int n = tile_rows(p, tile, row0);
+  Tile t;
+  t.seq = lane < n ? part_seq(p.part, row0 + lane) : -1;
+  t.len = lane < n ? part_len(p.a, p.part, row0 + lane, t.seq) : 0;
+  const uint32_t some = __ballot_sync(~0u, t.len > 0), up_to = (2u << lane) - 1;
+  const uint32_t before = some & (up_to >> 1);
+  const int prev = __shfl_sync(~0u, t.seq, before != 0 ? 31 - __clz(before) : 0);
+  const uint32_t leads = __ballot_sync(~0u, t.len > 0 && (before == 0 || prev != t.seq));
+  t.lead = (leads & up_to) != 0 ? 31 - __clz(leads & up_to) : -1;
+  t.most = t.len;
+  for (int off = 1; off < 32; off <<= 1) {
+    const int m = __shfl_down_sync(~0u, t.most, off), l = __shfl_down_sync(~0u, t.lead, off);
+    if (lane + off < 32 && l == t.lead) t.most = max(t.most, m);
+  }
+  const bool lead = (leads >> lane & 1) != 0;
+  const int nb = lead ? blocks_of<kBlk>(t.most) : 0, sum = warp_scan(nb);
+  t.first = lead ? sum - nb : INT_MAX;
+  t.nb = max(__shfl_sync(~0u, sum, 31), 1);
+  return t;
+}
+
+// Position of a worker in the line of blocks.  The loads run ahead of the sums, so a worker has two.
+template <int kBlk>
+struct Cursor {
+  Tile t;
+  long long tile;
+  int unit, b;
+  int lead, seq, most, t0;      // the run's first lane, sequence, tokens; the block's first token
+
+  ALR_DEV void enter() {
+    const uint32_t m = __ballot_sync(~0u, t.first <= b);
+    lead = m != 0 ? 31 - __clz(m) : -1;
+    const int from = max(lead, 0);
+    seq = __shfl_sync(~0u, t.seq, from);
+    most = lead < 0 ? 0 : __shfl_sync(~0u, t.most, from);
+    t0 = lead < 0 ? 0 : (b - __shfl_sync(~0u, t.first, from)) * kBlk;
+  }
+  // rest: blocks into the tile's items
+  ALR_DEV void start(const KvPass& p, long long tile_, long long rest) {
+    tile = tile_;
+    t = load_tile<kBlk>(p, tile);
+    unit = int(rest / t.nb);
+    b = int(rest - (long long)unit * t.nb);
+    enter();
+  }
+  // To the next block; whether it continues the run.
+  ALR_DEV bool advance(const KvPass& p) {
+    if (++b < t.nb) {
+      if (__ballot_sync(~0u, t.first == b) == 0) {
+        t0 += kBlk;
+        return true;
+      }
+      enter();
+      return false;
+    }
+    b = 0;
+    if (++unit == p.n_units) {
+      unit = 0;
+      ++tile;
+      t = load_tile<kBlk>(p, tile);
+    }
+    enter();
+    return false;
+  }
+};
+
+// Start of worker w's stretch of `total` blocks shared by `n` workers.
+ALR_DEV long long stretch(long long total, int n, long long w) { return total * w / n; }
+
+// Every block of the kernel counts the blocks of all tiles (a thread some consecutive ones), finds its
+// workers' starts, and leaves them in `at`: (tile, blocks into the tile's items).  Returns the total.
+struct WorkerStart {
+  long long tile, rest;
+};
+
+template <int kBlk, int kWarps, int kWorkers>
+ALR_DEV long long find_starts(const KvPass& p, WorkerStart* at, long long* buf) {
+  constexpr int kThreads = kWarps * 32;
+  const int tid = threadIdx.x;
+  const long long per = (p.n_tiles + kThreads - 1) / kThreads;
+  const long long a = min((long long)tid * per, p.n_tiles), e = min(a + per, p.n_tiles);
+  long long own = 0;
+  for (long long i = a; i < e; ++i) own += tile_blocks<kBlk>(p, i);
+  // exclusive sums over the threads
+  const int lane = tid & 31, warp = tid >> 5;
+  const long long up = warp_scan(own);
+  if (lane == 31) buf[warp] = up;
+  __syncthreads();
+  long long before = up - own, total = 0;
+  for (int i = 0; i < kWarps; ++i) {
+    if (i < warp) before += buf[i];
+    total += buf[i];
+  }
+  before *= p.n_units;
+  own *= p.n_units;
+  total *= p.n_units;
+  const int n = int(min((long long)p.workers, total));
+  for (int w = 0; w < kWorkers; ++w) {
+    const long long id = (long long)w * gridDim.x + blockIdx.x;
+    if (id >= n) break;
+    long long rest = stretch(total, n, id) - before;
+    if (rest < 0 || rest >= own) continue;
+    long long tile = a;
+    for (;; ++tile) {
+      const long long len = (long long)tile_blocks<kBlk>(p, tile) * p.n_units;
+      if (rest < len) break;
+      rest -= len;
+    }
+    at[w] = {tile, rest};
+  }
+  __syncthreads();
+  return total;
+}
+
+// ------------------------------------------------------------------ row by row ---
+// One query over tokens [t0, t1) of a sequence, token by token: lane i holds elements i, i + 32, ... of q
+// and of the sum; (m, l, o): running maximum (log2), sum, weighted values.
+constexpr int kLaneDims = kKvMaxDim / 32;
+
+template <typename E>
+ALR_DEV void walk_tokens(const KvAttention& a, int seq, int t0, int t1, int head,
+                         const float (&q)[kLaneDims], float& m, float& l, float (&o)[kLaneDims]) {
+  const int lane = threadIdx.x & 31;
+  const E* K = static_cast<const E*>(a.c.K) + head * a.c.sh;
+  const E* V = static_cast<const E*>(a.c.V) + head * a.c.sh;
+  for (int t = t0; t < t1; ++t) {
+    const int j = t / a.c.page, pg = a.table[(long long)seq * a.cols + j];
+    if (pg < 0 || pg >= a.c.n_pages) continue;
+    const long long at = pg * a.c.sp + (t - j * a.c.page) * a.c.st;
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < kLaneDims; ++i)
+      if (i * 32 + lane < a.c.dim) x = fmaf(q[i], to_float(K[at + i * 32 + lane]), x);
+    x = warp_reduce(x, AddOp()) * (a.scale * kLog2e);
+    if (x == kNegInf) continue;
+    const float up = fmaxf(m, x), c = ex2(m - up), e = ex2(x - up);
+    m = up;
+    l = fmaf(l, c, e);
+#pragma unroll
+    for (int i = 0; i < kLaneDims; ++i)
+      if (i * 32 + lane < a.c.dim) o[i] = fmaf(e, to_float(V[at + i * 32 + lane]), o[i] * c);
+  }
+}
+
+// Units, tiles and steps of a pass whose items have at most max_q queries in max_rows rows.
+inline void shape_pass(KvPass& p, int max_q, int max_rows, int blk) {
+  const int group = p.a.H / p.a.c.heads;
+  const auto least = [](long long a, long long b) { return a < b ? a : b; };
+  p.gs = (group + max_q - 1) / max_q;
+  p.gw = (group + p.gs - 1) / p.gs;
+  p.n_units = p.a.c.heads * p.gs;
+  p.per = int(least(p.part.per, p.a.N));
+  p.rows = int(least(least(max_q / p.gw, max_rows), p.per));
+  p.tg = (p.per + p.rows - 1) / p.rows;
+  p.rows = (p.per + p.tg - 1) / p.tg;
+  p.n_tiles = (p.a.N + p.per - 1) / p.per * p.tg;
+  p.step_pg = blk / p.a.c.page;
+  p.step_tok = blk % p.a.c.page;
+  p.max_q = max_q;
+}
+
+constexpr int kKvMostSms = 160;
+
+// kv_attention_tc.cu: a pass over tiles of up to 32 rows and 128 queries (bf16, dim <= 128, n_pages > 0);
+// p.part is set, the rest of the pass's shape is filled in.
+cudaError_t launch_kv_tc(KvPass& p, int sms, int* status, cudaStream_t s);
+
 }  // namespace alr
