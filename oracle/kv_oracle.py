@@ -56,7 +56,7 @@ def tokens_of(table, n_pages, page, seq, length):
 def attention(Q, K, V, table, parts, scale):
     """Q [N, H, D], K, V [n_pages, page, heads, D] fp64; parts: (seq, len) arrays by row.  Returns out,
     lse and for error bounds: size (sum of the weights times |v|), reach (largest sum of |q k| scale
-    over a row's tokens), n (tokens of the row)."""
+    over the tokens that have a weight), n (tokens of the row)."""
     N, H, D = Q.shape
     n_pages, page, heads, _ = K.shape
     g = H // heads
@@ -75,8 +75,8 @@ def attention(Q, K, V, table, parts, scale):
             m = x.max()
             if m == -np.inf:
                 continue
-            reach[r, h] = abs(scale) * np.max(np.abs(kh[x > -np.inf]) @ np.abs(Q[r, h]))
             e = np.exp(x - m)
+            reach[r, h] = abs(scale) * np.max(np.abs(kh[e > 0]) @ np.abs(Q[r, h]))
             out[r, h], size[r, h] = e @ vh / e.sum(), e @ np.abs(vh) / e.sum()
             lse[r, h] = m + np.log(e.sum())
     return out, lse, size, reach, n

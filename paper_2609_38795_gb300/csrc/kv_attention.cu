@@ -105,7 +105,7 @@ struct Bf16Core {
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[n][e] *= c;
+      for (int e = 0; e < 4; ++e) s[n][e] = __fmul_rn(s[n][e], c);   // never an fma with the reference
     if (!__all_sync(~0u, lim[0] >= kBlk && lim[1] >= kBlk && there == 0xffffu)) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
@@ -255,7 +255,7 @@ struct F32Core {
     float top[kQ];
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
-      s[i] = (s[i] + __shfl_xor_sync(~0u, s[i], 16)) * c;
+      s[i] = __fmul_rn(s[i] + __shfl_xor_sync(~0u, s[i], 16), c);    // never an fma with the reference
       if (tok >= lim[i] || !here) s[i] = kNegInf;
       top[i] = warp_max(s[i]);
       moves |= top[i] > m[i] + kLag;
@@ -626,7 +626,7 @@ cudaError_t run_f32(const KvPass& p, int sms, cudaStream_t s) {
 cudaError_t run_part(KvPass p, int sms, int* status, cudaStream_t s) {
   const int dim = p.a.c.dim;
   const long long queries = std::min<long long>(p.part.per, p.a.N) * (p.a.H / p.a.c.heads);
-  if (p.a.c.dtype == 0 && dim <= 128 && queries > 16 && p.a.c.n_pages > 0) {
+  if (p.a.c.dtype == 0 && dim <= 128 && queries > 16 && p.a.c.n_pages > 0 && p.a.scale >= 0.f) {
     const cudaError_t e = launch_kv_tc(p, sms, status, s);
     return e != cudaSuccess ? e : run_join<__nv_bfloat16>(p, s);
   }

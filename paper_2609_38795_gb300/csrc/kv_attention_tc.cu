@@ -58,7 +58,7 @@ template <class C>
 struct KvSmem {
   KvMisc m;
   float top[kSoftWarps][32];              // a slow tile's maxima
-  float ref[C::kNQ];                      // references (log2)
+  float ref[C::kNQ];                      // references (scores)
   int vis[C::kNQ];                        // tokens of the run that a query sees
 };
 
@@ -81,16 +81,16 @@ ALR_DEV bool any_of(int id, int threads, bool x) {
       : "=r"(r) : "r"(x ? 1u : 0u), "r"(id), "r"(threads) : "memory");
   return r != 0;
 }
-ALR_DEV void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
-      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
-      "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]),
-      "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
-      : "memory");
+ALR_DEV void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+                 "=r"(r[7])
+               : "r"(taddr));
+}
+ALR_DEV void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
+               : "memory");
 }
 ALR_DEV void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -108,9 +108,60 @@ ALR_DEV uint32_t bf16x2(float lo, float hi) {
   return r;
 }
 
-// Group of the ring that holds tile i's keys, values: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1).
-ALR_DEV long long k_group(long long i) { return i == 0 ? 0 : 2 * i - 1; }
-ALR_DEV long long v_group(long long i, long long n) { return i == n - 1 ? 2 * n - 1 : 2 * i + 2; }
+// A place of the ring; tiles are copied and used in the order K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1).
+template <int kSlots>
+struct Place {
+  int slot = 0;
+  uint32_t round = 0;
+  ALR_DEV void next() {
+    if (++slot == kSlots) slot = 0, ++round;
+  }
+};
+
+// The slow tile of a softmax group: the references of 32 columns move to the maxima with this tile, the
+// products so far (if any) are scaled.  Lane k returns the factor of column k.  pos: the thread's token,
+// INT_MAX if its page does not exist.
+__device__ __noinline__ float move_refs(uint32_t s_at, uint32_t o_at, float c, float* ref, const int* vis,
+                                        float (*top)[32], int bar, int pos, bool scale_o) {
+  const int lane = threadIdx.x & 31, wq = threadIdx.x >> 5 & 3;
+  float most = kNegInf;
+#pragma unroll 1
+  for (int k0 = 0; k0 < 32; k0 += 8) {
+    uint32_t s[8];
+    tmem_ld8(s_at + k0, s);
+    tmem_ld_wait();
+    reg_fence(s);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float m = warp_max(pos < vis[k0 + k] ? __uint_as_float(s[k]) : kNegInf);
+      if (lane == k0 + k) most = m;
+    }
+  }
+  top[wq][lane] = most;
+  named_bar_sync(bar, 128);
+  const float old = ref[lane];
+  float up = old;
+  for (int k = 0; k < 4; ++k) up = fmaxf(up, top[k][lane]);
+  const float f = old == up ? 1.f : ex2((old - up) * c);
+  named_bar_sync(bar, 128);
+  if (wq == 0) ref[lane] = up;
+  if (scale_o) {
+#pragma unroll 1
+    for (int k0 = 0; k0 < 32; k0 += 8) {
+      uint32_t s[8];
+      tmem_ld8(o_at + k0, s);
+      tmem_ld_wait();
+      reg_fence(s);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        s[k] = __float_as_uint(__uint_as_float(s[k]) * __shfl_sync(~0u, f, k0 + k));
+      tmem_st8(o_at + k0, s);
+    }
+    tmem_st_wait();
+  }
+  named_bar_sync(bar, 128);
+  return f;
+}
 
 template <class C>
 __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int* status) {
@@ -160,7 +211,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
   const uint32_t tmem = mi.tmem;
   const int n_workers = int(min((long long)p.workers, total)), id = blockIdx.x;
   const long long begin = id < n_workers ? stretch(total, n_workers, id) : 0;
-  const long long end = id < n_workers ? stretch(total, n_workers, id + 1) : 0, count = end - begin;
+  const long long end = id < n_workers ? stretch(total, n_workers, id + 1) : 0;
+  const int count = int(end - begin);
   if (threadIdx.x == 0 && count == 0 && id < p.workers) p.cuts[id] = make_int4(0, 0, 0, 0);
 
   if (warp >= kCopyWarp && warp < kMmaWarp) {
@@ -175,10 +227,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
     const auto place = [&](int r, int rows) {
       return uint32_t((pack >> 3) * rows * 128 + r * 128 + (((pack & 7) ^ (r & 7)) << 4));
     };
-    Cursor<kBlk> in;
-    if (count > 0) in.start(p, mi.start.tile, mi.start.rest);
-    int j = 0, off = 0, pg = -1;
-    const auto look_up = [&](bool runs_on) {
+    Cursor<kBlk> in{};
+    // What a tile's copies need.  The table is read a tile ahead: a page's number takes as long to come
+    // as its rows.
+    struct Next {
+      int pg, off, unit;
+      long long tile;
+      bool first, last;
+    } next = {-1, 0, 0, 0, true, true};
+    int j = 0, off = 0;
+    const auto look_up = [&](bool runs_on, int i) {
       if (runs_on) {
         j += p.step_pg;
         off += p.step_tok;
@@ -188,50 +246,61 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
         j = tok / a.c.page;
         off = tok - j * a.c.page;
       }
-      pg = in.t0 + w * 32 + lane < in.most ? a.table[(long long)in.seq * a.cols + j] : -1;
+      next.pg = in.t0 + w * 32 + lane < in.most ? a.table[(long long)in.seq * a.cols + j] : -1;
+      next.off = off;
+      next.unit = in.unit;
+      next.tile = in.tile;
+      next.first = i == 0 || in.b == 0;
+      next.last = i + 1 == count || in.b + 1 == in.t.nb;
     };
-    if (count > 0) look_up(false);
-    long long group = 0, item = -1;
+    if (count > 0) {
+      in.start(p, mi.start.tile, mi.start.rest);
+      look_up(false, 0);
+    }
+    Place<kSlots> to;
     const auto copy = [&](const void* cache, int kv, long long row, uint32_t all) {
-      const int slot = int(group % kSlots);
-      if (group >= kSlots) wait_on(&mi.empty[slot], uint32_t(group / kSlots - 1), ab);
+      if (to.round > 0) wait_on(&mi.empty[to.slot], to.round - 1, ab);
       const E* base = static_cast<const E*>(cache) + kv * a.c.sh + pack * 8;
-      const uint32_t dst = ring_at + slot * C::kTile;
+      const uint32_t dst = ring_at + to.slot * C::kTile;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int r = i * kRowsAt + sub;
         const long long from = __shfl_sync(~0u, row, r);
         if (has_pack) cp_async16_or_zero(dst + place(w * 32 + r, kBlk), base + from, all >> r & 1);
       }
-      cp_async_arrive(&mi.full[slot]);
+      cp_async_arrive(&mi.full[to.slot]);
       __syncwarp();
-      if (lane == 0) mbar_arrive(&mi.full[slot]);
-      ++group;
+      if (lane == 0) mbar_arrive(&mi.full[to.slot]);
+      to.next();
     };
     long long row_v = 0;
     uint32_t all_v = 0;
-    int kv_v = 0;
-    for (long long i = 0; i < count; ++i) {
-      const bool first = i == 0 || in.b == 0, last = i + 1 == count || in.b + 1 == in.t.nb;
-      const bool there = pg >= 0 && pg < a.c.n_pages;
+    int kv_v = 0, item = -1;
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+      const Next cur = next;
+      if (i + 1 < count) {
+        const bool on = in.advance(p);
+        look_up(on, i + 1);
+      }
+      const bool there = cur.pg >= 0 && cur.pg < a.c.n_pages;
       const uint32_t all = __ballot_sync(~0u, there);
-      const long long row = there ? pg * a.c.sp + off * a.c.st : 0;
-      const int kv = in.unit / p.gs;
+      const long long row = there ? cur.pg * a.c.sp + cur.off * a.c.st : 0;
+      const int kv = cur.unit / p.gs;
       // flags and masks of tile i: read after its keys have landed; tile i - kInfo is long done with
       // (its values' slot has been refilled since)
       if (lane == 0) {
         mi.there[i % kInfo][w] = all;
-        if (w == 0) mi.info[i % kInfo] = (first ? 1u : 0u) | (last ? 2u : 0u);
+        if (w == 0) mi.info[i % kInfo] = (cur.first ? 1u : 0u) | (cur.last ? 2u : 0u);
       }
-      if (first) {
+      if (cur.first) {
         ++item;
-        const int buf = int(item % C::kQBufs);
-        if (item >= C::kQBufs) wait_on(&mi.q_empty[buf], uint32_t(item / C::kQBufs - 1), ab);
+        if (item >= 2) wait_on(&mi.q_empty[item & 1], (item >> 1) - 1, ab);
         long long row0;
-        const int n_rows = max(tile_rows(p, in.tile, row0), 0);
-        const int group_q = a.H / a.c.heads, slice = (in.unit - kv * p.gs) * p.gw;
+        const int n_rows = max(tile_rows(p, cur.tile, row0), 0);
+        const int group_q = a.H / a.c.heads, slice = (cur.unit - kv * p.gs) * p.gw;
         const int gw = min(p.gw, group_q - slice), h0 = kv * group_q + slice;
-        const uint32_t dst = q_at + buf * C::kQBytes;
+        const uint32_t dst = q_at + (item & 1) * C::kQBytes;
         for (int q = w * kRowsAt + sub; q < kNQ; q += kCopyWarps * kRowsAt) {
           const int r = q / p.gw, h = q - r * p.gw;
           const bool ok = r < n_rows && h < gw;
@@ -244,7 +313,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       row_v = row;
       all_v = all;
       kv_v = kv;
-      if (i + 1 < count) look_up(in.advance(p));
     }
     if (count > 0) copy(a.c.V, kv_v, row_v, all_v);
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -256,41 +324,45 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       constexpr uint32_t i_o = idesc_make(false, 128, kNQ, true, true);
       const int n_k = (dim + 15) / 16;
       const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(qs), p_at = smem_u32(ps);
-      long long item = -1;
+      int item = -1;
       uint32_t prev = 0;
-      const auto values = [&](long long i, uint32_t info) {
-        const long long g = v_group(i, count);
-        const int slot = int(g % kSlots), pb = int(i % C::kPBufs);
-        wait_on(&mi.full[slot], uint32_t(g / kSlots), ab);
-        wait_on(&mi.p_full[pb], uint32_t(i / C::kPBufs), ab);
+      Place<kSlots> from;
+      // The proxy fences here, after the waits, order the copies' and the softmax's writes to shared
+      // memory before the products' reads (a fence in every writing thread cost 360 cycles a tile).
+      const auto values = [&](int i, uint32_t info) {
+        const int pb = C::kPBufs == 2 ? i & 1 : 0;
+        wait_on(&mi.full[from.slot], from.round, ab);
+        wait_on(&mi.p_full[pb], C::kPBufs == 2 ? i >> 1 : i, ab);
         fence_proxy_async_smem();
         tc_fence_after();
-        const uint32_t va = ring_at + slot * C::kTile, pa = p_at + pb * C::kPBytes;
+        const uint32_t va = ring_at + from.slot * C::kTile, pa = p_at + pb * C::kPBytes;
 #pragma unroll
         for (int k = 0; k < kBlk / 16; ++k)
           // dim <= 64: rows 64 to 127 of the result come from whatever lies behind the tile, unused
           mma_issue<false>(tmem + 2 * kNQ, sdesc_sw128(va + k * 2048, kBlk * 128, 1024),
                            sdesc_sw128(pa + k * 2048, kBlk * 128, 1024), i_o, !(info & 1) || k > 0);
-        mma_commit(&mi.empty[slot]);
+        mma_commit(&mi.empty[from.slot]);
         mma_commit(&mi.pv_done[pb]);
+        from.next();
       };
-      for (long long i = 0; i < count; ++i) {
-        const long long g = k_group(i);
-        const int slot = int(g % kSlots), sb = int(i & 1);
-        wait_on(&mi.full[slot], uint32_t(g / kSlots), ab);
-        fence_proxy_async_smem();
+#pragma unroll 1
+      for (int i = 0; i < count; ++i) {
+        const int sb = i & 1;
+        wait_on(&mi.full[from.slot], from.round, ab);
         const uint32_t info = mi.info[i % kInfo];
         if (info & 1) ++item;
-        const int buf = int(item % C::kQBufs);
-        if (i >= 2) wait_on(&mi.s_empty[sb], uint32_t(i / 2 - 1), ab);
+        if (i >= 2) wait_on(&mi.s_empty[sb], (i >> 1) - 1, ab);
+        fence_proxy_async_smem();
         tc_fence_after();
-        const uint32_t ka = ring_at + slot * C::kTile, qa = q_at + buf * C::kQBytes;
+        const uint32_t ka = ring_at + from.slot * C::kTile, qa = q_at + (item & 1) * C::kQBytes;
+#pragma unroll 4
         for (int k = 0; k < n_k; ++k)
           mma_issue<false>(tmem + sb * kNQ, sdesc_sw128(ka + (k >> 2) * (kBlk * 128) + (k & 3) * 32, 16, 1024),
                            sdesc_sw128(qa + (k >> 2) * (kNQ * 128) + (k & 3) * 32, 16, 1024), i_s, k > 0);
-        mma_commit(&mi.empty[slot]);
+        mma_commit(&mi.empty[from.slot]);
         mma_commit(&mi.s_full[sb]);
-        if (info & 2) mma_commit(&mi.q_empty[buf]);
+        if (info & 2) mma_commit(&mi.q_empty[item & 1]);
+        from.next();
         if (i > 0) values(i - 1, prev);
         prev = info;
       }
@@ -307,13 +379,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
     const uint32_t lanes = tmem + (uint32_t(wq * 32) << 16);
     const int tok = tid, q0 = wg * kHalf;
     const float c = a.scale * kLog2e;
+    const uint64_t c2 = f2_pack(c, c);
     float l[kHalf];
     Cursor<kBlk> at;
     if (count > 0) at.start(p, mi.start.tile, mi.start.rest);
     float (*lsum)[kHalf] = reinterpret_cast<float (*)[kHalf]>(ps);               // at an item's end
     KvRowOut* outs = reinterpret_cast<KvRowOut*>(ps + kSoftWarps * kHalf * sizeof(float));
     int4 cut = make_int4(0, 0, 0, 0);
-    long long i = 0;
+    int i = 0;
     while (i < count) {
       long long row0;
       const int n_rows = max(tile_rows(p, at.tile, row0), 0);
@@ -321,8 +394,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       const int gw = min(p.gw, group_q - slice), h0 = kv * group_q + slice, n_q = n_rows * p.gw;
       const Tile tile = at.t;
       const long long tile_id = at.tile;
-      const int unit = at.unit, b0 = at.b, b1 = int(min((long long)tile.nb, b0 + (count - i)));
-      const long long i0 = i;
+      const int unit = at.unit, b0 = at.b, b1 = min(tile.nb, b0 + (count - i));
+      const int i0 = i;
       if (tid < kHalf) sm.ref[q0 + tid] = kNoRef;
 #pragma unroll
       for (int k = 0; k < kHalf; ++k) l[k] = 0.f;
@@ -341,90 +414,60 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
             }
           named_bar_sync(bar, 128);
         }
-        const int sb = int(i & 1), pb = int(i % C::kPBufs);
-        wait_on(&mi.s_full[sb], uint32_t(i / 2), ab);
+        const int sb = i & 1, pb = C::kPBufs == 2 ? i & 1 : 0;
+        wait_on(&mi.s_full[sb], i >> 1, ab);
         tc_fence_after();
         const uint32_t* there = mi.there[i % kInfo];
-        const bool here = (there[wq] >> lane & 1) != 0;
-        const int pos = at.t0 + tok;
+        const int pos = there[wq] >> lane & 1 ? at.t0 + tok : INT_MAX;
         const bool plain = least - at.t0 >= kBlk && (there[0] & there[1] & there[2] & there[3]) == ~0u;
         const uint32_t s_at = lanes + sb * kNQ + q0, o_at = lanes + 2 * kNQ + q0;
         uint8_t* prow = ps + pb * C::kPBytes + tok * 128;
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
-          uint32_t s[32];
           float y[32];
-          tmem_ld32(s_at + part * 32, s);
-          tmem_ld_wait();
-          reg_fence(s);
-          const float* ref = sm.ref + q0 + part * 32;
-          float t = kNegInf;
-#pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            const float4 r = *reinterpret_cast<const float4*>(ref + k);
-            y[k] = fmaf(__uint_as_float(s[k]), c, -r.x);
-            y[k + 1] = fmaf(__uint_as_float(s[k + 1]), c, -r.y);
-            y[k + 2] = fmaf(__uint_as_float(s[k + 2]), c, -r.z);
-            y[k + 3] = fmaf(__uint_as_float(s[k + 3]), c, -r.w);
-          }
-          const auto mask = [&](float (&v)[32]) {
-            const int* vis = sm.vis + q0 + part * 32;
-#pragma unroll
-            for (int k = 0; k < 32; k += 4) {
-              const int4 r = *reinterpret_cast<const int4*>(vis + k);
-              v[k] = here && pos < r.x ? v[k] : kNegInf;
-              v[k + 1] = here && pos < r.y ? v[k + 1] : kNegInf;
-              v[k + 2] = here && pos < r.z ? v[k + 2] : kNegInf;
-              v[k + 3] = here && pos < r.w ? v[k + 3] : kNegInf;
-            }
-          };
-          if (!plain) mask(y);
-#pragma unroll
-          for (int k = 0; k < 32; k += 2) t = max3(t, y[k], y[k + 1]);
-          if (any_of(bar, 128, t > kLag)) {
-            // a reference moves: maxima over the tile, the sums so far scaled
+          // Exponents are differences of scores, times c (the fma s c - ref c would leave the rounding of
+          // ref c, which is more than 2^8 from |ref c| = 2^32 on): after a move none is above 0.
+          for (bool moved = false;; moved = true) {
+            uint32_t s[32];
             tmem_ld32(s_at + part * 32, s);
+            const float* ref = sm.ref + q0 + part * 32;
+            float t = kNegInf;
             tmem_ld_wait();
             reg_fence(s);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) y[k] = __uint_as_float(s[k]) * c;
-            if (!plain) mask(y);
-            float top = kNegInf;
-#pragma unroll
-            for (int k = 0; k < 32; ++k) {
-              const float m = warp_max(y[k]);
-              if (lane == k) top = m;
+            for (int k = 0; k < 32; k += 4) {
+              const float4 r = *reinterpret_cast<const float4*>(ref + k);
+              f2_unpack(f2_mul(f2_sub(f2_pack(__uint_as_float(s[k]), __uint_as_float(s[k + 1])),
+                                      f2_pack(r.x, r.y)), c2), y[k], y[k + 1]);
+              f2_unpack(f2_mul(f2_sub(f2_pack(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])),
+                                      f2_pack(r.z, r.w)), c2), y[k + 2], y[k + 3]);
             }
-            sm.top[warp][lane] = top;
-            named_bar_sync(bar, 128);
-            const float old = ref[lane];
-            float up = old;
-            for (int k = 0; k < 4; ++k) up = fmaxf(up, sm.top[wg * 4 + k][lane]);
-            const float f = old == up ? 1.f : ex2(old - up);
-            named_bar_sync(bar, 128);
-            if (wq == 0) sm.ref[q0 + part * 32 + lane] = up;
+            if (!plain) {
+              const int* vis = sm.vis + q0 + part * 32;
 #pragma unroll
-            for (int k = 0; k < 32; ++k) {
-              y[k] -= __shfl_sync(~0u, up, k);
-              l[part * 32 + k] *= __shfl_sync(~0u, f, k);
+              for (int k = 0; k < 32; k += 4) {
+                const int4 r = *reinterpret_cast<const int4*>(vis + k);
+                y[k] = pos < r.x ? y[k] : kNegInf;
+                y[k + 1] = pos < r.y ? y[k + 1] : kNegInf;
+                y[k + 2] = pos < r.z ? y[k + 2] : kNegInf;
+                y[k + 3] = pos < r.w ? y[k + 3] : kNegInf;
+              }
             }
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) t = max3(t, y[k], y[k + 1]);
+            if (moved || !any_of(bar, 128, t > kLag)) break;
             if (i > i0) {
-              wait_on(&mi.pv_done[(i - 1) % C::kPBufs], uint32_t((i - 1) / C::kPBufs), ab);
+              wait_on(&mi.pv_done[C::kPBufs == 2 ? (i - 1) & 1 : 0], C::kPBufs == 2 ? (i - 1) >> 1 : i - 1, ab);
               tc_fence_after();
-              tmem_ld32(o_at + part * 32, s);
-              tmem_ld_wait();
-              reg_fence(s);
-#pragma unroll
-              for (int k = 0; k < 32; ++k)
-                s[k] = __float_as_uint(__uint_as_float(s[k]) * __shfl_sync(~0u, f, k));
-              tmem_st32(o_at + part * 32, s);
-              tmem_st_wait();
             }
-            named_bar_sync(bar, 128);
+            const float f = move_refs(s_at + part * 32, o_at + part * 32, c, sm.ref + q0 + part * 32,
+                                      sm.vis + q0 + part * 32, sm.top + wg * 4, bar, pos, i > i0);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) l[part * 32 + k] *= __shfl_sync(~0u, f, k);
           }
           // this buffer's last product
           if (part == 0 && i >= C::kPBufs)
-            wait_on(&mi.pv_done[pb], uint32_t(i / C::kPBufs - 1), ab);
+            wait_on(&mi.pv_done[pb], C::kPBufs == 2 ? (i >> 1) - 1 : i - 1, ab);
 #pragma unroll
           for (int k = 0; k < 32; k += 8) {
             uint32_t x[4];
@@ -441,7 +484,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
           }
         }
         tc_fence_before();
-        fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&mi.s_empty[sb]);
@@ -450,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
         if (i + 1 < count) at.advance(p);
       }
       // ---- the item's results
-      wait_on(&mi.pv_done[(i - 1) % C::kPBufs], uint32_t((i - 1) / C::kPBufs), ab);
+      wait_on(&mi.pv_done[C::kPBufs == 2 ? (i - 1) & 1 : 0], C::kPBufs == 2 ? (i - 1) >> 1 : i - 1, ab);
       tc_fence_after();
       named_bar_sync(3, 256);                // both groups are past their last weights
       // sums over the warp's tokens: lane k ends with column k's
@@ -481,29 +523,42 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
         float s = 0.f;
         for (int k = 0; k < 4; ++k) s += lsum[wg * 4 + k][tid];
         KvRowOut o = {0.f, 0.f, nullptr, nullptr, nullptr};
-        if (q < n_q && q - r * p.gw < gw) o = out(q, r, s == 0.f ? kNegInf : sm.ref[q], s, true);
+        if (q < n_q && q - r * p.gw < gw) o = out(q, r, s == 0.f ? kNegInf : sm.ref[q] * c, s, true);
         if (!(s - s == 0.f)) atomicOr(&mi.bad[q >> 5], 1u << (q & 31));
         outs[q] = o;
       }
       named_bar_sync(bar, 128);
       const int d = wq * 32 + lane;
+      const bool final_row = whole && p.put_o == nullptr;
+      float odd = 0.f;                       // NaN after a value that is not finite
 #pragma unroll 1
-      for (int part = 0; part < kParts; ++part) {
-        if (q0 + part * 32 >= n_q) break;
-        uint32_t s[32];
-        tmem_ld32(lanes + 2 * kNQ + q0 + part * 32, s);
+      for (int k0 = 0; k0 < kHalf; k0 += 8) {
+        if (q0 + k0 >= n_q) break;
+        uint32_t s[8];
+        tmem_ld8(lanes + 2 * kNQ + q0 + k0, s);
+        float pre[8] = {};
+        if (final_row && p.pre_o != nullptr) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const KvRowOut& o = outs[q0 + k0 + k];
+            if (o.dst != nullptr && d < dim) pre[k] = o.pre[d] * o.f_pre;
+          }
+        }
         tmem_ld_wait();
         reg_fence(s);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          const int q = q0 + part * 32 + k;
-          const KvRowOut& o = outs[q];
-          const float v[1] = {__uint_as_float(s[k])};
-          if (q < n_q && d < dim && (o.dst != nullptr || o.dst_f != nullptr)) {
-            put<E, 1>(o, d, v);
-            if (!(v[0] - v[0] == 0.f)) atomicOr(&mi.bad[q >> 5], 1u << (q & 31));
+        for (int k = 0; k < 8; ++k) {
+          const KvRowOut& o = outs[q0 + k0 + k];
+          const float v = __uint_as_float(s[k]);
+          if (d < dim) {
+            if (o.dst != nullptr) static_cast<E*>(o.dst)[d] = E(fmaf(v, o.f, pre[k]));
+            if (o.dst_f != nullptr) o.dst_f[d] = v;
+            if (o.dst != nullptr || o.dst_f != nullptr) odd = fmaf(0.f, v, odd);
           }
         }
+      }
+      if (!(odd == 0.f)) {                   // which queries: rare
+        for (int k = 0; k < kHalf && q0 + k < n_q; ++k) atomicOr(&mi.bad[(q0 + k) >> 5], 1u << ((q0 + k) & 31));
       }
       tc_fence_before();
       named_bar_sync(3, 256);

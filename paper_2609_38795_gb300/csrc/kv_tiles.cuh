@@ -19,9 +19,8 @@ ALR_DEV int part_seq(const KvPart& p, long long row) {
   return p.seq != nullptr ? p.seq[row] : int(row / p.per);
 }
 
-ALR_DEV int part_len(const KvAttention& a, const KvPart& p, long long row, int seq) {
-  if (seq < 0 || seq >= a.n_seq) return 0;
-  return int(min((long long)max(p.len[row], 0), (long long)a.cols * a.c.page));
+ALR_DEV int seen_len(const KvAttention& a, int seq, int len) {
+  return seq < 0 || seq >= a.n_seq ? 0 : int(min((long long)max(len, 0), (long long)a.cols * a.c.page));
 }
 
 // One pass over a part.  The rows go in tiles: groups of `per` consecutive rows (those that usually read
@@ -150,15 +149,24 @@ ALR_DEV int tile_blocks(const KvPass& p, long long tile) {
   long long row0;
   const int n = tile_rows(p, tile, row0);
   int nb = 0, cur = 0, most = 0;
-  for (int i = 0; i < n; ++i) {
-    const int s = part_seq(p.part, row0 + i), len = part_len(p.a, p.part, row0 + i, s);
-    if (len == 0) continue;
-    if (most > 0 && s != cur) {
-      nb += blocks_of<kBlk>(most);
-      most = 0;
+  for (int i0 = 0; i0 < n; i0 += 8) {        // eight rows' loads at a time
+    int s[8], len[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      s[i] = i0 + i < n ? part_seq(p.part, row0 + i0 + i) : -1;
+      len[i] = i0 + i < n ? p.part.len[row0 + i0 + i] : 0;
     }
-    cur = s;
-    most = max(most, len);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int k = seen_len(p.a, s[i], len[i]);
+      if (k == 0) continue;
+      if (most > 0 && s[i] != cur) {
+        nb += blocks_of<kBlk>(most);
+        most = 0;
+      }
+      cur = s[i];
+      most = max(most, k);
+    }
   }
   return max(nb + blocks_of<kBlk>(most), 1);
 }
@@ -179,7 +187,7 @@ ALR_DEV Tile load_tile(const KvPass& p, long long tile) {
   const int n = tile_rows(p, tile, row0);
   Tile t;
   t.seq = lane < n ? part_seq(p.part, row0 + lane) : -1;
-  t.len = lane < n ? part_len(p.a, p.part, row0 + lane, t.seq) : 0;
+  t.len = seen_len(p.a, t.seq, lane < n ? p.part.len[row0 + lane] : 0);
   const uint32_t some = __ballot_sync(~0u, t.len > 0), up_to = (2u << lane) - 1;
   const uint32_t before = some & (up_to >> 1);
   const int prev = __shfl_sync(~0u, t.seq, before != 0 ? 31 - __clz(before) : 0);
@@ -309,7 +317,7 @@ ALR_DEV void walk_tokens(const KvAttention& a, int seq, int t0, int t1, int head
 #pragma unroll
     for (int i = 0; i < kLaneDims; ++i)
       if (i * 32 + lane < a.c.dim) x = fmaf(q[i], to_float(K[at + i * 32 + lane]), x);
-    x = warp_reduce(x, AddOp()) * (a.scale * kLog2e);
+    x = __fmul_rn(warp_reduce(x, AddOp()), a.scale * kLog2e);
     if (x == kNegInf) continue;
     const float up = fmaxf(m, x), c = ex2(m - up), e = ex2(x - up);
     m = up;
@@ -339,7 +347,8 @@ inline void shape_pass(KvPass& p, int max_q, int max_rows, int blk) {
 
 constexpr int kKvMostSms = 160;
 
-// kv_attention_tc.cu: a pass over tiles of up to 32 rows and 128 queries (bf16, dim <= 128, n_pages > 0);
+// kv_attention_tc.cu: a pass over tiles of up to 32 rows and 128 queries (bf16, dim <= 128, n_pages > 0,
+// scale >= 0: references are maxima of the scores before they are scaled);
 // p.part is set, the rest of the pass's shape is filled in.
 cudaError_t launch_kv_tc(KvPass& p, int sms, int* status, cudaStream_t s);
 

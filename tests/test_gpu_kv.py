@@ -299,12 +299,20 @@ def test_poison_reaches_only_its_readers(dtype, per):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("per", [1, 16])
-def test_extreme_scores(dtype, per):
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 1e-30, 3.0])
+def test_scales(dtype, scale):
+    rows = [(s, n) for s in range(3) for n in (0, 5, 200, 260)]
+    for per in (1, 4):
+        Case([270, 280, 261], rows, dim=64, dtype=dtype, group=8, scale=scale).check(per=per)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("per,group", [(1, 1), (16, 1), (16, 2), (16, 8)])
+def test_extreme_scores(dtype, per, group):
     """Keys of -inf (tokens masked in the cache), scores of thousands, one token that has all the mass,
     rising and falling scores."""
     n = 400
-    c = Case([n], [(0, n - 15 + j) for j in range(16)], dim=64, dtype=dtype, heads=1, group=1)
+    c = Case([n], [(0, n - 15 + j) for j in range(16)], dim=64, dtype=dtype, heads=1, group=group)
     flat_k, flat_v = c.K.clone(), c.V.clone()
     pg, pos = c.table[0, np.arange(n) // 16], np.arange(n) % 16
     q = c.Q.clone()
@@ -315,6 +323,17 @@ def test_extreme_scores(dtype, per):
         c.K[pg, pos, :, 0] = (torch.arange(n, device="cuda")[:, None] * slope / 64).to(dtype)
         c.__dict__.pop("_want", None)
         c.check(per=per)
+    for top in (1e9, -1e9, 1e30, -1e30):                     # large scores next to ordinary ones
+        c.K[pg, pos] = flat_k[pg, pos]
+        c.K[pg[::2], pos[::2], :, 0] = top
+        c.__dict__.pop("_want", None)
+        c.check(per=per)
+        c.K[pg, pos, :, 0] = top                             # all alike but for what is below their rounding
+        c.__dict__.pop("_want", None)
+        out, lse = c.run(per=per)
+        assert torch.isfinite(out.float()).all() and torch.isfinite(lse).all()
+        assert bool((out.float().abs() <= flat_v[pg, pos].float().abs().max() * 1.01).all())
+    c.K[pg, pos] = flat_k[pg, pos]
     c.K[pg[::3], pos[::3], :, 0] = -float("inf")             # a third of the tokens masked by their keys
     c.__dict__.pop("_want", None)
     c.check(per=per)
