@@ -1,5 +1,7 @@
 // Attention of query rows over the paged key-value cache, up to 16 queries of a tile at a time.
 #include <algorithm>
+#include <cfloat>
+#include <cstdlib>
 
 #include "launch.h"
 #include "kv_tiles.cuh"
@@ -10,14 +12,12 @@ namespace {
 constexpr int kBlk = 16;       // tokens of a block
 
 // ------------------------------------------------------------------------- cores ---
-// A core holds the sums of an item's queries for a warp: load_q, zero, add (one block from the ring, with
-// each query's count of visible tokens), finish.
-//   Shared memory rows of kDim elements in packs of 16 bytes; pack c of row r lies at place c ^ r
-// (of the lowest bits), so that eight rows' packs c fall in different banks.
-template <int kPacks>
-ALR_DEV int pack_at(int row, int c) {
-  return row * kPacks + (kPacks >= 8 ? c ^ (row & 7) : c ^ ((row / (8 / kPacks)) & (kPacks - 1)));
-}
+// A core holds the sums of an item's queries for a warp: load_q, see (how many tokens of the run each of
+// the lane's queries sees), add (one block from the ring), leave (the sums to shared memory).
+//   A token's row in shared memory is `row` bytes, its elements and 16 more where that makes an odd number
+// of packs of 16 bytes, so that eight rows' packs at the same place fall in different banks.
+constexpr int kNoQuery = INT_MAX;
+constexpr float kNoRef = -FLT_MAX;
 
 ALR_DEV void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -33,6 +33,12 @@ ALR_DEV void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint3
       "{%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Transpose of an 8 x 8 matrix of 16-bit elements, two of a row in each lane.
+ALR_DEV uint32_t transpose8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
 }
 ALR_DEV uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
@@ -50,12 +56,12 @@ constexpr float kLag = 8.f;
 //   A group of 4 queries leaves 12 rows unused, yet the products are far from the bound: 16 tokens of
 // 128 elements are 32 instructions and 8 KB.
 template <int kDim_>
-struct Bf16Core {
+struct ManyCore {
   using E = __nv_bfloat16;
-  static constexpr int kDim = kDim_, kWarps = kDim <= 128 ? 8 : 4, kMaxQ = 16;
+  static constexpr int kDim = kDim_, kMostWarps = 8, kMaxQ = 16;
   static constexpr int kSteps = kDim / 16, kPacks = kDim / 8;
-  static constexpr int kStages = kDim <= 32 ? 8 : kDim <= 64 ? 5 : 3;   // blocks of a worker's ring
   static constexpr int kScratch = 0;
+  int lim[2];
   uint32_t q[kSteps][4];
   float o[kDim / 8][4];
   float m[2], l[2];
@@ -85,10 +91,19 @@ struct Bf16Core {
 #pragma unroll
     for (int i = 0; i < kDim / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   }
-  // lim: visible tokens of the block for the lane's two queries; there: tokens whose page exists.
-  ALR_DEV void add(const KvPass& p, uint32_t k_at, uint32_t v_at, const int (&lim)[2], uint32_t there,
-                   void*) {
+  // tokens: of the run, by row (lane)
+  ALR_DEV void see(const KvPass& p, int tokens, int n_q) {
+    const int g = (threadIdx.x & 31) >> 2;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int v = __shfl_sync(~0u, tokens, ((g + 8 * h) / p.gw) & 31);
+      lim[h] = g + 8 * h < n_q ? v : kNoQuery;
+    }
+  }
+  // t0: the block's first token; there: tokens whose page exists; plain: all of them seen by all queries.
+  ALR_DEV void add(const KvPass& p, char* ring, int row_bytes, int t0, uint32_t there, bool plain, void*) {
     const int lane = threadIdx.x & 31, t = lane & 3;
+    const uint32_t k_at = smem_u32(ring), v_at = k_at + kBlk * row_bytes;
     float s[2][4] = {};
     {
       const int row = (lane >> 4) * 8 + (lane & 7), c = lane >> 3 & 1;
@@ -96,7 +111,7 @@ struct Bf16Core {
       for (int k = 0; k < kSteps; ++k) {
         if (k * 16 >= p.a.c.dim) break;
         uint32_t b[4];
-        ldmatrix4(b, k_at + 16 * pack_at<kPacks>(row, 2 * k + c));
+        ldmatrix4(b, k_at + row * row_bytes + 16 * (2 * k + c));
         mma_16816(s[0], q[k], b[0], b[1]);
         mma_16816(s[1], q[k], b[2], b[3]);
       }
@@ -106,13 +121,13 @@ struct Bf16Core {
     for (int n = 0; n < 2; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[n][e] = __fmul_rn(s[n][e], c);   // never an fma with the reference
-    if (!__all_sync(~0u, lim[0] >= kBlk && lim[1] >= kBlk && there == 0xffffu)) {
+    if (!plain) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int tok = n * 8 + 2 * t + (e & 1);
-          if (tok >= lim[e >> 1] || !(there >> tok & 1)) s[n][e] = kNegInf;
+          if (t0 + tok >= lim[e >> 1] || !(there >> tok & 1)) s[n][e] = kNegInf;
         }
     }
     float top[2];
@@ -156,40 +171,144 @@ struct Bf16Core {
     for (int i = 0; i < kDim / 16; ++i) {
       if (i * 16 >= p.a.c.dim) break;
       uint32_t b[4];
-      ldmatrix4_t(b, v_at + 16 * pack_at<kPacks>(row, 2 * i + c2));
+      ldmatrix4_t(b, v_at + row * row_bytes + 16 * (2 * i + c2));
       mma_16816(o[2 * i], w, b[0], b[1]);
       mma_16816(o[2 * i + 1], w, b[2], b[3]);
     }
   }
-  // Whether query `half` of the lane got a value that is not finite.
-  ALR_DEV bool odd(int half) const {
-    float x = l[half];
-#pragma unroll
-    for (int i = 0; i < kDim / 8; ++i) x = fmaf(0.f, o[i][2 * half] + o[i][2 * half + 1], x);
-    return !(x - x == 0.f);
-  }
-  template <typename Out>
-  ALR_DEV uint32_t finish(const KvPass& p, int n_q, void*, Out out) {
+  // The sums into shared memory: o as rows of dim + 4, m and l behind n_q of them.
+  ALR_DEV void leave(int n_q, int dim, float* to) {
     const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
-    uint32_t bad = 0;
+    float* ml = to + n_q * (dim + 4);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       l[h] += __shfl_xor_sync(~0u, l[h], 1);
       l[h] += __shfl_xor_sync(~0u, l[h], 2);
       const int i = g + 8 * h;
-      const uint32_t who = __ballot_sync(~0u, i < n_q && odd(h));
-      for (int k = 0; k < 8; ++k)
-        if (who >> (4 * k) & 15u) bad |= 1u << (k + 8 * h);
-      if (i >= n_q) continue;
-      const KvRowOut r = out(i, m[h], l[h], t == 0);
+      if (i < n_q) {
+        if (t == 0) ml[2 * i] = m[h], ml[2 * i + 1] = l[h];
 #pragma unroll
-      for (int k = 0; k < kDim / 8; ++k) {
-        const int d = k * 8 + 2 * t;
-        const float v[2] = {o[k][2 * h], o[k][2 * h + 1]};
-        if (d < p.a.c.dim) put<E, 2>(r, d, v);
+        for (int k = 0; k < kDim / 8; ++k)
+          if (k * 8 < dim) *reinterpret_cast<float2*>(to + i * (dim + 4) + k * 8 + 2 * t) = {o[k][2 * h], o[k][2 * h + 1]};
       }
     }
-    return bad;
+  }
+};
+
+// bf16, up to 8 queries, with the tokens (the elements of a value) on a product's 16 rows and the queries
+// on its 8 columns: half the products of ManyCore and half its registers.  Lane (g, t) has queries 2t and
+// 2t + 1 of tokens g and g + 8; the weights are transposed into the second product's operand.
+//   The reference lags, and no maximum is taken while a vote finds all scores below it + kLag: sums cross
+// lanes at an item's end only.
+template <int kDim_>
+struct FewCore {
+  using E = __nv_bfloat16;
+  static constexpr int kDim = kDim_, kMostWarps = kDim <= 128 ? 16 : 8, kMaxQ = 8;
+  static constexpr int kSteps = kDim / 16, kPacks = kDim / 8;
+  static constexpr int kScratch = 0;
+  uint32_t q[kSteps][2];
+  float o[kSteps][4];
+  float m[2], l[2];
+  int lim[2];
+
+  ALR_DEV void load_q(const KvPass& p, long long row0, int h0, int n_q, int gw, void*) {
+    const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3, r = g / p.gw;
+    const bool there = g < n_q && g - r * p.gw < gw;
+    const E* src = static_cast<const E*>(p.a.Q) + (there ? (row0 + r) * p.a.ldq + (h0 + g - r * p.gw) * p.a.c.dim : 0);
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int d = k * 16 + e * 8 + 2 * t;
+        q[k][e] = there && d < p.a.c.dim ? *reinterpret_cast<const uint32_t*>(src + d) : 0u;
+      }
+  }
+  ALR_DEV void zero() {
+    m[0] = m[1] = kNoRef;
+    l[0] = l[1] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  }
+  ALR_DEV void see(const KvPass& p, int tokens, int n_q) {
+    const int t = threadIdx.x & 3;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int v = __shfl_sync(~0u, tokens, (2 * t + h) / p.gw);
+      lim[h] = 2 * t + h < n_q ? v : kNoQuery;
+    }
+  }
+  ALR_DEV void add(const KvPass& p, char* ring, int row_bytes, int t0, uint32_t there, bool plain, void*) {
+    const int lane = threadIdx.x & 31, g = lane >> 2;
+    const uint32_t at = smem_u32(ring) + (lane & 15) * row_bytes + (lane >> 4) * 16;
+    float s[4] = {}, s2[4] = {};
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      if (k * 16 >= p.a.c.dim) break;
+      uint32_t a[4];
+      ldmatrix4(a, at + 32 * k);
+      mma_16816(k & 1 ? s2 : s, a, q[k][0], q[k][1]);
+    }
+    const float c = p.a.scale * kLog2e;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] = __fmul_rn(s[e] + s2[e], c);   // never an fma with the reference
+    if (!plain) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int tok = g + 8 * (e >> 1);
+        if (t0 + tok >= lim[e & 1] || !(there >> tok & 1)) s[e] = kNegInf;
+      }
+    }
+    if (__any_sync(~0u, fmaxf(s[0], s[2]) - m[0] > kLag || fmaxf(s[1], s[3]) - m[1] > kLag)) {
+      float f[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float up = fmaxf(s[h], s[h + 2]);
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) up = fmaxf(up, __shfl_xor_sync(~0u, up, off));
+        up = fmaxf(m[h], up);
+        f[h] = m[h] == up ? 1.f : ex2(m[h] - up);
+        m[h] = up;
+        l[h] *= f[h];
+      }
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        o[i][0] *= f[0], o[i][1] *= f[1];
+        o[i][2] *= f[0], o[i][3] *= f[1];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] = ex2(s[e] - m[e & 1]);
+    l[0] += s[0] + s[2];
+    l[1] += s[1] + s[3];
+    // the product's only operand type: a weight is off by 2^-8, l is not
+    const uint32_t b0 = transpose8(pack_bf16(s[0], s[1])), b1 = transpose8(pack_bf16(s[2], s[3]));
+    const uint32_t vat = smem_u32(ring) + kBlk * row_bytes + (((lane >> 4) << 3) + (lane & 7)) * row_bytes +
+                         (lane >> 3 & 1) * 16;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      if (i * 16 >= p.a.c.dim) break;
+      uint32_t a[4];
+      ldmatrix4_t(a, vat + 32 * i);
+      mma_16816(o[i], a, b0, b1);
+    }
+  }
+  ALR_DEV void leave(int n_q, int dim, float* to) {
+    const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+    float* ml = to + n_q * (dim + 4);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1) l[h] += __shfl_xor_sync(~0u, l[h], off);
+      const int i = 2 * t + h;
+      if (i < n_q) {
+        if (g == 0) ml[2 * i] = l[h] == 0.f ? kNegInf : m[h], ml[2 * i + 1] = l[h];
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (k * 16 + e * 8 < dim) to[i * (dim + 4) + k * 16 + e * 8 + g] = o[k][h + 2 * e];
+      }
+    }
   }
 };
 
@@ -200,14 +319,14 @@ struct Bf16Core {
 template <int kDim_, int kQ>
 struct F32Core {
   using E = float;
-  static constexpr int kDim = kDim_, kWarps = kDim <= 64 ? 8 : kDim <= 128 ? 4 : 2, kMaxQ = kQ;
-  static constexpr int kStages = kDim <= 32 ? 5 : 3;
+  static constexpr int kDim = kDim_, kMostWarps = kQ == 1 ? 16 : 8, kMaxQ = kQ;
   static constexpr int kPacks = kDim / 4;
   static constexpr int kOwn = kPacks > 32 ? kPacks / 32 : 1;       // packs of a lane
   static constexpr int kGroups = kPacks < 32 ? 32 / kPacks : 1;    // lanes that share a pack
   static constexpr int kScratch = (kQ * kDim + kBlk * kQ) * 4;     // queries, weights
   float o[kQ][kOwn][4];
   float m[kQ], l[kQ];          // l: of the lane's token
+  int lim[kQ];
 
   ALR_DEV void load_q(const KvPass& p, long long row0, int h0, int n_q, int gw, void* scratch) {
     float* qs = static_cast<float*>(scratch);
@@ -233,8 +352,13 @@ struct F32Core {
       for (int k = 0; k < kOwn; ++k) o[i][k][0] = o[i][k][1] = o[i][k][2] = o[i][k][3] = 0.f;
     }
   }
-  ALR_DEV void add(const KvPass& p, const char* ks, const char* vs, const int (&lim)[kQ], uint32_t there,
+  ALR_DEV void see(const KvPass& p, int tokens, int n_q) {
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) lim[i] = __shfl_sync(~0u, tokens, (i / p.gw) & 31);
+  }
+  ALR_DEV void add(const KvPass& p, const char* ks, int row_bytes, int t0, uint32_t there, bool plain,
                    void* scratch) {
+    const char* vs = ks + kBlk * row_bytes;
     const float* qs = static_cast<const float*>(scratch);
     float* ws = static_cast<float*>(scratch) + kQ * kDim;
     const int lane = threadIdx.x & 31, tok = lane & 15, half = lane >> 4;
@@ -242,7 +366,7 @@ struct F32Core {
     float s[kQ] = {};
 #pragma unroll 4
     for (int c = half; c < packs; c += 2) {
-      const float4 k = reinterpret_cast<const float4*>(ks)[pack_at<kPacks>(tok, c)];
+      const float4 k = *reinterpret_cast<const float4*>(ks + tok * row_bytes + 16 * c);
 #pragma unroll
       for (int i = 0; i < kQ; ++i) {
         const float4 x = reinterpret_cast<const float4*>(qs + i * kDim)[c];
@@ -256,7 +380,7 @@ struct F32Core {
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
       s[i] = __fmul_rn(s[i] + __shfl_xor_sync(~0u, s[i], 16), c);    // never an fma with the reference
-      if (tok >= lim[i] || !here) s[i] = kNegInf;
+      if (!plain && (t0 + tok >= lim[i] || !here)) s[i] = kNegInf;
       top[i] = warp_max(s[i]);
       moves |= top[i] > m[i] + kLag;
     }
@@ -292,7 +416,8 @@ struct F32Core {
       float4 v[kOwn];
 #pragma unroll
       for (int k = 0; k < kOwn; ++k)
-        v[k] = reinterpret_cast<const float4*>(vs)[pack_at<kPacks>(j, own + 32 * k)];
+        v[k] = own + 32 * k < packs ? *reinterpret_cast<const float4*>(vs + j * row_bytes + 16 * (own + 32 * k))
+                                 : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < kQ; ++i) {
         const float e = ws[j * kQ + i];
@@ -306,33 +431,25 @@ struct F32Core {
       }
     }
   }
-  template <typename Out>
-  ALR_DEV uint32_t finish(const KvPass& p, int n_q, void*, Out out) {
-    const int lane = threadIdx.x & 31;
-    const int own = kGroups > 1 ? lane % kPacks : lane;
-    uint32_t bad = 0;
+  ALR_DEV void leave(int n_q, int dim, float* to) {
+    const int lane = threadIdx.x & 31, own = kGroups > 1 ? lane % kPacks : lane;
+    float* ml = to + n_q * (dim + 4);
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
       if (i >= n_q) break;
       const float sum = warp_reduce(l[i], AddOp());
-      float x = sum;
-#pragma unroll
-      for (int k = 0; k < kOwn; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-#pragma unroll
-          for (int off = kPacks; off < 32; off <<= 1) o[i][k][e] += __shfl_xor_sync(~0u, o[i][k][e], off);
-          x = fmaf(0.f, o[i][k][e], x);
-        }
-      if (__any_sync(~0u, !(x - x == 0.f))) bad |= 1u << i;
-      const KvRowOut r = out(i, m[i], sum, lane == 0);
+      if (lane == 0) ml[2 * i] = m[i], ml[2 * i + 1] = sum;
 #pragma unroll
       for (int k = 0; k < kOwn; ++k) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int off = kPacks; off < 32; off <<= 1) o[i][k][e] += __shfl_xor_sync(~0u, o[i][k][e], off);
         const int d = 4 * (own + 32 * k);
-        if (lane < kPacks && d < p.a.c.dim) put<E, 4>(r, d, o[i][k]);
+        if (lane < kPacks && d < dim)
+          *reinterpret_cast<float4*>(to + i * (dim + 4) + d) = make_float4(o[i][k][0], o[i][k][1], o[i][k][2], o[i][k][3]);
       }
     }
-    return bad;
   }
 };
 
@@ -340,34 +457,55 @@ struct F32Core {
 ALR_DEV void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+// Arrive on `bar` once all copies this thread issued so far have landed.
+ALR_DEV void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 ALR_DEV void put_zeros16(uint32_t dst) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst), "r"(0) : "memory");
 }
 
+// Bytes of a token's row in shared memory: its packs of 16 bytes, of bf16 an even number of them (a
+// product takes 16 elements), and one more where that makes them odd.
+template <typename E>
+__host__ __device__ constexpr int row_bytes_of(int dim) {
+  const int packs = dim * int(sizeof(E)) / 16, full = sizeof(E) == 2 ? (packs + 1) / 2 * 2 : packs;
+  return (full | 1) * 16;
+}
+
+constexpr int kMostStages = 8;
+
 // Each warp is a worker with a ring of its own: no block-wide barrier after the start, so warps in
 // different items never wait for one another, and a ring's blocks (all but one ahead) are all that
-// hides latency: 128 KB of an SM's shared memory in flight.
+// hides latency.
 template <typename Core>
-__global__ void __launch_bounds__(Core::kWarps * 32, 1) kv_blocks_kernel(const KvPass p) {
+__global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(const KvPass p, int* status) {
   using E = typename Core::E;
-  constexpr int kWarps = Core::kWarps, kStages = Core::kStages, kPacks = Core::kPacks, kPack = 16 / sizeof(E);
-  constexpr int kHalf = kBlk * kPacks * 16, kSlot = 2 * kHalf;
+  constexpr int kPacks = Core::kPacks, kPack = 16 / sizeof(E);
   constexpr int kRowsAt = 32 / kPacks > 1 ? 32 / kPacks : 1;      // rows of one copy instruction
   constexpr int kCopies = kBlk * kPacks / 32;
   extern __shared__ __align__(128) char ring_smem[];
-  __shared__ WorkerStart starts[kWarps];
-  __shared__ long long buf[kWarps];
-  __shared__ uint32_t there_of[kWarps][kStages];
+  __shared__ WorkerStart starts[Core::kMostWarps];
+  __shared__ long long buf[Core::kMostWarps];
+  __shared__ uint32_t there_of[Core::kMostWarps][kMostStages];
+  __shared__ uint64_t landed[Core::kMostWarps][kMostStages];
+  __shared__ int abort_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  char* ring = ring_smem + warp * (kStages * kSlot + Core::kScratch);
-  void* scratch = ring + kStages * kSlot;
   const KvAttention& a = p.a;
-  if (a.c.dim != Core::kDim) {               // what lies past a row's end is never copied: zeros
-    for (int i = lane; i < kStages * kSlot / 16; i += 32)
+  const int stages = p.stages, row_bytes = row_bytes_of<E>(a.c.dim), slot_bytes = 2 * kBlk * row_bytes;
+  char* ring = ring_smem + warp * (stages * slot_bytes + Core::kScratch);
+  void* scratch = ring + stages * slot_bytes;
+  if (a.c.dim % 16 != 0)                     // what lies past a row's end is never copied: zeros
+    for (int i = lane; i < stages * slot_bytes / 16; i += 32)
       reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
+  if (lane == 0) {
+    for (int i = 0; i < stages; ++i) mbar_init(&landed[warp][i], 32);
+    fence_mbar_init();
   }
+  if (threadIdx.x == 0) abort_word = 0;
+  const AbortFlag ab{&abort_word, status};
   pdl_wait();
-  const long long total = find_starts<kBlk, kWarps, kWarps>(p, starts, buf);
+  const long long total = find_starts<kBlk>(p, blockDim.x / 32, starts, buf);
   const int n = int(min((long long)p.workers, total));
   const int id = warp * gridDim.x + blockIdx.x;
   if (id >= n) {
@@ -375,10 +513,11 @@ __global__ void __launch_bounds__(Core::kWarps * 32, 1) kv_blocks_kernel(const K
     pdl_release();
     return;
   }
-  const long long begin = stretch(total, n, id), end = stretch(total, n, id + 1);
-  Cursor<kBlk> in;                                // of the loads
+  const long long end = stretch(total, n, id + 1);
+  const int count = int(end - stretch(total, n, id));
+  Cursor<kBlk> in;                           // of the loads
   in.start(p, starts[warp].tile, starts[warp].rest);
-  Cursor<kBlk> at = in;                           // of the sums
+  Cursor<kBlk> at = in;                      // of the sums
 
   // page and position in it of the lane's token (lane % 16) in the next block to load
   int j = 0, off = 0, pg = -1;
@@ -396,132 +535,165 @@ __global__ void __launch_bounds__(Core::kWarps * 32, 1) kv_blocks_kernel(const K
   };
   look_up(false);
   const uint32_t ring_at = smem_u32(ring);
+  const bool block_in_page = a.c.page % kBlk == 0;
+  const int pack = lane % kPacks, sub = kPacks < 32 ? lane / kPacks : 0;
+  long long head = (long long)(in.unit / p.gs) * a.c.sh + pack * kPack;      // of the next block
   const auto load = [&](int slot) {
     const bool there = pg >= 0 && pg < a.c.n_pages;
     const uint32_t all = __ballot_sync(~0u, there) & 0xffffu;
     if (lane == 0) there_of[warp][slot] = all;
-    const long long row = there ? pg * a.c.sp + off * a.c.st : 0;
-    const int c = lane % kPacks;
-    const long long head = (long long)(in.unit / p.gs) * a.c.sh + c * kPack;
     const E* K = static_cast<const E*>(a.c.K) + head;
     const E* V = static_cast<const E*>(a.c.V) + head;
-    const uint32_t dst = ring_at + slot * kSlot;
+    const uint32_t dst = ring_at + slot * slot_bytes + pack * 16, v_off = kBlk * row_bytes;
+    if (block_in_page && all == 0xffffu) {
+      // one page: rows a fixed step apart
+      const long long from = pg * a.c.sp + (off - (lane & 15) + sub) * a.c.st;
+      const E* k = K + from;
+      const E* v = V + from;
+      uint32_t to = dst + sub * row_bytes;
 #pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-      int r, cc = c;
-      if constexpr (kPacks <= 32) r = i * kRowsAt + lane / kPacks;
-      else r = i / (kPacks / 32), cc = c + i % (kPacks / 32) * 32;
-      const long long from = __shfl_sync(~0u, row, r) + (cc - c) * kPack;
-      if (cc * kPack < a.c.dim) {
-        const uint32_t to = dst + 16 * pack_at<kPacks>(r, cc);
-        if (all >> r & 1) {
-          cp_async16(to, K + from);
-          cp_async16(to + kHalf, V + from);
-        } else {                             // weights of 0 meet zeros
-          put_zeros16(to);
-          put_zeros16(to + kHalf);
+      for (int i = 0; i < kCopies; ++i) {
+        constexpr int kSame = kPacks > 32 ? kPacks / 32 : 1;         // instructions of one row
+        const int cc = i % kSame * 32;
+        if ((pack + cc) * kPack < a.c.dim) {
+          cp_async16(to + cc * 16, k + cc * kPack);
+          cp_async16(to + v_off + cc * 16, v + cc * kPack);
+        }
+        if (i % kSame == kSame - 1) {
+          k += kRowsAt * a.c.st;
+          v += kRowsAt * a.c.st;
+          to += kRowsAt * row_bytes;
+        }
+      }
+    } else {
+      const long long row = there ? pg * a.c.sp + off * a.c.st : 0;
+#pragma unroll 4
+      for (int i = 0; i < kCopies; ++i) {
+        constexpr int kSame = kPacks > 32 ? kPacks / 32 : 1;
+        const int cc = i % kSame * 32, r = i / kSame * kRowsAt + sub;
+        const long long from = __shfl_sync(~0u, row, r) + cc * kPack;
+        if ((pack + cc) * kPack < a.c.dim) {
+          const uint32_t to = dst + r * row_bytes + cc * 16;
+          if (all >> r & 1) {
+            cp_async16(to, K + from);
+            cp_async16(to + v_off, V + from);
+          } else {                           // weights of 0 meet zeros
+            put_zeros16(to);
+            put_zeros16(to + v_off);
+          }
         }
       }
     }
+    cp_async_arrive(&landed[warp][slot]);
   };
-  const long long count = end - begin;
-  long long loaded = 0;
+  int loaded = 0, load_slot = 0, slot = 0;
+  uint32_t round = 0;
   const auto load_next = [&]() {
     if (loaded < count) {
-      load(int(loaded % kStages));
-      if (++loaded < count) look_up(in.advance(p));
+      load(load_slot);
+      if (++load_slot == stages) load_slot = 0;
+      if (++loaded < count) {
+        const bool on = in.advance(p);
+        if (!on) head = (long long)(in.unit / p.gs) * a.c.sh + pack * kPack;
+        look_up(on);
+      }
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
   };
   __syncwarp();
-  for (int i = 0; i < kStages - 1; ++i) load_next();
+  for (int i = 0; i < stages - 1; ++i) load_next();
 
   Core core;
   int4 cut = make_int4(0, 0, 0, 0);
-  long long i = 0;
+  int i = 0;
   while (i < count) {
     // an item, or what the stretch has of it
     long long row0;
-    const int n_rows = tile_rows(p, at.tile, row0);
+    const int n_rows = max(tile_rows(p, at.tile, row0), 0);
     const int group = a.H / a.c.heads, kv = at.unit / p.gs, slice = (at.unit - kv * p.gs) * p.gw;
-    const int gw = min(p.gw, group - slice), h0 = kv * group + slice;
-    const int n_q = max(n_rows, 0) * p.gw;
-    const int b0 = at.b, b1 = int(min((long long)at.t.nb, b0 + (count - i)));
-    const auto query = [&](int q, int& r) {      // row of query q; whether its head exists
-      r = q / p.gw;
-      return q < n_q && q - r * p.gw < gw;
-    };
+    const int gw = min(p.gw, group - slice), h0 = kv * group + slice, n_q = n_rows * p.gw;
+    const Tile tile = at.t;
+    const int b0 = at.b, b1 = min(tile.nb, b0 + (count - i));
     core.load_q(p, row0, h0, n_q, gw, scratch);
     core.zero();
-    const bool last_here = b1 == at.t.nb;
-    const Tile tile = at.t;
-    const long long tile_id = at.tile;
-    const int unit = at.unit;
+    const bool last_here = b1 == tile.nb;
+    const int tile_id = at.tile, unit = at.unit;
+    bool on = false;
+    int least = 0;                               // tokens of the run that all rows see
     for (int b = b0; b < b1; ++b, ++i) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-      __syncwarp();
-      const int slot = int(i % kStages);
+      if (!on) {
+        const int tokens = at.lead >= 0 && tile.lead == at.lead ? tile.len : 0;
+        least = warp_min(lane < n_rows ? tokens : INT_MAX);
+        core.see(p, tokens, n_q);
+      }
+      // a wait that runs out is recorded and passed over: the loop goes on to its end
+      if (!mbar_try_wait(&landed[warp][slot], round & 1) && !*ab.smem)
+        mbar_wait(&landed[warp][slot], round & 1, ab);
+      __syncwarp();                              // all lanes are done with the slot that is filled next
       load_next();
       const uint32_t there = there_of[warp][slot];
-      // tokens of the block that each query sees
-      const int left = at.lead < 0 || tile.lead != at.lead ? 0 : tile.len - at.t0;
-      if constexpr (sizeof(E) == 2) {
-        const int g = lane >> 2;
-        int lim[2];
-        lim[0] = __shfl_sync(~0u, left, (g / p.gw) & 31);
-        lim[1] = __shfl_sync(~0u, left, ((g + 8) / p.gw) & 31);
-        if (g >= n_q) lim[0] = kBlk;
-        if (g + 8 >= n_q) lim[1] = kBlk;
-        core.add(p, ring_at + slot * kSlot, ring_at + slot * kSlot + kHalf, lim, there, scratch);
-      } else {
-        int lim[Core::kMaxQ];
-#pragma unroll
-        for (int q = 0; q < Core::kMaxQ; ++q) lim[q] = __shfl_sync(~0u, left, (q / p.gw) & 31);
-        core.add(p, ring + slot * kSlot, ring + slot * kSlot + kHalf, lim, there, scratch);
-      }
-      if (i + 1 < count) at.advance(p);
+      core.add(p, ring + slot * slot_bytes, row_bytes, at.t0, there,
+               least - at.t0 >= kBlk && there == 0xffffu, scratch);
+      if (++slot == stages) slot = 0, ++round;
+      if (i + 1 < count) on = at.advance(p);
     }
-    const bool whole = b0 == 0 && last_here;
-    const bool opens = b0 == 0 && !last_here;
+    const bool whole = b0 == 0 && last_here, opens = b0 == 0 && !last_here;
     const long long part = 2ll * id + (opens ? 1 : 0);
-    const auto out = [&](int q, float m, float l, bool writer) {
-      int r;
-      if (!query(q, r)) return part_out(p, 2ll * p.workers, 0, m, l, writer);   // nowhere: a spare slot
-      return whole ? row_out(p, row0 + r, h0 + q - r * p.gw, m, l, writer)
-                   : part_out(p, part, q, m, l, writer);
+    const auto out = [&](int q, int r, float m, float l) {
+      return whole ? row_out(p, row0 + r, h0 + q - r * p.gw, m, l, lane == 0)
+                   : part_out(p, part, q, m, l, lane == 0);
     };
-    uint32_t bad = core.finish(p, n_q, scratch, out);
-    if (n_rows > 1 && bad != 0) {
-      // Weights of 0 times a value that is not finite: such a value may lie in a token that the query
-      // does not see but another of the tile does.  Its tokens again, one by one.
-      for (int q = 0; q < n_q; ++q) {
-        int r;
-        if (!(bad >> q & 1) || !query(q, r)) continue;
+    // through the slot just used, which is filled again only in the next block's turn, into whole packs
+    const int dim = a.c.dim, used = slot == 0 ? stages - 1 : slot - 1;
+    float* sums = reinterpret_cast<float*>(ring + used * slot_bytes);
+    __syncwarp();
+    core.leave(n_q, dim, sums);
+    __syncwarp();
+#pragma unroll 1
+    for (int q = 0; q < n_q; ++q) {
+      const int r = q / p.gw;
+      if (q - r * p.gw >= gw) continue;
+      const float m = sums[n_q * (dim + 4) + 2 * q], l = sums[n_q * (dim + 4) + 2 * q + 1];
+      const KvRowOut to = out(q, r, m, l);
+      float odd = l - l;                         // 0 while all values are finite
+      for (int d = 4 * lane; d < dim; d += 128) {
+        const float4 x = *reinterpret_cast<const float4*>(sums + q * (dim + 4) + d);
+        const float v[4] = {x.x, x.y, x.z, x.w};
+        put<E, 4>(to, d, v);
+        odd = fmaf(0.f, (x.x + x.y) + (x.z + x.w), odd);
+      }
+      if (n_rows > 1 && __any_sync(~0u, !(odd == 0.f))) {
+        // Weights of 0 times a value that is not finite: such a value may lie in a token that the query
+        // does not see but another of the tile does.  Its tokens again, one by one.
         __syncwarp();
-        float x[kLaneDims], o[kLaneDims] = {}, m = kNegInf, l = 0.f;
+        float x[kLaneDims], o[kLaneDims] = {}, m2 = kNegInf, l2 = 0.f;
 #pragma unroll
         for (int e = 0; e < kLaneDims; ++e)
-          x[e] = e * 32 + lane < a.c.dim
-                     ? to_float(static_cast<const E*>(a.Q)[(row0 + r) * a.ldq + (h0 + q - r * p.gw) * a.c.dim + e * 32 + lane])
+          x[e] = e * 32 + lane < dim
+                     ? to_float(static_cast<const E*>(a.Q)[(row0 + r) * a.ldq + (h0 + q - r * p.gw) * dim + e * 32 + lane])
                      : 0.f;
         const int lead = __shfl_sync(~0u, tile.lead, r), len = __shfl_sync(~0u, tile.len, r);
         const int seq = __shfl_sync(~0u, tile.seq, r), first = __shfl_sync(~0u, tile.first, max(lead, 0));
         const long long t0 = (long long)(b0 - first) * kBlk, t1 = (long long)(b1 - first) * kBlk;
         if (len > 0)
-          walk_tokens<E>(a, seq, int(max(t0, 0ll)), int(min(t1, (long long)len)), kv, x, m, l, o);
-        const KvRowOut to = out(q, m, l, lane == 0);
+          walk_tokens<E>(a, seq, int(max(t0, 0ll)), int(min(t1, (long long)len)), kv, x, m2, l2, o);
+        const KvRowOut again = out(q, r, m2, l2);
 #pragma unroll
         for (int e = 0; e < kLaneDims; ++e) {
           const float v[1] = {o[e]};
-          if (e * 32 + lane < a.c.dim) put<E, 1>(to, e * 32 + lane, v);
+          if (e * 32 + lane < dim) put<E, 1>(again, e * 32 + lane, v);
         }
       }
+    }
+    __syncwarp();
+    if (dim % 16 != 0) {                         // zeros past the rows' ends again
+      for (int k = lane; k < slot_bytes / 16; k += 32) reinterpret_cast<uint4*>(sums)[k] = make_uint4(0, 0, 0, 0);
+      __syncwarp();
     }
     if (opens) {
       // the workers up to the one with the item's last block
       const long long item_end = end + (tile.nb - b1);
       const int last = int((item_end * n + total - 1) / total) - 1;
-      cut = make_int4(int(tile_id), unit, last - id + 1, 0);
+      cut = make_int4(tile_id, unit, last - id + 1, 0);
     }
   }
   if (lane == 0) p.cuts[id] = cut;
@@ -530,13 +702,14 @@ __global__ void __launch_bounds__(Core::kWarps * 32, 1) kv_blocks_kernel(const K
 }
 
 // -------------------------------------------------------------------------- join ---
-// Partial results of an item in order: warps take a query and some of its parts each, then add up.
+// Partial results of an item.  A query's largest m and sum of l come from its parts' scalars, a lane a part;
+// its warps (16 in all) add up some of its parts each, every load independent of the others, and
+// their sums meet in shared memory.  The order is the parts', whatever the timing.
 constexpr int kJoinWarps = 16;
 
 template <typename E>
 __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvPass p) {
-  __shared__ float part_o[kJoinWarps][kKvMaxDim];
-  __shared__ float part_m[kJoinWarps], part_l[kJoinWarps];
+  __shared__ float4 sums[kJoinWarps][kKvMaxDim / 4];
   pdl_wait_and_release();
   const int id = blockIdx.x;
   const int4 cut = p.cuts[id];
@@ -546,54 +719,72 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvPass p
   const int n_rows = tile_rows(p, cut.x, row0);
   const int group = p.a.H / p.a.c.heads, kv = cut.y / p.gs, slice = (cut.y - kv * p.gs) * p.gw;
   const int gw = min(p.gw, group - slice), h0 = kv * group + slice, n_q = n_rows * gw;
-  const int share = n_q >= kJoinWarps ? 1 : kJoinWarps / n_q;       // warps of a query
-  const int stride = p.max_q * (dim + 2);
-  for (int q0 = 0; q0 < n_q; q0 += kJoinWarps / share) {
+  const int share = n_q >= kJoinWarps ? 1 : kJoinWarps / n_q, at_once = kJoinWarps / share;
+  const long long stride = part_floats(p.max_q, dim);
+  const float* first = p.parts + (2ll * id + 1) * stride;          // part 0; part k: first + k (2k - 1) ...
+  const float* rest = p.parts + 2ll * id * stride;                 // ... from worker id + k's place
+  for (int q0 = 0; q0 < n_q; q0 += at_once) {
     const int i = q0 + warp / share, sub = warp % share;
-    const bool there = warp / share < kJoinWarps / share && i < n_q;
+    const bool there = warp / share < at_once && i < n_q;
     const int r = there ? i / gw : 0, h = there ? i - r * gw : 0, q = r * p.gw + h;
-    float m = kNegInf, l = 0.f, o[kLaneDims] = {};
-    if (there)
+    float m = kNegInf, l = 0.f;
+    float4 o[2] = {};
+    if (there) {
+      const auto part = [&](int k) { return k == 0 ? first : rest + 2ll * k * stride; };
+      for (int k = lane; k < cut.z; k += 32) m = fmaxf(m, part(k)[p.max_q * dim + 2 * q]);
+      m = warp_max(m);
+      const float ref = m == kNegInf ? 0.f : m;
+      for (int k0 = 0; k0 < cut.z; k0 += 32) {
+        float w = 0.f;
+        if (k0 + lane < cut.z) {
+          const float2 ml = *reinterpret_cast<const float2*>(part(k0 + lane) + p.max_q * dim + 2 * q);
+          w = ml.x == ref ? 1.f : ex2(ml.x - ref);
+          l = fmaf(ml.y, w, l);
+        }
+        const int n = min(32, cut.z - k0);
 #pragma unroll 4
-      for (int k = sub; k < cut.z; k += share) {
-        const float* base = p.parts + (long long)(k == 0 ? 2 * id + 1 : 2 * (id + k)) * stride;
-        const float m2 = base[2 * q], l2 = base[2 * q + 1];
-        const float* o2 = base + 2 * p.max_q + q * dim;
-        float c, c2;
-        join_state(m, l, c, c2, m2, l2);
+        for (int k = sub; k < n; k += share) {
+          const float f = __shfl_sync(~0u, w, k);
+          const float4* x = reinterpret_cast<const float4*>(part(k0 + k) + q * dim);
 #pragma unroll
-        for (int e = 0; e < kLaneDims; ++e)
-          if (e * 32 + lane < dim) o[e] = o[e] * c + o2[e * 32 + lane] * c2;
+          for (int e = 0; e < 2; ++e)
+            if (4 * (lane + 32 * e) < dim) {
+              const float4 y = x[lane + 32 * e];
+              o[e] = make_float4(fmaf(y.x, f, o[e].x), fmaf(y.y, f, o[e].y), fmaf(y.z, f, o[e].z), fmaf(y.w, f, o[e].w));
+            }
+        }
       }
+      l = warp_reduce(l, AddOp());
+    }
     if (share > 1) {
 #pragma unroll
-      for (int e = 0; e < kLaneDims; ++e)
-        if (e * 32 + lane < dim) part_o[warp][e * 32 + lane] = o[e];
-      if (lane == 0) part_m[warp] = m, part_l[warp] = l;
+      for (int e = 0; e < 2; ++e)
+        if (4 * (lane + 32 * e) < dim) sums[warp][lane + 32 * e] = o[e];
       __syncthreads();
       if (there && sub == 0)
-        for (int k = 1; k < share; ++k) {
-          float c, c2;
-          join_state(m, l, c, c2, part_m[warp + k], part_l[warp + k]);
+        for (int k = 1; k < share; ++k)
 #pragma unroll
-          for (int e = 0; e < kLaneDims; ++e)
-            if (e * 32 + lane < dim) o[e] = o[e] * c + part_o[warp + k][e * 32 + lane] * c2;
-        }
+          for (int e = 0; e < 2; ++e)
+            if (4 * (lane + 32 * e) < dim) {
+              const float4 y = sums[warp + k][lane + 32 * e];
+              o[e] = make_float4(o[e].x + y.x, o[e].y + y.y, o[e].z + y.z, o[e].w + y.w);
+            }
       __syncthreads();
     }
     if (there && sub == 0) {
       const KvRowOut to = row_out(p, row0 + r, h0 + h, m, l, lane == 0);
 #pragma unroll
-      for (int e = 0; e < kLaneDims; ++e) {
-        const float v[1] = {o[e]};
-        if (e * 32 + lane < dim) put<E, 1>(to, e * 32 + lane, v);
+      for (int e = 0; e < 2; ++e) {
+        const float v[4] = {o[e].x, o[e].y, o[e].z, o[e].w};
+        if (4 * (lane + 32 * e) < dim) put<E, 4>(to, 4 * (lane + 32 * e), v);
       }
     }
   }
 }
 
 // ---------------------------------------------------------------------- launches ---
-constexpr int kMostWorkers = 8 * kKvMostSms;
+constexpr int kMostWorkers = 16 * kKvMostSms;
+constexpr int kRingsMost = 220 * 1024;       // bytes of all rings of a block
 
 template <typename E>
 cudaError_t run_join(const KvPass& p, cudaStream_t s) {
@@ -601,26 +792,31 @@ cudaError_t run_join(const KvPass& p, cudaStream_t s) {
 }
 
 template <typename Core>
-cudaError_t run_pass(KvPass p, int sms, cudaStream_t s) {
-  constexpr int kRing = Core::kWarps * (Core::kStages * 2 * kBlk * Core::kPacks * 16 + Core::kScratch);
-  static_assert(kRing <= 220 * 1024, "the rings fit an SM");
+cudaError_t run_pass(KvPass p, int sms, int* status, cudaStream_t s) {
+  using E = typename Core::E;
   shape_pass(p, Core::kMaxQ, 32, kBlk);
-  const int grid = std::min(sms, kKvMostSms);
-  p.workers = grid * Core::kWarps;
+  // as many warps as have two blocks each, then as many blocks
+  const int slot = 2 * kBlk * row_bytes_of<E>(p.a.c.dim);
+  const char* kvw = getenv("KVW"); /*EXP*/
+  const int warps = std::min(kvw ? std::min(atoi(kvw), Core::kMostWarps) : Core::kMostWarps, kRingsMost / (2 * slot + Core::kScratch));
+  p.stages = std::min(kMostStages, (kRingsMost / warps - Core::kScratch) / slot);
+  const int grid = std::min(sms, kKvMostSms), ring = warps * (p.stages * slot + Core::kScratch);
+  p.workers = grid * warps;
   const cudaError_t e = cudaFuncSetAttribute(kv_blocks_kernel<Core>,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
+                                             cudaFuncAttributeMaxDynamicSharedMemorySize, kRingsMost);
   if (e != cudaSuccess) return e;
-  const cudaError_t f = launch_pdl(kv_blocks_kernel<Core>, dim3(grid), dim3(Core::kWarps * 32), kRing, s, p);
-  return f != cudaSuccess ? f : run_join<typename Core::E>(p, s);
+  const cudaError_t f = launch_pdl(kv_blocks_kernel<Core>, dim3(grid), dim3(warps * 32), ring, s, p, status);
+  return f != cudaSuccess ? f : run_join<E>(p, s);
 }
 
 template <int kDim>
-cudaError_t run_f32(const KvPass& p, int sms, cudaStream_t s) {
-  const int group = p.a.H / p.a.c.heads;
-  const long long q = std::min<long long>(p.part.per, p.a.N) * group;
-  if (q <= 1) return run_pass<F32Core<kDim, 1>>(p, sms, s);
-  if (q <= 4) return run_pass<F32Core<kDim, 4>>(p, sms, s);
-  return run_pass<F32Core<kDim, 8>>(p, sms, s);
+cudaError_t run_dim(const KvPass& p, int sms, int* status, cudaStream_t s) {
+  const long long q = std::min<long long>(p.part.per, p.a.N) * (p.a.H / p.a.c.heads);
+  if (p.a.c.dtype == 0)
+    return q <= 8 ? run_pass<FewCore<kDim>>(p, sms, status, s) : run_pass<ManyCore<kDim>>(p, sms, status, s);
+  return q <= 1   ? run_pass<F32Core<kDim, 1>>(p, sms, status, s)
+         : q <= 4 ? run_pass<F32Core<kDim, 4>>(p, sms, status, s)
+                  : run_pass<F32Core<kDim, 8>>(p, sms, status, s);
 }
 
 cudaError_t run_part(KvPass p, int sms, int* status, cudaStream_t s) {
@@ -630,11 +826,9 @@ cudaError_t run_part(KvPass p, int sms, int* status, cudaStream_t s) {
     const cudaError_t e = launch_kv_tc(p, sms, status, s);
     return e != cudaSuccess ? e : run_join<__nv_bfloat16>(p, s);
   }
-  if (p.a.c.dtype == 0)
-    return dim <= 32 ? run_pass<Bf16Core<32>>(p, sms, s) : dim <= 64 ? run_pass<Bf16Core<64>>(p, sms, s)
-           : dim <= 128 ? run_pass<Bf16Core<128>>(p, sms, s) : run_pass<Bf16Core<256>>(p, sms, s);
-  return dim <= 32 ? run_f32<32>(p, sms, s) : dim <= 64 ? run_f32<64>(p, sms, s)
-         : dim <= 128 ? run_f32<128>(p, sms, s) : run_f32<256>(p, sms, s);
+  return dim <= 64    ? run_dim<64>(p, sms, status, s)
+         : dim <= 128 ? run_dim<128>(p, sms, status, s)
+                      : run_dim<256>(p, sms, status, s);
 }
 
 size_t up16(size_t x) { return (x + 15) / 16 * 16; }
@@ -646,8 +840,8 @@ struct Layout {
 Layout layout(long long N, int H, int dim, bool prefix) {
   Layout y;
   size_t at = 0;
-  y.parts = at;
-  at += up16(size_t(2 * kMostWorkers + 8) * 16 * (dim + 2) * sizeof(float));
+  y.parts = at;                              // 16 warps of 8 queries, 8 of 16, or one of 128 an SM
+  at += up16(size_t(2 * kMostWorkers + 8) * 8 * (dim + 4) * sizeof(float));
   y.cuts = at;
   at += size_t(kMostWorkers) * sizeof(int4);
   y.pre_o = at;

@@ -43,7 +43,7 @@ struct Cfg {
   static constexpr size_t kBig = size_t(kSlots) * kTile + kQBufs * kQBytes + kPBufs * kPBytes;
 };
 
-struct KvMisc {
+struct alignas(16) KvMisc {
   uint64_t full[8], empty[8], q_empty[2], s_full[2], s_empty[2], p_full[2], pv_done[2], drain;
   uint32_t there[kInfo][kCopyWarps];      // tokens of a tile whose page exists
   uint32_t info[kInfo];                   // 1: first of its item here, 2: last
@@ -61,6 +61,7 @@ struct KvSmem {
   float ref[C::kNQ];                      // references (scores)
   int vis[C::kNQ];                        // tokens of the run that a query sees
 };
+static_assert(sizeof(KvMisc) % 16 == 0, "what follows is read as packs of 16 bytes");
 
 template <class C>
 constexpr size_t smem_bytes() { return C::kBig + sizeof(KvSmem<C>); }
@@ -206,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
   }
   tc_fence_before();
   pdl_wait();
-  const long long total = find_starts<kBlk, kWarps, 1>(p, &mi.start, mi.buf);   // barriers within
+  const long long total = find_starts<kBlk>(p, 1, &mi.start, mi.buf);   // barriers within
   tc_fence_after();
   const uint32_t tmem = mi.tmem;
   const int n_workers = int(min((long long)p.workers, total)), id = blockIdx.x;
@@ -231,8 +232,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
     // What a tile's copies need.  The table is read a tile ahead: a page's number takes as long to come
     // as its rows.
     struct Next {
-      int pg, off, unit;
-      long long tile;
+      int pg, off, unit, tile;
       bool first, last;
     } next = {-1, 0, 0, 0, true, true};
     int j = 0, off = 0;
@@ -393,8 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       const int group_q = a.H / a.c.heads, kv = at.unit / p.gs, slice = (at.unit - kv * p.gs) * p.gw;
       const int gw = min(p.gw, group_q - slice), h0 = kv * group_q + slice, n_q = n_rows * p.gw;
       const Tile tile = at.t;
-      const long long tile_id = at.tile;
-      const int unit = at.unit, b0 = at.b, b1 = min(tile.nb, b0 + (count - i));
+      const int tile_id = at.tile, unit = at.unit, b0 = at.b, b1 = min(tile.nb, b0 + (count - i));
       const int i0 = i;
       if (tid < kHalf) sm.ref[q0 + tid] = kNoRef;
 #pragma unroll
@@ -595,7 +594,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       if (opens) {
         // the workers up to the one with the item's last block
         const long long item_end = end + (tile.nb - b1);
-        cut = make_int4(int(tile_id), unit, int((item_end * n_workers + total - 1) / total) - 1 - id + 1, 0);
+        cut = make_int4(tile_id, unit, int((item_end * n_workers + total - 1) / total) - 1 - id + 1, 0);
       }
     }
     if (threadIdx.x == 0 && count > 0) p.cuts[id] = cut;

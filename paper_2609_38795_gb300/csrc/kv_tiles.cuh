@@ -36,11 +36,12 @@ struct KvPass {
   KvPart part;
   int gw, gs, n_units;             // n_units = heads * gs
   int per, tg, rows;
-  long long n_tiles;
+  int n_tiles;
   int step_pg, step_tok;           // kBlk tokens on: pages and tokens
   int workers;
+  int stages;                      // blocks of a worker's ring
   int max_q;                       // queries of an item, at most
-  float* parts;                    // [2 * workers][max_q * (dim + 2)]: m and l of all queries, then o
+  float* parts;                    // [2 * workers][part_floats]: o of all queries, then m and l
   int4* cuts;                      // [workers]: (tile, unit, parts) of the item that a worker begins
                                    // and does not end; 0 parts: none
   float* put_o;                    // prefix pass: where results go, [N, H, dim] and [N, H, 2]
@@ -88,55 +89,43 @@ ALR_DEV KvRowOut row_out(const KvPass& p, long long r, int h, float m, float l, 
   return o;
 }
 
-// Partial results of query q in slot `slot`.
-ALR_DEV KvRowOut part_out(const KvPass& p, long long slot, int q, float m, float l, bool writer) {
-  float* base = p.parts + slot * p.max_q * (p.a.c.dim + 2);
-  if (writer) base[2 * q] = m, base[2 * q + 1] = l;
-  return {1.f, 0.f, nullptr, base + 2 * p.max_q + (long long)q * p.a.c.dim, nullptr};
+__host__ __device__ inline long long part_floats(int max_q, int dim) {
+  return (long long)max_q * dim + (2 * max_q + 3) / 4 * 4;
 }
 
-// kW consecutive elements from d on.
+// Partial results of query q in slot `slot`.
+ALR_DEV KvRowOut part_out(const KvPass& p, long long slot, int q, float m, float l, bool writer) {
+  float* base = p.parts + slot * part_floats(p.max_q, p.a.c.dim);
+  float* ml = base + p.max_q * p.a.c.dim;
+  if (writer) ml[2 * q] = m, ml[2 * q + 1] = l;
+  return {1.f, 0.f, nullptr, base + q * p.a.c.dim, nullptr};
+}
+
+// kW consecutive elements from d on (a multiple of kW).
 template <typename E, int kW>
 ALR_DEV void put(const KvRowOut& o, int d, const float (&v)[kW]) {
   struct alignas(kW * sizeof(float)) F { float e[kW]; };
   struct alignas(kW * sizeof(E)) T { E e[kW]; };
-  F x;
-#pragma unroll
-  for (int i = 0; i < kW; ++i) x.e[i] = v[i] * o.f;
   if (o.dst_f != nullptr) {
-    if constexpr (kW > 2) {      // partial rows begin at multiples of 8 bytes
+    F x;
 #pragma unroll
-      for (int i = 0; i < kW; i += 2) *reinterpret_cast<float2*>(o.dst_f + d + i) = {x.e[i], x.e[i + 1]};
-    } else {
-      *reinterpret_cast<F*>(o.dst_f + d) = x;
-    }
+    for (int i = 0; i < kW; ++i) x.e[i] = v[i];
+    *reinterpret_cast<F*>(o.dst_f + d) = x;
     return;
   }
-  if (o.pre != nullptr) {
-#pragma unroll
-    for (int i = 0; i < kW; ++i) x.e[i] = fmaf(o.pre[d + i], o.f_pre, x.e[i]);
-  }
+  F pre = {};
+  if (o.pre != nullptr) pre = *reinterpret_cast<const F*>(o.pre + d);
   T y;
 #pragma unroll
-  for (int i = 0; i < kW; ++i) y.e[i] = E(x.e[i]);
+  for (int i = 0; i < kW; ++i) y.e[i] = E(fmaf(pre.e[i], o.f_pre, v[i] * o.f));
   *reinterpret_cast<T*>(static_cast<E*>(o.dst) + d) = y;
-}
-
-// Join two running results.
-ALR_DEV void join_state(float& m, float& l, float& c, float& c2, float m2, float l2) {
-  const float top = m > m2 ? m : m2, ref = top == kNegInf ? 0.f : top;
-  c = m == ref ? 1.f : ex2(m - ref);
-  c2 = m2 == ref ? 1.f : ex2(m2 - ref);
-  l = l * c + l2 * c2;
-  m = top;
 }
 
 // ---------------------------------------------------------------------- schedule ---
 // First row and row count of a tile.
-ALR_DEV int tile_rows(const KvPass& p, long long tile, long long& row0) {
-  const long long g = tile / p.tg;
-  const int i = int(tile - g * p.tg);
-  row0 = g * p.per + (long long)i * p.rows;
+ALR_DEV int tile_rows(const KvPass& p, int tile, long long& row0) {
+  const int g = tile / p.tg, i = tile - g * p.tg;
+  row0 = (long long)g * p.per + (long long)i * p.rows;
   return int(min((long long)min(p.rows, p.per - i * p.rows), p.a.N - row0));
 }
 
@@ -145,7 +134,7 @@ ALR_DEV int blocks_of(int tokens) { return tokens / kBlk + (tokens % kBlk != 0);
 
 // Blocks of a tile, counted by one thread.
 template <int kBlk>
-ALR_DEV int tile_blocks(const KvPass& p, long long tile) {
+ALR_DEV int tile_blocks(const KvPass& p, int tile) {
   long long row0;
   const int n = tile_rows(p, tile, row0);
   int nb = 0, cur = 0, most = 0;
@@ -181,7 +170,7 @@ struct Tile {
 };
 
 template <int kBlk>
-ALR_DEV Tile load_tile(const KvPass& p, long long tile) {
+ALR_DEV Tile load_tile(const KvPass& p, int tile) {
   const int lane = threadIdx.x & 31;
   long long row0;
   const int n = tile_rows(p, tile, row0);
@@ -209,9 +198,9 @@ ALR_DEV Tile load_tile(const KvPass& p, long long tile) {
 template <int kBlk>
 struct Cursor {
   Tile t;
-  long long tile;
-  int unit, b;
+  int tile, unit, b;
   int lead, seq, most, t0;      // the run's first lane, sequence, tokens; the block's first token
+  int run_end;                  // first block of the next run
 
   ALR_DEV void enter() {
     const uint32_t m = __ballot_sync(~0u, t.first <= b);
@@ -220,9 +209,10 @@ struct Cursor {
     seq = __shfl_sync(~0u, t.seq, from);
     most = lead < 0 ? 0 : __shfl_sync(~0u, t.most, from);
     t0 = lead < 0 ? 0 : (b - __shfl_sync(~0u, t.first, from)) * kBlk;
+    run_end = min(warp_min(t.first > b ? t.first : INT_MAX), t.nb);
   }
   // rest: blocks into the tile's items
-  ALR_DEV void start(const KvPass& p, long long tile_, long long rest) {
+  ALR_DEV void start(const KvPass& p, int tile_, long long rest) {
     tile = tile_;
     t = load_tile<kBlk>(p, tile);
     unit = int(rest / t.nb);
@@ -231,19 +221,17 @@ struct Cursor {
   }
   // To the next block; whether it continues the run.
   ALR_DEV bool advance(const KvPass& p) {
-    if (++b < t.nb) {
-      if (__ballot_sync(~0u, t.first == b) == 0) {
-        t0 += kBlk;
-        return true;
-      }
-      enter();
-      return false;
+    if (++b < run_end) {
+      t0 += kBlk;
+      return true;
     }
-    b = 0;
-    if (++unit == p.n_units) {
-      unit = 0;
-      ++tile;
-      t = load_tile<kBlk>(p, tile);
+    if (b == t.nb) {
+      b = 0;
+      if (++unit == p.n_units) {
+        unit = 0;
+        ++tile;
+        t = load_tile<kBlk>(p, tile);
+      }
     }
     enter();
     return false;
@@ -254,45 +242,49 @@ struct Cursor {
 ALR_DEV long long stretch(long long total, int n, long long w) { return total * w / n; }
 
 // Every block of the kernel counts the blocks of all tiles (a thread some consecutive ones), finds its
-// workers' starts, and leaves them in `at`: (tile, blocks into the tile's items).  Returns the total.
+// n_own workers' starts (worker w of block i is w gridDim + i), and leaves them in `at`: (tile, blocks
+// into the tile's items).  buf: an entry a warp.  Returns the total.
 struct WorkerStart {
-  long long tile, rest;
+  long long begin;             // block of the line
+  long long rest;
+  int tile;
 };
 
-template <int kBlk, int kWarps, int kWorkers>
-ALR_DEV long long find_starts(const KvPass& p, WorkerStart* at, long long* buf) {
-  constexpr int kThreads = kWarps * 32;
-  const int tid = threadIdx.x;
-  const long long per = (p.n_tiles + kThreads - 1) / kThreads;
-  const long long a = min((long long)tid * per, p.n_tiles), e = min(a + per, p.n_tiles);
+template <int kBlk>
+ALR_DEV long long find_starts(const KvPass& p, int n_own, WorkerStart* at, long long* buf) {
+  const int tid = threadIdx.x, n_threads = blockDim.x, n_warps = n_threads / 32;
+  const int per = (p.n_tiles + n_threads - 1) / n_threads;
+  const int a = int(min((long long)tid * per, (long long)p.n_tiles)), e = min(a + per, p.n_tiles);
   long long own = 0;
-  for (long long i = a; i < e; ++i) own += tile_blocks<kBlk>(p, i);
+  for (int i = a; i < e; ++i) own += tile_blocks<kBlk>(p, i);
   // exclusive sums over the threads
   const int lane = tid & 31, warp = tid >> 5;
   const long long up = warp_scan(own);
   if (lane == 31) buf[warp] = up;
   __syncthreads();
   long long before = up - own, total = 0;
-  for (int i = 0; i < kWarps; ++i) {
+  for (int i = 0; i < n_warps; ++i) {
     if (i < warp) before += buf[i];
     total += buf[i];
   }
   before *= p.n_units;
   own *= p.n_units;
   total *= p.n_units;
-  const int n = int(min((long long)p.workers, total));
-  for (int w = 0; w < kWorkers; ++w) {
-    const long long id = (long long)w * gridDim.x + blockIdx.x;
-    if (id >= n) break;
-    long long rest = stretch(total, n, id) - before;
+  const long long n = min((long long)p.workers, total);
+  if (tid < n_own) at[tid].begin = stretch(total, int(n), (long long)tid * gridDim.x + blockIdx.x);
+  __syncthreads();
+  for (int w = 0; w < n_own; ++w) {
+    if ((long long)w * gridDim.x + blockIdx.x >= n) break;
+    long long rest = at[w].begin - before;
     if (rest < 0 || rest >= own) continue;
-    long long tile = a;
+    int tile = a;
     for (;; ++tile) {
       const long long len = (long long)tile_blocks<kBlk>(p, tile) * p.n_units;
       if (rest < len) break;
       rest -= len;
     }
-    at[w] = {tile, rest};
+    at[w].tile = tile;
+    at[w].rest = rest;
   }
   __syncthreads();
   return total;
@@ -339,7 +331,7 @@ inline void shape_pass(KvPass& p, int max_q, int max_rows, int blk) {
   p.rows = int(least(least(max_q / p.gw, max_rows), p.per));
   p.tg = (p.per + p.rows - 1) / p.rows;
   p.rows = (p.per + p.tg - 1) / p.tg;
-  p.n_tiles = (p.a.N + p.per - 1) / p.per * p.tg;
+  p.n_tiles = int((p.a.N + p.per - 1) / p.per * p.tg);
   p.step_pg = blk / p.a.c.page;
   p.step_tok = blk % p.a.c.page;
   p.max_q = max_q;
