@@ -475,6 +475,80 @@ __host__ __device__ constexpr int row_bytes_of(int dim) {
 
 constexpr int kMostStages = 8;
 
+// -------------------------------------------------------------------------- join ---
+// Partial results of an item.  A query's largest m and the weights of its parts come from the parts'
+// scalars, a lane a part; then a warp adds up all or some of the parts, each load independent of
+// the others.  The order is the parts', whatever the timing.
+constexpr int kJoinWarps = 16;
+
+struct JoinItem {
+  long long row0;
+  int n_rows, gw, h0, n_q;                   // n_q: queries that exist
+  ALR_DEV JoinItem(const KvPass& p, const int4& cut) {
+    n_rows = tile_rows(p, cut.x, row0);
+    const int group = p.a.H / p.a.c.heads, kv = cut.y / p.gs, slice = (cut.y - kv * p.gs) * p.gw;
+    gw = min(p.gw, group - slice);
+    h0 = kv * group + slice;
+    n_q = n_rows * gw;
+  }
+  ALR_DEV int query(const KvPass& p, int k, int& r) const {   // place of the k-th
+    r = k / gw;
+    return r * p.gw + (k - r * gw);
+  }
+};
+
+struct JoinSums {
+  float m = kNegInf, l = 0.f;                // l: to be added over the lanes
+  float4 o[2] = {};
+};
+
+// Parts 0 to n - 1 of query q: part k in place slot0 + 2 k, but part 0 in slot0 + 1 if `opened`; o of
+// those k = sub, sub + share, ...
+ALR_DEV void join_parts(const KvPass& p, const float* parts, int slot0, bool opened, int n, int q, int sub,
+                        int share, JoinSums& s) {
+  const int lane = threadIdx.x & 31, dim = p.a.c.dim;
+  const long long stride = part_floats(p.max_q, dim);
+  const auto part = [&](int k) { return parts + (slot0 + (k == 0 && opened ? 1 : 2 * k)) * stride; };
+  float2 first = {kNegInf, 0.f};
+  if (lane < n) {
+    first = *reinterpret_cast<const float2*>(part(lane) + p.max_q * dim + 2 * q);
+  }
+  float m = first.x;
+  for (int k = lane + 32; k < n; k += 32) m = fmaxf(m, part(k)[p.max_q * dim + 2 * q]);
+  s.m = warp_max(m);
+  const float ref = s.m == kNegInf ? 0.f : s.m;
+  for (int k0 = 0; k0 < n; k0 += 32) {
+    float w = 0.f;
+    if (k0 + lane < n) {
+      if (k0 > 0) first = *reinterpret_cast<const float2*>(part(k0 + lane) + p.max_q * dim + 2 * q);
+      w = first.x == ref ? 1.f : ex2(first.x - ref);
+      s.l = fmaf(first.y, w, s.l);
+    }
+    const int some = min(32, n - k0);
+#pragma unroll 4
+    for (int k = sub; k < some; k += share) {
+      const float f = __shfl_sync(~0u, w, k);
+      const float4* x = reinterpret_cast<const float4*>(part(k0 + k) + q * dim);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (4 * (lane + 32 * e) < dim) {
+          const float4 y = x[lane + 32 * e];
+          s.o[e] = make_float4(fmaf(y.x, f, s.o[e].x), fmaf(y.y, f, s.o[e].y), fmaf(y.z, f, s.o[e].z), fmaf(y.w, f, s.o[e].w));
+        }
+    }
+  }
+}
+
+template <typename E>
+ALR_DEV void put_sums(const KvPass& p, const KvRowOut& to, const JoinSums& s) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const float v[4] = {s.o[e].x, s.o[e].y, s.o[e].z, s.o[e].w};
+    if (4 * (lane + 32 * e) < p.a.c.dim) put<E, 4>(to, 4 * (lane + 32 * e), v);
+  }
+}
+
 // Each warp is a worker with a ring of its own: no block-wide barrier after the start, so warps in
 // different items never wait for one another, and a ring's blocks (all but one ahead) are all that
 // hides latency.
@@ -485,38 +559,38 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
   constexpr int kRowsAt = 32 / kPacks > 1 ? 32 / kPacks : 1;      // rows of one copy instruction
   constexpr int kCopies = kBlk * kPacks / 32;
   extern __shared__ __align__(128) char ring_smem[];
-  __shared__ WorkerStart starts[Core::kMostWarps];
+  __shared__ WorkerStart starts[Core::kMostWarps + 1];
   __shared__ long long buf[Core::kMostWarps];
   __shared__ uint32_t there_of[Core::kMostWarps][kMostStages];
   __shared__ uint64_t landed[Core::kMostWarps][kMostStages];
+  __shared__ int4 cut_of[Core::kMostWarps];  // (tile, unit, parts) of the item that a worker leaves open
+  __shared__ int4 head_cut;                  // ... of the item that the block's first worker continues
   __shared__ int abort_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const KvAttention& a = p.a;
   const int stages = p.stages, row_bytes = row_bytes_of<E>(a.c.dim), slot_bytes = 2 * kBlk * row_bytes;
   char* ring = ring_smem + warp * (stages * slot_bytes + Core::kScratch);
   void* scratch = ring + stages * slot_bytes;
-  if (a.c.dim % 16 != 0)                     // what lies past a row's end is never copied: zeros
-    for (int i = lane; i < stages * slot_bytes / 16; i += 32)
-      reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
   if (lane == 0) {
     for (int i = 0; i < stages; ++i) mbar_init(&landed[warp][i], 32);
     fence_mbar_init();
   }
-  if (threadIdx.x == 0) abort_word = 0;
+  if (threadIdx.x == 0) {
+    abort_word = 0;
+    head_cut = make_int4(0, 0, 0, 0);
+  }
+  if (lane == 0) cut_of[warp] = make_int4(0, 0, 0, 0);
   const AbortFlag ab{&abort_word, status};
   pdl_wait();
-  const long long total = find_starts<kBlk>(p, blockDim.x / 32, starts, buf);
-  const int n = int(min((long long)p.workers, total));
-  const int id = warp * gridDim.x + blockIdx.x;
-  if (id >= n) {
-    if (id < p.workers && lane == 0) p.cuts[id] = make_int4(0, 0, 0, 0);
-    pdl_release();
-    return;
-  }
-  const long long end = stretch(total, n, id + 1);
-  const int count = int(end - stretch(total, n, id));
-  Cursor<kBlk> in;                           // of the loads
-  in.start(p, starts[warp].tile, starts[warp].rest);
+  const Line line = find_starts<kBlk>(p, starts, reinterpret_cast<long long*>(ring_smem), buf);
+  if (a.c.dim % 16 != 0)                     // what lies past a row's end is never copied: zeros
+    for (int i = lane; i < stages * slot_bytes / 16; i += 32)
+      reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
+  const int id0 = blockIdx.x * line.per_block, id = id0 + warp;
+  const bool works = warp < line.per_block && id < line.n;
+  const int count = works ? int(starts[warp + 1].block - starts[warp].block) : 0;
+  Cursor<kBlk> in{};                         // of the loads
+  if (count > 0) in.start(p, starts[warp].tile, starts[warp].unit, starts[warp].b);
   Cursor<kBlk> at = in;                      // of the sums
 
   // page and position in it of the lane's token (lane % 16) in the next block to load
@@ -533,7 +607,7 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
     }
     pg = in.t0 + (lane & 15) < in.most ? a.table[(long long)in.seq * a.cols + j] : -1;
   };
-  look_up(false);
+  if (count > 0) look_up(false);
   const uint32_t ring_at = smem_u32(ring);
   const bool block_in_page = a.c.page % kBlk == 0;
   const int pack = lane % kPacks, sub = kPacks < 32 ? lane / kPacks : 0;
@@ -603,7 +677,6 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
   for (int i = 0; i < stages - 1; ++i) load_next();
 
   Core core;
-  int4 cut = make_int4(0, 0, 0, 0);
   int i = 0;
   while (i < count) {
     // an item, or what the stretch has of it
@@ -637,10 +710,10 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
       if (i + 1 < count) on = at.advance(p);
     }
     const bool whole = b0 == 0 && last_here, opens = b0 == 0 && !last_here;
-    const long long part = 2ll * id + (opens ? 1 : 0);
+    const int part = 2 * id + (opens ? 1 : 0);
     const auto out = [&](int q, int r, float m, float l) {
       return whole ? row_out(p, row0 + r, h0 + q - r * p.gw, m, l, lane == 0)
-                   : part_out(p, part, q, m, l, lane == 0);
+                   : part_out(p, p.parts, part, q, m, l, lane == 0);
     };
     // through the slot just used, which is filled again only in the next block's turn, into whole packs
     const int dim = a.c.dim, used = slot == 0 ? stages - 1 : slot - 1;
@@ -689,24 +762,43 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
       for (int k = lane; k < slot_bytes / 16; k += 32) reinterpret_cast<uint4*>(sums)[k] = make_uint4(0, 0, 0, 0);
       __syncwarp();
     }
-    if (opens) {
-      // the workers up to the one with the item's last block
-      const long long item_end = end + (tile.nb - b1);
-      const int last = int((item_end * n + total - 1) / total) - 1;
-      cut = make_int4(tile_id, unit, last - id + 1, 0);
+    if (!whole && lane == 0) {
+      const int parts = last_here ? 1 : line.last_before(line.start(id + 1) + (tile.nb - b1)) - id + 1;
+      if (opens) cut_of[warp] = make_int4(tile_id, unit, parts, 0);
+      else if (warp == 0) head_cut = make_int4(tile_id, unit, parts, 0);
     }
   }
-  if (lane == 0) p.cuts[id] = cut;
   asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  // ---- the items that the block's workers share: a warp a query
+  int4 cut = make_int4(0, 0, 0, 0);
+  int turn = 0;
+  for (int w = -1; w < line.per_block; ++w) {
+    const int4 c = w < 0 ? head_cut : cut_of[w];
+    if (c.z == 0) continue;
+    const JoinItem t(p, c);
+    const int from = w < 0 ? 0 : w, here = min(c.z, line.per_block - from), slot0 = 2 * (id0 + from);
+    const bool inside = w >= 0 && c.z == here;
+    const int to_slot = 2 * blockIdx.x + (w < 0 ? 0 : 1);
+    if (w >= 0 && !inside)
+      cut = make_int4(c.x, c.y, (id0 + w + c.z - 1) / line.per_block - int(blockIdx.x) + 1, 0);
+    for (int k = 0; k < t.n_q; ++k, ++turn) {
+      if (turn % (blockDim.x / 32) != warp) continue;
+      int r;
+      const int q = t.query(p, k, r);
+      JoinSums s;
+      join_parts(p, p.parts, slot0, w >= 0, here, q, 0, 1, s);
+      const float l = warp_reduce(s.l, AddOp());
+      const KvRowOut o = inside ? row_out(p, t.row0 + r, t.h0 + q - r * p.gw, s.m, l, lane == 0)
+                                : part_out(p, p.block_parts, to_slot, q, s.m, l, lane == 0);
+      put_sums<E>(p, o, s);
+    }
+  }
+  if (threadIdx.x == 0) p.cuts[blockIdx.x] = cut;
   pdl_release();
 }
 
-// -------------------------------------------------------------------------- join ---
-// Partial results of an item.  A query's largest m and sum of l come from its parts' scalars, a lane a part;
-// its warps (16 in all) add up some of its parts each, every load independent of the others, and
-// their sums meet in shared memory.  The order is the parts', whatever the timing.
-constexpr int kJoinWarps = 16;
-
+// --------------------------------------------------- join of items across blocks ---
 template <typename E>
 __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvPass p) {
   __shared__ float4 sums[kJoinWarps][kKvMaxDim / 4];
@@ -715,80 +807,40 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvPass p
   const int4 cut = p.cuts[id];
   if (cut.z == 0) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, dim = p.a.c.dim;
-  long long row0;
-  const int n_rows = tile_rows(p, cut.x, row0);
-  const int group = p.a.H / p.a.c.heads, kv = cut.y / p.gs, slice = (cut.y - kv * p.gs) * p.gw;
-  const int gw = min(p.gw, group - slice), h0 = kv * group + slice, n_q = n_rows * gw;
-  const int share = n_q >= kJoinWarps ? 1 : kJoinWarps / n_q, at_once = kJoinWarps / share;
-  const long long stride = part_floats(p.max_q, dim);
-  const float* first = p.parts + (2ll * id + 1) * stride;          // part 0; part k: first + k (2k - 1) ...
-  const float* rest = p.parts + 2ll * id * stride;                 // ... from worker id + k's place
-  for (int q0 = 0; q0 < n_q; q0 += at_once) {
-    const int i = q0 + warp / share, sub = warp % share;
-    const bool there = warp / share < at_once && i < n_q;
-    const int r = there ? i / gw : 0, h = there ? i - r * gw : 0, q = r * p.gw + h;
-    float m = kNegInf, l = 0.f;
-    float4 o[2] = {};
-    if (there) {
-      const auto part = [&](int k) { return k == 0 ? first : rest + 2ll * k * stride; };
-      for (int k = lane; k < cut.z; k += 32) m = fmaxf(m, part(k)[p.max_q * dim + 2 * q]);
-      m = warp_max(m);
-      const float ref = m == kNegInf ? 0.f : m;
-      for (int k0 = 0; k0 < cut.z; k0 += 32) {
-        float w = 0.f;
-        if (k0 + lane < cut.z) {
-          const float2 ml = *reinterpret_cast<const float2*>(part(k0 + lane) + p.max_q * dim + 2 * q);
-          w = ml.x == ref ? 1.f : ex2(ml.x - ref);
-          l = fmaf(ml.y, w, l);
-        }
-        const int n = min(32, cut.z - k0);
-#pragma unroll 4
-        for (int k = sub; k < n; k += share) {
-          const float f = __shfl_sync(~0u, w, k);
-          const float4* x = reinterpret_cast<const float4*>(part(k0 + k) + q * dim);
+  const JoinItem t(p, cut);
+  const int q_first = blockIdx.y * kJoinWarps, n_q = min(t.n_q - q_first, kJoinWarps);
+  if (n_q <= 0) return;
+  const int share = kJoinWarps / n_q, sub = warp % share;            // warps of a query
+  if (warp >= n_q * share) return;
+  int r;
+  const int q = t.query(p, q_first + warp / share, r);
+  JoinSums s;
+  join_parts(p, p.block_parts, 2 * id, true, cut.z, q, sub, share, s);
+  const float l = warp_reduce(s.l, AddOp());
+  if (share > 1) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (4 * (lane + 32 * e) < dim) {
-              const float4 y = x[lane + 32 * e];
-              o[e] = make_float4(fmaf(y.x, f, o[e].x), fmaf(y.y, f, o[e].y), fmaf(y.z, f, o[e].z), fmaf(y.w, f, o[e].w));
-            }
-        }
-      }
-      l = warp_reduce(l, AddOp());
-    }
-    if (share > 1) {
+    for (int e = 0; e < 2; ++e)
+      if (4 * (lane + 32 * e) < dim) sums[warp][lane + 32 * e] = s.o[e];
+    named_bar_sync(1 + warp / share, share * 32);
+    if (sub != 0) return;
+    for (int k = 1; k < share; ++k)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        if (4 * (lane + 32 * e) < dim) sums[warp][lane + 32 * e] = o[e];
-      __syncthreads();
-      if (there && sub == 0)
-        for (int k = 1; k < share; ++k)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (4 * (lane + 32 * e) < dim) {
-              const float4 y = sums[warp + k][lane + 32 * e];
-              o[e] = make_float4(o[e].x + y.x, o[e].y + y.y, o[e].z + y.z, o[e].w + y.w);
-            }
-      __syncthreads();
-    }
-    if (there && sub == 0) {
-      const KvRowOut to = row_out(p, row0 + r, h0 + h, m, l, lane == 0);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float v[4] = {o[e].x, o[e].y, o[e].z, o[e].w};
-        if (4 * (lane + 32 * e) < dim) put<E, 4>(to, 4 * (lane + 32 * e), v);
-      }
-    }
+        if (4 * (lane + 32 * e) < dim) {
+          const float4 y = sums[warp + k][lane + 32 * e];
+          s.o[e] = make_float4(s.o[e].x + y.x, s.o[e].y + y.y, s.o[e].z + y.z, s.o[e].w + y.w);
+        }
   }
+  put_sums<E>(p, row_out(p, t.row0 + r, t.h0 + q - r * p.gw, s.m, l, lane == 0), s);
 }
 
 // ---------------------------------------------------------------------- launches ---
-constexpr int kMostWorkers = 16 * kKvMostSms;
 constexpr int kRingsMost = 220 * 1024;       // bytes of all rings of a block
 
 template <typename E>
-cudaError_t run_join(const KvPass& p, cudaStream_t s) {
-  return launch_pdl(kv_join_kernel<E>, dim3(p.workers), dim3(kJoinWarps * 32), 0, s, p);
+cudaError_t run_join(const KvPass& p, int sms, cudaStream_t s) {
+  const dim3 grid(std::min(sms, kKvMostSms), (p.max_q + kJoinWarps - 1) / kJoinWarps);
+  return launch_pdl(kv_join_kernel<E>, grid, dim3(kJoinWarps * 32), 0, s, p);
 }
 
 template <typename Core>
@@ -801,12 +853,12 @@ cudaError_t run_pass(KvPass p, int sms, int* status, cudaStream_t s) {
   const int warps = std::min(kvw ? std::min(atoi(kvw), Core::kMostWarps) : Core::kMostWarps, kRingsMost / (2 * slot + Core::kScratch));
   p.stages = std::min(kMostStages, (kRingsMost / warps - Core::kScratch) / slot);
   const int grid = std::min(sms, kKvMostSms), ring = warps * (p.stages * slot + Core::kScratch);
-  p.workers = grid * warps;
+  p.block_workers = warps;
   const cudaError_t e = cudaFuncSetAttribute(kv_blocks_kernel<Core>,
                                              cudaFuncAttributeMaxDynamicSharedMemorySize, kRingsMost);
   if (e != cudaSuccess) return e;
   const cudaError_t f = launch_pdl(kv_blocks_kernel<Core>, dim3(grid), dim3(warps * 32), ring, s, p, status);
-  return f != cudaSuccess ? f : run_join<E>(p, s);
+  return f != cudaSuccess ? f : run_join<E>(p, sms, s);
 }
 
 template <int kDim>
@@ -824,7 +876,7 @@ cudaError_t run_part(KvPass p, int sms, int* status, cudaStream_t s) {
   const long long queries = std::min<long long>(p.part.per, p.a.N) * (p.a.H / p.a.c.heads);
   if (p.a.c.dtype == 0 && dim <= 128 && queries > 16 && p.a.c.n_pages > 0 && p.a.scale >= 0.f) {
     const cudaError_t e = launch_kv_tc(p, sms, status, s);
-    return e != cudaSuccess ? e : run_join<__nv_bfloat16>(p, s);
+    return e != cudaSuccess ? e : run_join<__nv_bfloat16>(p, sms, s);
   }
   return dim <= 64    ? run_dim<64>(p, sms, status, s)
          : dim <= 128 ? run_dim<128>(p, sms, status, s)
@@ -834,16 +886,18 @@ cudaError_t run_part(KvPass p, int sms, int* status, cudaStream_t s) {
 size_t up16(size_t x) { return (x + 15) / 16 * 16; }
 
 struct Layout {
-  size_t parts, cuts, pre_o, pre_ml, total;
+  size_t parts, block_parts, cuts, pre_o, pre_ml, total;
 };
 
 Layout layout(long long N, int H, int dim, bool prefix) {
   Layout y;
   size_t at = 0;
-  y.parts = at;                              // 16 warps of 8 queries, 8 of 16, or one of 128 an SM
-  at += up16(size_t(2 * kMostWorkers + 8) * 8 * (dim + 4) * sizeof(float));
+  y.parts = at;                              // 16 workers of 8 queries or 8 of 16 an SM
+  at += size_t(2 * 16 * kKvMostSms) * 8 * (dim + 4) * sizeof(float);
+  y.block_parts = at;                        // 128 queries at most
+  at += size_t(2 * kKvMostSms) * 128 * (dim + 4) * sizeof(float);
   y.cuts = at;
-  at += size_t(kMostWorkers) * sizeof(int4);
+  at += size_t(kKvMostSms) * sizeof(int4);
   y.pre_o = at;
   if (prefix) at += up16(size_t(N) * H * dim * sizeof(float));
   y.pre_ml = at;
@@ -864,6 +918,7 @@ cudaError_t launch_kv_attention(const KvAttention& a, int sms, int* status, cuda
   KvPass p{};
   p.a = a;
   p.parts = reinterpret_cast<float*>(ws + y.parts);
+  p.block_parts = reinterpret_cast<float*>(ws + y.block_parts);
   p.cuts = reinterpret_cast<int4*>(ws + y.cuts);
   if (a.prefix_len != nullptr) {
     KvPass f = p;

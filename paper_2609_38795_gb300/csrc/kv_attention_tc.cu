@@ -50,7 +50,8 @@ struct alignas(16) KvMisc {
   uint32_t tmem;
   int abort_word;
   uint32_t bad[4];                        // queries with a value that is not finite
-  WorkerStart start;
+  WorkerStart start[2];
+  Line line;                              // needed again at the end alone
   long long buf[kWarps];
 };
 
@@ -199,22 +200,22 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
     tmem_alloc(&mi.tmem, C::kCols);
     tmem_relinquish();
   }
+  tc_fence_before();
+  pdl_wait();
+  const Line line = find_starts<kBlk>(p, mi.start, reinterpret_cast<long long*>(ring), mi.buf);   // barriers within
+  tc_fence_after();
   if (dim != C::kChunks * 64) {              // what lies past a row's end is never copied: zeros
     uint4* z = reinterpret_cast<uint4*>(ring);
     for (int i = threadIdx.x; i < (kSlots * C::kTile + C::kQBufs * C::kQBytes) / 16; i += kThreads)
       z[i] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
+    __syncthreads();
   }
-  tc_fence_before();
-  pdl_wait();
-  const long long total = find_starts<kBlk>(p, 1, &mi.start, mi.buf);   // barriers within
-  tc_fence_after();
   const uint32_t tmem = mi.tmem;
-  const int n_workers = int(min((long long)p.workers, total)), id = blockIdx.x;
-  const long long begin = id < n_workers ? stretch(total, n_workers, id) : 0;
-  const long long end = id < n_workers ? stretch(total, n_workers, id + 1) : 0;
-  const int count = int(end - begin);
-  if (threadIdx.x == 0 && count == 0 && id < p.workers) p.cuts[id] = make_int4(0, 0, 0, 0);
+  const int id = blockIdx.x;                 // the block's one worker
+  const int count = id < line.n ? int(mi.start[1].block - mi.start[0].block) : 0;
+  if (threadIdx.x == 0) mi.line = line;
+  if (threadIdx.x == 0 && count == 0) p.cuts[id] = make_int4(0, 0, 0, 0);
 
   if (warp >= kCopyWarp && warp < kMmaWarp) {
     // ---- copies
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       next.last = i + 1 == count || in.b + 1 == in.t.nb;
     };
     if (count > 0) {
-      in.start(p, mi.start.tile, mi.start.rest);
+      in.start(p, mi.start[0].tile, mi.start[0].unit, mi.start[0].b);
       look_up(false, 0);
     }
     Place<kSlots> to;
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
     const uint64_t c2 = f2_pack(c, c);
     float l[kHalf];
     Cursor<kBlk> at;
-    if (count > 0) at.start(p, mi.start.tile, mi.start.rest);
+    if (count > 0) at.start(p, mi.start[0].tile, mi.start[0].unit, mi.start[0].b);
     float (*lsum)[kHalf] = reinterpret_cast<float (*)[kHalf]>(ps);               // at an item's end
     KvRowOut* outs = reinterpret_cast<KvRowOut*>(ps + kSoftWarps * kHalf * sizeof(float));
     int4 cut = make_int4(0, 0, 0, 0);
@@ -512,10 +513,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       }
       named_bar_sync(bar, 128);
       const bool whole = b0 == 0 && b1 == tile.nb, opens = b0 == 0 && b1 < tile.nb;
-      const long long part_id = 2ll * id + (opens ? 1 : 0);
+      const int part_id = 2 * id + (opens ? 1 : 0);
       const auto out = [&](int q, int r, float m, float s, bool writer) {
         return whole ? row_out(p, row0 + r, h0 + q - r * p.gw, m, s, writer)
-                     : part_out(p, part_id, q, m, s, writer);
+                     : part_out(p, p.block_parts, part_id, q, m, s, writer);
       };
       if (tid < kHalf) {
         const int q = q0 + tid, r = q / p.gw;
@@ -591,10 +592,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
         named_bar_sync(3, 256);
         if (threadIdx.x < 4) mi.bad[threadIdx.x] = 0;
       }
-      if (opens) {
-        // the workers up to the one with the item's last block
-        const long long item_end = end + (tile.nb - b1);
-        cut = make_int4(tile_id, unit, int((item_end * n_workers + total - 1) / total) - 1 - id + 1, 0);
+      if (opens && threadIdx.x == 0) {
+        cut = make_int4(tile_id, unit, mi.line.last_before(mi.line.start(id + 1) + (tile.nb - b1)) - id + 1, 0);
       }
     }
     if (threadIdx.x == 0 && count > 0) p.cuts[id] = cut;
@@ -611,11 +610,11 @@ cudaError_t run_tc(KvPass& p, int sms, int* status, cudaStream_t s) {
   static_assert(kSoftWarps * C::kHalf * 4 + C::kNQ * sizeof(KvRowOut) <= C::kPBytes * C::kPBufs,
                 "an item's end reuses the weights' place");
   shape_pass(p, C::kNQ, 32, kBlk);
-  p.workers = std::min(sms, kKvMostSms);
+  p.block_workers = 1;
   const cudaError_t e = cudaFuncSetAttribute(
       kv_tc_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem_bytes<C>()));
   if (e != cudaSuccess) return e;
-  return launch_pdl(kv_tc_kernel<C>, dim3(p.workers), dim3(kThreads), smem_bytes<C>(), s, p, status);
+  return launch_pdl(kv_tc_kernel<C>, dim3(std::min(sms, kKvMostSms)), dim3(kThreads), smem_bytes<C>(), s, p, status);
 }
 
 }  // namespace

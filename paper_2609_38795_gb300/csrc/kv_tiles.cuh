@@ -28,9 +28,12 @@ ALR_DEV int seen_len(const KvAttention& a, int seq, int len) {
 // rows with the same sequence, one run after the other, each in blocks of kBlk tokens; a tile of
 // no tokens has one empty block, so that its rows are written.  An item is a tile and a unit, `gw` query
 // heads of one key-value head (`gs` units a key-value head).
-//   All items' blocks in order (tile, unit, block) are one line, and each worker takes an equal stretch
-// of it, whatever the lengths are.  An item inside a stretch is finished by its worker; an item cut by a
-// border leaves partial results, two a worker at most, which a second kernel joins in order.
+//   All items in order (tile, unit), each with its blocks behind kItemCost places of no block (its queries,
+// its results), are one line, and each worker takes an equal stretch of it, whatever the lengths
+// are; a thread block's workers have consecutive stretches.  An item inside a
+// stretch is finished by its worker; an item cut by a border leaves partial results, two a worker at
+// most.  Its thread block joins those of its own workers in order, and a second kernel those of items
+// that cross thread blocks, again two a block at most.
 struct KvPass {
   KvAttention a;
   KvPart part;
@@ -38,12 +41,13 @@ struct KvPass {
   int per, tg, rows;
   int n_tiles;
   int step_pg, step_tok;           // kBlk tokens on: pages and tokens
-  int workers;
+  int block_workers;               // of a thread block, at most
   int stages;                      // blocks of a worker's ring
   int max_q;                       // queries of an item, at most
   float* parts;                    // [2 * workers][part_floats]: o of all queries, then m and l
-  int4* cuts;                      // [workers]: (tile, unit, parts) of the item that a worker begins
-                                   // and does not end; 0 parts: none
+  float* block_parts;              // [2 * blocks][part_floats]
+  int4* cuts;                      // [blocks]: (tile, unit, parts) of the item that a block begins and
+                                   // does not end; 0 parts: none
   float* put_o;                    // prefix pass: where results go, [N, H, dim] and [N, H, 2]
   float* put_ml;
   const float* pre_o;              // own pass after one: those results
@@ -93,9 +97,9 @@ __host__ __device__ inline long long part_floats(int max_q, int dim) {
   return (long long)max_q * dim + (2 * max_q + 3) / 4 * 4;
 }
 
-// Partial results of query q in slot `slot`.
-ALR_DEV KvRowOut part_out(const KvPass& p, long long slot, int q, float m, float l, bool writer) {
-  float* base = p.parts + slot * part_floats(p.max_q, p.a.c.dim);
+// Partial results of query q in place `slot` of `parts`.
+ALR_DEV KvRowOut part_out(const KvPass& p, float* parts, int slot, int q, float m, float l, bool writer) {
+  float* base = parts + slot * part_floats(p.max_q, p.a.c.dim);
   float* ml = base + p.max_q * p.a.c.dim;
   if (writer) ml[2 * q] = m, ml[2 * q + 1] = l;
   return {1.f, 0.f, nullptr, base + q * p.a.c.dim, nullptr};
@@ -211,12 +215,11 @@ struct Cursor {
     t0 = lead < 0 ? 0 : (b - __shfl_sync(~0u, t.first, from)) * kBlk;
     run_end = min(warp_min(t.first > b ? t.first : INT_MAX), t.nb);
   }
-  // rest: blocks into the tile's items
-  ALR_DEV void start(const KvPass& p, int tile_, long long rest) {
+  ALR_DEV void start(const KvPass& p, int tile_, int unit_, int b_) {
     tile = tile_;
+    unit = unit_;
+    b = b_;
     t = load_tile<kBlk>(p, tile);
-    unit = int(rest / t.nb);
-    b = int(rest - (long long)unit * t.nb);
     enter();
   }
   // To the next block; whether it continues the run.
@@ -238,27 +241,46 @@ struct Cursor {
   }
 };
 
-// Start of worker w's stretch of `total` blocks shared by `n` workers.
-ALR_DEV long long stretch(long long total, int n, long long w) { return total * w / n; }
+// a / b for a >= 0, b > 0: a 64-bit division costs half a microsecond, few are needed.
+ALR_DEV long long quotient(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? (long long)(uint32_t(a) / uint32_t(b)) : a / b;
+}
 
-// Every block of the kernel counts the blocks of all tiles (a thread some consecutive ones), finds its
-// n_own workers' starts (worker w of block i is w gridDim + i), and leaves them in `at`: (tile, blocks
-// into the tile's items).  buf: an entry a warp.  Returns the total.
-struct WorkerStart {
-  long long begin;             // block of the line
-  long long rest;
-  int tile;
+// Blocks that an item costs beside its own (decode of 64 x 0..32768 by logarithm, where the short ones
+// come together: 176 us without, 164 with).
+constexpr int kItemCost = 2;
+
+// The line: `n` workers (`per_block` consecutive ones of each thread block) have `each` places,
+// the first `more` of them one more.
+struct Line {
+  long long each;
+  int more, n, per_block;
+  ALR_DEV long long start(int w) const { return w * each + min(w, more); }
+  // Worker with the place before `end`.
+  ALR_DEV int last_before(long long end) const {
+    const long long i = end - 1 - more * (each + 1);
+    return int(i < 0 ? quotient(end - 1, each + 1) : more + quotient(i, each));
+  }
 };
 
+struct WorkerStart {
+  long long block;             // number of its first block among all
+  int tile, unit, b;
+};
+
+// Every thread block counts the places of all tiles, a thread some consecutive ones; a warp then finds the
+// start of a worker among the threads' sums and the tiles of the thread.  at[i]: start of the block's
+// i-th worker, at[own workers]: of the next one.  Few blocks go to few workers of every thread block.
+// sums: an entry a thread; buf: an entry a warp.
 template <int kBlk>
-ALR_DEV long long find_starts(const KvPass& p, int n_own, WorkerStart* at, long long* buf) {
+ALR_DEV Line find_starts(const KvPass& p, WorkerStart* at, long long* sums, long long* buf) {
   const int tid = threadIdx.x, n_threads = blockDim.x, n_warps = n_threads / 32;
+  const int lane = tid & 31, warp = tid >> 5;
   const int per = (p.n_tiles + n_threads - 1) / n_threads;
   const int a = int(min((long long)tid * per, (long long)p.n_tiles)), e = min(a + per, p.n_tiles);
   long long own = 0;
-  for (int i = a; i < e; ++i) own += tile_blocks<kBlk>(p, i);
-  // exclusive sums over the threads
-  const int lane = tid & 31, warp = tid >> 5;
+  for (int i = a; i < e; ++i) own += tile_blocks<kBlk>(p, i) + kItemCost;
+  own *= p.n_units;
   const long long up = warp_scan(own);
   if (lane == 31) buf[warp] = up;
   __syncthreads();
@@ -267,27 +289,48 @@ ALR_DEV long long find_starts(const KvPass& p, int n_own, WorkerStart* at, long 
     if (i < warp) before += buf[i];
     total += buf[i];
   }
-  before *= p.n_units;
-  own *= p.n_units;
-  total *= p.n_units;
-  const long long n = min((long long)p.workers, total);
-  if (tid < n_own) at[tid].begin = stretch(total, int(n), (long long)tid * gridDim.x + blockIdx.x);
+  sums[tid] = before;
+  Line line;
+  const long long items = (long long)p.n_tiles * p.n_units, blocks = total - kItemCost * items;
+  line.per_block = int(min(quotient(blocks + gridDim.x - 1, gridDim.x), (long long)p.block_workers));
+  line.n = int(min((long long)line.per_block * gridDim.x, blocks));
+  line.each = quotient(total, line.n);
+  line.more = int(total - line.each * line.n);
   __syncthreads();
-  for (int w = 0; w < n_own; ++w) {
-    if ((long long)w * gridDim.x + blockIdx.x >= n) break;
-    long long rest = at[w].begin - before;
-    if (rest < 0 || rest >= own) continue;
-    int tile = a;
-    for (;; ++tile) {
-      const long long len = (long long)tile_blocks<kBlk>(p, tile) * p.n_units;
-      if (rest < len) break;
-      rest -= len;
+  const int id0 = int(blockIdx.x) * line.per_block, n_own = min(line.per_block, line.n - id0);
+  for (int k = warp; k <= n_own; k += n_warps) {
+    if (id0 + k == line.n) {
+      if (lane == 0) at[k] = {blocks, 0, 0, 0};
+      continue;
     }
-    at[w].tile = tile;
-    at[w].rest = rest;
+    const long long pos = line.start(id0 + k);
+    int n = 0;                               // threads that begin at or before it
+    for (int i = lane; i < n_threads; i += 32) n += __popc(__ballot_sync(~0u, sums[i] <= pos));
+    long long rest = pos - sums[n - 1];
+    const int tile_end = min(n * per, p.n_tiles);
+    // rest is less than the thread's places (of lengths that do not change meanwhile)
+    for (int tile = (n - 1) * per; tile < tile_end; tile += 32) {
+      const int mine = tile + lane;
+      const long long len = mine < tile_end ? (long long)(tile_blocks<kBlk>(p, mine) + kItemCost) * p.n_units : 0;
+      const long long sum = warp_scan(len);
+      const uint32_t past = __ballot_sync(~0u, sum > rest);
+      if (past == 0) {
+        rest -= __shfl_sync(~0u, sum, 31);
+        continue;
+      }
+      const int k2 = __ffs(past) - 1;
+      tile += k2;
+      rest -= __shfl_sync(~0u, sum - len, k2);
+      const long long each = quotient(__shfl_sync(~0u, len, k2), p.n_units);
+      const int unit = int(quotient(rest, each)), off = int(rest - unit * each);
+      if (lane == 0)
+        at[k] = {pos - kItemCost * ((long long)tile * p.n_units + unit) - min(off, kItemCost), tile, unit,
+                 max(off - kItemCost, 0)};
+      break;
+    }
   }
   __syncthreads();
-  return total;
+  return line;
 }
 
 // ------------------------------------------------------------------ row by row ---
