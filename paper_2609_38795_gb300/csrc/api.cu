@@ -1639,6 +1639,33 @@ int check_cache(const alr_kv_cache* c, alr::KvCache* out) {
   return ALR_OK;
 }
 
+// The maps of a bf16 cache whose tokens' rows are rows of one matrix, its pages multiples of 8 tokens;
+// others leave box_rows 0.
+int cache_maps(const alr::KvCache& c, alr::KvMaps* m) {
+  const int64_t step = c.st;                 // elements between matrix rows
+  if (c.page % 8 != 0 || step < c.dim || (c.n_pages > 1 && c.sp % step != 0)) return ALR_OK;
+  int64_t head_rows = 0, head_cols = 0;
+  if (c.heads > 1) {
+    if ((c.heads - 1) * c.sh + c.dim <= step) head_cols = c.sh;
+    else if (c.sh % step == 0) head_rows = c.sh / step;
+    else return ALR_OK;
+  }
+  const int64_t page_rows = c.n_pages > 1 ? c.sp / step : 0;
+  const int64_t rows = (c.n_pages - 1) * page_rows + (c.heads - 1) * head_rows + c.page;
+  const int64_t cols = (c.heads - 1) * head_cols + c.dim;
+  if (rows >= INT32_MAX || step * 2 >= (int64_t(1) << 40)) return ALR_OK;
+  const int box = c.page % 32 == 0 ? 32 : c.page % 16 == 0 ? 16 : 8;
+  int rc = make_map(&m->k, c.K, ALR_BF16, cols, rows, step * 2, 64, box);
+  if (rc == ALR_OK) rc = make_map(&m->v, c.V, ALR_BF16, cols, rows, step * 2, 64, box);
+  if (rc != ALR_OK) return rc;
+  m->box_rows = box;
+  m->n_rows = int(rows);
+  m->page_rows = int(page_rows);
+  m->head_rows = int(head_rows);
+  m->head_cols = int(head_cols);
+  return ALR_OK;
+}
+
 constexpr int64_t kMostKvRows = int64_t(1) << 24;
 
 bool kv_rows_fit(int64_t N, int32_t H) { return N >= 0 && N <= kMostKvRows && H >= 1 && H <= 1024; }
@@ -1747,10 +1774,14 @@ int alr_kv_attention(const alr_kv_cache* cache, const alr_kv_attention_params* p
   if ((rc = require_sm103(&info)) != ALR_OK) return rc;
   int* status = alr::device_status_ptr();
   if (status == nullptr) return fail(ALR_ERR_CUDA, "device status word unavailable");
-  const cudaError_t e = alr::launch_kv_attention(
-      {c, p->N, p->ldq, p->ldo, p->H, p->n_seq, p->cols, p->rows_per_seq, p->rows_per_prefix,
-       p->scale, Q, table, len, seq, prefix_len, prefix_seq, out, lse, workspace},
-      info.sms, status, static_cast<cudaStream_t>(stream));
+  const alr::KvAttention a = {c, p->N, p->ldq, p->ldo, p->H, p->n_seq, p->cols, p->rows_per_seq,
+                              p->rows_per_prefix, p->scale, Q, table, len, seq, prefix_len, prefix_seq,
+                              out, lse, workspace};
+  alr::KvMaps maps{};
+  if (alr::kv_attention_takes_maps(a, p->rows_per_seq) ||
+      (prefix_len != nullptr && alr::kv_attention_takes_maps(a, p->rows_per_prefix)))
+    if ((rc = cache_maps(c, &maps)) != ALR_OK) return rc;
+  const cudaError_t e = alr::launch_kv_attention(a, maps, info.sms, status, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? ALR_OK : cuda_fail(e, "cache attention launch");
 }
 

@@ -313,8 +313,19 @@ struct KvAttention {
   float* lse;                  // may be nullptr
   void* ws;
 };
+// The cache as two matrices for TMA: a token's row of a head lies in matrix row
+// page * page_rows + token + head * head_rows, from column head * head_cols on.  Boxes of box_rows rows,
+// which divide a page, and 64 columns.
+struct KvMaps {
+  CUtensorMap k, v;
+  int box_rows;                // 0: the layout is no such matrix
+  int n_rows, page_rows, head_rows, head_cols;
+};
+// Whether a pass over parts of `rows` consecutive rows takes the maps.
+bool kv_attention_takes_maps(const KvAttention& a, int rows);
 size_t kv_attention_workspace(long long N, int H, int dim, bool prefix);
-cudaError_t launch_kv_attention(const KvAttention& a, int sms, int* status, cudaStream_t s);
+cudaError_t launch_kv_attention(const KvAttention& a, const KvMaps& maps, int sms, int* status,
+                                cudaStream_t s);
 
 // Record `msg` as this host thread's alr_last_error() text and return `code` (api.cu).
 int set_last_error(int code, const char* msg);

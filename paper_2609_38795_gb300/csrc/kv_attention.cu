@@ -1,7 +1,6 @@
 // Attention of query rows over the paged key-value cache, up to 16 queries of a tile at a time.
 #include <algorithm>
 #include <cfloat>
-#include <cstdlib>
 
 #include "launch.h"
 #include "kv_tiles.cuh"
@@ -563,6 +562,7 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
   __shared__ long long buf[Core::kMostWarps];
   __shared__ uint32_t there_of[Core::kMostWarps][kMostStages];
   __shared__ uint64_t landed[Core::kMostWarps][kMostStages];
+  __shared__ KvRowOut outs[Core::kMostWarps][Core::kMaxQ];
   __shared__ int4 cut_of[Core::kMostWarps];  // (tile, unit, parts) of the item that a worker leaves open
   __shared__ int4 head_cut;                  // ... of the item that the block's first worker continues
   __shared__ int abort_word;
@@ -711,9 +711,9 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
     }
     const bool whole = b0 == 0 && last_here, opens = b0 == 0 && !last_here;
     const int part = 2 * id + (opens ? 1 : 0);
-    const auto out = [&](int q, int r, float m, float l) {
-      return whole ? row_out(p, row0 + r, h0 + q - r * p.gw, m, l, lane == 0)
-                   : part_out(p, p.parts, part, q, m, l, lane == 0);
+    const auto out = [&](int q, int r, float m, float l, bool writer) {
+      return whole ? row_out(p, row0 + r, h0 + q - r * p.gw, m, l, writer)
+                   : part_out(p, p.parts, part, q, m, l, writer);
     };
     // through the slot just used, which is filled again only in the next block's turn, into whole packs
     const int dim = a.c.dim, used = slot == 0 ? stages - 1 : slot - 1;
@@ -721,22 +721,32 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
     __syncwarp();
     core.leave(n_q, dim, sums);
     __syncwarp();
+    const float* ml = sums + n_q * (dim + 4);
+    if (lane < n_q) {
+      const int r = lane / p.gw;
+      KvRowOut to = {0.f, 0.f, nullptr, nullptr, nullptr};
+      if (lane - r * p.gw < gw) to = out(lane, r, ml[2 * lane], ml[2 * lane + 1], true);
+      outs[warp][lane] = to;
+    }
+    __syncwarp();
+    float odd = lane < n_q ? ml[2 * lane + 1] * 0.f : 0.f;         // 0 while all values are finite
+    const int quads = dim / 4;
+#pragma unroll 2
+    for (int k = lane; k < n_q * quads; k += 32) {
+      const int q = k / quads, d = 4 * (k - q * quads);
+      const KvRowOut to = outs[warp][q];
+      const float4 x = *reinterpret_cast<const float4*>(sums + q * (dim + 4) + d);
+      const float v[4] = {x.x, x.y, x.z, x.w};
+      if (to.dst != nullptr || to.dst_f != nullptr) put<E, 4>(to, d, v);
+      odd = fmaf(0.f, (x.x + x.y) + (x.z + x.w), odd);
+    }
+    if (n_rows > 1 && __any_sync(~0u, !(odd == 0.f))) {
+      // Weights of 0 times a value that is not finite: such a value may lie in a token that a query does
+      // not see but another of the tile does.  All queries again, token by token.
 #pragma unroll 1
-    for (int q = 0; q < n_q; ++q) {
-      const int r = q / p.gw;
-      if (q - r * p.gw >= gw) continue;
-      const float m = sums[n_q * (dim + 4) + 2 * q], l = sums[n_q * (dim + 4) + 2 * q + 1];
-      const KvRowOut to = out(q, r, m, l);
-      float odd = l - l;                         // 0 while all values are finite
-      for (int d = 4 * lane; d < dim; d += 128) {
-        const float4 x = *reinterpret_cast<const float4*>(sums + q * (dim + 4) + d);
-        const float v[4] = {x.x, x.y, x.z, x.w};
-        put<E, 4>(to, d, v);
-        odd = fmaf(0.f, (x.x + x.y) + (x.z + x.w), odd);
-      }
-      if (n_rows > 1 && __any_sync(~0u, !(odd == 0.f))) {
-        // Weights of 0 times a value that is not finite: such a value may lie in a token that the query
-        // does not see but another of the tile does.  Its tokens again, one by one.
+      for (int q = 0; q < n_q; ++q) {
+        const int r = q / p.gw;
+        if (q - r * p.gw >= gw) continue;
         __syncwarp();
         float x[kLaneDims], o[kLaneDims] = {}, m2 = kNegInf, l2 = 0.f;
 #pragma unroll
@@ -749,7 +759,7 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
         const long long t0 = (long long)(b0 - first) * kBlk, t1 = (long long)(b1 - first) * kBlk;
         if (len > 0)
           walk_tokens<E>(a, seq, int(max(t0, 0ll)), int(min(t1, (long long)len)), kv, x, m2, l2, o);
-        const KvRowOut again = out(q, r, m2, l2);
+        const KvRowOut again = out(q, r, m2, l2, lane == 0);
 #pragma unroll
         for (int e = 0; e < kLaneDims; ++e) {
           const float v[1] = {o[e]};
@@ -835,7 +845,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvPass p
 }
 
 // ---------------------------------------------------------------------- launches ---
-constexpr int kRingsMost = 220 * 1024;       // bytes of all rings of a block
+constexpr int kRingsMost = 218 * 1024;       // bytes of all rings of a block
 
 template <typename E>
 cudaError_t run_join(const KvPass& p, int sms, cudaStream_t s) {
@@ -849,8 +859,7 @@ cudaError_t run_pass(KvPass p, int sms, int* status, cudaStream_t s) {
   shape_pass(p, Core::kMaxQ, 32, kBlk);
   // as many warps as have two blocks each, then as many blocks
   const int slot = 2 * kBlk * row_bytes_of<E>(p.a.c.dim);
-  const char* kvw = getenv("KVW"); /*EXP*/
-  const int warps = std::min(kvw ? std::min(atoi(kvw), Core::kMostWarps) : Core::kMostWarps, kRingsMost / (2 * slot + Core::kScratch));
+  const int warps = std::min(Core::kMostWarps, kRingsMost / (2 * slot + Core::kScratch));
   p.stages = std::min(kMostStages, (kRingsMost / warps - Core::kScratch) / slot);
   const int grid = std::min(sms, kKvMostSms), ring = warps * (p.stages * slot + Core::kScratch);
   p.block_workers = warps;
@@ -871,11 +880,16 @@ cudaError_t run_dim(const KvPass& p, int sms, int* status, cudaStream_t s) {
                   : run_pass<F32Core<kDim, 8>>(p, sms, status, s);
 }
 
-cudaError_t run_part(KvPass p, int sms, int* status, cudaStream_t s) {
+// More queries of the same tokens than one warp holds: tiles by tcgen05.
+bool takes_tiles(const KvAttention& a, int rows) {
+  return a.c.dtype == 0 && a.c.dim <= 128 && std::min<long long>(rows, a.N) * (a.H / a.c.heads) > 16 &&
+         a.c.n_pages > 0 && a.scale >= 0.f;
+}
+
+cudaError_t run_part(KvPass p, const KvMaps& maps, int sms, int* status, cudaStream_t s) {
   const int dim = p.a.c.dim;
-  const long long queries = std::min<long long>(p.part.per, p.a.N) * (p.a.H / p.a.c.heads);
-  if (p.a.c.dtype == 0 && dim <= 128 && queries > 16 && p.a.c.n_pages > 0 && p.a.scale >= 0.f) {
-    const cudaError_t e = launch_kv_tc(p, sms, status, s);
+  if (takes_tiles(p.a, p.part.per)) {
+    const cudaError_t e = launch_kv_tc(p, maps, sms, status, s);
     return e != cudaSuccess ? e : run_join<__nv_bfloat16>(p, sms, s);
   }
   return dim <= 64    ? run_dim<64>(p, sms, status, s)
@@ -912,7 +926,12 @@ size_t kv_attention_workspace(long long N, int H, int dim, bool prefix) {
   return layout(N, H, dim, prefix).total;
 }
 
-cudaError_t launch_kv_attention(const KvAttention& a, int sms, int* status, cudaStream_t s) {
+bool kv_attention_takes_maps(const KvAttention& a, int rows) {
+  return takes_tiles(a, rows) && a.c.dim % 16 == 0;
+}
+
+cudaError_t launch_kv_attention(const KvAttention& a, const KvMaps& maps, int sms, int* status,
+                                cudaStream_t s) {
   const Layout y = layout(a.N, a.H, a.c.dim, a.prefix_len != nullptr);
   char* ws = static_cast<char*>(a.ws);
   KvPass p{};
@@ -925,13 +944,13 @@ cudaError_t launch_kv_attention(const KvAttention& a, int sms, int* status, cuda
     f.part = {a.prefix_seq, a.prefix_len, a.rows_per_prefix};
     f.put_o = reinterpret_cast<float*>(ws + y.pre_o);
     f.put_ml = reinterpret_cast<float*>(ws + y.pre_ml);
-    const cudaError_t e = run_part(f, sms, status, s);
+    const cudaError_t e = run_part(f, maps, sms, status, s);
     if (e != cudaSuccess) return e;
     p.pre_o = f.put_o;
     p.pre_ml = f.put_ml;
   }
   p.part = {a.seq, a.len, a.rows_per_seq};
-  return run_part(p, sms, status, s);
+  return run_part(p, maps, sms, status, s);
 }
 
 }  // namespace alr

@@ -20,6 +20,11 @@ namespace {
 //   Warps: 8 softmax (two groups of 4, half the queries each), 4 copy (K and V tiles of 128 tokens,
 // gathered by rows of their pages, in a ring), 1 issues products and 3 make its group whole: registers
 // move between groups of 4 (launched with 128 a thread; 2 x 168 + 2 x 88 = 4 x 128).
+//   A copy warp has 32 tokens of a tile.  Where a token's row is a row of one matrix over the whole cache
+// and pages hold a multiple of 8 tokens, it fetches them by TMA in boxes of 8, 16 or 32 rows; the last
+// tokens of a run and other layouts come by 16-byte copies, which an SM carries out at 24 bytes a cycle
+// at most (all of it so: 128 blocks of 16 rows over 1024 to 3000 tokens 353 us; by tile::gather4, which
+// would serve any page, 644).
 constexpr int kBlk = 128;
 constexpr int kSoftWarps = 8, kCopyWarp = 8, kCopyWarps = 4, kMmaWarp = 12;
 constexpr int kWarps = 16, kThreads = kWarps * 32;
@@ -63,6 +68,12 @@ struct KvSmem {
   int vis[C::kNQ];                        // tokens of the run that a query sees
 };
 static_assert(sizeof(KvMisc) % 16 == 0, "what follows is read as packs of 16 bytes");
+
+// At an item's end: sums and destinations of all queries, and a place to turn 32 queries' rows.
+template <class C>
+constexpr int end_bytes() { return kSoftWarps * C::kHalf * 4 + C::kNQ * int(sizeof(KvRowOut)); }
+template <class C>
+constexpr int stage_bytes() { return 32 * C::kChunks * 128; }
 
 template <class C>
 constexpr size_t smem_bytes() { return C::kBig + sizeof(KvSmem<C>); }
@@ -108,6 +119,12 @@ ALR_DEV uint32_t bf16x2(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+
+// More bytes to come for `bar` in its present phase.
+ALR_DEV void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes)
+               : "memory");
 }
 
 // A place of the ring; tiles are copied and used in the order K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1).
@@ -166,7 +183,8 @@ __device__ __noinline__ float move_refs(uint32_t s_at, uint32_t o_at, float c, f
 }
 
 template <class C>
-__global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int* status) {
+__global__ void __launch_bounds__(kThreads, 1)
+    kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvPass p, int* status) {
   using E = __nv_bfloat16;
   constexpr int kNQ = C::kNQ, kSlots = C::kSlots;
   extern __shared__ __align__(1024) uint8_t tc_smem[];
@@ -204,13 +222,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
   pdl_wait();
   const Line line = find_starts<kBlk>(p, mi.start, reinterpret_cast<long long*>(ring), mi.buf);   // barriers within
   tc_fence_after();
-  if (dim != C::kChunks * 64) {              // what lies past a row's end is never copied: zeros
+  if (dim % 16 != 0) {                       // what lies past a row's end is never copied: zeros
     uint4* z = reinterpret_cast<uint4*>(ring);
     for (int i = threadIdx.x; i < (kSlots * C::kTile + C::kQBufs * C::kQBytes) / 16; i += kThreads)
       z[i] = make_uint4(0, 0, 0, 0);
-    fence_proxy_async_smem();
-    __syncthreads();
   }
+  fence_proxy_async_smem();                  // the copies come after this and the sums of the starts
+  __syncthreads();
   const uint32_t tmem = mi.tmem;
   const int id = blockIdx.x;                 // the block's one worker
   const int count = id < line.n ? int(mi.start[1].block - mi.start[0].block) : 0;
@@ -234,8 +252,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
     // as its rows.
     struct Next {
       int pg, off, unit, tile;
-      bool first, last;
-    } next = {-1, 0, 0, 0, true, true};
+      bool first, last, whole;               // whole: all of the warp's tokens are the run's
+    } next = {-1, 0, 0, 0, true, true, false};
     int j = 0, off = 0;
     const auto look_up = [&](bool runs_on, int i) {
       if (runs_on) {
@@ -249,6 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       }
       next.pg = in.t0 + w * 32 + lane < in.most ? a.table[(long long)in.seq * a.cols + j] : -1;
       next.off = off;
+      next.whole = in.t0 + w * 32 + 32 <= in.most;
       next.unit = in.unit;
       next.tile = in.tile;
       next.first = i == 0 || in.b == 0;
@@ -259,8 +278,23 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       look_up(false, 0);
     }
     Place<kSlots> to;
-    const auto copy = [&](const void* cache, int kv, long long row, uint32_t all) {
+    // box: first matrix row of the lane's box of the warp's tokens, -1: copies of 16 bytes
+    const int n_boxes = maps.box_rows > 0 ? 32 / maps.box_rows : 0, n_chunks = (dim + 63) / 64;
+    const auto copy = [&](const void* cache, const CUtensorMap* map, int kv, long long row, uint32_t all, int box) {
       if (to.round > 0) wait_on(&mi.empty[to.slot], to.round - 1, ab);
+      if (box >= 0) {
+        if (lane < n_boxes) {
+          mbar_expect_tx(&mi.full[to.slot], n_chunks * maps.box_rows * 128);
+          for (int c = 0; c < n_chunks; ++c)
+            tma_load_2d(ring + to.slot * C::kTile + c * (kBlk * 128) + (w * 32 + lane * maps.box_rows) * 128, map,
+                        &mi.full[to.slot], kv * maps.head_cols + c * 64, box);
+        }
+        cp_async_arrive(&mi.full[to.slot]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&mi.full[to.slot]);
+        to.next();
+        return;
+      }
       const E* base = static_cast<const E*>(cache) + kv * a.c.sh + pack * 8;
       const uint32_t dst = ring_at + to.slot * C::kTile;
 #pragma unroll
@@ -276,7 +310,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
     };
     long long row_v = 0;
     uint32_t all_v = 0;
-    int kv_v = 0, item = -1;
+    int kv_v = 0, item = -1, box_v = -1;
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
       const Next cur = next;
@@ -288,6 +322,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       const uint32_t all = __ballot_sync(~0u, there);
       const long long row = there ? cur.pg * a.c.sp + cur.off * a.c.st : 0;
       const int kv = cur.unit / p.gs;
+      int box = -1;
+      if (n_boxes > 0 && cur.whole) {
+        const int from = (lane * maps.box_rows) & 31;
+        const int pg = __shfl_sync(~0u, there ? cur.pg : -1, from), off = __shfl_sync(~0u, cur.off, from);
+        box = pg >= 0 ? pg * maps.page_rows + off + kv * maps.head_rows : maps.n_rows;   // past the end: zeros
+      }
       // flags and masks of tile i: read after its keys have landed; tile i - kInfo is long done with
       // (its values' slot has been refilled since)
       if (lane == 0) {
@@ -309,13 +349,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
           if (has_pack) cp_async16_or_zero(dst + place(q, kNQ), src + pack * 8, ok);
         }
       }
-      copy(a.c.K, kv, row, all);
-      if (i > 0) copy(a.c.V, kv_v, row_v, all_v);
+      copy(a.c.K, &maps.k, kv, row, all, box);
+      if (i > 0) copy(a.c.V, &maps.v, kv_v, row_v, all_v, box_v);
+      box_v = box;
       row_v = row;
       all_v = all;
       kv_v = kv;
     }
-    if (count > 0) copy(a.c.V, kv_v, row_v, all_v);
+    if (count > 0) copy(a.c.V, &maps.v, kv_v, row_v, all_v, box_v);
+    if (*ab.smem)                            // after a wait that ran out: no copy outlives the block
+      for (int k = 0; k < kSlots; ++k) {
+        const int round = int(to.round) - (k < to.slot ? 0 : 1);
+        if (round >= 0) mbar_wait_drain(&mi.full[k], round & 1);
+      }
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp >= kMmaWarp) {
     // ---- products
@@ -324,7 +370,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       constexpr uint32_t i_s = idesc_make(false, 128, kNQ, false, false);
       constexpr uint32_t i_o = idesc_make(false, 128, kNQ, true, true);
       const int n_k = (dim + 15) / 16;
-      const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(qs), p_at = smem_u32(ps);
+      // descriptors of the first places; others are this many 16 bytes further (one thread issues, and every
+      // instruction between two products is time)
+      const uint64_t k_desc = sdesc_sw128(smem_u32(ring), 16, 1024), q_desc = sdesc_sw128(smem_u32(qs), 16, 1024);
+      const uint64_t v_desc = sdesc_sw128(smem_u32(ring), kBlk * 128, 1024);
+      const uint64_t p_desc = sdesc_sw128(smem_u32(ps), kBlk * 128, 1024);
       int item = -1;
       uint32_t prev = 0;
       Place<kSlots> from;
@@ -336,12 +386,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
         wait_on(&mi.p_full[pb], C::kPBufs == 2 ? i >> 1 : i, ab);
         fence_proxy_async_smem();
         tc_fence_after();
-        const uint32_t va = ring_at + from.slot * C::kTile, pa = p_at + pb * C::kPBytes;
+        // dim <= 64: rows 64 to 127 of the result come from whatever lies behind the tile, unused
+        const uint64_t va = v_desc + from.slot * (C::kTile >> 4), pa = p_desc + pb * (C::kPBytes >> 4);
+        mma_issue<false>(tmem + 2 * kNQ, va, pa, i_o, !(info & 1));
 #pragma unroll
-        for (int k = 0; k < kBlk / 16; ++k)
-          // dim <= 64: rows 64 to 127 of the result come from whatever lies behind the tile, unused
-          mma_issue<false>(tmem + 2 * kNQ, sdesc_sw128(va + k * 2048, kBlk * 128, 1024),
-                           sdesc_sw128(pa + k * 2048, kBlk * 128, 1024), i_o, !(info & 1) || k > 0);
+        for (int k = 1; k < kBlk / 16; ++k)
+          mma_issue<false>(tmem + 2 * kNQ, va + k * (2048 >> 4), pa + k * (2048 >> 4), i_o, 1);
         mma_commit(&mi.empty[from.slot]);
         mma_commit(&mi.pv_done[pb]);
         from.next();
@@ -355,11 +405,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
         if (i >= 2) wait_on(&mi.s_empty[sb], (i >> 1) - 1, ab);
         fence_proxy_async_smem();
         tc_fence_after();
-        const uint32_t ka = ring_at + from.slot * C::kTile, qa = q_at + (item & 1) * C::kQBytes;
-#pragma unroll 4
-        for (int k = 0; k < n_k; ++k)
-          mma_issue<false>(tmem + sb * kNQ, sdesc_sw128(ka + (k >> 2) * (kBlk * 128) + (k & 3) * 32, 16, 1024),
-                           sdesc_sw128(qa + (k >> 2) * (kNQ * 128) + (k & 3) * 32, 16, 1024), i_s, k > 0);
+        const uint64_t ka = k_desc + from.slot * (C::kTile >> 4), qa = q_desc + (item & 1) * (C::kQBytes >> 4);
+        mma_issue<false>(tmem + sb * kNQ, ka, qa, i_s, 0);
+#pragma unroll
+        for (int k = 1; k < 4 * C::kChunks; ++k)
+          if (k < n_k)
+            mma_issue<false>(tmem + sb * kNQ, ka + (((k >> 2) * (kBlk * 128) + (k & 3) * 32) >> 4),
+                             qa + (((k >> 2) * (kNQ * 128) + (k & 3) * 32) >> 4), i_s, 1);
         mma_commit(&mi.empty[from.slot]);
         mma_commit(&mi.s_full[sb]);
         if (info & 2) mma_commit(&mi.q_empty[item & 1]);
@@ -386,6 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
     if (count > 0) at.start(p, mi.start[0].tile, mi.start[0].unit, mi.start[0].b);
     float (*lsum)[kHalf] = reinterpret_cast<float (*)[kHalf]>(ps);               // at an item's end
     KvRowOut* outs = reinterpret_cast<KvRowOut*>(ps + kSoftWarps * kHalf * sizeof(float));
+    constexpr int kEndBytes = end_bytes<C>(), kStageBytes = stage_bytes<C>();
     int4 cut = make_int4(0, 0, 0, 0);
     int i = 0;
     while (i < count) {
@@ -531,31 +584,48 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
       const int d = wq * 32 + lane;
       const bool final_row = whole && p.put_o == nullptr;
       float odd = 0.f;                       // NaN after a value that is not finite
+      // Sums and prefixes leave as they lie, 128 bytes a warp's store; final rows go through shared memory (this
+      // group's quarter of the weights' place, 32 queries at a time), into packs of 16 bytes.
+      E* stage = reinterpret_cast<E*>(ps + kEndBytes + wg * kStageBytes);
 #pragma unroll 1
-      for (int k0 = 0; k0 < kHalf; k0 += 8) {
-        if (q0 + k0 >= n_q) break;
-        uint32_t s[8];
-        tmem_ld8(lanes + 2 * kNQ + q0 + k0, s);
-        float pre[8] = {};
-        if (final_row && p.pre_o != nullptr) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const KvRowOut& o = outs[q0 + k0 + k];
-            if (o.dst != nullptr && d < dim) pre[k] = o.pre[d] * o.f_pre;
-          }
-        }
+      for (int k0 = 0; k0 < kHalf && q0 + k0 < n_q; k0 += 32) {
+        uint32_t s[32];
+        tmem_ld32(lanes + 2 * kNQ + q0 + k0, s);
         tmem_ld_wait();
         reg_fence(s);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const KvRowOut& o = outs[q0 + k0 + k];
-          const float v = __uint_as_float(s[k]);
-          if (d < dim) {
-            if (o.dst != nullptr) static_cast<E*>(o.dst)[d] = E(fmaf(v, o.f, pre[k]));
-            if (o.dst_f != nullptr) o.dst_f[d] = v;
-            if (o.dst != nullptr || o.dst_f != nullptr) odd = fmaf(0.f, v, odd);
+        for (int k = 0; k < 32; ++k) odd = fmaf(0.f, d < dim && q0 + k0 + k < n_q ? __uint_as_float(s[k]) : 0.f, odd);
+        if (!final_row) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            float* to = outs[q0 + k0 + k].dst_f;
+            if (q0 + k0 + k < n_q && to != nullptr && d < dim) to[d] = __uint_as_float(s[k]);
           }
+          continue;
         }
+        if (p.pre_o != nullptr) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            const KvRowOut& o = outs[q0 + k0 + k];
+            const float pre = q0 + k0 + k < n_q && o.dst != nullptr && d < dim ? o.pre[d] * o.f_pre : 0.f;
+            s[k] = __float_as_uint(fmaf(__uint_as_float(s[k]), o.f, pre));
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) s[k] = __float_as_uint(__uint_as_float(s[k]) * outs[q0 + k0 + k].f);
+        }
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+          if (d < C::kChunks * 64) stage[k * (C::kChunks * 64) + d] = E(__uint_as_float(s[k]));
+        named_bar_sync(bar, 128);
+        const int packs = dim / 8;
+        for (int i = tid; i < 32 * packs; i += 128) {
+          const int k = i / packs, c = i - k * packs;
+          E* to = q0 + k0 + k < n_q ? static_cast<E*>(outs[q0 + k0 + k].dst) : nullptr;
+          if (to != nullptr)
+            reinterpret_cast<uint4*>(to)[c] = reinterpret_cast<const uint4*>(stage + k * (C::kChunks * 64))[c];
+        }
+        named_bar_sync(bar, 128);
       }
       if (!(odd == 0.f)) {                   // which queries: rare
         for (int k = 0; k < kHalf && q0 + k < n_q; ++k) atomicOr(&mi.bad[(q0 + k) >> 5], 1u << ((q0 + k) & 31));
@@ -605,26 +675,27 @@ __global__ void __launch_bounds__(kThreads, 1) kv_tc_kernel(const KvPass p, int*
 }
 
 template <class C>
-cudaError_t run_tc(KvPass& p, int sms, int* status, cudaStream_t s) {
+cudaError_t run_tc(KvPass& p, const KvMaps& maps, int sms, int* status, cudaStream_t s) {
   static_assert(smem_bytes<C>() <= 227 * 1024, "fits an SM");
-  static_assert(kSoftWarps * C::kHalf * 4 + C::kNQ * sizeof(KvRowOut) <= C::kPBytes * C::kPBufs,
+  static_assert(end_bytes<C>() + 2 * stage_bytes<C>() <= C::kPBytes * C::kPBufs,
                 "an item's end reuses the weights' place");
   shape_pass(p, C::kNQ, 32, kBlk);
   p.block_workers = 1;
   const cudaError_t e = cudaFuncSetAttribute(
       kv_tc_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem_bytes<C>()));
   if (e != cudaSuccess) return e;
-  return launch_pdl(kv_tc_kernel<C>, dim3(std::min(sms, kKvMostSms)), dim3(kThreads), smem_bytes<C>(), s, p, status);
+  return launch_pdl(kv_tc_kernel<C>, dim3(std::min(sms, kKvMostSms)), dim3(kThreads), smem_bytes<C>(), s,
+                    maps, p, status);
 }
 
 }  // namespace
 
-cudaError_t launch_kv_tc(KvPass& p, int sms, int* status, cudaStream_t s) {
+cudaError_t launch_kv_tc(KvPass& p, const KvMaps& maps, int sms, int* status, cudaStream_t s) {
   const int group = p.a.H / p.a.c.heads;
   const long long queries = std::min<long long>(std::min<long long>(p.part.per, p.a.N), 32) * group;
   if (p.a.c.dim <= 64)
-    return queries <= 64 ? run_tc<Cfg<64, 1>>(p, sms, status, s) : run_tc<Cfg<128, 1>>(p, sms, status, s);
-  return queries <= 64 ? run_tc<Cfg<64, 2>>(p, sms, status, s) : run_tc<Cfg<128, 2>>(p, sms, status, s);
+    return queries <= 64 ? run_tc<Cfg<64, 1>>(p, maps, sms, status, s) : run_tc<Cfg<128, 1>>(p, maps, sms, status, s);
+  return queries <= 64 ? run_tc<Cfg<64, 2>>(p, maps, sms, status, s) : run_tc<Cfg<128, 2>>(p, maps, sms, status, s);
 }
 
 }  // namespace alr

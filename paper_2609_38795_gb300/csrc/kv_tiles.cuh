@@ -385,6 +385,6 @@ constexpr int kKvMostSms = 160;
 // kv_attention_tc.cu: a pass over tiles of up to 32 rows and 128 queries (bf16, dim <= 128, n_pages > 0,
 // scale >= 0: references are maxima of the scores before they are scaled);
 // p.part is set, the rest of the pass's shape is filled in.
-cudaError_t launch_kv_tc(KvPass& p, int sms, int* status, cudaStream_t s);
+cudaError_t launch_kv_tc(KvPass& p, const KvMaps& maps, int sms, int* status, cudaStream_t s);
 
 }  // namespace alr
