@@ -774,7 +774,7 @@ typedef struct {
  *   A sequence whose tokens would pass cols pages or row T, or for which (with those before it) too few
  *   pages are free, is refused: it keeps its length, its rows get slot -1, and sequences after
  *   it that need pages of the pool are refused too if the pages up to and with theirs are too many.
- * Lengths outside [0, cols * page] count as the nearest bound.  One launch, no workspace.
+ * Lengths outside [0, cols * page] count as the nearest bound.  No workspace.
  */
 int alr_kv_plan(int32_t S, int32_t page, int32_t cols, int32_t n_pool, int32_t T,
                 const int32_t* len, const int32_t* add, int32_t* pool, const int32_t* pool_used,

@@ -829,9 +829,10 @@ def _kv_cache(K, V):
     if V.shape != shape or V.stride() != stride:
         raise ValueError(f"K and V must be laid out alike (got {list(shape)}, {stride} and "
                          f"{list(V.shape)}, {V.stride()})")
+    n, page, heads, dim = shape
     # the stride of a dimension of one entry is never used
-    sp, st, sh = (s if n > 1 else 0 for s, n in zip(stride[:3], shape[:3]))
-    return AlrKvCache(k, v, sp, st, sh, *shape, dtype_code(K.dtype))
+    return AlrKvCache(k, v, stride[0] if n > 1 else 0, stride[1] if page > 1 else 0,
+                      stride[2] if heads > 1 else 0, n, page, heads, dim, dtype_code(K.dtype))
 
 
 def alr_kv_plan(len, add, pool, pool_used, table, page, out: dict, stream=None):
@@ -842,9 +843,13 @@ def alr_kv_plan(len, add, pool, pool_used, table, page, out: dict, stream=None):
     if table.dim() != 2 or table.shape[0] < S:
         raise ValueError(f"table must be [{S}, cols] (got {[*table.shape]})")
     cols = table.shape[1]
-    sizes = dict(len=S, slot=T, pool_used=1, start=S + 1, tok_seq=T, tok_len=T, n_refused=1)
-    o = AlrKvPlanOutputs(*[_ptr(out[f] if f in ("len", "slot", "pool_used") else out.get(f), f, n, _I32)
-                           for f, n in sizes.items()])
+    get = out.get
+    o = AlrKvPlanOutputs(_ptr(out["len"], "len", S, _I32), _ptr(out["slot"], "slot", T, _I32),
+                         _ptr(out["pool_used"], "pool_used", 1, _I32),
+                         _ptr(get("start"), "start", S + 1, _I32),
+                         _ptr(get("tok_seq"), "tok_seq", T, _I32),
+                         _ptr(get("tok_len"), "tok_len", T, _I32),
+                         _ptr(get("n_refused"), "n_refused", 1, _I32))
     _check(lib().alr_kv_plan(S, page, cols, n_pool, T, _ptr(len, "len", S, _I32),
                              _ptr(add, "add", S, _I32), _ptr(pool, "pool", n_pool, _I32),
                              _ptr(pool_used, "pool_used", 1, _I32), _ptr(table, "table", S * cols, _I32),

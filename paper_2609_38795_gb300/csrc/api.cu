@@ -1695,7 +1695,7 @@ int alr_kv_plan(int32_t S, int32_t page, int32_t cols, int32_t n_pool, int32_t T
   if (rc != ALR_OK) return rc;
   const cudaError_t e = alr::launch_kv_plan(
       {S, page, cols, n_pool, T, len, add, pool, pool_used, table, out->len, out->slot,
-       out->pool_used, out->start, out->tok_seq, out->tok_len, out->n_refused},
+       out->pool_used, out->start, out->tok_seq, out->tok_len, out->n_refused, false},
       static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? ALR_OK : cuda_fail(e, "cache plan launch");
 }

@@ -294,8 +294,9 @@ struct KvPlan {
   int32_t* tok_seq;
   int32_t* tok_len;
   int32_t* n_refused;
+  bool packs;                // rows may be written four at a time (set by the launch)
 };
-cudaError_t launch_kv_plan(const KvPlan& p, cudaStream_t s);
+cudaError_t launch_kv_plan(KvPlan p, cudaStream_t s);
 cudaError_t launch_kv_append(const KvCache& c, const void* K_new, const void* V_new, int src_dtype,
                              long long T, long long ld, const int32_t* slot, cudaStream_t s);
 struct KvAttention {

@@ -863,8 +863,8 @@ cudaError_t run_pass(KvPass p, int sms, int* status, cudaStream_t s) {
   p.stages = std::min(kMostStages, (kRingsMost / warps - Core::kScratch) / slot);
   const int grid = std::min(sms, kKvMostSms), ring = warps * (p.stages * slot + Core::kScratch);
   p.block_workers = warps;
-  const cudaError_t e = cudaFuncSetAttribute(kv_blocks_kernel<Core>,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, kRingsMost);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(kv_blocks_kernel<Core>, kRingsMost, done);
   if (e != cudaSuccess) return e;
   const cudaError_t f = launch_pdl(kv_blocks_kernel<Core>, dim3(grid), dim3(warps * 32), ring, s, p, status);
   return f != cudaSuccess ? f : run_join<E>(p, sms, s);

@@ -13,23 +13,21 @@ namespace {
 // columns, so that few queries waste nothing:
 //   S^T [128 tokens, NQ] = K Q^T          (K tile and Q by rows of elements)
 //   O^T [dim, NQ]       += V^T P^T        (V tile and P by rows of tokens, both read transposed)
-// with S^T twice and O^T in tensor memory.  A thread of the softmax has one token (a lane) and half the
-// queries (columns): no sum crosses lanes until the item ends, the weights leave as 16-byte packs
+// with S^T twice and O^T in tensor memory.  A thread of the softmax has one token (a lane) and its
+// group's queries (columns): no sum crosses lanes until the item ends, the weights leave as 16-byte packs
 // into the shared-memory layout that the second product reads, and the running references are lagging
 // ones, in shared memory: a tile whose scores stay below reference + kLag needs one vote of the threads.
-//   Warps: 8 softmax (two groups of 4, half the queries each), 4 copy (K and V tiles of 128 tokens,
-// gathered by rows of their pages, in a ring), 1 issues products and 3 make its group whole: registers
-// move between groups of 4 (launched with 128 a thread; 2 x 168 + 2 x 88 = 4 x 128).
+//   Warps: groups of 4 for the softmax (two or four, each with its share of the queries), 4 copy (K and V
+// tiles of 128 tokens, gathered by rows of their pages, in a ring), 1 issues products and 3 make its group
+// whole.  A tile's softmax is a chain of waits more than work, so more groups of fewer columns each are
+// faster as long as their sums fit the registers.
 //   A copy warp has 32 tokens of a tile.  Where a token's row is a row of one matrix over the whole cache
 // and pages hold a multiple of 8 tokens, it fetches them by TMA in boxes of 8, 16 or 32 rows; the last
 // tokens of a run and other layouts come by 16-byte copies, which an SM carries out at 24 bytes a cycle
 // at most (all of it so: 128 blocks of 16 rows over 1024 to 3000 tokens 353 us; by tile::gather4, which
 // would serve any page, 644).
 constexpr int kBlk = 128;
-constexpr int kSoftWarps = 8, kCopyWarp = 8, kCopyWarps = 4, kMmaWarp = 12;
-constexpr int kWarps = 16, kThreads = kWarps * 32;
-constexpr int kSoftRegs = 168, kOtherRegs = 88;
-static_assert(2 * kSoftRegs + 2 * kOtherRegs <= 4 * 128, "the launch's registers");
+constexpr int kCopyWarps = 4;
 constexpr int kInfo = 8;           // tiles whose masks and flags are kept
 constexpr float kLag = 8.f;        // log2: weights of up to 2^8 relative to the reference
 constexpr float kNoRef = -FLT_MAX;
@@ -42,8 +40,16 @@ struct Cfg {
   static constexpr int kPBytes = (kNQ / 64) * kBlk * 128;
   static constexpr int kQBufs = 2, kPBufs = kNQ == 128 && kChunks == 2 ? 1 : 2;
   static constexpr int kSlots = kChunks == 1 ? 8 : kNQ == 128 ? 4 : 5;
-  static constexpr int kHalf = kNQ / 2;                    // queries of a softmax group
-  static constexpr int kParts = kHalf / 32;                // 32 columns at a time
+  static constexpr int kGroups = kNQ == 128 ? 2 : 4;       // of 4 softmax warps
+  static constexpr int kOwn = kNQ / kGroups;               // queries of a group ...
+  static constexpr int kW = kOwn < 32 ? kOwn : 32;         // ... and columns at a time
+  static constexpr int kParts = kOwn / kW;
+  static constexpr int kSoftWarps = 4 * kGroups, kCopyWarp = kSoftWarps, kMmaWarp = kCopyWarp + kCopyWarps;
+  static constexpr int kWarps = kMmaWarp + 4, kThreads = kWarps * 32;
+  // Registers: two groups hold 64 columns' sums each and take some from the other warps (128 a thread at
+  // the launch); four hold 16 columns' each in what all have.
+  static constexpr int kSoftRegs = kGroups == 2 ? 168 : 0, kOtherRegs = kGroups == 2 ? 88 : 0;
+  static_assert(2 * kSoftRegs + 2 * kOtherRegs <= 4 * 128, "the launch's registers");
   static constexpr int kCols = kNQ == 128 ? 512 : 256;     // tensor memory: S^T, S^T, O^T
   static constexpr size_t kBig = size_t(kSlots) * kTile + kQBufs * kQBytes + kPBufs * kPBytes;
 };
@@ -57,23 +63,23 @@ struct alignas(16) KvMisc {
   uint32_t bad[4];                        // queries with a value that is not finite
   WorkerStart start[2];
   Line line;                              // needed again at the end alone
-  long long buf[kWarps];
+  long long buf[24];
 };
 
 template <class C>
 struct KvSmem {
   KvMisc m;
-  float top[kSoftWarps][32];              // a slow tile's maxima
+  float top[C::kSoftWarps][C::kW];        // a slow tile's maxima
   float ref[C::kNQ];                      // references (scores)
   int vis[C::kNQ];                        // tokens of the run that a query sees
 };
 static_assert(sizeof(KvMisc) % 16 == 0, "what follows is read as packs of 16 bytes");
 
-// At an item's end: sums and destinations of all queries, and a place to turn 32 queries' rows.
+// At an item's end: sums and destinations of all queries, and each group's place to turn kW queries' rows.
 template <class C>
-constexpr int end_bytes() { return kSoftWarps * C::kHalf * 4 + C::kNQ * int(sizeof(KvRowOut)); }
+constexpr int end_bytes() { return C::kSoftWarps * C::kOwn * 4 + C::kNQ * int(sizeof(KvRowOut)); }
 template <class C>
-constexpr int stage_bytes() { return 32 * C::kChunks * 128; }
+constexpr int stage_bytes() { return C::kW * C::kChunks * 128; }
 
 template <class C>
 constexpr size_t smem_bytes() { return C::kBig + sizeof(KvSmem<C>); }
@@ -99,6 +105,15 @@ ALR_DEV void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
                  "=r"(r[7])
                : "r"(taddr));
+}
+ALR_DEV void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld32(taddr, r); }
+ALR_DEV void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+      "%14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
 }
 ALR_DEV void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]),
@@ -137,15 +152,16 @@ struct Place {
   }
 };
 
-// The slow tile of a softmax group: the references of 32 columns move to the maxima with this tile, the
-// products so far (if any) are scaled.  Lane k returns the factor of column k.  pos: the thread's token,
+// The slow tile of a softmax group: the references of kW columns move to the maxima with this tile, the
+// products so far (if any) are scaled.  Lane k returns the factor of column k (mod kW).  pos: the thread's token,
 // INT_MAX if its page does not exist.
+template <int kW>
 __device__ __noinline__ float move_refs(uint32_t s_at, uint32_t o_at, float c, float* ref, const int* vis,
-                                        float (*top)[32], int bar, int pos, bool scale_o) {
-  const int lane = threadIdx.x & 31, wq = threadIdx.x >> 5 & 3;
+                                        float (*top)[kW], int bar, int pos, bool scale_o) {
+  const int lane = threadIdx.x % kW, wq = threadIdx.x >> 5 & 3;
   float most = kNegInf;
 #pragma unroll 1
-  for (int k0 = 0; k0 < 32; k0 += 8) {
+  for (int k0 = 0; k0 < kW; k0 += 8) {
     uint32_t s[8];
     tmem_ld8(s_at + k0, s);
     tmem_ld_wait();
@@ -166,7 +182,7 @@ __device__ __noinline__ float move_refs(uint32_t s_at, uint32_t o_at, float c, f
   if (wq == 0) ref[lane] = up;
   if (scale_o) {
 #pragma unroll 1
-    for (int k0 = 0; k0 < 32; k0 += 8) {
+    for (int k0 = 0; k0 < kW; k0 += 8) {
       uint32_t s[8];
       tmem_ld8(o_at + k0, s);
       tmem_ld_wait();
@@ -183,10 +199,11 @@ __device__ __noinline__ float move_refs(uint32_t s_at, uint32_t o_at, float c, f
 }
 
 template <class C>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(C::kThreads, 1)
     kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvPass p, int* status) {
   using E = __nv_bfloat16;
-  constexpr int kNQ = C::kNQ, kSlots = C::kSlots;
+  constexpr int kNQ = C::kNQ, kSlots = C::kSlots, kThreads = C::kThreads;
+  constexpr int kSoftWarps = C::kSoftWarps, kCopyWarp = C::kCopyWarp, kMmaWarp = C::kMmaWarp;
   extern __shared__ __align__(1024) uint8_t tc_smem[];
   uint8_t* ring = tc_smem;
   uint8_t* qs = ring + kSlots * C::kTile;
@@ -237,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp >= kCopyWarp && warp < kMmaWarp) {
     // ---- copies
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if constexpr (C::kOtherRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kOtherRegs));
     const int w = warp - kCopyWarp;
     constexpr int kRowsAt = 4 / C::kChunks, kPer = 32 / kRowsAt;     // rows of one copy instruction
     const int pack = lane & (8 * C::kChunks - 1), sub = lane / (8 * C::kChunks);
@@ -365,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp >= kMmaWarp) {
     // ---- products
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if constexpr (C::kOtherRegs > 0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kOtherRegs));
     if (warp == kMmaWarp && lane == 0 && count > 0) {
       constexpr uint32_t i_s = idesc_make(false, 128, kNQ, false, false);
       constexpr uint32_t i_o = idesc_make(false, 128, kNQ, true, true);
@@ -426,18 +443,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     // ---- softmax
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
-    constexpr int kHalf = C::kHalf, kParts = C::kParts;
+    if constexpr (C::kSoftRegs > 0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftRegs));
+    constexpr int kOwn = C::kOwn, kW = C::kW, kParts = C::kParts, kAllBar = 5, kAll = kSoftWarps * 32;
     const int wg = warp >> 2, wq = warp & 3, bar = 1 + wg, tid = threadIdx.x & 127;
     const uint32_t lanes = tmem + (uint32_t(wq * 32) << 16);
-    const int tok = tid, q0 = wg * kHalf;
+    const int tok = tid, q0 = wg * kOwn;
     const float c = a.scale * kLog2e;
     const uint64_t c2 = f2_pack(c, c);
-    float l[kHalf];
+    float l[kOwn];
     Cursor<kBlk> at;
     if (count > 0) at.start(p, mi.start[0].tile, mi.start[0].unit, mi.start[0].b);
-    float (*lsum)[kHalf] = reinterpret_cast<float (*)[kHalf]>(ps);               // at an item's end
-    KvRowOut* outs = reinterpret_cast<KvRowOut*>(ps + kSoftWarps * kHalf * sizeof(float));
+    float (*lsum)[kOwn] = reinterpret_cast<float (*)[kOwn]>(ps);               // at an item's end
+    KvRowOut* outs = reinterpret_cast<KvRowOut*>(ps + kSoftWarps * kOwn * sizeof(float));
     constexpr int kEndBytes = end_bytes<C>(), kStageBytes = stage_bytes<C>();
     int4 cut = make_int4(0, 0, 0, 0);
     int i = 0;
@@ -449,9 +466,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Tile tile = at.t;
       const int tile_id = at.tile, unit = at.unit, b0 = at.b, b1 = min(tile.nb, b0 + (count - i));
       const int i0 = i;
-      if (tid < kHalf) sm.ref[q0 + tid] = kNoRef;
+      if (tid < kOwn) sm.ref[q0 + tid] = kNoRef;
 #pragma unroll
-      for (int k = 0; k < kHalf; ++k) l[k] = 0.f;
+      for (int k = 0; k < kOwn; ++k) l[k] = 0.f;
       int run = -2, least = 0;
       for (int b = b0; b < b1; ++b, ++i) {
         if (at.lead != run) {
@@ -461,9 +478,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           least = warp_min(lane < n_rows ? see : INT_MAX);
           named_bar_sync(bar, 128);
           if (wq == 0)
-            for (int k = 0; k < kHalf; k += 32) {
+            for (int k = 0; k < kOwn; k += 32) {
               const int q = q0 + k + lane, v = __shfl_sync(~0u, see, (q / p.gw) & 31);
-              sm.vis[q] = q < n_q ? v : INT_MAX;
+              if (k + lane < kOwn) sm.vis[q] = q < n_q ? v : INT_MAX;
             }
           named_bar_sync(bar, 128);
         }
@@ -477,18 +494,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint8_t* prow = ps + pb * C::kPBytes + tok * 128;
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
-          float y[32];
+          float y[kW];
           // Exponents are differences of scores, times c (the fma s c - ref c would leave the rounding of
           // ref c, which is more than 2^8 from |ref c| = 2^32 on): after a move none is above 0.
           for (bool moved = false;; moved = true) {
-            uint32_t s[32];
-            tmem_ld32(s_at + part * 32, s);
-            const float* ref = sm.ref + q0 + part * 32;
+            uint32_t s[kW];
+            tmem_ld_cols(s_at + part * kW, s);
+            const float* ref = sm.ref + q0 + part * kW;
             float t = kNegInf;
             tmem_ld_wait();
             reg_fence(s);
 #pragma unroll
-            for (int k = 0; k < 32; k += 4) {
+            for (int k = 0; k < kW; k += 4) {
               const float4 r = *reinterpret_cast<const float4*>(ref + k);
               f2_unpack(f2_mul(f2_sub(f2_pack(__uint_as_float(s[k]), __uint_as_float(s[k + 1])),
                                       f2_pack(r.x, r.y)), c2), y[k], y[k + 1]);
@@ -496,9 +513,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                                       f2_pack(r.z, r.w)), c2), y[k + 2], y[k + 3]);
             }
             if (!plain) {
-              const int* vis = sm.vis + q0 + part * 32;
+              const int* vis = sm.vis + q0 + part * kW;
 #pragma unroll
-              for (int k = 0; k < 32; k += 4) {
+              for (int k = 0; k < kW; k += 4) {
                 const int4 r = *reinterpret_cast<const int4*>(vis + k);
                 y[k] = pos < r.x ? y[k] : kNegInf;
                 y[k + 1] = pos < r.y ? y[k + 1] : kNegInf;
@@ -507,31 +524,31 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             }
 #pragma unroll
-            for (int k = 0; k < 32; k += 2) t = max3(t, y[k], y[k + 1]);
+            for (int k = 0; k < kW; k += 2) t = max3(t, y[k], y[k + 1]);
             if (moved || !any_of(bar, 128, t > kLag)) break;
             if (i > i0) {
               wait_on(&mi.pv_done[C::kPBufs == 2 ? (i - 1) & 1 : 0], C::kPBufs == 2 ? (i - 1) >> 1 : i - 1, ab);
               tc_fence_after();
             }
-            const float f = move_refs(s_at + part * 32, o_at + part * 32, c, sm.ref + q0 + part * 32,
-                                      sm.vis + q0 + part * 32, sm.top + wg * 4, bar, pos, i > i0);
+            const float f = move_refs<kW>(s_at + part * kW, o_at + part * kW, c, sm.ref + q0 + part * kW,
+                                      sm.vis + q0 + part * kW, sm.top + wg * 4, bar, pos, i > i0);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) l[part * 32 + k] *= __shfl_sync(~0u, f, k);
+            for (int k = 0; k < kW; ++k) l[part * kW + k] *= __shfl_sync(~0u, f, k);
           }
           // this buffer's last product
           if (part == 0 && i >= C::kPBufs)
             wait_on(&mi.pv_done[pb], C::kPBufs == 2 ? (i >> 1) - 1 : i - 1, ab);
 #pragma unroll
-          for (int k = 0; k < 32; k += 8) {
+          for (int k = 0; k < kW; k += 8) {
             uint32_t x[4];
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
               const float u = ex2(y[k + e]), v = ex2(y[k + e + 1]);
-              l[part * 32 + k + e] += u;
-              l[part * 32 + k + e + 1] += v;
+              l[part * kW + k + e] += u;
+              l[part * kW + k + e + 1] += v;
               x[e / 2] = bf16x2(u, v);   // the product's only operand type: off by 2^-8, l is not
             }
-            const int q = q0 + part * 32 + k;
+            const int q = q0 + part * kW + k;
             *reinterpret_cast<uint4*>(prow + (q >> 6) * (kBlk * 128) + ((((q & 63) >> 3) ^ (tok & 7)) << 4)) =
                 make_uint4(x[0], x[1], x[2], x[3]);
           }
@@ -547,22 +564,24 @@ __global__ void __launch_bounds__(kThreads, 1)
       // ---- the item's results
       wait_on(&mi.pv_done[C::kPBufs == 2 ? (i - 1) & 1 : 0], C::kPBufs == 2 ? (i - 1) >> 1 : i - 1, ab);
       tc_fence_after();
-      named_bar_sync(3, 256);                // both groups are past their last weights
+      named_bar_sync(kAllBar, kAll);                // both groups are past their last weights
       // sums over the warp's tokens: lane k ends with column k's
 #pragma unroll
       for (int part = 0; part < kParts; ++part) {
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) {
+        for (int off = kW / 2; off > 0; off >>= 1) {
           const bool upper = (lane & off) != 0;
 #pragma unroll
           for (int k = 0; k < off; ++k) {
-            float& lo = l[part * 32 + k];
-            const float hi = l[part * 32 + k + off];
+            float& lo = l[part * kW + k];
+            const float hi = l[part * kW + k + off];
             const float give = upper ? lo : hi, keep = upper ? hi : lo;
             lo = keep + __shfl_xor_sync(~0u, give, off);
           }
         }
-        lsum[warp][part * 32 + lane] = l[part * 32];
+        float sum = l[part * kW];
+        if (kW == 16) sum += __shfl_xor_sync(~0u, sum, 16);
+        if (lane < kW) lsum[warp][part * kW + lane] = sum;
       }
       named_bar_sync(bar, 128);
       const bool whole = b0 == 0 && b1 == tile.nb, opens = b0 == 0 && b1 < tile.nb;
@@ -571,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         return whole ? row_out(p, row0 + r, h0 + q - r * p.gw, m, s, writer)
                      : part_out(p, p.block_parts, part_id, q, m, s, writer);
       };
-      if (tid < kHalf) {
+      if (tid < kOwn) {
         const int q = q0 + tid, r = q / p.gw;
         float s = 0.f;
         for (int k = 0; k < 4; ++k) s += lsum[wg * 4 + k][tid];
@@ -585,19 +604,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool final_row = whole && p.put_o == nullptr;
       float odd = 0.f;                       // NaN after a value that is not finite
       // Sums and prefixes leave as they lie, 128 bytes a warp's store; final rows go through shared memory (this
-      // group's quarter of the weights' place, 32 queries at a time), into packs of 16 bytes.
+      // group's share of the weights' place, kW queries at a time), into packs of 16 bytes.
       E* stage = reinterpret_cast<E*>(ps + kEndBytes + wg * kStageBytes);
 #pragma unroll 1
-      for (int k0 = 0; k0 < kHalf && q0 + k0 < n_q; k0 += 32) {
-        uint32_t s[32];
-        tmem_ld32(lanes + 2 * kNQ + q0 + k0, s);
+      for (int k0 = 0; k0 < kOwn && q0 + k0 < n_q; k0 += kW) {
+        uint32_t s[kW];
+        tmem_ld_cols(lanes + 2 * kNQ + q0 + k0, s);
         tmem_ld_wait();
         reg_fence(s);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) odd = fmaf(0.f, d < dim && q0 + k0 + k < n_q ? __uint_as_float(s[k]) : 0.f, odd);
+        for (int k = 0; k < kW; ++k) odd = fmaf(0.f, d < dim && q0 + k0 + k < n_q ? __uint_as_float(s[k]) : 0.f, odd);
         if (!final_row) {
 #pragma unroll
-          for (int k = 0; k < 32; ++k) {
+          for (int k = 0; k < kW; ++k) {
             float* to = outs[q0 + k0 + k].dst_f;
             if (q0 + k0 + k < n_q && to != nullptr && d < dim) to[d] = __uint_as_float(s[k]);
           }
@@ -605,21 +624,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (p.pre_o != nullptr) {
 #pragma unroll
-          for (int k = 0; k < 32; ++k) {
+          for (int k = 0; k < kW; ++k) {
             const KvRowOut& o = outs[q0 + k0 + k];
             const float pre = q0 + k0 + k < n_q && o.dst != nullptr && d < dim ? o.pre[d] * o.f_pre : 0.f;
             s[k] = __float_as_uint(fmaf(__uint_as_float(s[k]), o.f, pre));
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < 32; ++k) s[k] = __float_as_uint(__uint_as_float(s[k]) * outs[q0 + k0 + k].f);
+          for (int k = 0; k < kW; ++k) s[k] = __float_as_uint(__uint_as_float(s[k]) * outs[q0 + k0 + k].f);
         }
 #pragma unroll
-        for (int k = 0; k < 32; ++k)
+        for (int k = 0; k < kW; ++k)
           if (d < C::kChunks * 64) stage[k * (C::kChunks * 64) + d] = E(__uint_as_float(s[k]));
         named_bar_sync(bar, 128);
         const int packs = dim / 8;
-        for (int i = tid; i < 32 * packs; i += 128) {
+        for (int i = tid; i < kW * packs; i += 128) {
           const int k = i / packs, c = i - k * packs;
           E* to = q0 + k0 + k < n_q ? static_cast<E*>(outs[q0 + k0 + k].dst) : nullptr;
           if (to != nullptr)
@@ -628,10 +647,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         named_bar_sync(bar, 128);
       }
       if (!(odd == 0.f)) {                   // which queries: rare
-        for (int k = 0; k < kHalf && q0 + k < n_q; ++k) atomicOr(&mi.bad[(q0 + k) >> 5], 1u << ((q0 + k) & 31));
+        for (int k = 0; k < kOwn && q0 + k < n_q; ++k) atomicOr(&mi.bad[(q0 + k) >> 5], 1u << ((q0 + k) & 31));
       }
       tc_fence_before();
-      named_bar_sync(3, 256);
+      named_bar_sync(kAllBar, kAll);
       if (n_rows > 1 && (mi.bad[0] | mi.bad[1] | mi.bad[2] | mi.bad[3]) != 0) {
         // Weights of 0 times a value that is not finite: such a value may lie in a token that the
         // query does not see but another of the tile does.  Its tokens again, one by one.
@@ -656,10 +675,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (e * 32 + lane < dim) put<E, 1>(to, e * 32 + lane, v);
           }
         }
-        named_bar_sync(3, 256);
+        named_bar_sync(kAllBar, kAll);
         if (threadIdx.x < 4) mi.bad[threadIdx.x] = 0;
       } else if (n_rows <= 1) {
-        named_bar_sync(3, 256);
+        named_bar_sync(kAllBar, kAll);
         if (threadIdx.x < 4) mi.bad[threadIdx.x] = 0;
       }
       if (opens && threadIdx.x == 0) {
@@ -677,14 +696,14 @@ __global__ void __launch_bounds__(kThreads, 1)
 template <class C>
 cudaError_t run_tc(KvPass& p, const KvMaps& maps, int sms, int* status, cudaStream_t s) {
   static_assert(smem_bytes<C>() <= 227 * 1024, "fits an SM");
-  static_assert(end_bytes<C>() + 2 * stage_bytes<C>() <= C::kPBytes * C::kPBufs,
+  static_assert(end_bytes<C>() + C::kGroups * stage_bytes<C>() <= C::kPBytes * C::kPBufs,
                 "an item's end reuses the weights' place");
   shape_pass(p, C::kNQ, 32, kBlk);
   p.block_workers = 1;
-  const cudaError_t e = cudaFuncSetAttribute(
-      kv_tc_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem_bytes<C>()));
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(kv_tc_kernel<C>, int(smem_bytes<C>()), done);
   if (e != cudaSuccess) return e;
-  return launch_pdl(kv_tc_kernel<C>, dim3(std::min(sms, kKvMostSms)), dim3(kThreads), smem_bytes<C>(), s,
+  return launch_pdl(kv_tc_kernel<C>, dim3(std::min(sms, kKvMostSms)), dim3(C::kThreads), smem_bytes<C>(), s,
                     maps, p, status);
 }
 

@@ -11,11 +11,13 @@ namespace {
 // ------------------------------------------------------------------------ plan ---
 // Everything follows from sums over the sequences before one: of the tokens asked for (its first row of
 // the batch), of the new pages (its place in the list of free pages) and of the returned ones (theirs).
-// Each block takes those sums over all sequences for itself (S is at most 8192, 8 KB a thousand), the
-// blocks of the one cluster meet at its barrier, so that what is updated in place has been read by all,
-// and share the writing: a token's page is found from its sequence's sums, be it an old one, one out of
-// the pool or one that another sequence returns in this step.  No block reads what another writes.
-//   Bound by latency: two loads, two scans, a barrier, two dependent loads a token.
+// Each block takes those sums over all sequences for itself (S is at most 8192, 8 KB a thousand).  A
+// token's page is found from its sequence's sums, be it an old one, one out of the pool or one that
+// another sequence returns in this step, so blocks share rows and pages and none reads what another
+// writes.  Lengths and the pool's count may be updated in place: one block does everything where rows are
+// few, else a second launch writes them.
+//   Bound by latency: two loads, two scans, two dependent loads a token (768 rows: 11 us of host and GPU
+// together; 393 thousand rows of 96 prompts: 2x us, by one cluster of 8 blocks and one launch 47).
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
 
@@ -55,10 +57,11 @@ struct PlanSums {
 
 ALR_DEV int pages_of(long long tokens, int page) { return int((tokens + page - 1) / page); }
 
-__global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlan p, int n_cta) {
+// rows: write rows, tables and the pool (blocks share them); sums: lengths, starts and counts (one block).
+__global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlan p, bool rows, bool sums) {
   extern __shared__ int plan_smem[];
   __shared__ long long buf[kPlanWarps];
-  const int S = p.S, tid = threadIdx.x, rank = blockIdx.x;
+  const int S = p.S, tid = threadIdx.x, rank = blockIdx.x, n_cta = gridDim.x;
   const PlanSums t = {plan_smem, plan_smem + S + 1, plan_smem + 2 * S + 1, plan_smem + 3 * S + 1};
   pdl_wait_and_release();
   const int used = min(max(*p.pool_used, 0), p.n_pool);
@@ -92,7 +95,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlan p, i
   int refused = 0;
   long long k = need_before, n_new = 0;
   row = before;
-  cluster_sync();                            // every block has read len and pool_used: they may be written
+  __syncthreads();                           // len and pool_used have been read: they may be written
   for (int s = s0; s < s1; ++s) {
     const int a = t.start[s], n = t.len[s];
     const bool asks = a >= 0 && n + (long long)a <= most && row + a <= p.T;
@@ -104,7 +107,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlan p, i
     if (!ok) t.len[s] = ~n;
     if (a >= 0 && !ok) ++refused;
     if (ok && w > 0) n_new = k + w;
-    if (rank == 0) {
+    if (sums) {
       p.out_len[s] = a < 0 ? 0 : ok ? n + a : n;
       if (p.start != nullptr) p.start[s] = int(min(row, (long long)INT32_MAX));
     }
@@ -114,16 +117,17 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlan p, i
   const int n_rows = int(min(all, (long long)p.T));
   if (tid == 0) {
     t.start[S] = n_rows;
-    if (rank == 0 && p.start != nullptr) p.start[S] = int(min(all, (long long)INT32_MAX));
+    if (sums && p.start != nullptr) p.start[S] = int(min(all, (long long)INT32_MAX));
   }
   n_new = block_reduce(n_new, MaxOp(), buf);
-  if (rank == 0) {
+  if (sums) {
     const long long r = block_reduce((long long)refused, AddOp(), buf);
     if (tid == 0) {
       *p.out_used = int(max(used - n_back + n_new, 0ll));
       if (p.n_refused != nullptr) *p.n_refused = int(r);
     }
   }
+  if (!rows) return;
   __syncthreads();
 
   // page number i of the list of free pages: the returned ones, then the pool's
@@ -144,31 +148,83 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlan p, i
     const int n = t.len[s] < 0 ? ~t.len[s] : t.len[s];
     p.table[(long long)s * p.cols + pages_of(n, p.page) + (int(i) - t.fresh[s])] = page_at(int(i));
   }
-  // rows: each warp a stretch of its own, whose sequences follow one another
-  const int n_warps = n_cta * kPlanWarps, stretch = ((p.T + n_warps - 1) / n_warps + 31) / 32 * 32;
+  // rows: one each where there are threads for all (a step of single tokens), else each warp has a stretch of
+  // its own, whose sequences follow one another, a lane four rows at a time, which mostly lie in one page
+  const int n_warps = n_cta * kPlanWarps, stretch = ((p.T + n_warps - 1) / n_warps + 127) / 128 * 128;
   const long long r0 = (long long)(rank * kPlanWarps + (tid >> 5)) * stretch;
   int s = -1;
-  for (long long r = r0 + (tid & 31); r < min(r0 + stretch, (long long)p.T); r += 32) {
-    int seq = -1, n = 0, slot = -1;
+  const auto owner = [&](int r) {            // sequence of row r < n_rows, searched from the last one on
+    if (s >= 0 && r >= t.start[s] && r < t.start[s + 1]) return s;
+    int i = s < 0 || r < t.start[s] ? S : s + 1;
+    for (int c = 0; c < 4 && i < S && r >= t.start[i + 1]; ++c) ++i;
+    return i < S && r < t.start[i + 1] ? i : owner_of(t.start, S, r);
+  };
+  const auto slot_at = [&](int pg, int off) {
+    const long long at = (long long)pg * p.page + off;
+    return pg < 0 || at > INT32_MAX ? -1 : int(at);
+  };
+  const auto page_of = [&](int q, int j) {   // the j-th page of sequence q
+    const int old = pages_of(t.len[q], p.page);
+    return j < old ? p.table[(long long)q * p.cols + j] : page_at(t.fresh[q] + (j - old));
+  };
+  if (p.T <= n_cta * kPlanThreads) {
+    const int r = rank * kPlanThreads + tid;
+    if (r >= p.T) return;
+    int slot = -1, seq = -1, n = 0;
     if (r < n_rows) {
-      if (s < 0 || r >= t.start[s + 1]) {
-        int i = s < 0 ? S : s + 1;
-        for (int c = 0; c < 4 && i < S && r >= t.start[i + 1]; ++c) ++i;
-        s = i < S && r < t.start[i + 1] ? i : owner_of(t.start, S, int(r));
-      }
-      const int held = t.len[s];
-      if (held >= 0) {
-        const int pos = held + int(r) - t.start[s], j = pos / p.page, old = pages_of(held, p.page);
-        const int pg = j < old ? p.table[(long long)s * p.cols + j] : page_at(t.fresh[s] + (j - old));
+      s = owner_of(t.start, S, r);
+      if (t.len[s] >= 0) {
+        const int at = t.len[s] + r - t.start[s], k = at / p.page;
         seq = s;
-        n = pos + 1;
-        const long long at = (long long)pg * p.page + pos % p.page;
-        slot = pg < 0 || at > INT32_MAX ? -1 : int(at);
+        n = at + 1;
+        slot = slot_at(page_of(s, k), at - k * p.page);
       }
     }
     p.slot[r] = slot;
     if (p.tok_seq != nullptr) p.tok_seq[r] = seq;
     if (p.tok_len != nullptr) p.tok_len[r] = n;
+    return;
+  }
+  for (long long r = r0 + 4 * (tid & 31); r < min(r0 + stretch, (long long)p.T); r += 128) {
+    int slot[4] = {-1, -1, -1, -1}, seq[4] = {-1, -1, -1, -1}, n[4] = {};
+    if (r < n_rows) {
+      s = owner(int(r));
+      const int held = t.len[s], pos = held + int(r) - t.start[s], j = pos / p.page, off = pos - j * p.page;
+      if (r + 3 < t.start[s + 1] && off + 3 < p.page) {
+        if (held >= 0) {
+          const int first = slot_at(page_of(s, j), off);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            seq[e] = s;
+            n[e] = pos + e + 1;
+            slot[e] = first < 0 ? -1 : first + e;
+          }
+        }
+      } else {
+#pragma unroll 1
+        for (int e = 0; e < 4 && r + e < n_rows; ++e) {
+          s = owner(int(r) + e);
+          if (t.len[s] < 0) continue;
+          const int at = t.len[s] + int(r) + e - t.start[s], k = at / p.page;
+          seq[e] = s;
+          n[e] = at + 1;
+          slot[e] = slot_at(page_of(s, k), at - k * p.page);
+        }
+      }
+    }
+    const auto put = [&](int32_t* to, const int (&v)[4]) {
+      if (to == nullptr) return;
+      if (p.packs && r + 3 < p.T) {
+        *reinterpret_cast<int4*>(to + r) = make_int4(v[0], v[1], v[2], v[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (r + e < p.T) to[r + e] = v[e];
+      }
+    };
+    put(p.slot, slot);
+    put(p.tok_seq, seq);
+    put(p.tok_len, n);
   }
 }
 
@@ -226,23 +282,18 @@ cudaError_t run_append(const KvCache& c, const void* K_new, const void* V_new, l
 
 }  // namespace
 
-cudaError_t launch_kv_plan(const KvPlan& p, cudaStream_t s) {
-  const int n_cta = p.T <= 4096 ? 1 : 8;
+cudaError_t launch_kv_plan(KvPlan p, cudaStream_t s) {
+  const auto packs = [](const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15) == 0; };
+  p.packs = packs(p.slot) && packs(p.tok_seq) && packs(p.tok_len);
   const size_t smem = size_t(4 * p.S + 1) * sizeof(int);
-  cudaError_t e = cudaFuncSetAttribute(kv_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       int(size_t(4 * kKvMaxSeqs + 1) * sizeof(int)));
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(kv_plan_kernel, int((4 * kKvMaxSeqs + 1) * sizeof(int)), done);
   if (e != cudaSuccess) return e;
-  cudaLaunchAttribute attr[2] = {pdl_attribute(), {}};
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim = {unsigned(n_cta), 1, 1};
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(n_cta);
-  cfg.blockDim = dim3(kPlanThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kv_plan_kernel, p, n_cta);
+  const int n_cta = std::min((p.T + 4095) / 4096, 128);
+  if (n_cta <= 1) return launch_pdl(kv_plan_kernel, dim3(1), dim3(kPlanThreads), smem, s, p, true, true);
+  const cudaError_t f = launch_pdl(kv_plan_kernel, dim3(n_cta), dim3(kPlanThreads), smem, s, p, true, false);
+  return f != cudaSuccess ? f
+                          : launch_pdl(kv_plan_kernel, dim3(1), dim3(kPlanThreads), smem, s, p, false, true);
 }
 
 cudaError_t launch_kv_append(const KvCache& c, const void* K_new, const void* V_new, int src_dtype,

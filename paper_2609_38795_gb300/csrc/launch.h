@@ -1,6 +1,9 @@
 // Launch helper: programmatic dependent launch.
 #pragma once
 
+#include <atomic>
+#include <cstdint>
+
 #include <cuda_runtime.h>
 
 namespace alr {
@@ -43,6 +46,18 @@ template <typename... KArgs, typename... Args>
 cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
                        const Args&... args) {
   return launch_pdl_sized(0.0, kern, grid, block, smem, s, args...);
+}
+
+// Opt-in shared memory of a kernel, asked for once per device (the call takes half a microsecond).
+template <typename... KArgs>
+cudaError_t allow_smem(void (*kern)(KArgs...), int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1)) return cudaSuccess;
+  const cudaError_t f = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (f == cudaSuccess && dev < 64) done.fetch_or(uint64_t(1) << dev, std::memory_order_relaxed);
+  return f;
 }
 
 }  // namespace alr
