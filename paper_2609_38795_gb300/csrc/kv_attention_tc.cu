@@ -404,11 +404,11 @@ __global__ void __launch_bounds__(C::kThreads, 1)
         fence_proxy_async_smem();
         tc_fence_after();
         // dim <= 64: rows 64 to 127 of the result come from whatever lies behind the tile, unused
-        const uint64_t va = v_desc + from.slot * (C::kTile >> 4), pa = p_desc + pb * (C::kPBytes >> 4);
-        mma_issue<false>(tmem + 2 * kNQ, va, pa, i_o, !(info & 1));
-#pragma unroll
-        for (int k = 1; k < kBlk / 16; ++k)
-          mma_issue<false>(tmem + 2 * kNQ, va + k * (2048 >> 4), pa + k * (2048 >> 4), i_o, 1);
+        uint64_t va = v_desc + from.slot * (C::kTile >> 4), pa = p_desc + pb * (C::kPBytes >> 4);
+        uint32_t add = !(info & 1);
+#pragma unroll 1
+        for (int k = 0; k < kBlk / 16; ++k, va += 2048 >> 4, pa += 2048 >> 4, add = 1)
+          mma_issue<false>(tmem + 2 * kNQ, va, pa, i_o, add);
         mma_commit(&mi.empty[from.slot]);
         mma_commit(&mi.pv_done[pb]);
         from.next();
@@ -422,13 +422,14 @@ __global__ void __launch_bounds__(C::kThreads, 1)
         if (i >= 2) wait_on(&mi.s_empty[sb], (i >> 1) - 1, ab);
         fence_proxy_async_smem();
         tc_fence_after();
-        const uint64_t ka = k_desc + from.slot * (C::kTile >> 4), qa = q_desc + (item & 1) * (C::kQBytes >> 4);
-        mma_issue<false>(tmem + sb * kNQ, ka, qa, i_s, 0);
-#pragma unroll
-        for (int k = 1; k < 4 * C::kChunks; ++k)
-          if (k < n_k)
-            mma_issue<false>(tmem + sb * kNQ, ka + (((k >> 2) * (kBlk * 128) + (k & 3) * 32) >> 4),
-                             qa + (((k >> 2) * (kNQ * 128) + (k & 3) * 32) >> 4), i_s, 1);
+        uint64_t ka = k_desc + from.slot * (C::kTile >> 4), qa = q_desc + (item & 1) * (C::kQBytes >> 4);
+#pragma unroll 1
+        for (int k = 0; k < n_k; ++k) {
+          mma_issue<false>(tmem + sb * kNQ, ka, qa, i_s, k);
+          // 32 bytes on, or to the next chunk of 64 elements
+          ka += (k & 3) == 3 ? (kBlk * 128 - 96) >> 4 : 32 >> 4;
+          qa += (k & 3) == 3 ? (kNQ * 128 - 96) >> 4 : 32 >> 4;
+        }
         mma_commit(&mi.empty[from.slot]);
         mma_commit(&mi.s_full[sb]);
         if (info & 2) mma_commit(&mi.q_empty[item & 1]);
