@@ -552,7 +552,7 @@ ALR_DEV void put_sums(const KvPass& p, const KvRowOut& to, const JoinSums& s) {
 // different items never wait for one another, and a ring's blocks (all but one ahead) are all that
 // hides latency.
 template <typename Core>
-__global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(const KvPass p, int* status) {
+__global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(const __grid_constant__ KvPass p, int* status) {
   using E = typename Core::E;
   constexpr int kPacks = Core::kPacks, kPack = 16 / sizeof(E);
   constexpr int kRowsAt = 32 / kPacks > 1 ? 32 / kPacks : 1;      // rows of one copy instruction
@@ -698,9 +698,7 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
         least = warp_min(lane < n_rows ? tokens : INT_MAX);
         core.see(p, tokens, n_q);
       }
-      // a wait that runs out is recorded and passed over: the loop goes on to its end
-      if (!mbar_try_wait(&landed[warp][slot], round & 1) && !*ab.smem)
-        mbar_wait(&landed[warp][slot], round & 1, ab);
+      wait_on(&landed[warp][slot], round, ab);
       __syncwarp();                              // all lanes are done with the slot that is filled next
       load_next();
       const uint32_t there = there_of[warp][slot];
@@ -810,7 +808,7 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
 
 // --------------------------------------------------- join of items across blocks ---
 template <typename E>
-__global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const KvPass p) {
+__global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const __grid_constant__ KvPass p) {
   __shared__ float4 sums[kJoinWarps][kKvMaxDim / 4];
   pdl_wait_and_release();
   const int id = blockIdx.x;

@@ -122,14 +122,6 @@ ALR_DEV void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
 }
 ALR_DEV void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// A wait that runs out is recorded, and every role runs on to the end of its loop (on data that no one
-// will use) with all other waits passed over, so that no barrier is left half full.
-ALR_DEV void wait_on(uint64_t* bar, uint32_t n, const AbortFlag& ab) {   // for completion n (from 0)
-  if (mbar_try_wait(bar, n & 1)) return;
-  if (*ab.smem) return;
-  mbar_wait(bar, n & 1, ab);
-}
-
 ALR_DEV uint32_t bf16x2(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -200,7 +192,7 @@ __device__ __noinline__ float move_refs(uint32_t s_at, uint32_t o_at, float c, f
 
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, 1)
-    kv_tc_kernel(const __grid_constant__ KvMaps maps, const KvPass p, int* status) {
+    kv_tc_kernel(const __grid_constant__ KvMaps maps, const __grid_constant__ KvPass p, int* status) {
   using E = __nv_bfloat16;
   constexpr int kNQ = C::kNQ, kSlots = C::kSlots, kThreads = C::kThreads;
   constexpr int kSoftWarps = C::kSoftWarps, kCopyWarp = C::kCopyWarp, kMmaWarp = C::kMmaWarp;
@@ -314,7 +306,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
       }
       const E* base = static_cast<const E*>(cache) + kv * a.c.sh + pack * 8;
       const uint32_t dst = ring_at + to.slot * C::kTile;
-#pragma unroll
+#pragma unroll 4
       for (int i = 0; i < kPer; ++i) {
         const int r = i * kRowsAt + sub;
         const long long from = __shfl_sync(~0u, row, r);
@@ -329,51 +321,58 @@ __global__ void __launch_bounds__(C::kThreads, 1)
     uint32_t all_v = 0;
     int kv_v = 0, item = -1, box_v = -1;
 #pragma unroll 1
-    for (int i = 0; i < count; ++i) {
+    for (int i = 0; i <= count && count > 0; ++i) {
       const Next cur = next;
       if (i + 1 < count) {
         const bool on = in.advance(p);
         look_up(on, i + 1);
       }
-      const bool there = cur.pg >= 0 && cur.pg < a.c.n_pages;
-      const uint32_t all = __ballot_sync(~0u, there);
-      const long long row = there ? cur.pg * a.c.sp + cur.off * a.c.st : 0;
-      const int kv = cur.unit / p.gs;
-      int box = -1;
-      if (n_boxes > 0 && cur.whole) {
-        const int from = (lane * maps.box_rows) & 31;
-        const int pg = __shfl_sync(~0u, there ? cur.pg : -1, from), off = __shfl_sync(~0u, cur.off, from);
-        box = pg >= 0 ? pg * maps.page_rows + off + kv * maps.head_rows : maps.n_rows;   // past the end: zeros
-      }
-      // flags and masks of tile i: read after its keys have landed; tile i - kInfo is long done with
-      // (its values' slot has been refilled since)
-      if (lane == 0) {
-        mi.there[i % kInfo][w] = all;
-        if (w == 0) mi.info[i % kInfo] = (cur.first ? 1u : 0u) | (cur.last ? 2u : 0u);
-      }
-      if (cur.first) {
-        ++item;
-        if (item >= 2) wait_on(&mi.q_empty[item & 1], (item >> 1) - 1, ab);
-        long long row0;
-        const int n_rows = max(tile_rows(p, cur.tile, row0), 0);
-        const int group_q = a.H / a.c.heads, slice = (cur.unit - kv * p.gs) * p.gw;
-        const int gw = min(p.gw, group_q - slice), h0 = kv * group_q + slice;
-        const uint32_t dst = q_at + (item & 1) * C::kQBytes;
-        for (int q = w * kRowsAt + sub; q < kNQ; q += kCopyWarps * kRowsAt) {
-          const int r = q / p.gw, h = q - r * p.gw;
-          const bool ok = r < n_rows && h < gw;
-          const E* src = static_cast<const E*>(a.Q) + (ok ? (row0 + r) * a.ldq + (long long)(h0 + h) * dim : 0);
-          if (has_pack) cp_async16_or_zero(dst + place(q, kNQ), src + pack * 8, ok);
+      long long row = 0;
+      uint32_t all = 0;
+      int kv = 0, box = -1;
+      if (i < count) {
+        const bool there = cur.pg >= 0 && cur.pg < a.c.n_pages;
+        all = __ballot_sync(~0u, there);
+        row = there ? cur.pg * a.c.sp + cur.off * a.c.st : 0;
+        kv = cur.unit / p.gs;
+        if (n_boxes > 0 && cur.whole) {
+          const int from = (lane * maps.box_rows) & 31;
+          const int pg = __shfl_sync(~0u, there ? cur.pg : -1, from), off = __shfl_sync(~0u, cur.off, from);
+          box = pg >= 0 ? pg * maps.page_rows + off + kv * maps.head_rows : maps.n_rows;   // past the end: zeros
+        }
+        // flags and masks of tile i: read after its keys have landed; tile i - kInfo is long done with
+        // (its values' slot has been refilled since)
+        if (lane == 0) {
+          mi.there[i % kInfo][w] = all;
+          if (w == 0) mi.info[i % kInfo] = (cur.first ? 1u : 0u) | (cur.last ? 2u : 0u);
+        }
+        if (cur.first) {
+          ++item;
+          if (item >= 2) wait_on(&mi.q_empty[item & 1], (item >> 1) - 1, ab);
+          long long row0;
+          const int n_rows = max(tile_rows(p, cur.tile, row0), 0);
+          const int group_q = a.H / a.c.heads, slice = (cur.unit - kv * p.gs) * p.gw;
+          const int gw = min(p.gw, group_q - slice), h0 = kv * group_q + slice;
+          const uint32_t dst = q_at + (item & 1) * C::kQBytes;
+          for (int q = w * kRowsAt + sub; q < kNQ; q += kCopyWarps * kRowsAt) {
+            const int r = q / p.gw, h = q - r * p.gw;
+            const bool ok = r < n_rows && h < gw;
+            const E* src = static_cast<const E*>(a.Q) + (ok ? (row0 + r) * a.ldq + (long long)(h0 + h) * dim : 0);
+            if (has_pack) cp_async16_or_zero(dst + place(q, kNQ), src + pack * 8, ok);
+          }
         }
       }
-      copy(a.c.K, &maps.k, kv, row, all, box);
-      if (i > 0) copy(a.c.V, &maps.v, kv_v, row_v, all_v, box_v);
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {          // keys of tile i, values of the tile before
+        if (h == 0 ? i == count : i == 0) continue;
+        copy(h == 0 ? a.c.K : a.c.V, h == 0 ? &maps.k : &maps.v, h == 0 ? kv : kv_v, h == 0 ? row : row_v,
+             h == 0 ? all : all_v, h == 0 ? box : box_v);
+      }
       box_v = box;
       row_v = row;
       all_v = all;
       kv_v = kv;
     }
-    if (count > 0) copy(a.c.V, &maps.v, kv_v, row_v, all_v, box_v);
     if (*ab.smem)                            // after a wait that ran out: no copy outlives the block
       for (int k = 0; k < kSlots; ++k) {
         const int round = int(to.round) - (k < to.slot ? 0 : 1);
@@ -387,8 +386,9 @@ __global__ void __launch_bounds__(C::kThreads, 1)
       constexpr uint32_t i_s = idesc_make(false, 128, kNQ, false, false);
       constexpr uint32_t i_o = idesc_make(false, 128, kNQ, true, true);
       const int n_k = (dim + 15) / 16;
-      // descriptors of the first places; others are this many 16 bytes further (one thread issues, and every
-      // instruction between two products is time)
+      // Descriptors of the first places; others are so many 16 bytes further.  One thread issues, and every
+      // instruction between two products is time: unrolled loops, whose instructions come from beyond the
+      // nearest cache, took 110 cycles a product.
       const uint64_t k_desc = sdesc_sw128(smem_u32(ring), 16, 1024), q_desc = sdesc_sw128(smem_u32(qs), 16, 1024);
       const uint64_t v_desc = sdesc_sw128(smem_u32(ring), kBlk * 128, 1024);
       const uint64_t p_desc = sdesc_sw128(smem_u32(ps), kBlk * 128, 1024);
@@ -414,30 +414,32 @@ __global__ void __launch_bounds__(C::kThreads, 1)
         from.next();
       };
 #pragma unroll 1
-      for (int i = 0; i < count; ++i) {
-        const int sb = i & 1;
-        wait_on(&mi.full[from.slot], from.round, ab);
-        const uint32_t info = mi.info[i % kInfo];
-        if (info & 1) ++item;
-        if (i >= 2) wait_on(&mi.s_empty[sb], (i >> 1) - 1, ab);
-        fence_proxy_async_smem();
-        tc_fence_after();
-        uint64_t ka = k_desc + from.slot * (C::kTile >> 4), qa = q_desc + (item & 1) * (C::kQBytes >> 4);
+      for (int i = 0; i <= count; ++i) {
+        uint32_t info = 0;
+        if (i < count) {
+          const int sb = i & 1;
+          wait_on(&mi.full[from.slot], from.round, ab);
+          info = mi.info[i % kInfo];
+          if (info & 1) ++item;
+          if (i >= 2) wait_on(&mi.s_empty[sb], (i >> 1) - 1, ab);
+          fence_proxy_async_smem();
+          tc_fence_after();
+          uint64_t ka = k_desc + from.slot * (C::kTile >> 4), qa = q_desc + (item & 1) * (C::kQBytes >> 4);
 #pragma unroll 1
-        for (int k = 0; k < n_k; ++k) {
-          mma_issue<false>(tmem + sb * kNQ, ka, qa, i_s, k);
-          // 32 bytes on, or to the next chunk of 64 elements
-          ka += (k & 3) == 3 ? (kBlk * 128 - 96) >> 4 : 32 >> 4;
-          qa += (k & 3) == 3 ? (kNQ * 128 - 96) >> 4 : 32 >> 4;
+          for (int k = 0; k < n_k; ++k) {
+            mma_issue<false>(tmem + sb * kNQ, ka, qa, i_s, k);
+            // 32 bytes on, or to the next chunk of 64 elements
+            ka += (k & 3) == 3 ? (kBlk * 128 - 96) >> 4 : 32 >> 4;
+            qa += (k & 3) == 3 ? (kNQ * 128 - 96) >> 4 : 32 >> 4;
+          }
+          mma_commit(&mi.empty[from.slot]);
+          mma_commit(&mi.s_full[sb]);
+          if (info & 2) mma_commit(&mi.q_empty[item & 1]);
+          from.next();
         }
-        mma_commit(&mi.empty[from.slot]);
-        mma_commit(&mi.s_full[sb]);
-        if (info & 2) mma_commit(&mi.q_empty[item & 1]);
-        from.next();
         if (i > 0) values(i - 1, prev);
         prev = info;
       }
-      values(count - 1, prev);
       mma_commit(&mi.drain);                 // nothing is in flight when the memory is given back
       mbar_wait_drain(&mi.drain, 0);
     }

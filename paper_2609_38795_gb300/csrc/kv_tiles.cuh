@@ -222,21 +222,26 @@ struct Cursor {
     t = load_tile<kBlk>(p, tile);
     enter();
   }
+  // The rare part of a step, out of the loops' way (they run at the speed of their instructions' arrival).
+  ALR_DEV static Cursor past_run(const KvPass& p, Cursor c) {
+    if (c.b == c.t.nb) {
+      c.b = 0;
+      if (++c.unit == p.n_units) {
+        c.unit = 0;
+        ++c.tile;
+        c.t = load_tile<kBlk>(p, c.tile);
+      }
+    }
+    c.enter();
+    return c;
+  }
   // To the next block; whether it continues the run.
   ALR_DEV bool advance(const KvPass& p) {
     if (++b < run_end) {
       t0 += kBlk;
       return true;
     }
-    if (b == t.nb) {
-      b = 0;
-      if (++unit == p.n_units) {
-        unit = 0;
-        ++tile;
-        t = load_tile<kBlk>(p, tile);
-      }
-    }
-    enter();
+    *this = past_run(p, *this);
     return false;
   }
 };
@@ -361,6 +366,17 @@ ALR_DEV void walk_tokens(const KvAttention& a, int seq, int t0, int t1, int head
     for (int i = 0; i < kLaneDims; ++i)
       if (i * 32 + lane < a.c.dim) o[i] = fmaf(e, to_float(V[at + i * 32 + lane]), o[i] * c);
   }
+}
+
+// A wait that runs out is recorded and passed over, as all waits after it: every role runs on to the end of
+// its loop (on data that no one will use), so that no barrier is left half full.
+ALR_DEV void wait_longer(uint64_t* bar, uint32_t parity, volatile int* abort_word,
+                                                int* status) {
+  if (!*abort_word) mbar_wait(bar, parity, AbortFlag{abort_word, status});
+}
+// For completion n (from 0) of `bar`.
+ALR_DEV void wait_on(uint64_t* bar, uint32_t n, const AbortFlag& ab) {
+  if (!mbar_try_wait(bar, n & 1)) wait_longer(bar, n & 1, ab.smem, ab.status);
 }
 
 // Units, tiles and steps of a pass whose items have at most max_q queries in max_rows rows.
