@@ -40,16 +40,15 @@ struct Cfg {
   static constexpr int kPBytes = (kNQ / 64) * kBlk * 128;
   static constexpr int kQBufs = 2, kPBufs = kNQ == 128 && kChunks == 2 ? 1 : 2;
   static constexpr int kSlots = kChunks == 1 ? 8 : kNQ == 128 ? 4 : 5;
-  static constexpr int kGroups = kNQ == 128 ? 2 : 4;       // of 4 softmax warps
+  static constexpr int kGroups = 4;                        // of 4 softmax warps
   static constexpr int kOwn = kNQ / kGroups;               // queries of a group ...
-  static constexpr int kW = kOwn < 32 ? kOwn : 32;         // ... and columns at a time
+  static constexpr int kW = 16;                            // ... and columns at a time (tmem_ld16)
   static constexpr int kParts = kOwn / kW;
   static constexpr int kSoftWarps = 4 * kGroups, kCopyWarp = kSoftWarps, kMmaWarp = kCopyWarp + kCopyWarps;
   static constexpr int kWarps = kMmaWarp + 4, kThreads = kWarps * 32;
-  // Registers: two groups hold 64 columns' sums each and take some from the other warps (128 a thread at
-  // the launch); four hold 16 columns' each in what all have.
-  static constexpr int kSoftRegs = kGroups == 2 ? 168 : 0, kOtherRegs = kGroups == 2 ? 88 : 0;
-  static_assert(2 * kSoftRegs + 2 * kOtherRegs <= 4 * 128, "the launch's registers");
+  // Registers: 80 a thread at the launch; groups with 32 columns' sums take some from the other warps.
+  static constexpr int kSoftRegs = kNQ == 128 ? 88 : 0, kOtherRegs = kNQ == 128 ? 64 : 0;
+  static_assert(kGroups * kSoftRegs + 2 * kOtherRegs <= (kGroups + 2) * 80, "the launch's registers");
   static constexpr int kCols = kNQ == 128 ? 512 : 256;     // tensor memory: S^T, S^T, O^T
   static constexpr size_t kBig = size_t(kSlots) * kTile + kQBufs * kQBytes + kPBufs * kPBytes;
 };
@@ -106,8 +105,7 @@ ALR_DEV void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
                  "=r"(r[7])
                : "r"(taddr));
 }
-ALR_DEV void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[32]) { tmem_ld32(taddr, r); }
-ALR_DEV void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[16]) {
+ALR_DEV void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
       "%14, %15}, [%16];"
@@ -501,8 +499,8 @@ __global__ void __launch_bounds__(C::kThreads, 1)
           // Exponents are differences of scores, times c (the fma s c - ref c would leave the rounding of
           // ref c, which is more than 2^8 from |ref c| = 2^32 on): after a move none is above 0.
           for (bool moved = false;; moved = true) {
-            uint32_t s[kW];
-            tmem_ld_cols(s_at + part * kW, s);
+            uint32_t s[16];
+            tmem_ld16(s_at + part * kW, s);
             const float* ref = sm.ref + q0 + part * kW;
             float t = kNegInf;
             tmem_ld_wait();
@@ -583,7 +581,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
           }
         }
         float sum = l[part * kW];
-        if (kW == 16) sum += __shfl_xor_sync(~0u, sum, 16);
+        sum += __shfl_xor_sync(~0u, sum, 16);
         if (lane < kW) lsum[warp][part * kW + lane] = sum;
       }
       named_bar_sync(bar, 128);
@@ -611,8 +609,8 @@ __global__ void __launch_bounds__(C::kThreads, 1)
       E* stage = reinterpret_cast<E*>(ps + kEndBytes + wg * kStageBytes);
 #pragma unroll 1
       for (int k0 = 0; k0 < kOwn && q0 + k0 < n_q; k0 += kW) {
-        uint32_t s[kW];
-        tmem_ld_cols(lanes + 2 * kNQ + q0 + k0, s);
+        uint32_t s[16];
+        tmem_ld16(lanes + 2 * kNQ + q0 + k0, s);
         tmem_ld_wait();
         reg_fence(s);
 #pragma unroll
