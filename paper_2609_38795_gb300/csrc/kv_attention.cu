@@ -582,12 +582,15 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
   if (lane == 0) cut_of[warp] = make_int4(0, 0, 0, 0);
   const AbortFlag ab{&abort_word, status};
   pdl_wait();
-  const Line line = find_starts<kBlk>(p, starts, reinterpret_cast<long long*>(ring_smem), buf);
+  const Line line = p.one_each ? find_item_starts<kBlk>(p, starts, buf)
+                               : find_starts<kBlk>(p, starts, reinterpret_cast<long long*>(ring_smem), buf);
   if (a.c.dim % 16 != 0)                     // what lies past a row's end is never copied: zeros
     for (int i = lane; i < stages * slot_bytes / 16; i += 32)
       reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
-  const int id0 = blockIdx.x * line.per_block, id = id0 + warp;
-  const bool works = warp < line.per_block && id < line.n;
+  // this warp among all workers (its places for partial results), and on the line
+  const int id0 = blockIdx.x * (p.one_each ? p.block_workers : line.per_block), id = id0 + warp;
+  const int on_line = p.one_each ? warp : id;
+  const bool works = warp < line.per_block && on_line < line.n;
   const int count = works ? int(starts[warp + 1].block - starts[warp].block) : 0;
   Cursor<kBlk> in{};                         // of the loads
   if (count > 0) in.start(p, starts[warp].tile, starts[warp].unit, starts[warp].b);
@@ -771,7 +774,7 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
       __syncwarp();
     }
     if (!whole && lane == 0) {
-      const int parts = last_here ? 1 : line.last_before(line.start(id + 1) + (tile.nb - b1)) - id + 1;
+      const int parts = last_here ? 1 : line.last_before(line.start(on_line + 1) + (tile.nb - b1)) - on_line + 1;
       if (opens) cut_of[warp] = make_int4(tile_id, unit, parts, 0);
       else if (warp == 0) head_cut = make_int4(tile_id, unit, parts, 0);
     }
@@ -802,7 +805,7 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
       put_sums<E>(p, o, s);
     }
   }
-  if (threadIdx.x == 0) p.cuts[blockIdx.x] = cut;
+  if (threadIdx.x == 0 && !p.one_each) p.cuts[blockIdx.x] = cut;
   pdl_release();
 }
 
@@ -859,13 +862,19 @@ cudaError_t run_pass(KvPass p, int sms, int* status, cudaStream_t s) {
   const int slot = 2 * kBlk * row_bytes_of<E>(p.a.c.dim);
   const int warps = std::min(Core::kMostWarps, kRingsMost / (2 * slot + Core::kScratch));
   p.stages = std::min(kMostStages, (kRingsMost / warps - Core::kScratch) / slot);
-  const int grid = std::min(sms, kKvMostSms), ring = warps * (p.stages * slot + Core::kScratch);
+  // Few items of few blocks: each its own thread block, nothing to share out or to join (12 sequences of up
+  // to 60 tokens, 5 heads: 17.7 us, in even stretches and a join; 1x so).
+  const long long items = (long long)p.n_tiles * p.n_units;
+  const long long most = (long long)p.a.cols * p.a.c.page;             // tokens of a row
+  p.one_each = items <= std::min(sms, kKvMostSms) && (most + kBlk - 1) / kBlk * p.rows <= 4 * warps;
+  const int grid = p.one_each ? int(items) : std::min(sms, kKvMostSms);
+  const int ring = warps * (p.stages * slot + Core::kScratch);
   p.block_workers = warps;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = allow_smem(kv_blocks_kernel<Core>, kRingsMost, done);
   if (e != cudaSuccess) return e;
   const cudaError_t f = launch_pdl(kv_blocks_kernel<Core>, dim3(grid), dim3(warps * 32), ring, s, p, status);
-  return f != cudaSuccess ? f : run_join<E>(p, sms, s);
+  return f != cudaSuccess || p.one_each ? f : run_join<E>(p, sms, s);
 }
 
 template <int kDim>

@@ -43,6 +43,7 @@ struct KvPass {
   int step_pg, step_tok;           // kBlk tokens on: pages and tokens
   int block_workers;               // of a thread block, at most
   int stages;                      // blocks of a worker's ring
+  bool one_each;                   // a thread block has one item, its line is the item's blocks
   int max_q;                       // queries of an item, at most
   float* parts;                    // [2 * workers][part_floats]: o of all queries, then m and l
   float* block_parts;              // [2 * blocks][part_floats]
@@ -333,6 +334,25 @@ ALR_DEV Line find_starts(const KvPass& p, WorkerStart* at, long long* sums, long
                  max(off - kItemCost, 0)};
       break;
     }
+  }
+  __syncthreads();
+  return line;
+}
+
+// The same where every thread block has one item.
+template <int kBlk>
+ALR_DEV Line find_item_starts(const KvPass& p, WorkerStart* at, long long* buf) {
+  const int tile = blockIdx.x / p.n_units, unit = blockIdx.x - tile * p.n_units, tid = threadIdx.x;
+  if (tid == 0) buf[0] = tile_blocks<kBlk>(p, tile);
+  __syncthreads();
+  const int nb = int(buf[0]);
+  Line line;
+  line.per_block = line.n = min(nb, p.block_workers);
+  line.each = nb / line.n;
+  line.more = nb - int(line.each) * line.n;
+  if (tid <= line.n) {
+    const int b = int(line.start(tid));
+    at[tid] = {b, tile, unit, b};
   }
   __syncthreads();
   return line;
