@@ -812,14 +812,24 @@ def _strided(t, name, dims, dtype=None):
         raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
     if not t.is_contiguous():
         shape, stride = t.shape, t.stride()
-        reach = 1
-        for st, n in sorted((st, n) for st, n in zip(stride, shape) if n > 1):
-            if st < reach:
-                raise ValueError(f"{name}'s elements must not overlap (got strides {stride})")
-            reach = st * (n - 1) + reach
         if shape[-1] > 1 and stride[-1] != 1:
             raise ValueError(f"{name}'s last dimension must be contiguous (got strides {stride})")
+        if not (_nested(shape, stride, range(dims - 1, -1, -1)) or
+                _nested(shape, stride, sorted(range(dims), key=stride.__getitem__))):
+            raise ValueError(f"{name}'s elements must not overlap (got strides {stride})")
     return t.data_ptr()
+
+
+def _nested(shape, stride, order):
+    """Whether each dimension, in that order, steps over all that those before it reach."""
+    reach = 1
+    for i in order:
+        n = shape[i]
+        if n > 1:
+            if stride[i] < reach:
+                return False
+            reach += stride[i] * (n - 1)
+    return True
 
 
 def _kv_cache(K, V):

@@ -365,3 +365,185 @@ def test_long_offsets():
     row = torch.randn(1, heads, dim, generator=g).cuda()
     alr.alr_kv_append(row, row, K, V, slot)
     assert torch.equal(K[-1, -1], row[0].to(BF)) and torch.equal(V[-1, -1], row[0].to(BF))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("form", [dict(heads=4, group=2, dim=32, page=16), dict(heads=3, group=1, dim=128, page=32),
+                                  dict(heads=2, group=12, dim=64, page=20), dict(heads=5, group=5, dim=48, page=8, hnd=True)])
+def test_many_blocks(form, dtype):
+    """More blocks than workers: stretches that end inside items, items over many workers and thread blocks."""
+    rng = np.random.default_rng(5)
+    lengths = [0, 1, 3000, 5, 40, 2047, 0, 900] + [int(x) for x in np.exp(rng.uniform(0, 7.5, 40))] + [6000]
+    c = Case(lengths, list(enumerate(lengths)), dtype=dtype, **form)
+    out, lse = c.check(seq=False)
+    for _ in range(2):                         # whatever the workspace held
+        again, lse2 = c.run()
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("form", [dict(heads=2, group=4, dim=64, page=16), dict(heads=1, group=8, dim=128, page=32),
+                                  dict(heads=2, group=3, dim=80, page=20, hnd=True),
+                                  dict(heads=1, group=2, dim=24, page=64), dict(heads=1, group=4, dim=112, page=8)])
+def test_many_block_rows(form, dtype):
+    """Tiles of rows over long sequences, cut at stretches' ends, some rows ending tiles before others."""
+    rng = np.random.default_rng(6)
+    lengths, per = [3000, 16, 0, 1500, 129, 128, 127, 2500], 16
+    rows = [(s, max(0, n - int(rng.integers(0, 2 * per)))) if rng.random() < 0.9 else (s, int(rng.integers(0, n + 1)))
+            for s, n in enumerate(lengths) for _ in range(per)]
+    c = Case(lengths, rows, dtype=dtype, **form)
+    out, lse = c.check(per=per)
+    again, lse2 = c.run(per=per)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("heads,group,dim,dtype", [(1, 1, 64, BF), (2, 8, 128, BF), (1, 16, 256, BF), (1, 4, 128, F32)])
+def test_one_long_sequence(heads, group, dim, dtype):
+    c = Case([20011], [(0, 20011)], heads=heads, group=group, dim=dim, dtype=dtype, page=64)
+    c.check()
+
+
+def test_lengths_past_the_table():
+    """Lengths past what the table holds count as that; rows of a sequence that is not there are empty."""
+    c = Case([64, 64], [(0, 10 ** 6), (1, 2 ** 31 - 1), (1, -2 ** 31), (2 ** 31 - 1, 5), (-2 ** 31, 5)], page=16)
+    c.check()
+    c = Case([64, 64], [(s, 10 ** 6) for s in range(2) for _ in range(16)], page=16, group=4)
+    c.check(per=16)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_strided_rows(dtype):
+    """Queries out of a fused projection, results into wider rows, whose other elements stay."""
+    rows = [(s, 50 * s + j) for s in range(4) for j in range(8)]
+    for per, group in ((1, 2), (8, 2), (8, 4)):
+        c = Case([10, 60, 110, 160], rows, dtype=dtype, group=group, dim=64)
+        N, H, dim = c.Q.shape
+        wide = torch.randn(N, 3 * H * dim, device="cuda").to(dtype)
+        wide[:, H * dim:2 * H * dim] = c.Q.reshape(N, -1)
+        want, _ = c.run(per=per)
+        c.Q = wide[:, H * dim:2 * H * dim].unflatten(1, (H, dim))
+        to = torch.full((N + 2, H * dim + 64), 3.0, dtype=dtype, device="cuda")
+        got, _ = c.run(per=per, out=to[:N, 32:32 + H * dim].unflatten(1, (H, dim)))
+        assert torch.equal(got, want)
+        assert (to[N:] == 3).all() and (to[:, :32] == 3).all() and (to[:, 32 + H * dim:] == 3).all()
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with a workspace of its own."""
+    a = Case([4000] * 6, [(s, 4000 - s) for s in range(6)], heads=2, group=4, dim=128)
+    b = Case([3000] * 4, [(s, 3000 - j) for s in range(4) for j in range(16)], heads=2, group=4, dim=128, seed=1)
+    want = a.run()[0], b.run(per=16)[0]
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    calls = []
+    for c, per in ((a, 1), (b, 16)):
+        N, H, dim = c.Q.shape
+        n = alr.alr_kv_attention_workspace_size(N, H, dim)
+        calls.append((c, per, torch.empty_like(c.Q), torch.empty(n, dtype=torch.uint8, device="cuda"), _i(c.table),
+                      _i(c.rows[:, 1]), _i(c.rows[:, 0])))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, (c, per, out, ws, table, length, seq) in zip(streams, calls):
+            alr.alr_kv_attention(c.Q, c.K, c.V, table, length, out, ws, seq=seq, rows_per_seq=per, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(call[2], w) for call, w in zip(calls, want))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("most", [1, 5])
+def test_steps_in_a_graph(dtype, most):
+    """Plan, append and attention of a rollout's steps as one captured graph, replayed as sequences grow, end and
+    begin again; rows of the batch beyond its tokens are empty."""
+    S, page, cols, heads, group, dim, T = 9, 8, 6, 2, 2, 64, 24
+    n_pool, H = 40, heads * group
+    g = torch.Generator().manual_seed(most)
+    rng = np.random.default_rng(most)
+    K, V = _cache(n_pool, page, heads, dim, dtype, False, g, fill=NAN)
+    length, add, pool, used = _i(np.zeros(S)), _i(np.zeros(S)), _i(rng.permutation(n_pool)), _i([0])
+    table = torch.full((S, cols), -1, dtype=torch.int32, device="cuda")
+    e = lambda *n: torch.empty(*n, dtype=torch.int32, device="cuda")  # noqa: E731
+    plan = dict(len=length, slot=e(T), pool_used=used, start=e(S + 1), tok_seq=e(T), tok_len=e(T), n_refused=e(1))
+    qkv = torch.zeros(T, (H + 2 * heads) * dim, device="cuda")
+    cut = [H * dim, (H + heads) * dim]
+    k_new, v_new = (qkv[:, cut[i]:cut[i] + heads * dim].unflatten(1, (heads, dim)) for i in range(2))
+    q = torch.zeros(T, H, dim, dtype=dtype, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(T, H, device="cuda")
+    ws = torch.empty(alr.alr_kv_attention_workspace_size(T, H, dim), dtype=torch.uint8, device="cuda")
+
+    def step():
+        alr.alr_kv_plan(length, add, pool, used, table, page, plan)
+        alr.alr_kv_append(k_new, v_new, K, V, plan["slot"])
+        q.copy_(qkv[:, :H * dim].unflatten(1, (H, dim)))
+        alr.alr_kv_attention(q, K, V, table, plan["tok_len"], out, ws, seq=plan["tok_seq"], lse=lse, rows_per_seq=most)
+
+    step()                                                   # nothing to do: loads the kernels
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    held = {s: [] for s in range(S)}                         # each sequence's (key, value) rows
+    for n in range(25):
+        a = rng.integers(0, most + 1, S) if n % 5 else rng.integers(-1, most + 1, S)
+        add.copy_(_i(a))
+        qkv.copy_(torch.randn(qkv.shape, generator=g))
+        before = [len(held[s]) for s in range(S)]
+        graph.replay()
+        torch.cuda.synchronize()
+        start, slot = plan["start"].tolist(), plan["slot"].tolist()
+        for s in range(S):
+            if a[s] < 0:
+                held[s] = []
+            else:
+                rows = range(start[s], start[s] + a[s])
+                took = [r for r in rows if r < T and slot[r] >= 0]
+                assert len(took) in (0, a[s])
+                held[s] += [(k_new[r].to(dtype).clone(), v_new[r].to(dtype).clone()) for r in took]
+        assert length.tolist() == [len(held[s]) for s in range(S)]
+        seqs, lens = plan["tok_seq"].tolist(), plan["tok_len"].tolist()
+        for r in range(T):
+            if seqs[r] < 0:
+                assert lens[r] == 0 and not out[r].any() and (lse[r] == -float("inf")).all()
+                continue
+            assert lens[r] == before[seqs[r]] + r - start[seqs[r]] + 1
+            k, v = (torch.stack([x[i] for x in held[seqs[r]][:lens[r]]]).double().repeat_interleave(group, 1)
+                    for i in range(2))
+            x = (k * q[r].double()).sum(-1) * dim ** -0.5     # [tokens, H]
+            want = (torch.softmax(x, 0)[..., None] * v).sum(0)
+            # scores and values of order 3: two roundings of bf16, or the sums' of fp32
+            assert (out[r].double() - want).abs().max() <= (2 * 2.0 ** -8 if dtype == BF else 1e-5) * v.abs().max()
+            assert (lse[r].double() - torch.logsumexp(x, 0)).abs().max() <= 1e-5 * max(1.0, float(x.abs().max()))
+
+
+def test_binding_refuses_wrong_buffers():
+    c = Case([20], [(0, 20)])
+    N, H, dim = c.Q.shape
+    ws = torch.empty(alr.alr_kv_attention_workspace_size(N, H, dim), dtype=torch.uint8, device="cuda")
+    table, length, out = _i(c.table), _i([20]), torch.empty_like(c.Q)
+    call = lambda Q=c.Q, K=c.K, V=c.V, t=table, n=length, o=out, w=ws, **kw: (  # noqa: E731
+        alr.alr_kv_attention(Q, K, V, t, n, o, w, **kw))
+    call()
+    for match, kw in (("laid out alike", dict(V=c.V[:-1])), ("must be torch.bfloat16", dict(V=c.V.float())),
+                      ("4 dimensions", dict(K=c.K[0])), ("overlap", dict(K=c.K[:1].expand(5, -1, -1, -1), V=c.V)),
+                      ("last dimension", dict(K=c.K.transpose(2, 3))), ("must be torch.bfloat16", dict(Q=c.Q.float())),
+                      ("must be \\[N, H, 64\\]", dict(o=out[:, :1])), ("table must be", dict(t=table[0])),
+                      ("table must be torch.int32", dict(t=table.long())), ("len holds", dict(n=length[:0])),
+                      ("heads must be contiguous", dict(Q=torch.empty(1, H, 2 * dim, dtype=BF, device="cuda")[..., :dim])),
+                      ("lse holds", dict(lse=torch.empty(1, device="cuda")))):
+        with pytest.raises(ValueError, match=match):
+            call(**kw)
+    for match, kw in (("go together", dict(prefix_len=length)), ("workspace", dict(w=ws[:64])),
+                      ("workspace", dict(w=None)), ("rows_per_seq", dict(rows_per_seq=0)), ("scale", dict(scale=NAN))):
+        with pytest.raises(alr.AlrError, match=match):
+            call(**kw)
+    with pytest.raises(alr.AlrError, match="prefix|workspace"):
+        call(prefix_len=length, prefix_seq=_i([0]), w=ws[:-1])
+    new = torch.zeros(3, 2, 64, device="cuda")
+    with pytest.raises(ValueError, match="rows of"):
+        alr.alr_kv_append(new[:, :1], new[:, :1], c.K, c.V, _i([0, 1, 2]))
+    with pytest.raises(ValueError, match="slot holds"):
+        alr.alr_kv_append(new, new, c.K, c.V, _i([0, 1]))
+    with pytest.raises(ValueError, match="laid out alike"):
+        alr.alr_kv_append(new, new[:2], c.K, c.V, _i([0, 1, 2]))
+    with pytest.raises(ValueError, match="table must be"):
+        alr.alr_kv_plan(length, length, length, length, table[:0], 16, dict(len=length, slot=_i([0]), pool_used=_i([0])))
+    with pytest.raises(KeyError):
+        alr.alr_kv_plan(length, length, length, length, table, 16, dict(len=length))
