@@ -188,7 +188,7 @@ ALR_DEV Tile load_tile(const KvPass& p, int tile) {
   const uint32_t leads = __ballot_sync(~0u, t.len > 0 && (before == 0 || prev != t.seq));
   t.lead = (leads & up_to) != 0 ? 31 - __clz(leads & up_to) : -1;
   t.most = t.len;
-  for (int off = 1; off < 32; off <<= 1) {
+  for (int off = 1; off < p.rows; off <<= 1) {
     const int m = __shfl_down_sync(~0u, t.most, off), l = __shfl_down_sync(~0u, t.lead, off);
     if (lane + off < 32 && l == t.lead) t.most = max(t.most, m);
   }
@@ -275,33 +275,33 @@ struct WorkerStart {
 };
 
 // Every thread block counts the places of all tiles, a thread some consecutive ones; a warp then finds the
-// start of a worker among the threads' sums and the tiles of the thread.  at[i]: start of the block's
-// i-th worker, at[own workers]: of the next one.  Few blocks go to few workers of every thread block.
+// start of a worker among the warps' sums, its threads' and the tiles of the thread.  at[i]: start of the
+// block's i-th worker, at[own workers]: of the next one.  Few blocks go to few workers of every thread block.
 // sums: an entry a thread; buf: an entry a warp.
 template <int kBlk>
 ALR_DEV Line find_starts(const KvPass& p, WorkerStart* at, long long* sums, long long* buf) {
+  using N = long long;
   const int tid = threadIdx.x, n_threads = blockDim.x, n_warps = n_threads / 32;
   const int lane = tid & 31, warp = tid >> 5;
   const int per = (p.n_tiles + n_threads - 1) / n_threads;
   const int a = int(min((long long)tid * per, (long long)p.n_tiles)), e = min(a + per, p.n_tiles);
-  long long own = 0;
+  N own = 0;
   for (int i = a; i < e; ++i) own += tile_blocks<kBlk>(p, i) + kItemCost;
   own *= p.n_units;
-  const long long up = warp_scan(own);
+  const N up = warp_scan(own);
   if (lane == 31) buf[warp] = up;
   __syncthreads();
-  long long before = up - own, total = 0;
-  for (int i = 0; i < n_warps; ++i) {
-    if (i < warp) before += buf[i];
-    total += buf[i];
-  }
-  sums[tid] = before;
+  const N of_warps = warp_scan(lane < n_warps ? buf[lane] : N(0));
+  const N total = __shfl_sync(~0u, of_warps, 31);
+  const N before_warp = __shfl_sync(~0u, of_warps, max(warp - 1, 0));
+  sums[tid] = (warp > 0 ? before_warp : N(0)) + up - own;
   Line line;
-  const long long items = (long long)p.n_tiles * p.n_units, blocks = total - kItemCost * items;
-  line.per_block = int(min(quotient(blocks + gridDim.x - 1, gridDim.x), (long long)p.block_workers));
-  line.n = int(min((long long)line.per_block * gridDim.x, blocks));
-  line.each = quotient(total, line.n);
-  line.more = int(total - line.each * line.n);
+  const N items = N(p.n_tiles) * p.n_units, blocks = total - kItemCost * items;
+  line.per_block = int(min(quotient(blocks + gridDim.x - 1, gridDim.x), (N)p.block_workers));
+  line.n = int(min(N(line.per_block) * N(gridDim.x), blocks));
+  const N each = quotient(total, line.n);
+  line.each = each;
+  line.more = int(total - each * line.n);
   __syncthreads();
   const int id0 = int(blockIdx.x) * line.per_block, n_own = min(line.per_block, line.n - id0);
   for (int k = warp; k <= n_own; k += n_warps) {
@@ -309,16 +309,17 @@ ALR_DEV Line find_starts(const KvPass& p, WorkerStart* at, long long* sums, long
       if (lane == 0) at[k] = {blocks, 0, 0, 0};
       continue;
     }
-    const long long pos = line.start(id0 + k);
-    int n = 0;                               // threads that begin at or before it
-    for (int i = lane; i < n_threads; i += 32) n += __popc(__ballot_sync(~0u, sums[i] <= pos));
-    long long rest = pos - sums[n - 1];
+    const N pos = N(id0 + k) * each + min(id0 + k, line.more);
+    // the last thread that begins at or before it
+    const int w = __popc(__ballot_sync(~0u, lane < n_warps && sums[min(lane, n_warps - 1) * 32] <= pos)) - 1;
+    const int n = w * 32 + __popc(__ballot_sync(~0u, sums[w * 32 + lane] <= pos));
+    N rest = pos - sums[n - 1];
     const int tile_end = min(n * per, p.n_tiles);
     // rest is less than the thread's places (of lengths that do not change meanwhile)
     for (int tile = (n - 1) * per; tile < tile_end; tile += 32) {
       const int mine = tile + lane;
-      const long long len = mine < tile_end ? (long long)(tile_blocks<kBlk>(p, mine) + kItemCost) * p.n_units : 0;
-      const long long sum = warp_scan(len);
+      const N len = mine < tile_end ? N(tile_blocks<kBlk>(p, mine) + kItemCost) * p.n_units : N(0);
+      const N sum = per > 1 ? warp_scan(len) : len;
       const uint32_t past = __ballot_sync(~0u, sum > rest);
       if (past == 0) {
         rest -= __shfl_sync(~0u, sum, 31);
@@ -327,10 +328,10 @@ ALR_DEV Line find_starts(const KvPass& p, WorkerStart* at, long long* sums, long
       const int k2 = __ffs(past) - 1;
       tile += k2;
       rest -= __shfl_sync(~0u, sum - len, k2);
-      const long long each = quotient(__shfl_sync(~0u, len, k2), p.n_units);
-      const int unit = int(quotient(rest, each)), off = int(rest - unit * each);
+      const N places = quotient(__shfl_sync(~0u, len, k2), p.n_units);
+      const int unit = int(quotient(rest, places)), off = int(rest - unit * places);
       if (lane == 0)
-        at[k] = {pos - kItemCost * ((long long)tile * p.n_units + unit) - min(off, kItemCost), tile, unit,
+        at[k] = {pos - kItemCost * (N(tile) * p.n_units + unit) - min(off, kItemCost), tile, unit,
                  max(off - kItemCost, 0)};
       break;
     }
