@@ -745,7 +745,7 @@ typedef struct {
     int64_t stride_head;
     int32_t n_pages;
     int32_t page;       /* tokens of a page, 1 <= page <= ALR_KV_MAX_PAGE                     */
-    int32_t heads;      /* key-value heads                                                    */
+    int32_t heads;      /* key-value heads, 1 <= heads <= 1024                                */
     int32_t dim;        /* of a head                                                          */
     int32_t dtype;      /* ALR_BF16 or ALR_F32                                                */
 } alr_kv_cache;

@@ -1621,10 +1621,10 @@ int check_cache(const alr_kv_cache* c, alr::KvCache* out) {
   if (c->dtype != ALR_BF16 && c->dtype != ALR_F32)
     return fail(ALR_ERR_UNSUPPORTED, "dtype %d is not ALR_BF16 or ALR_F32", c->dtype);
   const int pack = int(16 / elem_size(c->dtype));
-  if (c->page < 1 || c->page > ALR_KV_MAX_PAGE || c->heads < 1 || c->n_pages < 0 ||
+  if (c->page < 1 || c->page > ALR_KV_MAX_PAGE || c->heads < 1 || c->heads > 1024 || c->n_pages < 0 ||
       int64_t(c->n_pages) * c->page > INT32_MAX)
     return fail(ALR_ERR_INVALID_ARG,
-                "bad cache sizes n_pages=%d page=%d heads=%d (page <= %d, n_pages * page < 2^31)",
+                "bad cache sizes n_pages=%d page=%d heads=%d (page <= %d, heads <= 1024, n_pages * page < 2^31)",
                 c->n_pages, c->page, c->heads, ALR_KV_MAX_PAGE);
   if (c->dim < 1 || c->dim > ALR_KV_MAX_DIM || c->dim % pack != 0)
     return fail(ALR_ERR_INVALID_ARG, "dim = %d must be a multiple of %d and at most %d", c->dim, pack,

@@ -37,7 +37,7 @@ def _run(lib, cases):
         assert rc == code and text in msg, (n, rc, msg)
 
 
-CACHES = [(dict(dtype=2), U, "dtype 2"), (dict(page=0), I, "page=0"), (dict(heads=0), I, "heads=0"),
+CACHES = [(dict(dtype=2), U, "dtype 2"), (dict(page=0), I, "page=0"), (dict(heads=0), I, "heads=0"), (dict(heads=1025), I, "heads=1025"),
           (dict(n_pages=-1), I, "n_pages=-1"), (dict(n_pages=1 << 27), I, "2^31"), (dict(page=65537), I, "page=65537"),
           (dict(dim=12), I, "dim = 12"), (dict(dim=264), I, "dim = 264"), (dict(dim=0), I, "dim = 0"),
           (dict(dim=6, dtype=1), I, "dim = 6"), (dict(stride_page=4), I, "strides"),
