@@ -874,7 +874,7 @@ def alr_kv_append(K_new, V_new, K, V, slot, stream=None):
     T, heads, dim = K_new.shape
     ld, st = K_new.stride(0) if T > 1 else heads * dim, K_new.stride(1)
     if (heads, dim) != (c.heads, c.dim) or (heads > 1 and st != dim) or V_new.shape != K_new.shape or \
-            (T > 0 and V_new.stride() != K_new.stride()):
+            (T > 1 and V_new.stride() != K_new.stride()):
         raise ValueError(f"K_new and V_new must be rows of [{c.heads}, {c.dim}] laid out alike (got "
                          f"{[*K_new.shape]}, {K_new.stride()} and {[*V_new.shape]}, {V_new.stride()})")
     _check(lib().alr_kv_append(ctypes.byref(c), k, v, dtype_code(K_new.dtype), T, ld,

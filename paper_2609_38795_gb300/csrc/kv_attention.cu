@@ -52,8 +52,8 @@ constexpr float kLag = 8.f;
 // bf16 on tensor cores (m16n8k16, fp32 accumulation).  Queries are the 16 rows of a product's result, so
 // the weights leave the first product in the registers that the second takes them from.  Lane
 // (g, t) = (lane / 4, lane % 4) has queries g and g + 8.
-//   A group of 4 queries leaves 12 rows unused, yet the products are far from the bound: 16 tokens of
-// 128 elements are 32 instructions and 8 KB.
+//   16 tokens of 128 elements are 8 KB and 32 product instructions, whatever part of the 16 rows is used
+// (64 sequences of 1000 to 3000 tokens, 4 heads of 128, 16 queries each: 262 MB in 101 us cold).
 template <int kDim_>
 struct ManyCore {
   using E = __nv_bfloat16;
@@ -195,8 +195,10 @@ struct ManyCore {
 };
 
 // bf16, up to 8 queries, with the tokens (the elements of a value) on a product's 16 rows and the queries
-// on its 8 columns: half the products of ManyCore and half its registers.  Lane (g, t) has queries 2t and
-// 2t + 1 of tokens g and g + 8; the weights are transposed into the second product's operand.
+// on its 8 columns: half the products of ManyCore and half its registers, so 12 warps an SM and not 8 (256
+// sequences of 0 to 8192 tokens, 8 heads of 128, 4 queries each: 825 us by ManyCore, 718 so, 6.0 TB/s).
+// Lane (g, t) has queries 2t and 2t + 1 of tokens g and g + 8; the weights are transposed into the
+// second product's operand.
 //   The reference lags, and no maximum is taken while a vote finds all scores below it + kLag: sums cross
 // lanes at an item's end only.
 template <int kDim_>
@@ -314,7 +316,7 @@ struct FewCore {
 // fp32 by fused multiply-adds (a tensor product in tf32 would lose 13 bits of the inputs).  Scores: lane
 // (h, i) = (lane / 16, lane % 16) takes half the packs of token i; weights go through shared memory;
 // values: a lane owns whole packs of the result, groups of lanes share the tokens where there are
-// fewer packs than lanes.
+// fewer packs than lanes.  (48 sequences of up to 4001 tokens, 16 heads of 80, one query each: 203 us, 4.8 TB/s.)
 template <int kDim_, int kQ>
 struct F32Core {
   using E = float;
@@ -550,7 +552,9 @@ ALR_DEV void put_sums(const KvPass& p, const KvRowOut& to, const JoinSums& s) {
 
 // Each warp is a worker with a ring of its own: no block-wide barrier after the start, so warps in
 // different items never wait for one another, and a ring's blocks (all but one ahead) are all that
-// hides latency.
+// hides latency.  Long sequences run near the memory's rate; short ones are latency, the chain of lengths,
+// table, keys, results and join (64 sequences of up to 1024 tokens: 62 us cold for 134 MB).
+//   Copies are of 16 bytes: bulk copies of a row each took 1020 us where these took 830.
 template <typename Core>
 __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(const __grid_constant__ KvPass p, int* status) {
   using E = typename Core::E;
@@ -863,7 +867,7 @@ cudaError_t run_pass(KvPass p, int sms, int* status, cudaStream_t s) {
   const int warps = std::min(Core::kMostWarps, kRingsMost / (2 * slot + Core::kScratch));
   p.stages = std::min(kMostStages, (kRingsMost / warps - Core::kScratch) / slot);
   // Few items of few blocks: each its own thread block, nothing to share out or to join (12 sequences of up
-  // to 60 tokens, 5 heads: 17.7 us, in even stretches and a join; 1x so).
+  // to 60 tokens, 5 heads: 17.7 us in even stretches and a join, 13.5 so).
   const long long items = (long long)p.n_tiles * p.n_units;
   const long long most = (long long)p.a.cols * p.a.c.page;             // tokens of a row
   p.one_each = items <= std::min(sms, kKvMostSms) && (most + kBlk - 1) / kBlk * p.rows <= 4 * warps;
@@ -878,13 +882,18 @@ cudaError_t run_pass(KvPass p, int sms, int* status, cudaStream_t s) {
 }
 
 template <int kDim>
-cudaError_t run_dim(const KvPass& p, int sms, int* status, cudaStream_t s) {
+cudaError_t run_f32(const KvPass& p, int sms, int* status, cudaStream_t s) {
   const long long q = std::min<long long>(p.part.per, p.a.N) * (p.a.H / p.a.c.heads);
-  if (p.a.c.dtype == 0)
-    return q <= 8 ? run_pass<FewCore<kDim>>(p, sms, status, s) : run_pass<ManyCore<kDim>>(p, sms, status, s);
   return q <= 1   ? run_pass<F32Core<kDim, 1>>(p, sms, status, s)
          : q <= 4 ? run_pass<F32Core<kDim, 4>>(p, sms, status, s)
                   : run_pass<F32Core<kDim, 8>>(p, sms, status, s);
+}
+
+template <int kDim>
+cudaError_t run_dim(const KvPass& p, int sms, int* status, cudaStream_t s) {
+  if (p.a.c.dtype != 0) return run_f32<kDim>(p, sms, status, s);
+  const long long q = std::min<long long>(p.part.per, p.a.N) * (p.a.H / p.a.c.heads);
+  return q <= 8 ? run_pass<FewCore<kDim>>(p, sms, status, s) : run_pass<ManyCore<kDim>>(p, sms, status, s);
 }
 
 // More queries of the same tokens than one warp holds: tiles by tcgen05.
@@ -899,6 +908,7 @@ cudaError_t run_part(KvPass p, const KvMaps& maps, int sms, int* status, cudaStr
     const cudaError_t e = launch_kv_tc(p, maps, sms, status, s);
     return e != cudaSuccess ? e : run_join<__nv_bfloat16>(p, sms, s);
   }
+  if (p.a.c.dtype != 0 && dim <= 32) return run_f32<32>(p, sms, status, s);   // bf16: no faster than by 64
   return dim <= 64    ? run_dim<64>(p, sms, status, s)
          : dim <= 128 ? run_dim<128>(p, sms, status, s)
                       : run_dim<256>(p, sms, status, s);

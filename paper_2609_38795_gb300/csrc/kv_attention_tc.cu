@@ -13,19 +13,24 @@ namespace {
 // columns, so that few queries waste nothing:
 //   S^T [128 tokens, NQ] = K Q^T          (K tile and Q by rows of elements)
 //   O^T [dim, NQ]       += V^T P^T        (V tile and P by rows of tokens, both read transposed)
-// with S^T twice and O^T in tensor memory.  A thread of the softmax has one token (a lane) and its
+// with S^T twice and O^T in tensor memory.  Bound by memory where the tokens are many (128 blocks of 16 rows over
+// 1024 to 3000 tokens, 8 heads of 128, 4 queries a head: 245 us, 4.4 TB/s of the 1.08 GB read; a tile of 128
+// tokens then takes 4200 cycles, of which a product's issue and wait 1000 each and a softmax 2200, one after
+// the other on three roles), by the softmax where they are shared (6 prefixes of 2032 tokens, 128 rollouts each:
+// 80 us).  A thread of the softmax has one token (a lane) and its
 // group's queries (columns): no sum crosses lanes until the item ends, the weights leave as 16-byte packs
 // into the shared-memory layout that the second product reads, and the running references are lagging
 // ones, in shared memory: a tile whose scores stay below reference + kLag needs one vote of the threads.
-//   Warps: groups of 4 for the softmax (two or four, each with its share of the queries), 4 copy (K and V
+//   Warps: groups of 4 for the softmax (each with its share of the queries), 4 copy (K and V
 // tiles of 128 tokens, gathered by rows of their pages, in a ring), 1 issues products and 3 make its group
-// whole.  A tile's softmax is a chain of waits more than work, so more groups of fewer columns each are
-// faster as long as their sums fit the registers.
+// whole.  A tile's softmax is a chain of waits more than work: four groups of 16 columns each take 297 us
+// where two of 32 take 314, and loops that stay in the nearest instruction cache count for as much (issuing
+// the products from rolled loops, 297 to 263; one place for all copies, 263 to 245).
 //   A copy warp has 32 tokens of a tile.  Where a token's row is a row of one matrix over the whole cache
 // and pages hold a multiple of 8 tokens, it fetches them by TMA in boxes of 8, 16 or 32 rows; the last
 // tokens of a run and other layouts come by 16-byte copies, which an SM carries out at 24 bytes a cycle
-// at most (all of it so: 128 blocks of 16 rows over 1024 to 3000 tokens 353 us; by tile::gather4, which
-// would serve any page, 644).
+// at most (all of it so: 300 us cold where boxes take 257; by tile::gather4, which would serve any page, it
+// took 644 where these copies took 353).
 constexpr int kBlk = 128;
 constexpr int kCopyWarps = 4;
 constexpr int kInfo = 8;           // tiles whose masks and flags are kept
@@ -274,7 +279,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
       }
       next.pg = in.t0 + w * 32 + lane < in.most ? a.table[(long long)in.seq * a.cols + j] : -1;
       next.off = off;
-      next.whole = in.t0 + w * 32 + 32 <= in.most;
+      next.whole = in.most - in.t0 >= w * 32 + 32;
       next.unit = in.unit;
       next.tile = in.tile;
       next.first = i == 0 || in.b == 0;

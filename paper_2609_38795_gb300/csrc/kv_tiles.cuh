@@ -252,9 +252,11 @@ ALR_DEV long long quotient(long long a, long long b) {
   return ((a | b) >> 32) == 0 ? (long long)(uint32_t(a) / uint32_t(b)) : a / b;
 }
 
-// Blocks that an item costs beside its own (decode of 64 x 0..32768 by logarithm, where the short ones
-// come together: 176 us without, 164 with).
-constexpr int kItemCost = 2;
+// Blocks that an item costs beside its own.  Blocks of 16: decode of 64 x 0..32768 tokens by logarithm, whose
+// short sequences come together, 153 us with 0, 138 with 2, 124 with 6 or 8; one of 64 x 0..1024 89, 69, 62.
+// Blocks of 128: 128 blocks of 16 rows 278 us with 0, 257 with 2 or 4, 269 with 8.  (GPU time, cold.)
+template <int kBlk>
+constexpr int kItemCost = kBlk < 128 ? 6 : 3;
 
 // The line: `n` workers (`per_block` consecutive ones of each thread block) have `each` places,
 // the first `more` of them one more.
@@ -286,7 +288,7 @@ ALR_DEV Line find_starts(const KvPass& p, WorkerStart* at, long long* sums, long
   const int per = (p.n_tiles + n_threads - 1) / n_threads;
   const int a = int(min((long long)tid * per, (long long)p.n_tiles)), e = min(a + per, p.n_tiles);
   N own = 0;
-  for (int i = a; i < e; ++i) own += tile_blocks<kBlk>(p, i) + kItemCost;
+  for (int i = a; i < e; ++i) own += tile_blocks<kBlk>(p, i) + kItemCost<kBlk>;
   own *= p.n_units;
   const N up = warp_scan(own);
   if (lane == 31) buf[warp] = up;
@@ -296,7 +298,7 @@ ALR_DEV Line find_starts(const KvPass& p, WorkerStart* at, long long* sums, long
   const N before_warp = __shfl_sync(~0u, of_warps, max(warp - 1, 0));
   sums[tid] = (warp > 0 ? before_warp : N(0)) + up - own;
   Line line;
-  const N items = N(p.n_tiles) * p.n_units, blocks = total - kItemCost * items;
+  const N items = N(p.n_tiles) * p.n_units, blocks = total - kItemCost<kBlk> * items;
   line.per_block = int(min(quotient(blocks + gridDim.x - 1, gridDim.x), (N)p.block_workers));
   line.n = int(min(N(line.per_block) * N(gridDim.x), blocks));
   const N each = quotient(total, line.n);
@@ -318,7 +320,7 @@ ALR_DEV Line find_starts(const KvPass& p, WorkerStart* at, long long* sums, long
     // rest is less than the thread's places (of lengths that do not change meanwhile)
     for (int tile = (n - 1) * per; tile < tile_end; tile += 32) {
       const int mine = tile + lane;
-      const N len = mine < tile_end ? N(tile_blocks<kBlk>(p, mine) + kItemCost) * p.n_units : N(0);
+      const N len = mine < tile_end ? N(tile_blocks<kBlk>(p, mine) + kItemCost<kBlk>) * p.n_units : N(0);
       const N sum = per > 1 ? warp_scan(len) : len;
       const uint32_t past = __ballot_sync(~0u, sum > rest);
       if (past == 0) {
@@ -331,8 +333,8 @@ ALR_DEV Line find_starts(const KvPass& p, WorkerStart* at, long long* sums, long
       const N places = quotient(__shfl_sync(~0u, len, k2), p.n_units);
       const int unit = int(quotient(rest, places)), off = int(rest - unit * places);
       if (lane == 0)
-        at[k] = {pos - kItemCost * (N(tile) * p.n_units + unit) - min(off, kItemCost), tile, unit,
-                 max(off - kItemCost, 0)};
+        at[k] = {pos - kItemCost<kBlk> * (N(tile) * p.n_units + unit) - min(off, kItemCost<kBlk>), tile, unit,
+                 max(off - kItemCost<kBlk>, 0)};
       break;
     }
   }

@@ -216,7 +216,9 @@ FORMS = [dict(heads=2, group=2, dim=64, page=16, dtype=BF), dict(heads=1, group=
          dict(heads=3, group=2, dim=4, page=1, dtype=F32)]
 
 
-@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("form", FORMS + [dict(heads=1, group=71, dim=64, page=16, dtype=BF),
+                                          dict(heads=2, group=32, dim=128, page=8, dtype=BF, hnd=True),
+                                          dict(heads=1, group=150, dim=80, page=20, dtype=BF)])
 def test_decode(form):
     """One row for each sequence: lengths from none on, either side of pages and of tiles."""
     p = form["page"]
