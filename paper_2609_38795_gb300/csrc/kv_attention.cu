@@ -74,7 +74,8 @@ struct ManyCore {
     for (int half = 0; half < 2; ++half) {
       const int i = g + 8 * half, r = i / p.gw;
       const bool there = i < n_q && i - r * p.gw < gw;
-      const E* src = static_cast<const E*>(p.a.Q) + (there ? (row0 + r) * p.a.ldq + (h0 + i - r * p.gw) * p.a.c.dim : 0);
+      const E* src = static_cast<const E*>(p.a.Q) +
+                     (there ? (row0 + r) * p.a.ldq + (h0 + i - r * p.gw) * p.a.c.dim : 0);
 #pragma unroll
       for (int k = 0; k < kSteps; ++k)
 #pragma unroll
@@ -188,7 +189,8 @@ struct ManyCore {
         if (t == 0) ml[2 * i] = m[h], ml[2 * i + 1] = l[h];
 #pragma unroll
         for (int k = 0; k < kDim / 8; ++k)
-          if (k * 8 < dim) *reinterpret_cast<float2*>(to + i * (dim + 4) + k * 8 + 2 * t) = {o[k][2 * h], o[k][2 * h + 1]};
+          if (k * 8 < dim)
+            *reinterpret_cast<float2*>(to + i * (dim + 4) + k * 8 + 2 * t) = {o[k][2 * h], o[k][2 * h + 1]};
       }
     }
   }
@@ -215,7 +217,8 @@ struct FewCore {
   ALR_DEV void load_q(const KvPass& p, long long row0, int h0, int n_q, int gw, void*) {
     const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3, r = g / p.gw;
     const bool there = g < n_q && g - r * p.gw < gw;
-    const E* src = static_cast<const E*>(p.a.Q) + (there ? (row0 + r) * p.a.ldq + (h0 + g - r * p.gw) * p.a.c.dim : 0);
+    const E* src = static_cast<const E*>(p.a.Q) +
+                   (there ? (row0 + r) * p.a.ldq + (h0 + g - r * p.gw) * p.a.c.dim : 0);
 #pragma unroll
     for (int k = 0; k < kSteps; ++k)
 #pragma unroll
@@ -316,7 +319,8 @@ struct FewCore {
 // fp32 by fused multiply-adds (a tensor product in tf32 would lose 13 bits of the inputs).  Scores: lane
 // (h, i) = (lane / 16, lane % 16) takes half the packs of token i; weights go through shared memory;
 // values: a lane owns whole packs of the result, groups of lanes share the tokens where there are
-// fewer packs than lanes.  (48 sequences of up to 4001 tokens, 16 heads of 80, one query each: 203 us, 4.8 TB/s.)
+// fewer packs than lanes.  (48 sequences of up to 4001 tokens, 16 heads of 80, one query each: 200 us, 4.9
+// TB/s; 32 blocks of 8 rows over 1000 to 3000, 32 heads of 128: 485 us cold, 17 TFLOP/s on five warps an SM.)
 template <int kDim_, int kQ>
 struct F32Core {
   using E = float;
@@ -335,7 +339,8 @@ struct F32Core {
 #pragma unroll 1
     for (int i = 0; i < kQ; ++i) {
       const int r = i / p.gw;
-      const float* src = static_cast<const float*>(p.a.Q) + (row0 + r) * p.a.ldq + (h0 + i - r * p.gw) * p.a.c.dim;
+      const float* src =
+          static_cast<const float*>(p.a.Q) + (row0 + r) * p.a.ldq + (h0 + i - r * p.gw) * p.a.c.dim;
       for (int c = threadIdx.x & 31; c < kPacks; c += 32) {
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
         if (i < n_q && i - r * p.gw < gw && 4 * c < p.a.c.dim) x = *reinterpret_cast<const float4*>(src + 4 * c);
@@ -448,7 +453,8 @@ struct F32Core {
           for (int off = kPacks; off < 32; off <<= 1) o[i][k][e] += __shfl_xor_sync(~0u, o[i][k][e], off);
         const int d = 4 * (own + 32 * k);
         if (lane < kPacks && d < dim)
-          *reinterpret_cast<float4*>(to + i * (dim + 4) + d) = make_float4(o[i][k][0], o[i][k][1], o[i][k][2], o[i][k][3]);
+          *reinterpret_cast<float4*>(to + i * (dim + 4) + d) =
+              make_float4(o[i][k][0], o[i][k][1], o[i][k][2], o[i][k][3]);
       }
     }
   }
@@ -534,7 +540,8 @@ ALR_DEV void join_parts(const KvPass& p, const float* parts, int slot0, bool ope
       for (int e = 0; e < 2; ++e)
         if (4 * (lane + 32 * e) < dim) {
           const float4 y = x[lane + 32 * e];
-          s.o[e] = make_float4(fmaf(y.x, f, s.o[e].x), fmaf(y.y, f, s.o[e].y), fmaf(y.z, f, s.o[e].z), fmaf(y.w, f, s.o[e].w));
+          s.o[e] = make_float4(fmaf(y.x, f, s.o[e].x), fmaf(y.y, f, s.o[e].y), fmaf(y.z, f, s.o[e].z),
+                               fmaf(y.w, f, s.o[e].w));
         }
     }
   }
@@ -556,7 +563,8 @@ ALR_DEV void put_sums(const KvPass& p, const KvRowOut& to, const JoinSums& s) {
 // table, keys, results and join (64 sequences of up to 1024 tokens: 62 us cold for 134 MB).
 //   Copies are of 16 bytes: bulk copies of a row each took 1020 us where these took 830.
 template <typename Core>
-__global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(const __grid_constant__ KvPass p, int* status) {
+__global__ void __launch_bounds__(Core::kMostWarps * 32, 1)
+    kv_blocks_kernel(const __grid_constant__ KvPass p, int* status) {
   using E = typename Core::E;
   constexpr int kPacks = Core::kPacks, kPack = 16 / sizeof(E);
   constexpr int kRowsAt = 32 / kPacks > 1 ? 32 / kPacks : 1;      // rows of one copy instruction
@@ -757,7 +765,8 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1) kv_blocks_kernel(con
 #pragma unroll
         for (int e = 0; e < kLaneDims; ++e)
           x[e] = e * 32 + lane < dim
-                     ? to_float(static_cast<const E*>(a.Q)[(row0 + r) * a.ldq + (h0 + q - r * p.gw) * dim + e * 32 + lane])
+                     ? to_float(static_cast<const E*>(
+                           a.Q)[(row0 + r) * a.ldq + (h0 + q - r * p.gw) * dim + e * 32 + lane])
                      : 0.f;
         const int lead = __shfl_sync(~0u, tile.lead, r), len = __shfl_sync(~0u, tile.len, r);
         const int seq = __shfl_sync(~0u, tile.seq, r), first = __shfl_sync(~0u, tile.first, max(lead, 0));

@@ -667,7 +667,8 @@ __global__ void __launch_bounds__(C::kThreads, 1)
 #pragma unroll
           for (int e = 0; e < kLaneDims; ++e)
             x[e] = e * 32 + lane < dim
-                       ? to_float(static_cast<const E*>(a.Q)[(row0 + r) * a.ldq + (long long)(h0 + q - r * p.gw) * dim + e * 32 + lane])
+                       ? to_float(static_cast<const E*>(
+                             a.Q)[(row0 + r) * a.ldq + (h0 + q - r * p.gw) * dim + e * 32 + lane])
                        : 0.f;
           const int lead = __shfl_sync(~0u, tile.lead, r), len = __shfl_sync(~0u, tile.len, r);
           const int seq = __shfl_sync(~0u, tile.seq, r), first = __shfl_sync(~0u, tile.first, max(lead, 0));
