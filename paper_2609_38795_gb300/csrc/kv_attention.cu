@@ -8,8 +8,6 @@
 namespace alr {
 namespace {
 
-constexpr int kBlk = 16;       // tokens of a block
-
 // ------------------------------------------------------------------------- cores ---
 // A core holds the sums of an item's queries for a warp: load_q, see (how many tokens of the run each of
 // the lane's queries sees), add (one block from the ring), leave (the sums to shared memory).
@@ -57,6 +55,7 @@ constexpr float kLag = 8.f;
 template <int kDim_>
 struct ManyCore {
   using E = __nv_bfloat16;
+  static constexpr int kBlk = 16;            // tokens of a block
   static constexpr int kDim = kDim_, kMostWarps = 8, kMaxQ = 16;
   static constexpr int kSteps = kDim / 16, kPacks = kDim / 8;
   static constexpr int kScratch = 0;
@@ -206,6 +205,7 @@ struct ManyCore {
 template <int kDim_>
 struct FewCore {
   using E = __nv_bfloat16;
+  static constexpr int kBlk = 16;
   static constexpr int kDim = kDim_, kMostWarps = kDim <= 128 ? 16 : 8, kMaxQ = 8;
   static constexpr int kSteps = kDim / 16, kPacks = kDim / 8;
   static constexpr int kScratch = 0;
@@ -243,7 +243,7 @@ struct FewCore {
   }
   ALR_DEV void add(const KvPass& p, char* ring, int row_bytes, int t0, uint32_t there, bool plain, void*) {
     const int lane = threadIdx.x & 31, g = lane >> 2;
-    const uint32_t at = smem_u32(ring) + (lane & 15) * row_bytes + (lane >> 4) * 16;
+    const uint32_t at = smem_u32(ring) + (lane & (kBlk - 1)) * row_bytes + (lane >> 4) * 16;
     float s[4] = {}, s2[4] = {};
 #pragma unroll
     for (int k = 0; k < kSteps; ++k) {
@@ -317,13 +317,17 @@ struct FewCore {
 };
 
 // fp32 by fused multiply-adds (a tensor product in tf32 would lose 13 bits of the inputs).  Scores: lane
-// (h, i) = (lane / 16, lane % 16) takes half the packs of token i; weights go through shared memory;
+// (h, i) = (lane / kBlk, lane % kBlk) takes its share of the packs of token i; weights go through shared memory;
 // values: a lane owns whole packs of the result, groups of lanes share the tokens where there are
 // fewer packs than lanes.  (48 sequences of up to 4001 tokens, 16 heads of 80, one query each: 200 us, 4.9
-// TB/s; 32 blocks of 8 rows over 1000 to 3000, 32 heads of 128: 485 us cold, 17 TFLOP/s on five warps an SM.)
+// TB/s; 32 blocks of 8 rows over 1000 to 3000, 32 heads of 128: 441 us, 19 TFLOP/s.)
 template <int kDim_, int kQ>
 struct F32Core {
   using E = float;
+  // Long rows of several queries in shorter blocks, whose rings leave room for more warps (128 rollouts of a
+  // prefix of 4000 tokens, 64 heads on 8 of 256: 1706 us by blocks of 16, 1081 so; 32 blocks of 8 rows, 32
+  // heads on 8 of 128: 486 and 441).
+  static constexpr int kBlk = kQ == 8 && kDim_ >= 128 ? 8 : 16, kShares = 32 / kBlk;
   static constexpr int kDim = kDim_, kMostWarps = kQ == 1 ? 16 : 8, kMaxQ = kQ;
   static constexpr int kPacks = kDim / 4;
   static constexpr int kOwn = kPacks > 32 ? kPacks / 32 : 1;       // packs of a lane
@@ -367,11 +371,11 @@ struct F32Core {
     const char* vs = ks + kBlk * row_bytes;
     const float* qs = static_cast<const float*>(scratch);
     float* ws = static_cast<float*>(scratch) + kQ * kDim;
-    const int lane = threadIdx.x & 31, tok = lane & 15, half = lane >> 4;
+    const int lane = threadIdx.x & 31, tok = lane % kBlk, share = lane / kBlk;
     const int packs = p.a.c.dim / 4;
     float s[kQ] = {};
 #pragma unroll 4
-    for (int c = half; c < packs; c += 2) {
+    for (int c = share; c < packs; c += kShares) {
       const float4 k = *reinterpret_cast<const float4*>(ks + tok * row_bytes + 16 * c);
 #pragma unroll
       for (int i = 0; i < kQ; ++i) {
@@ -385,7 +389,9 @@ struct F32Core {
     float top[kQ];
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
-      s[i] = __fmul_rn(s[i] + __shfl_xor_sync(~0u, s[i], 16), c);    // never an fma with the reference
+#pragma unroll
+      for (int off = kBlk; off < 32; off <<= 1) s[i] += __shfl_xor_sync(~0u, s[i], off);
+      s[i] = __fmul_rn(s[i], c);             // never an fma with the reference
       if (!plain && (t0 + tok >= lim[i] || !here)) s[i] = kNegInf;
       top[i] = warp_max(s[i]);
       moves |= top[i] > m[i] + kLag;
@@ -410,7 +416,7 @@ struct F32Core {
 #pragma unroll
     for (int i = 0; i < kQ; ++i) {
       const float e = ex2(s[i] - (m[i] == kNegInf ? 0.f : m[i]));
-      if (half == 0) {
+      if (share == 0) {
         l[i] += e;
         ws[tok * kQ + i] = e;
       }
@@ -566,7 +572,8 @@ template <typename Core>
 __global__ void __launch_bounds__(Core::kMostWarps * 32, 1)
     kv_blocks_kernel(const __grid_constant__ KvPass p, int* status) {
   using E = typename Core::E;
-  constexpr int kPacks = Core::kPacks, kPack = 16 / sizeof(E);
+  constexpr int kBlk = Core::kBlk, kPacks = Core::kPacks, kPack = 16 / sizeof(E);
+  constexpr uint32_t kAll = (1u << kBlk) - 1;
   constexpr int kRowsAt = 32 / kPacks > 1 ? 32 / kPacks : 1;      // rows of one copy instruction
   constexpr int kCopies = kBlk * kPacks / 32;
   extern __shared__ __align__(128) char ring_smem[];
@@ -608,7 +615,7 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1)
   if (count > 0) in.start(p, starts[warp].tile, starts[warp].unit, starts[warp].b);
   Cursor<kBlk> at = in;                      // of the sums
 
-  // page and position in it of the lane's token (lane % 16) in the next block to load
+  // page and position in it of the lane's token (lane % kBlk) in the next block to load
   int j = 0, off = 0, pg = -1;
   const auto look_up = [&](bool runs_on) {
     if (runs_on) {
@@ -616,11 +623,11 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1)
       off += p.step_tok;
       if (off >= a.c.page) off -= a.c.page, ++j;
     } else {
-      const int tok = in.t0 + (lane & 15);
+      const int tok = in.t0 + (lane & (kBlk - 1));
       j = tok / a.c.page;
       off = tok - j * a.c.page;
     }
-    pg = in.t0 + (lane & 15) < in.most ? a.table[(long long)in.seq * a.cols + j] : -1;
+    pg = in.t0 + (lane & (kBlk - 1)) < in.most ? a.table[(long long)in.seq * a.cols + j] : -1;
   };
   if (count > 0) look_up(false);
   const uint32_t ring_at = smem_u32(ring);
@@ -629,14 +636,14 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1)
   long long head = (long long)(in.unit / p.gs) * a.c.sh + pack * kPack;      // of the next block
   const auto load = [&](int slot) {
     const bool there = pg >= 0 && pg < a.c.n_pages;
-    const uint32_t all = __ballot_sync(~0u, there) & 0xffffu;
+    const uint32_t all = __ballot_sync(~0u, there) & kAll;
     if (lane == 0) there_of[warp][slot] = all;
     const E* K = static_cast<const E*>(a.c.K) + head;
     const E* V = static_cast<const E*>(a.c.V) + head;
     const uint32_t dst = ring_at + slot * slot_bytes + pack * 16, v_off = kBlk * row_bytes;
-    if (block_in_page && all == 0xffffu) {
+    if (block_in_page && all == kAll) {
       // one page: rows a fixed step apart
-      const long long from = pg * a.c.sp + (off - (lane & 15) + sub) * a.c.st;
+      const long long from = pg * a.c.sp + (off - (lane & (kBlk - 1)) + sub) * a.c.st;
       const E* k = K + from;
       const E* v = V + from;
       uint32_t to = dst + sub * row_bytes;
@@ -718,7 +725,7 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1)
       load_next();
       const uint32_t there = there_of[warp][slot];
       core.add(p, ring + slot * slot_bytes, row_bytes, at.t0, there,
-               least - at.t0 >= kBlk && there == 0xffffu, scratch);
+               least - at.t0 >= kBlk && there == kAll, scratch);
       if (++slot == stages) slot = 0, ++round;
       if (i + 1 < count) on = at.advance(p);
     }
@@ -870,6 +877,7 @@ cudaError_t run_join(const KvPass& p, int sms, cudaStream_t s) {
 template <typename Core>
 cudaError_t run_pass(KvPass p, int sms, int* status, cudaStream_t s) {
   using E = typename Core::E;
+  constexpr int kBlk = Core::kBlk;
   shape_pass(p, Core::kMaxQ, 32, kBlk);
   // as many warps as have two blocks each, then as many blocks
   const int slot = 2 * kBlk * row_bytes_of<E>(p.a.c.dim);
