@@ -326,8 +326,8 @@ struct F32Core {
   using E = float;
   // Long rows of several queries in shorter blocks, whose rings leave room for more warps (128 rollouts of a
   // prefix of 4000 tokens, 64 heads on 8 of 256: 1706 us by blocks of 16, 1081 so; 32 blocks of 8 rows, 32
-  // heads on 8 of 128: 486 and 441).
-  static constexpr int kBlk = kQ == 8 && kDim_ >= 128 ? 8 : 16, kShares = 32 / kBlk;
+  // heads on 8 of 128: 486 and 441; 48 sequences of up to 3000 tokens, 16 heads on 4 of 256: 135 and 121).
+  static constexpr int kBlk = kDim_ > 128 || (kQ == 8 && kDim_ >= 128) ? 8 : 16, kShares = 32 / kBlk;
   static constexpr int kDim = kDim_, kMostWarps = kQ == 1 ? 16 : 8, kMaxQ = kQ;
   static constexpr int kPacks = kDim / 4;
   static constexpr int kOwn = kPacks > 32 ? kPacks / 32 : 1;       // packs of a lane
