@@ -831,7 +831,7 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1)
 
 // --------------------------------------------------- join of items across blocks ---
 template <typename E>
-__global__ void __launch_bounds__(kJoinWarps * 32) kv_join_kernel(const __grid_constant__ KvPass p) {
+__global__ void __launch_bounds__(kJoinWarps * 32, 3) kv_join_kernel(const __grid_constant__ KvPass p) {
   __shared__ float4 sums[kJoinWarps][kKvMaxDim / 4];
   pdl_wait_and_release();
   const int id = blockIdx.x;
