@@ -197,7 +197,8 @@ struct ManyCore {
 
 // bf16, up to 8 queries, with the tokens (the elements of a value) on a product's 16 rows and the queries
 // on its 8 columns: half the products of ManyCore and half its registers, so 12 warps an SM and not 8 (256
-// sequences of 0 to 8192 tokens, 8 heads of 128, 4 queries each: 825 us by ManyCore, 718 so, 6.0 TB/s).
+// sequences of 0 to 8192 tokens, 8 heads of 128, 4 queries each: 825 us by ManyCore, 682 so, 6.3 TB/s).  Registers
+// are for 12 warps of 128 elements, not for 16 that the rings leave no room for: 718 us with a spill.
 // Lane (g, t) has queries 2t and 2t + 1 of tokens g and g + 8; the weights are transposed into the
 // second product's operand.
 //   The reference lags, and no maximum is taken while a vote finds all scores below it + kLag: sums cross
@@ -206,7 +207,7 @@ template <int kDim_>
 struct FewCore {
   using E = __nv_bfloat16;
   static constexpr int kBlk = 16;
-  static constexpr int kDim = kDim_, kMostWarps = kDim <= 128 ? 16 : 8, kMaxQ = 8;
+  static constexpr int kDim = kDim_, kMostWarps = kDim <= 64 ? 10 : kDim <= 128 ? 12 : 8, kMaxQ = 8;
   static constexpr int kSteps = kDim / 16, kPacks = kDim / 8;
   static constexpr int kScratch = 0;
   uint32_t q[kSteps][2];
