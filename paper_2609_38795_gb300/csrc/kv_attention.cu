@@ -762,31 +762,14 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1)
       odd = fmaf(0.f, (x.x + x.y) + (x.z + x.w), odd);
     }
     if (n_rows > 1 && __any_sync(~0u, !(odd == 0.f))) {
-      // Weights of 0 times a value that is not finite: such a value may lie in a token that a query does
-      // not see but another of the tile does.  All queries again, token by token.
 #pragma unroll 1
       for (int q = 0; q < n_q; ++q) {
         const int r = q / p.gw;
         if (q - r * p.gw >= gw) continue;
+        int seq, t0, t1;
+        row_tokens<kBlk>(tile, r, b0, b1, seq, t0, t1);
         __syncwarp();
-        float x[kLaneDims], o[kLaneDims] = {}, m2 = kNegInf, l2 = 0.f;
-#pragma unroll
-        for (int e = 0; e < kLaneDims; ++e)
-          x[e] = e * 32 + lane < dim
-                     ? to_float(static_cast<const E*>(
-                           a.Q)[(row0 + r) * a.ldq + (h0 + q - r * p.gw) * dim + e * 32 + lane])
-                     : 0.f;
-        const int lead = __shfl_sync(~0u, tile.lead, r), len = __shfl_sync(~0u, tile.len, r);
-        const int seq = __shfl_sync(~0u, tile.seq, r), first = __shfl_sync(~0u, tile.first, max(lead, 0));
-        const long long t0 = (long long)(b0 - first) * kBlk, t1 = (long long)(b1 - first) * kBlk;
-        if (len > 0)
-          walk_tokens<E>(a, seq, int(max(t0, 0ll)), int(min(t1, (long long)len)), kv, x, m2, l2, o);
-        const KvRowOut again = out(q, r, m2, l2, lane == 0);
-#pragma unroll
-        for (int e = 0; e < kLaneDims; ++e) {
-          const float v[1] = {o[e]};
-          if (e * 32 + lane < dim) put<E, 1>(again, e * 32 + lane, v);
-        }
+        take_again<E, Core::kDim, 1>(p, row0 + r, h0 + q - r * p.gw, seq, t0, t1, whole ? nullptr : p.parts, part, q);
       }
     }
     __syncwarp();

@@ -64,7 +64,7 @@ struct alignas(16) KvMisc {
   uint32_t info[kInfo];                   // 1: first of its item here, 2: last
   uint32_t tmem;
   int abort_word;
-  uint32_t bad[4];                        // queries with a value that is not finite
+  int odd;                                // whether some result was not finite
   WorkerStart start[2];
   Line line;                              // needed again at the end alone
   long long buf[24];
@@ -193,6 +193,40 @@ __device__ __noinline__ float move_refs(uint32_t s_at, uint32_t o_at, float c, f
   return f;
 }
 
+// The results of worker `id`'s stretch that are not finite, each taken again by one of n_warps warps.  They are
+// found where they were left: a list of them would have no bound.
+template <typename E, int kDim>
+__device__ __noinline__ void take_odd_again(const KvPass& p, const WorkerStart& from, int count, int id, int warp,
+                                            int n_warps) {
+  const int lane = threadIdx.x & 31, dim = p.a.c.dim, group = p.a.H / p.a.c.heads;
+  int tile_id = from.tile, unit = from.unit, b0 = from.b;
+  while (count > 0) {
+    const Tile tile = load_tile<kBlk>(p, tile_id);
+    long long row0;
+    const int n_rows = max(tile_rows(p, tile_id, row0), 0), b1 = min(tile.nb, b0 + count);
+    const int kv = unit / p.gs, slice = (unit - kv * p.gs) * p.gw, gw = min(p.gw, group - slice);
+    const bool whole = b0 == 0 && b1 == tile.nb, opens = b0 == 0 && b1 < tile.nb;
+    const int part = 2 * id + (opens ? 1 : 0);
+    for (int q = warp; q < n_rows * p.gw && n_rows > 1; q += n_warps) {
+      const int r = q / p.gw, h = kv * group + slice + q - r * p.gw;
+      if (q - r * p.gw >= gw) continue;
+      const float* sums = whole ? p.put_o + ((row0 + r) * p.a.H + h) * dim
+                                : p.block_parts + part * part_floats(p.max_q, dim) + q * dim;
+      const E* row = static_cast<const E*>(p.a.out) + (row0 + r) * p.a.ldo + (long long)h * dim;
+      const bool final_row = whole && p.put_o == nullptr;
+      float odd = 0.f;
+      for (int d = lane; d < dim; d += 32) odd = fmaf(0.f, final_row ? to_float(row[d]) : sums[d], odd);
+      if (!__any_sync(~0u, !(odd == 0.f))) continue;
+      int seq, t0, t1;
+      row_tokens<kBlk>(tile, r, b0, b1, seq, t0, t1);
+      take_again<E, kDim, 2>(p, row0 + r, h, seq, t0, t1, whole ? nullptr : p.block_parts, part, q);
+    }
+    count -= b1 - b0;
+    b0 = 0;
+    if (++unit == p.n_units) unit = 0, ++tile_id;
+  }
+}
+
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, 1)
     kv_tc_kernel(const __grid_constant__ KvMaps maps, const __grid_constant__ KvPass p, int* status) {
@@ -223,7 +257,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
     }
     mbar_init(&mi.drain, 1);
     mi.abort_word = 0;
-    for (int i = 0; i < 4; ++i) mi.bad[i] = 0;
+    mi.odd = 0;
     fence_mbar_init();
   }
   if (warp == kMmaWarp) {
@@ -602,7 +636,6 @@ __global__ void __launch_bounds__(C::kThreads, 1)
         for (int k = 0; k < 4; ++k) s += lsum[wg * 4 + k][tid];
         KvRowOut o = {0.f, 0.f, nullptr, nullptr, nullptr};
         if (q < n_q && q - r * p.gw < gw) o = out(q, r, s == 0.f ? kNegInf : sm.ref[q] * c, s, true);
-        if (!(s - s == 0.f)) atomicOr(&mi.bad[q >> 5], 1u << (q & 31));
         outs[q] = o;
       }
       named_bar_sync(bar, 128);
@@ -652,47 +685,17 @@ __global__ void __launch_bounds__(C::kThreads, 1)
         }
         named_bar_sync(bar, 128);
       }
-      if (!(odd == 0.f)) {                   // which queries: rare
-        for (int k = 0; k < kOwn && q0 + k < n_q; ++k) atomicOr(&mi.bad[(q0 + k) >> 5], 1u << ((q0 + k) & 31));
-      }
+      if (n_rows > 1 && !(odd == 0.f)) mi.odd = 1;
       tc_fence_before();
       named_bar_sync(kAllBar, kAll);
-      if (n_rows > 1 && (mi.bad[0] | mi.bad[1] | mi.bad[2] | mi.bad[3]) != 0) {
-        // Weights of 0 times a value that is not finite: such a value may lie in a token that the
-        // query does not see but another of the tile does.  Its tokens again, one by one.
-        for (int q = warp; q < n_q; q += kSoftWarps) {
-          const int r = q / p.gw;
-          if (!(mi.bad[q >> 5] >> (q & 31) & 1) || q - r * p.gw >= gw) continue;
-          float x[kLaneDims], o[kLaneDims] = {}, m = kNegInf, sum = 0.f;
-#pragma unroll
-          for (int e = 0; e < kLaneDims; ++e)
-            x[e] = e * 32 + lane < dim
-                       ? to_float(static_cast<const E*>(
-                             a.Q)[(row0 + r) * a.ldq + (h0 + q - r * p.gw) * dim + e * 32 + lane])
-                       : 0.f;
-          const int lead = __shfl_sync(~0u, tile.lead, r), len = __shfl_sync(~0u, tile.len, r);
-          const int seq = __shfl_sync(~0u, tile.seq, r), first = __shfl_sync(~0u, tile.first, max(lead, 0));
-          const long long t0 = (long long)(b0 - first) * kBlk, t1 = (long long)(b1 - first) * kBlk;
-          if (len > 0)
-            walk_tokens<E>(a, seq, int(max(t0, 0ll)), int(min(t1, (long long)len)), kv, x, m, sum, o);
-          const KvRowOut to = out(q, r, m, sum, lane == 0);
-#pragma unroll
-          for (int e = 0; e < kLaneDims; ++e) {
-            const float v[1] = {o[e]};
-            if (e * 32 + lane < dim) put<E, 1>(to, e * 32 + lane, v);
-          }
-        }
-        named_bar_sync(kAllBar, kAll);
-        if (threadIdx.x < 4) mi.bad[threadIdx.x] = 0;
-      } else if (n_rows <= 1) {
-        named_bar_sync(kAllBar, kAll);
-        if (threadIdx.x < 4) mi.bad[threadIdx.x] = 0;
-      }
       if (opens && threadIdx.x == 0) {
         cut = make_int4(tile_id, unit, mi.line.last_before(mi.line.start(id + 1) + (tile.nb - b1)) - id + 1, 0);
       }
     }
     if (threadIdx.x == 0 && count > 0) p.cuts[id] = cut;
+    // Results that are not finite are taken again here, when no role waits for this one any more: the time
+    // that it takes is bounded by nothing but the tokens, and a wait gives up after a limit.
+    if (count > 0 && mi.odd != 0 && !*ab.smem) take_odd_again<E, C::kChunks * 64>(p, mi.start[0], count, id, warp, kSoftWarps);
   }
   __syncthreads();
   tc_fence_after();

@@ -361,34 +361,95 @@ ALR_DEV Line find_item_starts(const KvPass& p, WorkerStart* at, long long* buf) 
   return line;
 }
 
-// ------------------------------------------------------------------ row by row ---
-// One query over tokens [t0, t1) of a sequence, token by token: lane i holds elements i, i + 32, ... of q
-// and of the sum; (m, l, o): running maximum (log2), sum, weighted values.
-constexpr int kLaneDims = kKvMaxDim / 32;
-
-template <typename E>
-ALR_DEV void walk_tokens(const KvAttention& a, int seq, int t0, int t1, int head,
-                         const float (&q)[kLaneDims], float& m, float& l, float (&o)[kLaneDims]) {
-  const int lane = threadIdx.x & 31;
+// ------------------------------------------------------------- a query by itself ---
+// Weights of 0 times a value that is not finite are NaN, and such a value may lie in a token that a query
+// does not see but another of its tile does.  A query whose sums came out so is taken again over its tokens
+// [t0, t1) of the item alone, by a warp, 32 tokens at a time: a score a lane, then the values of the tokens that
+// count, four at a time by 8 lanes each.  Its result replaces the one in place: the final row or the prefix's,
+// or with `parts` place `slot` there.
+//   Rare, so short of registers first: 0.12 us a token and query for 64 bf16 elements, 0.21 for 128 (16 warps an
+// SM, a million tokens a sequence; 0.83 and 1.08 by scores that a warp's lanes added up, token by token).
+// kAhead: packs of values that a lane has on their way.
+template <typename E, int kDim, int kAhead>
+ALR_DEV void take_again(const KvPass& p, long long row, int h, int seq, int t0, int t1, float* parts,
+                        int slot, int q) {
+  constexpr int kPack = 16 / sizeof(E), kOwn = (kDim / kPack + 7) / 8;
+  struct alignas(16) Pack { E e[kPack]; };
+  const KvAttention& a = p.a;
+  const int lane = threadIdx.x & 31, dim = a.c.dim, head = h / (a.H / a.c.heads);
+  const int group = lane >> 3, first = (lane & 7) * kPack;           // of a token; the lane's packs
+  const E* Q = static_cast<const E*>(a.Q) + row * a.ldq + (long long)h * dim;
   const E* K = static_cast<const E*>(a.c.K) + head * a.c.sh;
   const E* V = static_cast<const E*>(a.c.V) + head * a.c.sh;
-  for (int t = t0; t < t1; ++t) {
-    const int j = t / a.c.page, pg = a.table[(long long)seq * a.cols + j];
-    if (pg < 0 || pg >= a.c.n_pages) continue;
-    const long long at = pg * a.c.sp + (t - j * a.c.page) * a.c.st;
-    float x = 0.f;
+  float m = kNegInf, l = 0.f, o[kOwn][kPack] = {};
+  for (int b = t0; b < t1; b += min(32, t1 - b)) {
+    int pg = -1;
+    long long at = 0;
+    if (lane < t1 - b) {
+      const int t = b + lane, j = t / a.c.page;
+      pg = a.table[(long long)seq * a.cols + j];
+      at = pg * a.c.sp + (t - j * a.c.page) * a.c.st;
+    }
+    float x = kNegInf;
+    if (pg >= 0 && pg < a.c.n_pages) {
+      x = 0.f;
+#pragma unroll 2 * kAhead
+      for (int d = 0; d < dim; d += kPack) {
+        const Pack k = *reinterpret_cast<const Pack*>(K + at + d), y = *reinterpret_cast<const Pack*>(Q + d);
 #pragma unroll
-    for (int i = 0; i < kLaneDims; ++i)
-      if (i * 32 + lane < a.c.dim) x = fmaf(q[i], to_float(K[at + i * 32 + lane]), x);
-    x = __fmul_rn(warp_reduce(x, AddOp()), a.scale * kLog2e);
-    if (x == kNegInf) continue;
-    const float up = fmaxf(m, x), c = ex2(m - up), e = ex2(x - up);
+        for (int e = 0; e < kPack; ++e) x = fmaf(to_float(y.e[e]), to_float(k.e[e]), x);
+      }
+      x = __fmul_rn(x, a.scale * kLog2e);
+    }
+    if (__any_sync(~0u, !(x < INFINITY))) {    // a score of NaN or +inf: so are all results
+      l = NAN;
+      break;
+    }
+    const uint32_t counts = __ballot_sync(~0u, x != kNegInf);
+    if (counts == 0) continue;
+    const float up = fmaxf(m, warp_max(x)), c = ex2(m - up), w = ex2(x - up);
     m = up;
-    l = fmaf(l, c, e);
+    l = fmaf(l, c, w);
 #pragma unroll
-    for (int i = 0; i < kLaneDims; ++i)
-      if (i * 32 + lane < a.c.dim) o[i] = fmaf(e, to_float(V[at + i * 32 + lane]), o[i] * c);
+    for (int i = 0; i < kOwn; ++i)
+#pragma unroll
+      for (int e = 0; e < kPack; ++e) o[i][e] *= c;
+#pragma unroll kAhead
+    for (int k0 = 0; k0 < 32; k0 += 4) {
+      const int k = k0 + group;
+      const E* v = V + __shfl_sync(~0u, at, k) + first;
+      const float f = __shfl_sync(~0u, w, k);
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i)
+        if ((counts >> k & 1) && first + 8 * i * kPack < dim) {
+          const Pack y = *reinterpret_cast<const Pack*>(v + 8 * i * kPack);
+#pragma unroll
+          for (int e = 0; e < kPack; ++e) o[i][e] = fmaf(f, to_float(y.e[e]), o[i][e]);
+        }
+    }
   }
+  l = warp_reduce(l, AddOp());
+  const KvRowOut to = parts == nullptr ? row_out(p, row, h, m, l, lane == 0)
+                                       : part_out(p, parts, slot, q, m, l, lane == 0);
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+#pragma unroll
+    for (int e = 0; e < kPack; ++e) {
+      o[i][e] += __shfl_xor_sync(~0u, o[i][e], 8);
+      o[i][e] += __shfl_xor_sync(~0u, o[i][e], 16);
+    }
+    if (group == 0 && first + 8 * i * kPack < dim) put<E, kPack>(to, first + 8 * i * kPack, o[i]);
+  }
+}
+
+// Tokens [t0, t1) that row r of the tile sees of its run in blocks [b0, b1) (all lanes call it).
+template <int kBlk>
+ALR_DEV void row_tokens(const Tile& tile, int r, int b0, int b1, int& seq, int& t0, int& t1) {
+  const int lead = __shfl_sync(~0u, tile.lead, r), len = __shfl_sync(~0u, tile.len, r);
+  const int first = __shfl_sync(~0u, tile.first, max(lead, 0));
+  seq = __shfl_sync(~0u, tile.seq, r);
+  t0 = int(max((long long)(b0 - first) * kBlk, 0ll));
+  t1 = len > 0 ? int(min((long long)(b1 - first) * kBlk, (long long)len)) : 0;
 }
 
 // A wait that runs out is recorded and passed over, as all waits after it: every role runs on to the end of

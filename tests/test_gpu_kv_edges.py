@@ -1,0 +1,82 @@
+"""Calls of the paged key-value cache at the edges of what its documentation allows, on the GPU.
+
+u = 2^-24; bounds as in test_gpu_kv.py, each derived where it is used."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_38795_gb300 import alr, build_lib
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+NAN, INF = float("nan"), float("inf")
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA device")
+    build_lib.build()
+    alr.lib()
+    assert alr.alr_device_supported() == alr.ALR_OK, alr.alr_last_error()
+
+
+def _i(x):
+    return torch.as_tensor(np.asarray(x), dtype=torch.int32).cuda()
+
+
+def _attend(Q, K, V, table, length, seq, per=1, **kw):
+    N, H, dim = Q.shape
+    ws = torch.empty(alr.alr_kv_attention_workspace_size(N, H, dim, "prefix_len" in kw), dtype=torch.uint8, device="cuda")
+    out, lse = torch.full_like(Q, 9.0), torch.full((N, H), 9.0, device="cuda")
+    alr.alr_kv_attention(Q, K, V, table, length, out, ws, seq=seq, lse=lse, rows_per_seq=per, **kw)
+    torch.cuda.synchronize()
+    assert alr.alr_device_status(clear=True) == alr.ALR_OK, alr.alr_last_error()
+    return out, lse
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_poison_at_the_end_of_long_sequences(dim):
+    """Half of 64 sequences of a million tokens (pages used again and again) end with a value of NaN that the
+    last row of each block alone reads: taking the other rows' 112 queries again over 400 thousand tokens of a
+    thread block ends no wait, and no other item is touched."""
+    S, per, group, page, cols, common = 64, 8, 16, 1024, 1024, 3
+    g = torch.Generator(device="cuda").manual_seed(dim)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    K, V = rand(common + S, page, 1, dim).to(BF), (1 + 0.1 * rand(common + S, page, 1, dim)).to(BF)
+    table = torch.arange(cols)[None].repeat(S, 1) % common
+    table[:, -1] = common + torch.arange(S)
+    lens = cols * page - per + 1 + torch.arange(per).repeat(S)
+    seq = torch.arange(S).repeat_interleave(per)
+    Q = rand(S * per, group, dim).to(BF)
+    args = Q, K, V, _i(table), _i(lens), _i(seq)
+    clean, clean_lse = _attend(*args, per=per)
+    V[common::2, -1] = NAN
+    out, lse = _attend(*args, per=per)
+    hit = (seq % 2 == 0).cuda()
+    last = torch.arange(S * per, device="cuda") % per == per - 1
+    assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse[~hit], clean_lse[~hit])
+    assert out[hit & last].isnan().all()
+    # fp64, each page of the sequence as often as it is in it
+    scale = dim ** -0.5
+    V[common::2, -1] = 0                       # masked below
+    times = torch.bincount(table[0, :-1], minlength=common).double().cuda()
+    k = K[:common, :, 0].double().flatten(0, 1)
+    x = scale * Q.double() @ k.T                                         # [N, group, tokens]
+    own = scale * Q.double() @ K[common:, :, 0].double()[seq.cuda()].transpose(1, 2)
+    own = own.masked_fill((torch.arange(page) >= (lens - (cols - 1) * page)[:, None]).cuda()[:, None], -INF)
+    x = torch.cat([x + times.log().repeat_interleave(page), own], -1)
+    w = torch.softmax(x, -1)
+    n = common * page
+    want = w[..., :n] @ V[:common, :, 0].double().flatten(0, 1) + w[..., n:] @ V[common:, :, 0].double()[seq.cuda()]
+    # sums over a thread block's tokens (152 share them), products of bf16 weights, values of 1 +- 0.5
+    reach = scale * (Q.double().abs().amax((0, 1)) * K.double().abs().amax((0, 1, 2))).sum().item()
+    dx = 2 * (dim + 4) * U * reach
+    rel = 2 * dx + 2.0 ** -21 + 2 * (S * cols * page / 152 + 400) * U
+    some = ~(hit & last)
+    for o, l in ((clean, clean_lse), (out, lse)):  # noqa: E741
+        assert (o[some].double() - want[some]).abs().max().item() <= (rel + 2 * 2.0 ** -8) * 1.5
+        assert (l[some].double() - torch.logsumexp(x, -1)[some]).abs().max().item() <= dx + rel + 4 * U * 32
