@@ -824,8 +824,9 @@ size_t alr_kv_attention_workspace_size(int64_t N, int32_t H, int32_t dim, int32_
  *            NULL exactly, else usually) and the same prefix_seq (usually): a matter of speed, as rows
  *            that read the same tokens together share their loads.
  *   lse [N, H] float or NULL.  A row without tokens, or whose scores are all -inf, gives zeros and
- *            -inf; a score of NaN or +inf gives NaN.  What lies in slots that a row does not read (NaN
- *            included) does not reach it.
+ *            -inf; a score of NaN or +inf gives NaN.  What lies in slots that a row does not read, and the
+ *            value of a token whose score is -inf, does not reach the row, be it NaN.  Any other value that
+ *            is not finite gives NaN or an infinity, also where its weight underflows to 0.
  * Scores, exponentials, sums and outputs are held in fp32; for a bf16 cache the weights exp(x_t - m) are
  * rounded to bf16 for their product with v.  Calls that run at the same time need workspaces of their
  * own.

@@ -761,11 +761,12 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1)
       if (to.dst != nullptr || to.dst_f != nullptr) put<E, 4>(to, d, v);
       odd = fmaf(0.f, (x.x + x.y) + (x.z + x.w), odd);
     }
-    if (n_rows > 1 && __any_sync(~0u, !(odd == 0.f))) {
+    if (__any_sync(~0u, !(odd == 0.f))) {
 #pragma unroll 1
       for (int q = 0; q < n_q; ++q) {
         const int r = q / p.gw;
-        if (q - r * p.gw >= gw) continue;
+        const float sum = ml[2 * q + 1];         // NaN: of its own scores, and so are its results
+        if (q - r * p.gw >= gw || sum != sum) continue;
         int seq, t0, t1;
         row_tokens<kBlk>(tile, r, b0, b1, seq, t0, t1);
         __syncwarp();

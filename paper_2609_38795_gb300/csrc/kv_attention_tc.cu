@@ -207,7 +207,7 @@ __device__ __noinline__ void take_odd_again(const KvPass& p, const WorkerStart& 
     const int kv = unit / p.gs, slice = (unit - kv * p.gs) * p.gw, gw = min(p.gw, group - slice);
     const bool whole = b0 == 0 && b1 == tile.nb, opens = b0 == 0 && b1 < tile.nb;
     const int part = 2 * id + (opens ? 1 : 0);
-    for (int q = warp; q < n_rows * p.gw && n_rows > 1; q += n_warps) {
+    for (int q = warp; q < n_rows * p.gw; q += n_warps) {
       const int r = q / p.gw, h = kv * group + slice + q - r * p.gw;
       if (q - r * p.gw >= gw) continue;
       const float* sums = whole ? p.put_o + ((row0 + r) * p.a.H + h) * dim
@@ -685,7 +685,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
         }
         named_bar_sync(bar, 128);
       }
-      if (n_rows > 1 && !(odd == 0.f)) mi.odd = 1;
+      if (!(odd == 0.f)) mi.odd = 1;
       tc_fence_before();
       named_bar_sync(kAllBar, kAll);
       if (opens && threadIdx.x == 0) {

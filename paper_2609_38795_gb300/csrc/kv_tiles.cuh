@@ -363,10 +363,10 @@ ALR_DEV Line find_item_starts(const KvPass& p, WorkerStart* at, long long* buf) 
 
 // ------------------------------------------------------------- a query by itself ---
 // Weights of 0 times a value that is not finite are NaN, and such a value may lie in a token that a query
-// does not see but another of its tile does.  A query whose sums came out so is taken again over its tokens
-// [t0, t1) of the item alone, by a warp, 32 tokens at a time: a score a lane, then the values of the tokens that
-// count, four at a time by 8 lanes each.  Its result replaces the one in place: the final row or the prefix's,
-// or with `parts` place `slot` there.
+// does not see but another of its tile does, or whose score is -inf.  A query whose sums came out so is taken
+// again over its tokens [t0, t1) of the item alone, by a warp, 32 tokens at a time: a score a lane, then the
+// values of the tokens that count, four at a time by 8 lanes each.  Its result replaces the one in place: the
+// final row or the prefix's, or with `parts` place `slot` there.
 //   Rare, so short of registers first: 0.12 us a token and query for 64 bf16 elements, 0.21 for 128 (16 warps an
 // SM, a million tokens a sequence; 0.83 and 1.08 by scores that a warp's lanes added up, token by token).
 // kAhead: packs of values that a lane has on their way.

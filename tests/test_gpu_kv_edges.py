@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2609_38795_gb300 import alr, build_lib
+from tests.test_gpu_kv import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -80,3 +81,36 @@ def test_poison_at_the_end_of_long_sequences(dim):
     for o, l in ((clean, clean_lse), (out, lse)):  # noqa: E741
         assert (o[some].double() - want[some]).abs().max().item() <= (rel + 2 * 2.0 ** -8) * 1.5
         assert (l[some].double() - torch.logsumexp(x, -1)[some]).abs().max().item() <= dx + rel + 4 * U * 32
+
+
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("form", [dict(heads=3, group=1, dim=16), dict(heads=2, group=4, dim=64), dict(heads=2, group=12, dim=128),
+                                  dict(heads=1, group=20, dim=64), dict(heads=1, group=20, dim=128),
+                                  dict(heads=1, group=3, dim=256), dict(heads=1, group=16, dim=256)])
+def test_values_of_tokens_masked_by_their_scores(form, dtype, bad):
+    """A token whose score is -inf does not reach a row by its value either, be rows alone or in tiles, and in
+    own tokens as in a prefix; a row of such tokens alone is empty."""
+    n, per = 700, 5
+    rows = [(s, n - per + 1 + j) for s in range(2) for j in range(per)]
+    prefix = [(2 + s, 300 - j) for s in range(2) for j in range(per)]
+    for pre in (None, prefix):
+        c = Case([n, n, 300, 300], rows, prefix=pre, dtype=dtype, page=16, seed=4, **form)
+        c.Q[..., 0] = 8.0
+        t = np.arange(n)
+        for s, these in ((0, t[::3]), (1, t), (2, t[5:300:7]), (3, t[:300])):
+            pg, pos = c.table[s, these // 16], these % 16
+            c.K[pg, pos, :, 0] = -INF
+            c.V[pg, pos] = 0.0
+        c.expected()                           # weights of 0, values of 0
+        for s, these in ((0, t[::3]), (1, t), (2, t[5:300:7]), (3, t[:300])):
+            c.V[c.table[s, these // 16], these % 16] = bad
+        for p in (1, 2, per):
+            out, lse = c.check(per=p, per_prefix=p)
+        assert (lse[per:] == -INF).all() and not out[per:].any() and lse[:per].isfinite().all()
+        # one of them with an ordinary score: its value arrives
+        pg, pos = c.table[0, 0], 0
+        c.K[pg, pos, :, 0] = 0.0
+        for p in (1, 2, per):
+            out, lse = c.run(per=p, per_prefix=p)
+            assert not out[:per].isfinite().any() and lse[:per].isfinite().all() and not out[per:].any()
