@@ -242,8 +242,12 @@ __global__ void __launch_bounds__(kAppendThreads)
     kv_append_kernel(const KvCache c, const F* k_new, const F* v_new, long long T, long long ld,
                      const int32_t* slot, int pieces, uint32_t magic) {
   constexpr int kPack = 16 / sizeof(E);
+  // A pack of the new rows is as aligned as it is long, up to 16 bytes: of bf16 for an fp32 cache 8, of fp32 for a
+  // bf16 cache 32 at 16.
+  constexpr int kSrcBytes = kPack * int(sizeof(F));
   struct alignas(16) Dst { E e[kPack]; };
-  struct alignas(16) Src { F e[kPack]; };
+  struct alignas(kSrcBytes < 16 ? kSrcBytes : 16) Src { F e[kPack]; };
+  static_assert(sizeof(Dst) == 16 && sizeof(Src) == kSrcBytes, "a pack's elements and nothing behind them");
   pdl_wait_and_release();
   const long long w = (long long)blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32;
   const long long i = pieces == 1 ? w : w / pieces;
