@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlan p, b
   }
   // rows: one each where there are threads for all (a step of single tokens), else each warp has a stretch of
   // its own, whose sequences follow one another, a lane four rows at a time, which mostly lie in one page
-  const int n_warps = n_cta * kPlanWarps, stretch = ((p.T + n_warps - 1) / n_warps + 127) / 128 * 128;
+  const int n_warps = n_cta * kPlanWarps, stretch = ((p.T - 1) / n_warps + 128) / 128 * 128;   // T up to 2^31 - 1
   const long long r0 = (long long)(rank * kPlanWarps + (tid >> 5)) * stretch;
   int s = -1;
   const auto owner = [&](int r) {            // sequence of row r < n_rows, searched from the last one on
@@ -300,7 +300,7 @@ cudaError_t launch_kv_plan(KvPlan p, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = allow_smem(kv_plan_kernel, int((4 * kKvMaxSeqs + 1) * sizeof(int)), done);
   if (e != cudaSuccess) return e;
-  const int n_cta = std::min((p.T + 4095) / 4096, 128);
+  const int n_cta = int(std::min((p.T + 4095ll) / 4096, 128ll));
   if (n_cta <= 1) return launch_pdl(kv_plan_kernel, dim3(1), dim3(kPlanThreads), smem, s, p, true, true);
   const cudaError_t f = launch_pdl(kv_plan_kernel, dim3(n_cta), dim3(kPlanThreads), smem, s, p, true, false);
   return f != cudaSuccess ? f

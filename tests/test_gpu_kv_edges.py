@@ -114,3 +114,18 @@ def test_values_of_tokens_masked_by_their_scores(form, dtype, bad):
         for p in (1, 2, per):
             out, lse = c.run(per=p, per_prefix=p)
             assert not out[:per].isfinite().any() and lse[:per].isfinite().all() and not out[per:].any()
+
+
+@pytest.mark.parametrize("T", [2 ** 31 - 1, 2 ** 31 - 31, 2 ** 31 - 32, 2 ** 31 - 4096, 2 ** 26 + 1])
+def test_plan_of_the_largest_batches(T):
+    """Batches of up to 2^31 - 1 rows: every row is written, with its slot if its sequence has a place."""
+    a, page = T - 19, 16                       # refused: past the table
+    length, table = _i([0, 1, 0]), _i([[-1] * 4, [3, -1, -1, -1], [-1] * 4])
+    slot, n = torch.full((T,), 77, dtype=torch.int32, device="cuda"), _i([0] * 3)
+    start, refused = _i([0] * 4), _i([0])
+    alr.alr_kv_plan(length, _i([a, 7, 9]), _i([5, 6]), _i([0]), table, page,
+                    dict(len=n, slot=slot, pool_used=_i([0]), start=start, n_refused=refused))
+    assert n.tolist() == [0, 8, 9] and refused.tolist() == [1] and start.tolist() == [0, a, a + 7, a + 16]
+    assert slot[a:].tolist() == [3 * page + 1 + i for i in range(7)] + [5 * page + i for i in range(9)] + [-1] * 3
+    for part in slot[:a].split(1 << 28):
+        assert bool((part == -1).all())
