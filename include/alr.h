@@ -801,7 +801,8 @@ typedef struct {
     int32_t cols;             /* pages of each                                                */
     int32_t rows_per_seq;     /* see below, >= 1                                              */
     int32_t rows_per_prefix;  /* see below, >= 1                                              */
-    float scale;              /* of q k^T (usually dim^-1/2), finite                          */
+    float scale;              /* of q k^T (usually dim^-1/2), |scale| at most 2.35e38
+                                 (scale log2(e) is a float)                                   */
 } alr_kv_attention_params;
 
 /* Workspace bytes alr_kv_attention needs (0 on invalid sizes); has_prefix: with a prefix. */

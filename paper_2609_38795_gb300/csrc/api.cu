@@ -1749,7 +1749,8 @@ int alr_kv_attention(const alr_kv_cache* cache, const alr_kv_attention_params* p
   if (p->rows_per_seq < 1 || p->rows_per_prefix < 1)
     return fail(ALR_ERR_INVALID_ARG, "rows_per_seq = %d and rows_per_prefix = %d must be at least 1",
                 p->rows_per_seq, p->rows_per_prefix);
-  if (!std::isfinite(p->scale)) return fail(ALR_ERR_INVALID_ARG, "scale must be finite");
+  if (!std::isfinite(p->scale * 1.44269504f))
+    return fail(ALR_ERR_INVALID_ARG, "scale = %g must be finite, as its product with log2(e) in fp32", p->scale);
   const int64_t pack = int64_t(16 / elem_size(cache->dtype)), row = int64_t(p->H) * c.dim;
   for (const int64_t ld : {p->ldq, p->ldo})
     if (ld < row || ld > (int64_t(1) << 40) || ld % pack != 0)

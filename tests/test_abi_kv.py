@@ -118,3 +118,13 @@ def test_binding_refuses_host_tensors():
         alr.alr_kv_plan(i, i, i, i[:1], i[:, None], 4, dict(len=i, slot=i, pool_used=i[:1]))
     with pytest.raises(TypeError, match="torch.Tensor"):
         alr.alr_kv_attention(None, K.numpy(), K, None, i, None, None)
+
+
+@pytest.mark.parametrize("scale,fits", [(2.35e38, True), (-2.35e38, True), (2.36e38, False), (-2.36e38, False), (3.4e38, False)])
+def test_attention_refuses_a_scale_without_room_for_log2e(lib, scale, fits):
+    """Scores are held times log2(e): a larger scale made every score infinite."""
+    p = alr.AlrKvAttentionParams(N=0, ldq=1024, ldo=1024, H=8, n_seq=4, cols=8, rows_per_seq=1, rows_per_prefix=1,
+                                 scale=scale)
+    rc = lib.alr_kv_attention(ctypes.byref(_cache()), ctypes.byref(p), *[A16] * 7, None, A16, 1 << 40, None)
+    assert rc == (alr.ALR_OK if fits else I)
+    assert fits or "scale" in lib.alr_last_error().decode()
