@@ -1653,7 +1653,9 @@ int cache_maps(const alr::KvCache& c, alr::KvMaps* m) {
   const int64_t page_rows = c.n_pages > 1 ? c.sp / step : 0;
   const int64_t rows = (c.n_pages - 1) * page_rows + (c.heads - 1) * head_rows + c.page;
   const int64_t cols = (c.heads - 1) * head_cols + c.dim;
-  if (rows >= INT32_MAX || step * 2 >= (int64_t(1) << 40)) return ALR_OK;
+  // A box's coordinates are 32-bit numbers, and a column past them is no fill but an illegal instruction.  Both
+  // stay well below; heads so far apart, or so many rows, take copies of 16 bytes.
+  if (rows > (1 << 30) || cols > (1 << 24) || step * 2 >= (int64_t(1) << 40)) return ALR_OK;
   const int box = c.page % 32 == 0 ? 32 : c.page % 16 == 0 ? 16 : 8;
   int rc = make_map(&m->k, c.K, ALR_BF16, cols, rows, step * 2, 64, box);
   if (rc == ALR_OK) rc = make_map(&m->v, c.V, ALR_BF16, cols, rows, step * 2, 64, box);

@@ -129,3 +129,23 @@ def test_plan_of_the_largest_batches(T):
     assert slot[a:].tolist() == [3 * page + 1 + i for i in range(7)] + [5 * page + i for i in range(9)] + [-1] * 3
     for part in slot[:a].split(1 << 28):
         assert bool((part == -1).all())
+
+
+def test_heads_far_apart():
+    """Heads 2^30 elements apart within a token's row: places of the last head's elements pass 31 bits."""
+    page, heads, dim, group, far = 8, 3, 64, 4, 1 << 30
+    g = torch.Generator(device="cuda").manual_seed(0)
+    room = torch.empty(page * heads * far, dtype=BF, device="cuda")
+    K, V = (room.as_strided((1, page, heads, dim), (page * heads * far, heads * far, far, 1), at) for at in (0, dim))
+    near = [torch.randn(1, page, heads, dim, generator=g, device="cuda").to(BF) for _ in "KV"]
+    K.copy_(near[0])
+    V.copy_(near[1])
+    Q = torch.randn(8, heads * group, dim, generator=g, device="cuda").to(BF)
+    args = _i([[0] * 20] * 1), _i(np.arange(8) + 140), _i([0] * 8)
+    for per in (8, 1):
+        want, want_lse = _attend(Q, *near, *args, per=per)
+        out, lse = _attend(Q, K, V, *args, per=per)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    row = torch.randn(1, heads, dim, generator=g, device="cuda").to(BF)
+    alr.alr_kv_append(row, -row, K, V, _i([5]))
+    assert torch.equal(K[0, 5], row[0]) and torch.equal(V[0, 5], -row[0])
