@@ -785,7 +785,8 @@ int alr_kv_plan(int32_t S, int32_t page, int32_t cols, int32_t n_pool, int32_t T
  * elements apart, heads dim apart) to slot[i], rounded to the cache's type.  A slot outside
  * [0, n_pages * page) takes nothing.  Slots of a call are distinct (of rows with the same slot any
  * one may stay, in each 16 bytes of its own).
- * K_new, V_new 16-byte aligned, ld a multiple of 16 bytes.
+ * K_new, V_new 16-byte aligned; ld and dim a multiple of 16 bytes of src_dtype (so bf16 rows want dim
+ * a multiple of 8, into an fp32 cache too).
  */
 int alr_kv_append(const alr_kv_cache* cache, const void* K_new, const void* V_new,
                   int32_t src_dtype, int64_t T, int64_t ld, const int32_t* slot, void* stream);
@@ -828,9 +829,9 @@ size_t alr_kv_attention_workspace_size(int64_t N, int32_t H, int32_t dim, int32_
  *            -inf; a score of NaN or +inf gives NaN.  What lies in slots that a row does not read, and the
  *            value of a token whose score is -inf, does not reach the row, be it NaN.  Any other value that
  *            is not finite gives NaN or an infinity, also where its weight underflows to 0.
- * Scores, exponentials, sums and outputs are held in fp32; for a bf16 cache the weights exp(x_t - m) are
- * rounded to bf16 for their product with v.  Calls that run at the same time need workspaces of their
- * own.
+ * Scores, exponentials, sums and outputs are held in fp32 (scores times log2(e), so that one beyond
+ * 2.35e38 in size may count as infinite); for a bf16 cache the weights exp(x_t - m) are rounded to bf16
+ * for their product with v.  Calls that run at the same time need workspaces of their own.
  */
 int alr_kv_attention(const alr_kv_cache* cache, const alr_kv_attention_params* p, const void* Q,
                      const int32_t* table, const int32_t* len, const int32_t* seq,

@@ -604,7 +604,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
       // ---- the item's results
       wait_on(&mi.pv_done[C::kPBufs == 2 ? (i - 1) & 1 : 0], C::kPBufs == 2 ? (i - 1) >> 1 : i - 1, ab);
       tc_fence_after();
-      named_bar_sync(kAllBar, kAll);                // both groups are past their last weights
+      named_bar_sync(kAllBar, kAll);                // all groups are past their last weights
       // sums over the warp's tokens: lane k ends with column k's
 #pragma unroll
       for (int part = 0; part < kParts; ++part) {

@@ -88,7 +88,8 @@ ALR_DEV uint64_t f2_ex2(uint64_t v) {
   f2_unpack(v, a, b);
   return f2_pack(ex2(a), ex2(b));
 }
-// Three-input maximum (one instruction); no NaN inputs occur where it is used.
+// Three-input maximum (one instruction) of the inputs that are not NaN.  The attention over the paged cache
+// relies on that: its vote takes exponents of which some may be NaN, and the weights carry the NaN on.
 ALR_DEV float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
