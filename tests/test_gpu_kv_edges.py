@@ -149,3 +149,28 @@ def test_heads_far_apart():
     row = torch.randn(1, heads, dim, generator=g, device="cuda").to(BF)
     alr.alr_kv_append(row, -row, K, V, _i([5]))
     assert torch.equal(K[0, 5], row[0]) and torch.equal(V[0, 5], -row[0])
+
+
+@pytest.mark.parametrize("form", [dict(heads=2, group=4, dim=64, page=16), dict(heads=1, group=8, dim=128, page=32),
+                                  dict(heads=1, group=3, dim=80, page=20, hnd=True), dict(heads=2, group=1, dim=128, page=8),
+                                  dict(heads=1, group=40, dim=128, page=16), dict(heads=1, group=4, dim=256, page=16),
+                                  dict(heads=1, group=4, dim=64, page=16, dtype=F32)])
+def test_prompts(form):
+    """Hundreds of rows of each sequence, packed without gaps as a step's plan has them: many tiles of a sequence,
+    tiles of several, rows of single tokens between; whatever the hint."""
+    lengths, new = [700, 1, 33, 450, 64, 5], [650, 1, 33, 301, 1, 5]
+    rows = [(s, n - k + 1 + j) for s, (n, k) in enumerate(zip(lengths, new)) for j in range(k)]
+    c = Case(lengths, rows, seed=9, **form)
+    for per in (1, 32, 650, 10 ** 6, 7):
+        out, lse = c.check(per=per)
+    # each sequence's rows begin a group of their own, the rows behind them empty
+    c.rows = np.array([(s, lengths[s] - new[s] + 1 + j if j < new[s] else 0) for s in range(6) for j in range(650)])
+    Q, at = torch.zeros(6 * 650, *c.Q.shape[1:], dtype=c.Q.dtype, device="cuda"), np.flatnonzero(c.rows[:, 1])
+    Q[at] = c.Q
+    c.Q = Q
+    padded, padded_lse = c.run(per=650, seq=False)
+    # values of up to 5, weights and output of bf16 each off by 2^-8 on either side, or fp32 sums of 700
+    assert (padded[at].float() - out.float()).abs().max() <= 5 * (4 * 2.0 ** -8 if c.Q.dtype == BF else 1e-3)
+    assert (padded_lse[at] - lse).abs().max() <= 1e-3
+    empty = np.flatnonzero(c.rows[:, 1] == 0)
+    assert not padded[empty].any() and (padded_lse[empty] == -INF).all()
