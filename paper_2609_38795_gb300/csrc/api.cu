@@ -1779,7 +1779,7 @@ int alr_kv_attention(const alr_kv_cache* cache, const alr_kv_attention_params* p
   if (status == nullptr) return fail(ALR_ERR_CUDA, "device status word unavailable");
   const alr::KvAttention a = {c, p->N, p->ldq, p->ldo, p->H, p->n_seq, p->cols, p->rows_per_seq,
                               p->rows_per_prefix, p->scale, Q, table, len, seq, prefix_len, prefix_seq,
-                              out, lse, workspace};
+                              out, lse, workspace, g_withhold_next.exchange(0)};
   alr::KvMaps maps{};
   if (alr::kv_attention_takes_maps(a, p->rows_per_seq) ||
       (prefix_len != nullptr && alr::kv_attention_takes_maps(a, p->rows_per_prefix)))

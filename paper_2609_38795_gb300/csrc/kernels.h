@@ -313,6 +313,7 @@ struct KvAttention {
   void* out;
   float* lse;                  // may be nullptr
   void* ws;
+  int withhold_first_stage;    // test hook: no worker's first stage is ever filled
 };
 // The cache as two matrices for TMA: a token's row of a head lies in matrix row
 // page * page_rows + token + head * head_rows, from column head * head_cols on.  Boxes of box_rows rows,

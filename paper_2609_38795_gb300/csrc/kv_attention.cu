@@ -592,7 +592,8 @@ __global__ void __launch_bounds__(Core::kMostWarps * 32, 1)
   char* ring = ring_smem + warp * (stages * slot_bytes + Core::kScratch);
   void* scratch = ring + stages * slot_bytes;
   if (lane == 0) {
-    for (int i = 0; i < stages; ++i) mbar_init(&landed[warp][i], 32);
+    for (int i = 0; i < stages; ++i)         // one more than ever comes: withheld
+      mbar_init(&landed[warp][i], 32 + (i == 0 && a.withhold_first_stage ? 1 : 0));
     fence_mbar_init();
   }
   if (threadIdx.x == 0) {
@@ -967,6 +968,7 @@ cudaError_t launch_kv_attention(const KvAttention& a, const KvMaps& maps, int sm
     if (e != cudaSuccess) return e;
     p.pre_o = f.put_o;
     p.pre_ml = f.put_ml;
+    p.a.withhold_first_stage = 0;
   }
   p.part = {a.seq, a.len, a.rows_per_seq};
   return run_part(p, maps, sms, status, s);

@@ -245,7 +245,8 @@ __global__ void __launch_bounds__(C::kThreads, 1)
   const AbortFlag ab{&mi.abort_word, status};
   if (threadIdx.x == 0) {
     for (int i = 0; i < kSlots; ++i) {
-      mbar_init(&mi.full[i], kCopyWarps * 33);   // every copying thread's copies, and its warp's flags
+      // every copying thread's copies, and its warp's flags; one that never comes: withheld
+      mbar_init(&mi.full[i], kCopyWarps * 33 + (i == 0 && p.a.withhold_first_stage ? 1 : 0));
       mbar_init(&mi.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -326,8 +327,15 @@ __global__ void __launch_bounds__(C::kThreads, 1)
     Place<kSlots> to;
     // box: first matrix row of the lane's box of the warp's tokens, -1: copies of 16 bytes
     const int n_boxes = maps.box_rows > 0 ? 32 / maps.box_rows : 0, n_chunks = (dim + 63) / 64;
+    bool stop = false;
     const auto copy = [&](const void* cache, const CUtensorMap* map, int kv, long long row, uint32_t all, int box) {
-      if (to.round > 0) wait_on(&mi.empty[to.slot], to.round - 1, ab);
+      // Without its place empty nothing more is copied: copies of two rounds would count for one phase of the
+      // place's barrier.
+      if (to.round > 0 && !wait_on(&mi.empty[to.slot], to.round - 1, ab)) stop = true;
+      if (__any_sync(~0u, stop)) {
+        stop = true;
+        return;
+      }
       if (box >= 0) {
         if (lane < n_boxes) {
           mbar_expect_tx(&mi.full[to.slot], n_chunks * maps.box_rows * 128);
@@ -358,7 +366,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
     uint32_t all_v = 0;
     int kv_v = 0, item = -1, box_v = -1;
 #pragma unroll 1
-    for (int i = 0; i <= count && count > 0; ++i) {
+    for (int i = 0; i <= count && count > 0 && !stop; ++i) {
       const Next cur = next;
       if (i + 1 < count) {
         const bool on = in.advance(p);
@@ -401,7 +409,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
       }
 #pragma unroll 1
       for (int h = 0; h < 2; ++h) {          // keys of tile i, values of the tile before
-        if (h == 0 ? i == count : i == 0) continue;
+        if (h == 0 ? i == count : i == 0 || stop) continue;
         copy(h == 0 ? a.c.K : a.c.V, h == 0 ? &maps.k : &maps.v, h == 0 ? kv : kv_v, h == 0 ? row : row_v,
              h == 0 ? all : all_v, h == 0 ? box : box_v);
       }
@@ -410,7 +418,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
       all_v = all;
       kv_v = kv;
     }
-    if (*ab.smem)                            // after a wait that ran out: no copy outlives the block
+    if (*ab.smem)                            // no copy outlives the block
       for (int k = 0; k < kSlots; ++k) {
         const int round = int(to.round) - (k < to.slot ? 0 : 1);
         if (round >= 0) mbar_wait_drain(&mi.full[k], round & 1);
@@ -431,12 +439,13 @@ __global__ void __launch_bounds__(C::kThreads, 1)
       const uint64_t p_desc = sdesc_sw128(smem_u32(ps), kBlk * 128, 1024);
       int item = -1;
       uint32_t prev = 0;
+      bool gone = false;                     // a place was not filled in time: none is called empty any more
       Place<kSlots> from;
       // The proxy fences here, after the waits, order the copies' and the softmax's writes to shared
       // memory before the products' reads (a fence in every writing thread cost 360 cycles a tile).
       const auto values = [&](int i, uint32_t info) {
         const int pb = C::kPBufs == 2 ? i & 1 : 0;
-        wait_on(&mi.full[from.slot], from.round, ab);
+        if (!wait_on(&mi.full[from.slot], from.round, ab)) gone = true;
         wait_on(&mi.p_full[pb], C::kPBufs == 2 ? i >> 1 : i, ab);
         fence_proxy_async_smem();
         tc_fence_after();
@@ -446,7 +455,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
 #pragma unroll 1
         for (int k = 0; k < kBlk / 16; ++k, va += 2048 >> 4, pa += 2048 >> 4, add = 1)
           mma_issue<false>(tmem + 2 * kNQ, va, pa, i_o, add);
-        mma_commit(&mi.empty[from.slot]);
+        if (!gone) mma_commit(&mi.empty[from.slot]);
         mma_commit(&mi.pv_done[pb]);
         from.next();
       };
@@ -455,7 +464,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
         uint32_t info = 0;
         if (i < count) {
           const int sb = i & 1;
-          wait_on(&mi.full[from.slot], from.round, ab);
+          if (!wait_on(&mi.full[from.slot], from.round, ab)) gone = true;
           info = mi.info[i % kInfo];
           if (info & 1) ++item;
           if (i >= 2) wait_on(&mi.s_empty[sb], (i >> 1) - 1, ab);
@@ -469,7 +478,7 @@ __global__ void __launch_bounds__(C::kThreads, 1)
             ka += (k & 3) == 3 ? (kBlk * 128 - 96) >> 4 : 32 >> 4;
             qa += (k & 3) == 3 ? (kNQ * 128 - 96) >> 4 : 32 >> 4;
           }
-          mma_commit(&mi.empty[from.slot]);
+          if (!gone) mma_commit(&mi.empty[from.slot]);
           mma_commit(&mi.s_full[sb]);
           if (info & 2) mma_commit(&mi.q_empty[item & 1]);
           from.next();

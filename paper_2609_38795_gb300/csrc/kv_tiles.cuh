@@ -454,13 +454,12 @@ ALR_DEV void row_tokens(const Tile& tile, int r, int b0, int b1, int& seq, int& 
 
 // A wait that runs out is recorded and passed over, as all waits after it: every role runs on to the end of
 // its loop (on data that no one will use), so that no barrier is left half full.
-ALR_DEV void wait_longer(uint64_t* bar, uint32_t parity, volatile int* abort_word,
-                                                int* status) {
-  if (!*abort_word) mbar_wait(bar, parity, AbortFlag{abort_word, status});
+ALR_DEV bool wait_longer(uint64_t* bar, uint32_t parity, volatile int* abort_word, int* status) {
+  return !*abort_word && mbar_wait(bar, parity, AbortFlag{abort_word, status});
 }
-// For completion n (from 0) of `bar`.
-ALR_DEV void wait_on(uint64_t* bar, uint32_t n, const AbortFlag& ab) {
-  if (!mbar_try_wait(bar, n & 1)) wait_longer(bar, n & 1, ab.smem, ab.status);
+// For completion n (from 0) of `bar`; false: passed over.
+ALR_DEV bool wait_on(uint64_t* bar, uint32_t n, const AbortFlag& ab) {
+  return mbar_try_wait(bar, n & 1) || wait_longer(bar, n & 1, ab.smem, ab.status);
 }
 
 // Units, tiles and steps of a pass whose items have at most max_q queries in max_rows rows.

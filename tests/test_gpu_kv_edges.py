@@ -2,6 +2,8 @@
 
 u = 2^-24; bounds as in test_gpu_kv.py, each derived where it is used."""
 
+import time
+
 import numpy as np
 import pytest
 import torch
@@ -174,3 +176,34 @@ def test_prompts(form):
     assert (padded_lse[at] - lse).abs().max() <= 1e-3
     empty = np.flatnonzero(c.rows[:, 1] == 0)
     assert not padded[empty].any() and (padded_lse[empty] == -INF).all()
+
+
+@pytest.mark.parametrize("lengths,per,prefix,form", [
+    ([3000, 0, 70, 1500], 1, 0, dict(heads=2, group=4, dim=128)), ([60, 1, 0, 17], 1, 0, dict(heads=2, group=4, dim=64)),
+    ([3000, 0, 70, 1500], 1, 0, dict(heads=1, group=12, dim=64)), ([3000, 0, 70, 1500], 4, 0, dict(heads=2, group=4, dim=80, dtype=F32)),
+    ([60, 1, 0, 17], 1, 0, dict(heads=1, group=1, dim=32, dtype=F32)),
+    ([40000, 0, 70, 1500], 8, 0, dict(heads=4, group=8, dim=128)), ([40000, 0, 70, 1500], 8, 0, dict(heads=4, group=8, dim=64, page=20)),
+    ([70, 300], 8, 0, dict(heads=2, group=4, dim=64)), ([9, 12, 5, 2], 1, 4, dict(heads=2, group=8, dim=128))])
+def test_withheld_stage_times_out_and_context_survives(lengths, per, prefix, form):
+    """The first stage of every warp's ring, or of a thread block's, is never filled: the waits give up after their
+    limit, the kernels run to their end, the timeout is reported, and the next call is right."""
+    rows = [(s, max(0, n - j)) for s, n in enumerate(lengths) for j in range(per)]
+    pre = [(len(lengths), 900 - 50 * j) for j in range(len(rows))] if prefix else None
+    c = Case(lengths + [900] * bool(prefix), rows, prefix=pre, **{"page": 16, **form})
+    want, want_lse = c.check(per=per, per_prefix=max(prefix, 1))
+    N, H, dim = c.Q.shape
+    ws = torch.empty(alr.alr_kv_attention_workspace_size(N, H, dim, prefix > 0), dtype=torch.uint8, device="cuda")
+    kw = dict(prefix_seq=_i([p[0] for p in pre]), prefix_len=_i([p[1] for p in pre]), rows_per_prefix=prefix) if prefix else {}
+    args = c.Q, c.K, c.V, _i(c.table), _i(c.rows[:, 1]), torch.empty_like(c.Q), ws
+    seq = _i(c.rows[:, 0])
+    torch.cuda.synchronize()
+    assert alr.alr_device_status(clear=True) == alr.ALR_OK
+    alr.alr_debug_withhold_next_stage(True)
+    t0 = time.monotonic()
+    alr.alr_kv_attention(*args, seq=seq, rows_per_seq=per, **kw)
+    rc = alr.alr_device_status(clear=True)
+    waited = time.monotonic() - t0
+    assert rc == alr.ALR_ERR_TIMEOUT, alr.alr_last_error()
+    assert 1.0 < waited < 20.0
+    out, lse = c.run(per=per, per_prefix=max(prefix, 1))
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
