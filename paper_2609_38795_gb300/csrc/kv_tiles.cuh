@@ -106,11 +106,12 @@ ALR_DEV KvRowOut part_out(const KvPass& p, float* parts, int slot, int q, float 
   return {1.f, 0.f, nullptr, base + q * p.a.c.dim, nullptr};
 }
 
-// kW consecutive elements from d on (a multiple of kW).
+// kW consecutive elements from d on (a multiple of kW).  Workspaces are aligned to 16 bytes, no more.
 template <typename E, int kW>
 ALR_DEV void put(const KvRowOut& o, int d, const float (&v)[kW]) {
-  struct alignas(kW * sizeof(float)) F { float e[kW]; };
+  struct alignas(kW < 4 ? kW * sizeof(float) : 16) F { float e[kW]; };
   struct alignas(kW * sizeof(E)) T { E e[kW]; };
+  static_assert(kW * sizeof(E) <= 16, "a store of the result");
   if (o.dst_f != nullptr) {
     F x;
 #pragma unroll

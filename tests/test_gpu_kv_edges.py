@@ -207,3 +207,24 @@ def test_withheld_stage_times_out_and_context_survives(lengths, per, prefix, for
     assert 1.0 < waited < 20.0
     out, lse = c.run(per=per, per_prefix=max(prefix, 1))
     assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("form", [dict(heads=2, group=1, dim=8), dict(heads=1, group=12, dim=72), dict(heads=1, group=20, dim=104),
+                                  dict(heads=2, group=4, dim=128), dict(heads=2, group=3, dim=36, dtype=F32)])
+def test_workspaces_aligned_to_16_bytes(form):
+    """A workspace 16 bytes past a multiple of more, for items cut between workers, prefixes and queries taken
+    again."""
+    per = 4
+    lengths = [5000, 3000, 2000]
+    rows = [(s, n - per + 1 + j) for s, n in ((0, 5000), (1, 3000)) for j in range(per)]
+    for pre in (None, [(2, 2000 - j // 2) for j in range(2 * per)]):
+        c = Case(lengths, rows, prefix=pre, page=16, **form)
+        for t, s in ((4999, 0), (1999, 2)):    # the last row of one sequence and some of the prefix read these
+            c.V[c.table[s, t // 16], t % 16] = INF
+        N, H, dim = c.Q.shape
+        ws = torch.empty(alr.alr_kv_attention_workspace_size(N, H, dim, pre is not None) + 64, dtype=torch.uint8, device="cuda")
+        assert ws.data_ptr() % 64 == 0
+        want = c.run(per=per, per_prefix=2 * per, ws=ws)
+        got = c.run(per=per, per_prefix=2 * per, ws=ws[16:])
+        assert not want[0].isfinite().all() and want[0].isfinite().any()
+        assert torch.equal(got[0].nan_to_num(7.0), want[0].nan_to_num(7.0)) and torch.equal(got[1], want[1])
