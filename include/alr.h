@@ -816,7 +816,8 @@ size_t alr_kv_attention_workspace_size(int64_t N, int32_t H, int32_t dim, int32_
  *   x_t = scale q k_t,   out[r, h] = sum_t exp(x_t - lse) v_t,   lse[r, h] = log sum_t exp(x_t).
  * One row for each sequence is a decoding step; several rows with len counting up are a block of new
  * tokens under a causal mask (tok_seq and tok_len of alr_kv_plan are its seq and len); a prefix shared
- * by many rows is stored once.
+ * by many rows is stored once (a rollout from position a of alr_ira_draw's anchor_pos reads a + 1
+ * tokens of its sample's sequence, x_0..x_a: none for the -1 of a place without an anchor).
  *   Q [N, H, dim], out [N, H, dim] of the cache's type (row strides ldq, ldo; out may not overlap Q);
  *   table [n_seq, cols] int32; len [N], prefix_len [N] int32: outside [0, cols * page] the nearest
  *            bound counts;

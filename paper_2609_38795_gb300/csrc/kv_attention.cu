@@ -197,7 +197,7 @@ struct ManyCore {
 
 // bf16, up to 8 queries, with the tokens (the elements of a value) on a product's 16 rows and the queries
 // on its 8 columns: half the products of ManyCore and half its registers, so 12 warps an SM and not 8 (256
-// sequences of 0 to 8192 tokens, 8 heads of 128, 4 queries each: 825 us by ManyCore, 682 so, 6.3 TB/s).  Registers
+// sequences of 0 to 8192 tokens, 8 heads of 128, 4 queries each: 825 us by ManyCore, 682 to 712 so, 6 TB/s).  Registers
 // are for 12 warps of 128 elements, not for 16 that the rings leave no room for: 718 us with a spill.
 // Lane (g, t) has queries 2t and 2t + 1 of tokens g and g + 8; the weights are transposed into the
 // second product's operand.
@@ -320,7 +320,7 @@ struct FewCore {
 // fp32 by fused multiply-adds (a tensor product in tf32 would lose 13 bits of the inputs).  Scores: lane
 // (h, i) = (lane / kBlk, lane % kBlk) takes its share of the packs of token i; weights go through shared memory;
 // values: a lane owns whole packs of the result, groups of lanes share the tokens where there are
-// fewer packs than lanes.  (48 sequences of up to 4001 tokens, 16 heads of 80, one query each: 200 us, 4.9
+// fewer packs than lanes.  (48 sequences of up to 4001 tokens, 16 heads of 80, one query each: 206 us, 4.8
 // TB/s; 32 blocks of 8 rows over 1000 to 3000, 32 heads of 128: 441 us, 19 TFLOP/s.)
 template <int kDim_, int kQ>
 struct F32Core {
