@@ -131,6 +131,8 @@ def test_plan_of_the_largest_batches(T):
     assert slot[a:].tolist() == [3 * page + 1 + i for i in range(7)] + [5 * page + i for i in range(9)] + [-1] * 3
     for part in slot[:a].split(1 << 28):
         assert bool((part == -1).all())
+    del slot, part
+    torch.cuda.empty_cache()
 
 
 def test_heads_far_apart():
@@ -151,6 +153,8 @@ def test_heads_far_apart():
     row = torch.randn(1, heads, dim, generator=g, device="cuda").to(BF)
     alr.alr_kv_append(row, -row, K, V, _i([5]))
     assert torch.equal(K[0, 5], row[0]) and torch.equal(V[0, 5], -row[0])
+    del room, K, V
+    torch.cuda.empty_cache()
 
 
 @pytest.mark.parametrize("form", [dict(heads=2, group=4, dim=64, page=16), dict(heads=1, group=8, dim=128, page=32),
